@@ -268,6 +268,96 @@ int sb_sab_batches(const sb_perf_table *perf, const int32_t *lengths, const doub
                    int32_t dp_size, int32_t dp_rank, int32_t num_microbatches, double *weights_out,
                    int32_t *dp_bin_out, int32_t *mb_bin_out);
 
+/* ---- rotary positions ----
+ *
+ * Turns the first rot_dim elements of every head of q and k by the token's position: pair i of a head, (x, y) = elements (i, i + rot_dim/2)
+ * in SB_ROPE_HALF or (2i, 2i + 1) in SB_ROPE_INTERLEAVED, becomes amplitude * (x cos a - y sin a, y cos a + x sin a) with
+ * a = 2 pi * position * turns[i]; elements from rot_dim on are copied.  Angles are reduced in 64 bits, so that far positions lose nothing.
+ *
+ * sb_rope is plain data that the caller keeps; sb_rope_init fills it, a caller with frequencies of its own may write `turns` (revolutions per
+ * token, pairs 0 .. rot_dim/2 - 1) and `amplitude` itself. */
+#define SB_ROPE_HALF 0
+#define SB_ROPE_INTERLEAVED 1
+#define SB_ROPE_PLAIN 0  /* f_i = base^(-2i/rot_dim) radians per token */
+#define SB_ROPE_LINEAR 1 /* f_i / factor */
+#define SB_ROPE_NTK 2    /* base * factor^(rot_dim/(rot_dim-2)) in place of base */
+#define SB_ROPE_YARN 3   /* f_i / factor for pairs that turn less than `low` times in original_length tokens, f_i for those that turn more than
+                            `high` times, between the two linear in i (bounds rounded outwards to whole pairs); amplitude 0.1 ln(factor) + 1 */
+#define SB_ROPE_BANDS 4  /* likewise, linear in the number of turns, amplitude 1 */
+#define SB_ROPE_MAX_PAIRS 64
+typedef struct sb_rope {
+  int32_t rot_dim; /* even, 2 .. head_dim */
+  int32_t layout;  /* SB_ROPE_HALF | SB_ROPE_INTERLEAVED */
+  float amplitude;
+  int32_t reserved;
+  double turns[SB_ROPE_MAX_PAIRS];
+} sb_rope;
+
+/* Host only.  rot_dim even, 2 .. 2*SB_ROPE_MAX_PAIRS (SB_ROPE_NTK: from 4 on); base > 1; factor >= 1 (read from SB_ROPE_LINEAR on);
+ * original_length > 0, low, high (read by SB_ROPE_YARN and SB_ROPE_BANDS; low, high <= 0 mean 1 and 32, or 1 and 4; low < high). */
+int sb_rope_init(sb_rope *out, int32_t rot_dim, int32_t layout, double base, int32_t scaling, double factor, double original_length,
+                 double low, double high);
+
+/* q_out, k_out (contiguous) from q, k, whose tokens lie q_pitch and k_pitch elements apart (0: contiguous, else at least H*D; a slice of a
+ * fused projection); dtype per p->dtype.  positions: dev int32 [T], or null for the token's index in its sequence.  direction SB_ROPE_FORWARD
+ * turns by the angle, SB_ROPE_BACKWARD by its negative, which makes gradients of q and k from those of q_out and k_out.  q or k may be
+ * null together with its output.  An output may be its own input (contiguous); other overlaps are not allowed.  Of `p` this reads
+ * total_tokens, num_seqs, the heads, head_dim, dtype and cu_seqlens (cu_seqlens_dev only where positions is null); no workspace. */
+#define SB_ROPE_FORWARD 0
+#define SB_ROPE_BACKWARD 1
+int sb_rope_apply(const sb_problem *p, const sb_rope *r, const int32_t *positions, const void *q, int64_t q_pitch, const void *k,
+                  int64_t k_pitch, void *q_out, void *k_out, int direction, void *stream);
+
+/* ---- attention with a sliding window and sinks ----
+ *
+ * Causal attention of the same packed batches at the granularity of tokens: row t of a sequence sees the keys u <= t with t - u < window or
+ * u < sinks (the window counts the row itself, the sinks are the first tokens of the row's sequence).  window >= 1, sinks >= 0; a window of at
+ * least the longest sequence is dense causal attention.  O, LSE and the gradients are those of sb_sparse_attn_fwd / _bwd with these keys
+ * in place of the selected ones.  Of `p` this reads total_tokens, num_seqs, the heads, head_dim, dtype, softmax_scale and cu_seqlens (both
+ * copies); block_size, select_mode and the budgets are not read and may be anything.  SB_F32 tensors are computed in float32 throughout (matrix
+ * instructions of that type), not rounded to bfloat16.  Non-finite values: a row's output depends on the elements of keys that it sees and, where a
+ * V is not finite, on those of other keys of its sequence in the same 64-token tiles; in the backward also of Q, K and dO there.
+ * Deterministic.  ws: dev, sizes from sb_window_ws_bytes (host only; either output may be null). */
+int sb_window_ws_bytes(const sb_problem *p, int32_t window, int32_t sinks, int64_t *fwd_bytes_out, int64_t *bwd_bytes_out);
+int sb_window_attn_fwd(const sb_problem *p, int32_t window, int32_t sinks, const void *q, const void *k, const void *v, void *o, float *lse,
+                       void *ws, void *stream);
+int sb_window_attn_bwd(const sb_problem *p, int32_t window, int32_t sinks, const void *q, const void *k, const void *v, const void *o,
+                       const float *lse, const void *d_o, void *dq, void *dk, void *dv, void *ws, void *stream);
+
+/* ---- a paged cache of keys and values, and attention of new tokens over it (serving) ----
+ *
+ * Tokens j*page_size .. (j+1)*page_size - 1 of sequence s live in page page_table[s][j].  An entry outside 0 .. num_pages - 1 is no page: nothing
+ * is written there and its keys are seen by no row; so are tokens from max_pages*page_size on.  Nothing of a page behind the sequence's last token is
+ * used, whatever it holds.  Pages may be shared between sequences.  All sizes that change from step to step are on the device, so that
+ * a captured graph can be replayed with other lengths within max_new and max_pages. */
+typedef struct sb_cache {
+  int32_t num_pages, page_size; /* page_size: a power of two, 16 .. 1024 */
+  int32_t num_kv_heads, head_dim, dtype; /* head_dim 64 or 128; SB_BF16 | SB_F32 */
+  int32_t max_pages;            /* entries of a row of page_table */
+  void *k, *v;                  /* dev [num_pages][num_kv_heads][page_size][head_dim] */
+  const int32_t *page_table;    /* dev [num_seqs][max_pages] */
+} sb_cache;
+typedef struct sb_chunk {       /* the new tokens of num_seqs sequences, packed: rows cu_new[s] .. cu_new[s+1] - 1 are those of sequence s */
+  int32_t num_seqs, num_q_heads;
+  int32_t total_new;            /* rows of q, k, v and the outputs.  Rows from cu_new[num_seqs] on belong to no sequence and are left as they were */
+  int32_t max_new;              /* no sequence has more new tokens; rows beyond are left as they were */
+  int32_t max_length;           /* about how long the longest sequence gets: what the work is split by, no bound */
+  float softmax_scale;          /* <= 0 means 1/sqrt(head_dim) */
+  const int32_t *cu_new;        /* dev [num_seqs+1], non-decreasing */
+  const int32_t *cached;        /* dev [num_seqs]: tokens in front of the new ones */
+} sb_chunk;
+
+/* Writes the new tokens' k (turned by their positions cached[s] + i, unless r is null) and v into their pages, and q turned likewise to q_out.
+ * k, v: dev [total_new][Hkv][D], tokens k_pitch, v_pitch elements apart (0: contiguous); q: [total_new][Hq][D] with q_pitch, or null together with q_out (contiguous). */
+int sb_cache_append(const sb_cache *c, const sb_chunk *n, const sb_rope *r, const void *q, int64_t q_pitch, const void *k, int64_t k_pitch,
+                    const void *v, int64_t v_pitch, void *q_out, void *stream);
+
+/* Attention of the new tokens over the cache, which holds them already (sb_cache_append): row i of sequence s is token t = cached[s] + i and sees
+ * the keys u <= t with t - u < window or u < sinks.  q, o: dev [total_new][Hq][D]; lse: dev [Hq][total_new] float.  A row that sees no key (its
+ * pages are missing) has O = 0 and LSE = -infinity.  From one token to whole prompts.  ws: dev, sb_cache_attn_ws_bytes (host only). */
+int sb_cache_attn_ws_bytes(const sb_cache *c, const sb_chunk *n, int32_t window, int32_t sinks, int64_t *bytes_out);
+int sb_cache_attn(const sb_cache *c, const sb_chunk *n, int32_t window, int32_t sinks, const void *q, void *o, float *lse, void *ws, void *stream);
+
 /* Instrumentation (measurement only; off by default).  `flag` is a bit set:
  *   SB_INSTR_CU_BUSY  the attention kernels add, for every workgroup, its run time in ticks of the
  *                     100 MHz constant clock to a per-compute-unit slot inside `ws`; sb_read_cu_busy
@@ -283,7 +373,8 @@ int sb_sab_batches(const sb_perf_table *perf, const int32_t *lengths, const doub
 #define SB_CU_SLOTS 512
 #define SB_INSTR_CU_BUSY 1
 #define SB_INSTR_KERNEL_EVENTS 2
-#define SB_NUM_KERNELS 10 /* pool, score, topk, plan, fwd, bwd_prep, bwd_dq, bwd_dkv, coverage, score_select; bwd_prep is the
+#define SB_NUM_KERNELS 15 /* pool, score, topk, plan, fwd, bwd_prep, bwd_dq, bwd_dkv, coverage, score_select, rope (and append), window_fwd,
+                             window_dq (and what prepares it), window_dkv, cache_attn; bwd_prep is the
                              conversion of float32 inputs in the backward call (nothing for bf16 inputs); score_select is the
                              single kernel of sb_score_select, without scores_out or in small problems */
 int sb_set_instrumentation(int flag);

@@ -22,7 +22,8 @@ SB_CU_SLOTS = 512
 
 EXPORTS = ["sb_get_layout", "sb_keep_ratio_to_topk", "sb_sel_rowptr_host", "sb_block_scores", "sb_select_topk", "sb_select_topk_static", "sb_score_select",
            "sb_plan_worklist", "sb_plan_sections", "sb_sparse_attn_fwd", "sb_sparse_attn_bwd", "sb_score_coverage", "sb_perf_predict", "sb_perf_align", "sb_dst_tune",
-           "sb_spar_update", "sb_spar_predict", "sb_balanced_partition", "sb_sab_batches",
+           "sb_rope_init", "sb_rope_apply", "sb_window_ws_bytes", "sb_window_attn_fwd", "sb_window_attn_bwd", "sb_cache_append",
+           "sb_cache_attn_ws_bytes", "sb_cache_attn", "sb_spar_update", "sb_spar_predict", "sb_balanced_partition", "sb_sab_batches",
            "sb_set_instrumentation", "sb_read_cu_busy", "sb_read_kernel_times",
            "sb_last_error", "sb_version"]
 
@@ -44,6 +45,24 @@ class sb_layout(C.Structure):
 class sb_perf_table(C.Structure):
     _fields_ = [("num_lengths", C.c_int32), ("num_budgets", C.c_int32), ("lengths", C.c_void_p), ("budgets", C.c_void_p),
                 ("latency", C.c_void_p)]
+
+
+SB_ROPE_MAX_PAIRS = 64
+
+
+class sb_rope(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("layout", C.c_int32), ("amplitude", C.c_float), ("reserved", C.c_int32),
+                ("turns", C.c_double * SB_ROPE_MAX_PAIRS)]
+
+
+class sb_cache(C.Structure):
+    _fields_ = [("num_pages", C.c_int32), ("page_size", C.c_int32), ("num_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("max_pages", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("page_table", C.c_void_p)]
+
+
+class sb_chunk(C.Structure):
+    _fields_ = [("num_seqs", C.c_int32), ("num_q_heads", C.c_int32), ("total_new", C.c_int32), ("max_new", C.c_int32), ("max_length", C.c_int32),
+                ("softmax_scale", C.c_float), ("cu_new", C.c_void_p), ("cached", C.c_void_p)]
 
 
 _lib = None
@@ -285,8 +304,192 @@ def sb_sab_batches(tab: PerfTable, lengths, k_pred, dp_size, dp_rank, num_microb
     return w[:n], dp[:n], mb[:n]
 
 
+# ------------------------------------------------------------------ rotary positions, window attention, paged cache
+SB_ROPE_HALF, SB_ROPE_INTERLEAVED = 0, 1
+SB_ROPE_PLAIN, SB_ROPE_LINEAR, SB_ROPE_NTK, SB_ROPE_YARN, SB_ROPE_BANDS = range(5)
+_TORCH_DTYPE = {SB_BF16: torch.bfloat16, SB_F32: torch.float32}
+
+
+def _tensor(name, t, shape, dtype, pitch=False):
+    """Refuses a tensor that the library could not use as it lies in memory.  pitch: tokens may be further apart than their elements."""
+    def need(ok, what):
+        if not ok:
+            raise SparseBalError(f"{name}: {what}")
+    need(isinstance(t, torch.Tensor) and t.is_cuda, "a GPU tensor is needed")
+    need(t.device.index == torch.cuda.current_device(), f"lies on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    need(t.dtype == dtype, f"{t.dtype} given, {dtype} needed")
+    need(tuple(t.shape) == tuple(shape), f"shape {tuple(t.shape)} given, {tuple(shape)} needed")
+    if not pitch:
+        need(t.is_contiguous(), "must be contiguous")
+    elif t.numel():
+        need(t[0].is_contiguous() and (t.shape[0] == 1 or t.stride(0) >= t[0].numel()), "a token's heads must be contiguous, and tokens in order")
+
+
+def _pitch(t):
+    return C.c_int64(t.stride(0) if t is not None and t.shape[0] > 1 else 0)
+
+
+def _address(t):
+    return None if t is None else C.c_void_p(t.data_ptr())
+
+
+class Rope:
+    """Holds sb_rope: how many revolutions a token each pair of elements turns.  `low`, `high`: 0 for the scaling's own values."""
+
+    def __init__(self, rot_dim, layout=SB_ROPE_HALF, base=10000.0, scaling=SB_ROPE_PLAIN, factor=1.0, original_length=0.0, low=0.0, high=0.0):
+        self.c = sb_rope()
+        _check(lib().sb_rope_init(C.byref(self.c), int(rot_dim), int(layout), C.c_double(base), int(scaling), C.c_double(factor),
+                                  C.c_double(original_length), C.c_double(low), C.c_double(high)))
+
+    def ref(self):
+        return C.byref(self.c)
+
+
+def sb_rope_apply(pb: Problem, rope: Rope, q, k, positions=None, backward=False, q_out=None, k_out=None):
+    """(q, k) turned by their positions (the tokens' indices in their sequences, or `positions`), or gradients turned back.  q and k may
+    be slices of a fused projection; either may be None.  q_out, k_out may be q and k where these are contiguous."""
+    dt = _TORCH_DTYPE[pb.dtype]
+    out = []
+    for name, x, y, heads in (("q", q, q_out, pb.Hq), ("k", k, k_out, pb.Hkv)):
+        shape = (pb.T, heads, pb.D)
+        if x is None:
+            out.append(None)
+            continue
+        _tensor(name, x, shape, dt, pitch=True)
+        if y is None:
+            y = torch.empty(shape, dtype=dt, device=x.device)
+        _tensor(name + "_out", y, shape, dt)
+        out.append(y)
+    if positions is not None:
+        _tensor("positions", positions, (pb.T,), torch.int32)
+    _check(lib().sb_rope_apply(pb.ref(), rope.ref(), _address(positions), _address(q), _pitch(q), _address(k), _pitch(k), _address(out[0]), _address(out[1]),
+                               1 if backward else 0, _stream()))
+    return out[0], out[1]
+
+
+def sb_window_ws_bytes(pb: Problem, window, sinks):
+    """(forward, backward) bytes of the workspaces of sb_window_attn_fwd and sb_window_attn_bwd."""
+    f, b = C.c_int64(), C.c_int64()
+    _check(lib().sb_window_ws_bytes(pb.ref(), int(window), int(sinks), C.byref(f), C.byref(b)))
+    return f.value, b.value
+
+
+def _window_ws(ws, need, device):
+    if ws is None:
+        return _bytes(need, device)
+    if ws.device != device or not ws.is_contiguous() or ws.numel() * ws.element_size() < need:
+        raise SparseBalError(f"ws: {need} contiguous bytes on {device} are needed")
+    return ws
+
+
+def sb_window_attn_fwd(pb: Problem, window, sinks, q, k, v, o=None, lse=None, ws=None):
+    """Attention with a sliding window and sinks; pb's budgets and blocks are not read.  Returns (o, lse)."""
+    dt = _TORCH_DTYPE[pb.dtype]
+    for name, x, heads in (("q", q, pb.Hq), ("k", k, pb.Hkv), ("v", v, pb.Hkv)):
+        _tensor(name, x, (pb.T, heads, pb.D), dt)
+    o = o if o is not None else torch.empty_like(q)
+    lse = lse if lse is not None else torch.empty((pb.Hq, pb.T), dtype=torch.float32, device=q.device)
+    _tensor("o", o, q.shape, dt)
+    _tensor("lse", lse, (pb.Hq, pb.T), torch.float32)
+    ws = _window_ws(ws, sb_window_ws_bytes(pb, window, sinks)[0], q.device)
+    _check(lib().sb_window_attn_fwd(pb.ref(), int(window), int(sinks), _address(q), _address(k), _address(v), _address(o), _address(lse), _address(ws), _stream()))
+    return o, lse
+
+
+def sb_window_attn_bwd(pb: Problem, window, sinks, q, k, v, o, lse, d_o, dq=None, dk=None, dv=None, ws=None):
+    dt = _TORCH_DTYPE[pb.dtype]
+    dq = dq if dq is not None else torch.empty_like(q)
+    dk = dk if dk is not None else torch.empty_like(k)
+    dv = dv if dv is not None else torch.empty_like(v)
+    for name, x, heads in (("q", q, pb.Hq), ("k", k, pb.Hkv), ("v", v, pb.Hkv), ("o", o, pb.Hq), ("d_o", d_o, pb.Hq), ("dq", dq, pb.Hq), ("dk", dk, pb.Hkv),
+                           ("dv", dv, pb.Hkv)):
+        _tensor(name, x, (pb.T, heads, pb.D), dt)
+    _tensor("lse", lse, (pb.Hq, pb.T), torch.float32)
+    ws = _window_ws(ws, sb_window_ws_bytes(pb, window, sinks)[1], q.device)
+    _check(lib().sb_window_attn_bwd(pb.ref(), int(window), int(sinks), _address(q), _address(k), _address(v), _address(o), _address(lse), _address(d_o),
+                                    _address(dq), _address(dk), _address(dv), _address(ws), _stream()))
+    return dq, dk, dv
+
+
+class Cache:
+    """Holds sb_cache plus the tensors it points to: k, v [pages][KV heads][tokens of a page][head_dim], page_table [sequences][most pages of one] int32."""
+
+    def __init__(self, k, v, page_table):
+        if k.dim() != 4 or k.dtype not in _TORCH_DTYPE.values():
+            raise SparseBalError("k: [pages][KV heads][tokens of a page][head_dim] in bfloat16 or float32 is needed")
+        if page_table.dim() != 2:
+            raise SparseBalError("page_table: [sequences][pages] is needed")
+        _tensor("k", k, k.shape, k.dtype)
+        _tensor("v", v, k.shape, k.dtype)
+        _tensor("page_table", page_table, page_table.shape, torch.int32)
+        self.k, self.v, self.page_table = k, v, page_table
+        self.c = sb_cache(k.shape[0], k.shape[2], k.shape[1], k.shape[3], SB_F32 if k.dtype == torch.float32 else SB_BF16, page_table.shape[1],
+                          k.data_ptr(), v.data_ptr(), page_table.data_ptr())
+
+    def ref(self):
+        return C.byref(self.c)
+
+
+class Chunk:
+    """Holds sb_chunk plus the tensors it points to: the new tokens of every sequence.  Sizes on the host are bounds (see sb_chunk); the tensors may change between calls."""
+
+    def __init__(self, cu_new, cached, Hq, total_new, max_new, max_length, softmax_scale=0.0):
+        S = cu_new.shape[0] - 1
+        _tensor("cu_new", cu_new, (max(S, 0) + 1,), torch.int32)
+        _tensor("cached", cached, (S,), torch.int32)
+        self.cu_new, self.cached, self.Hq, self.total_new = cu_new, cached, int(Hq), int(total_new)
+        self.c = sb_chunk(S, int(Hq), int(total_new), int(max_new), int(max_length), float(softmax_scale), cu_new.data_ptr(), cached.data_ptr())
+
+    def ref(self):
+        return C.byref(self.c)
+
+
+def _same_sequences(cache, chunk):
+    if cache.page_table.shape[0] != chunk.c.num_seqs:
+        raise SparseBalError(f"page_table: {cache.page_table.shape[0]} rows for {chunk.c.num_seqs} sequences")
+
+
+def sb_cache_append(cache: Cache, chunk: Chunk, k, v, rope: Rope = None, q=None, q_out=None):
+    """New tokens' k (turned) and v into their pages; returns q turned likewise (None without q)."""
+    _same_sequences(cache, chunk)
+    n, D, Hkv = chunk.total_new, cache.c.head_dim, cache.c.num_kv_heads
+    _tensor("k", k, (n, Hkv, D), cache.k.dtype, pitch=True)
+    _tensor("v", v, (n, Hkv, D), cache.k.dtype, pitch=True)
+    if q is not None:
+        _tensor("q", q, (n, chunk.Hq, D), cache.k.dtype, pitch=True)
+        if q_out is None:
+            q_out = torch.empty((n, chunk.Hq, D), dtype=q.dtype, device=q.device)
+        _tensor("q_out", q_out, (n, chunk.Hq, D), cache.k.dtype)
+    elif q_out is not None:
+        raise SparseBalError("q_out without q")
+    _check(lib().sb_cache_append(cache.ref(), chunk.ref(), rope.ref() if rope is not None else None, _address(q), _pitch(q), _address(k), _pitch(k), _address(v),
+                                 _pitch(v), _address(q_out), _stream()))
+    return q_out
+
+
+def sb_cache_attn_ws_bytes(cache: Cache, chunk: Chunk, window, sinks) -> int:
+    out = C.c_int64()
+    _check(lib().sb_cache_attn_ws_bytes(cache.ref(), chunk.ref(), int(window), int(sinks), C.byref(out)))
+    return out.value
+
+
+def sb_cache_attn(cache: Cache, chunk: Chunk, q, window=2 ** 31 - 1, sinks=0, o=None, lse=None, ws=None):
+    """Attention of the new tokens over the cache, which holds them already.  Returns (o, lse)."""
+    _same_sequences(cache, chunk)
+    shape = (chunk.total_new, chunk.Hq, cache.c.head_dim)
+    _tensor("q", q, shape, cache.k.dtype)
+    o = o if o is not None else torch.empty_like(q)
+    lse = lse if lse is not None else torch.empty((chunk.Hq, chunk.total_new), dtype=torch.float32, device=q.device)
+    _tensor("o", o, shape, cache.k.dtype)
+    _tensor("lse", lse, (chunk.Hq, chunk.total_new), torch.float32)
+    ws = _window_ws(ws, sb_cache_attn_ws_bytes(cache, chunk, window, sinks), q.device)
+    _check(lib().sb_cache_attn(cache.ref(), chunk.ref(), int(window), int(sinks), _address(q), _address(o), _address(lse), _address(ws), _stream()))
+    return o, lse
+
+
 SB_INSTR_CU_BUSY, SB_INSTR_KERNEL_EVENTS = 1, 2
-KERNEL_NAMES = ["pool", "score", "topk", "plan", "fwd", "bwd_prep", "bwd_dq", "bwd_dkv", "coverage", "score_select"]
+KERNEL_NAMES = ["pool", "score", "topk", "plan", "fwd", "bwd_prep", "bwd_dq", "bwd_dkv", "coverage", "score_select", "rope", "window_fwd", "window_dq", "window_dkv",
+                "cache_attn"]
 
 
 def sb_set_instrumentation(flag: int):

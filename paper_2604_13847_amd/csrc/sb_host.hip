@@ -130,6 +130,30 @@ int make_geo(const sb_problem* p, Geo* g) {
   return SB_OK;
 }
 
+int make_batch(const sb_problem* p, Geo* g) {
+  if (!p) { set_error("null problem"); return SB_ERR_INVALID_ARG; }
+  if (p->total_tokens < 0 || p->num_seqs < 0) { set_error("negative T or S"); return SB_ERR_INVALID_ARG; }
+  if (p->num_q_heads < 1 || p->num_kv_heads < 1 || p->num_q_heads % p->num_kv_heads != 0) {
+    set_error("num_q_heads (%d) must be a positive multiple of num_kv_heads (%d)", p->num_q_heads, p->num_kv_heads);
+    return SB_ERR_INVALID_ARG;
+  }
+  if (p->dtype != SB_BF16 && p->dtype != SB_F32) { set_error("dtype must be SB_BF16 or SB_F32"); return SB_ERR_INVALID_ARG; }
+  if (p->head_dim != 64 && p->head_dim != 128) { set_error("head_dim %d unsupported (64 or 128)", p->head_dim); return SB_ERR_UNSUPPORTED; }
+  if (p->num_seqs == 0 && p->total_tokens != 0) { set_error("T != 0 with S == 0"); return SB_ERR_INVALID_ARG; }
+  if (p->num_seqs > 0) {
+    const int32_t* cu = p->cu_seqlens_host;
+    if (!cu) { set_error("cu_seqlens_host is required"); return SB_ERR_INVALID_ARG; }
+    if (cu[0] != 0 || cu[p->num_seqs] != p->total_tokens) { set_error("cu_seqlens must start at 0 and end at T"); return SB_ERR_INVALID_ARG; }
+    for (int s = 0; s < p->num_seqs; ++s)
+      if (cu[s + 1] < cu[s]) { set_error("cu_seqlens decreases at %d", s); return SB_ERR_INVALID_ARG; }
+  }
+  *g = Geo();
+  g->T = p->total_tokens; g->S = p->num_seqs; g->Hq = p->num_q_heads; g->Hkv = p->num_kv_heads; g->G = g->Hq / g->Hkv;
+  g->D = p->head_dim; g->dtype = p->dtype;
+  g->softmax_scale = p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)g->D);
+  return SB_OK;
+}
+
 TableOffsets table_offsets(const Geo& g) {
   TableOffsets t{};
   size_t o = 0;

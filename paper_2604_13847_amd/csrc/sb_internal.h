@@ -76,6 +76,8 @@ inline __host__ __device__ int64_t tile_entries_before(int64_t it, int64_t k, in
 
 // Validates p and fills g; returns SB_OK or an error (message set).
 int make_geo(const sb_problem* p, Geo* g);
+// The same for the calls that read neither budgets nor blocks: only T, S, Hq, Hkv, G, D, dtype and softmax_scale are set.
+int make_batch(const sb_problem* p, Geo* g);
 
 inline size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
 constexpr int kMaxDevices = 64;  // per-device state (attributes set, symbol addresses) is kept for this many ordinals
@@ -300,7 +302,8 @@ int fill_words(void* dst, size_t bytes, uint32_t value, hipStream_t st);
 extern std::atomic<int> g_instrument;  // bit 0: per-CU busy ticks, bit 1: HIP events around each kernel
 
 // HIP-event bracket around one kernel launch on its own stream (only when bit 1 is set).
-enum KernelSlot { K_POOL = 0, K_SCORE, K_TOPK, K_PLAN, K_FWD, K_BWD_PREP, K_BWD_DQ, K_BWD_DKV, K_COVERAGE, K_SCORE_SELECT, K_NUM };
+enum KernelSlot { K_POOL = 0, K_SCORE, K_TOPK, K_PLAN, K_FWD, K_BWD_PREP, K_BWD_DQ, K_BWD_DKV, K_COVERAGE, K_SCORE_SELECT, K_ROPE, K_WINDOW_FWD, K_WINDOW_DQ,
+                  K_WINDOW_DKV, K_CACHE_ATTN, K_NUM };
 static_assert(K_NUM == SB_NUM_KERNELS, "kernel slots");
 struct KernelTimer {
   int slot; hipStream_t st; void* start = nullptr;
