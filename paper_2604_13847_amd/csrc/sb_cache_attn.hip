@@ -68,7 +68,7 @@ int sb_cache_attn(const sb_cache* c, const sb_chunk* n, int32_t window, int32_t 
   P.scale_log2e = P.scale * 1.4426950408889634f;
   P.cache = make_paged(c);
   KernelTimer kt(K_CACHE_ATTN, (hipStream_t)stream);
-  return launch_window_fwd(P, c->head_dim, c->dtype, true, row_tiles_most(P.T, P.S, P.G, 32), 0, (hipStream_t)stream);
+  return launch_window_fwd(P, c->head_dim, c->dtype, true, row_tiles_most(P.T, P.S, P.G, forward_rows(c->dtype)), (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -86,10 +86,114 @@ struct KeyTiles {
 };
 __device__ inline bool sees(int t, int u, int window, int sinks) { return u <= t && (t - u < window || u < sinks); }
 
+// One wavefront's part of copying a 64-key tile of K or V into LDS (layout as in sb_attn_common.h), eight wavefronts to a tile: 8 rows each, as buffer loads whose resource covers
+// the rows that exist, so that the others arrive as zeros.  A load's rows (4, or 8 at head_dim 64) lie in one page.
+template <int D>
+struct RowsLoader {
+  static constexpr int C = D / 8, RPI = 64 / C, LOADS = 8 / RPI;  // 16-byte chunks per row, rows per load, loads per wavefront
+  unsigned voff[LOADS];
+  unsigned pitch;  // bytes from row to row
+  int wave;
+  __device__ inline void init(unsigned pitch_, int wave_, int lane) {
+    pitch = pitch_;
+    wave = wave_;
+#pragma unroll
+    for (int a = 0; a < LOADS; ++a) {
+      const int r = 8 * wave + a * RPI + lane / C;
+      voff[a] = (lane / C) * pitch + 16 * ((lane % C) ^ chunk_swizzle<D>(r));
+    }
+  }
+  // `rows` of the wavefront's 8 rows exist, from `base` on (wave-uniform, by scalar instructions: see QuadLoader)
+  __device__ inline void issue(unsigned long long base, int rows, unsigned slot) const {
+#pragma unroll
+    for (int a = 0; a < LOADS; ++a) {
+      const int n = min(rows - a * RPI, RPI);
+      const i32x4 rsrc = QuadLoader<D>::resource(base + (unsigned long long)(a * RPI) * pitch, n > 0 ? (unsigned)(n - 1) * pitch + D * 2 : 0u);
+      asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds" : : "v"(voff[a]), "s"(slot + (8 * wave + a * RPI) * D * 2), "s"(rsrc) : "memory", "m0");
+    }
+  }
+};
+
+// Where the keys of a sequence and KV head lie, for wave-uniform questions.
+template <int D, bool PAGED>
+struct KeySource {
+  unsigned long long k, v;  // first row (paged: of page 0)
+  unsigned pitch;           // bytes from row to row
+  const int32_t* pages;     // the sequence's row of the page table
+  int end, lo;              // keys u with lo <= u < end or u < sinks are read
+  __device__ inline void init(const WindowParams& P, const RowTile& t, int g, int lo_, int end_) {
+    if (PAGED) {
+      const unsigned long long o = ((unsigned long long)g << P.cache.page_shift) * (D * 2);
+      k = (unsigned long long)P.cache.k + o;
+      v = (unsigned long long)P.cache.v + o;
+      pitch = D * 2;
+      pages = P.cache.table + (int64_t)t.s * P.cache.max_pages;
+    } else {
+      const unsigned long long o = ((unsigned long long)t.row0 * P.Hkv + g) * (D * 2);
+      k = (unsigned long long)P.k + o;
+      v = (unsigned long long)P.v + o;
+      pitch = (unsigned)P.Hkv * (D * 2);
+      pages = nullptr;
+    }
+    end = end_;
+    lo = lo_;
+  }
+  __device__ inline int page_of(const WindowParams& P, int u) const {  // of a key that is read, or -1
+    const int p = ((const __attribute__((address_space(4))) int32_t*)(uintptr_t)pages)[u >> P.cache.page_shift];
+    return (unsigned)p < (unsigned)P.cache.num_pages ? p : -1;
+  }
+  // rows u .. u + n - 1 (n <= 16, u a multiple of n): bytes from the first row, and how many exist from there on
+  __device__ inline unsigned long long rows_at(const WindowParams& P, int u, int n, int& rows) const {
+    rows = min(end - u, n);
+    if (u + n <= lo && u >= P.sinks) rows = 0;
+    if (!PAGED) return (unsigned long long)(unsigned)u * pitch;
+    if (rows <= 0) return 0;
+    const int p = page_of(P, u);
+    if (p < 0) { rows = 0; return 0; }
+    return (((unsigned long long)(unsigned)p * P.Hkv << P.cache.page_shift) + (unsigned)(u & (P.cache.page_size - 1))) * (D * 2);
+  }
+  // bit x: keys u0 + 16x .. + 15 have no page
+  __device__ inline unsigned missing(const WindowParams& P, int u0) const {
+    if (!PAGED) return 0;
+    unsigned m = 0;
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      if (u0 + 16 * x < end && page_of(P, u0 + 16 * x) < 0) m |= 1u << x;
+    return m;
+  }
+};
+
+// Rows of a wavefront's 32, held as C tiles (lane%32: row, value(dt, v): column 32dt + c_row(v, lane/32)), to memory through LDS (`buf`, the wavefront's own, 32 rows), whole rows
+// at a time; address(r): row r's, or null.  (store_rows in sb_attn_common.h, for rows that are no constant pitch apart.)
+template <int D, typename V, typename A>
+__device__ inline void store_tile(char* buf, int lane, V value, A address) {
+  constexpr int C = D / 8, RPI = 64 / C;
+  const int l32 = lane & 31, hf = lane >> 5;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int vg = 0; vg < 4; ++vg) {
+      const int byte = (32 * dt + 8 * vg + 4 * hf) * 2;
+      bf16x4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = (bf16)value(dt, 4 * vg + e);
+      *(bf16x4*)(buf + l32 * (D * 2) + 16 * ((byte >> 4) ^ (l32 & (C - 1))) + (byte & 15)) = y;
+    }
+  asm volatile("" ::: "memory");  // (LDS operations of a wavefront complete in order)
+#pragma unroll
+  for (int a = 0; a < 32 / RPI; ++a) {
+    const int r = a * RPI + lane / C, c = lane % C;
+    const f32x4 x = *(const f32x4*)(buf + r * (D * 2) + 16 * (c ^ (r & (C - 1))));
+    bf16* to = address(r);
+    if (to) *(f32x4*)(to + 8 * c) = x;
+  }
+}
+
 int64_t row_tiles(const int32_t* cu_host, int S, int G, int rows);  // of a packed batch
 int64_t row_tiles_most(int total, int S, int G, int rows);          // where the lengths are not known to the host
 
-// Forward launch of all query rows; P is complete.  dtype as in sb_problem.
-int launch_window_fwd(const WindowParams& P, int D, int dtype, bool paged, int64_t tiles32, int64_t tiles, hipStream_t st);
+// Forward launch of all query rows; P is complete.  dtype as in sb_problem; tiles: of forward_rows(dtype) flattened rows.
+constexpr int forward_rows(int dtype) { return dtype == SB_F32 ? 32 : 256; }
+int launch_window_fwd(const WindowParams& P, int D, int dtype, bool paged, int64_t tiles, hipStream_t st);
 
 }  // namespace sb

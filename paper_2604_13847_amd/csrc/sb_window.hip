@@ -7,6 +7,8 @@
 // per lane, and a result is the next product's operand without any cross-lane movement (c_row).
 #include <math.h>
 
+#include <type_traits>
+
 #include "sb_window.h"
 
 namespace sb {
@@ -244,6 +246,183 @@ __global__ __launch_bounds__(256) void window_dkv_f32_kernel(WindowParams P, int
 }
 
 // ---------------------------------------------------------------------------------------------
+// bfloat16 forward.  A workgroup of eight wavefronts owns 256 flattened rows of a KV head, 32 a wavefront, and walks the 64-key tiles that any of them sees; K and V tiles are
+// shared in LDS and double-buffered by asynchronous loads.  A wavefront takes a tile as two halves of 32 keys, a step of the running softmax each.  A tile that a wavefront's rows
+// all see carries no mask; one that none of them sees is only waited for.  256 registers, so two wavefronts share a SIMD: one runs its exponentials while the other runs matrix
+// instructions.
+template <int D, bool PAGED>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void window_fwd_kernel(WindowParams P) {
+  constexpr int ROWS = 256, ROW_B = D * 2, TILE_B = 64 * ROW_B, NOP = D / 16;
+  constexpr float kLazy = 8.0f;
+  __shared__ __attribute__((aligned(1024))) char tiles[2][2][TILE_B];  // [buffer][K, V]
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
+  const RowTile t = locate_tile<ROWS, PAGED>(P, blockIdx.x / P.Hkv);
+  if (t.s < 0) return;
+  const int g = (int)(blockIdx.x % P.Hkv);
+  const int64_t rows = (int64_t)t.n * P.G, mb = (int64_t)t.tile * ROWS, mw = mb + 32 * wave;
+  auto token = [&](int64_t m) { return (int)(min(m, rows - 1) / P.G); };
+  const int i = token(mw + l32), h = g * P.G + (int)(min(mw + l32, rows - 1) - (int64_t)i * P.G), pos = t.pos0 + i;
+  const int ta = t.pos0 + token(mb);
+  const int tb = PAGED ? min(t.pos0 + token(mb + ROWS - 1), P.cache.max_pages * P.cache.page_size - 1) : token(mb + ROWS - 1);
+  const int wa = t.pos0 + token(mw), wb = t.pos0 + token(mw + 31);  // this wavefront's
+  const bool working = mw < rows;
+  const KeyTiles<64> keys(ta, tb, P.window, P.sinks);
+  const int count = keys.count();
+  KeySource<D, PAGED> src;
+  src.init(P, t, g, max(0, ta - P.window + 1), tb + 1);
+  RowsLoader<D> loader;
+  loader.init(src.pitch, wave, lane);
+  const unsigned tiles0 = lds_offset(&tiles[0][0][0]);
+  auto issue = [&](int x) {
+    const int u = 64 * keys.at(x) + 8 * wave;
+    int there;
+    const unsigned long long o = src.rows_at(P, u, 8, there);
+    const unsigned slot = tiles0 + (x & 1) * 2 * TILE_B;
+    loader.issue(src.k + o, there, slot);
+    loader.issue(src.v + o, there, slot + TILE_B);
+  };
+
+  // B operand of S^T = K Q^T: column = row lane%32, slots = d 16ks + 8hf + (0..7)
+  bf16x8 qf[NOP];
+  {
+    const bf16* qp = (const bf16*)P.q + ((int64_t)(t.row0 + i) * P.Hq + h) * D + 8 * hf;
+#pragma unroll
+    for (int ks = 0; ks < NOP; ++ks) qf[ks] = *(const bf16x8*)(qp + 16 * ks);
+  }
+  // the query operands must have landed before the tile loads start: from here on only those are in flight, and waited for by hand
+#pragma unroll
+  for (int ks = 0; ks < NOP; ++ks) asm volatile("" : "+v"(qf[ks]));
+  issue(0);
+
+  unsigned row_a[NOP], tr_a[D / 32][2];
+#pragma unroll
+  for (int ks = 0; ks < NOP; ++ks) row_a[ks] = tiles0 + l32 * ROW_B + 16 * ((2 * ks + hf) ^ chunk_swizzle<D>(l32));
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int r = 8 * half + 4 * hf + ((lane & 15) >> 2), d = 32 * dt + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+      tr_a[dt][half] = tiles0 + TILE_B + r * ROW_B + 16 * ((d >> 3) ^ chunk_swizzle<D>(r)) + 2 * (d & 7);
+    }
+  auto ld_row = [&](int ks, unsigned off) __attribute__((always_inline)) {
+    return *(const bf16x8 __attribute__((address_space(3)))*)(uintptr_t)(row_a[ks] + off);
+  };
+  // A operand of O^T += V^T P^T: row = d (32dt + lane%32), slots = keys 16kk + 8(e/4) + 4hf + e%4
+  auto ld_tr = [&](int kk, int dt, unsigned off) __attribute__((always_inline)) {
+    const unsigned o = off + kk * 16 * ROW_B;
+    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4 __attribute__((address_space(3)))*)(uintptr_t)(tr_a[dt][0] + o));
+    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4 __attribute__((address_space(3)))*)(uintptr_t)(tr_a[dt][1] + o));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+
+  f32x16 oacc[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) oacc[dt] = zero16();
+  float m = -__builtin_inff(), neg_m = 0.f, l = 0.f;
+  bf16x8 op[NOP];
+
+  auto tile = [&](auto mask_c, auto buf_c, int u0, unsigned missing) __attribute__((always_inline)) {
+    constexpr bool MASK = decltype(mask_c)::value;
+    constexpr unsigned BO = decltype(buf_c)::value * 2 * TILE_B;  // the tile's buffer, as an immediate offset of every LDS read
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) {  // keys 32mt .. 32mt + 31 of the tile
+#pragma unroll
+      for (int ks = 0; ks < NOP; ++ks) op[ks] = ld_row(ks, BO + mt * 32 * ROW_B);  // K rows
+      __builtin_amdgcn_sched_barrier(0);
+      f32x16 sacc = zero16();
+#pragma unroll
+      for (int ks = 0; ks < NOP; ++ks) {  // S^T = K Q^T, refilling every operand register with a V^T operand
+        sacc = mfma32(op[ks], qf[ks], sacc);
+        op[ks] = ld_tr(2 * mt + ks / (D / 32), ks % (D / 32), BO);
+      }
+#pragma unroll
+      for (int x = 0; x < NOP; ++x) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (MASK) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int r = 32 * mt + c_row(v, hf);
+          if (!sees(pos, u0 + r, P.window, P.sinks) || (PAGED && (missing >> (r >> 4) & 1))) sacc[v] = -__builtin_inff();
+        }
+      } else {
+        // max3 is inline asm, whose reads of a matrix instruction's result the compiler's hazard recogniser does not see: 12 wait states
+        asm volatile("s_nop 7\n\ts_nop 3" : "+v"(sacc));
+      }
+      // running maximum, followed lazily: the reference moves only when a score exceeds it by 2^kLazy
+      float mx = max3(sacc[0], sacc[1], sacc[2]);
+#pragma unroll
+      for (int v = 3; v < 15; v += 2) mx = max3(mx, sacc[v], sacc[v + 1]);
+      mx = max3(mx, sacc[15], sacc[15]);
+      if (__builtin_amdgcn_ballot_w64(!((mx - m) * P.scale_log2e <= kLazy)) != 0) {
+        mx = max_across_halves(mx);
+        const bool first = m == -__builtin_inff();  // nothing accumulated yet for this row
+        const bool move = first | ((mx - m) * P.scale_log2e > kLazy);
+        const float m_new = move ? fmaxf(m, mx) : m;
+        const float m_use = m_new == -__builtin_inff() ? 0.f : m_new;  // no key seen yet: keep the exponent finite
+        const float alpha = first ? 1.0f : fast_exp2((m - m_use) * P.scale_log2e);
+        neg_m = -m_use * P.scale_log2e;
+        m = m_new;
+        if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+          l *= alpha;
+#pragma unroll
+          for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) oacc[dt][v] *= alpha;
+        }
+      }
+      // The sum is that of the probabilities before they are rounded to bf16 for the product with V: LSE keeps float32's precision
+      bf16x8 pb[2];
+      float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const float x = fast_exp2(__builtin_fmaf(sacc[v], P.scale_log2e, neg_m));
+        part[v & 3] += x;
+        pb[v >> 3][v & 7] = (bf16)x;
+      }
+      l += (part[0] + part[1]) + (part[2] + part[3]);
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) oacc[dt] = mfma32(op[kk * (D / 32) + dt], pb[kk], oacc[dt]);
+    }
+  };
+  auto visit = [&](auto buf_c, int x) __attribute__((always_inline)) {
+    const int u0 = 64 * keys.at(x);
+    const unsigned missing = src.missing(P, u0);
+    wait_vmcnt<0>();
+    __builtin_amdgcn_s_barrier();  // tile x has landed for everyone; everyone is done with tile x - 1
+    if (x + 1 < count) issue(x + 1);
+    const bool none = !working || u0 > wb || (wa - (u0 + 63) >= P.window && u0 >= P.sinks);
+    const bool all = u0 + 63 <= wa && (wb - u0 < P.window || u0 + 63 < P.sinks) && missing == 0;
+    if (none) return;
+    if (all) tile(std::false_type(), buf_c, u0, 0u);
+    else tile(std::true_type(), buf_c, u0, missing);
+  };
+  int x = 0;
+  for (; x + 2 <= count; x += 2) {  // two tiles a turn, so that a tile's buffer is known at compile time
+    visit(std::integral_constant<int, 0>(), x);
+    visit(std::integral_constant<int, 1>(), x + 1);
+  }
+  if (x < count) visit(std::integral_constant<int, 0>(), x);
+  wait_vmcnt<0>();
+
+  l += __shfl_xor(l, 32, 64);  // the two lane halves hold different keys of the same row
+  const float inv = l > 0.f ? 1.0f / l : 0.f;
+  __syncthreads();  // the tiles' LDS is free
+  store_tile<D>(&tiles[0][0][0] + wave * 32 * ROW_B, lane, [&](int dt, int v) __attribute__((always_inline)) { return oacc[dt][v] * inv; },
+                [&](int r) __attribute__((always_inline)) -> bf16* {
+                  if (mw + r >= rows) return nullptr;
+                  const int j = token(mw + r);
+                  return (bf16*)P.o + ((int64_t)(t.row0 + j) * P.Hq + g * P.G + (int)(mw + r - (int64_t)j * P.G)) * D;
+                });
+  if (hf == 0 && mw + l32 < rows)
+    P.lse[(int64_t)h * P.T + t.row0 + i] = l > 0.f ? (m * P.scale_log2e + __builtin_log2f(l)) * 0.69314718055994531f : -__builtin_inff();
+}
+
+// ---------------------------------------------------------------------------------------------
 int64_t row_tiles(const int32_t* cu, int S, int G, int rows) {
   int64_t n = 0;
   for (int s = 0; s < S; ++s) n += ((int64_t)(cu[s + 1] - cu[s]) * G + rows - 1) / rows;
@@ -262,19 +441,21 @@ static int grid_of(int64_t workgroups, dim3* grid) {
   return SB_OK;
 }
 
-int launch_window_fwd(const WindowParams& P, int D, int dtype, bool paged, int64_t tiles32, int64_t tiles, hipStream_t st) {
-  const int64_t items = tiles32 * P.Hkv;
+int launch_window_fwd(const WindowParams& P, int D, int dtype, bool paged, int64_t tiles, hipStream_t st) {
+  const int64_t items = tiles * P.Hkv;
   dim3 grid;
-  const int rc = grid_of((items + 3) / 4, &grid);
+  const int rc = grid_of(dtype == SB_F32 ? (items + 3) / 4 : items, &grid);
   if (rc != SB_OK) return rc;
-  return with_types(D, dtype, [&](auto t, auto d) {
-    using T = decltype(t);
+  auto launch = [&](auto d, auto pg) {
     constexpr int DD = decltype(d)::value;
-    if (paged) hipLaunchKernelGGL((window_fwd_f32_kernel<T, DD, true>), grid, dim3(256), 0, st, P, items);
-    else hipLaunchKernelGGL((window_fwd_f32_kernel<T, DD, false>), grid, dim3(256), 0, st, P, items);
-    SB_LAUNCH_CHECK("window_fwd_f32_kernel");
-    return SB_OK;
-  });
+    constexpr bool PAGED = decltype(pg)::value;
+    if (dtype == SB_F32) hipLaunchKernelGGL((window_fwd_f32_kernel<float, DD, PAGED>), grid, dim3(256), 0, st, P, items);
+    else hipLaunchKernelGGL((window_fwd_kernel<DD, PAGED>), grid, dim3(512), 0, st, P);
+  };
+  auto with_d = [&](auto pg) { if (D == 128) launch(std::integral_constant<int, 128>(), pg); else launch(std::integral_constant<int, 64>(), pg); };
+  if (paged) with_d(std::true_type()); else with_d(std::false_type());
+  SB_LAUNCH_CHECK("window_fwd_kernel");
+  return SB_OK;
 }
 
 static int check_window(const sb_problem* p, int32_t window, int32_t sinks, Geo* g) {
@@ -327,7 +508,7 @@ int sb_window_attn_fwd(const sb_problem* p, int32_t window, int32_t sinks, const
   WindowParams P = window_params(g, p, window, sinks);
   P.q = q; P.k = k; P.v = v; P.o = o; P.lse = lse;
   KernelTimer kt(K_WINDOW_FWD, (hipStream_t)stream);
-  return launch_window_fwd(P, g.D, g.dtype, false, row_tiles(p->cu_seqlens_host, g.S, g.G, 32), 0, (hipStream_t)stream);
+  return launch_window_fwd(P, g.D, g.dtype, false, row_tiles(p->cu_seqlens_host, g.S, g.G, forward_rows(g.dtype)), (hipStream_t)stream);
 }
 
 int sb_window_attn_bwd(const sb_problem* p, int32_t window, int32_t sinks, const void* q, const void* k, const void* v, const void* o,
