@@ -21,7 +21,7 @@ int check_cache(const sb_cache* c, const sb_chunk* n) {
     set_error("page_size %d unsupported (a power of two, 16 .. 1024)", c->page_size);
     return SB_ERR_UNSUPPORTED;
   }
-  if ((int64_t)c->max_pages * c->page_size > 0x7fffffffll) { set_error("max_pages * page_size passes 32 bits"); return SB_ERR_UNSUPPORTED; }
+  if ((int64_t)c->max_pages * c->page_size > 0x7fffffffll - 1024) { set_error("max_pages * page_size passes 32 bits"); return SB_ERR_UNSUPPORTED; }
   return SB_OK;
 }
 int check_cache_arrays(const sb_cache* c, const sb_chunk* n) {
@@ -37,7 +37,7 @@ static int check_cache_attn(const sb_cache* c, const sb_chunk* n, int32_t window
   const int rc = check_cache(c, n);
   if (rc != SB_OK) return rc;
   if (window < 1 || sinks < 0) { set_error("window (%d) must be at least 1 and sinks (%d) not negative", window, sinks); return SB_ERR_INVALID_ARG; }
-  return SB_OK;
+  return check_rows(n->total_new, n->num_q_heads / c->num_kv_heads);
 }
 
 }  // namespace sb

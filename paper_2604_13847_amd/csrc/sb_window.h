@@ -11,7 +11,10 @@ struct WindowParams {
   const void* o_in;
   void* o;
   float* lse;         // [Hq][T]
-  float* delta;       // [Hq][T] rowsum(dO * O), backward
+  float* lse2;        // [T][Hq] LSE * log2 e and
+  float* dr;          // rowsum(dO * O): backward, the order in which flattened rows need them
+  float* partials;    // dK, dV of sinks from rows far behind, see window_dkv_kernel
+  int far_rows;       // tokens of a far item
   void *dq, *dk, *dv;
   const int32_t* cu;  // [S+1]: packed rows of the sequences (paged: of their new tokens)
   int T, S, Hq, Hkv, G;
@@ -49,7 +52,7 @@ __device__ inline RowTile locate_tile(const WindowParams& P, int64_t x) {
       n = max(n - row0, 0);
       if (PAGED) n = min(n, P.max_new);
     }
-    const int64_t c = ((int64_t)n * P.G + ROWS - 1) / ROWS;
+    const int64_t c = (int64_t)(((unsigned)n * (unsigned)P.G + (unsigned)ROWS - 1) / (unsigned)ROWS);  // (rows of a sequence fit 31 bits: see check_rows)
     int64_t incl = c;
     for (int off = 1; off < 64; off <<= 1) {
       const int64_t t = __shfl_up(incl, off, 64);
@@ -83,6 +86,14 @@ struct KeyTiles {
   }
   __device__ inline int count() const { return far + end - near; }
   __device__ inline int at(int i) const { return i < far ? i : near + i - far; }
+};
+// the same question about key u0 + k + 4 hf of a tile at u0, k known at compile time: three comparisons with a constant
+struct Sight {
+  int t, w, s;
+  __device__ inline Sight(int pos, int u0, int hf, int window, int sinks) : t(pos - u0 - 4 * hf), w(t - window), s(sinks - u0 - 4 * hf) {
+    asm volatile("" : "+v"(t), "+v"(w), "+v"(s));  // (else the compiler keeps pos - k for every k in registers around the loop)
+  }
+  __device__ inline bool operator()(int k) const { return (k <= t) & ((k > w) | (k < s)); }
 };
 __device__ inline bool sees(int t, int u, int window, int sinks) { return u <= t && (t - u < window || u < sinks); }
 
@@ -189,6 +200,7 @@ __device__ inline void store_tile(char* buf, int lane, V value, A address) {
   }
 }
 
+int check_rows(int64_t tokens, int G);  // flattened rows fit 31 bits
 int64_t row_tiles(const int32_t* cu_host, int S, int G, int rows);  // of a packed batch
 int64_t row_tiles_most(int total, int S, int G, int rows);          // where the lengths are not known to the host
 

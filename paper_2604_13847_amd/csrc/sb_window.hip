@@ -141,7 +141,7 @@ __global__ __launch_bounds__(256) void window_fwd_f32_kernel(WindowParams P, int
   if (hf == 0) P.lse[(int64_t)h * P.T + t.row0 + i] = l == 0.f ? -__builtin_inff() : (top + __builtin_log2f(l)) * 0.69314718055994531f;
 }
 
-// Dr = rowsum(dO * O), one wavefront per row: 16 or 32 lanes each hold four elements.
+// Dr = rowsum(dO * O): 16 or 32 lanes to a row, four elements each.  (bfloat16: the dQ kernel does this.)
 template <typename T, int D>
 __global__ __launch_bounds__(256) void window_delta_kernel(WindowParams P, int64_t rows) {
   constexpr int LANES = D / 4, PER = 256 / LANES;
@@ -154,7 +154,10 @@ __global__ __launch_bounds__(256) void window_delta_kernel(WindowParams P, int64
   }
 #pragma unroll
   for (int off = LANES / 2; off > 0; off >>= 1) x += __shfl_xor(x, off, 64);
-  if (row < rows && c == 0) P.delta[row % P.Hq * P.T + row / P.Hq] = x;
+  if (row < rows && c == 0) {
+    P.dr[row] = x;
+    P.lse2[row] = P.lse[row % P.Hq * P.T + row / P.Hq] * 1.4426950408889634f;
+  }
 }
 
 template <typename T, int D>
@@ -172,7 +175,7 @@ __global__ __launch_bounds__(256) void window_dq_f32_kernel(WindowParams P, int6
   RowOperand<D> qr, dor, x;
   load_row<D>(qr, (const T*)P.q + at, hf);
   load_row<D>(dor, (const T*)P.d_o + at, hf);
-  const float lse2 = P.lse[(int64_t)h * P.T + t.row0 + i] * 1.4426950408889634f, dr = P.delta[(int64_t)h * P.T + t.row0 + i];
+  const float lse2 = P.lse2[at / D], dr = P.dr[at / D];
   const KeyTiles<32> tiles(ta, tb, P.window, P.sinks);
   const Keys<T, D, false> keys{P, t, g, max(0, ta - P.window + 1), tb + 1};
   f32x16 acc[D / 32];
@@ -199,7 +202,7 @@ __global__ __launch_bounds__(256) void window_dkv_f32_kernel(WindowParams P, int
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
   const int64_t item = (int64_t)blockIdx.x * 4 + wave;
   if (item >= items) return;
-  WindowParams one = P;  // tiles of 32 keys: one "row" a token
+  WindowParams one = P;  // tiles of 32 keys: one row a token
   one.G = 1;
   const RowTile t = locate_tile<32, false>(one, item / P.Hkv);
   if (t.s < 0) return;
@@ -223,8 +226,7 @@ __global__ __launch_bounds__(256) void window_dkv_f32_kernel(WindowParams P, int
     const f32x16 dp = dot_rows<D>(x, vr);
     // statistics of row m0 + lane%32, passed on to the lanes that hold the row
     const int64_t m = there ? m0 + l32 : end - 1;
-    const int64_t stat = (int64_t)(g * P.G + (int)(m % P.G)) * P.T + t.row0 + (int)(m / P.G);
-    const float lse2 = P.lse[stat] * 1.4426950408889634f, dr = P.delta[stat];
+    const float lse2 = P.lse2[row(m) / D], dr = P.dr[row(m) / D];
     const int pos = there ? (int)(m / P.G) : -1;
     float p[16], ds[16];
 #pragma unroll
@@ -259,9 +261,9 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void w
   const RowTile t = locate_tile<ROWS, PAGED>(P, blockIdx.x / P.Hkv);
   if (t.s < 0) return;
   const int g = (int)(blockIdx.x % P.Hkv);
-  const int64_t rows = (int64_t)t.n * P.G, mb = (int64_t)t.tile * ROWS, mw = mb + 32 * wave;
-  auto token = [&](int64_t m) { return (int)(min(m, rows - 1) / P.G); };
-  const int i = token(mw + l32), h = g * P.G + (int)(min(mw + l32, rows - 1) - (int64_t)i * P.G), pos = t.pos0 + i;
+  const int rows = t.n * P.G, mb = t.tile * ROWS, mw = mb + 32 * wave;
+  auto token = [&](int m) { return (int)((unsigned)min(m, rows - 1) / (unsigned)P.G); };
+  const int i = token(mw + l32), h = g * P.G + min(mw + l32, rows - 1) - i * P.G, pos = t.pos0 + i;
   const int ta = t.pos0 + token(mb);
   const int tb = PAGED ? min(t.pos0 + token(mb + ROWS - 1), P.cache.max_pages * P.cache.page_size - 1) : token(mb + ROWS - 1);
   const int wa = t.pos0 + token(mw), wb = t.pos0 + token(mw + 31);  // this wavefront's
@@ -273,7 +275,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void w
   RowsLoader<D> loader;
   loader.init(src.pitch, wave, lane);
   const unsigned tiles0 = lds_offset(&tiles[0][0][0]);
-  auto issue = [&](int x) {
+  auto issue = [&](int x) __attribute__((always_inline)) {
     const int u = 64 * keys.at(x) + 8 * wave;
     int there;
     const unsigned long long o = src.rows_at(P, u, 8, there);
@@ -321,8 +323,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void w
   float m = -__builtin_inff(), neg_m = 0.f, l = 0.f;
   bf16x8 op[NOP];
 
-  auto tile = [&](auto mask_c, auto buf_c, int u0, unsigned missing) __attribute__((always_inline)) {
-    constexpr bool MASK = decltype(mask_c)::value;
+  auto tile = [&](auto buf_c, int u0, bool all, unsigned missing) __attribute__((always_inline)) {
     constexpr unsigned BO = decltype(buf_c)::value * 2 * TILE_B;  // the tile's buffer, as an immediate offset of every LDS read
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt) {  // keys 32mt .. 32mt + 31 of the tile
@@ -341,15 +342,13 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void w
         __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
       }
       __builtin_amdgcn_sched_barrier(0);
-      if (MASK) {
+      // max3 is inline asm, whose reads of a matrix instruction's result the compiler's hazard recogniser does not see: 12 wait states
+      asm volatile("s_nop 7\n\ts_nop 3" : "+v"(sacc));
+      if (!all) {  // (one body with the mask in a branch: with a masked form of its own the accumulators were copied where the two meet)
+        const Sight sees(pos, u0 + 32 * mt, hf, P.window, P.sinks);
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int r = 32 * mt + c_row(v, hf);
-          if (!sees(pos, u0 + r, P.window, P.sinks) || (PAGED && (missing >> (r >> 4) & 1))) sacc[v] = -__builtin_inff();
-        }
-      } else {
-        // max3 is inline asm, whose reads of a matrix instruction's result the compiler's hazard recogniser does not see: 12 wait states
-        asm volatile("s_nop 7\n\ts_nop 3" : "+v"(sacc));
+        for (int v = 0; v < 16; ++v)
+          if (!sees(c_row(v, 0)) || (PAGED && (missing >> (2 * mt + (v >> 3)) & 1))) sacc[v] = -__builtin_inff();
       }
       // running maximum, followed lazily: the reference moves only when a score exceeds it by 2^kLazy
       float mx = max3(sacc[0], sacc[1], sacc[2]);
@@ -397,9 +396,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void w
     if (x + 1 < count) issue(x + 1);
     const bool none = !working || u0 > wb || (wa - (u0 + 63) >= P.window && u0 >= P.sinks);
     const bool all = u0 + 63 <= wa && (wb - u0 < P.window || u0 + 63 < P.sinks) && missing == 0;
-    if (none) return;
-    if (all) tile(std::false_type(), buf_c, u0, 0u);
-    else tile(std::true_type(), buf_c, u0, missing);
+    if (!none) tile(buf_c, u0, all, missing);
   };
   int x = 0;
   for (; x + 2 <= count; x += 2) {  // two tiles a turn, so that a tile's buffer is known at compile time
@@ -416,13 +413,447 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void w
                 [&](int r) __attribute__((always_inline)) -> bf16* {
                   if (mw + r >= rows) return nullptr;
                   const int j = token(mw + r);
-                  return (bf16*)P.o + ((int64_t)(t.row0 + j) * P.Hq + g * P.G + (int)(mw + r - (int64_t)j * P.G)) * D;
+                  return (bf16*)P.o + ((int64_t)(t.row0 + j) * P.Hq + g * P.G + mw + r - j * P.G) * D;
                 });
   if (hf == 0 && mw + l32 < rows)
     P.lse[(int64_t)h * P.T + t.row0 + i] = l > 0.f ? (m * P.scale_log2e + __builtin_log2f(l)) * 0.69314718055994531f : -__builtin_inff();
 }
 
 // ---------------------------------------------------------------------------------------------
+// bfloat16 dQ.  Rows, tiles and their walk as in the forward kernel; a half tile is S, dP and dQ += dS K, whose operands go through one set of registers.  Every row belongs to one
+// workgroup here, so this is also where Dr is computed, from the dO in registers and one read of O, and left with LSE log2 e for the next kernel.
+template <int D>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void window_dq_kernel(WindowParams P) {
+  constexpr int ROWS = 256, ROW_B = D * 2, TILE_B = 64 * ROW_B, NOP = D / 16;
+  __shared__ __attribute__((aligned(1024))) char tiles[2][2][TILE_B];  // [buffer][K, V]
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
+  const RowTile t = locate_tile<ROWS, false>(P, blockIdx.x / P.Hkv);
+  if (t.s < 0) return;
+  const int g = (int)(blockIdx.x % P.Hkv);
+  const int rows = t.n * P.G, mb = t.tile * ROWS, mw = mb + 32 * wave;
+  auto token = [&](int m) { return (int)((unsigned)min(m, rows - 1) / (unsigned)P.G); };
+  const int i = token(mw + l32), h = g * P.G + min(mw + l32, rows - 1) - i * P.G;
+  const int ta = token(mb), tb = token(mb + ROWS - 1), wa = token(mw), wb = token(mw + 31);
+  const bool working = mw < rows;
+  const KeyTiles<64> keys(ta, tb, P.window, P.sinks);
+  const int count = keys.count();
+  KeySource<D, false> src;
+  src.init(P, t, g, max(0, ta - P.window + 1), tb + 1);
+  RowsLoader<D> loader;
+  loader.init(src.pitch, wave, lane);
+  const unsigned tiles0 = lds_offset(&tiles[0][0][0]);
+  auto issue = [&](int x) __attribute__((always_inline)) {
+    int there;
+    const unsigned long long o = src.rows_at(P, 64 * keys.at(x) + 8 * wave, 8, there);
+    const unsigned slot = tiles0 + (x & 1) * 2 * TILE_B;
+    loader.issue(src.k + o, there, slot);
+    loader.issue(src.v + o, there, slot + TILE_B);
+  };
+  // B operands of S^T = K Q^T and dP^T = V dO^T: column = row lane%32, slots = d 16ks + 8hf + (0..7)
+  bf16x8 qf[NOP], dof[NOP];
+  const int64_t row = (int64_t)(t.row0 + i) * P.Hq + h;
+  float lse2, dr = 0.f;
+  {
+    const bf16* const qp = (const bf16*)P.q + row * D + 8 * hf;
+    const bf16* const dp = (const bf16*)P.d_o + row * D + 8 * hf;
+    const bf16* const op = (const bf16*)P.o_in + row * D + 8 * hf;
+    bf16x8 of[NOP];
+#pragma unroll
+    for (int ks = 0; ks < NOP; ++ks) { dof[ks] = *(const bf16x8*)(dp + 16 * ks); of[ks] = *(const bf16x8*)(op + 16 * ks); qf[ks] = *(const bf16x8*)(qp + 16 * ks); }
+    lse2 = P.lse[(int64_t)h * P.T + t.row0 + i] * 1.4426950408889634f;
+#pragma unroll
+    for (int ks = 0; ks < NOP; ++ks)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dr = __builtin_fmaf((float)dof[ks][e], (float)of[ks][e], dr);
+    dr += __shfl_xor(dr, 32, 64);
+    if (hf == 0 && mw + l32 < rows) {
+      P.lse2[row] = lse2;
+      P.dr[row] = dr;
+    }
+  }
+#pragma unroll
+  for (int ks = 0; ks < NOP; ++ks) asm volatile("" : "+v"(qf[ks]), "+v"(dof[ks]));
+  asm volatile("" : "+v"(lse2), "+v"(dr));
+  wait_vmcnt<0>();  // (the stores too: from here on only tile loads are in flight)
+  issue(0);
+
+  unsigned row_a[NOP], tr_a[D / 32][2];
+#pragma unroll
+  for (int ks = 0; ks < NOP; ++ks) row_a[ks] = tiles0 + l32 * ROW_B + 16 * ((2 * ks + hf) ^ chunk_swizzle<D>(l32));
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int r = 8 * half + 4 * hf + ((lane & 15) >> 2), d = 32 * dt + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+      tr_a[dt][half] = tiles0 + r * ROW_B + 16 * ((d >> 3) ^ chunk_swizzle<D>(r)) + 2 * (d & 7);
+    }
+  auto ld_row = [&](int ks, unsigned off) __attribute__((always_inline)) {
+    return *(const bf16x8 __attribute__((address_space(3)))*)(uintptr_t)(row_a[ks] + off);
+  };
+  auto ld_tr = [&](int kk, int dt, unsigned off) __attribute__((always_inline)) {
+    const unsigned o = off + kk * 16 * ROW_B;
+    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4 __attribute__((address_space(3)))*)(uintptr_t)(tr_a[dt][0] + o));
+    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4 __attribute__((address_space(3)))*)(uintptr_t)(tr_a[dt][1] + o));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zero16();
+  bf16x8 op[NOP];
+  auto tile = [&](auto buf_c, int u0, bool all) __attribute__((always_inline)) {
+    constexpr unsigned BO = decltype(buf_c)::value * 2 * TILE_B;
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) {
+#pragma unroll
+      for (int ks = 0; ks < NOP; ++ks) op[ks] = ld_row(ks, BO + mt * 32 * ROW_B);  // K rows
+      __builtin_amdgcn_sched_barrier(0);
+      f32x16 sacc = zero16(), dp = zero16();
+#pragma unroll
+      for (int ks = 0; ks < NOP; ++ks) {
+        sacc = mfma32(op[ks], qf[ks], sacc);
+        op[ks] = ld_row(ks, BO + TILE_B + mt * 32 * ROW_B);  // V rows
+      }
+#pragma unroll
+      for (int x = 0; x < NOP; ++x) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int ks = 0; ks < NOP; ++ks) {
+        dp = mfma32(op[ks], dof[ks], dp);
+        op[ks] = ld_tr(2 * mt + ks / (D / 32), ks % (D / 32), BO);  // K^T
+      }
+      float p[16];
+#pragma unroll
+      for (int v = 0; v < 16; ++v) p[v] = fast_exp2(__builtin_fmaf(sacc[v], P.scale_log2e, -lse2));
+      if (!all) {
+        const Sight sees(i, u0 + 32 * mt, hf, P.window, P.sinks);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          if (!sees(c_row(v, 0))) { p[v] = 0.f; dp[v] = 0.f; }
+        }
+      }
+      bf16x8 ds[2];
+#pragma unroll
+      for (int v = 0; v < 16; ++v) ds[v >> 3][v & 7] = (bf16)(p[v] * (dp[v] - dr));
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) acc[dt] = mfma32(op[kk * (D / 32) + dt], ds[kk], acc[dt]);
+    }
+  };
+  auto visit = [&](auto buf_c, int x) __attribute__((always_inline)) {
+    const int u0 = 64 * keys.at(x);
+    wait_vmcnt<0>();
+    __builtin_amdgcn_s_barrier();  // tile x has landed for everyone; everyone is done with tile x - 1
+    if (x + 1 < count) issue(x + 1);
+    const bool none = !working || u0 > wb || (wa - (u0 + 63) >= P.window && u0 >= P.sinks);
+    if (!none) tile(buf_c, u0, u0 + 63 <= wa && (wb - u0 < P.window || u0 + 63 < P.sinks));
+  };
+  int x = 0;
+  for (; x + 2 <= count; x += 2) {
+    visit(std::integral_constant<int, 0>(), x);
+    visit(std::integral_constant<int, 1>(), x + 1);
+  }
+  if (x < count) visit(std::integral_constant<int, 0>(), x);
+  wait_vmcnt<0>();
+  __syncthreads();  // the tiles' LDS is free
+  store_tile<D>(&tiles[0][0][0] + wave * 32 * ROW_B, lane, [&](int dt, int v) __attribute__((always_inline)) { return acc[dt][v] * P.scale; },
+                [&](int r) __attribute__((always_inline)) -> bf16* {
+                  if (mw + r >= rows) return nullptr;
+                  const int j = token(mw + r);
+                  return (bf16*)P.dq + ((int64_t)(t.row0 + j) * P.Hq + g * P.G + mw + r - j * P.G) * D;
+                });
+}
+
+// ---------------------------------------------------------------------------------------------
+// bfloat16 dK and dV.  A workgroup owns PAIRS * 32 keys of a KV head and walks the flattened rows that see any of them, 32 a stage.  32 keys are the work of two wavefronts on one
+// SIMD: the first computes S and P and adds P^T dO to dV, the second, a stage behind, dP and dS = P (dP - Dr) and adds dS^T Q to dK; P goes from one to the other through LDS
+// in float32, lane by lane (both hold keys in columns).  Each so needs 150 registers where one wavefront for both would need more than the 256 that let two share a SIMD,
+// and has as many matrix instructions as the other.  The stages' Q and dO rows, LSE and Dr come by asynchronous loads into three slots.
+//
+// Sinks are seen by all rows of their sequence.  The rows behind a sink tile's ordinary ones (far rows) are the work of other workgroups (FAR), far_rows tokens each, that leave their
+// sums in float32; the tile's own workgroup, launched after them, adds them in order.  So the result does not depend on who is ahead, and no workgroup has more than its share.
+constexpr int kDkvKeys = 128;   // keys of a workgroup without FAR
+constexpr int kFarKeys = 32;    // with
+constexpr int kFarSinks = 512;  // with more sinks than this there are sink tiles enough to fill the chip: their own workgroups take all rows
+// Far items of a sequence of n tokens: far_blocks blocks of sinks, far_segments each (some may be empty: the first rows of a block's last ones).
+__host__ __device__ inline int far_blocks(int n, int sinks) { return ((sinks < n ? sinks : n) + kFarKeys - 1) / kFarKeys; }
+__host__ __device__ inline int far_segments(int n, int window, int far_rows) { return n > window ? (n - window + far_rows - 1) / far_rows : 0; }
+__host__ __device__ inline int64_t far_items(int n, int window, int sinks, int far_rows) {
+  return sinks > kFarSinks ? 0 : (int64_t)far_blocks(n, sinks) * far_segments(n, window, far_rows);
+}
+// the first token that none but sinks of the 128 keys around u show themselves to
+__host__ __device__ inline int near_end(int u, int n, int window) {
+  const int last = (u | (kDkvKeys - 1)) < n ? (u | (kDkvKeys - 1)) : n - 1;
+  return n - last > window ? last + window : n;
+}
+
+template <int D, int PAIRS, bool FAR>
+__global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))) void window_dkv_kernel(WindowParams P) {
+  constexpr int ROW_B = D * 2, TILE_B = 32 * ROW_B, NOP = D / 16, KEYS = 32 * PAIRS, NW = 2 * PAIRS;
+  constexpr int kSlots = 3, STAT_B = 256, STAGE_B = 2 * TILE_B;
+  constexpr int kNr = 16 * (D / 32);  // accumulator registers
+  __shared__ __attribute__((aligned(1024))) char stage[kSlots][STAGE_B];  // Q, dO
+  __shared__ __attribute__((aligned(1024))) float pbuf[kSlots][PAIRS][16 * 64];
+  __shared__ __attribute__((aligned(256))) float stat[kSlots][64];        // LSE log2 e of 32 rows, Dr
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
+  const int pair = wave % PAIRS;
+  const bool second = wave >= PAIRS;  // wavefronts w and w + 4 share a SIMD
+  const int g = (int)(blockIdx.x % P.Hkv);
+  // which sequence, and what of it
+  int s = -1, seq0 = 0, n = 0;
+  int64_t x = blockIdx.x / P.Hkv, far0 = 0;  // far0: far items of the earlier sequences
+  for (int base = 0; base < P.S && s < 0; base += 64) {
+    int first = 0, len = 0;
+    if (base + lane < P.S) { first = P.cu[base + lane]; len = P.cu[base + lane + 1] - first; }
+    const int64_t c_far = far_items(len, P.window, P.sinks, P.far_rows);
+    const int64_t c = FAR ? c_far : (int64_t)((len + KEYS - 1) / KEYS);
+    int64_t incl = c, incl_far = c_far;
+    for (int off = 1; off < 64; off <<= 1) {
+      const int64_t a = __shfl_up(incl, off, 64), b = __shfl_up(incl_far, off, 64);
+      if (lane >= off) { incl += a; incl_far += b; }
+    }
+    const unsigned long long hit = __builtin_amdgcn_ballot_w64(x < incl);
+    const int src = hit ? __builtin_ctzll(hit) : 63;
+    if (hit) {
+      s = base + src;
+      seq0 = __builtin_amdgcn_readlane(first, src);
+      n = __builtin_amdgcn_readlane(len, src);
+      x -= __shfl(incl - c, src, 64);
+      far0 += __shfl(incl_far - c_far, src, 64);
+    } else {
+      x -= __shfl(incl, 63, 64);
+      far0 += __shfl(incl_far, 63, 64);
+    }
+  }
+  if (s < 0) return;
+  const int segments = far_segments(n, P.window, P.far_rows);
+  const int item = __builtin_amdgcn_readfirstlane((int)x);
+  int u0, r0, r1;  // first key; rows: tokens r0 .. r1 - 1
+  if (FAR) {
+    u0 = item / segments * KEYS;
+    const int64_t from = (int64_t)near_end(u0, n, P.window) + (int64_t)(item % segments) * P.far_rows;
+    if (from >= n) return;
+    r0 = (int)from;
+    r1 = (int)min(from + P.far_rows, (int64_t)n);
+  } else {
+    u0 = item * KEYS;
+    r0 = u0;
+    r1 = P.sinks > kFarSinks && u0 < P.sinks ? n : near_end(u0, n, P.window);
+  }
+  const int ku = u0 + 32 * pair, kl = min(ku + 31, n - 1);  // this pair's keys (none: ku >= n)
+  const int key = min(ku + l32, n - 1);
+  const int m0 = r0 * P.G, m1 = r1 * P.G, stages = (m1 - m0 + 31) / 32;
+
+  // loads: 32 rows of Q and of dO a stage, RPI rows an instruction; the wavefronts share them, and the first one takes the rows' statistics
+  constexpr int C = D / 8, RPI = 64 / C, LOADS = 2 * (32 / RPI), LPW = (LOADS + NW - 1) / NW;
+  const unsigned G = (unsigned)P.G;
+  const float inv_g = 1.0f / (float)P.G;
+  int lm[LPW], lt[LPW], lh[LPW];  // flattened row, its token and head, of this lane's loads
+  const int step_t = 32 / (int)G, step_h = 32 % (int)G;
+#pragma unroll
+  for (int a = 0; a < LPW; ++a) {
+    const int r = (wave * LPW + a) % (32 / RPI) * RPI + lane / C;
+    lm[a] = m0 + r;
+    lt[a] = (int)((unsigned)lm[a] / G);
+    lh[a] = lm[a] - lt[a] * (int)G;
+  }
+  int sm = m0 + l32, st = (int)((unsigned)sm / G), sh = sm - st * (int)G;
+  const unsigned stage0 = lds_offset(&stage[0][0]), stat0 = lds_offset(&stat[0][0]);
+  auto issue = [&](int slot) __attribute__((always_inline)) {  // the next stage; rows past the last one repeat it, and are masked
+#pragma unroll
+    for (int a = 0; a < LPW; ++a) {
+      const int id = wave * LPW + a;
+      if (id < LOADS) {
+        const int r = id % (32 / RPI) * RPI + lane / C;
+        const bool there = lm[a] < m1;
+        const int64_t row = (int64_t)(seq0 + (there ? lt[a] : r1 - 1)) * P.Hq + g * P.G + (there ? lh[a] : P.G - 1);
+        const bf16* from = (const bf16*)(id < 32 / RPI ? P.q : P.d_o) + row * D + 8 * ((lane % C) ^ chunk_swizzle<D>(r));
+        dma16(from, stage0 + slot * STAGE_B + (id < 32 / RPI ? 0 : TILE_B) + id % (32 / RPI) * 1024);
+      }
+      lm[a] += 32;
+      lt[a] += step_t;
+      lh[a] += step_h;
+      if (lh[a] >= P.G) { lh[a] -= P.G; ++lt[a]; }
+    }
+    if (wave == 0) {
+      const bool there = sm < m1;
+      const int64_t row = (int64_t)(seq0 + (there ? st : r1 - 1)) * P.Hq + g * P.G + (there ? sh : P.G - 1);
+      const float* from = (hf ? P.dr : P.lse2) + row;
+      asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(from), "s"(stat0 + slot * STAT_B) : "memory", "m0");
+      sm += 32;
+      st += step_t;
+      sh += step_h;
+      if (sh >= P.G) { sh -= P.G; ++st; }
+    }
+  };
+
+  // B operand: K or V rows; column = key lane%32, slots = d 16ks + 8hf + (0..7)
+  bf16x8 kv[NOP];
+  {
+    const bf16* kp = (const bf16*)(second ? P.v : P.k) + ((int64_t)(seq0 + key) * P.Hkv + g) * D + 8 * hf;
+#pragma unroll
+    for (int ks = 0; ks < NOP; ++ks) kv[ks] = *(const bf16x8*)(kp + 16 * ks);
+  }
+#pragma unroll
+  for (int ks = 0; ks < NOP; ++ks) asm volatile("" : "+v"(kv[ks]));
+  issue(0);
+
+  // rows of Q (dO for the second wavefront), transposed reads of the other
+  unsigned row_a[NOP], tr_a[D / 32][2];
+#pragma unroll
+  for (int ks = 0; ks < NOP; ++ks) row_a[ks] = stage0 + (second ? TILE_B : 0) + l32 * ROW_B + 16 * ((2 * ks + hf) ^ chunk_swizzle<D>(l32));
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int r = 8 * half + 4 * hf + ((lane & 15) >> 2), d = 32 * dt + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+      tr_a[dt][half] = stage0 + (second ? 0 : TILE_B) + r * ROW_B + 16 * ((d >> 3) ^ chunk_swizzle<D>(r)) + 2 * (d & 7);
+    }
+  auto ld_row = [&](int ks, unsigned off) __attribute__((always_inline)) {
+    return *(const bf16x8 __attribute__((address_space(3)))*)(uintptr_t)(row_a[ks] + off);
+  };
+  auto ld_tr = [&](int kk, int dt, unsigned off) __attribute__((always_inline)) {
+    const unsigned o = off + kk * 16 * ROW_B;
+    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4 __attribute__((address_space(3)))*)(uintptr_t)(tr_a[dt][0] + o));
+    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4 __attribute__((address_space(3)))*)(uintptr_t)(tr_a[dt][1] + o));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zero16();
+
+  // Does the pair see anything of stage x?  Both its wavefronts ask.
+  auto nothing = [&](int x) __attribute__((always_inline)) {
+    const int a = (int)((unsigned)(m0 + 32 * x) / G), b = (int)((unsigned)min(m0 + 32 * x + 31, m1 - 1) / G);  // its tokens
+    return ku >= n || b < ku || (a - kl >= P.window && ku >= P.sinks);
+  };
+  bf16x8 op[NOP];
+  auto products = [&](f32x16& c, unsigned off) __attribute__((always_inline)) {  // c = rows x kv, the operand registers refilled with transposed ones
+#pragma unroll
+    for (int ks = 0; ks < NOP; ++ks) op[ks] = ld_row(ks, off);
+    __builtin_amdgcn_sched_barrier(0);
+    c = zero16();
+#pragma unroll
+    for (int ks = 0; ks < NOP; ++ks) {
+      c = mfma32(op[ks], kv[ks], c);
+      op[ks] = ld_tr(ks / (D / 32), ks % (D / 32), off);
+    }
+#pragma unroll
+    for (int x = 0; x < NOP; ++x) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto add = [&](const bf16x8 (&w)[2]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) acc[dt] = mfma32(op[kk * (D / 32) + dt], w[kk], acc[dt]);
+  };
+  // before stage x of the loop: what it reads is there, and what the next loads replace is no longer read
+  auto turn = [&](int x, int next) __attribute__((always_inline)) {
+    wait_vmcnt<0>();
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the probabilities are written
+    __builtin_amdgcn_s_barrier();        // stage x has landed; the first wavefronts are done with x - 1, the second with x - 2
+    if (x + 1 < stages) issue(next);
+  };
+  // (a loop each, with the slot as a number: forms for every slot made the compiler copy the accumulators where they meet)
+  if (!second) {
+    int slot = 0;
+    for (int x = 0; x <= stages; ++x) {
+      const int next = slot == kSlots - 1 ? 0 : slot + 1;
+      turn(x, next);
+      if (x < stages && !nothing(x)) {
+        f32x16 sc;
+        products(sc, slot * STAGE_B);
+        f32x4 e[4];
+#pragma unroll
+        for (int vg = 0; vg < 4; ++vg) e[vg] = *(const f32x4*)&stat[slot][8 * vg + 4 * hf];
+        float p[16];
+#pragma unroll
+        for (int v = 0; v < 16; ++v) p[v] = fast_exp2(__builtin_fmaf(sc[v], P.scale_log2e, -e[v >> 2][v & 3]));
+        const int first = m0 + 32 * x, a = (int)((unsigned)first / G), b = (int)((unsigned)min(first + 31, m1 - 1) / G);
+        const bool all = a >= kl && (b - ku < P.window || kl < P.sinks) && first + 32 <= m1;
+        if (!all) {
+          const int rest = first - a * (int)G;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const int r = c_row(v, hf), tok = a + (int)(((float)(rest + r) + 0.5f) * inv_g);  // (exact: 1 / 2 is further from a multiple of G than the product is off)
+            if (first + r >= m1 || !sees(tok, key, P.window, P.sinks)) p[v] = 0.f;
+          }
+        }
+        bf16x8 w[2];
+#pragma unroll
+        for (int v = 0; v < 16; ++v) w[v >> 3][v & 7] = (bf16)p[v];
+#pragma unroll
+        for (int vg = 0; vg < 4; ++vg) *(f32x4*)&pbuf[slot][pair][(vg * 64 + lane) * 4] = f32x4{p[4 * vg], p[4 * vg + 1], p[4 * vg + 2], p[4 * vg + 3]};
+        add(w);
+      }
+      slot = next;
+    }
+  } else {
+    int slot = 0, before = kSlots - 1;
+    for (int x = 0; x <= stages; ++x) {
+      const int next = slot == kSlots - 1 ? 0 : slot + 1;
+      turn(x, next);
+      if (x > 0 && !nothing(x - 1)) {
+        f32x16 dp;
+        products(dp, before * STAGE_B);
+        bf16x8 w[2];
+#pragma unroll
+        for (int vg = 0; vg < 4; ++vg) {
+          const f32x4 dr = *(const f32x4*)&stat[before][32 + 8 * vg + 4 * hf], p = *(const f32x4*)&pbuf[before][pair][(vg * 64 + lane) * 4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[vg >> 1][4 * (vg & 1) + e] = (bf16)(p[e] * (dp[4 * vg + e] - dr[e]));
+        }
+        add(w);
+      }
+      before = slot;
+      slot = next;
+    }
+  }
+  wait_vmcnt<0>();
+
+  // a far item's sums: [item][KV head][dV, dK][register][lane]
+  auto slot_of = [&](int64_t it) { return P.partials + ((it * P.Hkv + g) * 2 + (second ? 1 : 0)) * (kNr * 64) + lane; };
+  if (FAR) {
+    float* to = slot_of(far0 + item);
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) to[(16 * dt + v) * 64] = acc[dt][v];
+    return;
+  }
+  if (ku < min(P.sinks, n) && P.sinks <= kFarSinks) {
+    const int end = near_end(u0, n, P.window), have = (n - end + P.far_rows - 1) / P.far_rows;
+    const int64_t it = far0 + (int64_t)(ku / kFarKeys) * segments;
+    for (int z = 0; z < have; ++z) {
+      const float* from = slot_of(it + z);
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[dt][v] += from[(16 * dt + v) * 64];
+    }
+  }
+  __syncthreads();  // the stages' LDS is free
+  static_assert(NW * 32 * ROW_B <= (int)sizeof(stage) + (int)sizeof(pbuf) || FAR, "every wavefront's rows");
+  char* const buf = wave * 32 * ROW_B + 32 * ROW_B <= (int)sizeof(stage) ? &stage[0][0] + wave * 32 * ROW_B : (char*)&pbuf[0][0][0] + (wave * 32 * ROW_B - (int)sizeof(stage) / (32 * ROW_B) * 32 * ROW_B);
+  const float f = second ? P.scale : 1.0f;
+  store_tile<D>(buf, lane, [&](int dt, int v) __attribute__((always_inline)) { return acc[dt][v] * f; },
+                [&](int r) __attribute__((always_inline)) -> bf16* {
+                  return ku + r < n ? (bf16*)(second ? P.dk : P.dv) + ((int64_t)(seq0 + ku + r) * P.Hkv + g) * D : nullptr;
+                });
+}
+
+// ---------------------------------------------------------------------------------------------
+int check_rows(int64_t tokens, int G) {
+  if (tokens * G > 0x7fffffffll - 512) { set_error("%lld tokens of %d query heads per KV head pass 32 bits", (long long)tokens, G); return SB_ERR_UNSUPPORTED; }
+  return SB_OK;
+}
 int64_t row_tiles(const int32_t* cu, int S, int G, int rows) {
   int64_t n = 0;
   for (int s = 0; s < S; ++s) n += ((int64_t)(cu[s + 1] - cu[s]) * G + rows - 1) / rows;
@@ -430,11 +861,6 @@ int64_t row_tiles(const int32_t* cu, int S, int G, int rows) {
 }
 int64_t row_tiles_most(int total, int S, int G, int rows) { return ((int64_t)total * G) / rows + S; }
 
-template <typename F>
-static int with_types(int D, int dtype, F f) {
-  if (dtype == SB_F32) return D == 128 ? f(float(), std::integral_constant<int, 128>()) : f(float(), std::integral_constant<int, 64>());
-  return D == 128 ? f(bf16(), std::integral_constant<int, 128>()) : f(bf16(), std::integral_constant<int, 64>());
-}
 static int grid_of(int64_t workgroups, dim3* grid) {
   if (workgroups > 0x3fffffll) { set_error("too many tiles for one launch"); return SB_ERR_UNSUPPORTED; }
   *grid = dim3((unsigned)workgroups);
@@ -462,7 +888,7 @@ static int check_window(const sb_problem* p, int32_t window, int32_t sinks, Geo*
   const int rc = make_batch(p, g);
   if (rc != SB_OK) return rc;
   if (window < 1 || sinks < 0) { set_error("window (%d) must be at least 1 and sinks (%d) not negative", window, sinks); return SB_ERR_INVALID_ARG; }
-  return SB_OK;
+  return check_rows(g->T, g->G);
 }
 static WindowParams window_params(const Geo& g, const sb_problem* p, int32_t window, int32_t sinks) {
   WindowParams P{};
@@ -473,11 +899,17 @@ static WindowParams window_params(const Geo& g, const sb_problem* p, int32_t win
   return P;
 }
 
-struct WindowWs { size_t delta, bytes; };
-static WindowWs window_bwd_ws(const Geo& g) {
+// Far rows a far item takes: about as many as an ordinary item has, within limits that keep a long window's items short and a short one's few.
+static int far_rows_of(int window) { return window + kDkvKeys < 512 ? 512 : window + kDkvKeys > 4096 ? 4096 : window + kDkvKeys; }
+struct WindowWs { size_t lse2, dr, partials, bytes; int64_t far; };
+static WindowWs window_bwd_ws(const Geo& g, const int32_t* cu, int window, int sinks) {
   WindowWs w{};
   size_t o = 0;
-  w.delta = o; o = align_up(o + sizeof(float) * (size_t)g.T * g.Hq);
+  w.lse2 = o; o = align_up(o + sizeof(float) * (size_t)g.T * g.Hq);
+  w.dr = o;   o = align_up(o + sizeof(float) * (size_t)g.T * g.Hq);
+  if (g.dtype == SB_BF16)
+    for (int s = 0; s < g.S; ++s) w.far += far_items(cu[s + 1] - cu[s], window, sinks, far_rows_of(window));
+  w.partials = o; o = align_up(o + (size_t)w.far * g.Hkv * 2 * kFarKeys * g.D * sizeof(float));
   w.bytes = o;
   return w;
 }
@@ -493,7 +925,7 @@ int sb_window_ws_bytes(const sb_problem* p, int32_t window, int32_t sinks, int64
   const int rc = check_window(p, window, sinks, &g);
   if (rc != SB_OK) return rc;
   if (fwd_bytes) *fwd_bytes = 0;
-  if (bwd_bytes) *bwd_bytes = (int64_t)window_bwd_ws(g).bytes;
+  if (bwd_bytes) *bwd_bytes = (int64_t)window_bwd_ws(g, p->cu_seqlens_host, window, sinks).bytes;
   return SB_OK;
 }
 
@@ -522,28 +954,46 @@ int sb_window_attn_bwd(const sb_problem* p, int32_t window, int32_t sinks, const
   const hipStream_t st = (hipStream_t)stream;
   WindowParams P = window_params(g, p, window, sinks);
   P.q = q; P.k = k; P.v = v; P.o_in = o; P.lse = (float*)lse; P.d_o = d_o; P.dq = dq; P.dk = dk; P.dv = dv;
-  P.delta = (float*)((char*)ws + window_bwd_ws(g).delta);
+  const int32_t* cu = p->cu_seqlens_host;
+  const WindowWs w = window_bwd_ws(g, cu, window, sinks);
+  P.lse2 = (float*)((char*)ws + w.lse2);
+  P.dr = (float*)((char*)ws + w.dr);
+  P.partials = (float*)((char*)ws + w.partials);
+  P.far_rows = far_rows_of(window);
+  const bool f32 = g.dtype == SB_F32;
   const int64_t rows = (int64_t)g.T * g.Hq, per = 1024 / g.D;
-  const int64_t q_items = row_tiles(p->cu_seqlens_host, g.S, g.G, 32) * g.Hkv, k_items = row_tiles(p->cu_seqlens_host, g.S, 1, 32) * g.Hkv;
-  dim3 delta_grid, q_grid, k_grid;
-  if ((rc = grid_of((rows + per - 1) / per, &delta_grid)) != SB_OK || (rc = grid_of((q_items + 3) / 4, &q_grid)) != SB_OK ||
-      (rc = grid_of((k_items + 3) / 4, &k_grid)) != SB_OK)
+  const int64_t q_items = row_tiles(cu, g.S, g.G, f32 ? 32 : 256) * g.Hkv, k_items = row_tiles(cu, g.S, 1, f32 ? 32 : kDkvKeys) * g.Hkv;
+  dim3 delta_grid, q_grid, k_grid, far_grid;
+  if ((rc = grid_of((rows + per - 1) / per, &delta_grid)) != SB_OK || (rc = grid_of(f32 ? (q_items + 3) / 4 : q_items, &q_grid)) != SB_OK ||
+      (rc = grid_of(f32 ? (k_items + 3) / 4 : k_items, &k_grid)) != SB_OK || (rc = grid_of(w.far * g.Hkv, &far_grid)) != SB_OK)
     return rc;
-  return with_types(g.D, g.dtype, [&](auto t, auto d) {
-    using T = decltype(t);
-    constexpr int DD = decltype(d)::value;
+  auto launch = [&](auto d) {
+    constexpr int D = decltype(d)::value;
     {
       KernelTimer kt(K_WINDOW_DQ, st);
-      hipLaunchKernelGGL((window_delta_kernel<T, DD>), delta_grid, dim3(256), 0, st, P, rows);
-      SB_LAUNCH_CHECK("window_delta_kernel");
-      hipLaunchKernelGGL((window_dq_f32_kernel<T, DD>), q_grid, dim3(256), 0, st, P, q_items);
-      SB_LAUNCH_CHECK("window_dq_f32_kernel");
+      if (f32) {
+        hipLaunchKernelGGL((window_delta_kernel<float, D>), delta_grid, dim3(256), 0, st, P, rows);
+        SB_LAUNCH_CHECK("window_delta_kernel");
+        hipLaunchKernelGGL((window_dq_f32_kernel<float, D>), q_grid, dim3(256), 0, st, P, q_items);
+      } else {
+        hipLaunchKernelGGL((window_dq_kernel<D>), q_grid, dim3(512), 0, st, P);
+      }
+      SB_LAUNCH_CHECK("window_dq_kernel");
     }
     KernelTimer kt(K_WINDOW_DKV, st);
-    hipLaunchKernelGGL((window_dkv_f32_kernel<T, DD>), k_grid, dim3(256), 0, st, P, k_items);
-    SB_LAUNCH_CHECK("window_dkv_f32_kernel");
-    return SB_OK;
-  });
+    if (f32) {
+      hipLaunchKernelGGL((window_dkv_f32_kernel<float, D>), k_grid, dim3(256), 0, st, P, k_items);
+    } else {
+      if (w.far > 0) {
+        hipLaunchKernelGGL((window_dkv_kernel<D, kFarKeys / 32, true>), far_grid, dim3(kFarKeys * 4), 0, st, P);
+        SB_LAUNCH_CHECK("window_dkv_kernel, far rows");
+      }
+      hipLaunchKernelGGL((window_dkv_kernel<D, kDkvKeys / 32, false>), k_grid, dim3(kDkvKeys * 4), 0, st, P);
+    }
+    SB_LAUNCH_CHECK("window_dkv_kernel");
+    return (int)SB_OK;
+  };
+  return g.D == 128 ? launch(std::integral_constant<int, 128>()) : launch(std::integral_constant<int, 64>());
 }
 
 }  // extern "C"
