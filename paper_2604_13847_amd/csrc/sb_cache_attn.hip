@@ -1,5 +1,12 @@
 // Attention of new tokens over a paged cache (serving).
+//
+// Whole chunks of a prompt go through the kernel of packed batches (sb_window.hip), which looks its key tiles up in the page table.  Few rows a sequence (single tokens above
+// all) are another matter: every key is read for a handful of products, so what bounds them is memory, and what fills the chip is splitting the keys.  cache_split_kernel
+// gives each (sequence, KV head, run of keys) to a workgroup of four wavefronts that stage their own strips and never wait for each other until they add up at the
+// end; cache_merge_kernel joins the runs.
 #include <math.h>
+
+#include <type_traits>
 
 #include "sb_window.h"
 
@@ -40,6 +47,290 @@ static int check_cache_attn(const sb_cache* c, const sb_chunk* n, int32_t window
   return check_rows(n->total_new, n->num_q_heads / c->num_kv_heads);
 }
 
+// ---------------------------------------------------------------------------------------------
+// Few rows (bfloat16): an item is up to 32 flattened rows of a KV head and per_split strips of 32 keys; wavefront w takes every fourth strip from the w-th on.  A wavefront's
+// strips of K and V come by buffer loads straight into its own LDS, the next strip's while one is worked on: 64 KiB a CU on their way (head_dim 128), no barrier, and the
+// products of a strip take a quarter of the time that memory takes to deliver four.  Pages are looked up 64 strips ahead, a lane a strip.
+template <int D>
+__global__ __launch_bounds__(256) void cache_split_kernel(WindowParams P) {
+  constexpr int ROW_B = D * 2, STRIP_B = 32 * ROW_B, NOP = D / 16, C = D / 8, RPI = 64 / C, LPG = 16 / RPI;  // loads per 16 rows
+  constexpr int OUT_P = D + 4;  // floats from row to row of a wavefront's sums in LDS
+  __shared__ __attribute__((aligned(1024))) char ring[4][2][2 * STRIP_B];  // K, V
+  __shared__ float stats[2][4][32];
+  static_assert(32 * OUT_P * 4 <= 4 * STRIP_B, "the sums take the strips' place");
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
+  // (what follows a division is the same in every lane but lies in vector registers, where what the loads' resources are made of must not come from)
+  const int z = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (unsigned)P.Hkv % (unsigned)P.splits));
+  const RowTile t = locate_tile<kSplitRows, true>(P, blockIdx.x / (unsigned)P.Hkv / (unsigned)P.splits);
+  if (t.s < 0) return;
+  const int g = __builtin_amdgcn_readfirstlane((int)(blockIdx.x % (unsigned)P.Hkv));
+  const int rows = t.n * P.G, m0 = t.tile * kSplitRows, mine = min(rows - m0, kSplitRows);
+  auto token = [&](int m) { return (int)((unsigned)min(m, rows - 1) / (unsigned)P.G); };
+  const int i = token(m0 + l32), h = g * P.G + min(m0 + l32, rows - 1) - i * P.G, pos = t.pos0 + i;
+  const int ta = __builtin_amdgcn_readfirstlane(t.pos0 + token(m0)), last = __builtin_amdgcn_readfirstlane(t.pos0 + token(m0 + 31));
+  const int tb = min(last, P.cache.max_pages * P.cache.page_size - 1), end = tb + 1, lo = max(0, ta - P.window + 1);
+  const KeyTiles<32> strips(ta, tb, P.window, P.sinks);
+  const int begin = (int)min((int64_t)z * P.per_split, (int64_t)strips.count());
+  const int count = z < P.splits - 1 ? min(begin + P.per_split, strips.count()) : strips.count();
+  const int turns = (count - begin - wave + 3) / 4;  // strips of this wavefront: begin + wave + 4 x (may be none)
+  const int32_t* const table = P.cache.table + (int64_t)t.s * P.cache.max_pages;
+  const unsigned page_b = (unsigned)P.Hkv << P.cache.page_shift;  // rows of a page
+
+  // Of strip begin + wave + 4 (x0 + lane): the first row, in units of 16 rows, of its keys 0 .. 15 and 16 .. 31 in the cache, and how many of each exist; -1, 0: none
+  int where[2], there[2], x0 = 0;
+  auto look_up = [&](int from) __attribute__((always_inline)) {
+    x0 = from;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      where[b] = 0;
+      there[b] = 0;
+      if (from + lane < turns) {
+        const int u = 32 * strips.at(begin + wave + 4 * (from + lane)) + 16 * b;
+        if (u < end && (u + 16 > lo || u < P.sinks)) {
+          const int page = table[u >> P.cache.page_shift];
+          if ((unsigned)page < (unsigned)P.cache.num_pages) {
+            there[b] = min(end - u, 16);
+            where[b] = page;
+          }
+        }
+      }
+    }
+  };
+  unsigned voff[LPG];
+#pragma unroll
+  for (int a = 0; a < LPG; ++a) {
+    const int r = a * RPI + lane / C;  // (the swizzle repeats every 16 rows)
+    voff[a] = (unsigned)(r * ROW_B + 16 * ((lane % C) ^ chunk_swizzle<D>(r)));
+  }
+  const unsigned ring0 = lds_offset(&ring[wave][0][0]);
+  const unsigned long long head = ((unsigned long long)g << P.cache.page_shift) * ROW_B;
+  auto issue = [&](int x) __attribute__((always_inline)) {  // strip x of this wavefront, or, past its last, as many loads of nothing
+    const unsigned slot = ring0 + (x & 1) * 2 * STRIP_B;
+    const int at = min(x - x0, 63);
+    const int u = __builtin_amdgcn_readfirstlane(32 * strips.at(min(begin + wave + 4 * x, max(strips.count() - 1, 0))));
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const unsigned page = (unsigned)__builtin_amdgcn_readlane(where[b], at);
+      const int n = x < turns ? __builtin_amdgcn_readlane(there[b], at) : 0;
+      const unsigned long long o = head + ((unsigned long long)page * page_b + ((u + 16 * b) & (P.cache.page_size - 1))) * ROW_B;
+      const unsigned bytes = (unsigned)n * ROW_B;
+      const i32x4 rk = QuadLoader<D>::resource((unsigned long long)P.cache.k + o, bytes), rv = QuadLoader<D>::resource((unsigned long long)P.cache.v + o, bytes);
+#pragma unroll
+      for (int a = 0; a < LPG; ++a)
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds" : : "v"(voff[a]), "s"(slot + b * 16 * ROW_B + a * 1024), "s"(rk) : "memory", "m0");
+#pragma unroll
+      for (int a = 0; a < LPG; ++a)
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds" : : "v"(voff[a]), "s"(slot + STRIP_B + b * 16 * ROW_B + a * 1024), "s"(rv) : "memory", "m0");
+    }
+  };
+
+  // B operand of S^T = K Q^T: column = row lane%32, slots = d 16ks + 8hf + (0..7)
+  bf16x8 qf[NOP];
+  {
+    const bf16* qp = (const bf16*)P.q + ((int64_t)(t.row0 + i) * P.Hq + h) * D + 8 * hf;
+#pragma unroll
+    for (int ks = 0; ks < NOP; ++ks) qf[ks] = *(const bf16x8*)(qp + 16 * ks);
+  }
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zero16();
+  float top = -__builtin_inff(), l = 0.f;  // largest score, in units of log 2, and sum
+  if (turns > 0) {
+    look_up(0);
+#pragma unroll
+    for (int ks = 0; ks < NOP; ++ks) asm volatile("" : "+v"(qf[ks]));
+    asm volatile("" : "+v"(where[0]), "+v"(where[1]), "+v"(there[0]), "+v"(there[1]));
+    issue(0);
+  }
+  unsigned row_a[NOP], tr_a[D / 32][2];
+#pragma unroll
+  for (int ks = 0; ks < NOP; ++ks) row_a[ks] = ring0 + l32 * ROW_B + 16 * ((2 * ks + hf) ^ chunk_swizzle<D>(l32));
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int r = 8 * half + 4 * hf + ((lane & 15) >> 2), d = 32 * dt + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+      tr_a[dt][half] = ring0 + STRIP_B + r * ROW_B + 16 * ((d >> 3) ^ chunk_swizzle<D>(r)) + 2 * (d & 7);
+    }
+  for (int x = 0; x < turns; ++x) {
+    const int u0 = 32 * strips.at(begin + wave + 4 * x);
+    const unsigned off = (x & 1) * 2 * STRIP_B;
+    const unsigned have = (1u << __builtin_amdgcn_readlane(there[0], x - x0)) - 1 | ((1u << __builtin_amdgcn_readlane(there[1], x - x0)) - 1) << 16;  // keys that exist
+    const bool refill = x + 1 < turns && x + 1 - x0 == 64;
+    if (refill) look_up(x + 1);
+    if (refill) asm volatile("s_waitcnt vmcnt(0)" : "+v"(where[0]), "+v"(where[1]), "+v"(there[0]), "+v"(there[1]) : : "memory");
+    issue(x + 1);
+    wait_vmcnt<4 * LPG>();  // strip x has landed
+    bf16x8 op[NOP];
+#pragma unroll
+    for (int ks = 0; ks < NOP; ++ks) op[ks] = *(const bf16x8 __attribute__((address_space(3)))*)(uintptr_t)(row_a[ks] + off);
+    f32x16 sc = zero16();
+#pragma unroll
+    for (int ks = 0; ks < NOP; ++ks) sc = mfma32(op[ks], qf[ks], sc);
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) {
+        const unsigned o = off + kk * 16 * ROW_B;
+        const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4 __attribute__((address_space(3)))*)(uintptr_t)(tr_a[dt][0] + o));
+        const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4 __attribute__((address_space(3)))*)(uintptr_t)(tr_a[dt][1] + o));
+        op[kk * (D / 32) + dt] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+    float p[16], mx = -__builtin_inff();
+#pragma unroll
+    for (int v = 0; v < 16; ++v) p[v] = sc[v] * P.scale_log2e;
+    if (u0 + 31 > ta || (last - u0 >= P.window && u0 + 31 >= P.sinks) || have != ~0u) {
+      const Sight sees(pos, u0, hf, P.window, P.sinks);
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        if (!sees(c_row(v, 0)) || !(have >> c_row(v, hf) & 1)) p[v] = -__builtin_inff();
+    }
+#pragma unroll
+    for (int v = 0; v < 16; ++v) mx = fmaxf(mx, p[v]);
+    mx = fmaxf(top, max_across_halves(mx));
+    const float ref = mx == -__builtin_inff() ? 0.f : mx;  // nothing seen yet: keep the exponents finite
+    const float alpha = fast_exp2(top - ref);
+    top = mx;
+    l *= alpha;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[dt][v] *= alpha;
+    bf16x8 w[2];
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const float e = fast_exp2(p[v] - ref);
+      l += e;  // (before the rounding: LSE keeps float32's precision)
+      w[v >> 3][v & 7] = (bf16)e;
+    }
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) acc[dt] = mfma32(op[kk * (D / 32) + dt], w[kk], acc[dt]);
+  }
+  wait_vmcnt<0>();
+  // the four wavefronts' sums, through LDS (each in its own strips' place)
+  l += __shfl_xor(l, 32, 64);
+  float* const out = (float*)&ring[wave][0][0];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int vg = 0; vg < 4; ++vg)
+      *(f32x4*)(out + l32 * OUT_P + 32 * dt + 8 * vg + 4 * hf) = f32x4{acc[dt][4 * vg], acc[dt][4 * vg + 1], acc[dt][4 * vg + 2], acc[dt][4 * vg + 3]};
+  if (hf == 0) { stats[0][wave][l32] = top; stats[1][wave][l32] = l; }
+  __syncthreads();
+  constexpr int LANES = D / 4;
+  const int c = threadIdx.x % LANES;
+  for (int r = threadIdx.x / LANES; r < mine; r += 256 / LANES) {
+    float best = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) best = fmaxf(best, stats[0][w][r]);
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if (stats[1][w][r] == 0.f) continue;
+      const float f = fast_exp2(stats[0][w][r] - best);
+      sum += f * stats[1][w][r];
+      x += f * *(const f32x4*)((const float*)&ring[w][0][0] + r * OUT_P + 4 * c);
+    }
+    const int j = token(m0 + r), hh = g * P.G + m0 + r - j * P.G;
+    const int64_t row = (int64_t)(t.row0 + j) * P.Hq + hh;
+    const float inv = sum > 0.f ? 1.0f / sum : 0.f, lse2 = sum > 0.f ? best + __builtin_log2f(sum) : -__builtin_inff();
+    x *= inv;
+    if (P.splits > 1) {
+      const int64_t at = (int64_t)z * P.T * P.Hq + row;
+      if (c == 0) P.part_lse[at] = lse2;
+      if (sum > 0.f) *(f32x4*)(P.part_o + at * D + 4 * c) = x;
+    } else {
+      bf16x4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = (bf16)x[e];
+      *(bf16x4*)((bf16*)P.o + row * D + 4 * c) = y;
+      if (c == 0) P.lse[(int64_t)hh * P.T + t.row0 + j] = lse2 * 0.69314718055994531f;
+    }
+  }
+}
+
+// Joins the runs of keys: one wavefront a row and head.  A run that saw nothing has left LSE -infinity and no sums.  `few`, `many`: runs of sequences of up to few_rows
+// flattened rows and of the others; where that is one, the rows are complete.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void cache_merge_kernel(WindowParams P, int few_rows, int few, int many) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * 4 + wave, all = (int64_t)P.T * P.Hq;
+  if (row >= all) return;
+  const int tok = (int)(row / P.Hq), h = (int)(row % P.Hq);
+  const int s = sequence_of(P.cu, P.S, tok, lane);
+  if (s >= P.S) return;  // a row of no sequence: left as it was
+  const int row0 = max(P.cu[s], 0), n = min(min(P.cu[s + 1], P.T) - row0, P.max_new);
+  if (tok - row0 < 0 || tok - row0 >= n) return;
+  const int splits = n * P.G <= few_rows ? few : many;
+  if (splits <= 1) return;
+  constexpr int E = D / 64;
+  float best = -__builtin_inff();
+  for (int z0 = 0; z0 < splits; z0 += 64) best = fmaxf(best, z0 + lane < splits ? P.part_lse[(z0 + lane) * all + row] : -__builtin_inff());
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) best = fmaxf(best, __shfl_xor(best, off, 64));
+  float x[E] = {}, sum = 0.f;
+  if (best > -__builtin_inff()) {
+    for (int z0 = 0; z0 < splits; z0 += 64) {
+      const float mine = z0 + lane < splits ? fast_exp2(P.part_lse[(z0 + lane) * all + row] - best) : 0.f;
+      const int n = min(64, splits - z0);
+      for (int z = 0; z < n; ++z) {
+        const float f = __shfl(mine, z, 64);
+        if (f == 0.f) continue;
+        sum += f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(f, P.part_o[((z0 + z) * all + row) * D + E * lane + e], x[e]);
+      }
+    }
+  }
+  const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) ((T*)P.o)[row * D + E * lane + e] = (T)(x[e] * inv);
+  if (lane == 0) P.lse[(int64_t)h * P.T + tok] = sum > 0.f ? (best + __builtin_log2f(sum)) * 0.69314718055994531f : -__builtin_inff();
+}
+
+// How the work is cut.  Sequences of up to kFewRows flattened rows are cache_split_kernel's (bfloat16), the others the packed batches' kernel's; a batch of one kind costs one launch.
+constexpr int kFewRows = 2 * kSplitRows;
+struct CacheLaunch { int64_t items; int splits, per_split; };  // tiles of rows; keys in `splits` runs of per_split tiles
+struct CachePlan {
+  CacheLaunch few, many;           // items 0: no such launch
+  size_t part_o, part_lse, bytes;  // workspace
+};
+static CachePlan plan_cache(const sb_cache* c, const sb_chunk* n, int window, int sinks) {
+  CachePlan p{};
+  const int G = n->num_q_heads / c->num_kv_heads, S = n->num_seqs;
+  const int64_t most = (int64_t)(n->max_new < n->total_new ? n->max_new : n->total_new) * G;  // rows of a sequence
+  auto launch = [&](int64_t most_rows, int rows, int tile, int64_t wanted, int64_t least, int64_t largest) {
+    CacheLaunch l{};
+    const int64_t by_total = row_tiles_most(n->total_new, S, G, rows), by_seq = (most_rows + rows - 1) / rows * S;
+    l.items = by_total < by_seq ? by_total : by_seq;
+    // key tiles of an item, about: what max_length, the window and the sinks leave
+    const int64_t in_window = (int64_t)window + (rows + G - 1) / G + sinks + 2 * tile;
+    const int64_t keys = in_window < n->max_length ? in_window : n->max_length, tiles = (keys + tile - 1) / tile;
+    int64_t per = (tiles * l.items * c->num_kv_heads + wanted - 1) / wanted;
+    per = (per + least - 1) / least * least;
+    if (per < least) per = least;
+    if (per > largest) per = largest;
+    l.splits = (int)((tiles + per - 1) / per);
+    if (l.splits < 1) l.splits = 1;
+    l.per_split = (int)per;
+    return l;
+  };
+  p.few.splits = p.many.splits = 1;
+  const bool f32 = c->dtype == SB_F32;
+  // Two workgroups a CU; a strip for each wavefront at least, and 1024 keys at most, so that sequences of unequal lengths even out.
+  if (!f32 && (S > 1 || most <= kFewRows)) p.few = launch(most < kFewRows ? most : kFewRows, kSplitRows, 32, 512, 4, 32);
+  // A workgroup (float32: four items) a CU, of 8 tiles at least.
+  if (f32 || most > kFewRows) p.many = launch(most, forward_rows(c->dtype), f32 ? 32 : 64, f32 ? 1024 : 256, 8, 1 << 30);
+  const size_t splits = (size_t)(p.few.splits > p.many.splits ? p.few.splits : p.many.splits), all = (size_t)n->total_new * n->num_q_heads;
+  if (splits > 1) {
+    p.part_o = align_up(splits * all * sizeof(float));
+    p.bytes = align_up(p.part_o + splits * all * c->head_dim * sizeof(float));
+  }
+  return p;
+}
+
 }  // namespace sb
 
 using namespace sb;
@@ -50,7 +341,7 @@ int sb_cache_attn_ws_bytes(const sb_cache* c, const sb_chunk* n, int32_t window,
   if (!bytes) { set_error("null output"); return SB_ERR_INVALID_ARG; }
   const int rc = check_cache_attn(c, n, window, sinks);
   if (rc != SB_OK) return rc;
-  *bytes = 0;
+  *bytes = n->num_seqs == 0 || n->max_new == 0 ? 0 : (int64_t)plan_cache(c, n, window, sinks).bytes;
   return SB_OK;
 }
 
@@ -67,8 +358,43 @@ int sb_cache_attn(const sb_cache* c, const sb_chunk* n, int32_t window, int32_t 
   P.scale = n->softmax_scale > 0.f ? n->softmax_scale : 1.0f / sqrtf((float)c->head_dim);
   P.scale_log2e = P.scale * 1.4426950408889634f;
   P.cache = make_paged(c);
-  KernelTimer kt(K_CACHE_ATTN, (hipStream_t)stream);
-  return launch_window_fwd(P, c->head_dim, c->dtype, true, row_tiles_most(P.T, P.S, P.G, forward_rows(c->dtype)), (hipStream_t)stream);
+  const CachePlan plan = plan_cache(c, n, window, sinks);
+  const bool joined = plan.few.splits > 1 || plan.many.splits > 1;
+  if (joined) {
+    if (!ws) { set_error("null argument"); return SB_ERR_INVALID_ARG; }
+    P.part_o = (float*)((char*)ws + plan.part_o);
+    P.part_lse = (float*)((char*)ws + plan.part_lse);
+  }
+  const hipStream_t st = (hipStream_t)stream;
+  const bool f32 = c->dtype == SB_F32;
+  dim3 grid, merge_grid;
+  if ((rc = grid_of(plan.few.items * P.Hkv * plan.few.splits, &grid)) != SB_OK || (rc = grid_of(((int64_t)P.T * P.Hq + 3) / 4, &merge_grid)) != SB_OK) return rc;
+  KernelTimer kt(K_CACHE_ATTN, st);
+  if (plan.many.items > 0) {
+    P.splits = plan.many.splits;
+    P.per_split = plan.many.per_split;
+    P.rows_from = f32 || plan.few.items == 0 ? 0 : kFewRows + 1;
+    P.rows_to = 0x7fffffff;
+    if ((rc = launch_window_fwd(P, c->head_dim, c->dtype, true, plan.many.items, st)) != SB_OK) return rc;
+  }
+  if (plan.few.items > 0) {
+    P.splits = plan.few.splits;
+    P.per_split = plan.few.per_split;
+    P.rows_from = 0;
+    P.rows_to = kFewRows;
+    if (c->head_dim == 128) hipLaunchKernelGGL((cache_split_kernel<128>), grid, dim3(256), 0, st, P);
+    else hipLaunchKernelGGL((cache_split_kernel<64>), grid, dim3(256), 0, st, P);
+    SB_LAUNCH_CHECK("cache_split_kernel");
+  }
+  if (joined) {
+    auto merge = [&](auto t, auto d) {
+      hipLaunchKernelGGL((cache_merge_kernel<decltype(t), decltype(d)::value>), merge_grid, dim3(256), 0, st, P, plan.few.items > 0 ? kFewRows : 0, plan.few.splits, plan.many.splits);
+    };
+    auto with_d = [&](auto t) { if (c->head_dim == 128) merge(t, std::integral_constant<int, 128>()); else merge(t, std::integral_constant<int, 64>()); };
+    if (f32) with_d(float()); else with_d(bf16());
+    SB_LAUNCH_CHECK("cache_merge_kernel");
+  }
+  return SB_OK;
 }
 
 }  // extern "C"

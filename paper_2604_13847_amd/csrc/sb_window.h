@@ -24,6 +24,10 @@ struct WindowParams {
   PagedCache cache;
   const int32_t* cached;
   int max_new;
+  // keys split over `splits` workgroups, per_split tiles each (the last one takes what is left); part_o [splits][T][Hq][D] normalised, part_lse [splits][T][Hq] in base 2
+  int splits, per_split;
+  float *part_o, *part_lse;
+  int rows_from, rows_to;  // sequences of these many flattened rows are this launch's, the others another's
 };
 
 // The query rows of a KV head's group are flattened: row m of a sequence is token m / G, query head m % G of the group.  Heads of a token so share
@@ -50,7 +54,10 @@ __device__ inline RowTile locate_tile(const WindowParams& P, int64_t x) {
         n = min(n, P.T);
       }
       n = max(n - row0, 0);
-      if (PAGED) n = min(n, P.max_new);
+      if (PAGED) {
+        n = min(n, P.max_new);
+        if (n * P.G < P.rows_from || n * P.G > P.rows_to) n = 0;
+      }
     }
     const int64_t c = (int64_t)(((unsigned)n * (unsigned)P.G + (unsigned)ROWS - 1) / (unsigned)ROWS);  // (rows of a sequence fit 31 bits: see check_rows)
     int64_t incl = c;
@@ -67,7 +74,7 @@ __device__ inline RowTile locate_tile(const WindowParams& P, int64_t x) {
       t.n = __builtin_amdgcn_readlane(n, src);
       const int64_t first = __shfl(incl - c, src, 64), tiles = __shfl(c, src, 64);
       t.tile = __builtin_amdgcn_readfirstlane((int)(tiles - 1 - (x - first)));
-      t.pos0 = PAGED ? min(max(P.cached[t.s], 0), 0x7fffffff - t.n) : 0;
+      t.pos0 = PAGED ? __builtin_amdgcn_readfirstlane(min(max(P.cached[t.s], 0), 0x7fffffff - t.n)) : 0;
       return t;
     }
     x -= __shfl(incl, 63, 64);
@@ -200,7 +207,9 @@ __device__ inline void store_tile(char* buf, int lane, V value, A address) {
   }
 }
 
+int grid_of(int64_t workgroups, dim3* grid);
 int check_rows(int64_t tokens, int G);  // flattened rows fit 31 bits
+constexpr int kSplitRows = 32;  // flattened rows of an item of cache_split_kernel
 int64_t row_tiles(const int32_t* cu_host, int S, int G, int rows);  // of a packed batch
 int64_t row_tiles_most(int total, int S, int G, int rows);          // where the lengths are not known to the host
 

@@ -90,7 +90,8 @@ __global__ __launch_bounds__(256) void window_fwd_f32_kernel(WindowParams P, int
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
   const int64_t item = (int64_t)blockIdx.x * 4 + wave;
   if (item >= items) return;
-  const RowTile t = locate_tile<32, PAGED>(P, item / P.Hkv);
+  const int splits = PAGED ? P.splits : 1, z = (int)(item / P.Hkv % splits);
+  const RowTile t = locate_tile<32, PAGED>(P, item / P.Hkv / splits);
   if (t.s < 0) return;
   const int g = (int)(item % P.Hkv);
   const int64_t rows = (int64_t)t.n * P.G, m0 = (int64_t)t.tile * 32, m = min(m0 + l32, rows - 1);
@@ -106,7 +107,9 @@ __global__ __launch_bounds__(256) void window_fwd_f32_kernel(WindowParams P, int
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zero16();
   float top = -__builtin_inff(), l = 0.f;  // largest score seen (in units of log 2), sum of exponentials
-  for (int x = 0; x < tiles.count(); ++x) {
+  const int x0 = PAGED ? (int)min((int64_t)z * P.per_split, (int64_t)tiles.count()) : 0;
+  const int x1 = PAGED && z < splits - 1 ? min(x0 + P.per_split, tiles.count()) : tiles.count();
+  for (int x = x0; x < x1; ++x) {
     const int u0 = 32 * tiles.at(x);
     const T* kp = keys.k(u0 + l32);
     load_row<D>(kr, kp, hf);
@@ -137,6 +140,11 @@ __global__ __launch_bounds__(256) void window_fwd_f32_kernel(WindowParams P, int
   }
   l += __shfl_xor(l, 32, 64);
   if (m0 + l32 >= rows) return;
+  if (splits > 1) {
+    if (l != 0.f) store_column<D>(P.part_o + (int64_t)z * P.T * P.Hq * D + at, acc, 1.0f / l, hf);
+    if (hf == 0) P.part_lse[(int64_t)z * P.T * P.Hq + at / D] = l == 0.f ? -__builtin_inff() : top + __builtin_log2f(l);
+    return;
+  }
   store_column<D>((T*)P.o + at, acc, l == 0.f ? 0.f : 1.0f / l, hf);
   if (hf == 0) P.lse[(int64_t)h * P.T + t.row0 + i] = l == 0.f ? -__builtin_inff() : (top + __builtin_log2f(l)) * 0.69314718055994531f;
 }
@@ -258,18 +266,21 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void w
   constexpr float kLazy = 8.0f;
   __shared__ __attribute__((aligned(1024))) char tiles[2][2][TILE_B];  // [buffer][K, V]
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
-  const RowTile t = locate_tile<ROWS, PAGED>(P, blockIdx.x / P.Hkv);
+  const int splits = PAGED ? P.splits : 1, z = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (unsigned)P.Hkv % (unsigned)splits));
+  const RowTile t = locate_tile<ROWS, PAGED>(P, blockIdx.x / (unsigned)P.Hkv / (unsigned)splits);
   if (t.s < 0) return;
-  const int g = (int)(blockIdx.x % P.Hkv);
+  const int g = __builtin_amdgcn_readfirstlane((int)(blockIdx.x % (unsigned)P.Hkv));
   const int rows = t.n * P.G, mb = t.tile * ROWS, mw = mb + 32 * wave;
   auto token = [&](int m) { return (int)((unsigned)min(m, rows - 1) / (unsigned)P.G); };
   const int i = token(mw + l32), h = g * P.G + min(mw + l32, rows - 1) - i * P.G, pos = t.pos0 + i;
-  const int ta = t.pos0 + token(mb);
-  const int tb = PAGED ? min(t.pos0 + token(mb + ROWS - 1), P.cache.max_pages * P.cache.page_size - 1) : token(mb + ROWS - 1);
-  const int wa = t.pos0 + token(mw), wb = t.pos0 + token(mw + 31);  // this wavefront's
+  // (the same in every lane, but a division leaves it in vector registers, where what the loads' resources are made of must not come from)
+  auto position = [&](int m) { return __builtin_amdgcn_readfirstlane(t.pos0 + token(m)); };
+  const int ta = position(mb), all_rows = position(mb + ROWS - 1), tb = PAGED ? min(all_rows, P.cache.max_pages * P.cache.page_size - 1) : all_rows;
+  const int wa = position(mw), wb = position(mw + 31);  // this wavefront's
   const bool working = mw < rows;
   const KeyTiles<64> keys(ta, tb, P.window, P.sinks);
-  const int count = keys.count();
+  const int begin = PAGED ? (int)min((int64_t)z * P.per_split, (int64_t)keys.count()) : 0;
+  const int count = PAGED && z < splits - 1 ? min(begin + P.per_split, keys.count()) : keys.count();
   KeySource<D, PAGED> src;
   src.init(P, t, g, max(0, ta - P.window + 1), tb + 1);
   RowsLoader<D> loader;
@@ -279,7 +290,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void w
     const int u = 64 * keys.at(x) + 8 * wave;
     int there;
     const unsigned long long o = src.rows_at(P, u, 8, there);
-    const unsigned slot = tiles0 + (x & 1) * 2 * TILE_B;
+    const unsigned slot = tiles0 + ((x - begin) & 1) * 2 * TILE_B;
     loader.issue(src.k + o, there, slot);
     loader.issue(src.v + o, there, slot + TILE_B);
   };
@@ -294,7 +305,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void w
   // the query operands must have landed before the tile loads start: from here on only those are in flight, and waited for by hand
 #pragma unroll
   for (int ks = 0; ks < NOP; ++ks) asm volatile("" : "+v"(qf[ks]));
-  issue(0);
+  if (begin < count) issue(begin);
 
   unsigned row_a[NOP], tr_a[D / 32][2];
 #pragma unroll
@@ -398,7 +409,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void w
     const bool all = u0 + 63 <= wa && (wb - u0 < P.window || u0 + 63 < P.sinks) && missing == 0;
     if (!none) tile(buf_c, u0, all, missing);
   };
-  int x = 0;
+  int x = begin;
   for (; x + 2 <= count; x += 2) {  // two tiles a turn, so that a tile's buffer is known at compile time
     visit(std::integral_constant<int, 0>(), x);
     visit(std::integral_constant<int, 1>(), x + 1);
@@ -408,6 +419,13 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void w
 
   l += __shfl_xor(l, 32, 64);  // the two lane halves hold different keys of the same row
   const float inv = l > 0.f ? 1.0f / l : 0.f;
+  if (PAGED && splits > 1) {
+    if (mw + l32 >= rows) return;
+    const int64_t row = ((int64_t)z * P.T + t.row0 + i) * P.Hq + h;
+    if (hf == 0) P.part_lse[row] = l > 0.f ? m * P.scale_log2e + __builtin_log2f(l) : -__builtin_inff();
+    if (l > 0.f) store_column<D>(P.part_o + row * D, oacc, inv, hf);
+    return;
+  }
   __syncthreads();  // the tiles' LDS is free
   store_tile<D>(&tiles[0][0][0] + wave * 32 * ROW_B, lane, [&](int dt, int v) __attribute__((always_inline)) { return oacc[dt][v] * inv; },
                 [&](int r) __attribute__((always_inline)) -> bf16* {
@@ -429,11 +447,12 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void w
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
   const RowTile t = locate_tile<ROWS, false>(P, blockIdx.x / P.Hkv);
   if (t.s < 0) return;
-  const int g = (int)(blockIdx.x % P.Hkv);
+  const int g = __builtin_amdgcn_readfirstlane((int)(blockIdx.x % (unsigned)P.Hkv));
   const int rows = t.n * P.G, mb = t.tile * ROWS, mw = mb + 32 * wave;
   auto token = [&](int m) { return (int)((unsigned)min(m, rows - 1) / (unsigned)P.G); };
   const int i = token(mw + l32), h = g * P.G + min(mw + l32, rows - 1) - i * P.G;
-  const int ta = token(mb), tb = token(mb + ROWS - 1), wa = token(mw), wb = token(mw + 31);
+  auto position = [&](int m) { return __builtin_amdgcn_readfirstlane(token(m)); };  // (see the forward kernel)
+  const int ta = position(mb), tb = position(mb + ROWS - 1), wa = position(mw), wb = position(mw + 31);
   const bool working = mw < rows;
   const KeyTiles<64> keys(ta, tb, P.window, P.sinks);
   const int count = keys.count();
@@ -601,7 +620,7 @@ __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
   const int pair = wave % PAIRS;
   const bool second = wave >= PAIRS;  // wavefronts w and w + 4 share a SIMD
-  const int g = (int)(blockIdx.x % P.Hkv);
+  const int g = __builtin_amdgcn_readfirstlane((int)(blockIdx.x % (unsigned)P.Hkv));
   // which sequence, and what of it
   int s = -1, seq0 = 0, n = 0;
   int64_t x = blockIdx.x / P.Hkv, far0 = 0;  // far0: far items of the earlier sequences
@@ -861,14 +880,14 @@ int64_t row_tiles(const int32_t* cu, int S, int G, int rows) {
 }
 int64_t row_tiles_most(int total, int S, int G, int rows) { return ((int64_t)total * G) / rows + S; }
 
-static int grid_of(int64_t workgroups, dim3* grid) {
+int grid_of(int64_t workgroups, dim3* grid) {
   if (workgroups > 0x3fffffll) { set_error("too many tiles for one launch"); return SB_ERR_UNSUPPORTED; }
   *grid = dim3((unsigned)workgroups);
   return SB_OK;
 }
 
 int launch_window_fwd(const WindowParams& P, int D, int dtype, bool paged, int64_t tiles, hipStream_t st) {
-  const int64_t items = tiles * P.Hkv;
+  const int64_t items = tiles * P.Hkv * (paged ? P.splits : 1);
   dim3 grid;
   const int rc = grid_of(dtype == SB_F32 ? (items + 3) / 4 : items, &grid);
   if (rc != SB_OK) return rc;
