@@ -12,7 +12,8 @@ struct WindowParams {
   void* o;
   float* lse;         // [Hq][T]
   float* lse2;        // [T][Hq] LSE * log2 e and
-  float* dr;          // rowsum(dO * O): backward, the order in which flattened rows need them
+  float* dr;          // rowsum(dO * O): backward, the order in which flattened rows need them (float32)
+  bf16x8* stats;      // [T][Hq][2] the same as operands of matrix instructions (bfloat16), see split3
   float* partials;    // dK, dV of sinks from rows far behind, see window_dkv_kernel
   int far_rows;       // tokens of a far item
   void *dq, *dk, *dv;
@@ -80,6 +81,17 @@ __device__ inline RowTile locate_tile(const WindowParams& P, int64_t x) {
     x -= __shfl(incl, 63, 64);
   }
   return RowTile{-1, 0, 0, 0, 0};
+}
+
+// x as three bfloat16 numbers that add up to it but for 2^-25 of it, followed by zeros: a product with (-1, -1, -1, 0, ...) subtracts x from an accumulator.
+__device__ inline bf16x8 split3(float x) {
+  bf16x8 r = zero_bf16x8();
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    r[i] = (bf16)x;
+    x -= (float)r[i];
+  }
+  return r;
 }
 
 // Keys of rows at positions ta .. tb, in tiles of `TILE`: sink tiles 0 .. far - 1, then tiles near .. end - 1.  (tb: that of the last key that can exist, if that is less.)

@@ -439,7 +439,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void w
 
 // ---------------------------------------------------------------------------------------------
 // bfloat16 dQ.  Rows, tiles and their walk as in the forward kernel; a half tile is S, dP and dQ += dS K, whose operands go through one set of registers.  Every row belongs to one
-// workgroup here, so this is also where Dr is computed, from the dO in registers and one read of O, and left with LSE log2 e for the next kernel.
+// workgroup here, so this is also where Dr is computed, from the dO in registers and one read of O, and left with LSE for the next kernel.
 template <int D>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void window_dq_kernel(WindowParams P) {
   constexpr int ROWS = 256, ROW_B = D * 2, TILE_B = 64 * ROW_B, NOP = D / 16;
@@ -479,16 +479,14 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void w
     bf16x8 of[NOP];
 #pragma unroll
     for (int ks = 0; ks < NOP; ++ks) { dof[ks] = *(const bf16x8*)(dp + 16 * ks); of[ks] = *(const bf16x8*)(op + 16 * ks); qf[ks] = *(const bf16x8*)(qp + 16 * ks); }
-    lse2 = P.lse[(int64_t)h * P.T + t.row0 + i] * 1.4426950408889634f;
+    const float lse = P.lse[(int64_t)h * P.T + t.row0 + i];
+    lse2 = lse * 1.4426950408889634f;
 #pragma unroll
     for (int ks = 0; ks < NOP; ++ks)
 #pragma unroll
       for (int e = 0; e < 8; ++e) dr = __builtin_fmaf((float)dof[ks][e], (float)of[ks][e], dr);
     dr += __shfl_xor(dr, 32, 64);
-    if (hf == 0 && mw + l32 < rows) {
-      P.lse2[row] = lse2;
-      P.dr[row] = dr;
-    }
+    if (mw + l32 < rows) P.stats[2 * row + hf] = split3(hf ? dr : lse / P.scale);
   }
 #pragma unroll
   for (int ks = 0; ks < NOP; ++ks) asm volatile("" : "+v"(qf[ks]), "+v"(dof[ks]));
@@ -590,7 +588,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void w
 // bfloat16 dK and dV.  A workgroup owns PAIRS * 32 keys of a KV head and walks the flattened rows that see any of them, 32 a stage.  32 keys are the work of two wavefronts on one
 // SIMD: the first computes S and P and adds P^T dO to dV, the second, a stage behind, dP and dS = P (dP - Dr) and adds dS^T Q to dK; P goes from one to the other through LDS
 // in float32, lane by lane (both hold keys in columns).  Each so needs 150 registers where one wavefront for both would need more than the 256 that let two share a SIMD,
-// and has as many matrix instructions as the other.  The stages' Q and dO rows, LSE and Dr come by asynchronous loads into three slots.
+// and has as many matrix instructions as the other.  The stages' Q and dO rows, LSE and Dr come by asynchronous loads, five stages ahead.
 //
 // Sinks are seen by all rows of their sequence.  The rows behind a sink tile's ordinary ones (far rows) are the work of other workgroups (FAR), far_rows tokens each, that leave their
 // sums in float32; the tile's own workgroup, launched after them, adds them in order.  So the result does not depend on who is ahead, and no workgroup has more than its share.
@@ -612,11 +610,11 @@ __host__ __device__ inline int near_end(int u, int n, int window) {
 template <int D, int PAIRS, bool FAR>
 __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))) void window_dkv_kernel(WindowParams P) {
   constexpr int ROW_B = D * 2, TILE_B = 32 * ROW_B, NOP = D / 16, KEYS = 32 * PAIRS, NW = 2 * PAIRS;
-  constexpr int kSlots = 3, STAT_B = 256, STAGE_B = 2 * TILE_B;
+  constexpr int kSlots = 7, kAhead = 5, STAT_B = 1024, STAGE_B = 2 * TILE_B;
   constexpr int kNr = 16 * (D / 32);  // accumulator registers
   __shared__ __attribute__((aligned(1024))) char stage[kSlots][STAGE_B];  // Q, dO
-  __shared__ __attribute__((aligned(1024))) float pbuf[kSlots][PAIRS][16 * 64];
-  __shared__ __attribute__((aligned(256))) float stat[kSlots][64];        // LSE log2 e of 32 rows, Dr
+  __shared__ __attribute__((aligned(1024))) float pbuf[2][PAIRS][16 * 64];
+  __shared__ __attribute__((aligned(1024))) bf16x8 stat[kSlots][64];      // LSE / scale of 32 rows, Dr (split3)
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
   const int pair = wave % PAIRS;
   const bool second = wave >= PAIRS;  // wavefronts w and w + 4 share a SIMD
@@ -665,47 +663,67 @@ __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))
   const int ku = u0 + 32 * pair, kl = min(ku + 31, n - 1);  // this pair's keys (none: ku >= n)
   const int key = min(ku + l32, n - 1);
   const int m0 = r0 * P.G, m1 = r1 * P.G, stages = (m1 - m0 + 31) / 32;
+  // The stages are walked in a circle from y0 on: where a row's number is a multiple of an ordinary item's rows.  Neighbouring items, which an XCD works on at the same time and which have
+  // most of their rows in common, so ask for the same rows at about the same time and meet them in the XCD's L2, which could not hold the rows of one item for the next.
+  int y0 = 0;
+  if (!FAR) {
+    const int64_t around = ((int64_t)P.window + kDkvKeys) * P.G;
+    const int64_t start = (around - m0 % around) % around / 32;
+    if (start < stages) y0 = (int)start;
+  }
 
-  // loads: 32 rows of Q and of dO a stage, RPI rows an instruction; the wavefronts share them, and the first one takes the rows' statistics
-  constexpr int C = D / 8, RPI = 64 / C, LOADS = 2 * (32 / RPI), LPW = (LOADS + NW - 1) / NW;
+  // The rows of a stage: its first row's token and head, its last row's token.  Carried along, 32 flattened rows at a time: step_t tokens and step_h heads.
+  struct Rows {
+    int first, head, last;
+  };
   const unsigned G = (unsigned)P.G;
   const float inv_g = 1.0f / (float)P.G;
-  int lm[LPW], lt[LPW], lh[LPW];  // flattened row, its token and head, of this lane's loads
-  const int step_t = 32 / (int)G, step_h = 32 % (int)G;
-#pragma unroll
-  for (int a = 0; a < LPW; ++a) {
-    const int r = (wave * LPW + a) % (32 / RPI) * RPI + lane / C;
-    lm[a] = m0 + r;
-    lt[a] = (int)((unsigned)lm[a] / G);
-    lh[a] = lm[a] - lt[a] * (int)G;
-  }
-  int sm = m0 + l32, st = (int)((unsigned)sm / G), sh = sm - st * (int)G;
+  const int step_t = 32 / (int)G, step_h = 32 % (int)G, last_t = 31 / (int)G, last_h = 31 % (int)G;
+  auto rows_from = [&](int y) {
+    const int t = __builtin_amdgcn_readfirstlane((int)((unsigned)(32 * y) / G)), h = 32 * y - t * (int)G;
+    return Rows{r0 + t, h, r0 + t + last_t + (h + last_h >= P.G ? 1 : 0)};
+  };
+  auto next_rows = [&](Rows& x) __attribute__((always_inline)) {
+    x.first += step_t;
+    x.head += step_h;
+    if (x.head >= P.G) { x.head -= P.G; ++x.first; }
+    x.last = x.first + last_t + (x.head + last_h >= P.G ? 1 : 0);
+  };
+  // x / G for x < G + 32 (exact: 1 / 2 is further from a multiple of G than the product is off)
+  auto token_of = [&](int x) __attribute__((always_inline)) { return (int)(((float)x + 0.5f) * inv_g); };
+
+  // Loads: 32 rows of Q and of dO a stage, RPI rows an instruction; the wavefronts share them, and the first one takes the rows' statistics.  A scalar address for the stage's first
+  // token, a lane's own row from there on.
+  constexpr int C = D / 8, RPI = 64 / C, LOADS = 2 * (32 / RPI), LPW = LOADS / PAIRS;  // load id: tensor id % 2, rows RPI (id / 2) .. of the stage
+  static_assert(LPW * PAIRS == LOADS && LPW % 2 == 0, "every second wavefront has as many");
   const unsigned stage0 = lds_offset(&stage[0][0]), stat0 = lds_offset(&stat[0][0]);
-  auto issue = [&](int slot) __attribute__((always_inline)) {  // the next stage; rows past the last one repeat it, and are masked
+  const int wrap = P.Hq - P.G;  // rows of Q from the group's last head of a token to its first of the next, but for one
+  int load_y = y0;
+  Rows load_rows = rows_from(y0);
+  auto issue = [&](int slot) __attribute__((always_inline)) {  // the next stage; in place of rows past the item's last, which are masked, the stage's first
+    const int left = m1 - m0 - 32 * load_y;
+    const unsigned long long row = (unsigned long long)(seq0 + load_rows.first) * (unsigned)P.Hq + (unsigned)(g * P.G);
+    auto row_of = [&](int r) __attribute__((always_inline)) {  // from `row` on
+      const int x = load_rows.head + (r < left ? r : 0);
+      return (unsigned)x + (unsigned)token_of(x) * (unsigned)wrap;
+    };
+    unsigned voff = 0;
 #pragma unroll
     for (int a = 0; a < LPW; ++a) {
-      const int id = wave * LPW + a;
-      if (id < LOADS) {
-        const int r = id % (32 / RPI) * RPI + lane / C;
-        const bool there = lm[a] < m1;
-        const int64_t row = (int64_t)(seq0 + (there ? lt[a] : r1 - 1)) * P.Hq + g * P.G + (there ? lh[a] : P.G - 1);
-        const bf16* from = (const bf16*)(id < 32 / RPI ? P.q : P.d_o) + row * D + 8 * ((lane % C) ^ chunk_swizzle<D>(r));
-        dma16(from, stage0 + slot * STAGE_B + (id < 32 / RPI ? 0 : TILE_B) + id % (32 / RPI) * 1024);
-      }
-      lm[a] += 32;
-      lt[a] += step_t;
-      lh[a] += step_h;
-      if (lh[a] >= P.G) { lh[a] -= P.G; ++lt[a]; }
+      const int id = pair * LPW + a, r = id / 2 * RPI + lane / C;
+      if (a % 2 == 0) voff = row_of(r) * (D * 2) + 16 * ((lane % C) ^ chunk_swizzle<D>(r));  // (the next one is the other tensor's)
+      const unsigned long long base = (unsigned long long)(id % 2 ? P.d_o : P.q) + row * (D * 2);
+      asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2" : : "v"(voff), "s"(stage0 + slot * STAGE_B + id % 2 * TILE_B + id / 2 * 1024), "s"(base) : "memory", "m0");
     }
-    if (wave == 0) {
-      const bool there = sm < m1;
-      const int64_t row = (int64_t)(seq0 + (there ? st : r1 - 1)) * P.Hq + g * P.G + (there ? sh : P.G - 1);
-      const float* from = (hf ? P.dr : P.lse2) + row;
-      asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(from), "s"(stat0 + slot * STAT_B) : "memory", "m0");
-      sm += 32;
-      st += step_t;
-      sh += step_h;
-      if (sh >= P.G) { sh -= P.G; ++st; }
+    if (pair == 0) {
+      const unsigned off = row_of(l32) * 32 + hf * 16;
+      const unsigned long long base = (unsigned long long)P.stats + row * 32;
+      asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2" : : "v"(off), "s"(stat0 + slot * STAT_B), "s"(base) : "memory", "m0");
+    }
+    next_rows(load_rows);
+    if (++load_y == stages) {
+      load_y = 0;
+      load_rows = rows_from(0);
     }
   };
 
@@ -718,122 +736,133 @@ __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))
   }
 #pragma unroll
   for (int ks = 0; ks < NOP; ++ks) asm volatile("" : "+v"(kv[ks]));
-  issue(0);
+  if (second) {
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x)
+      if (x < stages) issue(x);
+  }
 
-  // rows of Q (dO for the second wavefront), transposed reads of the other
-  unsigned row_a[NOP], tr_a[D / 32][2];
-#pragma unroll
-  for (int ks = 0; ks < NOP; ++ks) row_a[ks] = stage0 + (second ? TILE_B : 0) + l32 * ROW_B + 16 * ((2 * ks + hf) ^ chunk_swizzle<D>(l32));
-#pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int r = 8 * half + 4 * hf + ((lane & 15) >> 2), d = 32 * dt + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-      tr_a[dt][half] = stage0 + (second ? 0 : TILE_B) + r * ROW_B + 16 * ((d >> 3) ^ chunk_swizzle<D>(r)) + 2 * (d & 7);
-    }
+  // Rows of Q (dO for the second wavefront), transposed reads of the other.  The chunk of a row that an operand needs differs from that of the first one in bits that the
+  // swizzle leaves to be turned over, so one address serves all.
+  const unsigned row_a = stage0 + (second ? TILE_B : 0) + l32 * ROW_B + 16 * (hf ^ chunk_swizzle<D>(l32));
+  const unsigned tr_a = stage0 + (second ? 0 : TILE_B) + [&] {
+    const int r = 4 * hf + ((lane & 15) >> 2), d = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    return r * ROW_B + 16 * ((d >> 3) ^ chunk_swizzle<D>(r)) + 2 * (d & 7);
+  }();
   auto ld_row = [&](int ks, unsigned off) __attribute__((always_inline)) {
-    return *(const bf16x8 __attribute__((address_space(3)))*)(uintptr_t)(row_a[ks] + off);
+    return *(const bf16x8 __attribute__((address_space(3)))*)(uintptr_t)((row_a + off) ^ (32 * ks));
   };
   auto ld_tr = [&](int kk, int dt, unsigned off) __attribute__((always_inline)) {
-    const unsigned o = off + kk * 16 * ROW_B;
-    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4 __attribute__((address_space(3)))*)(uintptr_t)(tr_a[dt][0] + o));
-    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4 __attribute__((address_space(3)))*)(uintptr_t)(tr_a[dt][1] + o));
+    const unsigned at = (tr_a + off) ^ (64 * dt);
+    static_assert(D == 128 || D == 64, "rows 8 further: the swizzle turns chunk bit 1");
+    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4 __attribute__((address_space(3)))*)(uintptr_t)(at + kk * 16 * ROW_B));
+    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4 __attribute__((address_space(3)))*)(uintptr_t)((at ^ 32) + (kk * 16 + 8) * ROW_B));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
+  const unsigned stat_a = stat0 + (second ? 512 : 0) + l32 * 16;
+  auto ld_stat = [&](int slot) __attribute__((always_inline)) { return *(const bf16x8 __attribute__((address_space(3)))*)(uintptr_t)(stat_a + slot * STAT_B); };
+  bf16x8 minus = zero_bf16x8();  // B operand that subtracts what split3 made
+  if (hf == 0) minus[0] = minus[1] = minus[2] = (bf16)-1.0f;
   f32x16 acc[D / 32];
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zero16();
 
-  // Does the pair see anything of stage x?  Both its wavefronts ask.
-  auto nothing = [&](int x) __attribute__((always_inline)) {
-    const int a = (int)((unsigned)(m0 + 32 * x) / G), b = (int)((unsigned)min(m0 + 32 * x + 31, m1 - 1) / G);  // its tokens
-    return ku >= n || b < ku || (a - kl >= P.window && ku >= P.sinks);
+  // before stage x of the loop: stages x and x + 1 are there, and what the next loads replace is no longer read
+  int load_slot = kAhead;
+  auto turn = [&](int x) __attribute__((always_inline)) {
+    if (second) {
+      if (x + kAhead > stages) wait_vmcnt<0>();
+      else if (pair == 0) wait_vmcnt<(kAhead - 2) * (LPW + 1)>();  // the stages behind x + 1 may still be on their way
+      else wait_vmcnt<(kAhead - 2) * LPW>();
+    }
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the probabilities are written, the operands read
+    __builtin_amdgcn_s_barrier();
+    if (second && x + kAhead < stages) {
+      issue(load_slot);
+      load_slot = load_slot == kSlots - 1 ? 0 : load_slot + 1;
+    }
   };
-  bf16x8 op[NOP];
-  auto products = [&](f32x16& c, unsigned off) __attribute__((always_inline)) {  // c = rows x kv, the operand registers refilled with transposed ones
+  // One set of operand registers goes through both contractions: every register is refilled with an operand of the next one when its matrix instruction has been issued, so that LDS is
+  // read at an even pace and no product waits for operands; the steps are fenced.
+  bf16x8 op[NOP], less;
+  auto add = [&](const bf16x8 (&w)[2], int next) __attribute__((always_inline)) {  // acc += transposed x w; then rows of slot `next`
 #pragma unroll
-    for (int ks = 0; ks < NOP; ++ks) op[ks] = ld_row(ks, off);
-    __builtin_amdgcn_sched_barrier(0);
-    c = zero16();
+    for (int x = 0; x < NOP; ++x) {
+      acc[x % (D / 32)] = mfma32(op[x], w[x / (D / 32)], acc[x % (D / 32)]);
+      op[x] = ld_row(x, next * STAGE_B);
+      if (x == 0) less = ld_stat(next);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto product = [&](int slot) __attribute__((always_inline)) {  // S - LSE / scale, or dP - Dr (the subtraction is one more step of the contraction); then transposed operands
+    f32x16 c = mfma32(less, minus, zero16());
 #pragma unroll
     for (int ks = 0; ks < NOP; ++ks) {
       c = mfma32(op[ks], kv[ks], c);
-      op[ks] = ld_tr(ks / (D / 32), ks % (D / 32), off);
+      op[ks] = ld_tr(ks / (D / 32), ks % (D / 32), slot * STAGE_B);
+      __builtin_amdgcn_sched_barrier(0);
     }
-#pragma unroll
-    for (int x = 0; x < NOP; ++x) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-    }
-    __builtin_amdgcn_sched_barrier(0);
+    return c;
   };
-  auto add = [&](const bf16x8 (&w)[2]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt) acc[dt] = mfma32(op[kk * (D / 32) + dt], w[kk], acc[dt]);
-  };
-  // before stage x of the loop: what it reads is there, and what the next loads replace is no longer read
-  auto turn = [&](int x, int next) __attribute__((always_inline)) {
-    wait_vmcnt<0>();
-    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the probabilities are written
-    __builtin_amdgcn_s_barrier();        // stage x has landed; the first wavefronts are done with x - 1, the second with x - 2
-    if (x + 1 < stages) issue(next);
-  };
-  // (a loop each, with the slot as a number: forms for every slot made the compiler copy the accumulators where they meet)
+  auto after = [](int slot) { return slot == kSlots - 1 ? 0 : slot + 1; };
+  int slot = 0;
+  turn(0);
   if (!second) {
-    int slot = 0;
-    for (int x = 0; x <= stages; ++x) {
-      const int next = slot == kSlots - 1 ? 0 : slot + 1;
-      turn(x, next);
-      if (x < stages && !nothing(x)) {
-        f32x16 sc;
-        products(sc, slot * STAGE_B);
-        f32x4 e[4];
+    // stage x: S(x); P(x); dV += P(x)^T dO(x)
+    less = ld_stat(0);
 #pragma unroll
-        for (int vg = 0; vg < 4; ++vg) e[vg] = *(const f32x4*)&stat[slot][8 * vg + 4 * hf];
-        float p[16];
+    for (int ks = 0; ks < NOP; ++ks) op[ks] = ld_row(ks, 0);
+    int y = y0;
+    Rows at_rows = rows_from(y0);
+    for (int x = 0; x < stages; ++x) {
+      const f32x16 s = product(slot);
+      float p[16];
 #pragma unroll
-        for (int v = 0; v < 16; ++v) p[v] = fast_exp2(__builtin_fmaf(sc[v], P.scale_log2e, -e[v >> 2][v & 3]));
-        const int first = m0 + 32 * x, a = (int)((unsigned)first / G), b = (int)((unsigned)min(first + 31, m1 - 1) / G);
-        const bool all = a >= kl && (b - ku < P.window || kl < P.sinks) && first + 32 <= m1;
-        if (!all) {
-          const int rest = first - a * (int)G;
+      for (int v = 0; v < 16; ++v) p[v] = fast_exp2(s[v] * P.scale_log2e);
+      const int left = m1 - m0 - 32 * y;  // rows that exist
+      const bool all = at_rows.first >= kl && (at_rows.last - ku < P.window || kl < P.sinks) && left >= 32;
+      if (!all) {
+        // Row r of the stage is (head + r) / G tokens behind the first, so it sees the key if lo <= r < hi without any division: (key - first) G <= head + r < (key - first + window) G
+        const int64_t behind = key - at_rows.first, until = key < P.sinks ? 64 : behind + P.window;
+        auto bound = [&](int64_t tokens) { return (int)max(min(tokens, (int64_t)64), (int64_t)-1) * P.G - at_rows.head - 4 * hf; };
+        int lo = bound(behind), hi = min(bound(until), left - 4 * hf);
+        asm volatile("" : "+v"(lo), "+v"(hi));  // (else the compiler keeps row numbers in registers around the loop)
 #pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            const int r = c_row(v, hf), tok = a + (int)(((float)(rest + r) + 0.5f) * inv_g);  // (exact: 1 / 2 is further from a multiple of G than the product is off)
-            if (first + r >= m1 || !sees(tok, key, P.window, P.sinks)) p[v] = 0.f;
-          }
-        }
-        bf16x8 w[2];
-#pragma unroll
-        for (int v = 0; v < 16; ++v) w[v >> 3][v & 7] = (bf16)p[v];
-#pragma unroll
-        for (int vg = 0; vg < 4; ++vg) *(f32x4*)&pbuf[slot][pair][(vg * 64 + lane) * 4] = f32x4{p[4 * vg], p[4 * vg + 1], p[4 * vg + 2], p[4 * vg + 3]};
-        add(w);
+        for (int v = 0; v < 16; ++v) p[v] = (c_row(v, 0) >= lo) & (c_row(v, 0) < hi) ? p[v] : 0.f;
       }
-      slot = next;
+      bf16x8 w[2];
+#pragma unroll
+      for (int v = 0; v < 16; ++v) w[v >> 3][v & 7] = (bf16)p[v];
+#pragma unroll
+      for (int vg = 0; vg < 4; ++vg) *(f32x4*)&pbuf[x & 1][pair][(vg * 64 + lane) * 4] = f32x4{p[4 * vg], p[4 * vg + 1], p[4 * vg + 2], p[4 * vg + 3]};
+      __builtin_amdgcn_sched_barrier(0);
+      slot = after(slot);
+      add(w, slot);
+      next_rows(at_rows);
+      if (++y == stages) {
+        y = 0;
+        at_rows = rows_from(0);
+      }
+      turn(x + 1);
     }
   } else {
-    int slot = 0, before = kSlots - 1;
-    for (int x = 0; x <= stages; ++x) {
-      const int next = slot == kSlots - 1 ? 0 : slot + 1;
-      turn(x, next);
-      if (x > 0 && !nothing(x - 1)) {
-        f32x16 dp;
-        products(dp, before * STAGE_B);
-        bf16x8 w[2];
+    // stage x: dK += dS(x - 2)^T Q(x - 2); dP(x - 1); dS(x - 1).  So its matrix instructions come while the other wavefront has its exponentials.
+    bf16x8 w[2] = {zero_bf16x8(), zero_bf16x8()};
 #pragma unroll
-        for (int vg = 0; vg < 4; ++vg) {
-          const f32x4 dr = *(const f32x4*)&stat[before][32 + 8 * vg + 4 * hf], p = *(const f32x4*)&pbuf[before][pair][(vg * 64 + lane) * 4];
+    for (int ks = 0; ks < NOP; ++ks) op[ks] = zero_bf16x8();
+    for (int x = 1; x <= stages; ++x) {
+      turn(x);
+      add(w, slot);
+      const f32x16 dp = product(slot);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) w[vg >> 1][4 * (vg & 1) + e] = (bf16)(p[e] * (dp[4 * vg + e] - dr[e]));
-        }
-        add(w);
+      for (int vg = 0; vg < 4; ++vg) {
+        const f32x4 p = *(const f32x4*)&pbuf[(x - 1) & 1][pair][(vg * 64 + lane) * 4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[vg >> 1][4 * (vg & 1) + e] = (bf16)(p[e] * dp[4 * vg + e]);
       }
-      before = slot;
-      slot = next;
+      slot = after(slot);
     }
+    add(w, 0);
   }
   wait_vmcnt<0>();
 
@@ -918,16 +947,25 @@ static WindowParams window_params(const Geo& g, const sb_problem* p, int32_t win
   return P;
 }
 
-// Far rows a far item takes: about as many as an ordinary item has, within limits that keep a long window's items short and a short one's few.
-static int far_rows_of(int window) { return window + kDkvKeys < 512 ? 512 : window + kDkvKeys > 4096 ? 4096 : window + kDkvKeys; }
-struct WindowWs { size_t lse2, dr, partials, bytes; int64_t far; };
+// Far rows a far item takes: short enough that a long sequence's sinks are many workgroups' work, and no more than 32 of them to a block of sinks, whose sums its own workgroup adds.
+static int far_rows_of(const int32_t* cu, int S, int window) {
+  int64_t most = 0;
+  for (int s = 0; s < S; ++s)
+    if (cu[s + 1] - cu[s] > most) most = cu[s + 1] - cu[s];
+  const int64_t rows = (most - window + 31) / 32;
+  return rows < 256 ? 256 : (int)((rows + 31) / 32 * 32);
+}
+struct WindowWs { size_t lse2, dr, stats, partials, bytes; int64_t far; int far_rows; };
 static WindowWs window_bwd_ws(const Geo& g, const int32_t* cu, int window, int sinks) {
   WindowWs w{};
   size_t o = 0;
-  w.lse2 = o; o = align_up(o + sizeof(float) * (size_t)g.T * g.Hq);
-  w.dr = o;   o = align_up(o + sizeof(float) * (size_t)g.T * g.Hq);
+  const size_t rows = (size_t)g.T * g.Hq, f32 = g.dtype == SB_F32 ? 1 : 0;
+  w.lse2 = o;  o = align_up(o + sizeof(float) * rows * f32);
+  w.dr = o;    o = align_up(o + sizeof(float) * rows * f32);
+  w.stats = o; o = align_up(o + 2 * sizeof(bf16x8) * rows * (1 - f32));
+  w.far_rows = far_rows_of(cu, g.S, window);
   if (g.dtype == SB_BF16)
-    for (int s = 0; s < g.S; ++s) w.far += far_items(cu[s + 1] - cu[s], window, sinks, far_rows_of(window));
+    for (int s = 0; s < g.S; ++s) w.far += far_items(cu[s + 1] - cu[s], window, sinks, w.far_rows);
   w.partials = o; o = align_up(o + (size_t)w.far * g.Hkv * 2 * kFarKeys * g.D * sizeof(float));
   w.bytes = o;
   return w;
@@ -977,8 +1015,9 @@ int sb_window_attn_bwd(const sb_problem* p, int32_t window, int32_t sinks, const
   const WindowWs w = window_bwd_ws(g, cu, window, sinks);
   P.lse2 = (float*)((char*)ws + w.lse2);
   P.dr = (float*)((char*)ws + w.dr);
+  P.stats = (bf16x8*)((char*)ws + w.stats);
   P.partials = (float*)((char*)ws + w.partials);
-  P.far_rows = far_rows_of(window);
+  P.far_rows = w.far_rows;
   const bool f32 = g.dtype == SB_F32;
   const int64_t rows = (int64_t)g.T * g.Hq, per = 1024 / g.D;
   const int64_t q_items = row_tiles(cu, g.S, g.G, f32 ? 32 : 256) * g.Hkv, k_items = row_tiles(cu, g.S, 1, f32 ? 32 : kDkvKeys) * g.Hkv;
