@@ -305,32 +305,71 @@ def sb_sab_batches(tab: PerfTable, lengths, k_pred, dp_size, dp_rank, num_microb
 
 
 # ------------------------------------------------------------------ rotary positions, window attention, paged cache
+# A call of a serving step takes the GPU a few microseconds, so what the binding takes counts: a tensor is checked by one expression (and looked at again for the message
+# if that fails), addresses go to the library as plain integers, and device and stream are asked for once a call.
 SB_ROPE_HALF, SB_ROPE_INTERLEAVED = 0, 1
 SB_ROPE_PLAIN, SB_ROPE_LINEAR, SB_ROPE_NTK, SB_ROPE_YARN, SB_ROPE_BANDS = range(5)
 _TORCH_DTYPE = {SB_BF16: torch.bfloat16, SB_F32: torch.float32}
 
 
-def _tensor(name, t, shape, dtype, pitch=False):
-    """Refuses a tensor that the library could not use as it lies in memory.  pitch: tokens may be further apart than their elements."""
+def _operator_calls():
+    """{name: function} of the calls below, their argument types set."""
+    global _calls
+    if _calls is None:
+        P, I, L = C.c_void_p, C.c_int32, C.c_int64
+        types = {"sb_rope_apply": [P, P, P, P, L, P, L, P, P, I, P], "sb_window_attn_fwd": [P, I, I] + [P] * 7, "sb_window_attn_bwd": [P, I, I] + [P] * 11,
+                 "sb_cache_append": [P, P, P, P, L, P, L, P, L, P, P], "sb_cache_attn": [P, P, I, I] + [P] * 5}
+        _calls = {}
+        for name, args in types.items():
+            _calls[name] = C.CFUNCTYPE(C.c_int, *args)((name, lib()))  # (a function object of its own: those of `lib()` keep taking what ctypes makes of their arguments)
+    return _calls
+
+
+_calls = None
+
+
+def _here():
+    """(current device, its current stream)"""
+    try:
+        device = torch.cuda.current_device()
+    except RuntimeError:
+        return -2, 0  # no GPU: no tensor lies on the device, and each is refused
+    return device, torch._C._cuda_getCurrentRawStream(device)
+
+
+def _tensor(name, t, shape, dtype, device, pitch=False):
+    """Refuses a tensor that the library could not use as it lies in memory.  pitch: tokens [T][H][D] may be further apart than their elements."""
+    if isinstance(t, torch.Tensor) and t.get_device() == device and t.dtype is dtype and t.shape == shape:
+        if t.is_contiguous():
+            return
+        if pitch:
+            token, head, element = t.stride()
+            if element == 1 and (head == shape[2] or shape[1] == 1) and (shape[0] == 1 or token >= shape[1] * shape[2]):
+                return
     def need(ok, what):
         if not ok:
             raise SparseBalError(f"{name}: {what}")
     need(isinstance(t, torch.Tensor) and t.is_cuda, "a GPU tensor is needed")
-    need(t.device.index == torch.cuda.current_device(), f"lies on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-    need(t.dtype == dtype, f"{t.dtype} given, {dtype} needed")
-    need(tuple(t.shape) == tuple(shape), f"shape {tuple(t.shape)} given, {tuple(shape)} needed")
-    if not pitch:
-        need(t.is_contiguous(), "must be contiguous")
-    elif t.numel():
-        need(t[0].is_contiguous() and (t.shape[0] == 1 or t.stride(0) >= t[0].numel()), "a token's heads must be contiguous, and tokens in order")
+    need(t.get_device() == device, f"lies on {t.device}, the current device is cuda:{device}")
+    need(t.dtype is dtype, f"{t.dtype} given, {dtype} needed")
+    need(t.shape == shape, f"shape {tuple(t.shape)} given, {tuple(shape)} needed")
+    need(False, "a token's heads must be contiguous, and tokens in order" if pitch else "must be contiguous")
 
 
 def _pitch(t):
-    return C.c_int64(t.stride(0) if t is not None and t.shape[0] > 1 else 0)
+    return 0 if t is None or t.shape[0] < 2 else t.stride(0)
 
 
 def _address(t):
-    return None if t is None else C.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
+
+
+def _workspace(ws, need, device):
+    if ws is None:
+        return _bytes(need, torch.device("cuda", device)) if need else None
+    if ws.get_device() != device or not ws.is_contiguous() or ws.numel() * ws.element_size() < need:
+        raise SparseBalError(f"ws: {need} contiguous bytes on cuda:{device} are needed")
+    return ws
 
 
 class Rope:
@@ -348,23 +387,26 @@ class Rope:
 def sb_rope_apply(pb: Problem, rope: Rope, q, k, positions=None, backward=False, q_out=None, k_out=None):
     """(q, k) turned by their positions (the tokens' indices in their sequences, or `positions`), or gradients turned back.  q and k may
     be slices of a fused projection; either may be None.  q_out, k_out may be q and k where these are contiguous."""
-    dt = _TORCH_DTYPE[pb.dtype]
-    out = []
-    for name, x, y, heads in (("q", q, q_out, pb.Hq), ("k", k, k_out, pb.Hkv)):
-        shape = (pb.T, heads, pb.D)
-        if x is None:
-            out.append(None)
-            continue
-        _tensor(name, x, shape, dt, pitch=True)
-        if y is None:
-            y = torch.empty(shape, dtype=dt, device=x.device)
-        _tensor(name + "_out", y, shape, dt)
-        out.append(y)
+    dt, (device, stream) = _TORCH_DTYPE[pb.dtype], _here()
+    if q is not None:
+        shape = (pb.T, pb.Hq, pb.D)
+        _tensor("q", q, shape, dt, device, pitch=True)
+        if q_out is None:
+            q_out = torch.empty(shape, dtype=dt, device=q.device)
+        else:
+            _tensor("q_out", q_out, shape, dt, device)
+    if k is not None:
+        shape = (pb.T, pb.Hkv, pb.D)
+        _tensor("k", k, shape, dt, device, pitch=True)
+        if k_out is None:
+            k_out = torch.empty(shape, dtype=dt, device=k.device)
+        else:
+            _tensor("k_out", k_out, shape, dt, device)
     if positions is not None:
-        _tensor("positions", positions, (pb.T,), torch.int32)
-    _check(lib().sb_rope_apply(pb.ref(), rope.ref(), _address(positions), _address(q), _pitch(q), _address(k), _pitch(k), _address(out[0]), _address(out[1]),
-                               1 if backward else 0, _stream()))
-    return out[0], out[1]
+        _tensor("positions", positions, (pb.T,), torch.int32, device)
+    _check(_operator_calls()["sb_rope_apply"](C.addressof(pb.c), C.addressof(rope.c), _address(positions), _address(q), _pitch(q), _address(k), _pitch(k), _address(q_out),
+                                              _address(k_out), 1 if backward else 0, stream))
+    return q_out, k_out
 
 
 def sb_window_ws_bytes(pb: Problem, window, sinks):
@@ -374,40 +416,41 @@ def sb_window_ws_bytes(pb: Problem, window, sinks):
     return f.value, b.value
 
 
-def _window_ws(ws, need, device):
-    if ws is None:
-        return _bytes(need, device)
-    if ws.device != device or not ws.is_contiguous() or ws.numel() * ws.element_size() < need:
-        raise SparseBalError(f"ws: {need} contiguous bytes on {device} are needed")
-    return ws
-
-
 def sb_window_attn_fwd(pb: Problem, window, sinks, q, k, v, o=None, lse=None, ws=None):
     """Attention with a sliding window and sinks; pb's budgets and blocks are not read.  Returns (o, lse)."""
-    dt = _TORCH_DTYPE[pb.dtype]
-    for name, x, heads in (("q", q, pb.Hq), ("k", k, pb.Hkv), ("v", v, pb.Hkv)):
-        _tensor(name, x, (pb.T, heads, pb.D), dt)
-    o = o if o is not None else torch.empty_like(q)
-    lse = lse if lse is not None else torch.empty((pb.Hq, pb.T), dtype=torch.float32, device=q.device)
-    _tensor("o", o, q.shape, dt)
-    _tensor("lse", lse, (pb.Hq, pb.T), torch.float32)
-    ws = _window_ws(ws, sb_window_ws_bytes(pb, window, sinks)[0], q.device)
-    _check(lib().sb_window_attn_fwd(pb.ref(), int(window), int(sinks), _address(q), _address(k), _address(v), _address(o), _address(lse), _address(ws), _stream()))
+    dt, (device, stream) = _TORCH_DTYPE[pb.dtype], _here()
+    queries, keys, rows = (pb.T, pb.Hq, pb.D), (pb.T, pb.Hkv, pb.D), (pb.Hq, pb.T)
+    _tensor("q", q, queries, dt, device)
+    _tensor("k", k, keys, dt, device)
+    _tensor("v", v, keys, dt, device)
+    if o is None:
+        o = torch.empty_like(q)
+    else:
+        _tensor("o", o, queries, dt, device)
+    if lse is None:
+        lse = torch.empty(rows, dtype=torch.float32, device=q.device)
+    else:
+        _tensor("lse", lse, rows, torch.float32, device)
+    ws = _workspace(ws, sb_window_ws_bytes(pb, window, sinks)[0], device)
+    _check(_operator_calls()["sb_window_attn_fwd"](C.addressof(pb.c), window, sinks, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), _address(ws),
+                                                   stream))
     return o, lse
 
 
 def sb_window_attn_bwd(pb: Problem, window, sinks, q, k, v, o, lse, d_o, dq=None, dk=None, dv=None, ws=None):
-    dt = _TORCH_DTYPE[pb.dtype]
+    dt, (device, stream) = _TORCH_DTYPE[pb.dtype], _here()
+    queries, keys = (pb.T, pb.Hq, pb.D), (pb.T, pb.Hkv, pb.D)
+    for name, x, shape in (("q", q, queries), ("k", k, keys), ("v", v, keys), ("o", o, queries), ("d_o", d_o, queries)):
+        _tensor(name, x, shape, dt, device)
+    _tensor("lse", lse, (pb.Hq, pb.T), torch.float32, device)
     dq = dq if dq is not None else torch.empty_like(q)
     dk = dk if dk is not None else torch.empty_like(k)
     dv = dv if dv is not None else torch.empty_like(v)
-    for name, x, heads in (("q", q, pb.Hq), ("k", k, pb.Hkv), ("v", v, pb.Hkv), ("o", o, pb.Hq), ("d_o", d_o, pb.Hq), ("dq", dq, pb.Hq), ("dk", dk, pb.Hkv),
-                           ("dv", dv, pb.Hkv)):
-        _tensor(name, x, (pb.T, heads, pb.D), dt)
-    _tensor("lse", lse, (pb.Hq, pb.T), torch.float32)
-    ws = _window_ws(ws, sb_window_ws_bytes(pb, window, sinks)[1], q.device)
-    _check(lib().sb_window_attn_bwd(pb.ref(), int(window), int(sinks), _address(q), _address(k), _address(v), _address(o), _address(lse), _address(d_o),
-                                    _address(dq), _address(dk), _address(dv), _address(ws), _stream()))
+    for name, x, shape in (("dq", dq, queries), ("dk", dk, keys), ("dv", dv, keys)):
+        _tensor(name, x, shape, dt, device)
+    ws = _workspace(ws, sb_window_ws_bytes(pb, window, sinks)[1], device)
+    _check(_operator_calls()["sb_window_attn_bwd"](C.addressof(pb.c), window, sinks, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
+                                                   d_o.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _address(ws), stream))
     return dq, dk, dv
 
 
@@ -419,9 +462,10 @@ class Cache:
             raise SparseBalError("k: [pages][KV heads][tokens of a page][head_dim] in bfloat16 or float32 is needed")
         if page_table.dim() != 2:
             raise SparseBalError("page_table: [sequences][pages] is needed")
-        _tensor("k", k, k.shape, k.dtype)
-        _tensor("v", v, k.shape, k.dtype)
-        _tensor("page_table", page_table, page_table.shape, torch.int32)
+        device = _here()[0]
+        _tensor("k", k, k.shape, k.dtype, device)
+        _tensor("v", v, k.shape, k.dtype, device)
+        _tensor("page_table", page_table, page_table.shape, torch.int32, device)
         self.k, self.v, self.page_table = k, v, page_table
         self.c = sb_cache(k.shape[0], k.shape[2], k.shape[1], k.shape[3], SB_F32 if k.dtype == torch.float32 else SB_BF16, page_table.shape[1],
                           k.data_ptr(), v.data_ptr(), page_table.data_ptr())
@@ -434,9 +478,9 @@ class Chunk:
     """Holds sb_chunk plus the tensors it points to: the new tokens of every sequence.  Sizes on the host are bounds (see sb_chunk); the tensors may change between calls."""
 
     def __init__(self, cu_new, cached, Hq, total_new, max_new, max_length, softmax_scale=0.0):
-        S = cu_new.shape[0] - 1
-        _tensor("cu_new", cu_new, (max(S, 0) + 1,), torch.int32)
-        _tensor("cached", cached, (S,), torch.int32)
+        S, device = cached.shape[0], _here()[0]
+        _tensor("cu_new", cu_new, (S + 1,), torch.int32, device)
+        _tensor("cached", cached, (S,), torch.int32, device)
         self.cu_new, self.cached, self.Hq, self.total_new = cu_new, cached, int(Hq), int(total_new)
         self.c = sb_chunk(S, int(Hq), int(total_new), int(max_new), int(max_length), float(softmax_scale), cu_new.data_ptr(), cached.data_ptr())
 
@@ -452,18 +496,20 @@ def _same_sequences(cache, chunk):
 def sb_cache_append(cache: Cache, chunk: Chunk, k, v, rope: Rope = None, q=None, q_out=None):
     """New tokens' k (turned) and v into their pages; returns q turned likewise (None without q)."""
     _same_sequences(cache, chunk)
-    n, D, Hkv = chunk.total_new, cache.c.head_dim, cache.c.num_kv_heads
-    _tensor("k", k, (n, Hkv, D), cache.k.dtype, pitch=True)
-    _tensor("v", v, (n, Hkv, D), cache.k.dtype, pitch=True)
+    n, D, dt, (device, stream) = chunk.total_new, cache.c.head_dim, cache.k.dtype, _here()
+    keys, queries = (n, cache.c.num_kv_heads, D), (n, chunk.Hq, D)
+    _tensor("k", k, keys, dt, device, pitch=True)
+    _tensor("v", v, keys, dt, device, pitch=True)
     if q is not None:
-        _tensor("q", q, (n, chunk.Hq, D), cache.k.dtype, pitch=True)
+        _tensor("q", q, queries, dt, device, pitch=True)
         if q_out is None:
-            q_out = torch.empty((n, chunk.Hq, D), dtype=q.dtype, device=q.device)
-        _tensor("q_out", q_out, (n, chunk.Hq, D), cache.k.dtype)
+            q_out = torch.empty(queries, dtype=dt, device=q.device)
+        else:
+            _tensor("q_out", q_out, queries, dt, device)
     elif q_out is not None:
         raise SparseBalError("q_out without q")
-    _check(lib().sb_cache_append(cache.ref(), chunk.ref(), rope.ref() if rope is not None else None, _address(q), _pitch(q), _address(k), _pitch(k), _address(v),
-                                 _pitch(v), _address(q_out), _stream()))
+    _check(_operator_calls()["sb_cache_append"](C.addressof(cache.c), C.addressof(chunk.c), C.addressof(rope.c) if rope is not None else None, _address(q), _pitch(q),
+                                                k.data_ptr(), _pitch(k), v.data_ptr(), _pitch(v), _address(q_out), stream))
     return q_out
 
 
@@ -476,14 +522,19 @@ def sb_cache_attn_ws_bytes(cache: Cache, chunk: Chunk, window, sinks) -> int:
 def sb_cache_attn(cache: Cache, chunk: Chunk, q, window=2 ** 31 - 1, sinks=0, o=None, lse=None, ws=None):
     """Attention of the new tokens over the cache, which holds them already.  Returns (o, lse)."""
     _same_sequences(cache, chunk)
-    shape = (chunk.total_new, chunk.Hq, cache.c.head_dim)
-    _tensor("q", q, shape, cache.k.dtype)
-    o = o if o is not None else torch.empty_like(q)
-    lse = lse if lse is not None else torch.empty((chunk.Hq, chunk.total_new), dtype=torch.float32, device=q.device)
-    _tensor("o", o, shape, cache.k.dtype)
-    _tensor("lse", lse, (chunk.Hq, chunk.total_new), torch.float32)
-    ws = _window_ws(ws, sb_cache_attn_ws_bytes(cache, chunk, window, sinks), q.device)
-    _check(lib().sb_cache_attn(cache.ref(), chunk.ref(), int(window), int(sinks), _address(q), _address(o), _address(lse), _address(ws), _stream()))
+    dt, (device, stream) = cache.k.dtype, _here()
+    queries, rows = (chunk.total_new, chunk.Hq, cache.c.head_dim), (chunk.Hq, chunk.total_new)
+    _tensor("q", q, queries, dt, device)
+    if o is None:
+        o = torch.empty_like(q)
+    else:
+        _tensor("o", o, queries, dt, device)
+    if lse is None:
+        lse = torch.empty(rows, dtype=torch.float32, device=q.device)
+    else:
+        _tensor("lse", lse, rows, torch.float32, device)
+    ws = _workspace(ws, sb_cache_attn_ws_bytes(cache, chunk, window, sinks), device)
+    _check(_operator_calls()["sb_cache_attn"](C.addressof(cache.c), C.addressof(chunk.c), window, sinks, q.data_ptr(), o.data_ptr(), lse.data_ptr(), _address(ws), stream))
     return o, lse
 
 

@@ -321,7 +321,7 @@ static CachePlan plan_cache(const sb_cache* c, const sb_chunk* n, int window, in
   const bool f32 = c->dtype == SB_F32;
   // Two workgroups a CU; a strip for each wavefront at least, and 1024 keys at most, so that sequences of unequal lengths even out.
   if (!f32 && (S > 1 || most <= kFewRows)) p.few = launch(most < kFewRows ? most : kFewRows, kSplitRows, 32, 512, 4, 32);
-  // A workgroup (float32: four items) a CU, of 8 tiles at least.
+  // A workgroup a CU (float32, where one takes 32 rows: four), of 8 tiles at least.
   if (f32 || most > kFewRows) p.many = launch(most, forward_rows(c->dtype), f32 ? 32 : 64, f32 ? 1024 : 256, 8, 1 << 30);
   const size_t splits = (size_t)(p.few.splits > p.many.splits ? p.few.splits : p.many.splits), all = (size_t)n->total_new * n->num_q_heads;
   if (splits > 1) {

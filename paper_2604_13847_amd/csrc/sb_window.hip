@@ -14,8 +14,8 @@
 namespace sb {
 
 // ---------------------------------------------------------------------------------------------
-// float32 arithmetic throughout: v_mfma_f32_32x32x2_f32, operands straight from memory.  One wavefront owns 32 rows (or 32 keys)
-// and walks strips of 32 keys (rows).  Operand layout per lane: A row / B column = lane%32, contraction slot = lane/32.
+// float32 arithmetic throughout: v_mfma_f32_32x32x2_f32, operands straight from memory.  A workgroup owns 32 rows (or 32 keys) and walks strips of 32 keys (rows), every
+// fourth strip a wavefront's; the wavefronts' sums are added in order at the end.  Operand layout per lane: A row / B column = lane%32, contraction slot = lane/32.
 __device__ inline f32x16 mfma_f32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
 
 __device__ inline f32x4 load4(const float* p) { return *(const f32x4*)p; }
@@ -33,10 +33,16 @@ __device__ inline void store4(bf16* p, f32x4 x) {
 
 // A row of D elements as an operand of a product over d: step x covers d = 8x .. 8x + 7, four instructions with slot hf at 8x + 4hf + j.
 template <int D> struct RowOperand { f32x4 x[D / 8]; };
+// A row that is null counts as zeros; `any`, some row that may be read, stands in for it, so that no load is behind a branch and all are on their way together.
 template <int D, typename T>
-__device__ inline void load_row(RowOperand<D>& r, const T* row, int hf) {
+__device__ inline void load_row(RowOperand<D>& r, const T* row, const T* any, int hf) {
+  const T* const from = row ? row : any;
 #pragma unroll
-  for (int x = 0; x < D / 8; ++x) r.x[x] = row ? load4(row + 8 * x + 4 * hf) : f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int x = 0; x < D / 8; ++x) r.x[x] = load4(from + 8 * x + 4 * hf);
+  if (!row) {
+#pragma unroll
+    for (int x = 0; x < D / 8; ++x) r.x[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
 }
 template <int D>
 __device__ inline f32x16 dot_rows(const RowOperand<D>& a, const RowOperand<D>& b) {
@@ -49,12 +55,22 @@ __device__ inline f32x16 dot_rows(const RowOperand<D>& a, const RowOperand<D>& b
 }
 // acc[dt] += X^T w over 32 rows of X, row c_row(v, hf) with weight w[v]; row(r) is a row's address or null
 template <int D, typename T, typename F>
-__device__ inline void add_rows(f32x16 (&acc)[D / 32], const float (&w)[16], int l32, int hf, F row) {
+__device__ inline void add_rows(f32x16 (&acc)[D / 32], const float (&w)[16], const T* any, int l32, int hf, F row) {
 #pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    const T* x = row(c_row(v, hf));
+  for (int v0 = 0; v0 < 16; v0 += 8) {
+    T x[8][D / 32];
+    bool there[8];
 #pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt) acc[dt] = mfma_f32(x ? (float)x[32 * dt + l32] : 0.f, w[v], acc[dt]);
+    for (int v = 0; v < 8; ++v) {
+      const T* const r = row(c_row(v0 + v, hf));
+      there[v] = r != nullptr;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) x[v][dt] = (r ? r : any)[32 * dt + l32];
+    }
+#pragma unroll
+    for (int v = 0; v < 8; ++v)
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) acc[dt] = mfma_f32(there[v] ? (float)x[v][dt] : 0.f, w[v0 + v], acc[dt]);
   }
 }
 template <int D, typename T>
@@ -85,11 +101,19 @@ struct Keys {
   __device__ inline const T* v(int u) const { const int64_t o = offset(u); return o < 0 ? nullptr : (const T*)(PAGED ? P.cache.v : P.v) + o; }
 };
 
+// The other wavefronts' registers for the first one
+template <int N>
+struct Sums {
+  float x[3][N][64];
+  __device__ inline void put(int wave, int i, int lane, float v) { if (wave > 0) x[wave - 1][i][lane] = v; }
+};
+
 template <typename T, int D, bool PAGED>
-__global__ __launch_bounds__(256) void window_fwd_f32_kernel(WindowParams P, int64_t items) {
+__global__ __launch_bounds__(256) void window_fwd_f32_kernel(WindowParams P) {
+  constexpr int NR = 16 * (D / 32);
+  __shared__ Sums<NR + 2> sums;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
-  const int64_t item = (int64_t)blockIdx.x * 4 + wave;
-  if (item >= items) return;
+  const unsigned item = blockIdx.x;
   const int splits = PAGED ? P.splits : 1, z = (int)(item / P.Hkv % splits);
   const RowTile t = locate_tile<32, PAGED>(P, item / P.Hkv / splits);
   if (t.s < 0) return;
@@ -99,7 +123,8 @@ __global__ __launch_bounds__(256) void window_fwd_f32_kernel(WindowParams P, int
   const int ta = t.pos0 + (int)(m0 / P.G), tb = t.pos0 + (int)(min(m0 + 31, rows - 1) / P.G), pos = t.pos0 + i;
   const int64_t at = ((int64_t)(t.row0 + i) * P.Hq + h) * D;
   RowOperand<D> qr, kr;
-  load_row<D>(qr, (const T*)P.q + at, hf);
+  const T* const any = (const T*)P.q + at;
+  load_row<D>(qr, any, any, hf);
   const int last = PAGED ? min(tb, P.cache.max_pages * P.cache.page_size - 1) : tb;
   const KeyTiles<32> tiles(ta, last, P.window, P.sinks);
   const Keys<T, D, PAGED> keys{P, t, g, max(0, ta - P.window + 1), last + 1};
@@ -109,10 +134,10 @@ __global__ __launch_bounds__(256) void window_fwd_f32_kernel(WindowParams P, int
   float top = -__builtin_inff(), l = 0.f;  // largest score seen (in units of log 2), sum of exponentials
   const int x0 = PAGED ? (int)min((int64_t)z * P.per_split, (int64_t)tiles.count()) : 0;
   const int x1 = PAGED && z < splits - 1 ? min(x0 + P.per_split, tiles.count()) : tiles.count();
-  for (int x = x0; x < x1; ++x) {
+  for (int x = x0 + wave; x < x1; x += 4) {
     const int u0 = 32 * tiles.at(x);
     const T* kp = keys.k(u0 + l32);
-    load_row<D>(kr, kp, hf);
+    load_row<D>(kr, kp, any, hf);
     f32x16 sc = dot_rows<D>(kr, qr);
     const unsigned exists = (unsigned)__builtin_amdgcn_ballot_w64(kp != nullptr);
     float mx = -__builtin_inff(), p[16];
@@ -136,9 +161,36 @@ __global__ __launch_bounds__(256) void window_fwd_f32_kernel(WindowParams P, int
       p[v] = fast_exp2(p[v] - ref);
       l += p[v];
     }
-    add_rows<D, T>(acc, p, l32, hf, [&](int r) { return keys.v(u0 + r); });
+    add_rows<D, T>(acc, p, any, l32, hf, [&](int r) { return keys.v(u0 + r); });
   }
   l += __shfl_xor(l, 32, 64);
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) sums.put(wave, 16 * dt + v, lane, acc[dt][v]);
+  sums.put(wave, NR, lane, top);
+  sums.put(wave, NR + 1, lane, l);
+  __syncthreads();
+  if (wave > 0) return;
+  float best = top;
+#pragma unroll
+  for (int w = 0; w < 3; ++w) best = fmaxf(best, sums.x[w][NR][lane]);
+  const float ref = best == -__builtin_inff() ? 0.f : best, f0 = fast_exp2(top - ref);
+  l *= f0;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[dt][v] *= f0;
+#pragma unroll
+  for (int w = 0; w < 3; ++w) {
+    const float f = fast_exp2(sums.x[w][NR][lane] - ref);
+    l += f * sums.x[w][NR + 1][lane];
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[dt][v] = __builtin_fmaf(f, sums.x[w][16 * dt + v][lane], acc[dt][v]);
+  }
+  top = best;
   if (m0 + l32 >= rows) return;
   if (splits > 1) {
     if (l != 0.f) store_column<D>(P.part_o + (int64_t)z * P.T * P.Hq * D + at, acc, 1.0f / l, hf);
@@ -169,10 +221,10 @@ __global__ __launch_bounds__(256) void window_delta_kernel(WindowParams P, int64
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(256) void window_dq_f32_kernel(WindowParams P, int64_t items) {
+__global__ __launch_bounds__(256) void window_dq_f32_kernel(WindowParams P) {
+  __shared__ Sums<16 * (D / 32)> sums;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
-  const int64_t item = (int64_t)blockIdx.x * 4 + wave;
-  if (item >= items) return;
+  const unsigned item = blockIdx.x;
   const RowTile t = locate_tile<32, false>(P, item / P.Hkv);
   if (t.s < 0) return;
   const int g = (int)(item % P.Hkv);
@@ -181,61 +233,75 @@ __global__ __launch_bounds__(256) void window_dq_f32_kernel(WindowParams P, int6
   const int ta = (int)(m0 / P.G), tb = (int)(min(m0 + 31, rows - 1) / P.G);
   const int64_t at = ((int64_t)(t.row0 + i) * P.Hq + h) * D;
   RowOperand<D> qr, dor, x;
-  load_row<D>(qr, (const T*)P.q + at, hf);
-  load_row<D>(dor, (const T*)P.d_o + at, hf);
+  const T* const any = (const T*)P.q + at;
+  load_row<D>(qr, any, any, hf);
+  load_row<D>(dor, (const T*)P.d_o + at, any, hf);
   const float lse2 = P.lse2[at / D], dr = P.dr[at / D];
   const KeyTiles<32> tiles(ta, tb, P.window, P.sinks);
   const Keys<T, D, false> keys{P, t, g, max(0, ta - P.window + 1), tb + 1};
   f32x16 acc[D / 32];
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zero16();
-  for (int y = 0; y < tiles.count(); ++y) {
+  for (int y = wave; y < tiles.count(); y += 4) {
     const int u0 = 32 * tiles.at(y);
-    load_row<D>(x, keys.k(u0 + l32), hf);
+    load_row<D>(x, keys.k(u0 + l32), any, hf);
     const f32x16 sc = dot_rows<D>(x, qr);
-    load_row<D>(x, keys.v(u0 + l32), hf);
+    load_row<D>(x, keys.v(u0 + l32), any, hf);
     const f32x16 dp = dot_rows<D>(x, dor);
     float ds[16];
 #pragma unroll
     for (int v = 0; v < 16; ++v)
       ds[v] = sees(i, u0 + c_row(v, hf), P.window, P.sinks) ? fast_exp2(__builtin_fmaf(sc[v], P.scale_log2e, -lse2)) * (dp[v] - dr) : 0.f;
-    add_rows<D, T>(acc, ds, l32, hf, [&](int r) { return keys.k(u0 + r); });
+    add_rows<D, T>(acc, ds, any, l32, hf, [&](int r) { return keys.k(u0 + r); });
   }
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) sums.put(wave, 16 * dt + v, lane, acc[dt][v]);
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int w = 0; w < 3; ++w)
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[dt][v] += sums.x[w][16 * dt + v][lane];
   if (m0 + l32 < rows) store_column<D>((T*)P.dq + at, acc, P.scale, hf);
 }
 
-// Key-major: one wavefront owns 32 keys of a KV head and walks the flattened rows that see any of them, 32 at a time, in order.
+// Key-major: a workgroup owns 32 keys of a KV head and walks the flattened rows that see any of them, 32 at a time, every fourth 32 a wavefront's; the four sums are added in order.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void window_dkv_f32_kernel(WindowParams P, int64_t items) {
+__global__ __launch_bounds__(256) void window_dkv_f32_kernel(WindowParams P) {
+  constexpr int NR = 16 * (D / 32);
+  __shared__ Sums<2 * NR> sums;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
-  const int64_t item = (int64_t)blockIdx.x * 4 + wave;
-  if (item >= items) return;
   WindowParams one = P;  // tiles of 32 keys: one row a token
   one.G = 1;
-  const RowTile t = locate_tile<32, false>(one, item / P.Hkv);
+  const RowTile t = locate_tile<32, false>(one, blockIdx.x / (unsigned)P.Hkv);
   if (t.s < 0) return;
-  const int g = (int)(item % P.Hkv);
+  const int g = (int)(blockIdx.x % (unsigned)P.Hkv);
   const int u0 = t.tile * 32, u = min(u0 + l32, t.n - 1), last = min(u0 + 31, t.n - 1);
   const int64_t at = ((int64_t)(t.row0 + u) * P.Hkv + g) * D;
+  const T* const any = (const T*)P.k + at;
   RowOperand<D> kr, vr, x;
-  load_row<D>(kr, (const T*)P.k + at, hf);
-  load_row<D>(vr, (const T*)P.v + at, hf);
+  load_row<D>(kr, any, any, hf);
+  load_row<D>(vr, (const T*)P.v + at, any, hf);
   f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt) dk[dt] = dv[dt] = zero16();
-  const int64_t behind = u0 < P.sinks ? t.n : min((int64_t)t.n, (int64_t)last + P.window);  // the first token that sees none of them
-  const int64_t end = behind * P.G;
-  auto row = [&](int64_t m) { return ((int64_t)(t.row0 + (int)(m / P.G)) * P.Hq + g * P.G + (int)(m % P.G)) * D; };
-  for (int64_t m0 = (int64_t)u0 * P.G; m0 < end; m0 += 32) {
-    const bool there = m0 + l32 < end;
-    load_row<D>(x, there ? (const T*)P.q + row(m0 + l32) : nullptr, hf);
+  const int behind = u0 < P.sinks || t.n - last <= P.window ? t.n : last + P.window;  // the first token that sees none of them
+  const int end = behind * P.G;
+  auto row = [&](int m) { const int tok = (int)((unsigned)m / (unsigned)P.G); return (int64_t)(t.row0 + tok) * P.Hq + g * P.G + m - tok * P.G; };
+  for (int m0 = u0 * P.G + 32 * wave; m0 < end; m0 += 128) {
+    const int m = min(m0 + l32, end - 1);
+    const int64_t mine = row(m);
+    load_row<D>(x, (const T*)P.q + mine * D, any, hf);
     const f32x16 sc = dot_rows<D>(x, kr);
-    load_row<D>(x, there ? (const T*)P.d_o + row(m0 + l32) : nullptr, hf);
+    load_row<D>(x, (const T*)P.d_o + mine * D, any, hf);
     const f32x16 dp = dot_rows<D>(x, vr);
     // statistics of row m0 + lane%32, passed on to the lanes that hold the row
-    const int64_t m = there ? m0 + l32 : end - 1;
-    const float lse2 = P.lse2[row(m) / D], dr = P.dr[row(m) / D];
-    const int pos = there ? (int)(m / P.G) : -1;
+    const float lse2 = P.lse2[mine], dr = P.dr[mine];
+    const int pos = m0 + l32 < end ? (int)((unsigned)m / (unsigned)P.G) : -1;
     float p[16], ds[16];
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
@@ -246,9 +312,27 @@ __global__ __launch_bounds__(256) void window_dkv_f32_kernel(WindowParams P, int
       p[v] = seen ? fast_exp2(__builtin_fmaf(sc[v], P.scale_log2e, -e)) : 0.f;
       ds[v] = seen ? p[v] * (dp[v] - d) : 0.f;
     }
-    add_rows<D, T>(dv, p, l32, hf, [&](int r) { return m0 + r < end ? (const T*)P.d_o + row(m0 + r) : nullptr; });
-    add_rows<D, T>(dk, ds, l32, hf, [&](int r) { return m0 + r < end ? (const T*)P.q + row(m0 + r) : nullptr; });
+    add_rows<D, T>(dv, p, any, l32, hf, [&](int r) { return m0 + r < end ? (const T*)P.d_o + row(m0 + r) * D : nullptr; });
+    add_rows<D, T>(dk, ds, any, l32, hf, [&](int r) { return m0 + r < end ? (const T*)P.q + row(m0 + r) * D : nullptr; });
   }
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      sums.put(wave, 16 * dt + v, lane, dk[dt][v]);
+      sums.put(wave, NR + 16 * dt + v, lane, dv[dt][v]);
+    }
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int w = 0; w < 3; ++w)
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        dk[dt][v] += sums.x[w][16 * dt + v][lane];
+        dv[dt][v] += sums.x[w][NR + 16 * dt + v][lane];
+      }
   if (u0 + l32 < t.n) {
     store_column<D>((T*)P.dk + at, dk, P.scale, hf);
     store_column<D>((T*)P.dv + at, dv, 1.0f, hf);
@@ -918,12 +1002,12 @@ int grid_of(int64_t workgroups, dim3* grid) {
 int launch_window_fwd(const WindowParams& P, int D, int dtype, bool paged, int64_t tiles, hipStream_t st) {
   const int64_t items = tiles * P.Hkv * (paged ? P.splits : 1);
   dim3 grid;
-  const int rc = grid_of(dtype == SB_F32 ? (items + 3) / 4 : items, &grid);
+  const int rc = grid_of(items, &grid);
   if (rc != SB_OK) return rc;
   auto launch = [&](auto d, auto pg) {
     constexpr int DD = decltype(d)::value;
     constexpr bool PAGED = decltype(pg)::value;
-    if (dtype == SB_F32) hipLaunchKernelGGL((window_fwd_f32_kernel<float, DD, PAGED>), grid, dim3(256), 0, st, P, items);
+    if (dtype == SB_F32) hipLaunchKernelGGL((window_fwd_f32_kernel<float, DD, PAGED>), grid, dim3(256), 0, st, P);
     else hipLaunchKernelGGL((window_fwd_kernel<DD, PAGED>), grid, dim3(512), 0, st, P);
   };
   auto with_d = [&](auto pg) { if (D == 128) launch(std::integral_constant<int, 128>(), pg); else launch(std::integral_constant<int, 64>(), pg); };
@@ -1022,8 +1106,8 @@ int sb_window_attn_bwd(const sb_problem* p, int32_t window, int32_t sinks, const
   const int64_t rows = (int64_t)g.T * g.Hq, per = 1024 / g.D;
   const int64_t q_items = row_tiles(cu, g.S, g.G, f32 ? 32 : 256) * g.Hkv, k_items = row_tiles(cu, g.S, 1, f32 ? 32 : kDkvKeys) * g.Hkv;
   dim3 delta_grid, q_grid, k_grid, far_grid;
-  if ((rc = grid_of((rows + per - 1) / per, &delta_grid)) != SB_OK || (rc = grid_of(f32 ? (q_items + 3) / 4 : q_items, &q_grid)) != SB_OK ||
-      (rc = grid_of(f32 ? (k_items + 3) / 4 : k_items, &k_grid)) != SB_OK || (rc = grid_of(w.far * g.Hkv, &far_grid)) != SB_OK)
+  if ((rc = grid_of((rows + per - 1) / per, &delta_grid)) != SB_OK || (rc = grid_of(q_items, &q_grid)) != SB_OK ||
+      (rc = grid_of(k_items, &k_grid)) != SB_OK || (rc = grid_of(w.far * g.Hkv, &far_grid)) != SB_OK)
     return rc;
   auto launch = [&](auto d) {
     constexpr int D = decltype(d)::value;
@@ -1032,7 +1116,7 @@ int sb_window_attn_bwd(const sb_problem* p, int32_t window, int32_t sinks, const
       if (f32) {
         hipLaunchKernelGGL((window_delta_kernel<float, D>), delta_grid, dim3(256), 0, st, P, rows);
         SB_LAUNCH_CHECK("window_delta_kernel");
-        hipLaunchKernelGGL((window_dq_f32_kernel<float, D>), q_grid, dim3(256), 0, st, P, q_items);
+        hipLaunchKernelGGL((window_dq_f32_kernel<float, D>), q_grid, dim3(256), 0, st, P);
       } else {
         hipLaunchKernelGGL((window_dq_kernel<D>), q_grid, dim3(512), 0, st, P);
       }
@@ -1040,7 +1124,7 @@ int sb_window_attn_bwd(const sb_problem* p, int32_t window, int32_t sinks, const
     }
     KernelTimer kt(K_WINDOW_DKV, st);
     if (f32) {
-      hipLaunchKernelGGL((window_dkv_f32_kernel<float, D>), k_grid, dim3(256), 0, st, P, k_items);
+      hipLaunchKernelGGL((window_dkv_f32_kernel<float, D>), k_grid, dim3(256), 0, st, P);
     } else {
       if (w.far > 0) {
         hipLaunchKernelGGL((window_dkv_kernel<D, kFarKeys / 32, true>), far_grid, dim3(kFarKeys * 4), 0, st, P);
