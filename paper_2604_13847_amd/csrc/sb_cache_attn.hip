@@ -2,7 +2,7 @@
 //
 // Whole chunks of a prompt go through the kernel of packed batches (sb_window.hip), which looks its key tiles up in the page table.  Few rows a sequence (single tokens above
 // all) are another matter: every key is read for a handful of products, so what bounds them is memory, and what fills the chip is splitting the keys.  cache_split_kernel
-// gives each (sequence, KV head, run of keys) to a workgroup of four wavefronts that stage their own strips and never wait for each other until they add up at the
+// gives each (sequence, KV head, run of keys) to a workgroup of two or four wavefronts that stage their own strips and never wait for each other until they add up at the
 // end; cache_merge_kernel joins the runs.
 #include <math.h>
 
@@ -48,15 +48,16 @@ static int check_cache_attn(const sb_cache* c, const sb_chunk* n, int32_t window
 }
 
 // ---------------------------------------------------------------------------------------------
-// Few rows (bfloat16): an item is up to 32 flattened rows of a KV head and per_split strips of 32 keys; wavefront w takes every fourth strip from the w-th on.  A wavefront's
+// Few rows (bfloat16): an item is up to 32 flattened rows of a KV head and per_split strips of 32 keys; wavefront w takes every NW-th strip from the w-th on.  A wavefront's
 // strips of K and V come by buffer loads straight into its own LDS, the next strip's while one is worked on: 64 KiB a CU on their way (head_dim 128), no barrier, and the
 // products of a strip take a quarter of the time that memory takes to deliver four.  Pages are looked up 64 strips ahead, a lane a strip.
-template <int D>
-__global__ __launch_bounds__(256) void cache_split_kernel(WindowParams P) {
+// Four wavefronts (NW) where there are no more workgroups than CUs, two otherwise: two such workgroups share a CU's LDS, and one's start and end are hidden by the other's stream.
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW) void cache_split_kernel(WindowParams P) {
   constexpr int ROW_B = D * 2, STRIP_B = 32 * ROW_B, NOP = D / 16, C = D / 8, RPI = 64 / C, LPG = 16 / RPI;  // loads per 16 rows
   constexpr int OUT_P = D + 4;  // floats from row to row of a wavefront's sums in LDS
-  __shared__ __attribute__((aligned(1024))) char ring[4][2][2 * STRIP_B];  // K, V
-  __shared__ float stats[2][4][32];
+  __shared__ __attribute__((aligned(1024))) char ring[NW][2][2 * STRIP_B];  // K, V
+  __shared__ float stats[2][NW][32];
   static_assert(32 * OUT_P * 4 <= 4 * STRIP_B, "the sums take the strips' place");
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
   // (what follows a division is the same in every lane but lies in vector registers, where what the loads' resources are made of must not come from)
@@ -72,11 +73,11 @@ __global__ __launch_bounds__(256) void cache_split_kernel(WindowParams P) {
   const KeyTiles<32> strips(ta, tb, P.window, P.sinks);
   const int begin = (int)min((int64_t)z * P.per_split, (int64_t)strips.count());
   const int count = z < P.splits - 1 ? min(begin + P.per_split, strips.count()) : strips.count();
-  const int turns = (count - begin - wave + 3) / 4;  // strips of this wavefront: begin + wave + 4 x (may be none)
+  const int turns = (count - begin - wave + NW - 1) / NW;  // strips of this wavefront: begin + wave + NW x (may be none)
   const int32_t* const table = P.cache.table + (int64_t)t.s * P.cache.max_pages;
   const unsigned page_b = (unsigned)P.Hkv << P.cache.page_shift;  // rows of a page
 
-  // Of strip begin + wave + 4 (x0 + lane): the first row, in units of 16 rows, of its keys 0 .. 15 and 16 .. 31 in the cache, and how many of each exist; -1, 0: none
+  // Of strip begin + wave + NW (x0 + lane): the first row, in units of 16 rows, of its keys 0 .. 15 and 16 .. 31 in the cache, and how many of each exist; -1, 0: none
   int where[2], there[2], x0 = 0;
   auto look_up = [&](int from) __attribute__((always_inline)) {
     x0 = from;
@@ -85,7 +86,7 @@ __global__ __launch_bounds__(256) void cache_split_kernel(WindowParams P) {
       where[b] = 0;
       there[b] = 0;
       if (from + lane < turns) {
-        const int u = 32 * strips.at(begin + wave + 4 * (from + lane)) + 16 * b;
+        const int u = 32 * strips.at(begin + wave + NW * (from + lane)) + 16 * b;
         if (u < end && (u + 16 > lo || u < P.sinks)) {
           const int page = table[u >> P.cache.page_shift];
           if ((unsigned)page < (unsigned)P.cache.num_pages) {
@@ -107,7 +108,7 @@ __global__ __launch_bounds__(256) void cache_split_kernel(WindowParams P) {
   auto issue = [&](int x) __attribute__((always_inline)) {  // strip x of this wavefront, or, past its last, as many loads of nothing
     const unsigned slot = ring0 + (x & 1) * 2 * STRIP_B;
     const int at = min(x - x0, 63);
-    const int u = __builtin_amdgcn_readfirstlane(32 * strips.at(min(begin + wave + 4 * x, max(strips.count() - 1, 0))));
+    const int u = __builtin_amdgcn_readfirstlane(32 * strips.at(min(begin + wave + NW * x, max(strips.count() - 1, 0))));
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const unsigned page = (unsigned)__builtin_amdgcn_readlane(where[b], at);
@@ -153,7 +154,7 @@ __global__ __launch_bounds__(256) void cache_split_kernel(WindowParams P) {
       tr_a[dt][half] = ring0 + STRIP_B + r * ROW_B + 16 * ((d >> 3) ^ chunk_swizzle<D>(r)) + 2 * (d & 7);
     }
   for (int x = 0; x < turns; ++x) {
-    const int u0 = 32 * strips.at(begin + wave + 4 * x);
+    const int u0 = 32 * strips.at(begin + wave + NW * x);
     const unsigned off = (x & 1) * 2 * STRIP_B;
     const unsigned have = (1u << __builtin_amdgcn_readlane(there[0], x - x0)) - 1 | ((1u << __builtin_amdgcn_readlane(there[1], x - x0)) - 1) << 16;  // keys that exist
     const bool refill = x + 1 < turns && x + 1 - x0 == 64;
@@ -209,7 +210,7 @@ __global__ __launch_bounds__(256) void cache_split_kernel(WindowParams P) {
       for (int dt = 0; dt < D / 32; ++dt) acc[dt] = mfma32(op[kk * (D / 32) + dt], w[kk], acc[dt]);
   }
   wait_vmcnt<0>();
-  // the four wavefronts' sums, through LDS (each in its own strips' place)
+  // the wavefronts' sums, through LDS (each in its own strips' place)
   l += __shfl_xor(l, 32, 64);
   float* const out = (float*)&ring[wave][0][0];
 #pragma unroll
@@ -221,13 +222,13 @@ __global__ __launch_bounds__(256) void cache_split_kernel(WindowParams P) {
   __syncthreads();
   constexpr int LANES = D / 4;
   const int c = threadIdx.x % LANES;
-  for (int r = threadIdx.x / LANES; r < mine; r += 256 / LANES) {
+  for (int r = threadIdx.x / LANES; r < mine; r += 64 * NW / LANES) {
     float best = -__builtin_inff(), sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) best = fmaxf(best, stats[0][w][r]);
+    for (int w = 0; w < NW; ++w) best = fmaxf(best, stats[0][w][r]);
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < NW; ++w) {
       if (stats[1][w][r] == 0.f) continue;
       const float f = fast_exp2(stats[0][w][r] - best);
       sum += f * stats[1][w][r];
@@ -251,37 +252,67 @@ __global__ __launch_bounds__(256) void cache_split_kernel(WindowParams P) {
   }
 }
 
-// Joins the runs of keys: one wavefront a row and head.  A run that saw nothing has left LSE -infinity and no sums.  `few`, `many`: runs of sequences of up to few_rows
-// flattened rows and of the others; where that is one, the rows are complete.
+// Joins the runs of keys of the sequences that a launch before had: a workgroup to a row and head, every fourth run a wavefront's.  A run that saw nothing has left LSE -infinity and no
+// sums.  seq_rows > 0: workgroups for that many rows of every sequence, else for all rows.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void cache_merge_kernel(WindowParams P, int few_rows, int few, int many) {
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + wave, all = (int64_t)P.T * P.Hq;
-  if (row >= all) return;
-  const int tok = (int)(row / P.Hq), h = (int)(row % P.Hq);
-  const int s = sequence_of(P.cu, P.S, tok, lane);
-  if (s >= P.S) return;  // a row of no sequence: left as it was
-  const int row0 = max(P.cu[s], 0), n = min(min(P.cu[s + 1], P.T) - row0, P.max_new);
-  if (tok - row0 < 0 || tok - row0 >= n) return;
-  const int splits = n * P.G <= few_rows ? few : many;
-  if (splits <= 1) return;
+__global__ __launch_bounds__(256) void cache_merge_kernel(WindowParams P, int seq_rows) {
   constexpr int E = D / 64;
-  float best = -__builtin_inff();
-  for (int z0 = 0; z0 < splits; z0 += 64) best = fmaxf(best, z0 + lane < splits ? P.part_lse[(z0 + lane) * all + row] : -__builtin_inff());
+  __shared__ float sums[4][E + 2][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int h = (int)(blockIdx.x % (unsigned)P.Hq), at = (int)(blockIdx.x / (unsigned)P.Hq);
+  const int s = seq_rows > 0 ? at / seq_rows : sequence_of(P.cu, P.S, at, lane);
+  if (s >= P.S) return;  // a row of no sequence: left as it was
+  const int row0 = min(max(P.cu[s], 0), P.T), n = min(min(P.cu[s + 1], P.T) - row0, P.max_new), tok = seq_rows > 0 ? row0 + at % seq_rows : at;
+  if (tok - row0 < 0 || tok - row0 >= n || n * P.G < P.rows_from || n * P.G > P.rows_to) return;
+  const int splits = P.splits;
+  const int64_t all = (int64_t)P.T * P.Hq, row = (int64_t)tok * P.Hq + h;
+  constexpr int kRuns = 8;  // on their way at a time
+  float x[E] = {}, best = -__builtin_inff(), sum = 0.f;
+  for (int z0 = wave; z0 < splits; z0 += 4 * kRuns) {
+    float lse[kRuns], part[kRuns][E], top = best;
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) best = fmaxf(best, __shfl_xor(best, off, 64));
-  float x[E] = {}, sum = 0.f;
+    for (int i = 0; i < kRuns; ++i) {  // (past the last run, it again)
+      const int z = min(z0 + 4 * i, splits - 1);
+      lse[i] = P.part_lse[z * all + row];
+#pragma unroll
+      for (int e = 0; e < E; ++e) part[i][e] = P.part_o[(z * all + row) * D + E * lane + e];
+      if (z0 + 4 * i >= splits) lse[i] = -__builtin_inff();
+    }
+#pragma unroll
+    for (int i = 0; i < kRuns; ++i) top = fmaxf(top, lse[i]);
+    if (top == -__builtin_inff()) continue;
+    const float old = fast_exp2(best - top);
+    sum *= old;
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] *= old;
+#pragma unroll
+    for (int i = 0; i < kRuns; ++i) {
+      const float f = fast_exp2(lse[i] - top);
+      sum += f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(f, lse[i] == -__builtin_inff() ? 0.f : part[i][e], x[e]);  // (a run without sums holds whatever was there)
+    }
+    best = top;
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) sums[wave][e][lane] = x[e];
+  sums[wave][E][lane] = best;
+  sums[wave][E + 1][lane] = sum;
+  __syncthreads();
+  if (wave > 0) return;
+  best = -__builtin_inff();
+#pragma unroll
+  for (int w = 0; w < 4; ++w) best = fmaxf(best, sums[w][E][lane]);
+  sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = 0.f;
   if (best > -__builtin_inff()) {
-    for (int z0 = 0; z0 < splits; z0 += 64) {
-      const float mine = z0 + lane < splits ? fast_exp2(P.part_lse[(z0 + lane) * all + row] - best) : 0.f;
-      const int n = min(64, splits - z0);
-      for (int z = 0; z < n; ++z) {
-        const float f = __shfl(mine, z, 64);
-        if (f == 0.f) continue;
-        sum += f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(f, P.part_o[((z0 + z) * all + row) * D + E * lane + e], x[e]);
-      }
+    for (int w = 0; w < 4; ++w) {
+      const float f = fast_exp2(sums[w][E][lane] - best);
+      sum += f * sums[w][E + 1][lane];
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(f, sums[w][e][lane], x[e]);
     }
   }
   const float inv = sum > 0.f ? 1.0f / sum : 0.f;
@@ -359,40 +390,46 @@ int sb_cache_attn(const sb_cache* c, const sb_chunk* n, int32_t window, int32_t 
   P.scale_log2e = P.scale * 1.4426950408889634f;
   P.cache = make_paged(c);
   const CachePlan plan = plan_cache(c, n, window, sinks);
-  const bool joined = plan.few.splits > 1 || plan.many.splits > 1;
-  if (joined) {
+  if (plan.few.splits > 1 || plan.many.splits > 1) {
     if (!ws) { set_error("null argument"); return SB_ERR_INVALID_ARG; }
     P.part_o = (float*)((char*)ws + plan.part_o);
     P.part_lse = (float*)((char*)ws + plan.part_lse);
   }
   const hipStream_t st = (hipStream_t)stream;
   const bool f32 = c->dtype == SB_F32;
-  dim3 grid, merge_grid;
-  if ((rc = grid_of(plan.few.items * P.Hkv * plan.few.splits, &grid)) != SB_OK || (rc = grid_of(((int64_t)P.T * P.Hq + 3) / 4, &merge_grid)) != SB_OK) return rc;
+  const int64_t rows = P.T, few_seq_rows = kFewRows / P.G < P.max_new ? kFewRows / P.G : P.max_new;
+  dim3 grid, all_rows, few_rows;
+  if ((rc = grid_of(plan.few.items * P.Hkv * plan.few.splits, &grid)) != SB_OK || (rc = grid_of(rows * P.Hq, &all_rows)) != SB_OK ||
+      (rc = grid_of(few_seq_rows * P.S * P.Hq, &few_rows)) != SB_OK)
+    return rc;
   KernelTimer kt(K_CACHE_ATTN, st);
+  auto merge = [&](dim3 workgroups, int seq_rows) {
+    auto launch = [&](auto t, auto d) { hipLaunchKernelGGL((cache_merge_kernel<decltype(t), decltype(d)::value>), workgroups, dim3(256), 0, st, P, seq_rows); };
+    auto with_d = [&](auto t) { if (c->head_dim == 128) launch(t, std::integral_constant<int, 128>()); else launch(t, std::integral_constant<int, 64>()); };
+    if (f32) with_d(float()); else with_d(bf16());
+    SB_LAUNCH_CHECK("cache_merge_kernel");
+    return (int)SB_OK;
+  };
   if (plan.many.items > 0) {
     P.splits = plan.many.splits;
     P.per_split = plan.many.per_split;
     P.rows_from = f32 || plan.few.items == 0 ? 0 : kFewRows + 1;
     P.rows_to = 0x7fffffff;
     if ((rc = launch_window_fwd(P, c->head_dim, c->dtype, true, plan.many.items, st)) != SB_OK) return rc;
+    if (P.splits > 1 && (rc = merge(all_rows, 0)) != SB_OK) return rc;
   }
   if (plan.few.items > 0) {
     P.splits = plan.few.splits;
     P.per_split = plan.few.per_split;
     P.rows_from = 0;
     P.rows_to = kFewRows;
-    if (c->head_dim == 128) hipLaunchKernelGGL((cache_split_kernel<128>), grid, dim3(256), 0, st, P);
-    else hipLaunchKernelGGL((cache_split_kernel<64>), grid, dim3(256), 0, st, P);
-    SB_LAUNCH_CHECK("cache_split_kernel");
-  }
-  if (joined) {
-    auto merge = [&](auto t, auto d) {
-      hipLaunchKernelGGL((cache_merge_kernel<decltype(t), decltype(d)::value>), merge_grid, dim3(256), 0, st, P, plan.few.items > 0 ? kFewRows : 0, plan.few.splits, plan.many.splits);
+    auto split = [&](auto d, auto nw) {
+      hipLaunchKernelGGL((cache_split_kernel<decltype(d)::value, decltype(nw)::value>), grid, dim3(64 * decltype(nw)::value), 0, st, P);
     };
-    auto with_d = [&](auto t) { if (c->head_dim == 128) merge(t, std::integral_constant<int, 128>()); else merge(t, std::integral_constant<int, 64>()); };
-    if (f32) with_d(float()); else with_d(bf16());
-    SB_LAUNCH_CHECK("cache_merge_kernel");
+    auto with_nw = [&](auto d) { if (grid.x <= 320) split(d, std::integral_constant<int, 4>()); else split(d, std::integral_constant<int, 2>()); };
+    if (c->head_dim == 128) with_nw(std::integral_constant<int, 128>()); else with_nw(std::integral_constant<int, 64>());
+    SB_LAUNCH_CHECK("cache_split_kernel");
+    if (P.splits > 1 && (rc = merge(few_rows, (int)few_seq_rows)) != SB_OK) return rc;
   }
   return SB_OK;
 }

@@ -16,6 +16,8 @@ struct WindowParams {
   bf16x8* stats;      // [T][Hq][2] the same as operands of matrix instructions (bfloat16), see split3
   float* partials;    // dK, dV of sinks from rows far behind, see window_dkv_kernel
   int far_rows;       // tokens of a far item
+  float* parts;       // dK, dV of an item whose rows several workgroups share
+  int near_parts;     // that many
   void *dq, *dk, *dv;
   const int32_t* cu;  // [S+1]: packed rows of the sequences (paged: of their new tokens)
   int T, S, Hq, Hkv, G;
@@ -46,11 +48,12 @@ template <int ROWS, bool PAGED>
 __device__ inline RowTile locate_tile(const WindowParams& P, int64_t x) {
   const int lane = threadIdx.x & 63;
   for (int base = 0; base < P.S; base += 64) {
-    int row0 = 0, n = 0;
+    int row0 = 0, n = 0, pos0 = 0;
     if (base + lane < P.S) {
       row0 = P.cu[base + lane];
       n = P.cu[base + lane + 1];
       if (PAGED) {
+        pos0 = max(P.cached[base + lane], 0);
         row0 = min(max(row0, 0), P.T);
         n = min(n, P.T);
       }
@@ -58,27 +61,27 @@ __device__ inline RowTile locate_tile(const WindowParams& P, int64_t x) {
       if (PAGED) {
         n = min(n, P.max_new);
         if (n * P.G < P.rows_from || n * P.G > P.rows_to) n = 0;
+        pos0 = min(pos0, 0x7fffffff - n);
       }
     }
-    const int64_t c = (int64_t)(((unsigned)n * (unsigned)P.G + (unsigned)ROWS - 1) / (unsigned)ROWS);  // (rows of a sequence fit 31 bits: see check_rows)
-    int64_t incl = c;
-    for (int off = 1; off < 64; off <<= 1) {
-      const int64_t t = __shfl_up(incl, off, 64);
+    const int c = (int)(((unsigned)n * (unsigned)P.G + (unsigned)ROWS - 1) / (unsigned)ROWS);  // (rows of a sequence, and tiles of 64 of them, fit 31 bits: see check_rows)
+    int incl = c;
+    for (int off = 1; off < 64 && off < P.S - base; off <<= 1) {
+      const int t = __shfl_up(incl, off, 64);
       if (lane >= off) incl += t;
     }
-    const unsigned long long hit = __builtin_amdgcn_ballot_w64(x < incl);
-    const int src = hit ? __builtin_ctzll(hit) : 63;
+    const unsigned long long hit = __builtin_amdgcn_ballot_w64(base + lane < P.S && x < incl);
     if (hit) {
+      const int src = __builtin_ctzll(hit), tiles = __builtin_amdgcn_readlane(c, src);
       RowTile t;
       t.s = base + src;
       t.row0 = __builtin_amdgcn_readlane(row0, src);
       t.n = __builtin_amdgcn_readlane(n, src);
-      const int64_t first = __shfl(incl - c, src, 64), tiles = __shfl(c, src, 64);
-      t.tile = __builtin_amdgcn_readfirstlane((int)(tiles - 1 - (x - first)));
-      t.pos0 = PAGED ? __builtin_amdgcn_readfirstlane(min(max(P.cached[t.s], 0), 0x7fffffff - t.n)) : 0;
+      t.pos0 = __builtin_amdgcn_readlane(pos0, src);
+      t.tile = __builtin_amdgcn_readfirstlane(tiles - 1 - (int)(x - (__builtin_amdgcn_readlane(incl, src) - tiles)));
       return t;
     }
-    x -= __shfl(incl, 63, 64);
+    x -= __builtin_amdgcn_readlane(incl, min(P.S - base, 64) - 1);
   }
   return RowTile{-1, 0, 0, 0, 0};
 }

@@ -691,7 +691,9 @@ __host__ __device__ inline int near_end(int u, int n, int window) {
   return n - last > window ? last + window : n;
 }
 
-template <int D, int PAIRS, bool FAR>
+// Where there are fewer items than CUs, an item's rows are shared by near_parts workgroups (kPart) that leave their sums too, which a last launch adds in order (kJoin).
+enum DkvMode { kWhole, kFar, kPart, kJoin };
+template <int D, int PAIRS, DkvMode MODE>
 __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))) void window_dkv_kernel(WindowParams P) {
   constexpr int ROW_B = D * 2, TILE_B = 32 * ROW_B, NOP = D / 16, KEYS = 32 * PAIRS, NW = 2 * PAIRS;
   constexpr int kSlots = 7, kAhead = 5, STAT_B = 1024, STAGE_B = 2 * TILE_B;
@@ -705,19 +707,21 @@ __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))
   const int g = __builtin_amdgcn_readfirstlane((int)(blockIdx.x % (unsigned)P.Hkv));
   // which sequence, and what of it
   int s = -1, seq0 = 0, n = 0;
-  int64_t x = blockIdx.x / P.Hkv, far0 = 0;  // far0: far items of the earlier sequences
+  const unsigned tile_part = blockIdx.x / (unsigned)P.Hkv;
+  int64_t x = MODE == kPart ? tile_part / (unsigned)P.near_parts : tile_part, far0 = 0;  // far0: far items of the earlier sequences
+  const int64_t tile_id = x;
   for (int base = 0; base < P.S && s < 0; base += 64) {
     int first = 0, len = 0;
     if (base + lane < P.S) { first = P.cu[base + lane]; len = P.cu[base + lane + 1] - first; }
     const int64_t c_far = far_items(len, P.window, P.sinks, P.far_rows);
-    const int64_t c = FAR ? c_far : (int64_t)((len + KEYS - 1) / KEYS);
+    const int64_t c = MODE == kFar ? c_far : (int64_t)((len + KEYS - 1) / KEYS);
     int64_t incl = c, incl_far = c_far;
-    for (int off = 1; off < 64; off <<= 1) {
+    for (int off = 1; off < 64 && off < P.S - base; off <<= 1) {
       const int64_t a = __shfl_up(incl, off, 64), b = __shfl_up(incl_far, off, 64);
       if (lane >= off) { incl += a; incl_far += b; }
     }
-    const unsigned long long hit = __builtin_amdgcn_ballot_w64(x < incl);
-    const int src = hit ? __builtin_ctzll(hit) : 63;
+    const unsigned long long hit = __builtin_amdgcn_ballot_w64(base + lane < P.S && x < incl);
+    const int src = hit ? __builtin_ctzll(hit) : min(P.S - base, 64) - 1;
     if (hit) {
       s = base + src;
       seq0 = __builtin_amdgcn_readlane(first, src);
@@ -725,15 +729,15 @@ __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))
       x -= __shfl(incl - c, src, 64);
       far0 += __shfl(incl_far - c_far, src, 64);
     } else {
-      x -= __shfl(incl, 63, 64);
-      far0 += __shfl(incl_far, 63, 64);
+      x -= __shfl(incl, src, 64);
+      far0 += __shfl(incl_far, src, 64);
     }
   }
   if (s < 0) return;
   const int segments = far_segments(n, P.window, P.far_rows);
   const int item = __builtin_amdgcn_readfirstlane((int)x);
   int u0, r0, r1;  // first key; rows: tokens r0 .. r1 - 1
-  if (FAR) {
+  if (MODE == kFar) {
     u0 = item / segments * KEYS;
     const int64_t from = (int64_t)near_end(u0, n, P.window) + (int64_t)(item % segments) * P.far_rows;
     if (from >= n) return;
@@ -746,11 +750,20 @@ __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))
   }
   const int ku = u0 + 32 * pair, kl = min(ku + 31, n - 1);  // this pair's keys (none: ku >= n)
   const int key = min(ku + l32, n - 1);
-  const int m0 = r0 * P.G, m1 = r1 * P.G, stages = (m1 - m0 + 31) / 32;
+  int m0 = r0 * P.G, m1 = r1 * P.G;
+  if (MODE == kPart) {
+    // tokens in equal shares, of whole stages
+    const int z = (int)(tile_part % (unsigned)P.near_parts), share = ((r1 - r0 + P.near_parts - 1) / P.near_parts + 31) / 32 * 32;
+    r0 = min(r0 + z * share, r1);
+    r1 = min(r0 + share, r1);
+    m0 = r0 * P.G;
+    m1 = r1 * P.G;
+  }
+  const int stages = MODE == kJoin ? 0 : (m1 - m0 + 31) / 32;
   // The stages are walked in a circle from y0 on: where a row's number is a multiple of an ordinary item's rows.  Neighbouring items, which an XCD works on at the same time and which have
   // most of their rows in common, so ask for the same rows at about the same time and meet them in the XCD's L2, which could not hold the rows of one item for the next.
   int y0 = 0;
-  if (!FAR) {
+  if (MODE == kWhole) {
     const int64_t around = ((int64_t)P.window + kDkvKeys) * P.G;
     const int64_t start = (around - m0 % around) % around / 32;
     if (start < stages) y0 = (int)start;
@@ -890,8 +903,9 @@ __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))
   };
   auto after = [](int slot) { return slot == kSlots - 1 ? 0 : slot + 1; };
   int slot = 0;
-  turn(0);
-  if (!second) {
+  if (MODE != kJoin) turn(0);
+  if (MODE == kJoin) {
+  } else if (!second) {
     // stage x: S(x); P(x); dV += P(x)^T dO(x)
     less = ld_stat(0);
 #pragma unroll
@@ -950,29 +964,38 @@ __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))
   }
   wait_vmcnt<0>();
 
-  // a far item's sums: [item][KV head][dV, dK][register][lane]
-  auto slot_of = [&](int64_t it) { return P.partials + ((it * P.Hkv + g) * 2 + (second ? 1 : 0)) * (kNr * 64) + lane; };
-  if (FAR) {
-    float* to = slot_of(far0 + item);
+  // sums left in float32: of a far item [item][KV head][dV, dK][register][lane], of a part [tile][part][KV head][pair][dV, dK][register][lane]
+  auto leave = [&](float* to) {
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) to[(16 * dt + v) * 64] = acc[dt][v];
+      for (int v = 0; v < 16; ++v) to[(16 * dt + v) * 64 + lane] = acc[dt][v];
+  };
+  auto take = [&](const float* from) {
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[dt][v] += from[(16 * dt + v) * 64 + lane];
+  };
+  auto far_sums = [&](int64_t it) { return P.partials + ((it * P.Hkv + g) * 2 + (second ? 1 : 0)) * (kNr * 64); };
+  auto part_sums = [&](int z) { return P.parts + ((((tile_id * P.near_parts + z) * P.Hkv + g) * PAIRS + pair) * 2 + (second ? 1 : 0)) * (kNr * 64); };
+  if (MODE == kFar) {
+    leave(far_sums(far0 + item));
     return;
   }
+  if (MODE == kPart) {
+    leave(part_sums((int)(tile_part % (unsigned)P.near_parts)));
+    return;
+  }
+  if (MODE == kJoin)
+    for (int z = 0; z < P.near_parts; ++z) take(part_sums(z));
   if (ku < min(P.sinks, n) && P.sinks <= kFarSinks) {
     const int end = near_end(u0, n, P.window), have = (n - end + P.far_rows - 1) / P.far_rows;
     const int64_t it = far0 + (int64_t)(ku / kFarKeys) * segments;
-    for (int z = 0; z < have; ++z) {
-      const float* from = slot_of(it + z);
-#pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) acc[dt][v] += from[(16 * dt + v) * 64];
-    }
+    for (int z = 0; z < have; ++z) take(far_sums(it + z));
   }
   __syncthreads();  // the stages' LDS is free
-  static_assert(NW * 32 * ROW_B <= (int)sizeof(stage) + (int)sizeof(pbuf) || FAR, "every wavefront's rows");
+  static_assert(NW * 32 * ROW_B <= (int)sizeof(stage) + (int)sizeof(pbuf) || MODE == kFar, "every wavefront's rows");
   char* const buf = wave * 32 * ROW_B + 32 * ROW_B <= (int)sizeof(stage) ? &stage[0][0] + wave * 32 * ROW_B : (char*)&pbuf[0][0][0] + (wave * 32 * ROW_B - (int)sizeof(stage) / (32 * ROW_B) * 32 * ROW_B);
   const float f = second ? P.scale : 1.0f;
   store_tile<D>(buf, lane, [&](int dt, int v) __attribute__((always_inline)) { return acc[dt][v] * f; },
@@ -1039,7 +1062,7 @@ static int far_rows_of(const int32_t* cu, int S, int window) {
   const int64_t rows = (most - window + 31) / 32;
   return rows < 256 ? 256 : (int)((rows + 31) / 32 * 32);
 }
-struct WindowWs { size_t lse2, dr, stats, partials, bytes; int64_t far; int far_rows; };
+struct WindowWs { size_t lse2, dr, stats, partials, parts, bytes; int64_t far; int far_rows, near_parts; };
 static WindowWs window_bwd_ws(const Geo& g, const int32_t* cu, int window, int sinks) {
   WindowWs w{};
   size_t o = 0;
@@ -1051,6 +1074,21 @@ static WindowWs window_bwd_ws(const Geo& g, const int32_t* cu, int window, int s
   if (g.dtype == SB_BF16)
     for (int s = 0; s < g.S; ++s) w.far += far_items(cu[s + 1] - cu[s], window, sinks, w.far_rows);
   w.partials = o; o = align_up(o + (size_t)w.far * g.Hkv * 2 * kFarKeys * g.D * sizeof(float));
+  // Parts where items are fewer than CUs: up to 8, of 16 stages at least
+  w.near_parts = 1;
+  if (g.dtype == SB_BF16) {
+    const int64_t items = row_tiles(cu, g.S, 1, kDkvKeys) * g.Hkv;
+    int64_t most = 0;  // tokens of an item
+    for (int s = 0; s < g.S; ++s)
+      if (cu[s + 1] - cu[s] > most) most = cu[s + 1] - cu[s];
+    if ((int64_t)window + kDkvKeys < most) most = (int64_t)window + kDkvKeys;
+    int64_t parts = items > 0 ? 384 / items : 1;
+    if (parts > most * g.G / (32 * 16)) parts = most * g.G / (32 * 16);
+    if (parts > 8) parts = 8;
+    if (parts > 1) w.near_parts = (int)parts;
+    w.parts = o;
+    if (parts > 1) o = align_up(o + (size_t)items * parts * 2 * kDkvKeys * g.D * sizeof(float));
+  }
   w.bytes = o;
   return w;
 }
@@ -1102,12 +1140,15 @@ int sb_window_attn_bwd(const sb_problem* p, int32_t window, int32_t sinks, const
   P.stats = (bf16x8*)((char*)ws + w.stats);
   P.partials = (float*)((char*)ws + w.partials);
   P.far_rows = w.far_rows;
+  P.parts = (float*)((char*)ws + w.parts);
+  P.near_parts = w.near_parts;
   const bool f32 = g.dtype == SB_F32;
   const int64_t rows = (int64_t)g.T * g.Hq, per = 1024 / g.D;
   const int64_t q_items = row_tiles(cu, g.S, g.G, f32 ? 32 : 256) * g.Hkv, k_items = row_tiles(cu, g.S, 1, f32 ? 32 : kDkvKeys) * g.Hkv;
-  dim3 delta_grid, q_grid, k_grid, far_grid;
+  dim3 delta_grid, q_grid, k_grid, far_grid, part_grid;
   if ((rc = grid_of((rows + per - 1) / per, &delta_grid)) != SB_OK || (rc = grid_of(q_items, &q_grid)) != SB_OK ||
-      (rc = grid_of(k_items, &k_grid)) != SB_OK || (rc = grid_of(w.far * g.Hkv, &far_grid)) != SB_OK)
+      (rc = grid_of(k_items, &k_grid)) != SB_OK || (rc = grid_of(w.far * g.Hkv, &far_grid)) != SB_OK ||
+      (rc = grid_of(k_items * w.near_parts, &part_grid)) != SB_OK)
     return rc;
   auto launch = [&](auto d) {
     constexpr int D = decltype(d)::value;
@@ -1127,10 +1168,16 @@ int sb_window_attn_bwd(const sb_problem* p, int32_t window, int32_t sinks, const
       hipLaunchKernelGGL((window_dkv_f32_kernel<float, D>), k_grid, dim3(256), 0, st, P);
     } else {
       if (w.far > 0) {
-        hipLaunchKernelGGL((window_dkv_kernel<D, kFarKeys / 32, true>), far_grid, dim3(kFarKeys * 4), 0, st, P);
+        hipLaunchKernelGGL((window_dkv_kernel<D, kFarKeys / 32, kFar>), far_grid, dim3(kFarKeys * 4), 0, st, P);
         SB_LAUNCH_CHECK("window_dkv_kernel, far rows");
       }
-      hipLaunchKernelGGL((window_dkv_kernel<D, kDkvKeys / 32, false>), k_grid, dim3(kDkvKeys * 4), 0, st, P);
+      if (w.near_parts > 1) {
+        hipLaunchKernelGGL((window_dkv_kernel<D, kDkvKeys / 32, kPart>), part_grid, dim3(kDkvKeys * 4), 0, st, P);
+        SB_LAUNCH_CHECK("window_dkv_kernel, parts");
+        hipLaunchKernelGGL((window_dkv_kernel<D, kDkvKeys / 32, kJoin>), k_grid, dim3(kDkvKeys * 4), 0, st, P);
+      } else {
+        hipLaunchKernelGGL((window_dkv_kernel<D, kDkvKeys / 32, kWhole>), k_grid, dim3(kDkvKeys * 4), 0, st, P);
+      }
     }
     SB_LAUNCH_CHECK("window_dkv_kernel");
     return (int)SB_OK;
