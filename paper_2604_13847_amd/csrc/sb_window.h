@@ -119,11 +119,11 @@ struct Sight {
 };
 __device__ inline bool sees(int t, int u, int window, int sinks) { return u <= t && (t - u < window || u < sinks); }
 
-// One wavefront's part of copying a 64-key tile of K or V into LDS (layout as in sb_attn_common.h), eight wavefronts to a tile: 8 rows each, as buffer loads whose resource covers
+// One wavefront's part of copying a 64-key tile of K or V into LDS (layout as in sb_attn_common.h), NW wavefronts to a tile, as buffer loads whose resource covers
 // the rows that exist, so that the others arrive as zeros.  A load's rows (4, or 8 at head_dim 64) lie in one page.
-template <int D>
+template <int D, int NW>
 struct RowsLoader {
-  static constexpr int C = D / 8, RPI = 64 / C, LOADS = 8 / RPI;  // 16-byte chunks per row, rows per load, loads per wavefront
+  static constexpr int MINE = 64 / NW, C = D / 8, RPI = 64 / C, LOADS = MINE / RPI;  // 16-byte chunks per row, rows per load, loads per wavefront
   unsigned voff[LOADS];
   unsigned pitch;  // bytes from row to row
   int wave;
@@ -132,17 +132,17 @@ struct RowsLoader {
     wave = wave_;
 #pragma unroll
     for (int a = 0; a < LOADS; ++a) {
-      const int r = 8 * wave + a * RPI + lane / C;
+      const int r = MINE * wave + a * RPI + lane / C;
       voff[a] = (lane / C) * pitch + 16 * ((lane % C) ^ chunk_swizzle<D>(r));
     }
   }
-  // `rows` of the wavefront's 8 rows exist, from `base` on (wave-uniform, by scalar instructions: see QuadLoader)
+  // `rows` of the wavefront's rows exist, from `base` on (wave-uniform, by scalar instructions: see QuadLoader)
   __device__ inline void issue(unsigned long long base, int rows, unsigned slot) const {
 #pragma unroll
     for (int a = 0; a < LOADS; ++a) {
       const int n = min(rows - a * RPI, RPI);
       const i32x4 rsrc = QuadLoader<D>::resource(base + (unsigned long long)(a * RPI) * pitch, n > 0 ? (unsigned)(n - 1) * pitch + D * 2 : 0u);
-      asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds" : : "v"(voff[a]), "s"(slot + (8 * wave + a * RPI) * D * 2), "s"(rsrc) : "memory", "m0");
+      asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds" : : "v"(voff[a]), "s"(slot + (MINE * wave + a * RPI) * D * 2), "s"(rsrc) : "memory", "m0");
     }
   }
 };
@@ -229,7 +229,8 @@ int64_t row_tiles(const int32_t* cu_host, int S, int G, int rows);  // of a pack
 int64_t row_tiles_most(int total, int S, int G, int rows);          // where the lengths are not known to the host
 
 // Forward launch of all query rows; P is complete.  dtype as in sb_problem; tiles: of forward_rows(dtype) flattened rows.
-constexpr int forward_rows(int dtype) { return dtype == SB_F32 ? 32 : 256; }
+constexpr int kWaves = 4;  // of a forward or dQ workgroup (bfloat16)
+constexpr int forward_rows(int dtype) { return dtype == SB_F32 ? 32 : 32 * kWaves; }
 int launch_window_fwd(const WindowParams& P, int D, int dtype, bool paged, int64_t tiles, hipStream_t st);
 
 }  // namespace sb

@@ -340,13 +340,13 @@ __global__ __launch_bounds__(256) void window_dkv_f32_kernel(WindowParams P) {
 }
 
 // ---------------------------------------------------------------------------------------------
-// bfloat16 forward.  A workgroup of eight wavefronts owns 256 flattened rows of a KV head, 32 a wavefront, and walks the 64-key tiles that any of them sees; K and V tiles are
+// bfloat16 forward.  A workgroup of four wavefronts owns 128 flattened rows of a KV head, 32 a wavefront, and walks the 64-key tiles that any of them sees; K and V tiles are
 // shared in LDS and double-buffered by asynchronous loads.  A wavefront takes a tile as two halves of 32 keys, a step of the running softmax each.  A tile that a wavefront's rows
 // all see carries no mask; one that none of them sees is only waited for.  256 registers, so two wavefronts share a SIMD: one runs its exponentials while the other runs matrix
 // instructions.
 template <int D, bool PAGED>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void window_fwd_kernel(WindowParams P) {
-  constexpr int ROWS = 256, ROW_B = D * 2, TILE_B = 64 * ROW_B, NOP = D / 16;
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void window_fwd_kernel(WindowParams P) {
+  constexpr int ROWS = 32 * kWaves, ROW_B = D * 2, TILE_B = 64 * ROW_B, NOP = D / 16;
   constexpr float kLazy = 8.0f;
   __shared__ __attribute__((aligned(1024))) char tiles[2][2][TILE_B];  // [buffer][K, V]
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
@@ -367,13 +367,13 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void w
   const int count = PAGED && z < splits - 1 ? min(begin + P.per_split, keys.count()) : keys.count();
   KeySource<D, PAGED> src;
   src.init(P, t, g, max(0, ta - P.window + 1), tb + 1);
-  RowsLoader<D> loader;
+  RowsLoader<D, kWaves> loader;
   loader.init(src.pitch, wave, lane);
   const unsigned tiles0 = lds_offset(&tiles[0][0][0]);
   auto issue = [&](int x) __attribute__((always_inline)) {
-    const int u = 64 * keys.at(x) + 8 * wave;
+    const int u = 64 * keys.at(x) + 64 / kWaves * wave;
     int there;
-    const unsigned long long o = src.rows_at(P, u, 8, there);
+    const unsigned long long o = src.rows_at(P, u, 64 / kWaves, there);
     const unsigned slot = tiles0 + ((x - begin) & 1) * 2 * TILE_B;
     loader.issue(src.k + o, there, slot);
     loader.issue(src.v + o, there, slot + TILE_B);
@@ -525,8 +525,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void w
 // bfloat16 dQ.  Rows, tiles and their walk as in the forward kernel; a half tile is S, dP and dQ += dS K, whose operands go through one set of registers.  Every row belongs to one
 // workgroup here, so this is also where Dr is computed, from the dO in registers and one read of O, and left with LSE for the next kernel.
 template <int D>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void window_dq_kernel(WindowParams P) {
-  constexpr int ROWS = 256, ROW_B = D * 2, TILE_B = 64 * ROW_B, NOP = D / 16;
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void window_dq_kernel(WindowParams P) {
+  constexpr int ROWS = 32 * kWaves, ROW_B = D * 2, TILE_B = 64 * ROW_B, NOP = D / 16;
   __shared__ __attribute__((aligned(1024))) char tiles[2][2][TILE_B];  // [buffer][K, V]
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
   const RowTile t = locate_tile<ROWS, false>(P, blockIdx.x / P.Hkv);
@@ -542,12 +542,12 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void w
   const int count = keys.count();
   KeySource<D, false> src;
   src.init(P, t, g, max(0, ta - P.window + 1), tb + 1);
-  RowsLoader<D> loader;
+  RowsLoader<D, kWaves> loader;
   loader.init(src.pitch, wave, lane);
   const unsigned tiles0 = lds_offset(&tiles[0][0][0]);
   auto issue = [&](int x) __attribute__((always_inline)) {
     int there;
-    const unsigned long long o = src.rows_at(P, 64 * keys.at(x) + 8 * wave, 8, there);
+    const unsigned long long o = src.rows_at(P, 64 * keys.at(x) + 64 / kWaves * wave, 64 / kWaves, there);
     const unsigned slot = tiles0 + (x & 1) * 2 * TILE_B;
     loader.issue(src.k + o, there, slot);
     loader.issue(src.v + o, there, slot + TILE_B);
@@ -672,16 +672,16 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void w
 // bfloat16 dK and dV.  A workgroup owns PAIRS * 32 keys of a KV head and walks the flattened rows that see any of them, 32 a stage.  32 keys are the work of two wavefronts on one
 // SIMD: the first computes S and P and adds P^T dO to dV, the second, a stage behind, dP and dS = P (dP - Dr) and adds dS^T Q to dK; P goes from one to the other through LDS
 // in float32, lane by lane (both hold keys in columns).  Each so needs 150 registers where one wavefront for both would need more than the 256 that let two share a SIMD,
-// and has as many matrix instructions as the other.  The stages' Q and dO rows, LSE and Dr come by asynchronous loads, five stages ahead.
+// and has as many matrix instructions as the other.  The stages' Q and dO rows, LSE and Dr come by asynchronous loads, three stages ahead.
 //
-// Sinks are seen by all rows of their sequence.  The rows behind a sink tile's ordinary ones (far rows) are the work of other workgroups (FAR), far_rows tokens each, that leave their
+// Sinks are seen by all rows of their sequence.  The rows behind a sink tile's ordinary ones (far rows) are the work of other workgroups (kFar), far_rows tokens each, that leave their
 // sums in float32; the tile's own workgroup, launched after them, adds them in order.  So the result does not depend on who is ahead, and no workgroup has more than its share.
-constexpr int kDkvKeys = 128;   // keys of a workgroup without FAR
-constexpr int kFarKeys = 32;    // with
+constexpr int kDkvKeys = 128;   // keys of a workgroup, but of kFar
+constexpr int kFarKeys = 32;    // of kFar
 constexpr int kFarSinks = 512;  // with more sinks than this there are sink tiles enough to fill the chip: their own workgroups take all rows
 // Far items of a sequence of n tokens: far_blocks blocks of sinks, far_segments each (some may be empty: the first rows of a block's last ones).
 __host__ __device__ inline int far_blocks(int n, int sinks) { return ((sinks < n ? sinks : n) + kFarKeys - 1) / kFarKeys; }
-__host__ __device__ inline int far_segments(int n, int window, int far_rows) { return n > window ? (n - window + far_rows - 1) / far_rows : 0; }
+__host__ __device__ inline int far_segments(int n, int window, int far_rows) { return far_rows > 0 && n > window ? (n - window + far_rows - 1) / far_rows : 0; }
 __host__ __device__ inline int64_t far_items(int n, int window, int sinks, int far_rows) {
   return sinks > kFarSinks ? 0 : (int64_t)far_blocks(n, sinks) * far_segments(n, window, far_rows);
 }
@@ -696,7 +696,7 @@ enum DkvMode { kWhole, kFar, kPart, kJoin };
 template <int D, int PAIRS, DkvMode MODE>
 __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))) void window_dkv_kernel(WindowParams P) {
   constexpr int ROW_B = D * 2, TILE_B = 32 * ROW_B, NOP = D / 16, KEYS = 32 * PAIRS, NW = 2 * PAIRS;
-  constexpr int kSlots = 7, kAhead = 5, STAT_B = 1024, STAGE_B = 2 * TILE_B;
+  constexpr int kSlots = 5, kAhead = 3, STAT_B = 1024, STAGE_B = 2 * TILE_B;
   constexpr int kNr = 16 * (D / 32);  // accumulator registers
   __shared__ __attribute__((aligned(1024))) char stage[kSlots][STAGE_B];  // Q, dO
   __shared__ __attribute__((aligned(1024))) float pbuf[2][PAIRS][16 * 64];
@@ -746,7 +746,7 @@ __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))
   } else {
     u0 = item * KEYS;
     r0 = u0;
-    r1 = P.sinks > kFarSinks && u0 < P.sinks ? n : near_end(u0, n, P.window);
+    r1 = (P.sinks > kFarSinks || P.far_rows == 0) && u0 < P.sinks ? n : near_end(u0, n, P.window);
   }
   const int ku = u0 + 32 * pair, kl = min(ku + 31, n - 1);  // this pair's keys (none: ku >= n)
   const int key = min(ku + l32, n - 1);
@@ -945,6 +945,7 @@ __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))
     }
   } else {
     // stage x: dK += dS(x - 2)^T Q(x - 2); dP(x - 1); dS(x - 1).  So its matrix instructions come while the other wavefront has its exponentials.
+    __builtin_amdgcn_s_setprio(2);
     bf16x8 w[2] = {zero_bf16x8(), zero_bf16x8()};
 #pragma unroll
     for (int ks = 0; ks < NOP; ++ks) op[ks] = zero_bf16x8();
@@ -989,7 +990,7 @@ __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))
   }
   if (MODE == kJoin)
     for (int z = 0; z < P.near_parts; ++z) take(part_sums(z));
-  if (ku < min(P.sinks, n) && P.sinks <= kFarSinks) {
+  if (ku < min(P.sinks, n) && P.sinks <= kFarSinks && P.far_rows > 0) {
     const int end = near_end(u0, n, P.window), have = (n - end + P.far_rows - 1) / P.far_rows;
     const int64_t it = far0 + (int64_t)(ku / kFarKeys) * segments;
     for (int z = 0; z < have; ++z) take(far_sums(it + z));
@@ -1031,7 +1032,7 @@ int launch_window_fwd(const WindowParams& P, int D, int dtype, bool paged, int64
     constexpr int DD = decltype(d)::value;
     constexpr bool PAGED = decltype(pg)::value;
     if (dtype == SB_F32) hipLaunchKernelGGL((window_fwd_f32_kernel<float, DD, PAGED>), grid, dim3(256), 0, st, P);
-    else hipLaunchKernelGGL((window_fwd_kernel<DD, PAGED>), grid, dim3(512), 0, st, P);
+    else hipLaunchKernelGGL((window_fwd_kernel<DD, PAGED>), grid, dim3(64 * kWaves), 0, st, P);
   };
   auto with_d = [&](auto pg) { if (D == 128) launch(std::integral_constant<int, 128>(), pg); else launch(std::integral_constant<int, 64>(), pg); };
   if (paged) with_d(std::true_type()); else with_d(std::false_type());
@@ -1054,12 +1055,17 @@ static WindowParams window_params(const Geo& g, const sb_problem* p, int32_t win
   return P;
 }
 
-// Far rows a far item takes: short enough that a long sequence's sinks are many workgroups' work, and no more than 32 of them to a block of sinks, whose sums its own workgroup adds.
-static int far_rows_of(const int32_t* cu, int S, int window) {
-  int64_t most = 0;
+static int64_t longest(const int32_t* cu, int S) {
+  int64_t n = 0;
   for (int s = 0; s < S; ++s)
-    if (cu[s + 1] - cu[s] > most) most = cu[s + 1] - cu[s];
-  const int64_t rows = (most - window + 31) / 32;
+    if (cu[s + 1] - cu[s] > n) n = cu[s + 1] - cu[s];
+  return n;
+}
+// Far rows a far item takes: short enough that a long sequence's sinks are many workgroups' work, and no more than 32 of them to a block of sinks, whose sums its own workgroup adds.  None
+// where all of a sequence is at most twice an ordinary item's rows: a launch of their own costs more than the sinks' workgroups are longer then (2039 tokens in short sequences: 20 us).
+static int far_rows_of(int64_t longest, int window) {
+  if (longest <= 2 * ((int64_t)window + kDkvKeys)) return 0;
+  const int64_t rows = (longest - window + 31) / 32;
   return rows < 256 ? 256 : (int)((rows + 31) / 32 * 32);
 }
 struct WindowWs { size_t lse2, dr, stats, partials, parts, bytes; int64_t far; int far_rows, near_parts; };
@@ -1070,7 +1076,8 @@ static WindowWs window_bwd_ws(const Geo& g, const int32_t* cu, int window, int s
   w.lse2 = o;  o = align_up(o + sizeof(float) * rows * f32);
   w.dr = o;    o = align_up(o + sizeof(float) * rows * f32);
   w.stats = o; o = align_up(o + 2 * sizeof(bf16x8) * rows * (1 - f32));
-  w.far_rows = far_rows_of(cu, g.S, window);
+  const int64_t n = longest(cu, g.S);
+  w.far_rows = far_rows_of(n, window);
   if (g.dtype == SB_BF16)
     for (int s = 0; s < g.S; ++s) w.far += far_items(cu[s + 1] - cu[s], window, sinks, w.far_rows);
   w.partials = o; o = align_up(o + (size_t)w.far * g.Hkv * 2 * kFarKeys * g.D * sizeof(float));
@@ -1078,10 +1085,7 @@ static WindowWs window_bwd_ws(const Geo& g, const int32_t* cu, int window, int s
   w.near_parts = 1;
   if (g.dtype == SB_BF16) {
     const int64_t items = row_tiles(cu, g.S, 1, kDkvKeys) * g.Hkv;
-    int64_t most = 0;  // tokens of an item
-    for (int s = 0; s < g.S; ++s)
-      if (cu[s + 1] - cu[s] > most) most = cu[s + 1] - cu[s];
-    if ((int64_t)window + kDkvKeys < most) most = (int64_t)window + kDkvKeys;
+    const int64_t most = n < (int64_t)window + kDkvKeys ? n : (int64_t)window + kDkvKeys;  // tokens of an item
     int64_t parts = items > 0 ? 384 / items : 1;
     if (parts > most * g.G / (32 * 16)) parts = most * g.G / (32 * 16);
     if (parts > 8) parts = 8;
@@ -1144,7 +1148,7 @@ int sb_window_attn_bwd(const sb_problem* p, int32_t window, int32_t sinks, const
   P.near_parts = w.near_parts;
   const bool f32 = g.dtype == SB_F32;
   const int64_t rows = (int64_t)g.T * g.Hq, per = 1024 / g.D;
-  const int64_t q_items = row_tiles(cu, g.S, g.G, f32 ? 32 : 256) * g.Hkv, k_items = row_tiles(cu, g.S, 1, f32 ? 32 : kDkvKeys) * g.Hkv;
+  const int64_t q_items = row_tiles(cu, g.S, g.G, forward_rows(g.dtype)) * g.Hkv, k_items = row_tiles(cu, g.S, 1, f32 ? 32 : kDkvKeys) * g.Hkv;
   dim3 delta_grid, q_grid, k_grid, far_grid, part_grid;
   if ((rc = grid_of((rows + per - 1) / per, &delta_grid)) != SB_OK || (rc = grid_of(q_items, &q_grid)) != SB_OK ||
       (rc = grid_of(k_items, &k_grid)) != SB_OK || (rc = grid_of(w.far * g.Hkv, &far_grid)) != SB_OK ||
@@ -1159,7 +1163,7 @@ int sb_window_attn_bwd(const sb_problem* p, int32_t window, int32_t sinks, const
         SB_LAUNCH_CHECK("window_delta_kernel");
         hipLaunchKernelGGL((window_dq_f32_kernel<float, D>), q_grid, dim3(256), 0, st, P);
       } else {
-        hipLaunchKernelGGL((window_dq_kernel<D>), q_grid, dim3(512), 0, st, P);
+        hipLaunchKernelGGL((window_dq_kernel<D>), q_grid, dim3(64 * kWaves), 0, st, P);
       }
       SB_LAUNCH_CHECK("window_dq_kernel");
     }
