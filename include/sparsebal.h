@@ -317,7 +317,8 @@ int sb_rope_apply(const sb_problem *p, const sb_rope *r, const int32_t *position
  * copies); block_size, select_mode and the budgets are not read and may be anything.  SB_F32 tensors are computed in float32 throughout (matrix
  * instructions of that type), not rounded to bfloat16.  Non-finite values: a row's output depends on the elements of keys that it sees and, where a
  * V is not finite, on those of other keys of its sequence in the same 64-token tiles; in the backward also of Q, K and dO there.
- * Deterministic.  ws: dev, sizes from sb_window_ws_bytes (host only; either output may be null). */
+ * Deterministic.  Tensors and ws start at multiples of 16 bytes; T * Hq/Hkv fits 31 bits.  ws: dev, sizes from sb_window_ws_bytes (host only; either output
+ * may be null); of zero bytes it may be null. */
 int sb_window_ws_bytes(const sb_problem *p, int32_t window, int32_t sinks, int64_t *fwd_bytes_out, int64_t *bwd_bytes_out);
 int sb_window_attn_fwd(const sb_problem *p, int32_t window, int32_t sinks, const void *q, const void *k, const void *v, void *o, float *lse,
                        void *ws, void *stream);
@@ -329,7 +330,7 @@ int sb_window_attn_bwd(const sb_problem *p, int32_t window, int32_t sinks, const
  * Tokens j*page_size .. (j+1)*page_size - 1 of sequence s live in page page_table[s][j].  An entry outside 0 .. num_pages - 1 is no page: nothing
  * is written there and its keys are seen by no row; so are tokens from max_pages*page_size on.  Nothing of a page behind the sequence's last token is
  * used, whatever it holds.  Pages may be shared between sequences.  All sizes that change from step to step are on the device, so that
- * a captured graph can be replayed with other lengths within max_new and max_pages. */
+ * a captured graph can be replayed with other lengths within max_new and max_pages.  Tensors, pages and ws start at multiples of 16 bytes. */
 typedef struct sb_cache {
   int32_t num_pages, page_size; /* page_size: a power of two, 16 .. 1024 */
   int32_t num_kv_heads, head_dim, dtype; /* head_dim 64 or 128; SB_BF16 | SB_F32 */

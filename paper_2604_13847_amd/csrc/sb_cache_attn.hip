@@ -382,6 +382,8 @@ int sb_cache_attn(const sb_cache* c, const sb_chunk* n, int32_t window, int32_t 
   if (n->total_new == 0 || n->num_seqs == 0 || n->max_new == 0) return SB_OK;
   if (!q || !o || !lse) { set_error("null argument"); return SB_ERR_INVALID_ARG; }
   if ((rc = check_cache_arrays(c, n)) != SB_OK) return rc;
+  const void* const buffers[] = {q, o, c->k, c->v, ws};
+  if ((rc = check_aligned(buffers, 5)) != SB_OK) return rc;
   WindowParams P{};
   P.q = q; P.o = o; P.lse = lse; P.cu = n->cu_new; P.cached = n->cached; P.max_new = n->max_new;
   P.T = n->total_new; P.S = n->num_seqs; P.Hq = n->num_q_heads; P.Hkv = c->num_kv_heads; P.G = P.Hq / P.Hkv;
@@ -399,8 +401,8 @@ int sb_cache_attn(const sb_cache* c, const sb_chunk* n, int32_t window, int32_t 
   const bool f32 = c->dtype == SB_F32;
   const int64_t rows = P.T, few_seq_rows = kFewRows / P.G < P.max_new ? kFewRows / P.G : P.max_new;
   dim3 grid, all_rows, few_rows;
-  if ((rc = grid_of(plan.few.items * P.Hkv * plan.few.splits, &grid)) != SB_OK || (rc = grid_of(rows * P.Hq, &all_rows)) != SB_OK ||
-      (rc = grid_of(few_seq_rows * P.S * P.Hq, &few_rows)) != SB_OK)
+  if ((rc = grid_of(plan.few.items * P.Hkv * plan.few.splits, 256, &grid)) != SB_OK || (plan.many.splits > 1 && (rc = grid_of(rows * P.Hq, 256, &all_rows)) != SB_OK) ||
+      (plan.few.splits > 1 && (rc = grid_of(few_seq_rows * P.S * P.Hq, 256, &few_rows)) != SB_OK))
     return rc;
   KernelTimer kt(K_CACHE_ATTN, st);
   auto merge = [&](dim3 workgroups, int seq_rows) {

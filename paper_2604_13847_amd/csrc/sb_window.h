@@ -222,7 +222,8 @@ __device__ inline void store_tile(char* buf, int lane, V value, A address) {
   }
 }
 
-int grid_of(int64_t workgroups, dim3* grid);
+int grid_of(int64_t workgroups, int threads, dim3* grid);  // a launch has fewer than 2^32 threads
+int check_aligned(const void* const* p, int n);           // tensors are read and written 16 bytes at a time
 int check_rows(int64_t tokens, int G);  // flattened rows fit 31 bits
 constexpr int kSplitRows = 32;  // flattened rows of an item of cache_split_kernel
 int64_t row_tiles(const int32_t* cu_host, int S, int G, int rows);  // of a packed batch

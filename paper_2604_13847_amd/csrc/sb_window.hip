@@ -1017,16 +1017,21 @@ int64_t row_tiles(const int32_t* cu, int S, int G, int rows) {
 }
 int64_t row_tiles_most(int total, int S, int G, int rows) { return ((int64_t)total * G) / rows + S; }
 
-int grid_of(int64_t workgroups, dim3* grid) {
-  if (workgroups > 0x3fffffll) { set_error("too many tiles for one launch"); return SB_ERR_UNSUPPORTED; }
+int grid_of(int64_t workgroups, int threads, dim3* grid) {
+  if (workgroups * threads > 0xffffffffll) { set_error("too many tiles for one launch"); return SB_ERR_UNSUPPORTED; }
   *grid = dim3((unsigned)workgroups);
+  return SB_OK;
+}
+int check_aligned(const void* const* p, int n) {
+  for (int i = 0; i < n; ++i)
+    if ((uintptr_t)p[i] % 16 != 0) { set_error("a buffer does not start at a multiple of 16 bytes"); return SB_ERR_INVALID_ARG; }
   return SB_OK;
 }
 
 int launch_window_fwd(const WindowParams& P, int D, int dtype, bool paged, int64_t tiles, hipStream_t st) {
   const int64_t items = tiles * P.Hkv * (paged ? P.splits : 1);
   dim3 grid;
-  const int rc = grid_of(items, &grid);
+  const int rc = grid_of(items, dtype == SB_F32 ? 256 : 64 * kWaves, &grid);
   if (rc != SB_OK) return rc;
   auto launch = [&](auto d, auto pg) {
     constexpr int DD = decltype(d)::value;
@@ -1115,11 +1120,13 @@ int sb_window_ws_bytes(const sb_problem* p, int32_t window, int32_t sinks, int64
 int sb_window_attn_fwd(const sb_problem* p, int32_t window, int32_t sinks, const void* q, const void* k, const void* v, void* o, float* lse, void* ws,
                        void* stream) {
   Geo g;
-  const int rc = check_window(p, window, sinks, &g);
+  int rc = check_window(p, window, sinks, &g);
   if (rc != SB_OK) return rc;
   if (g.T == 0) return SB_OK;
   if (!p->cu_seqlens_dev) { set_error("cu_seqlens_dev is required"); return SB_ERR_INVALID_ARG; }
   if (!q || !k || !v || !o || !lse) { set_error("null argument"); return SB_ERR_INVALID_ARG; }
+  const void* const buffers[] = {q, k, v, o};
+  if ((rc = check_aligned(buffers, 4)) != SB_OK) return rc;
   WindowParams P = window_params(g, p, window, sinks);
   P.q = q; P.k = k; P.v = v; P.o = o; P.lse = lse;
   KernelTimer kt(K_WINDOW_FWD, (hipStream_t)stream);
@@ -1134,6 +1141,8 @@ int sb_window_attn_bwd(const sb_problem* p, int32_t window, int32_t sinks, const
   if (g.T == 0) return SB_OK;
   if (!p->cu_seqlens_dev) { set_error("cu_seqlens_dev is required"); return SB_ERR_INVALID_ARG; }
   if (!q || !k || !v || !o || !lse || !d_o || !dq || !dk || !dv || !ws) { set_error("null argument"); return SB_ERR_INVALID_ARG; }
+  const void* const buffers[] = {q, k, v, o, d_o, dq, dk, dv, ws};
+  if ((rc = check_aligned(buffers, 9)) != SB_OK) return rc;
   const hipStream_t st = (hipStream_t)stream;
   WindowParams P = window_params(g, p, window, sinks);
   P.q = q; P.k = k; P.v = v; P.o_in = o; P.lse = (float*)lse; P.d_o = d_o; P.dq = dq; P.dk = dk; P.dv = dv;
@@ -1150,9 +1159,9 @@ int sb_window_attn_bwd(const sb_problem* p, int32_t window, int32_t sinks, const
   const int64_t rows = (int64_t)g.T * g.Hq, per = 1024 / g.D;
   const int64_t q_items = row_tiles(cu, g.S, g.G, forward_rows(g.dtype)) * g.Hkv, k_items = row_tiles(cu, g.S, 1, f32 ? 32 : kDkvKeys) * g.Hkv;
   dim3 delta_grid, q_grid, k_grid, far_grid, part_grid;
-  if ((rc = grid_of((rows + per - 1) / per, &delta_grid)) != SB_OK || (rc = grid_of(q_items, &q_grid)) != SB_OK ||
-      (rc = grid_of(k_items, &k_grid)) != SB_OK || (rc = grid_of(w.far * g.Hkv, &far_grid)) != SB_OK ||
-      (rc = grid_of(k_items * w.near_parts, &part_grid)) != SB_OK)
+  if ((rc = grid_of((rows + per - 1) / per, 256, &delta_grid)) != SB_OK || (rc = grid_of(q_items, 256, &q_grid)) != SB_OK ||
+      (rc = grid_of(k_items, 4 * kDkvKeys, &k_grid)) != SB_OK || (rc = grid_of(w.far * g.Hkv, 4 * kFarKeys, &far_grid)) != SB_OK ||
+      (rc = grid_of(k_items * w.near_parts, 4 * kDkvKeys, &part_grid)) != SB_OK)
     return rc;
   auto launch = [&](auto d) {
     constexpr int D = decltype(d)::value;

@@ -121,6 +121,18 @@ def test_window_refusals():
         a = [BUF] * 10
         a[missing] = None
         refused(L.sb_window_attn_bwd(pb.ref(), 8, 2, *a, None), -1, "null argument")
+    for odd in (0, 1, 2, 3):
+        a = [BUF] * 5
+        a[odd] = C.c_void_p(4096 + 8)
+        refused(L.sb_window_attn_fwd(pb.ref(), 8, 2, *a, BUF, None), -1, "16 bytes")
+    for odd in (0, 1, 2, 3, 5, 6, 7, 8, 9):
+        a = [BUF] * 10
+        a[odd] = C.c_void_p(4096 + 2)
+        refused(L.sb_window_attn_bwd(pb.ref(), 8, 2, *a, None), -1, "16 bytes")
+    # flattened rows pass 32 bits: 2^26 tokens, 64 query heads on one KV head
+    cu = np.array([0, 1 << 26], dtype=np.int32)
+    refused(L.sb_window_attn_fwd(problem(total_tokens=1 << 26, num_seqs=1, cu_seqlens_host=cu.ctypes.data, num_q_heads=64, num_kv_heads=1).ref(), 8, 2, BUF, BUF, BUF, BUF, BUF, BUF,
+                                 None), -2, "32 bits")
     # budgets and blocks are not read
     pb = problem(topk_host=None, topk_dev=None, block_size=7, select_mode=9)
     assert sb.sb_window_ws_bytes(pb, 8, 2)[1] > 0
@@ -159,7 +171,13 @@ def test_cache_argument_refusals():
     refused(L.sb_cache_attn(c, n, 0, 2, BUF, BUF, BUF, BUF, None), -1, "window")
     refused(L.sb_cache_attn(c, n, 8, -2, BUF, BUF, BUF, BUF, None), -1, "sinks")
     refused(L.sb_cache_attn(c, n, 8, 2, None, BUF, BUF, BUF, None), -1, "null argument")
+    refused(L.sb_cache_attn(c, n, 8, 2, C.c_void_p(4096 + 4), BUF, BUF, BUF, None), -1, "16 bytes")
+    refused(L.sb_cache_attn(*serving(dict(k=4096 + 8)), 8, 2, BUF, BUF, BUF, BUF, None), -1, "16 bytes")
     refused(L.sb_cache_attn_ws_bytes(c, n, 8, 2, None), -1, "null output")
+    # runs of keys need a workspace: 64 sequences of 30000 tokens
+    many = serving(dict(max_pages=500), dict(num_seqs=64, total_new=64, max_new=1, max_length=30000))
+    assert L.sb_cache_attn_ws_bytes(*many, 8000, 2, C.byref(out)) == 0 and out.value >= 64 * 4 * 128 * 4
+    refused(L.sb_cache_attn(*many, 8000, 2, BUF, BUF, BUF, None, None), -1, "null argument")
     refused(L.sb_cache_attn_ws_bytes(c, n, 0, 2, C.byref(out)), -1, "window")
     refused(L.sb_cache_append(c, n, sb.Rope(64).ref(), BUF, z, BUF, z, BUF, z, None, None), -1, "q without q_out")
     refused(L.sb_cache_append(c, n, None, None, z, None, z, BUF, z, None, None), -1, "null argument")
