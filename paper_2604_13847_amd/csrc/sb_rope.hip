@@ -49,13 +49,17 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeParams P) {
   const int64_t tok0 = ((int64_t)blockIdx.x * 4 + wave) * P.run;
   float2* const cs = table[wave];
   const double turns = lane < P.rot / 2 ? P.turns[lane] : 0.0;
+  int s = 0, first = 0, behind = -1;  // the token's sequence, its first row and the one behind its last
   for (int64_t tok = tok0; tok < min(tok0 + P.run, (int64_t)P.T); ++tok) {
-    int s = 0;
     int64_t pos;
     if (PAGED || !P.positions) {
-      s = sequence_of(P.cu, P.S, (int)tok, lane);
-      if (s >= P.S) break;  // behind the last sequence
-      pos = tok - P.cu[s];
+      if (tok >= behind) {
+        s = sequence_of(P.cu, P.S, (int)tok, lane);
+        if (s >= P.S) break;  // behind the last sequence
+        first = P.cu[s];
+        behind = P.cu[s + 1];
+      }
+      pos = tok - first;
       if (PAGED) {
         if (pos < 0 || pos >= P.max_new) continue;
         pos += max(P.cached[s], 0);

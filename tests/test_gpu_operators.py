@@ -416,6 +416,68 @@ def test_training_pass_in_a_captured_graph():
         assert all(torch.equal(a, b) for a, b in zip(got, (*buf, lse)))
 
 
+def test_pages_behind_four_gigabytes():
+    """A cache of 6 GB of keys and as much of values, its last pages in use; two sequences share their first page."""
+    Hq, Hkv, D, page = 16, 8, 128, 64
+    pages = 46000
+    kp, vp = (torch.empty(pages, Hkv, page, D, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    assert kp.numel() * 2 > 5 << 30
+    table = torch.stack([pages - 1 - torch.arange(12, dtype=torch.int32, device=DEV), pages - 101 - torch.arange(12, dtype=torch.int32, device=DEV)])
+    table[1, 0] = table[0, 0]
+    rope = sb.Rope(D)
+    for new in ([1, 1], [300, 1]):
+        have = [400, 330]
+        k, v = ([normal(20 * j + i, have[i] + new[i], Hkv, D) for i in (0, 1)] for j in (1, 2))
+        k[1][:page], v[1][:page] = k[0][:page], v[0][:page]
+        for x, p in ((k, kp), (v, vp)):
+            for s in (0, 1):
+                u = torch.arange(have[s], device=DEV)
+                p[table[s, u // page].long(), :, u % page] = x[s][: have[s]]
+        cu = torch.tensor([0, new[0], sum(new)], dtype=torch.int32, device=DEV)
+        cache = sb.Cache(kp, vp, table)
+        chunk = sb.Chunk(cu, torch.tensor(have, dtype=torch.int32, device=DEV), Hq, sum(new), max(new), 1000)
+        q = normal(9, sum(new), Hq, D)
+        kn, vn = (torch.cat([x[s][have[s]:] for s in (0, 1)]) for x in (k, v))
+        qn = sb.sb_cache_append(cache, chunk, kn, vn, rope=rope, q=q)
+        turns = torch.tensor(rope.c.turns[: D // 2], dtype=torch.float64, device=DEV)
+        o, lse = sb.sb_cache_attn(cache, chunk, qn)
+        for s in (0, 1):
+            u = torch.arange(have[s] + new[s], device=DEV)
+            held = kp[table[s, u // page].long(), :, u % page]
+            turned, tol = ref.turn(k[s][have[s]:].double(), u[have[s]:], turns, 1.0, True)
+            ref.check("k", held[have[s]:], turned, tol + ref.HALF[torch.bfloat16] * turned.abs())
+            assert torch.equal(held[: have[s]], k[s][: have[s]])
+            rows = slice(int(cu[s]), int(cu[s + 1]))
+            r = ref.Attention(qn[rows].double(), held.double(), v[s].double(), ref.visible(u[have[s]:], u, NONE, 0), D ** -0.5, ref.HALF[torch.bfloat16])
+            ref.check("o", o[rows], r.o, r.o_tol)
+            ref.check("lse", lse[:, rows], r.lse, r.lse_tol)
+
+
+def test_rows_behind_four_gigabytes():
+    """540001 tokens of 32 query heads: queries, outputs and their gradients pass 4 GB each.  The last rows against the reference."""
+    T, Hq, Hkv, D, window, tail = 540001, 32, 1, 128, 70, 300
+    pb = batch((T,), Hq, Hkv, D)
+    q, k, v, do = (normal(i, T, h, D) for i, h in enumerate((Hq, Hkv, Hkv, Hq)))
+    assert q.numel() * 2 > 4 << 30
+    rope = sb.Rope(D)
+    turned = sb.sb_rope_apply(pb, rope, q, k)
+    turns = torch.tensor(rope.c.turns[: D // 2], dtype=torch.float64, device=DEV)
+    for x, y in zip((q, k), turned):
+        want, tol = ref.turn(x[-tail:].double(), torch.arange(T - tail, T, device=DEV), turns, 1.0, True)
+        ref.check("rope", y[-tail:], want, tol + ref.HALF[torch.bfloat16] * want.abs())
+    del turned, x, y
+    o, lse = sb.sb_window_attn_fwd(pb, window, 0, q, k, v)
+    dq, dk, dv = sb.sb_window_attn_bwd(pb, window, 0, q, k, v, o, lse, do)
+    assert all(bool(torch.isfinite(x).all()) for x in (lse, dk, dv))
+    a = T - tail
+    u = torch.arange(a, T, device=DEV)
+    r = ref.Attention(q[a:].double(), k[a:].double(), v[a:].double(), ref.visible(u, u, window, 0), D ** -0.5, ref.HALF[torch.bfloat16], do[a:].double())
+    near = slice(window, None)   # rows that see none of the keys in front of the tail, and keys that all their rows are there for
+    for n, x in (("o", o), ("dq", dq), ("dk", dk), ("dv", dv)):
+        ref.check(n, x[a:][near], getattr(r, n)[near], getattr(r, n + "_tol")[near])
+    ref.check("lse", lse[:, a:][:, near], r.lse[:, near], r.lse_tol[:, near])
+
+
 def test_on_another_stream():
     pb, x, got = run_window((700,), 4, 2, 128, 130, 9, "bf16")
     q, k, v, do = x
