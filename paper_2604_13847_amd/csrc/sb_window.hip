@@ -750,6 +750,29 @@ __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))
   }
   const int ku = u0 + 32 * pair, kl = min(ku + 31, n - 1);  // this pair's keys (none: ku >= n)
   const int key = min(ku + l32, n - 1);
+  // sums left in float32: of a far item [item][KV head][dV, dK][register][lane], of a part [tile][part][KV head][pair][dV, dK][register][lane]
+  auto far_sums = [&](int64_t it) { return P.partials + ((it * P.Hkv + g) * 2 + (second ? 1 : 0)) * (kNr * 64) + lane; };
+  auto part_sums = [&](int z) { return P.parts + ((((tile_id * P.near_parts + z) * P.Hkv + g) * PAIRS + pair) * 2 + (second ? 1 : 0)) * (kNr * 64) + lane; };
+  const bool has_far = MODE != kFar && P.far_rows > 0 && P.sinks <= kFarSinks && ku < min(P.sinks, n);
+  const int far_end = near_end(u0, n, P.window), far_count = has_far ? (n - far_end + P.far_rows - 1) / P.far_rows : 0;
+  const int64_t far_first = far0 + (int64_t)(ku / kFarKeys) * segments;
+  if constexpr (MODE == kJoin) {  // 32 columns a workgroup
+    const int dt = blockIdx.y;
+    float sum[16] = {};
+    auto take = [&](const float* from) __attribute__((always_inline)) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) sum[v] += from[(16 * dt + v) * 64];
+    };
+#pragma unroll 4
+    for (int z = 0; z < P.near_parts; ++z) take(part_sums(z));
+    for (int z = 0; z < far_count; ++z) take(far_sums(far_first + z));
+    if (ku + l32 >= n) return;
+    const float f = second ? P.scale : 1.0f;
+    bf16* const to = (bf16*)(second ? P.dk : P.dv) + ((int64_t)(seq0 + ku + l32) * P.Hkv + g) * D + 32 * dt + 4 * hf;
+#pragma unroll
+    for (int vg = 0; vg < 4; ++vg) store4(to + 8 * vg, f32x4{sum[4 * vg] * f, sum[4 * vg + 1] * f, sum[4 * vg + 2] * f, sum[4 * vg + 3] * f});
+    return;
+  }
   int m0 = r0 * P.G, m1 = r1 * P.G;
   if (MODE == kPart) {
     // tokens in equal shares, of whole stages
@@ -759,7 +782,7 @@ __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))
     m0 = r0 * P.G;
     m1 = r1 * P.G;
   }
-  const int stages = MODE == kJoin ? 0 : (m1 - m0 + 31) / 32;
+  const int stages = (m1 - m0 + 31) / 32;
   // The stages are walked in a circle from y0 on: where a row's number is a multiple of an ordinary item's rows.  Neighbouring items, which an XCD works on at the same time and which have
   // most of their rows in common, so ask for the same rows at about the same time and meet them in the XCD's L2, which could not hold the rows of one item for the next.
   int y0 = 0;
@@ -903,9 +926,8 @@ __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))
   };
   auto after = [](int slot) { return slot == kSlots - 1 ? 0 : slot + 1; };
   int slot = 0;
-  if (MODE != kJoin) turn(0);
-  if (MODE == kJoin) {
-  } else if (!second) {
+  turn(0);
+  if (!second) {
     // stage x: S(x); P(x); dV += P(x)^T dO(x)
     less = ld_stat(0);
 #pragma unroll
@@ -965,38 +987,23 @@ __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))
   }
   wait_vmcnt<0>();
 
-  // sums left in float32: of a far item [item][KV head][dV, dK][register][lane], of a part [tile][part][KV head][pair][dV, dK][register][lane]
-  auto leave = [&](float* to) {
+  if (MODE == kFar || MODE == kPart) {
+    float* const to = MODE == kFar ? far_sums(far0 + item) : part_sums((int)(tile_part % (unsigned)P.near_parts));
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) to[(16 * dt + v) * 64 + lane] = acc[dt][v];
-  };
-  auto take = [&](const float* from) {
+      for (int v = 0; v < 16; ++v) to[(16 * dt + v) * 64] = acc[dt][v];
+    return;
+  }
+  for (int z = 0; z < far_count; ++z) {
+    const float* const from = far_sums(far_first + z);
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) acc[dt][v] += from[(16 * dt + v) * 64 + lane];
-  };
-  auto far_sums = [&](int64_t it) { return P.partials + ((it * P.Hkv + g) * 2 + (second ? 1 : 0)) * (kNr * 64); };
-  auto part_sums = [&](int z) { return P.parts + ((((tile_id * P.near_parts + z) * P.Hkv + g) * PAIRS + pair) * 2 + (second ? 1 : 0)) * (kNr * 64); };
-  if (MODE == kFar) {
-    leave(far_sums(far0 + item));
-    return;
-  }
-  if (MODE == kPart) {
-    leave(part_sums((int)(tile_part % (unsigned)P.near_parts)));
-    return;
-  }
-  if (MODE == kJoin)
-    for (int z = 0; z < P.near_parts; ++z) take(part_sums(z));
-  if (ku < min(P.sinks, n) && P.sinks <= kFarSinks && P.far_rows > 0) {
-    const int end = near_end(u0, n, P.window), have = (n - end + P.far_rows - 1) / P.far_rows;
-    const int64_t it = far0 + (int64_t)(ku / kFarKeys) * segments;
-    for (int z = 0; z < have; ++z) take(far_sums(it + z));
+      for (int v = 0; v < 16; ++v) acc[dt][v] += from[(16 * dt + v) * 64];
   }
   __syncthreads();  // the stages' LDS is free
-  static_assert(NW * 32 * ROW_B <= (int)sizeof(stage) + (int)sizeof(pbuf) || MODE == kFar, "every wavefront's rows");
+  static_assert(NW * 32 * ROW_B <= (int)sizeof(stage) + (int)sizeof(pbuf) || MODE != kWhole, "every wavefront's rows");
   char* const buf = wave * 32 * ROW_B + 32 * ROW_B <= (int)sizeof(stage) ? &stage[0][0] + wave * 32 * ROW_B : (char*)&pbuf[0][0][0] + (wave * 32 * ROW_B - (int)sizeof(stage) / (32 * ROW_B) * 32 * ROW_B);
   const float f = second ? P.scale : 1.0f;
   store_tile<D>(buf, lane, [&](int dt, int v) __attribute__((always_inline)) { return acc[dt][v] * f; },
@@ -1086,12 +1093,12 @@ static WindowWs window_bwd_ws(const Geo& g, const int32_t* cu, int window, int s
   if (g.dtype == SB_BF16)
     for (int s = 0; s < g.S; ++s) w.far += far_items(cu[s + 1] - cu[s], window, sinks, w.far_rows);
   w.partials = o; o = align_up(o + (size_t)w.far * g.Hkv * 2 * kFarKeys * g.D * sizeof(float));
-  // Parts where items are fewer than CUs: up to 8, of 16 stages at least
+  // Parts where items are fewer than workgroups fit the chip (a CU's LDS holds one at head_dim 128, two at 64): up to 8, of 16 stages at least
   w.near_parts = 1;
   if (g.dtype == SB_BF16) {
     const int64_t items = row_tiles(cu, g.S, 1, kDkvKeys) * g.Hkv;
     const int64_t most = n < (int64_t)window + kDkvKeys ? n : (int64_t)window + kDkvKeys;  // tokens of an item
-    int64_t parts = items > 0 ? 384 / items : 1;
+    int64_t parts = items > 0 ? (g.D == 128 ? 256 : 512) / items : 1;
     if (parts > most * g.G / (32 * 16)) parts = most * g.G / (32 * 16);
     if (parts > 8) parts = 8;
     if (parts > 1) w.near_parts = (int)parts;
@@ -1187,7 +1194,7 @@ int sb_window_attn_bwd(const sb_problem* p, int32_t window, int32_t sinks, const
       if (w.near_parts > 1) {
         hipLaunchKernelGGL((window_dkv_kernel<D, kDkvKeys / 32, kPart>), part_grid, dim3(kDkvKeys * 4), 0, st, P);
         SB_LAUNCH_CHECK("window_dkv_kernel, parts");
-        hipLaunchKernelGGL((window_dkv_kernel<D, kDkvKeys / 32, kJoin>), k_grid, dim3(kDkvKeys * 4), 0, st, P);
+        hipLaunchKernelGGL((window_dkv_kernel<D, kDkvKeys / 32, kJoin>), dim3(k_grid.x, D / 32), dim3(kDkvKeys * 4), 0, st, P);
       } else {
         hipLaunchKernelGGL((window_dkv_kernel<D, kDkvKeys / 32, kWhole>), k_grid, dim3(kDkvKeys * 4), 0, st, P);
       }
