@@ -702,10 +702,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
 // Sinks are seen by all rows of their sequence.  The rows behind a sink tile's ordinary ones (far rows) are the work of other workgroups (kFar), far_rows tokens each, that leave their
 // sums in float32; the tile's own workgroup, launched after them, adds them in order.  So the result does not depend on who is ahead, and no workgroup has more than its share.
 constexpr int kDkvKeys = 128;   // keys of a workgroup, but of kFar
-constexpr int kFarKeys = 32;    // of kFar
 constexpr int kFarSinks = 512;  // with more sinks than this there are sink tiles enough to fill the chip: their own workgroups take all rows
 // Far items of a sequence of n tokens: far_blocks blocks of sinks, far_segments each (some may be empty: the first rows of a block's last ones).
-__host__ __device__ inline int far_blocks(int n, int sinks) { return ((sinks < n ? sinks : n) + kFarKeys - 1) / kFarKeys; }
+// The rows are read once a block, at the rate of the memory, so a block is 64 sinks where there are more than 32 (65536 tokens, 14/2 heads, 64 sinks: 95 us in two blocks).
+__host__ __device__ inline int far_keys(int sinks) { return sinks > 32 ? 64 : 32; }
+__host__ __device__ inline int far_blocks(int n, int sinks) { return ((sinks < n ? sinks : n) + far_keys(sinks) - 1) / far_keys(sinks); }
 __host__ __device__ inline int far_segments(int n, int window, int far_rows) { return far_rows > 0 && n > window ? (n - window + far_rows - 1) / far_rows : 0; }
 __host__ __device__ inline int64_t far_items(int n, int window, int sinks, int far_rows) {
   return sinks > kFarSinks ? 0 : (int64_t)far_blocks(n, sinks) * far_segments(n, window, far_rows);
@@ -721,7 +722,7 @@ enum DkvMode { kWhole, kFar, kPart, kJoin };
 template <int D, int PAIRS, DkvMode MODE>
 __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))) void window_dkv_kernel(WindowParams P) {
   constexpr int ROW_B = D * 2, TILE_B = 32 * ROW_B, NOP = D / 16, KEYS = 32 * PAIRS, NW = 2 * PAIRS;
-  constexpr int kSlots = 5, kAhead = 3, STAT_B = 1024, STAGE_B = 2 * TILE_B;
+  constexpr int kSlots = MODE == kFar ? 4 : 5, kAhead = kSlots - 2, STAT_B = 1024, STAGE_B = 2 * TILE_B;
   constexpr int kNr = 16 * (D / 32);  // accumulator registers
   __shared__ __attribute__((aligned(1024))) char stage[kSlots][STAGE_B];  // Q, dO
   __shared__ __attribute__((aligned(1024))) float pbuf[2][PAIRS][16 * 64];
@@ -763,7 +764,7 @@ __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))
   const int item = __builtin_amdgcn_readfirstlane((int)x);
   int u0, r0, r1;  // first key; rows: tokens r0 .. r1 - 1
   if (MODE == kFar) {
-    u0 = item / segments * KEYS;
+    u0 = item / segments * KEYS;  // (KEYS is far_keys(sinks))
     const int64_t from = (int64_t)near_end(u0, n, P.window) + (int64_t)(item % segments) * P.far_rows;
     if (from >= n) return;
     r0 = (int)from;
@@ -775,12 +776,13 @@ __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))
   }
   const int ku = u0 + 32 * pair, kl = min(ku + 31, n - 1);  // this pair's keys (none: ku >= n)
   const int key = min(ku + l32, n - 1);
-  // sums left in float32: of a far item [item][KV head][dV, dK][register][lane], of a part [tile][part][KV head][pair][dV, dK][register][lane]
-  auto far_sums = [&](int64_t it) { return P.partials + ((it * P.Hkv + g) * 2 + (second ? 1 : 0)) * (kNr * 64) + lane; };
+  // sums left in float32: of a far item [item][KV head][pair][dV, dK][register][lane], of a part [tile][part][KV head][pair][dV, dK][register][lane]
+  const int block = far_keys(P.sinks) / 32;  // pairs of a far item
+  auto far_sums = [&](int64_t it) { return P.partials + (((it * P.Hkv + g) * block + ku / 32 % block) * 2 + (second ? 1 : 0)) * (kNr * 64) + lane; };
   auto part_sums = [&](int z) { return P.parts + ((((tile_id * P.near_parts + z) * P.Hkv + g) * PAIRS + pair) * 2 + (second ? 1 : 0)) * (kNr * 64) + lane; };
   const bool has_far = MODE != kFar && P.far_rows > 0 && P.sinks <= kFarSinks && ku < min(P.sinks, n);
   const int far_end = near_end(u0, n, P.window), far_count = has_far ? (n - far_end + P.far_rows - 1) / P.far_rows : 0;
-  const int64_t far_first = far0 + (int64_t)(ku / kFarKeys) * segments;
+  const int64_t far_first = far0 + (int64_t)(ku / far_keys(P.sinks)) * segments;
   if constexpr (MODE == kJoin) {  // 32 columns a workgroup
     const int dt = blockIdx.y;
     float sum[16] = {};
@@ -837,7 +839,7 @@ __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))
   // x / G for x < G + 32 (exact: 1 / 2 is further from a multiple of G than the product is off)
   auto token_of = [&](int x) __attribute__((always_inline)) { return (int)(((float)x + 0.5f) * inv_g); };
 
-  // Loads: 32 rows of Q and of dO a stage, RPI rows an instruction; the wavefronts share them, and the first one takes the rows' statistics.  A scalar address for the stage's first
+  // Loads: 32 rows of Q and of dO a stage, RPI rows an instruction; the second wavefronts share them, and the first of these takes the rows' statistics.  A scalar address for the stage's first
   // token, a lane's own row from there on.
   constexpr int C = D / 8, RPI = 64 / C, LOADS = 2 * (32 / RPI), LPW = LOADS / PAIRS;  // load id: tensor id % 2, rows RPI (id / 2) .. of the stage
   static_assert(LPW * PAIRS == LOADS && LPW % 2 == 0, "every second wavefront has as many");
@@ -1098,11 +1100,11 @@ static int64_t longest(const int32_t* cu, int S) {
     if (cu[s + 1] - cu[s] > n) n = cu[s + 1] - cu[s];
   return n;
 }
-// Far rows a far item takes: short enough that a long sequence's sinks are many workgroups' work, and no more than 32 of them to a block of sinks, whose sums its own workgroup adds.  None
+// Far rows a far item takes: short enough that a long sequence's sinks are many workgroups' work, and no more than 64 of them to a block of sinks, whose sums its own workgroup adds.  None
 // where all of a sequence is at most twice an ordinary item's rows: a launch of their own costs more than the sinks' workgroups are longer then (2039 tokens in short sequences: 20 us).
 static int far_rows_of(int64_t longest, int window) {
   if (longest <= 2 * ((int64_t)window + kDkvKeys)) return 0;
-  const int64_t rows = (longest - window + 31) / 32;
+  const int64_t rows = (longest - window + 63) / 64;
   return rows < 256 ? 256 : (int)((rows + 31) / 32 * 32);
 }
 struct WindowWs { size_t lse2, dr, stats, partials, parts, bytes; int64_t far; int far_rows, near_parts; };
@@ -1117,7 +1119,7 @@ static WindowWs window_bwd_ws(const Geo& g, const int32_t* cu, int window, int s
   w.far_rows = far_rows_of(n, window);
   if (g.dtype == SB_BF16)
     for (int s = 0; s < g.S; ++s) w.far += far_items(cu[s + 1] - cu[s], window, sinks, w.far_rows);
-  w.partials = o; o = align_up(o + (size_t)w.far * g.Hkv * 2 * kFarKeys * g.D * sizeof(float));
+  w.partials = o; o = align_up(o + (size_t)w.far * g.Hkv * 2 * far_keys(sinks) * g.D * sizeof(float));
   // Parts where items are fewer than workgroups fit the chip (a CU's LDS holds one at head_dim 128, two at 64): up to 8, of 16 stages at least
   w.near_parts = 1;
   if (g.dtype == SB_BF16) {
@@ -1192,7 +1194,7 @@ int sb_window_attn_bwd(const sb_problem* p, int32_t window, int32_t sinks, const
   const int64_t q_items = row_tiles(cu, g.S, g.G, forward_rows(g.dtype)) * g.Hkv, k_items = row_tiles(cu, g.S, 1, f32 ? 32 : kDkvKeys) * g.Hkv;
   dim3 delta_grid, q_grid, k_grid, far_grid, part_grid;
   if ((rc = grid_of((rows + per - 1) / per, 256, &delta_grid)) != SB_OK || (rc = grid_of(q_items, 256, &q_grid)) != SB_OK ||
-      (rc = grid_of(k_items, 4 * kDkvKeys, &k_grid)) != SB_OK || (rc = grid_of(w.far * g.Hkv, 4 * kFarKeys, &far_grid)) != SB_OK ||
+      (rc = grid_of(k_items, 4 * kDkvKeys, &k_grid)) != SB_OK || (rc = grid_of(w.far * g.Hkv, 4 * far_keys(sinks), &far_grid)) != SB_OK ||
       (rc = grid_of(k_items * w.near_parts, 4 * kDkvKeys, &part_grid)) != SB_OK)
     return rc;
   auto launch = [&](auto d) {
@@ -1213,7 +1215,8 @@ int sb_window_attn_bwd(const sb_problem* p, int32_t window, int32_t sinks, const
       hipLaunchKernelGGL((window_dkv_f32_kernel<float, D>), k_grid, dim3(256), 0, st, P);
     } else {
       if (w.far > 0) {
-        hipLaunchKernelGGL((window_dkv_kernel<D, kFarKeys / 32, kFar>), far_grid, dim3(kFarKeys * 4), 0, st, P);
+        if (far_keys(sinks) == 32) hipLaunchKernelGGL((window_dkv_kernel<D, 1, kFar>), far_grid, dim3(128), 0, st, P);
+        else hipLaunchKernelGGL((window_dkv_kernel<D, 2, kFar>), far_grid, dim3(256), 0, st, P);
         SB_LAUNCH_CHECK("window_dkv_kernel, far rows");
       }
       if (w.near_parts > 1) {

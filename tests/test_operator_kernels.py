@@ -84,8 +84,8 @@ def test_forms_of_the_backward(launches):
     # (0 whole items, 1 far rows, 2 parts, 3 their join)
     x = launches("window", [20000], 32, 8, 128, 0, 1000, 4)
     assert [k for k, _, _ in x] == ["window_fwd_kernel", "window_dq_kernel", "window_dkv_kernel", "window_dkv_kernel"] and form(x) == ["1", "0"]
-    # the largest far item list the workspace was sized by: one block of 4 sinks, 32 runs of the rows behind the first 1128, by KV head
-    assert x[2][2] == 8 * -(-(20000 - 1000) // 608) and x[3][2] == 8 * 157
+    # the far items that the workspace was sized by: one block of 4 sinks, 64 runs of the rows behind the first 1000, by KV head
+    assert x[2][2] == 8 * -(-(20000 - 1000) // 320) and x[3][2] == 8 * 157
     assert form(launches("window", [20000], 32, 8, 128, 0, 1000, 0)) == ["0"]        # no sinks
     assert form(launches("window", [20000], 32, 8, 128, 0, 1000, 600)) == ["0"]      # so many that their tiles take all rows
     assert form(launches("window", [20000], 32, 8, 128, 0, NONE, 4)) == ["0"]
