@@ -6,7 +6,9 @@
 //
 // Memory-bound: every element is read and written once.  A wavefront takes a token at a time: each lane works out one pair's angle (a float64
 // product and one sine and cosine), which all heads of the token then share through LDS, and handles units of 2 VEC elements, VEC pairs,
-// of one head after the other, with kBatch heads' loads in flight.
+// of one head after the other, with kBatch heads' loads in flight.  65536 tokens, 32/8 heads, head_dim 128, bfloat16: 282 us, 4.8 TB/s, where a copy of
+// 2 GiB reaches 4.95 (stores past the caches: 426 us).  The append of 64 single tokens takes 6 us, of 8192 new tokens 36 us (5.6 TB/s: most of it stays in the
+// last-level cache).
 #include <math.h>
 
 #include "sb_cache.h"

@@ -343,7 +343,11 @@ __global__ __launch_bounds__(256) void window_dkv_f32_kernel(WindowParams P) {
 // bfloat16 forward.  A workgroup of four wavefronts owns 128 flattened rows of a KV head, 32 a wavefront, and walks the 64-key tiles that any of them sees; K and V tiles are
 // shared in LDS and double-buffered by asynchronous loads.  A wavefront takes a tile as two halves of 32 keys, a step of the running softmax each.  A tile that a wavefront's rows
 // all see carries no mask; one that none of them sees is only waited for.  256 registers, so two wavefronts share a SIMD: one runs its exponentials while the other runs matrix
-// instructions.
+// instructions, and a CU holds two workgroups (three or four at head_dim 64).  What bounds it is power: matrix cores 52 % busy at the 1.66 - 1.8 GHz that the chip keeps under this
+// load; at head_dim 64 vector work, 11.7 instructions per matrix instruction.  One sequence of 100001 tokens, 32/8 heads, window 2000: 3.3 ms, 1.0 PFLOP/s; 65536 tokens, 14/2 heads,
+// head_dim 64, window 1024: 0.29 ms, 0.8.  Measured against it: the halves' products and probabilities interleaved in one wavefront, S1 beside the probabilities of half 0 and O0 beside those
+// of half 1: the same at head_dim 128, 0.29 -> 0.36 ms at 64; priorities between the wavefronts: the same; eight wavefronts and 256 rows a workgroup: the same on long sequences, 2039
+// tokens in short ones 26 -> 20 us with four.
 template <int D, bool PAGED>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void window_fwd_kernel(WindowParams P) {
   constexpr int ROWS = 32 * kWaves, ROW_B = D * 2, TILE_B = 64 * ROW_B, NOP = D / 16;
@@ -523,7 +527,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
 
 // ---------------------------------------------------------------------------------------------
 // bfloat16 dQ.  Rows, tiles and their walk as in the forward kernel; a half tile is S, dP and dQ += dS K, whose operands go through one set of registers.  Every row belongs to one
-// workgroup here, so this is also where Dr is computed, from the dO in registers and one read of O, and left with LSE for the next kernel.
+// workgroup here, so this is also where Dr is computed, from the dO in registers and one read of O, and left with LSE for the next kernel.  32768 tokens, 32/8 heads, window 4096: 1.8 ms,
+// 1.12 PFLOP/s, matrix cores 64 % busy; 65536 tokens, 14/2 heads, head_dim 64, window 1024: 0.38 ms, 0.92 PFLOP/s (with eight wavefronts a workgroup, whose four SIMDs all wait at the same
+// barrier, 0.48).
 template <int D>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void window_dq_kernel(WindowParams P) {
   constexpr int ROWS = 32 * kWaves, ROW_B = D * 2, TILE_B = 64 * ROW_B, NOP = D / 16;
@@ -697,7 +703,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
 // bfloat16 dK and dV.  A workgroup owns PAIRS * 32 keys of a KV head and walks the flattened rows that see any of them, 32 a stage.  32 keys are the work of two wavefronts on one
 // SIMD: the first computes S and P and adds P^T dO to dV, the second, a stage behind, dP and dS = P (dP - Dr) and adds dS^T Q to dK; P goes from one to the other through LDS
 // in float32, lane by lane (both hold keys in columns).  Each so needs 150 registers where one wavefront for both would need more than the 256 that let two share a SIMD,
-// and has as many matrix instructions as the other.  The stages' Q and dO rows, LSE and Dr come by asynchronous loads, three stages ahead.
+// and has as many matrix instructions as the other.  The second one has the loads to issue besides, and goes first (32768 tokens, 32/8 heads, window 4096: 3.28 -> 2.75 ms; the first
+// going first 3.07; the first with the loads 3.17).  What it measured in all: 0.97 PFLOP/s there, matrix cores 60 % busy; 65536 tokens, 14/2 heads, head_dim 64: 0.61 ms, 0.77.  What took it
+// there from 5.15 ms: no spilled registers in the loop (a reload waits for all loads in flight: 7 - 11 ms with a pipeline of two stages that needed 16 more), no integer division in it, LSE
+// and Dr subtracted by a step of the matrix product instead of 32 registers and LDS reads of them, and far rows in many short items.  The stages' Q and dO rows, LSE and Dr come by asynchronous loads, three stages ahead.
 //
 // Sinks are seen by all rows of their sequence.  The rows behind a sink tile's ordinary ones (far rows) are the work of other workgroups (kFar), far_rows tokens each, that leave their
 // sums in float32; the tile's own workgroup, launched after them, adds them in order.  So the result does not depend on who is ahead, and no workgroup has more than its share.
