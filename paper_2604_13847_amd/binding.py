@@ -409,8 +409,16 @@ def sb_rope_apply(pb: Problem, rope: Rope, q, k, positions=None, backward=False,
     return q_out, k_out
 
 
+def _window(window, sinks):
+    """Both as the library's 32-bit numbers; a larger one would lose its upper bits on the way."""
+    if window > 2 ** 31 - 1 or sinks > 2 ** 31 - 1 or window < 1 or sinks < 0:
+        raise SparseBalError(f"window ({window}) must be 1 .. 2^31 - 1 and sinks ({sinks}) 0 .. 2^31 - 1")
+    return int(window), int(sinks)
+
+
 def sb_window_ws_bytes(pb: Problem, window, sinks):
     """(forward, backward) bytes of the workspaces of sb_window_attn_fwd and sb_window_attn_bwd."""
+    window, sinks = _window(window, sinks)
     f, b = C.c_int64(), C.c_int64()
     _check(lib().sb_window_ws_bytes(pb.ref(), int(window), int(sinks), C.byref(f), C.byref(b)))
     return f.value, b.value
@@ -431,6 +439,7 @@ def sb_window_attn_fwd(pb: Problem, window, sinks, q, k, v, o=None, lse=None, ws
         lse = torch.empty(rows, dtype=torch.float32, device=q.device)
     else:
         _tensor("lse", lse, rows, torch.float32, device)
+    window, sinks = _window(window, sinks)
     ws = _workspace(ws, sb_window_ws_bytes(pb, window, sinks)[0], device)
     _check(_operator_calls()["sb_window_attn_fwd"](C.addressof(pb.c), window, sinks, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), _address(ws),
                                                    stream))
@@ -448,6 +457,7 @@ def sb_window_attn_bwd(pb: Problem, window, sinks, q, k, v, o, lse, d_o, dq=None
     dv = dv if dv is not None else torch.empty_like(v)
     for name, x, shape in (("dq", dq, queries), ("dk", dk, keys), ("dv", dv, keys)):
         _tensor(name, x, shape, dt, device)
+    window, sinks = _window(window, sinks)
     ws = _workspace(ws, sb_window_ws_bytes(pb, window, sinks)[1], device)
     _check(_operator_calls()["sb_window_attn_bwd"](C.addressof(pb.c), window, sinks, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
                                                    d_o.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _address(ws), stream))
@@ -514,7 +524,7 @@ def sb_cache_append(cache: Cache, chunk: Chunk, k, v, rope: Rope = None, q=None,
 
 
 def sb_cache_attn_ws_bytes(cache: Cache, chunk: Chunk, window, sinks) -> int:
-    out = C.c_int64()
+    out, (window, sinks) = C.c_int64(), _window(window, sinks)
     _check(lib().sb_cache_attn_ws_bytes(cache.ref(), chunk.ref(), int(window), int(sinks), C.byref(out)))
     return out.value
 
@@ -533,6 +543,7 @@ def sb_cache_attn(cache: Cache, chunk: Chunk, q, window=2 ** 31 - 1, sinks=0, o=
         lse = torch.empty(rows, dtype=torch.float32, device=q.device)
     else:
         _tensor("lse", lse, rows, torch.float32, device)
+    window, sinks = _window(window, sinks)
     ws = _workspace(ws, sb_cache_attn_ws_bytes(cache, chunk, window, sinks), device)
     _check(_operator_calls()["sb_cache_attn"](C.addressof(cache.c), C.addressof(chunk.c), window, sinks, q.data_ptr(), o.data_ptr(), lse.data_ptr(), _address(ws), stream))
     return o, lse

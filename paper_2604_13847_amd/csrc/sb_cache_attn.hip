@@ -2,7 +2,7 @@
 //
 // Whole chunks of a prompt go through the kernel of packed batches (sb_window.hip), which looks its key tiles up in the page table.  Few rows a sequence (single tokens above
 // all) are another matter: every key is read for a handful of products, so what bounds them is memory, and what fills the chip is splitting the keys.  cache_split_kernel
-// gives each (sequence, KV head, run of keys) to a workgroup of two or four wavefronts that stage their own strips and never wait for each other until they add up at the
+// gives each (sequence, KV head, run of keys) to a workgroup of two wavefronts that stage their own strips and never wait for each other until they add up at the
 // end; cache_merge_kernel joins the runs.
 #include <math.h>
 
@@ -48,14 +48,15 @@ static int check_cache_attn(const sb_cache* c, const sb_chunk* n, int32_t window
 }
 
 // ---------------------------------------------------------------------------------------------
-// Few rows (bfloat16): an item is up to 32 flattened rows of a KV head and per_split strips of 32 keys; wavefront w takes every NW-th strip from the w-th on.  A wavefront's
+// Few rows (bfloat16): an item is up to 32 flattened rows of a KV head and per_split strips of 32 keys; a wavefront takes every second strip.  A wavefront's
 // strips of K and V come by buffer loads straight into its own LDS, the next strip's while one is worked on: 64 KiB a CU on their way (head_dim 128), no barrier, and the
 // products of a strip take a quarter of the time that memory takes to deliver four.  Pages are looked up 64 strips ahead, a lane a strip.
-// 64 sequences of 500 to 32768 tokens, 32/8 heads: 0.39 ms, 5.1 TB/s, where a copy of 2 GiB reaches 4.95 (four wavefronts, one workgroup a CU: 0.50 ms).  One sequence of 4097 tokens: 12 us and 4 to
-// join, a chain of dependent loads (lengths, page, keys) behind the launch.
-// Four wavefronts (NW) where there are no more workgroups than CUs, two otherwise: two such workgroups share a CU's LDS, and one's start and end are hidden by the other's stream.
-template <int D, int NW>
-__global__ __launch_bounds__(64 * NW) void cache_split_kernel(WindowParams P) {
+// 64 sequences of 500 to 32768 tokens, 32/8 heads: 0.39 ms, 5.1 TB/s, where a copy of 2 GiB reaches 4.95 (workgroups of four wavefronts, one a CU: 0.50 ms).  One sequence of 4097 tokens: 8.6 us (four wavefronts: 12)
+// and 4 to join, a chain of dependent loads (lengths, page, keys) behind the launch.
+// Two wavefronts: two such workgroups share a CU's LDS, and one's start and end are hidden by the other's stream.
+template <int D>
+__global__ __launch_bounds__(128) void cache_split_kernel(WindowParams P) {
+  constexpr int NW = 2;
   constexpr int ROW_B = D * 2, STRIP_B = 32 * ROW_B, NOP = D / 16, C = D / 8, RPI = 64 / C, LPG = 16 / RPI;  // loads per 16 rows
   constexpr int OUT_P = D + 4;  // floats from row to row of a wavefront's sums in LDS
   __shared__ __attribute__((aligned(1024))) char ring[NW][2][2 * STRIP_B];  // K, V
@@ -353,7 +354,7 @@ static CachePlan plan_cache(const sb_cache* c, const sb_chunk* n, int window, in
   p.few.splits = p.many.splits = 1;
   const bool f32 = c->dtype == SB_F32;
   // Two workgroups a CU; a strip for each wavefront at least, and 1024 keys at most, so that sequences of unequal lengths even out.
-  if (!f32 && (S > 1 || most <= kFewRows)) p.few = launch(most < kFewRows ? most : kFewRows, kSplitRows, 32, 512, 4, 32);
+  if (!f32 && G <= kFewRows && (S > 1 || most <= kFewRows)) p.few = launch(most < kFewRows ? most : kFewRows, kSplitRows, 32, 512, 2, 32);
   // A workgroup a CU (float32, where one takes 32 rows: four), of 8 tiles at least.
   if (f32 || most > kFewRows) p.many = launch(most, forward_rows(c->dtype), f32 ? 32 : 64, f32 ? 1024 : 256, 8, 1 << 30);
   const size_t splits = (size_t)(p.few.splits > p.many.splits ? p.few.splits : p.many.splits), all = (size_t)n->total_new * n->num_q_heads;
@@ -427,11 +428,8 @@ int sb_cache_attn(const sb_cache* c, const sb_chunk* n, int32_t window, int32_t 
     P.per_split = plan.few.per_split;
     P.rows_from = 0;
     P.rows_to = kFewRows;
-    auto split = [&](auto d, auto nw) {
-      hipLaunchKernelGGL((cache_split_kernel<decltype(d)::value, decltype(nw)::value>), grid, dim3(64 * decltype(nw)::value), 0, st, P);
-    };
-    auto with_nw = [&](auto d) { if (grid.x <= 320) split(d, std::integral_constant<int, 4>()); else split(d, std::integral_constant<int, 2>()); };
-    if (c->head_dim == 128) with_nw(std::integral_constant<int, 128>()); else with_nw(std::integral_constant<int, 64>());
+    if (c->head_dim == 128) hipLaunchKernelGGL((cache_split_kernel<128>), grid, dim3(128), 0, st, P);
+    else hipLaunchKernelGGL((cache_split_kernel<64>), grid, dim3(128), 0, st, P);
     SB_LAUNCH_CHECK("cache_split_kernel");
     if (P.splits > 1 && (rc = merge(few_rows, (int)few_seq_rows)) != SB_OK) return rc;
   }

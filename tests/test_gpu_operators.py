@@ -110,7 +110,7 @@ def check_window(pb, x, got, window, sinks, half, scale=None, values=("o", "dq",
 SHAPES = [((1,), 4, 2, 128, 1, 0), ((1, 2, 0, 3), 8, 1, 64, 2, 1), ((64, 65, 63, 128, 129), 4, 4, 128, 64, 0), ((64, 65, 63, 128, 129), 4, 2, 64, 65, 5),
           ((200, 31, 33), 7, 1, 128, 17, 3), ((300,), 14, 2, 64, 1, 0), ((300,), 6, 2, 128, 1, 70), ((257, 90), 8, 2, 128, 100, 64), ((500, 12), 4, 1, 128, 128, 65),
           ((500,), 2, 2, 64, 63, 129), ((700, 1, 300), 4, 2, 128, 250, 4), ((700,), 10, 2, 64, NONE, 0), ((333, 500), 32, 8, 128, 400, NONE),
-          ((520,), 16, 2, 128, NONE, 7), ((1950, 60), 2, 1, 128, 40, 70), ((1800,), 3, 1, 64, 300, 600), ((450,), 1, 1, 64, 449, 1), ((900,), 3, 1, 128, 129, 200)]
+          ((520,), 16, 2, 128, NONE, 7), ((1950, 60), 2, 1, 128, 40, 70), ((150, 9), 40, 1, 128, 33, 5), ((70,), 100, 1, 64, 20, 3), ((1, 60), 33, 1, 128, 64, 2), ((1800,), 3, 1, 64, 300, 600), ((450,), 1, 1, 64, 449, 1), ((900,), 3, 1, 128, 129, 200)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -246,7 +246,7 @@ SERVED = [  # have, new, Hq, Hkv, D, page, window, sinks
     ([0], [600], 28, 4, 128, 32, 128, 4), ([513, 100], [64, 65], 3, 3, 64, 16, NONE, 0), ([3000], [33], 32, 8, 128, 16, 1000, 64), ([1500] * 70, [1] * 70, 2, 1, 64, 64, NONE, 0),
     # prompts and single tokens in one batch; a long cache and rows that fill one tile, two, and a few
     ([2000, 900, 30, 0], [1, 200, 1, 90], 8, 2, 128, 16, NONE, 0), ([5000, 4900, 3], [1, 2, 150], 4, 1, 64, 64, 2000, 10), ([9000], [12], 4, 1, 128, 64, NONE, 0),
-    ([6000, 100], [8, 8], 8, 1, 64, 16, NONE, 0), ([9500], [20], 8, 2, 128, 32, NONE, 0)]
+    ([6000, 100], [8, 8], 8, 1, 64, 16, NONE, 0), ([700, 3], [1, 1], 40, 1, 128, 16, NONE, 0), ([700, 64], [1, 2], 100, 1, 64, 64, 200, 9), ([9500], [20], 8, 2, 128, 32, NONE, 0)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -23,7 +23,7 @@ def without_float32(lines):
             yield l
 
 
-@pytest.mark.parametrize("source,least", [("sb_window.hip", 12), ("sb_cache_attn.hip", 8)])
+@pytest.mark.parametrize("source,least", [("sb_window.hip", 12), ("sb_cache_attn.hip", 6)])
 def test_waits_and_spills(source, least):
     lines = hazards.assembly(source)
     seen = products = loads = 0
@@ -35,7 +35,7 @@ def test_waits_and_spills(source, least):
         assert not bad, (name, bad[:3])
         # a spilled register in these loops would also make the compiler wait for all loads in flight
         assert not [x.text for x in code if x.op.startswith("scratch_")], name
-    assert seen >= least and loads >= 16 and products >= 48
+    assert seen >= least and loads >= 16 and products >= 24
 
 
 CALLS = """
@@ -98,15 +98,16 @@ def test_forms_of_the_backward(launches):
 def test_forms_of_a_chunk(launches):
     names = lambda *a: [k for k, _, _ in launches("cache", *a)]
     assert names(1, 1, 1, 4098, 32, 8, 128, 0, NONE) == ["cache_split_kernel", "cache_merge_kernel"]
-    assert names(64, 64, 1, 100, 32, 8, 128, 0, NONE) == ["cache_split_kernel"]                        # no more than four strips
+    assert names(64, 64, 1, 100, 32, 8, 128, 0, NONE) == ["cache_split_kernel"]
     assert names(1, 3000, 3000, 3000, 32, 8, 128, 0, NONE) == ["window_fwd_kernel"]
     assert names(1, 100, 100, 30000, 4, 1, 128, 0, NONE) == ["window_fwd_kernel", "cache_merge_kernel"]
     assert names(10, 3000, 2000, 30000, 32, 8, 64, 0, NONE) == ["window_fwd_kernel", "cache_split_kernel", "cache_merge_kernel"]
     assert names(1, 1, 1, 20000, 4, 1, 64, 1, NONE) == ["window_fwd_f32_kernel", "cache_merge_kernel"]
     # 131072 new tokens of 32 heads are a launch, though as many workgroups that join runs would not be
     assert names(1, 131072, 131072, 131072, 32, 8, 128, 0, NONE) == ["window_fwd_kernel"]
-    wide = launches("cache", 1, 1, 1, 4098, 32, 8, 128, 0, NONE)[0]
-    many = launches("cache", 64, 64, 1, 32769, 32, 8, 128, 0, NONE)[0]
-    assert wide[1].endswith("Li4E") and wide[2] == 8 * 33 and many[1].endswith("Li2E") and many[2] == 64 * 8 * 33
+    # runs of 128 keys for one sequence, of 1024 for 64; no more than two strips are one run
+    assert launches("cache", 1, 1, 1, 4098, 32, 8, 128, 0, NONE)[0][2] == 8 * 33
+    assert launches("cache", 64, 64, 1, 32769, 32, 8, 128, 0, NONE)[0][2] == 64 * 8 * 33
+    assert names(1, 1, 1, 64, 32, 8, 128, 0, NONE) == ["cache_split_kernel"]
     # a window bounds the runs, whatever the length
     assert launches("cache", 64, 64, 1, 1 << 20, 32, 8, 128, 0, 1000)[0][2] <= 64 * 8 * 2

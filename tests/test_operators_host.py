@@ -113,6 +113,9 @@ def test_window_refusals():
         refused(L.sb_window_attn_fwd(pb.ref(), w, s, BUF, BUF, BUF, BUF, BUF, BUF, None), -1, "window")
         with pytest.raises(sb.SparseBalError, match="window"):
             sb.sb_window_ws_bytes(pb, w, s)
+    for w, s in ((2 ** 32 + 5, 0), (2 ** 31, 0), (5, 2 ** 32)):  # would arrive as another number
+        with pytest.raises(sb.SparseBalError, match="window"):
+            sb.sb_window_ws_bytes(pb, w, s)
     for missing in range(5):
         a = [BUF] * 5
         a[missing] = None
