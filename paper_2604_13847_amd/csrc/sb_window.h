@@ -78,7 +78,7 @@ __device__ inline RowTile locate_tile(const WindowParams& P, int64_t x) {
       t.row0 = __builtin_amdgcn_readlane(row0, src);
       t.n = __builtin_amdgcn_readlane(n, src);
       t.pos0 = __builtin_amdgcn_readlane(pos0, src);
-      t.tile = __builtin_amdgcn_readfirstlane(tiles - 1 - (int)(x - (__builtin_amdgcn_readlane(incl, src) - tiles)));
+      t.tile = __builtin_amdgcn_readfirstlane(min(max(tiles - 1 - (int)(x - (__builtin_amdgcn_readlane(incl, src) - tiles)), 0), tiles - 1));
       return t;
     }
     x -= __builtin_amdgcn_readlane(incl, min(P.S - base, 64) - 1);
@@ -109,6 +109,7 @@ struct KeyTiles {
   __device__ inline int count() const { return far + end - near; }
   __device__ inline int at(int i) const { return i < far ? i : near + i - far; }
 };
+__device__ inline bool sees(int t, int u, int window, int sinks) { return u <= t && (t - u < window || u < sinks); }
 // the same question about key u0 + k + 4 hf of a tile at u0, k known at compile time: three comparisons with a constant
 struct Sight {
   int t, w, s;
@@ -117,7 +118,6 @@ struct Sight {
   }
   __device__ inline bool operator()(int k) const { return (k <= t) & ((k > w) | (k < s)); }
 };
-__device__ inline bool sees(int t, int u, int window, int sinks) { return u <= t && (t - u < window || u < sinks); }
 
 // One wavefront's part of copying a 64-key tile of K or V into LDS (layout as in sb_attn_common.h), NW wavefronts to a tile, as buffer loads whose resource covers
 // the rows that exist, so that the others arrive as zeros.  A load's rows (4, or 8 at head_dim 64) lie in one page.

@@ -706,27 +706,29 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
 // and has as many matrix instructions as the other.  The second one has the loads to issue besides, and goes first (32768 tokens, 32/8 heads, window 4096: 3.28 -> 2.75 ms; the first
 // going first 3.07; the first with the loads 3.17).  What it measured in all: 0.97 PFLOP/s there, matrix cores 60 % busy; 65536 tokens, 14/2 heads, head_dim 64: 0.61 ms, 0.77.  What took it
 // there from 5.15 ms: no spilled registers in the loop (a reload waits for all loads in flight: 7 - 11 ms with a pipeline of two stages that needed 16 more), no integer division in it, LSE
-// and Dr subtracted by a step of the matrix product instead of 32 registers and LDS reads of them, and far rows in many short items.  The stages' Q and dO rows, LSE and Dr come by asynchronous loads, three stages ahead.
+// and Dr subtracted by a step of the matrix product instead of 32 registers and LDS reads of them, and far rows in many short items.
+// The stages' Q and dO rows, LSE and Dr come by asynchronous loads, three stages ahead (kFar: two, so that two of its workgroups share a CU's LDS).
 //
 // Sinks are seen by all rows of their sequence.  The rows behind a sink tile's ordinary ones (far rows) are the work of other workgroups (kFar), far_rows tokens each, that leave their
 // sums in float32; the tile's own workgroup, launched after them, adds them in order.  So the result does not depend on who is ahead, and no workgroup has more than its share.
 constexpr int kDkvKeys = 128;   // keys of a workgroup, but of kFar
 constexpr int kFarSinks = 512;  // with more sinks than this there are sink tiles enough to fill the chip: their own workgroups take all rows
 // Far items of a sequence of n tokens: far_blocks blocks of sinks, far_segments each (some may be empty: the first rows of a block's last ones).
-// The rows are read once a block, at the rate of the memory, so a block is 64 sinks where there are more than 32 (65536 tokens, 14/2 heads, 64 sinks: 95 us in two blocks).
+// The rows are read once a block, so a block is 64 sinks where there are more than 32 (65536 tokens, 14/2 heads, 64 sinks: 66 us, in two blocks 105).
 __host__ __device__ inline int far_keys(int sinks) { return sinks > 32 ? 64 : 32; }
 __host__ __device__ inline int far_blocks(int n, int sinks) { return ((sinks < n ? sinks : n) + far_keys(sinks) - 1) / far_keys(sinks); }
 __host__ __device__ inline int far_segments(int n, int window, int far_rows) { return far_rows > 0 && n > window ? (n - window + far_rows - 1) / far_rows : 0; }
 __host__ __device__ inline int64_t far_items(int n, int window, int sinks, int far_rows) {
   return sinks > kFarSinks ? 0 : (int64_t)far_blocks(n, sinks) * far_segments(n, window, far_rows);
 }
-// the first token that none but sinks of the 128 keys around u show themselves to
+// the first token that sees none of the 128 keys around u, but for sinks
 __host__ __device__ inline int near_end(int u, int n, int window) {
   const int last = (u | (kDkvKeys - 1)) < n ? (u | (kDkvKeys - 1)) : n - 1;
   return n - last > window ? last + window : n;
 }
 
-// Where there are fewer items than CUs, an item's rows are shared by near_parts workgroups (kPart) that leave their sums too, which a last launch adds in order (kJoin).
+// Where there are fewer items than the chip works on at a time, an item's rows are shared by near_parts workgroups (kPart) that leave their sums too, which a last launch adds in order
+// (kJoin).  2039 tokens in short sequences, 16/2 heads: 186 us whole, 38 and 8 in six parts.
 enum DkvMode { kWhole, kFar, kPart, kJoin };
 template <int D, int PAIRS, DkvMode MODE>
 __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))) void window_dkv_kernel(WindowParams P) {
