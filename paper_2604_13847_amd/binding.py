@@ -312,17 +312,19 @@ SB_ROPE_PLAIN, SB_ROPE_LINEAR, SB_ROPE_NTK, SB_ROPE_YARN, SB_ROPE_BANDS = range(
 _TORCH_DTYPE = {SB_BF16: torch.bfloat16, SB_F32: torch.float32}
 
 
-def _operator_calls():
-    """{name: function} of the calls below, their argument types set."""
+def _call(name, *args):
+    """One of the calls below, by a function object whose argument types are set."""
     global _calls
     if _calls is None:
         P, I, L = C.c_void_p, C.c_int32, C.c_int64
         types = {"sb_rope_apply": [P, P, P, P, L, P, L, P, P, I, P], "sb_window_attn_fwd": [P, I, I] + [P] * 7, "sb_window_attn_bwd": [P, I, I] + [P] * 11,
                  "sb_cache_append": [P, P, P, P, L, P, L, P, L, P, P], "sb_cache_attn": [P, P, I, I] + [P] * 5}
         _calls = {}
-        for name, args in types.items():
-            _calls[name] = C.CFUNCTYPE(C.c_int, *args)((name, lib()))  # (a function object of its own: those of `lib()` keep taking what ctypes makes of their arguments)
-    return _calls
+        for n, t in types.items():
+            _calls[n] = C.CFUNCTYPE(C.c_int, *t)((n, lib()))  # (a function object of its own: those of `lib()` keep taking what ctypes makes of their arguments)
+    rc = _calls[name](*args)
+    if rc != SB_OK:
+        _check(rc)
 
 
 _calls = None
@@ -331,10 +333,10 @@ _calls = None
 def _here():
     """(current device, its current stream)"""
     try:
-        device = torch.cuda.current_device()
+        device = torch._C._cuda_getDevice()
+        return device, torch._C._cuda_getCurrentRawStream(device)
     except RuntimeError:
         return -2, 0  # no GPU: no tensor lies on the device, and each is refused
-    return device, torch._C._cuda_getCurrentRawStream(device)
 
 
 def _tensor(name, t, shape, dtype, device, pitch=False):
@@ -404,8 +406,8 @@ def sb_rope_apply(pb: Problem, rope: Rope, q, k, positions=None, backward=False,
             _tensor("k_out", k_out, shape, dt, device)
     if positions is not None:
         _tensor("positions", positions, (pb.T,), torch.int32, device)
-    _check(_operator_calls()["sb_rope_apply"](C.addressof(pb.c), C.addressof(rope.c), _address(positions), _address(q), _pitch(q), _address(k), _pitch(k), _address(q_out),
-                                              _address(k_out), 1 if backward else 0, stream))
+    _call("sb_rope_apply", C.addressof(pb.c), C.addressof(rope.c), _address(positions), _address(q), _pitch(q), _address(k), _pitch(k), _address(q_out),
+          _address(k_out), 1 if backward else 0, stream)
     return q_out, k_out
 
 
@@ -441,8 +443,8 @@ def sb_window_attn_fwd(pb: Problem, window, sinks, q, k, v, o=None, lse=None, ws
         _tensor("lse", lse, rows, torch.float32, device)
     window, sinks = _window(window, sinks)
     ws = _workspace(ws, sb_window_ws_bytes(pb, window, sinks)[0], device)
-    _check(_operator_calls()["sb_window_attn_fwd"](C.addressof(pb.c), window, sinks, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), _address(ws),
-                                                   stream))
+    _call("sb_window_attn_fwd", C.addressof(pb.c), window, sinks, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), _address(ws),
+          stream)
     return o, lse
 
 
@@ -459,8 +461,8 @@ def sb_window_attn_bwd(pb: Problem, window, sinks, q, k, v, o, lse, d_o, dq=None
         _tensor(name, x, shape, dt, device)
     window, sinks = _window(window, sinks)
     ws = _workspace(ws, sb_window_ws_bytes(pb, window, sinks)[1], device)
-    _check(_operator_calls()["sb_window_attn_bwd"](C.addressof(pb.c), window, sinks, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
-                                                   d_o.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _address(ws), stream))
+    _call("sb_window_attn_bwd", C.addressof(pb.c), window, sinks, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
+          d_o.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _address(ws), stream)
     return dq, dk, dv
 
 
@@ -518,8 +520,8 @@ def sb_cache_append(cache: Cache, chunk: Chunk, k, v, rope: Rope = None, q=None,
             _tensor("q_out", q_out, queries, dt, device)
     elif q_out is not None:
         raise SparseBalError("q_out without q")
-    _check(_operator_calls()["sb_cache_append"](C.addressof(cache.c), C.addressof(chunk.c), C.addressof(rope.c) if rope is not None else None, _address(q), _pitch(q),
-                                                k.data_ptr(), _pitch(k), v.data_ptr(), _pitch(v), _address(q_out), stream))
+    _call("sb_cache_append", C.addressof(cache.c), C.addressof(chunk.c), C.addressof(rope.c) if rope is not None else None, _address(q), _pitch(q),
+          k.data_ptr(), _pitch(k), v.data_ptr(), _pitch(v), _address(q_out), stream)
     return q_out
 
 
@@ -545,7 +547,7 @@ def sb_cache_attn(cache: Cache, chunk: Chunk, q, window=2 ** 31 - 1, sinks=0, o=
         _tensor("lse", lse, rows, torch.float32, device)
     window, sinks = _window(window, sinks)
     ws = _workspace(ws, sb_cache_attn_ws_bytes(cache, chunk, window, sinks), device)
-    _check(_operator_calls()["sb_cache_attn"](C.addressof(cache.c), C.addressof(chunk.c), window, sinks, q.data_ptr(), o.data_ptr(), lse.data_ptr(), _address(ws), stream))
+    _call("sb_cache_attn", C.addressof(cache.c), C.addressof(chunk.c), window, sinks, q.data_ptr(), o.data_ptr(), lse.data_ptr(), _address(ws), stream)
     return o, lse
 
 
