@@ -14,8 +14,8 @@
 namespace sb {
 
 // ---------------------------------------------------------------------------------------------
-// float32 arithmetic throughout: v_mfma_f32_32x32x2_f32, operands straight from memory.  A workgroup owns 32 rows (or 32 keys) and walks strips of 32 keys (rows), every
-// fourth strip a wavefront's; the wavefronts' sums are added in order at the end.  Operand layout per lane: A row / B column = lane%32, contraction slot = lane/32.
+// float32 arithmetic throughout: v_mfma_f32_32x32x2_f32, operands straight from memory.  A workgroup owns 32 rows (or 32 keys) and walks strips of 32 keys (rows), in
+// turn to its wavefronts; the wavefronts' sums are added in order at the end.  Operand layout per lane: A row / B column = lane%32, contraction slot = lane/32.
 __device__ inline f32x16 mfma_f32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
 
 __device__ inline f32x4 load4(const float* p) { return *(const f32x4*)p; }
@@ -51,6 +51,17 @@ __device__ inline f32x16 dot_rows(const RowOperand<D>& a, const RowOperand<D>& b
   for (int x = 0; x < D / 8; ++x)
 #pragma unroll
     for (int j = 0; j < 4; ++j) s = mfma_f32(a.x[x][j], b.x[x][j], s);
+  return s;
+}
+template <int D>
+__device__ inline f32x16 dot_rows(const RowOperand<D>& a, const f32x4 (&b)[D / 8][64], int lane) {
+  f32x16 s = zero16();
+#pragma unroll
+  for (int x = 0; x < D / 8; ++x) {
+    const f32x4 y = b[x][lane];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s = mfma_f32(a.x[x][j], y[j], s);
+  }
   return s;
 }
 // acc[dt] += X^T w over 32 rows of X, row c_row(v, hf) with weight w[v]; row(r) is a row's address or null
@@ -102,16 +113,16 @@ struct Keys {
 };
 
 // The other wavefronts' registers for the first one
-template <int N>
+template <int N, int W>
 struct Sums {
-  float x[3][N][64];
+  float x[W - 1][N][64];
   __device__ inline void put(int wave, int i, int lane, float v) { if (wave > 0) x[wave - 1][i][lane] = v; }
 };
 
 template <typename T, int D, bool PAGED>
 __global__ __launch_bounds__(256) void window_fwd_f32_kernel(WindowParams P) {
   constexpr int NR = 16 * (D / 32);
-  __shared__ Sums<NR + 2> sums;
+  __shared__ Sums<NR + 2, 4> sums;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
   const unsigned item = blockIdx.x;
   const int splits = PAGED ? P.splits : 1, z = (int)(item / P.Hkv % splits);
@@ -222,7 +233,7 @@ __global__ __launch_bounds__(256) void window_delta_kernel(WindowParams P, int64
 
 template <typename T, int D>
 __global__ __launch_bounds__(256) void window_dq_f32_kernel(WindowParams P) {
-  __shared__ Sums<16 * (D / 32)> sums;
+  __shared__ Sums<16 * (D / 32), 4> sums;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
   const unsigned item = blockIdx.x;
   const RowTile t = locate_tile<32, false>(P, item / P.Hkv);
@@ -269,36 +280,49 @@ __global__ __launch_bounds__(256) void window_dq_f32_kernel(WindowParams P) {
   if (m0 + l32 < rows) store_column<D>((T*)P.dq + at, acc, P.scale, hf);
 }
 
-// Key-major: a workgroup owns 32 keys of a KV head and walks the flattened rows that see any of them, 32 at a time, every fourth 32 a wavefront's; the four sums are added in order.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void window_dkv_f32_kernel(WindowParams P) {
-  constexpr int NR = 16 * (D / 32);
-  __shared__ Sums<2 * NR> sums;
+// Key-major: a workgroup owns 32 keys of a KV head and walks the flattened rows that see any of them, 32 at a time, in turn to its wavefronts; their sums are added in order.  At
+// head_dim 64 two wavefronts share a SIMD, each with 256 registers (16384 tokens, 8/2 heads, window 1024: 5.4 ms with one, 4.1 with two); at 128 the sums alone take 256.
+// PARTS: where items are few, near_parts workgroups share the rows of one, and window_dkv_f32_join_kernel adds their sums in order.  1024 tokens, one head, head_dim 64, window 200,
+// 4 sinks: 60 us whole (four wavefronts 72), 26 in four parts, their join included; 4000 tokens, 2/1 heads, window 500: 525 -> 221; 1024 tokens, 4/2 heads, head_dim 128: 210 -> 66.
+template <int D>
+constexpr int kDkvWavesF32 = D == 64 ? 8 : 4;
+
+template <typename T, int D, bool PARTS>
+__global__ __launch_bounds__(64 * kDkvWavesF32<D>) void window_dkv_f32_kernel(WindowParams P) {
+  constexpr int NR = 16 * (D / 32), W = kDkvWavesF32<D>;
+  __shared__ Sums<2 * NR, W> sums;
+  __shared__ f32x4 own[2][D / 8][64];  // the keys' operands, the same in every wavefront
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
   WindowParams one = P;  // tiles of 32 keys: one row a token
   one.G = 1;
-  const RowTile t = locate_tile<32, false>(one, blockIdx.x / (unsigned)P.Hkv);
+  const unsigned parts = PARTS ? P.near_parts : 1, part = blockIdx.x / (unsigned)P.Hkv % parts;
+  const RowTile t = locate_tile<32, false>(one, blockIdx.x / (unsigned)P.Hkv / parts);
   if (t.s < 0) return;
   const int g = (int)(blockIdx.x % (unsigned)P.Hkv);
   const int u0 = t.tile * 32, u = min(u0 + l32, t.n - 1), last = min(u0 + 31, t.n - 1);
   const int64_t at = ((int64_t)(t.row0 + u) * P.Hkv + g) * D;
   const T* const any = (const T*)P.k + at;
-  RowOperand<D> kr, vr, x;
-  load_row<D>(kr, any, any, hf);
-  load_row<D>(vr, (const T*)P.v + at, any, hf);
+  RowOperand<D> x;
+  if (wave < 2) {
+    load_row<D>(x, wave == 0 ? any : (const T*)P.v + at, any, hf);
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) own[wave][i][lane] = x.x[i];
+  }
+  __syncthreads();
   f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt) dk[dt] = dv[dt] = zero16();
   const int behind = u0 < P.sinks || t.n - last <= P.window ? t.n : last + P.window;  // the first token that sees none of them
   const int end = behind * P.G;
   auto row = [&](int m) { const int tok = (int)((unsigned)m / (unsigned)P.G); return (int64_t)(t.row0 + tok) * P.Hq + g * P.G + m - tok * P.G; };
-  for (int m0 = u0 * P.G + 32 * wave; m0 < end; m0 += 128) {
+  for (int m0 = u0 * P.G + 32 * (int)(part * W + wave); m0 < end; m0 += 32 * (int)(parts * W)) {
     const int m = min(m0 + l32, end - 1);
     const int64_t mine = row(m);
     load_row<D>(x, (const T*)P.q + mine * D, any, hf);
-    const f32x16 sc = dot_rows<D>(x, kr);
+    asm volatile("" ::: "memory");  // the keys' operands are read again each time: kept in registers they would spill others
+    const f32x16 sc = dot_rows<D>(x, own[0], lane);
     load_row<D>(x, (const T*)P.d_o + mine * D, any, hf);
-    const f32x16 dp = dot_rows<D>(x, vr);
+    const f32x16 dp = dot_rows<D>(x, own[1], lane);
     // statistics of row m0 + lane%32, passed on to the lanes that hold the row
     const float lse2 = P.lse2[mine], dr = P.dr[mine];
     const int pos = m0 + l32 < end ? (int)((unsigned)m / (unsigned)P.G) : -1;
@@ -325,7 +349,7 @@ __global__ __launch_bounds__(256) void window_dkv_f32_kernel(WindowParams P) {
   __syncthreads();
   if (wave > 0) return;
 #pragma unroll
-  for (int w = 0; w < 3; ++w)
+  for (int w = 0; w < W - 1; ++w)
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -333,10 +357,44 @@ __global__ __launch_bounds__(256) void window_dkv_f32_kernel(WindowParams P) {
         dk[dt][v] += sums.x[w][16 * dt + v][lane];
         dv[dt][v] += sums.x[w][NR + 16 * dt + v][lane];
       }
+  if (PARTS) {
+    float* const to = P.parts + (int64_t)blockIdx.x * (2 * NR * 64) + lane;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        to[64 * (16 * dt + v)] = dk[dt][v];
+        to[64 * (NR + 16 * dt + v)] = dv[dt][v];
+      }
+    return;
+  }
   if (u0 + l32 < t.n) {
     store_column<D>((T*)P.dk + at, dk, P.scale, hf);
     store_column<D>((T*)P.dv + at, dv, 1.0f, hf);
   }
+}
+// 32 columns of dK or dV of an item a workgroup, four registers of the parts' sums a thread
+template <int D>
+__global__ __launch_bounds__(256) void window_dkv_f32_join_kernel(WindowParams P) {
+  constexpr int NR = 16 * (D / 32);
+  const int vg = threadIdx.x >> 6, lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
+  const int dt = blockIdx.y % (D / 32), value = blockIdx.y / (D / 32);
+  WindowParams one = P;
+  one.G = 1;
+  const unsigned tile = blockIdx.x / (unsigned)P.Hkv, g = blockIdx.x % (unsigned)P.Hkv;
+  const RowTile t = locate_tile<32, false>(one, tile);
+  const int u = t.tile * 32 + l32;
+  if (t.s < 0 || u >= t.n) return;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int j = 0; j < P.near_parts; ++j) {
+    const float* const from = P.parts + ((int64_t)(tile * P.near_parts + j) * P.Hkv + g) * (2 * NR * 64) + 64 * (value * NR + 16 * dt + 4 * vg) + lane;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] += from[64 * e];
+  }
+  const float f = value ? 1.0f : P.scale;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] *= f;
+  store4((float*)(value ? P.dv : P.dk) + ((int64_t)(t.row0 + u) * P.Hkv + g) * D + 32 * dt + 8 * vg + 4 * hf, x);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1142,6 +1200,16 @@ static WindowWs window_bwd_ws(const Geo& g, const int32_t* cu, int window, int s
     if (parts > 1) w.near_parts = (int)parts;
     w.parts = o;
     if (parts > 1) o = align_up(o + (size_t)items * parts * 2 * kDkvKeys * g.D * sizeof(float));
+  } else {
+    // float32: the same from four strips of 32 rows a wavefront on.  (The sinks' keys are seen by all rows.)
+    const int64_t items = row_tiles(cu, g.S, 1, 32) * g.Hkv, waves = g.D == 64 ? kDkvWavesF32<64> : kDkvWavesF32<128>;
+    const int64_t most = sinks > 0 || n < (int64_t)window + 32 ? n : (int64_t)window + 32, strips = most * g.G / 32;
+    int64_t parts = items > 0 && strips >= 4 * waves ? 256 / items : 1;
+    if (parts > strips / waves) parts = strips / waves;
+    if (parts > 8) parts = 8;
+    if (parts > 1) w.near_parts = (int)parts;
+    w.parts = o;
+    if (parts > 1) o = align_up(o + (size_t)items * parts * 2 * 32 * g.D * sizeof(float));
   }
   w.bytes = o;
   return w;
@@ -1223,7 +1291,14 @@ int sb_window_attn_bwd(const sb_problem* p, int32_t window, int32_t sinks, const
     }
     KernelTimer kt(K_WINDOW_DKV, st);
     if (f32) {
-      hipLaunchKernelGGL((window_dkv_f32_kernel<float, D>), k_grid, dim3(256), 0, st, P);
+      constexpr int threads = 64 * kDkvWavesF32<D>;
+      if (w.near_parts > 1) {
+        hipLaunchKernelGGL((window_dkv_f32_kernel<float, D, true>), part_grid, dim3(threads), 0, st, P);
+        SB_LAUNCH_CHECK("window_dkv_f32_kernel");
+        hipLaunchKernelGGL((window_dkv_f32_join_kernel<D>), dim3(k_grid.x, 2 * (D / 32)), dim3(256), 0, st, P);
+      } else {
+        hipLaunchKernelGGL((window_dkv_f32_kernel<float, D, false>), k_grid, dim3(threads), 0, st, P);
+      }
     } else {
       if (w.far > 0) {
         if (far_keys(sinks) == 32) hipLaunchKernelGGL((window_dkv_kernel<D, 1, kFar>), far_grid, dim3(128), 0, st, P);

@@ -111,3 +111,13 @@ def test_forms_of_a_chunk(launches):
     assert names(1, 1, 1, 64, 32, 8, 128, 0, NONE) == ["cache_split_kernel"]
     # a window bounds the runs, whatever the length
     assert launches("cache", 64, 64, 1, 1 << 20, 32, 8, 128, 0, 1000)[0][2] <= 64 * 8 * 2
+
+
+def test_forms_of_the_float32_backward(launches):
+    of = lambda *a: [(k, n) for k, _, n in launches("window", *a) if "dkv" in k]
+    assert of([1024], 1, 1, 64, 1, 200, 4) == [("window_dkv_f32_kernel", 32 * 4), ("window_dkv_f32_join_kernel", 32)]  # 32 strips of eight wavefronts
+    assert of([1024], 1, 1, 64, 1, 200, 0) == [("window_dkv_f32_kernel", 32)]      # 7 strips without sinks
+    assert of([1000, 24], 1, 1, 64, 1, 200, 4) == [("window_dkv_f32_kernel", 33)]  # 31
+    assert of([1000, 24], 2, 1, 128, 1, NONE, 0) == [("window_dkv_f32_kernel", 33 * 7), ("window_dkv_f32_join_kernel", 33)]
+    assert of([4096], 2, 1, 128, 1, NONE, 0) == [("window_dkv_f32_kernel", 128 * 2), ("window_dkv_f32_join_kernel", 128)]
+    assert of([4097], 2, 1, 128, 1, NONE, 0) == [("window_dkv_f32_kernel", 129)]   # items enough to be one round by themselves
