@@ -97,14 +97,15 @@ __device__ inline bf16x8 split3(float x) {
   return r;
 }
 
-// Keys of rows at positions ta .. tb, in tiles of `TILE`: sink tiles 0 .. far - 1, then tiles near .. end - 1.  (tb: that of the last key that can exist, if that is less.)
+// Keys of rows at positions ta .. tb, in tiles of `TILE`: sink tiles 0 .. far - 1, then tiles near .. end - 1.  (tb: that of the last key that can exist, if that is less; where all
+// rows are behind it, there are sink tiles up to it and no others.)
 template <int TILE>
 struct KeyTiles {
   int far, near, end;
   __device__ inline KeyTiles(int ta, int tb, int window, int sinks) {
     near = max(0, ta - window + 1) / TILE;
     end = max(tb / TILE + 1, near);
-    far = min((int)(((int64_t)sinks + TILE - 1) / TILE), near);
+    far = min((int)(((int64_t)sinks + TILE - 1) / TILE), min(near, tb / TILE + 1));
   }
   __device__ inline int count() const { return far + end - near; }
   __device__ inline int at(int i) const { return i < far ? i : near + i - far; }
@@ -185,13 +186,13 @@ struct KeySource {
     if (p < 0) { rows = 0; return 0; }
     return (((unsigned long long)(unsigned)p * P.Hkv << P.cache.page_shift) + (unsigned)(u & (P.cache.page_size - 1))) * (D * 2);
   }
-  // bit x: keys u0 + 16x .. + 15 have no page
+  // bit x: keys u0 + 16x .. + 15 have no page.  (Those behind `end` too: where that is the page table's end, rows behind it would take them, zeros in LDS, for keys.)
   __device__ inline unsigned missing(const WindowParams& P, int u0) const {
     if (!PAGED) return 0;
     unsigned m = 0;
 #pragma unroll
     for (int x = 0; x < 4; ++x)
-      if (u0 + 16 * x < end && page_of(P, u0 + 16 * x) < 0) m |= 1u << x;
+      if (u0 + 16 * x >= end || page_of(P, u0 + 16 * x) < 0) m |= 1u << x;
     return m;
   }
 };
