@@ -239,12 +239,12 @@ __global__ __launch_bounds__(128) void cache_split_kernel(WindowParams P) {
     }
     const int j = token(m0 + r), hh = g * P.G + m0 + r - j * P.G;
     const int64_t row = (int64_t)(t.row0 + j) * P.Hq + hh;
-    const float inv = sum > 0.f ? 1.0f / sum : 0.f, lse2 = sum > 0.f ? best + __builtin_log2f(sum) : -__builtin_inff();
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum, lse2 = sum == 0.f ? -__builtin_inff() : best + __builtin_log2f(sum);  // (a sum that is no number is passed on)
     x *= inv;
     if (P.splits > 1) {
       const int64_t at = (int64_t)z * P.T * P.Hq + row;
       if (c == 0) P.part_lse[at] = lse2;
-      if (sum > 0.f) *(f32x4*)(P.part_o + at * D + 4 * c) = x;
+      if (sum != 0.f) *(f32x4*)(P.part_o + at * D + 4 * c) = x;
     } else {
       bf16x4 y;
 #pragma unroll
@@ -256,7 +256,7 @@ __global__ __launch_bounds__(128) void cache_split_kernel(WindowParams P) {
 }
 
 // Joins the runs of keys of the sequences that a launch before had: a workgroup to a row and head, every fourth run a wavefront's.  A run that saw nothing has left LSE -infinity and no
-// sums.  seq_rows > 0: workgroups for that many rows of every sequence, else for all rows.
+// sums; one that saw what is no number has left that, and so is the row's result.  seq_rows > 0: workgroups for that many rows of every sequence, else for all rows.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cache_merge_kernel(WindowParams P, int seq_rows) {
   constexpr int E = D / 64;
@@ -283,14 +283,14 @@ __global__ __launch_bounds__(256) void cache_merge_kernel(WindowParams P, int se
     }
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) top = fmaxf(top, lse[i]);
-    if (top == -__builtin_inff()) continue;
-    const float old = fast_exp2(best - top);
+    const float ref = top == -__builtin_inff() ? 0.f : top;  // nothing seen yet: keep the exponents finite
+    const float old = fast_exp2(best - ref);
     sum *= old;
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] *= old;
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) {
-      const float f = fast_exp2(lse[i] - top);
+      const float f = fast_exp2(lse[i] - ref);
       sum += f;
 #pragma unroll
       for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(f, lse[i] == -__builtin_inff() ? 0.f : part[i][e], x[e]);  // (a run without sums holds whatever was there)
@@ -309,19 +309,18 @@ __global__ __launch_bounds__(256) void cache_merge_kernel(WindowParams P, int se
   sum = 0.f;
 #pragma unroll
   for (int e = 0; e < E; ++e) x[e] = 0.f;
-  if (best > -__builtin_inff()) {
+  const float ref = best == -__builtin_inff() ? 0.f : best;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float f = fast_exp2(sums[w][E][lane] - best);
-      sum += f * sums[w][E + 1][lane];
+  for (int w = 0; w < 4; ++w) {
+    const float f = fast_exp2(sums[w][E][lane] - ref);
+    sum += f * sums[w][E + 1][lane];
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(f, sums[w][e][lane], x[e]);
-    }
+    for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(f, sums[w][e][lane], x[e]);
   }
-  const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
 #pragma unroll
   for (int e = 0; e < E; ++e) ((T*)P.o)[row * D + E * lane + e] = (T)(x[e] * inv);
-  if (lane == 0) P.lse[(int64_t)h * P.T + tok] = sum > 0.f ? (best + __builtin_log2f(sum)) * 0.69314718055994531f : -__builtin_inff();
+  if (lane == 0) P.lse[(int64_t)h * P.T + tok] = sum == 0.f ? -__builtin_inff() : (best + __builtin_log2f(sum)) * 0.69314718055994531f;
 }
 
 // How the work is cut.  Sequences of up to kFewRows flattened rows are cache_split_kernel's (bfloat16), the others the packed batches' kernel's; a batch of one kind costs one launch.

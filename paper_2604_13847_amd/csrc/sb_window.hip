@@ -564,12 +564,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   wait_vmcnt<0>();
 
   l += __shfl_xor(l, 32, 64);  // the two lane halves hold different keys of the same row
-  const float inv = l > 0.f ? 1.0f / l : 0.f;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;  // (a sum that is no number is not one that saw nothing)
   if (PAGED && splits > 1) {
     if (mw + l32 >= rows) return;
     const int64_t row = ((int64_t)z * P.T + t.row0 + i) * P.Hq + h;
-    if (hf == 0) P.part_lse[row] = l > 0.f ? m * P.scale_log2e + __builtin_log2f(l) : -__builtin_inff();
-    if (l > 0.f) store_column<D>(P.part_o + row * D, oacc, inv, hf);
+    if (hf == 0) P.part_lse[row] = l == 0.f ? -__builtin_inff() : m * P.scale_log2e + __builtin_log2f(l);
+    if (l != 0.f) store_column<D>(P.part_o + row * D, oacc, inv, hf);
     return;
   }
   __syncthreads();  // the tiles' LDS is free
@@ -580,7 +580,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
                   return (bf16*)P.o + ((int64_t)(t.row0 + j) * P.Hq + g * P.G + mw + r - j * P.G) * D;
                 });
   if (hf == 0 && mw + l32 < rows)
-    P.lse[(int64_t)h * P.T + t.row0 + i] = l > 0.f ? (m * P.scale_log2e + __builtin_log2f(l)) * 0.69314718055994531f : -__builtin_inff();
+    P.lse[(int64_t)h * P.T + t.row0 + i] = l == 0.f ? -__builtin_inff() : (m * P.scale_log2e + __builtin_log2f(l)) * 0.69314718055994531f;
 }
 
 // ---------------------------------------------------------------------------------------------

@@ -28,3 +28,72 @@ def test_tokens_behind_the_page_table_are_seen_by_no_row(have, new, page, column
         if columns == 0 or (a - window + 1 >= columns * page and sinks == 0):
             rows = slice(x.cu[s], x.cu[s + 1])
             assert float(o[rows].abs().max()) == 0 and bool((lse[:, rows] == -INF).all())
+
+
+# ---------------------------------------------------------------- what is no number
+# have, new, window, sinks, the key: one run of keys and several, single tokens and chunks; rows that see the key and rows that do not
+PLANTED = [([50, 20], [1, 1], NONE, 0, 33), ([4000, 300], [1, 1], NONE, 0, 1003), ([4000, 300], [1, 1], 100, 0, 1003), ([0, 40], [300, 5], 100, 0, 130), ([0], [300], 100, 7, 5),
+           ([3000], [100], 500, 0, 2550), ([3000], [100], NONE, 0, 3050), ([3000, 64], [12, 1], 300, 2, 2707)]
+
+
+def check_planted(k, v, q, seen, o, lse, u, clean):
+    """Rows [n] of one sequence, all heads: NaN where a score is NaN or +infinity, else what they are without the key: it is not seen or its weight is zero."""
+    G, D = q.shape[1] // k.shape[1], q.shape[2]
+    scores = torch.einsum("nhd,hd->nh", q.double(), k[u].double().repeat_interleave(G, 0))
+    lost = seen[:, u, None] & (torch.isnan(scores) | (scores == INF))
+    assert bool(torch.isnan(o[lost]).all()) and bool(torch.isnan(lse.T[lost]).all())
+    without, kk = seen.clone(), k.double().clone()
+    without[:, u], kk[u] = False, 0
+    r = ref.Attention(q.double(), kk, v.double(), without, D ** -0.5, ref.HALF[o.dtype])
+    hidden = ~lost & (~seen[:, u, None] | (scores == -INF))
+    for name, got, want, tol in (("o", o, r.o, r.o_tol), ("lse", lse.T, r.lse.T, r.lse_tol.T)):
+        ref.check(name, got[hidden], want[hidden], tol[hidden])
+    rest = ~lost & ~hidden                                     # other KV heads' rows: the key is a number there
+    assert torch.equal(o[rest], clean[0][rest]) and torch.equal(lse.T[rest], clean[1].T[rest])
+    return int(lost.sum())
+
+
+@pytest.mark.parametrize("value", [float("nan"), INF])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("have,new,window,sinks,u", PLANTED)
+def test_keys_that_are_no_number_reach_the_rows_that_see_them(have, new, window, sinks, u, dtype, value):
+    x = Served(have, new, 4, 2, 128, 16, dtype)
+    clean = x.check(window, sinks)
+    x.k[0][u, 1, 5] = value
+    x.k_pages[x.table[0, u // 16].long(), 1, u % 16, 5] = value
+    o, lse = x.attend(window, sinks)
+    n, length = new[0], have[0] + new[0]
+    seen = ref.visible(torch.arange(have[0], length, device=DEV), torch.arange(length, device=DEV), window, sinks)
+    lost = check_planted(x.k[0], x.v[0], x.q[:n], seen, o[:n], lse[:, :n], u, (clean[0][:n], clean[1][:, :n]))
+    assert lost > 0 or not bool(seen[:, u].any()) or (value == INF and n == 1)
+    assert torch.equal(o[n:], clean[0][n:]) and torch.equal(lse[:, n:], clean[1][:, n:])   # the other sequences
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("have,new", [([50], [1]), ([4000], [1]), ([0], [300]), ([3000], [100])])
+def test_queries_that_are_no_number(have, new, dtype):
+    x = Served(have, new, 4, 2, 64, 64, dtype)
+    clean = x.check()
+    i = new[0] // 2
+    x.q[i, 1, 3], x.q[0, 2, 0] = float("nan"), float("nan")
+    o, lse = x.attend()
+    lost = torch.zeros(new[0], 4, dtype=torch.bool, device=DEV)
+    lost[i, 1], lost[0, 2] = True, True
+    assert bool(torch.isnan(o[lost]).all()) and bool(torch.isnan(lse.T[lost]).all())
+    assert torch.equal(o[~lost], clean[0][~lost]) and torch.equal(lse.T[~lost], clean[1].T[~lost])
+
+
+@pytest.mark.parametrize("value", [float("nan"), INF])
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 64)])
+def test_keys_that_are_no_number_in_a_packed_batch(dtype, D, value):
+    window, sinks, u, lens = 90, 3, 70, (250, 40)
+    pb = batch(lens, 4, 2, D, dtype)
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    q, k, v = (normal(i, pb.T, h, D, dtype=t) for i, h in enumerate((4, 2, 2)))
+    clean = sb.sb_window_attn_fwd(pb, window, sinks, q, k, v)
+    k[u, 1, 5] = value
+    o, lse = sb.sb_window_attn_fwd(pb, window, sinks, q, k, v)
+    at = torch.arange(lens[0], device=DEV)
+    n = lens[0]
+    assert check_planted(k[:n], v[:n], q[:n], ref.visible(at, at, window, sinks), o[:n], lse[:, :n], u, (clean[0][:n], clean[1][:, :n])) > 0
+    assert torch.equal(o[n:], clean[0][n:]) and torch.equal(lse[:, n:], clean[1][:, n:])
