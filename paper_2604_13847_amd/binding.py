@@ -319,9 +319,8 @@ def _call(name, *args):
         P, I, L = C.c_void_p, C.c_int32, C.c_int64
         types = {"sb_rope_apply": [P, P, P, P, L, P, L, P, P, I, P], "sb_window_attn_fwd": [P, I, I] + [P] * 7, "sb_window_attn_bwd": [P, I, I] + [P] * 11,
                  "sb_cache_append": [P, P, P, P, L, P, L, P, L, P, P], "sb_cache_attn": [P, P, I, I] + [P] * 5}
-        _calls = {}
-        for n, t in types.items():
-            _calls[n] = C.CFUNCTYPE(C.c_int, *t)((n, lib()))  # (a function object of its own: those of `lib()` keep taking what ctypes makes of their arguments)
+        # (function objects of their own: those of `lib()` keep taking what ctypes makes of their arguments.  All at once: another thread may be here too)
+        _calls = {n: C.CFUNCTYPE(C.c_int, *t)((n, lib())) for n, t in types.items()}
     rc = _calls[name](*args)
     if rc != SB_OK:
         _check(rc)
