@@ -357,6 +357,16 @@ def _tensor(name, t, shape, dtype, device, pitch=False):
     need(False, "a token's heads must be contiguous, and tokens in order" if pitch else "must be contiguous")
 
 
+def _elsewhere(name, there, device):
+    raise SparseBalError(f"{name}: lies on {'cuda:' + str(there) if there >= 0 else 'the CPU'}, the current device is cuda:{device}")
+
+
+def _batch(pb, device):
+    """Refuses a batch whose lengths the kernels would have to read on another device.  (Without any on a device the library refuses it.)"""
+    if pb.cu_dev is not None and pb.cu_dev.get_device() != device:
+        _elsewhere("cu_seqlens", pb.cu_dev.get_device(), device)
+
+
 def _pitch(t):
     return 0 if t is None or t.shape[0] < 2 else t.stride(0)
 
@@ -389,6 +399,8 @@ def sb_rope_apply(pb: Problem, rope: Rope, q, k, positions=None, backward=False,
     """(q, k) turned by their positions (the tokens' indices in their sequences, or `positions`), or gradients turned back.  q and k may
     be slices of a fused projection; either may be None.  q_out, k_out may be q and k where these are contiguous."""
     dt, (device, stream) = _TORCH_DTYPE[pb.dtype], _here()
+    if positions is None:
+        _batch(pb, device)
     if q is not None:
         shape = (pb.T, pb.Hq, pb.D)
         _tensor("q", q, shape, dt, device, pitch=True)
@@ -428,6 +440,7 @@ def sb_window_ws_bytes(pb: Problem, window, sinks):
 def sb_window_attn_fwd(pb: Problem, window, sinks, q, k, v, o=None, lse=None, ws=None):
     """Attention with a sliding window and sinks; pb's budgets and blocks are not read.  Returns (o, lse)."""
     dt, (device, stream) = _TORCH_DTYPE[pb.dtype], _here()
+    _batch(pb, device)
     queries, keys, rows = (pb.T, pb.Hq, pb.D), (pb.T, pb.Hkv, pb.D), (pb.Hq, pb.T)
     _tensor("q", q, queries, dt, device)
     _tensor("k", k, keys, dt, device)
@@ -449,6 +462,7 @@ def sb_window_attn_fwd(pb: Problem, window, sinks, q, k, v, o=None, lse=None, ws
 
 def sb_window_attn_bwd(pb: Problem, window, sinks, q, k, v, o, lse, d_o, dq=None, dk=None, dv=None, ws=None):
     dt, (device, stream) = _TORCH_DTYPE[pb.dtype], _here()
+    _batch(pb, device)
     queries, keys = (pb.T, pb.Hq, pb.D), (pb.T, pb.Hkv, pb.D)
     for name, x, shape in (("q", q, queries), ("k", k, keys), ("v", v, keys), ("o", o, queries), ("d_o", d_o, queries)):
         _tensor(name, x, shape, dt, device)
@@ -473,7 +487,7 @@ class Cache:
             raise SparseBalError("k: [pages][KV heads][tokens of a page][head_dim] in bfloat16 or float32 is needed")
         if page_table.dim() != 2:
             raise SparseBalError("page_table: [sequences][pages] is needed")
-        device = _here()[0]
+        self.device = device = _here()[0]
         _tensor("k", k, k.shape, k.dtype, device)
         _tensor("v", v, k.shape, k.dtype, device)
         _tensor("page_table", page_table, page_table.shape, torch.int32, device)
@@ -490,6 +504,7 @@ class Chunk:
 
     def __init__(self, cu_new, cached, Hq, total_new, max_new, max_length, softmax_scale=0.0):
         S, device = cached.shape[0], _here()[0]
+        self.device = device
         _tensor("cu_new", cu_new, (S + 1,), torch.int32, device)
         _tensor("cached", cached, (S,), torch.int32, device)
         self.cu_new, self.cached, self.Hq, self.total_new = cu_new, cached, int(Hq), int(total_new)
@@ -499,15 +514,19 @@ class Chunk:
         return C.byref(self.c)
 
 
-def _same_sequences(cache, chunk):
+def _same_sequences(cache, chunk, device):
+    if cache.device != device:
+        _elsewhere("cache", cache.device, device)
+    if chunk.device != device:
+        _elsewhere("chunk", chunk.device, device)
     if cache.page_table.shape[0] != chunk.c.num_seqs:
         raise SparseBalError(f"page_table: {cache.page_table.shape[0]} rows for {chunk.c.num_seqs} sequences")
 
 
 def sb_cache_append(cache: Cache, chunk: Chunk, k, v, rope: Rope = None, q=None, q_out=None):
     """New tokens' k (turned) and v into their pages; returns q turned likewise (None without q)."""
-    _same_sequences(cache, chunk)
     n, D, dt, (device, stream) = chunk.total_new, cache.c.head_dim, cache.k.dtype, _here()
+    _same_sequences(cache, chunk, device)
     keys, queries = (n, cache.c.num_kv_heads, D), (n, chunk.Hq, D)
     _tensor("k", k, keys, dt, device, pitch=True)
     _tensor("v", v, keys, dt, device, pitch=True)
@@ -532,8 +551,8 @@ def sb_cache_attn_ws_bytes(cache: Cache, chunk: Chunk, window, sinks) -> int:
 
 def sb_cache_attn(cache: Cache, chunk: Chunk, q, window=2 ** 31 - 1, sinks=0, o=None, lse=None, ws=None):
     """Attention of the new tokens over the cache, which holds them already.  Returns (o, lse)."""
-    _same_sequences(cache, chunk)
     dt, (device, stream) = cache.k.dtype, _here()
+    _same_sequences(cache, chunk, device)
     queries, rows = (chunk.total_new, chunk.Hq, cache.c.head_dim), (chunk.Hq, chunk.total_new)
     _tensor("q", q, queries, dt, device)
     if o is None:
