@@ -77,9 +77,10 @@ def lib():
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise SparseBalError(f"{LIB_PATH} is not built; run `python -c 'import __graft_entry__ as g; g.build()'`")
-        _lib = C.CDLL(LIB_PATH)
-        _lib.sb_last_error.restype = C.c_char_p
-        _lib.sb_version.restype = C.c_char_p
+        loaded = C.CDLL(LIB_PATH)
+        loaded.sb_last_error.restype = C.c_char_p
+        loaded.sb_version.restype = C.c_char_p
+        _lib = loaded  # (complete: another thread may be here too)
     return _lib
 
 

@@ -55,3 +55,16 @@ def test_what_a_call_keeps_on_another_device_is_refused(monkeypatch):
     # positions are read in place of the batch's lengths
     with pytest.raises(sb.SparseBalError, match="^q: a GPU tensor"):
         sb.sb_rope_apply(pb, sb.Rope(64), q, None, positions=torch.zeros(100, dtype=torch.int32))
+
+
+def test_the_library_is_there_for_all_threads_at_once(monkeypatch):
+    """Nobody finds the library before its functions' result types are set: its messages would be numbers."""
+    class Loaded:
+        def __getattr__(self, name):
+            assert sb._lib is None, name
+            self.__dict__[name] = f = lambda: None
+            return f
+
+    monkeypatch.setattr(sb, "_lib", None)
+    monkeypatch.setattr(sb.C, "CDLL", lambda path: Loaded())
+    assert isinstance(sb.lib(), Loaded) and sb._lib is sb.lib()
