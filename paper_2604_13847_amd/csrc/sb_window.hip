@@ -1272,7 +1272,7 @@ int sb_window_attn_bwd(const sb_problem* p, int32_t window, int32_t sinks, const
   const int64_t rows = (int64_t)g.T * g.Hq, per = 1024 / g.D;
   const int64_t q_items = row_tiles(cu, g.S, g.G, forward_rows(g.dtype)) * g.Hkv, k_items = row_tiles(cu, g.S, 1, f32 ? 32 : kDkvKeys) * g.Hkv;
   dim3 delta_grid, q_grid, k_grid, far_grid, part_grid;
-  if ((rc = grid_of((rows + per - 1) / per, 256, &delta_grid)) != SB_OK || (rc = grid_of(q_items, 256, &q_grid)) != SB_OK ||
+  if ((f32 && (rc = grid_of((rows + per - 1) / per, 256, &delta_grid)) != SB_OK) || (rc = grid_of(q_items, 256, &q_grid)) != SB_OK ||
       (rc = grid_of(k_items, 4 * kDkvKeys, &k_grid)) != SB_OK || (rc = grid_of(w.far * g.Hkv, 4 * far_keys(sinks), &far_grid)) != SB_OK ||
       (rc = grid_of(k_items * w.near_parts, 4 * kDkvKeys, &part_grid)) != SB_OK)
     return rc;
