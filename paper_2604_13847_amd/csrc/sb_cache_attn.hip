@@ -6,6 +6,7 @@
 // end; cache_merge_kernel joins the runs.
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "sb_window.h"
@@ -242,7 +243,7 @@ __global__ __launch_bounds__(128) void cache_split_kernel(WindowParams P) {
     const float inv = sum == 0.f ? 0.f : 1.0f / sum, lse2 = sum == 0.f ? -__builtin_inff() : best + __builtin_log2f(sum);  // (a sum that is no number is passed on)
     x *= inv;
     if (P.splits > 1) {
-      const int64_t at = (int64_t)z * P.T * P.Hq + row;
+      const int64_t at = ((int64_t)z * P.part_rows + (P.part_seq_rows > 0 ? t.s * P.part_seq_rows : t.row0) + j) * P.Hq + hh;
       if (c == 0) P.part_lse[at] = lse2;
       if (sum != 0.f) *(f32x4*)(P.part_o + at * D + 4 * c) = x;
     } else {
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(256) void cache_merge_kernel(WindowParams P, int se
   const int row0 = min(max(P.cu[s], 0), P.T), n = min(min(P.cu[s + 1], P.T) - row0, P.max_new), tok = seq_rows > 0 ? row0 + at % seq_rows : at;
   if (tok - row0 < 0 || tok - row0 >= n || n * P.G < P.rows_from || n * P.G > P.rows_to) return;
   const int splits = P.splits;
-  const int64_t all = (int64_t)P.T * P.Hq, row = (int64_t)tok * P.Hq + h;
+  const int64_t all = (int64_t)P.part_rows * P.Hq, row = (int64_t)(P.part_seq_rows > 0 ? s * P.part_seq_rows + tok - row0 : tok) * P.Hq + h;
   constexpr int kRuns = 8;  // on their way at a time
   float x[E] = {}, best = -__builtin_inff(), sum = 0.f;
   for (int z0 = wave; z0 < splits; z0 += 4 * kRuns) {
@@ -319,13 +320,18 @@ __global__ __launch_bounds__(256) void cache_merge_kernel(WindowParams P, int se
   }
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
 #pragma unroll
-  for (int e = 0; e < E; ++e) ((T*)P.o)[row * D + E * lane + e] = (T)(x[e] * inv);
+  for (int e = 0; e < E; ++e) ((T*)P.o)[((int64_t)tok * P.Hq + h) * D + E * lane + e] = (T)(x[e] * inv);
   if (lane == 0) P.lse[(int64_t)h * P.T + tok] = sum == 0.f ? -__builtin_inff() : (best + __builtin_log2f(sum)) * 0.69314718055994531f;
 }
 
 // How the work is cut.  Sequences of up to kFewRows flattened rows are cache_split_kernel's (bfloat16), the others the packed batches' kernel's; a batch of one kind costs one launch.
 constexpr int kFewRows = 2 * kSplitRows;
-struct CacheLaunch { int64_t items; int splits, per_split; };  // tiles of rows; keys in `splits` runs of per_split tiles
+static int few_seq_rows(int G, int max_new) { return std::min(kFewRows / G, max_new); }  // tokens of such a sequence, at most
+struct CacheLaunch {
+  int64_t items;          // tiles of rows
+  int splits, per_split;  // keys in `splits` runs of per_split tiles
+  int part_rows, part_seq_rows;
+};
 struct CachePlan {
   CacheLaunch few, many;           // items 0: no such launch
   size_t part_o, part_lse, bytes;  // workspace
@@ -356,11 +362,18 @@ static CachePlan plan_cache(const sb_cache* c, const sb_chunk* n, int window, in
   if (!f32 && G <= kFewRows && (S > 1 || most <= kFewRows)) p.few = launch(most < kFewRows ? most : kFewRows, kSplitRows, 32, 512, 2, 32);
   // A workgroup a CU (float32, where one takes 32 rows: four), of 8 tiles at least.
   if (f32 || most > kFewRows) p.many = launch(most, forward_rows(c->dtype), f32 ? 32 : 64, f32 ? 1024 : 256, 8, 1 << 30);
-  const size_t splits = (size_t)(p.few.splits > p.many.splits ? p.few.splits : p.many.splits), all = (size_t)n->total_new * n->num_q_heads;
-  if (splits > 1) {
-    p.part_o = align_up(splits * all * sizeof(float));
-    p.bytes = align_up(p.part_o + splits * all * c->head_dim * sizeof(float));
+  p.few.part_rows = p.many.part_rows = n->total_new;
+  // Sums of few rows are laid out by sequence where that is less: a prompt in the batch has none (64 sequences of 32768 tokens, one of them 8192 new ones: 0.56 GB and not 4.4)
+  const int seq_rows = few_seq_rows(G, n->max_new);
+  if ((int64_t)seq_rows * S < n->total_new) {
+    p.few.part_seq_rows = seq_rows;
+    p.few.part_rows = seq_rows * S;
   }
+  size_t most_sums = 0;
+  for (const CacheLaunch* l : {&p.few, &p.many})
+    if (l->splits > 1) most_sums = std::max(most_sums, (size_t)l->splits * l->part_rows * n->num_q_heads);
+  p.part_o = align_up(most_sums * sizeof(float));
+  p.bytes = align_up(p.part_o + most_sums * c->head_dim * sizeof(float));
   return p;
 }
 
@@ -401,10 +414,10 @@ int sb_cache_attn(const sb_cache* c, const sb_chunk* n, int32_t window, int32_t 
   }
   const hipStream_t st = (hipStream_t)stream;
   const bool f32 = c->dtype == SB_F32;
-  const int64_t rows = P.T, few_seq_rows = kFewRows / P.G < P.max_new ? kFewRows / P.G : P.max_new;
+  const int64_t rows = P.T, seq_rows = few_seq_rows(P.G, P.max_new);
   dim3 grid, all_rows, few_rows;
   if ((rc = grid_of(plan.few.items * P.Hkv * plan.few.splits, 256, &grid)) != SB_OK || (plan.many.splits > 1 && (rc = grid_of(rows * P.Hq, 256, &all_rows)) != SB_OK) ||
-      (plan.few.splits > 1 && (rc = grid_of(few_seq_rows * P.S * P.Hq, 256, &few_rows)) != SB_OK))
+      (plan.few.splits > 1 && (rc = grid_of(seq_rows * P.S * P.Hq, 256, &few_rows)) != SB_OK))
     return rc;
   KernelTimer kt(K_CACHE_ATTN, st);
   auto merge = [&](dim3 workgroups, int seq_rows) {
@@ -417,6 +430,7 @@ int sb_cache_attn(const sb_cache* c, const sb_chunk* n, int32_t window, int32_t 
   if (plan.many.items > 0) {
     P.splits = plan.many.splits;
     P.per_split = plan.many.per_split;
+    P.part_rows = plan.many.part_rows;
     P.rows_from = f32 || plan.few.items == 0 ? 0 : kFewRows + 1;
     P.rows_to = 0x7fffffff;
     if ((rc = launch_window_fwd(P, c->head_dim, c->dtype, true, plan.many.items, st)) != SB_OK) return rc;
@@ -425,12 +439,14 @@ int sb_cache_attn(const sb_cache* c, const sb_chunk* n, int32_t window, int32_t 
   if (plan.few.items > 0) {
     P.splits = plan.few.splits;
     P.per_split = plan.few.per_split;
+    P.part_rows = plan.few.part_rows;
+    P.part_seq_rows = plan.few.part_seq_rows;
     P.rows_from = 0;
     P.rows_to = kFewRows;
     if (c->head_dim == 128) hipLaunchKernelGGL((cache_split_kernel<128>), grid, dim3(128), 0, st, P);
     else hipLaunchKernelGGL((cache_split_kernel<64>), grid, dim3(128), 0, st, P);
     SB_LAUNCH_CHECK("cache_split_kernel");
-    if (P.splits > 1 && (rc = merge(few_rows, (int)few_seq_rows)) != SB_OK) return rc;
+    if (P.splits > 1 && (rc = merge(few_rows, (int)seq_rows)) != SB_OK) return rc;
   }
   return SB_OK;
 }

@@ -27,8 +27,10 @@ struct WindowParams {
   PagedCache cache;
   const int32_t* cached;
   int max_new;
-  // keys split over `splits` workgroups, per_split tiles each (the last one takes what is left); part_o [splits][T][Hq][D] normalised, part_lse [splits][T][Hq] in base 2
+  // keys split over `splits` workgroups, per_split tiles each (the last one takes what is left); part_o [splits][part_rows][Hq][D] normalised, part_lse [splits][part_rows][Hq] in
+  // base 2.  Row i of sequence s is there part_seq_rows * s + i or, where that is 0 (and part_rows T), the packed row.
   int splits, per_split;
+  int part_rows, part_seq_rows;
   float *part_o, *part_lse;
   int rows_from, rows_to;  // sequences of these many flattened rows are this launch's, the others another's
 };

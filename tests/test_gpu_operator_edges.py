@@ -97,3 +97,17 @@ def test_keys_that_are_no_number_in_a_packed_batch(dtype, D, value):
     n = lens[0]
     assert check_planted(k[:n], v[:n], q[:n], ref.visible(at, at, window, sinks), o[:n], lse[:, :n], u, (clean[0][:n], clean[1][:, :n])) > 0
     assert torch.equal(o[n:], clean[0][n:]) and torch.equal(lse[:, n:], clean[1][:, n:])
+
+
+# ---------------------------------------------------------------- workspaces
+@pytest.mark.parametrize("have,new,Hq,Hkv", [([2000, 900, 30, 0], [1, 200, 1, 90], 8, 2), ([2000, 1500], [1, 1], 8, 2), ([1500] * 5 + [4000], [1, 2, 16, 7, 1, 400], 4, 1),
+                                             ([3000, 100], [3, 64], 1, 1), ([5000, 0, 2500], [1, 300, 1], 64, 1), ([3000], [100], 4, 1)])
+def test_a_workspace_of_the_size_that_was_asked_for(have, new, Hq, Hkv):
+    x = Served(have, new, Hq, Hkv, 128, 16)
+    o, lse = x.check()
+    need = sb.sb_cache_attn_ws_bytes(x.cache, x.chunk, NONE, 0)
+    assert need > 0 and need % 4 == 0
+    around = torch.full((need + 2048,), 0x5A, dtype=torch.uint8, device=DEV)
+    again = sb.sb_cache_attn(x.cache, x.chunk, x.q, ws=around[1024: 1024 + need])
+    assert torch.equal(again[0], o) and torch.equal(again[1], lse)
+    assert bool((around[:1024] == 0x5A).all()) and bool((around[1024 + need:] == 0x5A).all())
