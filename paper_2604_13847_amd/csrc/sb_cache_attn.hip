@@ -344,9 +344,10 @@ static CachePlan plan_cache(const sb_cache* c, const sb_chunk* n, int window, in
     CacheLaunch l{};
     const int64_t by_total = row_tiles_most(n->total_new, S, G, rows), by_seq = (most_rows + rows - 1) / rows * S;
     l.items = by_total < by_seq ? by_total : by_seq;
-    // key tiles of an item, about: what max_length, the window and the sinks leave
+    // key tiles of an item, about: what max_length, the page table, the window and the sinks leave
     const int64_t in_window = (int64_t)window + (rows + G - 1) / G + sinks + 2 * tile;
-    const int64_t keys = in_window < n->max_length ? in_window : n->max_length, tiles = (keys + tile - 1) / tile;
+    const int64_t longest = std::min<int64_t>(n->max_length, (int64_t)c->max_pages * c->page_size);
+    const int64_t keys = std::min(in_window, longest), tiles = (keys + tile - 1) / tile;
     int64_t per = (tiles * l.items * c->num_kv_heads + wanted - 1) / wanted;
     per = (per + least - 1) / least * least;
     if (per < least) per = least;
@@ -363,7 +364,7 @@ static CachePlan plan_cache(const sb_cache* c, const sb_chunk* n, int window, in
   // A workgroup a CU (float32, where one takes 32 rows: four), of 8 tiles at least.
   if (f32 || most > kFewRows) p.many = launch(most, forward_rows(c->dtype), f32 ? 32 : 64, f32 ? 1024 : 256, 8, 1 << 30);
   p.few.part_rows = p.many.part_rows = n->total_new;
-  // Sums of few rows are laid out by sequence where that is less: a prompt in the batch has none (64 sequences of 32768 tokens, one of them 8192 new ones: 0.56 GB and not 4.4)
+  // Sums of few rows are laid out by sequence where that is less: a prompt in the batch has none (64 sequences of 32768 tokens, one of them with 8192 new ones: 0.54 GB and not 4.4)
   const int seq_rows = few_seq_rows(G, n->max_new);
   if ((int64_t)seq_rows * S < n->total_new) {
     p.few.part_seq_rows = seq_rows;

@@ -30,3 +30,10 @@ def test_a_prompt_beside_single_tokens_asks_for_no_sums_of_its_own():
     assert ws_bytes(*serving(64, 8192 + 63, 8192, 32768)) <= 16 * alone
     assert ws_bytes(*serving(64, 65536 + 63, 65536, 131072)) <= 4 * 16 * alone
     assert ws_bytes(*serving(64, 100, 37, 32768)) <= alone * 100 // 64 + 512           # fewer tokens in all than that
+
+
+def test_a_length_that_the_table_cannot_hold():
+    """max_length is about how long a sequence gets, whatever the caller knows of that; keys behind the page table do not exist."""
+    assert ws_bytes(*serving(64, 64, 1, NONE, pages=512)) == ws_bytes(*serving(64, 64, 1, 32768))
+    assert ws_bytes(*serving(2, 300, 200, NONE, pages=512)) == ws_bytes(*serving(2, 300, 200, 32768))
+    assert ws_bytes(*serving(1, 1, 1, NONE, pages=1)) == ws_bytes(*serving(1, 1, 1, NONE, pages=0)) == 0
