@@ -174,6 +174,7 @@ static int enqueue_rope(RopeParams& P, int D, int dtype, bool half, bool paged, 
                     aligned16(P.cache.k) && aligned16(P.cache.v) && P.q_pitch * esize % 16 == 0 && P.k_pitch * esize % 16 == 0 &&
                     P.v_pitch * esize % 16 == 0;
   P.run = P.T / 8192 < 1 ? 1 : P.T / 8192 > 8 ? 8 : P.T / 8192;
+  if (P.T >> 25 > P.run) P.run = P.T >> 25;  // (a launch has fewer than 2^32 threads)
   const dim3 grid((unsigned)(((int64_t)P.T + 4 * P.run - 1) / (4 * P.run)));
   KernelTimer kt(K_ROPE, st);
   if (dtype == SB_F32) {

@@ -1,8 +1,11 @@
 """Which launches the calls of window attention and of the paged cache take, and which of them are refused, at sizes that no test runs (see test_operator_kernels.py)."""
 import ctypes as C
+import os
+import subprocess
+import sys
 
 from paper_2604_13847_amd import binding as sb
-from test_operator_kernels import NONE, launches  # noqa: F401 (the fixture)
+from test_operator_kernels import NONE, ROOT, launches  # noqa: F401 (the fixture)
 
 
 def test_the_largest_backward(launches):  # noqa: F811
@@ -37,3 +40,31 @@ def test_a_length_that_the_table_cannot_hold():
     assert ws_bytes(*serving(64, 64, 1, NONE, pages=512)) == ws_bytes(*serving(64, 64, 1, 32768))
     assert ws_bytes(*serving(2, 300, 200, NONE, pages=512)) == ws_bytes(*serving(2, 300, 200, 32768))
     assert ws_bytes(*serving(1, 1, 1, NONE, pages=1)) == ws_bytes(*serving(1, 1, 1, NONE, pages=0)) == 0
+
+
+ROTATIONS = """
+import ctypes as C, sys
+shim = C.CDLL(sys.argv[1], mode=C.RTLD_GLOBAL)
+shim.recorded_kernel.restype = C.c_char_p
+import numpy as np
+from paper_2604_13847_amd import binding as sb
+T = int(sys.argv[2])
+cu, b, z = np.array([0, T], dtype=np.int32), C.c_void_p(4096), C.c_int64(0)
+pb = sb.Problem([0, 100], [1], 1, 1, 64)
+pb.c.total_tokens, pb.c.cu_seqlens_host, pb.c.cu_seqlens_dev = T, cu.ctypes.data, 4096
+sb._check(sb.lib().sb_rope_apply(pb.ref(), sb.Rope(64).ref(), None, None, z, b, z, None, b, 0, None))
+out = np.zeros((256, 6), dtype=np.uint32)
+assert shim.recorded_launches(out.ctypes.data_as(C.c_void_p)) == 1
+print("launch", *out[0])
+"""
+
+
+def test_rotations_of_very_many_tokens(tmp_path):
+    """A launch has fewer than 2^32 threads; 2^29 tokens and more, at one a wavefront or eight, would take as many."""
+    shim = str(tmp_path / "record_launches.so")
+    subprocess.run(["gcc", "-O1", "-shared", "-fPIC", "-o", shim, os.path.join(ROOT, "tests", "launch", "record_launches.c")], check=True)
+    for T, workgroups in ((2039, 510), (65536, 2048), (1 << 28, 1 << 23), (1 << 30, 1 << 23), (2 ** 31 - 1, (1 << 23) + (1 << 18))):
+        r = subprocess.run([sys.executable, "-c", ROTATIONS, shim, str(T)], cwd=ROOT, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        assert r.returncode == 0, r.stdout[-2000:]
+        x, y, z, threads, _, _ = (int(n) for n in r.stdout.split("launch")[1].split())
+        assert (y, z, threads) == (1, 1, 256) and x <= workgroups and x * threads < 1 << 32, (T, x)
