@@ -355,7 +355,7 @@ int sb_cache_append(const sb_cache *c, const sb_chunk *n, const sb_rope *r, cons
 
 /* Attention of the new tokens over the cache, which holds them already (sb_cache_append): row i of sequence s is token t = cached[s] + i and sees
  * the keys u <= t with t - u < window or u < sinks.  q, o: dev [total_new][Hq][D]; lse: dev [Hq][total_new] float.  A row that sees no key (its
- * pages are missing) has O = 0 and LSE = -infinity.  From one token to whole prompts.  ws: dev, sb_cache_attn_ws_bytes (host only). */
+ * pages are missing), or only keys whose scores are -infinity, has O = 0 and LSE = -infinity.  From one token to whole prompts.  ws: dev, sb_cache_attn_ws_bytes (host only). */
 int sb_cache_attn_ws_bytes(const sb_cache *c, const sb_chunk *n, int32_t window, int32_t sinks, int64_t *bytes_out);
 int sb_cache_attn(const sb_cache *c, const sb_chunk *n, int32_t window, int32_t sinks, const void *q, void *o, float *lse, void *ws, void *stream);
 

@@ -112,6 +112,9 @@ struct Keys {
   __device__ inline const T* v(int u) const { const int64_t o = offset(u); return o < 0 ? nullptr : (const T*)(PAGED ? P.cache.v : P.v) + o; }
 };
 
+// LSE of a row without any score above -infinity.  Over a cache it may see no key; in a packed batch it sees itself, and has no softmax: NaN, as in the block-sparse forward.
+template <bool PAGED> __device__ inline float empty_lse() { return PAGED ? -__builtin_inff() : __builtin_nanf(""); }
+
 // The other wavefronts' registers for the first one
 template <int N, int W>
 struct Sums {
@@ -208,8 +211,8 @@ __global__ __launch_bounds__(256) void window_fwd_f32_kernel(WindowParams P) {
     if (hf == 0) P.part_lse[(int64_t)z * P.T * P.Hq + at / D] = l == 0.f ? -__builtin_inff() : top + __builtin_log2f(l);
     return;
   }
-  store_column<D>((T*)P.o + at, acc, l == 0.f ? 0.f : 1.0f / l, hf);
-  if (hf == 0) P.lse[(int64_t)h * P.T + t.row0 + i] = l == 0.f ? -__builtin_inff() : (top + __builtin_log2f(l)) * 0.69314718055994531f;
+  store_column<D>((T*)P.o + at, acc, PAGED && l == 0.f ? 0.f : 1.0f / l, hf);  // (see the bfloat16 kernel)
+  if (hf == 0) P.lse[(int64_t)h * P.T + t.row0 + i] = l == 0.f ? empty_lse<PAGED>() : (top + __builtin_log2f(l)) * 0.69314718055994531f;
 }
 
 // Dr = rowsum(dO * O): 16 or 32 lanes to a row, four elements each.  (bfloat16: the dQ kernel does this.)
@@ -564,7 +567,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   wait_vmcnt<0>();
 
   l += __shfl_xor(l, 32, 64);  // the two lane halves hold different keys of the same row
-  const float inv = l == 0.f ? 0.f : 1.0f / l;  // (a sum that is no number is not one that saw nothing)
+  // (a sum that is no number is not one that saw nothing; in a packed batch a sum of zero makes O what it makes LSE: 0 / 0)
+  const float inv = PAGED && l == 0.f ? 0.f : 1.0f / l;
   if (PAGED && splits > 1) {
     if (mw + l32 >= rows) return;
     const int64_t row = ((int64_t)z * P.T + t.row0 + i) * P.Hq + h;
@@ -580,7 +584,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
                   return (bf16*)P.o + ((int64_t)(t.row0 + j) * P.Hq + g * P.G + mw + r - j * P.G) * D;
                 });
   if (hf == 0 && mw + l32 < rows)
-    P.lse[(int64_t)h * P.T + t.row0 + i] = l == 0.f ? -__builtin_inff() : (m * P.scale_log2e + __builtin_log2f(l)) * 0.69314718055994531f;
+    P.lse[(int64_t)h * P.T + t.row0 + i] = l == 0.f ? empty_lse<PAGED>() : (m * P.scale_log2e + __builtin_log2f(l)) * 0.69314718055994531f;
 }
 
 // ---------------------------------------------------------------------------------------------

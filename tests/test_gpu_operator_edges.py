@@ -111,3 +111,25 @@ def test_a_workspace_of_the_size_that_was_asked_for(have, new, Hq, Hkv):
     again = sb.sb_cache_attn(x.cache, x.chunk, x.q, ws=around[1024: 1024 + need])
     assert torch.equal(again[0], o) and torch.equal(again[1], lse)
     assert bool((around[:1024] == 0x5A).all()) and bool((around[1024 + need:] == 0x5A).all())
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 64)])
+def test_rows_whose_scores_are_all_minus_infinity(dtype, D):
+    """Such a row has no softmax: NaN in a packed batch, as in the block-sparse forward; over a cache it is a row that sees nothing."""
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    pb = batch((100, 30), 2, 1, D, dtype)
+    q, k, v = (normal(i, pb.T, h, D, dtype=t) for i, h in enumerate((2, 1, 1)))
+    q[:, 0, 0], q[:, 1, 0] = 1.0, -1.0
+    k[50:53, 0, 0] = -INF                                       # head 0: scores of -infinity, head 1: of +infinity
+    o, lse = sb.sb_window_attn_fwd(pb, 2, 0, q, k, v)
+    empty = torch.zeros(pb.T, dtype=torch.bool, device=DEV)
+    empty[51:53] = True                                         # both keys of the window
+    assert bool(torch.isnan(o[empty, 0]).all()) and bool(torch.isnan(lse[0, empty]).all())
+    assert bool(torch.isfinite(o[~empty, 0]).all()) and bool(torch.isfinite(lse[0, ~empty]).all())
+    assert torch.equal(o[50, 0], v[49, 0]) and torch.equal(o[53, 0], v[53, 0])
+    for have, new in (([99], [1]), ([40], [60])):
+        x = Served(have, new, 2, 1, D, 16, dtype)
+        x.q[:, 0, 0], x.q[:, 1, 0] = 1.0, 1.0
+        x.k_pages[:, :, :, 0] = -INF
+        o, lse = x.attend()
+        assert float(o.abs().max()) == 0 and bool((lse == -INF).all())
