@@ -315,8 +315,11 @@ int sb_rope_apply(const sb_problem *p, const sb_rope *r, const int32_t *position
  * least the longest sequence is dense causal attention.  O, LSE and the gradients are those of sb_sparse_attn_fwd / _bwd with these keys
  * in place of the selected ones.  Of `p` this reads total_tokens, num_seqs, the heads, head_dim, dtype, softmax_scale and cu_seqlens (both
  * copies); block_size, select_mode and the budgets are not read and may be anything.  SB_F32 tensors are computed in float32 throughout (matrix
- * instructions of that type), not rounded to bfloat16.  Non-finite values: a row's output depends on the elements of keys that it sees and, where a
- * V is not finite, on those of other keys of its sequence in the same 64-token tiles; in the backward also of Q, K and dO there.
+ * instructions of that type), not rounded to bfloat16.  Non-finite values: NaN and +infinity among the scores that a row sees make its O and
+ * LSE NaN.  What the mask hides has weight zero in products that take whole tiles (counted from the sequence's start), and zero times no number is none.
+ * So a V that is not finite (in the backward a K too) may reach O and dQ of rows that see any key of its 64-token tile, and of rows up to 31 tokens from such;
+ * and a row whose Q, O, LSE or dO is not finite may reach dK and dV of all keys of a 128-token block that it sees any key of: with sinks, of all keys of
+ * the block that they are in, from every later row.  It reaches nothing else, and no other sequence or KV head.  A row whose scores are all -infinity has O and LSE NaN.
  * Deterministic.  Tensors and ws start at multiples of 16 bytes; T * Hq/Hkv fits 31 bits.  ws: dev, sizes from sb_window_ws_bytes (host only; either output
  * may be null); of zero bytes it may be null. */
 int sb_window_ws_bytes(const sb_problem *p, int32_t window, int32_t sinks, int64_t *fwd_bytes_out, int64_t *bwd_bytes_out);
@@ -354,7 +357,7 @@ int sb_cache_append(const sb_cache *c, const sb_chunk *n, const sb_rope *r, cons
                     const void *v, int64_t v_pitch, void *q_out, void *stream);
 
 /* Attention of the new tokens over the cache, which holds them already (sb_cache_append): row i of sequence s is token t = cached[s] + i and sees
- * the keys u <= t with t - u < window or u < sinks.  q, o: dev [total_new][Hq][D]; lse: dev [Hq][total_new] float.  A row that sees no key (its
+ * the keys u <= t with t - u < window or u < sinks.  Non-finite values as in sb_window_attn_fwd.  q, o: dev [total_new][Hq][D]; lse: dev [Hq][total_new] float.  A row that sees no key (its
  * pages are missing), or only keys whose scores are -infinity, has O = 0 and LSE = -infinity.  From one token to whole prompts.  ws: dev, sb_cache_attn_ws_bytes (host only). */
 int sb_cache_attn_ws_bytes(const sb_cache *c, const sb_chunk *n, int32_t window, int32_t sinks, int64_t *bytes_out);
 int sb_cache_attn(const sb_cache *c, const sb_chunk *n, int32_t window, int32_t sinks, const void *q, void *o, float *lse, void *ws, void *stream);

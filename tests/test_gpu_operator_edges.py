@@ -133,3 +133,66 @@ def test_rows_whose_scores_are_all_minus_infinity(dtype, D):
         x.k_pages[:, :, :, 0] = -INF
         o, lse = x.attend()
         assert float(o.abs().max()) == 0 and bool((lse == -INF).all())
+
+
+def near(rows, n):
+    """Rows within 31 tokens of these."""
+    out = rows.clone()
+    for i in range(1, 32):
+        out[i:] |= rows[:n - i]
+        out[: n - i] |= rows[i:]
+    return out
+
+
+# head counts and lengths: dK/dV whole, in parts, with far rows and without, and in float32
+@pytest.mark.parametrize("what", ["q", "d_o", "k", "v"])
+@pytest.mark.parametrize("lens,Hq,Hkv,D,window,sinks,dtype", [((4200, 300), 16, 8, 128, 150, 0, "bf16"), ((4200, 300), 16, 8, 128, 150, 3, "bf16"), ((1300, 200), 4, 1, 64, 90, 70, "bf16"),
+                                                              ((900, 200), 7, 1, 128, 400, 4, "bf16"), ((2500,), 2, 1, 64, 100, 600, "bf16"), ((900, 100), 4, 2, 64, 90, 4, "f32"),
+                                                              ((600,), 2, 2, 128, 50, 0, "f32")])
+def test_how_far_what_is_no_number_reaches_in_the_backward(lens, Hq, Hkv, D, window, sinks, dtype, what):
+    """One NaN in the longest sequence.  Rows and keys that it must not reach are what they are without it, bit for bit."""
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    pb = batch(lens, Hq, Hkv, D, dtype)
+    x = {n: normal(i, pb.T, h, D, dtype=t) for i, (n, h) in enumerate((("q", Hq), ("k", Hkv), ("v", Hkv), ("d_o", Hq)))}
+
+    def run():
+        o, lse = sb.sb_window_attn_fwd(pb, window, sinks, x["q"], x["k"], x["v"])
+        return (o, lse.T, *sb.sb_window_attn_bwd(pb, window, sinks, x["q"], x["k"], x["v"], o, lse, x["d_o"]))
+    clean = run()
+    n, at, g = lens[0], 407, Hkv - 1
+    head = g if what in ("k", "v") else Hq - 1
+    x[what][at, head, 3] = float("nan")
+    got = run()
+    u = torch.arange(n, device=DEV)
+    seen = ref.visible(u, u, window, sinks)
+    tiles = lambda rows, size: torch.stack([seen[:, i: i + size][rows].any() for i in range(0, n, size)]).repeat_interleave(size)[:n]
+    rows = torch.zeros(n, dtype=torch.bool, device=DEV)
+    if what in ("q", "d_o"):
+        rows[at] = True                                   # that row alone, and the keys of the 128-token blocks that it sees any key of
+        must = rows
+    else:
+        tile = slice(at // 64 * 64, at // 64 * 64 + 64)
+        rows = near(seen[:, tile].any(1), n)              # rows that see a key of its 64-token tile, and those near them
+        must = seen[:, at]
+    keys = tiles(rows, 128)
+    keys[at] |= what in ("k", "v")
+    assert not bool(rows.all()) and (not bool(keys.all()) or sinks == 600)
+    group = slice(g * (Hq // Hkv), (g + 1) * (Hq // Hkv))
+    heads = slice(Hq - 1, Hq) if what in ("q", "d_o") else group
+    o, lse, dq, dk, dv = got
+    for name, a, b in zip(("o", "lse", "dq", "dk", "dv"), got, clean):
+        kv = name in ("dk", "dv")
+        same = torch.ones(pb.T, dtype=torch.bool, device=DEV)
+        same[:n] = ~(keys if kv else rows)
+        assert torch.equal(a[same], b[same]), name         # rows and keys that are too far, and other sequences
+        others = [h for h in range(a.shape[1]) if not (h == g if kv else heads.start <= h < heads.stop)]
+        assert torch.equal(a[:, others], b[:, others]), name
+        assert bool(torch.isfinite(b).all())
+    # and what it has to reach
+    nan_rows = lambda y: bool(torch.isnan(y).all())
+    mine = [Hq - 1] if what in ("q", "d_o") else list(range(group.start, group.stop))
+    for h in mine:
+        assert nan_rows(dq[:n, h][must])
+        if what in ("q", "k"):
+            assert nan_rows(o[:n, h][must]) and nan_rows(lse[:n, h][must])
+    assert nan_rows(dk[:n, g][seen[must].any(0)])
