@@ -439,7 +439,7 @@ def sb_window_ws_bytes(pb: Problem, window, sinks):
 
 
 def sb_window_attn_fwd(pb: Problem, window, sinks, q, k, v, o=None, lse=None, ws=None):
-    """Attention with a sliding window and sinks; pb's budgets and blocks are not read.  Returns (o, lse)."""
+    """Attention with a sliding window and sinks; pb's budgets and blocks are not read.  Returns (o, lse).  (ws: the forward needs none.)"""
     dt, (device, stream) = _TORCH_DTYPE[pb.dtype], _here()
     _batch(pb, device)
     queries, keys, rows = (pb.T, pb.Hq, pb.D), (pb.T, pb.Hkv, pb.D), (pb.Hq, pb.T)
@@ -455,7 +455,7 @@ def sb_window_attn_fwd(pb: Problem, window, sinks, q, k, v, o=None, lse=None, ws
     else:
         _tensor("lse", lse, rows, torch.float32, device)
     window, sinks = _window(window, sinks)
-    ws = _workspace(ws, sb_window_ws_bytes(pb, window, sinks)[0], device)
+    ws = _workspace(ws, 0, device)
     _call("sb_window_attn_fwd", C.addressof(pb.c), window, sinks, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), _address(ws),
           stream)
     return o, lse

@@ -19,10 +19,6 @@ namespace sb {
 __device__ inline f32x16 mfma_f32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
 
 __device__ inline f32x4 load4(const float* p) { return *(const f32x4*)p; }
-__device__ inline f32x4 load4(const bf16* p) {
-  const bf16x4 x = *(const bf16x4*)p;
-  return f32x4{(float)x[0], (float)x[1], (float)x[2], (float)x[3]};
-}
 __device__ inline void store4(float* p, f32x4 x) { *(f32x4*)p = x; }
 __device__ inline void store4(bf16* p, f32x4 x) {
   bf16x4 y;
@@ -1103,8 +1099,8 @@ __global__ __launch_bounds__(128 * PAIRS) __attribute__((amdgpu_waves_per_eu(2))
       for (int v = 0; v < 16; ++v) acc[dt][v] += from[(16 * dt + v) * 64];
   }
   __syncthreads();  // the stages' LDS is free
-  static_assert(NW * 32 * ROW_B <= (int)sizeof(stage) + (int)sizeof(pbuf) || MODE != kWhole, "every wavefront's rows");
-  char* const buf = wave * 32 * ROW_B + 32 * ROW_B <= (int)sizeof(stage) ? &stage[0][0] + wave * 32 * ROW_B : (char*)&pbuf[0][0][0] + (wave * 32 * ROW_B - (int)sizeof(stage) / (32 * ROW_B) * 32 * ROW_B);
+  static_assert(NW * 32 * ROW_B <= (int)sizeof(stage), "every wavefront's rows");
+  char* const buf = &stage[0][0] + wave * 32 * ROW_B;
   const float f = second ? P.scale : 1.0f;
   store_tile<D>(buf, lane, [&](int dt, int v) __attribute__((always_inline)) { return acc[dt][v] * f; },
                 [&](int r) __attribute__((always_inline)) -> bf16* {
