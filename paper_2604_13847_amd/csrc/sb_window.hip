@@ -280,7 +280,8 @@ __global__ __launch_bounds__(256) void window_dq_f32_kernel(WindowParams P) {
 }
 
 // Key-major: a workgroup owns 32 keys of a KV head and walks the flattened rows that see any of them, 32 at a time, in turn to its wavefronts; their sums are added in order.  At
-// head_dim 64 two wavefronts share a SIMD, each with 256 registers (16384 tokens, 8/2 heads, window 1024: 5.4 ms with one, 4.1 with two); at 128 the sums alone take 256.
+// head_dim 64 two wavefronts share a SIMD, each with 256 registers (16384 tokens, 8/2 heads, window 1024, 4 sinks: 5.4 ms with one, 4.2 with two); at 128 the sums alone take 256.
+// Sinks have no items of their own here: their tile's workgroup walks all rows of its sequence, and the launch is as long as that (the same without sinks: 1.0 ms).
 // PARTS: where items are few, near_parts workgroups share the rows of one, and window_dkv_f32_join_kernel adds their sums in order.  1024 tokens, one head, head_dim 64, window 200,
 // 4 sinks: 60 us whole (four wavefronts 72), 26 in four parts, their join included; 4000 tokens, 2/1 heads, window 500: 525 -> 221; 1024 tokens, 4/2 heads, head_dim 128: 210 -> 66.
 template <int D>
@@ -399,10 +400,12 @@ __global__ __launch_bounds__(256) void window_dkv_f32_join_kernel(WindowParams P
 // ---------------------------------------------------------------------------------------------
 // bfloat16 forward.  A workgroup of four wavefronts owns 128 flattened rows of a KV head, 32 a wavefront, and walks the 64-key tiles that any of them sees; K and V tiles are
 // shared in LDS and double-buffered by asynchronous loads.  A wavefront takes a tile as two halves of 32 keys, a step of the running softmax each.  A tile that a wavefront's rows
-// all see carries no mask; one that none of them sees is only waited for.  256 registers, so two wavefronts share a SIMD: one runs its exponentials while the other runs matrix
-// instructions, and a CU holds two workgroups (three or four at head_dim 64).  What bounds it is power: matrix cores 52 % busy at the 1.66 - 1.8 GHz that the chip keeps under this
-// load; at head_dim 64 vector work, 11.7 instructions per matrix instruction.  One sequence of 100001 tokens, 32/8 heads, window 2000: 3.3 ms, 1.0 PFLOP/s; 65536 tokens, 14/2 heads,
-// head_dim 64, window 1024: 0.29 ms, 0.8.  Measured against it: the halves' products and probabilities interleaved in one wavefront, S1 beside the probabilities of half 0 and O0 beside those
+// all see carries no mask; one that none of them sees is only waited for.  256 registers, so two wavefronts share a SIMD, and a CU holds two workgroups (three or four at
+// head_dim 64).  What bounds it: at head_dim 128 matrix instructions take 52 to 54 % of the cycles and vector instructions 49 %, about all of them between them, so the one
+// wavefront's exponentials hardly run beside the other's matrix instructions; of a wavefront's time 23 % are waits for loads and barriers, 33 % waits for its turn.  The chip keeps
+// 1.5 GHz in the longest launches, as under the library's product, whose matrix cores are 75 % busy.  At head_dim 64 it is vector work: 83 % of the cycles, 11.7 instructions per
+// matrix instruction.  One sequence of 100001 tokens, 32/8 heads, window 2000: 3.55 ms, 0.92 PFLOP/s; dense causal, 32768 tokens: 8.2 ms, 1.07; 65536 tokens, 14/2 heads, head_dim 64,
+// window 1024: 0.31 ms, 0.75.  Measured against it: the halves' products and probabilities interleaved in one wavefront, S1 beside the probabilities of half 0 and O0 beside those
 // of half 1: the same at head_dim 128, 0.29 -> 0.36 ms at 64; priorities between the wavefronts: the same; eight wavefronts and 256 rows a workgroup: the same on long sequences, 2039
 // tokens in short ones 26 -> 20 us with four.
 template <int D, bool PAGED>
@@ -585,9 +588,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
 
 // ---------------------------------------------------------------------------------------------
 // bfloat16 dQ.  Rows, tiles and their walk as in the forward kernel; a half tile is S, dP and dQ += dS K, whose operands go through one set of registers.  Every row belongs to one
-// workgroup here, so this is also where Dr is computed, from the dO in registers and one read of O, and left with LSE for the next kernel.  32768 tokens, 32/8 heads, window 4096: 1.8 ms,
-// 1.12 PFLOP/s, matrix cores 64 % busy; 65536 tokens, 14/2 heads, head_dim 64, window 1024: 0.38 ms, 0.92 PFLOP/s (with eight wavefronts a workgroup, whose four SIMDs all wait at the same
-// barrier, 0.48).
+// workgroup here, so this is also where Dr is computed, from the dO in registers and one read of O, and left with LSE for the next kernel.  32768 tokens, 32/8 heads, window 4096: 1.87 ms,
+// 1.08 PFLOP/s, matrix cores 63 % busy, vector instructions 42 % of the cycles; 65536 tokens, 14/2 heads, head_dim 64, window 1024: 0.42 ms, 0.84 PFLOP/s, 52 and 67 % (with eight
+// wavefronts a workgroup, whose four SIMDs all wait at the same barrier, 0.38 -> 0.48 on another card).
 template <int D>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void window_dq_kernel(WindowParams P) {
   constexpr int ROWS = 32 * kWaves, ROW_B = D * 2, TILE_B = 64 * ROW_B, NOP = D / 16;
@@ -762,7 +765,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
 // SIMD: the first computes S and P and adds P^T dO to dV, the second, a stage behind, dP and dS = P (dP - Dr) and adds dS^T Q to dK; P goes from one to the other through LDS
 // in float32, lane by lane (both hold keys in columns).  Each so needs 150 registers where one wavefront for both would need more than the 256 that let two share a SIMD,
 // and has as many matrix instructions as the other.  The second one has the loads to issue besides, and goes first (32768 tokens, 32/8 heads, window 4096: 3.28 -> 2.75 ms; the first
-// going first 3.07; the first with the loads 3.17).  What it measured in all: 0.97 PFLOP/s there, matrix cores 60 % busy; 65536 tokens, 14/2 heads, head_dim 64: 0.61 ms, 0.77.  What took it
+// going first 3.07; the first with the loads 3.17).  What it measures in all, on a card whose library product
+// is 5 % slower than on that one: 2.9 ms and 0.93 PFLOP/s there, matrix cores 60 % busy; 65536 tokens, 14/2 heads, head_dim 64: 0.65 ms, 0.72, 50 %.  What took it
 // there from 5.15 ms: no spilled registers in the loop (a reload waits for all loads in flight: 7 - 11 ms with a pipeline of two stages that needed 16 more), no integer division in it, LSE
 // and Dr subtracted by a step of the matrix product instead of 32 registers and LDS reads of them, and far rows in many short items.
 // The stages' Q and dO rows, LSE and Dr come by asynchronous loads, three stages ahead (kFar: two, so that two of its workgroups share a CU's LDS).
@@ -770,7 +774,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
 // Sinks are seen by all rows of their sequence.  The rows behind a sink tile's ordinary ones (far rows) are the work of other workgroups (kFar), far_rows tokens each, that leave their
 // sums in float32; the tile's own workgroup, launched after them, adds them in order.  So the result does not depend on who is ahead, and no workgroup has more than its share.
 constexpr int kDkvKeys = 128;   // keys of a workgroup, but of kFar
-constexpr int kFarSinks = 512;  // with more sinks than this there are sink tiles enough to fill the chip: their own workgroups take all rows
+// With more sinks than this their own workgroups take all rows, since there are then sink tiles enough to fill the chip, if KV heads are several.  Backward of 65536 tokens, 32/8 heads, window 1024, with
+// far items and without: 4 sinks 4.5 and 10.9 ms, 256: 5.6 and 9.8, 512: 7.0 and 10.2, 1024: 9.8 and 10.6, 2048: 15.1 and 12.1.  (With few heads far items are ahead throughout: 32768 tokens, 8/2
+// heads, head_dim 64, 2048 sinks: 0.85 and 2.67 ms.)
+constexpr int kFarSinks = 512;
 // Far items of a sequence of n tokens: far_blocks blocks of sinks, far_segments each (some may be empty: the first rows of a block's last ones).
 // The rows are read once a block, so a block is 64 sinks where there are more than 32 (65536 tokens, 14/2 heads, 64 sinks: 66 us, in two blocks 105).
 __host__ __device__ inline int far_keys(int sinks) { return sinks > 32 ? 64 : 32; }
@@ -1170,7 +1177,9 @@ static int64_t longest(const int32_t* cu, int S) {
   return n;
 }
 // Far rows a far item takes: short enough that a long sequence's sinks are many workgroups' work, and no more than 64 of them to a block of sinks, whose sums its own workgroup adds.  None
-// where all of a sequence is at most twice an ordinary item's rows: a launch of their own costs more than the sinks' workgroups are longer then (2039 tokens in short sequences: 20 us).
+// where all of a sequence is at most twice an ordinary item's rows: a launch of their own costs more than the sinks' workgroups are longer then.  Backward of one sequence, 16/2 heads, 4 sinks,
+// without far items and with them: window 512, 2 times its rows 74 and 121 us, 3 times 99 and 127, 4 times 150 and 141; window 2048, 1.5 times 262 and 258 us, 2 times 440 and 332, 3 times 905 and 458.
+// (Batches of many sequences with 32/8 heads fill the chip either way: with them 0 to 6 % less time from 1.2 to 3 times, 16 % at 4.)
 static int far_rows_of(int64_t longest, int window) {
   if (longest <= 2 * ((int64_t)window + kDkvKeys)) return 0;
   const int64_t rows = (longest - window + 63) / 64;
