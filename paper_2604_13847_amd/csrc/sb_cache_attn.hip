@@ -417,7 +417,7 @@ int sb_cache_attn(const sb_cache* c, const sb_chunk* n, int32_t window, int32_t 
   const bool f32 = c->dtype == SB_F32;
   const int64_t rows = P.T, seq_rows = few_seq_rows(P.G, P.max_new);
   dim3 grid, all_rows, few_rows;
-  if ((rc = grid_of(plan.few.items * P.Hkv * plan.few.splits, 256, &grid)) != SB_OK || (plan.many.splits > 1 && (rc = grid_of(rows * P.Hq, 256, &all_rows)) != SB_OK) ||
+  if ((rc = grid_of(plan.few.items * P.Hkv * plan.few.splits, 128, &grid)) != SB_OK || (plan.many.splits > 1 && (rc = grid_of(rows * P.Hq, 256, &all_rows)) != SB_OK) ||
       (plan.few.splits > 1 && (rc = grid_of(seq_rows * P.S * P.Hq, 256, &few_rows)) != SB_OK))
     return rc;
   KernelTimer kt(K_CACHE_ATTN, st);

@@ -68,3 +68,9 @@ def test_rotations_of_very_many_tokens(tmp_path):
         assert r.returncode == 0, r.stdout[-2000:]
         x, y, z, threads, _, _ = (int(n) for n in r.stdout.split("launch")[1].split())
         assert (y, z, threads) == (1, 1, 256) and x <= workgroups and x * threads < 1 << 32, (T, x)
+
+
+def test_single_tokens_of_very_many_sequences(launches):  # noqa: F811
+    # 65536 sequences, 8 KV heads, 32 runs of keys: 2^24 workgroups of two wavefronts
+    x = launches("cache", 65536, 65536, 1, 32700, 32, 8, 128, 0, NONE)
+    assert [k for k, _, _ in x] == ["cache_split_kernel", "cache_merge_kernel"] and x[0][2] == 65536 * 8 * 32
