@@ -508,6 +508,9 @@ class Chunk:
         self.device = device
         _tensor("cu_new", cu_new, (S + 1,), torch.int32, device)
         _tensor("cached", cached, (S,), torch.int32, device)
+        for name, x in (("Hq", Hq), ("total_new", total_new), ("max_new", max_new), ("max_length", max_length)):
+            if not -2 ** 31 <= x < 2 ** 31:
+                raise SparseBalError(f"{name}: {x} does not fit 32 bits")
         self.cu_new, self.cached, self.Hq, self.total_new = cu_new, cached, int(Hq), int(total_new)
         self.c = sb_chunk(S, int(Hq), int(total_new), int(max_new), int(max_length), float(softmax_scale), cu_new.data_ptr(), cached.data_ptr())
 

@@ -68,3 +68,16 @@ def test_the_library_is_there_for_all_threads_at_once(monkeypatch):
     monkeypatch.setattr(sb, "_lib", None)
     monkeypatch.setattr(sb.C, "CDLL", lambda path: Loaded())
     assert isinstance(sb.lib(), Loaded) and sb._lib is sb.lib()
+
+
+def test_sizes_of_new_tokens_that_do_not_fit_32_bits(monkeypatch):
+    """They would arrive as other numbers."""
+    import torch
+    monkeypatch.setattr(sb, "_here", lambda: (-1, 0))
+    cu, cached = torch.zeros(3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    sb.Chunk(cu, cached, 4, 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1)
+    for sizes in ((2 ** 32 + 2, 1, 10), (2, 2 ** 32 + 1, 10), (2, 1, 2 ** 31), (2, 1, -(2 ** 32) + 10)):
+        with pytest.raises(sb.SparseBalError, match="32 bits"):
+            sb.Chunk(cu, cached, 4, *sizes)
+    with pytest.raises(sb.SparseBalError, match="32 bits"):
+        sb.Chunk(cu, cached, 2 ** 32 + 4, 2, 1, 10)
