@@ -30,6 +30,26 @@ def test_tokens_behind_the_page_table_are_seen_by_no_row(have, new, page, column
             assert float(o[rows].abs().max()) == 0 and bool((lse[:, rows] == -INF).all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new,window,sinks", [([200, 1], 16, NONE), ([200, 1], NONE, 0), ([1, 2], 16, 70), ([1, 2], 100, 0), ([150, 3], 300, 64)])
+def test_positions_far_behind_the_page_table(new, window, sinks, dtype):
+    """Rows at the last positions that there are, over a table of 80 tokens: they see its sinks, or all of it in a window of everything, and no call walks what does not exist."""
+    x = Served([60, 79], [20, 1], 8, 2, 64, 16, dtype)
+    first = [2 ** 31 - 1 - n for n in new]
+    cu = torch.tensor([0, new[0], sum(new)], dtype=torch.int32, device=DEV)
+    chunk = sb.Chunk(cu, torch.tensor(first, dtype=torch.int32, device=DEV), 8, sum(new), max(new), NONE)
+    assert x.table.shape[1] == 5
+    q = normal(3, sum(new), 8, 64, dtype=x.dtype)
+    o, lse = sb.sb_cache_attn(x.cache, chunk, q, window, sinks)
+    u = torch.arange(80, device=DEV)
+    for s in (0, 1):
+        rows = slice(int(cu[s]), int(cu[s + 1]))
+        seen = ref.visible(torch.arange(first[s], first[s] + new[s], device=DEV), u, window, sinks)
+        r = ref.Attention(q[rows].double(), x.k[s].double(), x.v[s].double(), seen, 64 ** -0.5, ref.HALF[x.dtype])
+        ref.check("o", o[rows], r.o, r.o_tol)
+        ref.check("lse", lse[:, rows], r.lse, r.lse_tol)
+
+
 # ---------------------------------------------------------------- what is no number
 # have, new, window, sinks, the key: one run of keys and several, single tokens and chunks; rows that see the key and rows that do not
 PLANTED = [([50, 20], [1, 1], NONE, 0, 33), ([4000, 300], [1, 1], NONE, 0, 1003), ([4000, 300], [1, 1], 100, 0, 1003), ([0, 40], [300, 5], 100, 0, 130), ([0], [300], 100, 7, 5),
