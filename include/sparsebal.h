@@ -333,7 +333,8 @@ int sb_window_attn_bwd(const sb_problem *p, int32_t window, int32_t sinks, const
  * Tokens j*page_size .. (j+1)*page_size - 1 of sequence s live in page page_table[s][j].  An entry outside 0 .. num_pages - 1 is no page: nothing
  * is written there and its keys are seen by no row; so are tokens from max_pages*page_size on.  Nothing of a page behind the sequence's last token is
  * used, whatever it holds.  Pages may be shared between sequences; one that sb_cache_append writes to belongs to one sequence, and stands in its row
- * once.  All sizes that change from step to step are on the device, so that a captured graph can be replayed with other lengths within max_new and max_pages.  Tensors, pages and ws start at multiples of 16 bytes. */
+ * once.  All sizes that change from step to step are on the device, so that a captured graph can be replayed with other lengths within max_new and
+ * max_pages.  Tensors, pages and ws start at multiples of 16 bytes. */
 typedef struct sb_cache {
   int32_t num_pages, page_size; /* page_size: a power of two, 16 .. 1024 */
   int32_t num_kv_heads, head_dim, dtype; /* head_dim 64 or 128; SB_BF16 | SB_F32 */
