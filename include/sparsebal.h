@@ -308,6 +308,30 @@ int sb_rope_init(sb_rope *out, int32_t rot_dim, int32_t layout, double base, int
 int sb_rope_apply(const sb_problem *p, const sb_rope *r, const int32_t *positions, const void *q, int64_t q_pitch, const void *k,
                   int64_t k_pitch, void *q_out, void *k_out, int direction, void *stream);
 
+/* Positions with several axes (time, height and width of image and video tokens): pair i turns by the position on axis axis[i], so
+ * a = 2 pi * positions[axis[i]][token] * turns[i].
+ *
+ * sb_rope_axes is plain data like sb_rope; sb_rope_axes_init fills it from how many pairs each axis has: SB_AXES_SECTIONS, the first pairs are axis 0's, the next
+ * ones axis 1's; SB_AXES_IN_TURN, pairs are dealt to axes 0, 1, .., num_axes - 1, 0, 1, .. and an axis that has all of its pairs is left out.  Frequencies stay those of the
+ * rope.  Where each axis has frequencies of its own that start anew, sb_rope_join puts the axes' ropes one behind the other (SB_AXES_SECTIONS then): rot_dim is the sum, layout and
+ * amplitude have to be the same in all. */
+#define SB_ROPE_MAX_AXES 8
+#define SB_AXES_SECTIONS 0
+#define SB_AXES_IN_TURN 1
+typedef struct sb_rope_axes {
+  int32_t num_axes;                  /* 1 .. SB_ROPE_MAX_AXES */
+  uint8_t axis[SB_ROPE_MAX_PAIRS];   /* of pairs 0 .. rot_dim/2 - 1, below num_axes */
+} sb_rope_axes;
+
+/* Host only.  pairs: host [num_axes], none negative, at least one and at most SB_ROPE_MAX_PAIRS in all. */
+int sb_rope_axes_init(sb_rope_axes *out, int32_t num_axes, const int32_t *pairs, int32_t order);
+/* Host only.  `out` may be one of the ropes. */
+int sb_rope_join(sb_rope *out, const sb_rope *ropes, int32_t num_ropes);
+
+/* sb_rope_apply with positions of several axes: dev int32 [num_axes][T].  cu_seqlens is not read on the device. */
+int sb_rope_axes_apply(const sb_problem *p, const sb_rope *r, const sb_rope_axes *axes, const int32_t *positions, const void *q, int64_t q_pitch,
+                       const void *k, int64_t k_pitch, void *q_out, void *k_out, int direction, void *stream);
+
 /* ---- attention with a sliding window and sinks ----
  *
  * Causal attention of the same packed batches at the granularity of tokens: row t of a sequence sees the keys u <= t with t - u < window or
@@ -357,11 +381,69 @@ typedef struct sb_chunk {       /* the new tokens of num_seqs sequences, packed:
 int sb_cache_append(const sb_cache *c, const sb_chunk *n, const sb_rope *r, const void *q, int64_t q_pitch, const void *k, int64_t k_pitch,
                     const void *v, int64_t v_pitch, void *q_out, void *stream);
 
+/* sb_cache_append with positions of several axes: dev int32 [num_axes][total_new].  What a token turns by is theirs; where it is kept, and what it sees, still goes by cached[s] + i. */
+int sb_cache_append_axes(const sb_cache *c, const sb_chunk *n, const sb_rope *r, const sb_rope_axes *axes, const int32_t *positions, const void *q, int64_t q_pitch,
+                         const void *k, int64_t k_pitch, const void *v, int64_t v_pitch, void *q_out, void *stream);
+
 /* Attention of the new tokens over the cache, which holds them already (sb_cache_append): row i of sequence s is token t = cached[s] + i and sees
  * the keys u <= t with t - u < window or u < sinks.  Non-finite values as in sb_window_attn_fwd.  q, o: dev [total_new][Hq][D]; lse: dev [Hq][total_new] float.  A row that sees no key (its
  * pages are missing), or only keys whose scores are -infinity, has O = 0 and LSE = -infinity.  From one token to whole prompts.  ws: dev, sb_cache_attn_ws_bytes (host only). */
 int sb_cache_attn_ws_bytes(const sb_cache *c, const sb_chunk *n, int32_t window, int32_t sinks, int64_t *bytes_out);
 int sb_cache_attn(const sb_cache *c, const sb_chunk *n, int32_t window, int32_t sinks, const void *q, void *o, float *lse, void *ws, void *stream);
+
+/* ---- page tables built on the GPU ----
+ *
+ * A pool of pages and the tables of the sequences that hold them, all on the device.  Row s of page_table holds the sequence's pages in entries 0 .. held[s] - 1 and
+ * -1 behind them; a page that no row holds is one of free_pages[0 .. free_count - 1], a stack.  The caller fills them once (free_pages with all pages, free_count
+ * num_pages, held 0, the table -1), and sb_cache_tables keeps them: after the call row s holds as many pages as its tokens take, ceil(length / page_size), at most max_pages,
+ * where its length is cached[s] + added[s], or 0 where added[s] < 0 (the sequence is finished).  Entries that are too many go back first, the last entry of the last
+ * row before all others; then the rows' missing entries are filled in order from the stack's top.  So two calls that undo each other's lengths (room for drafted tokens,
+ * and the end of those that were rejected) leave everything as it was.  Where pages run out, the first rows get them; missing_out (dev, may be null) is how many lacked.
+ * Negative `cached` counts as 0; held and free_count outside what the arrays hold are taken as the nearest value inside.  Rows own their pages: none stands in two rows.
+ *
+ * Also written, all of the call's new tokens packed as in sb_chunk: cu_new_out dev [num_seqs+1] (of max(added, 0); sums stop at 2^31 - 1); and, each unless null, for tokens
+ * 0 .. total_new - 1 positions_out dev int32 (cached[s] + i) and slots_out dev int64 (page * page_size + token of the page, -1: no page).  Of tokens behind the last sequence
+ * the slot is -1 and the position 0.  total_new is the arrays' size, and with them null it is not read.  cached and added: dev [num_seqs].  No workspace; a captured call serves all steps. */
+typedef struct sb_page_pool {
+  int32_t num_seqs, max_pages, num_pages;
+  int32_t page_size;          /* a power of two, 16 .. 1024 */
+  int32_t *page_table;        /* dev [num_seqs][max_pages] */
+  int32_t *held;              /* dev [num_seqs] */
+  int32_t *free_pages;        /* dev [num_pages] */
+  int32_t *free_count;        /* dev [1] */
+} sb_page_pool;
+int sb_cache_tables(const sb_page_pool *pool, const int32_t *cached, const int32_t *added, int32_t total_new, int32_t *cu_new_out, int32_t *positions_out,
+                    int64_t *slots_out, int32_t *missing_out, void *stream);
+
+/* ---- a paged cache in four bits ----
+ *
+ * The cache of sb_cache_append and sb_cache_attn with keys and values in four bits: 32 neighbouring elements of a head share a step, and an element is that step times 0, 1/2, 1, 3/2,
+ * 2, 3, 4 or 6 (codes 0 .. 7; 8 more: negative).  The step is 1/6 of the 32 elements' largest magnitude (their product with the float nearest 1/6), rounded to six significant bits (and a multiple of 2^-131; halves
+ * away from zero) and at most 1.3125 * 2^125; a code is that of the nearest value, ties to the even code, of the largest where an element is beyond it, and 0 where the step is 0 or no number.  So every value held is a bfloat16 number; where it
+ * is used nothing is rounded again.  32 elements of which one is no number or infinite are all NaN.  Keys are turned in float64 and rounded to float32 before that, so that codes do
+ * not depend on how the turn is computed.
+ *
+ * Per token and KV head D/2 bytes of codes (the lower half of a byte first) and D/32 steps (bfloat16).  Byte D/8 b + 4 c + e of a key holds elements 32 c + 8 b + 2 e and
+ * the next (c < D/32, b < 4, e < 4); byte D/32 i + e of a value holds elements 32 e + i and 32 e + 16 + i (i < 16).  80 bytes at head_dim 128 where bfloat16 takes 256. */
+typedef struct sb_cache4 {
+  int32_t num_pages, page_size;          /* as in sb_cache */
+  int32_t num_kv_heads, head_dim, dtype; /* dtype: of the new tokens, the queries and the output (SB_BF16 | SB_F32); the pages are the same */
+  int32_t max_pages;
+  void *k, *v;                  /* dev [num_pages][num_kv_heads][page_size][head_dim/2] bytes */
+  void *k_step, *v_step;        /* dev [num_pages][num_kv_heads][page_size][head_dim/32] bfloat16 */
+  const int32_t *page_table;    /* dev [num_seqs][max_pages] */
+} sb_cache4;
+
+/* sb_cache_append (axes and positions null) or sb_cache_append_axes into such pages.  r may be null only without axes.  k_held, v_held (dev, contiguous, [total_new][Hkv][D] in c->dtype, or null): the
+ * values as they are held from now on, for attention over the packed tokens of a first prompt. */
+int sb_cache4_append(const sb_cache4 *c, const sb_chunk *n, const sb_rope *r, const sb_rope_axes *axes, const int32_t *positions, const void *q, int64_t q_pitch, const void *k,
+                     int64_t k_pitch, const void *v, int64_t v_pitch, void *q_out, void *k_held, void *v_held, void *stream);
+
+/* sb_cache_attn over such pages: the same rows, mask and outputs.  In SB_BF16 probabilities are rounded to bfloat16 once for the product with V; in SB_F32 queries and probabilities are taken as
+ * three bfloat16 numbers that add up to them, so that products are exact but for 2^-24.  Keys that a row does not see reach it only where their steps are no numbers, and then
+ * only from the same tile of 64 keys.  ws: dev, sb_cache4_attn_ws_bytes (host only). */
+int sb_cache4_attn_ws_bytes(const sb_cache4 *c, const sb_chunk *n, int32_t window, int32_t sinks, int64_t *bytes_out);
+int sb_cache4_attn(const sb_cache4 *c, const sb_chunk *n, int32_t window, int32_t sinks, const void *q, void *o, float *lse, void *ws, void *stream);
 
 /* Instrumentation (measurement only; off by default).  `flag` is a bit set:
  *   SB_INSTR_CU_BUSY  the attention kernels add, for every workgroup, its run time in ticks of the
@@ -378,8 +460,8 @@ int sb_cache_attn(const sb_cache *c, const sb_chunk *n, int32_t window, int32_t 
 #define SB_CU_SLOTS 512
 #define SB_INSTR_CU_BUSY 1
 #define SB_INSTR_KERNEL_EVENTS 2
-#define SB_NUM_KERNELS 15 /* pool, score, topk, plan, fwd, bwd_prep, bwd_dq, bwd_dkv, coverage, score_select, rope (and append), window_fwd,
-                             window_dq (and what prepares it), window_dkv, cache_attn; bwd_prep is the
+#define SB_NUM_KERNELS 15 /* pool, score, topk, plan (and page tables), fwd, bwd_prep, bwd_dq, bwd_dkv, coverage, score_select, rope (and append), window_fwd,
+                             window_dq (and what prepares it), window_dkv, cache_attn (in four bits too); bwd_prep is the
                              conversion of float32 inputs in the backward call (nothing for bf16 inputs); score_select is the
                              single kernel of sb_score_select, without scores_out or in small problems */
 int sb_set_instrumentation(int flag);

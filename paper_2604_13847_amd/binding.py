@@ -23,7 +23,8 @@ SB_CU_SLOTS = 512
 EXPORTS = ["sb_get_layout", "sb_keep_ratio_to_topk", "sb_sel_rowptr_host", "sb_block_scores", "sb_select_topk", "sb_select_topk_static", "sb_score_select",
            "sb_plan_worklist", "sb_plan_sections", "sb_sparse_attn_fwd", "sb_sparse_attn_bwd", "sb_score_coverage", "sb_perf_predict", "sb_perf_align", "sb_dst_tune",
            "sb_rope_init", "sb_rope_apply", "sb_window_ws_bytes", "sb_window_attn_fwd", "sb_window_attn_bwd", "sb_cache_append",
-           "sb_cache_attn_ws_bytes", "sb_cache_attn", "sb_spar_update", "sb_spar_predict", "sb_balanced_partition", "sb_sab_batches",
+           "sb_cache_attn_ws_bytes", "sb_cache_attn", "sb_rope_axes_init", "sb_rope_join", "sb_rope_axes_apply", "sb_cache_append_axes", "sb_cache_tables",
+           "sb_cache4_append", "sb_cache4_attn_ws_bytes", "sb_cache4_attn", "sb_spar_update", "sb_spar_predict", "sb_balanced_partition", "sb_sab_batches",
            "sb_set_instrumentation", "sb_read_cu_busy", "sb_read_kernel_times",
            "sb_last_error", "sb_version"]
 
@@ -53,6 +54,23 @@ SB_ROPE_MAX_PAIRS = 64
 class sb_rope(C.Structure):
     _fields_ = [("rot_dim", C.c_int32), ("layout", C.c_int32), ("amplitude", C.c_float), ("reserved", C.c_int32),
                 ("turns", C.c_double * SB_ROPE_MAX_PAIRS)]
+
+
+SB_ROPE_MAX_AXES = 8
+
+
+class sb_rope_axes(C.Structure):
+    _fields_ = [("num_axes", C.c_int32), ("axis", C.c_uint8 * SB_ROPE_MAX_PAIRS)]
+
+
+class sb_page_pool(C.Structure):
+    _fields_ = [("num_seqs", C.c_int32), ("max_pages", C.c_int32), ("num_pages", C.c_int32), ("page_size", C.c_int32), ("page_table", C.c_void_p), ("held", C.c_void_p),
+                ("free_pages", C.c_void_p), ("free_count", C.c_void_p)]
+
+
+class sb_cache4(C.Structure):
+    _fields_ = [("num_pages", C.c_int32), ("page_size", C.c_int32), ("num_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("max_pages", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("k_step", C.c_void_p), ("v_step", C.c_void_p), ("page_table", C.c_void_p)]
 
 
 class sb_cache(C.Structure):
@@ -319,7 +337,9 @@ def _call(name, *args):
     if _calls is None:
         P, I, L = C.c_void_p, C.c_int32, C.c_int64
         types = {"sb_rope_apply": [P, P, P, P, L, P, L, P, P, I, P], "sb_window_attn_fwd": [P, I, I] + [P] * 7, "sb_window_attn_bwd": [P, I, I] + [P] * 11,
-                 "sb_cache_append": [P, P, P, P, L, P, L, P, L, P, P], "sb_cache_attn": [P, P, I, I] + [P] * 5}
+                 "sb_cache_append": [P, P, P, P, L, P, L, P, L, P, P], "sb_cache_attn": [P, P, I, I] + [P] * 5,
+                 "sb_rope_axes_apply": [P, P, P, P, P, L, P, L, P, P, I, P], "sb_cache_append_axes": [P, P, P, P, P, P, L, P, L, P, L, P, P],
+                 "sb_cache_tables": [P, P, P, I] + [P] * 5, "sb_cache4_append": [P, P, P, P, P, P, L, P, L, P, L] + [P] * 4, "sb_cache4_attn": [P, P, I, I] + [P] * 5}
         # (function objects of their own: those of `lib()` keep taking what ctypes makes of their arguments.  All at once: another thread may be here too)
         _calls = {n: C.CFUNCTYPE(C.c_int, *t)((n, lib())) for n, t in types.items()}
     rc = _calls[name](*args)
@@ -392,6 +412,28 @@ class Rope:
         _check(lib().sb_rope_init(C.byref(self.c), int(rot_dim), int(layout), C.c_double(base), int(scaling), C.c_double(factor),
                                   C.c_double(original_length), C.c_double(low), C.c_double(high)))
 
+    @classmethod
+    def joined(cls, ropes):
+        """The pairs of several ropes one behind the other, each with frequencies of its own: for axes whose frequencies start anew."""
+        self, all_of = cls.__new__(cls), (sb_rope * max(len(ropes), 1))(*[r.c for r in ropes])
+        self.c = sb_rope()
+        _check(lib().sb_rope_join(C.byref(self.c), all_of, len(ropes)))
+        return self
+
+    def ref(self):
+        return C.byref(self.c)
+
+
+SB_AXES_SECTIONS, SB_AXES_IN_TURN = 0, 1
+
+
+class RopeAxes:
+    """Holds sb_rope_axes: which axis each pair of elements turns by, from how many pairs every axis has."""
+
+    def __init__(self, pairs, order=SB_AXES_SECTIONS):
+        self.c, n = sb_rope_axes(), np.ascontiguousarray(pairs, dtype=np.int32)
+        _check(lib().sb_rope_axes_init(C.byref(self.c), len(n), _ptr(n), int(order)))
+
     def ref(self):
         return C.byref(self.c)
 
@@ -420,6 +462,29 @@ def sb_rope_apply(pb: Problem, rope: Rope, q, k, positions=None, backward=False,
         _tensor("positions", positions, (pb.T,), torch.int32, device)
     _call("sb_rope_apply", C.addressof(pb.c), C.addressof(rope.c), _address(positions), _address(q), _pitch(q), _address(k), _pitch(k), _address(q_out),
           _address(k_out), 1 if backward else 0, stream)
+    return q_out, k_out
+
+
+def sb_rope_axes_apply(pb: Problem, rope: Rope, axes: RopeAxes, positions, q, k, backward=False, q_out=None, k_out=None):
+    """sb_rope_apply with positions of several axes, [axes][tokens] int32.  Returns (q, k) turned, or gradients turned back."""
+    dt, (device, stream) = _TORCH_DTYPE[pb.dtype], _here()
+    if q is not None:
+        shape = (pb.T, pb.Hq, pb.D)
+        _tensor("q", q, shape, dt, device, pitch=True)
+        if q_out is None:
+            q_out = torch.empty(shape, dtype=dt, device=q.device)
+        else:
+            _tensor("q_out", q_out, shape, dt, device)
+    if k is not None:
+        shape = (pb.T, pb.Hkv, pb.D)
+        _tensor("k", k, shape, dt, device, pitch=True)
+        if k_out is None:
+            k_out = torch.empty(shape, dtype=dt, device=k.device)
+        else:
+            _tensor("k_out", k_out, shape, dt, device)
+    _tensor("positions", positions, (axes.c.num_axes, pb.T), torch.int32, device)
+    _call("sb_rope_axes_apply", C.addressof(pb.c), C.addressof(rope.c), C.addressof(axes.c), positions.data_ptr(), _address(q), _pitch(q), _address(k), _pitch(k),
+          _address(q_out), _address(k_out), 1 if backward else 0, stream)
     return q_out, k_out
 
 
@@ -570,6 +635,162 @@ def sb_cache_attn(cache: Cache, chunk: Chunk, q, window=2 ** 31 - 1, sinks=0, o=
     window, sinks = _window(window, sinks)
     ws = _workspace(ws, sb_cache_attn_ws_bytes(cache, chunk, window, sinks), device)
     _call("sb_cache_attn", C.addressof(cache.c), C.addressof(chunk.c), window, sinks, q.data_ptr(), o.data_ptr(), lse.data_ptr(), _address(ws), stream)
+    return o, lse
+
+
+def sb_cache_append_axes(cache: Cache, chunk: Chunk, k, v, rope: Rope, axes: RopeAxes, positions, q=None, q_out=None):
+    """sb_cache_append with positions of several axes, [axes][new tokens] int32."""
+    n, D, dt, (device, stream) = chunk.total_new, cache.c.head_dim, cache.k.dtype, _here()
+    _same_sequences(cache, chunk, device)
+    keys, queries = (n, cache.c.num_kv_heads, D), (n, chunk.Hq, D)
+    _tensor("k", k, keys, dt, device, pitch=True)
+    _tensor("v", v, keys, dt, device, pitch=True)
+    if q is not None:
+        _tensor("q", q, queries, dt, device, pitch=True)
+        if q_out is None:
+            q_out = torch.empty(queries, dtype=dt, device=q.device)
+        else:
+            _tensor("q_out", q_out, queries, dt, device)
+    elif q_out is not None:
+        raise SparseBalError("q_out without q")
+    _tensor("positions", positions, (axes.c.num_axes, n), torch.int32, device)
+    _call("sb_cache_append_axes", C.addressof(cache.c), C.addressof(chunk.c), C.addressof(rope.c), C.addressof(axes.c), positions.data_ptr(), _address(q), _pitch(q),
+          k.data_ptr(), _pitch(k), v.data_ptr(), _pitch(v), _address(q_out), stream)
+    return q_out
+
+
+class PagePool:
+    """Holds sb_page_pool plus the tensors it points to, all int32: page_table [sequences][most pages of one], held [sequences], free_pages [pages], free_count [1]."""
+
+    def __init__(self, page_table, held, free_pages, free_count, page_size):
+        if page_table.dim() != 2:
+            raise SparseBalError("page_table: [sequences][pages] is needed")
+        if free_pages.dim() != 1:
+            raise SparseBalError("free_pages: [pages] is needed")
+        self.device = device = _here()[0]
+        _tensor("page_table", page_table, page_table.shape, torch.int32, device)
+        _tensor("held", held, (page_table.shape[0],), torch.int32, device)
+        _tensor("free_pages", free_pages, free_pages.shape, torch.int32, device)
+        _tensor("free_count", free_count, (1,), torch.int32, device)
+        self.page_table, self.held, self.free_pages, self.free_count = page_table, held, free_pages, free_count
+        self.c = sb_page_pool(page_table.shape[0], page_table.shape[1], free_pages.shape[0], int(page_size), page_table.data_ptr(), held.data_ptr(), free_pages.data_ptr(),
+                              free_count.data_ptr())
+
+    @classmethod
+    def empty(cls, num_seqs, max_pages, num_pages, page_size):
+        """A pool none of whose pages is held yet."""
+        device = torch.device("cuda", _here()[0])
+        of = lambda *shape, value=0: torch.full(shape, value, dtype=torch.int32, device=device)
+        return cls(of(num_seqs, max_pages, value=-1), of(num_seqs), torch.arange(num_pages, dtype=torch.int32, device=device), of(1, value=num_pages), page_size)
+
+    def ref(self):
+        return C.byref(self.c)
+
+
+def sb_cache_tables(pool: PagePool, cached, added, total_new, cu_new=None, positions=None, slots=None, missing=None):
+    """Pages for cached[s] + added[s] tokens of every sequence (none where added[s] < 0), and where the added ones go.  Returns (cu_new, positions, slots, missing)."""
+    device, stream = _here()
+    if pool.device != device:
+        _elsewhere("pool", pool.device, device)
+    S = pool.c.num_seqs
+    _tensor("cached", cached, (S,), torch.int32, device)
+    _tensor("added", added, (S,), torch.int32, device)
+    if not 0 <= total_new < 2 ** 31:
+        raise SparseBalError(f"total_new: {total_new} does not fit 31 bits")
+    out = []
+    for name, x, shape, dt in (("cu_new", cu_new, (S + 1,), torch.int32), ("positions", positions, (total_new,), torch.int32), ("slots", slots, (total_new,), torch.int64),
+                               ("missing", missing, (1,), torch.int32)):
+        if x is None:
+            x = torch.empty(shape, dtype=dt, device=cached.device)
+        else:
+            _tensor(name, x, shape, dt, device)
+        out.append(x)
+    _call("sb_cache_tables", C.addressof(pool.c), cached.data_ptr(), added.data_ptr(), int(total_new), out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), out[3].data_ptr(),
+          stream)
+    return tuple(out)
+
+
+class Cache4:
+    """Holds sb_cache4 plus the tensors it points to: codes k, v [pages][KV heads][tokens of a page][head_dim/2] uint8, their steps [..][head_dim/32] bfloat16, page_table
+    [sequences][most pages of one] int32.  dtype: of the new tokens and queries."""
+
+    def __init__(self, k, v, k_step, v_step, page_table, dtype=torch.bfloat16):
+        if k.dim() != 4 or k.dtype is not torch.uint8:
+            raise SparseBalError("k: [pages][KV heads][tokens of a page][head_dim/2] in uint8 is needed")
+        if dtype not in _TORCH_DTYPE.values():
+            raise SparseBalError("dtype: bfloat16 or float32 is needed")
+        if page_table.dim() != 2:
+            raise SparseBalError("page_table: [sequences][pages] is needed")
+        self.device = device = _here()[0]
+        steps = (*k.shape[:3], k.shape[3] // 16)
+        _tensor("k", k, k.shape, torch.uint8, device)
+        _tensor("v", v, k.shape, torch.uint8, device)
+        _tensor("k_step", k_step, steps, torch.bfloat16, device)
+        _tensor("v_step", v_step, steps, torch.bfloat16, device)
+        _tensor("page_table", page_table, page_table.shape, torch.int32, device)
+        self.k, self.v, self.k_step, self.v_step, self.page_table, self.dtype = k, v, k_step, v_step, page_table, dtype
+        self.c = sb_cache4(k.shape[0], k.shape[2], k.shape[1], 2 * k.shape[3], SB_F32 if dtype == torch.float32 else SB_BF16, page_table.shape[1], k.data_ptr(), v.data_ptr(),
+                           k_step.data_ptr(), v_step.data_ptr(), page_table.data_ptr())
+
+    def ref(self):
+        return C.byref(self.c)
+
+
+def sb_cache4_append(cache: Cache4, chunk: Chunk, k, v, rope: Rope = None, axes: RopeAxes = None, positions=None, q=None, q_out=None, held=False, k_held=None, v_held=None):
+    """New tokens' k (turned) and v into their pages; returns q turned likewise (None without q), and with `held` (q, k, v), k and v as the cache holds them from now on."""
+    n, D, dt, (device, stream) = chunk.total_new, cache.c.head_dim, cache.dtype, _here()
+    _same_sequences(cache, chunk, device)
+    keys, queries = (n, cache.c.num_kv_heads, D), (n, chunk.Hq, D)
+    _tensor("k", k, keys, dt, device, pitch=True)
+    _tensor("v", v, keys, dt, device, pitch=True)
+    if q is not None:
+        _tensor("q", q, queries, dt, device, pitch=True)
+        if q_out is None:
+            q_out = torch.empty(queries, dtype=dt, device=q.device)
+        else:
+            _tensor("q_out", q_out, queries, dt, device)
+    elif q_out is not None:
+        raise SparseBalError("q_out without q")
+    if (axes is None) != (positions is None):
+        raise SparseBalError("axes without positions, or the other way round")
+    if axes is not None:
+        _tensor("positions", positions, (axes.c.num_axes, n), torch.int32, device)
+    if held and k_held is None:
+        k_held = torch.empty(keys, dtype=dt, device=k.device)
+    elif k_held is not None:
+        _tensor("k_held", k_held, keys, dt, device)
+    if held and v_held is None:
+        v_held = torch.empty(keys, dtype=dt, device=k.device)
+    elif v_held is not None:
+        _tensor("v_held", v_held, keys, dt, device)
+    _call("sb_cache4_append", C.addressof(cache.c), C.addressof(chunk.c), C.addressof(rope.c) if rope is not None else None, C.addressof(axes.c) if axes is not None else None,
+          _address(positions), _address(q), _pitch(q), k.data_ptr(), _pitch(k), v.data_ptr(), _pitch(v), _address(q_out), _address(k_held), _address(v_held), stream)
+    return (q_out, k_held, v_held) if held else q_out
+
+
+def sb_cache4_attn_ws_bytes(cache: Cache4, chunk: Chunk, window, sinks) -> int:
+    out, (window, sinks) = C.c_int64(), _window(window, sinks)
+    _check(lib().sb_cache4_attn_ws_bytes(cache.ref(), chunk.ref(), int(window), int(sinks), C.byref(out)))
+    return out.value
+
+
+def sb_cache4_attn(cache: Cache4, chunk: Chunk, q, window=2 ** 31 - 1, sinks=0, o=None, lse=None, ws=None):
+    """Attention of the new tokens over the cache, which holds them already.  Returns (o, lse)."""
+    dt, (device, stream) = cache.dtype, _here()
+    _same_sequences(cache, chunk, device)
+    queries, rows = (chunk.total_new, chunk.Hq, cache.c.head_dim), (chunk.Hq, chunk.total_new)
+    _tensor("q", q, queries, dt, device)
+    if o is None:
+        o = torch.empty_like(q)
+    else:
+        _tensor("o", o, queries, dt, device)
+    if lse is None:
+        lse = torch.empty(rows, dtype=torch.float32, device=q.device)
+    else:
+        _tensor("lse", lse, rows, torch.float32, device)
+    window, sinks = _window(window, sinks)
+    ws = _workspace(ws, sb_cache4_attn_ws_bytes(cache, chunk, window, sinks), device)
+    _call("sb_cache4_attn", C.addressof(cache.c), C.addressof(chunk.c), window, sinks, q.data_ptr(), o.data_ptr(), lse.data_ptr(), _address(ws), stream)
     return o, lse
 
 

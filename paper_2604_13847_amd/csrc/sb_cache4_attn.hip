@@ -1,0 +1,434 @@
+// Attention of new tokens over a paged cache in four bits (serving).
+//
+//   S_tu = scale sum_c step_uc (sum over d in group c of q_td n_ud),   O_td = sum_u (P_tu step_uc) m_ud   (c: d's group)
+//
+// n and m, the levels of keys and values, are exact as operands of matrix instructions; steps are applied in float32, to the scores of a group's product and to the probabilities.
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "sb_cache4.h"
+#include "sb_window.h"
+
+namespace sb {
+
+struct Cache4Params {
+  WindowParams w;  // (its cache is not read)
+  PagedCache4 cache;
+};
+
+typedef __amdgpu_buffer_rsrc_t Rsrc;
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+__device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+// byte SEL of x, two levels, as bfloat16: lower half first
+template <int SEL> __device__ inline bf16x2 levels(unsigned x) { return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, 1.0f, SEL); }
+__device__ inline bf16x8 levels8(unsigned x) {
+  const bf16x2 a = levels<0>(x), b = levels<1>(x), c = levels<2>(x), d = levels<3>(x);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+__device__ inline float step_at(unsigned pair, int i) { return __uint_as_float(i & 1 ? pair & 0xffff0000u : pair << 16); }
+
+// A strip: 32 keys, as a lane holds them.  Matrix instructions 16x16x32: lane = (l16, qd).
+//   scores S^T = K Q^T: A row = key 16 b + l16, slots of quarter qd = elements 32 c + 8 qd + (0 .. 7); C row 4 qd + v = key 16 b + 4 qd + v, column l16 = query
+//   output O^T += V^T P^T: slot j of quarter qd = key 16 (j / 4) + 4 qd + j % 4, which is where the scores are; A row = element 16 t + l16 of tile t
+template <int D>
+struct Strip {
+  static constexpr int GROUPS = D / 32;
+  unsigned k[2][GROUPS];          // [b][c]
+  unsigned v[8];                  // word l16 of slot j's key (head_dim 64: 16 bits)
+  unsigned ks[2][2 * GROUPS], vs[2][2 * GROUPS];  // steps of keys 16 b + 4 qd + (0 .. 3): pairs of bfloat16
+  __device__ inline float k_step(int b, int v, int c) const { return step_at(ks[b][(v * GROUPS + c) / 2], c); }
+  __device__ inline float v_step(int b, int v, int c) const { return step_at(vs[b][(v * GROUPS + c) / 2], c); }
+};
+
+__device__ inline Rsrc resource(const void* base, unsigned bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x20000); }
+template <int D>
+__device__ inline void load_steps(unsigned (&to)[2 * (D / 32)], Rsrc r, unsigned at) {
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) {
+    const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(r, at + 16 * i, 0, 0);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) to[4 * i + e] = x[e];
+  }
+}
+
+// An item is up to 16 NT flattened rows of a KV head and per_split strips; a wavefront takes every NW-th strip, straight into registers, the next one's loads on their way while one
+// is worked on.  PIECES: a query and a probability as that many bfloat16 numbers.
+constexpr int kWaves4 = 4;
+template <typename T, int D, int NT, int PIECES>
+__global__ __launch_bounds__(64 * kWaves4) void cache4_split_kernel(Cache4Params A) {
+  const WindowParams& P = A.w;
+  constexpr int NW = kWaves4, ROWS = 16 * NT, GROUPS = D / 32, TILES = D / 16;
+  constexpr int OUT_P = D + 4;
+  __shared__ float sums[NW][ROWS][OUT_P];
+  __shared__ float stats[2][NW][ROWS];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l16 = lane & 15, qd = lane >> 4;
+  const int z = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (unsigned)P.Hkv % (unsigned)P.splits));
+  const RowTile t = locate_tile<ROWS, true>(P, blockIdx.x / (unsigned)P.Hkv / (unsigned)P.splits);
+  if (t.s < 0) return;
+  const int g = __builtin_amdgcn_readfirstlane((int)(blockIdx.x % (unsigned)P.Hkv));
+  const int rows = t.n * P.G, m0 = t.tile * ROWS, mine = min(rows - m0, ROWS);
+  auto token = [&](int m) { return (int)((unsigned)min(m, rows - 1) / (unsigned)P.G); };
+  const int ta = __builtin_amdgcn_readfirstlane(t.pos0 + token(m0)), last = __builtin_amdgcn_readfirstlane(t.pos0 + token(m0 + ROWS - 1));
+  const int tb = min(last, A.cache.max_pages * A.cache.page_size - 1), end = tb + 1, lo = max(0, ta - P.window + 1);
+  const KeyTiles<32> strips(ta, tb, P.window, P.sinks);
+  const int begin = (int)min((int64_t)z * P.per_split, (int64_t)strips.count());
+  const int count = z < P.splits - 1 ? min(begin + P.per_split, strips.count()) : strips.count();
+  const int turns = (count - begin - wave + NW - 1) / NW;  // strips of this wavefront: begin + wave + NW x (may be none)
+  const int32_t* const table = A.cache.table + (int64_t)t.s * A.cache.max_pages;
+
+  // Of strip begin + wave + NW (x0 + lane): the page of its keys 0 .. 15 and 16 .. 31, and how many of each exist (0: none)
+  int where[2], there[2], x0 = 0;
+  auto look_up = [&](int from) __attribute__((always_inline)) {
+    x0 = from;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      where[b] = 0;
+      there[b] = 0;
+      if (from + lane < turns) {
+        const int u = 32 * strips.at(begin + wave + NW * (from + lane)) + 16 * b;
+        if (u < end && (u + 16 > lo || u < P.sinks)) {
+          const int page = table[u >> A.cache.page_shift];
+          if ((unsigned)page < (unsigned)A.cache.num_pages) {
+            there[b] = min(end - u, 16);
+            where[b] = page;
+          }
+        }
+      }
+    }
+  };
+  auto load = [&](Strip<D>& s, int x) __attribute__((always_inline)) {  // strip x of this wavefront; past its last, nothing is read
+    const int at = min(x - x0, 63);
+    const int u = __builtin_amdgcn_readfirstlane(32 * strips.at(min(begin + wave + NW * x, max(strips.count() - 1, 0))));
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const unsigned page = (unsigned)__builtin_amdgcn_readlane(where[b], at);
+      const bool any = x < turns && __builtin_amdgcn_readlane(there[b], at) > 0;
+      // (16 rows of a page, all of them in memory, whether or not they have been written)
+      const int64_t row = (((int64_t)page * A.cache.Hkv + g) << A.cache.page_shift) + ((u + 16 * b) & (A.cache.page_size - 1));
+      const unsigned code_b = any ? 16 * (D / 2) : 0, step_b = any ? 16 * GROUPS * 2 : 0;
+      const Rsrc rk = resource(A.cache.k + row * (D / 2), code_b), rv = resource(A.cache.v + row * (D / 2), code_b);
+      const Rsrc rks = resource(A.cache.k_step + row * GROUPS, step_b), rvs = resource(A.cache.v_step + row * GROUPS, step_b);
+      if constexpr (D == 128) {
+        const u32x4 y = __builtin_amdgcn_raw_buffer_load_b128(rk, l16 * (D / 2) + qd * (D / 8), 0, 0);
+#pragma unroll
+        for (int c = 0; c < GROUPS; ++c) s.k[b][c] = y[c];
+      } else {
+        const u32x2 y = __builtin_amdgcn_raw_buffer_load_b64(rk, l16 * (D / 2) + qd * (D / 8), 0, 0);
+#pragma unroll
+        for (int c = 0; c < GROUPS; ++c) s.k[b][c] = y[c];
+      }
+      load_steps<D>(s.ks[b], rks, qd * 4 * GROUPS * 2);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const unsigned at_v = (4 * qd + j) * (D / 2) + l16 * (D / 32);
+        if constexpr (D == 128) s.v[4 * b + j] = __builtin_amdgcn_raw_buffer_load_b32(rv, at_v, 0, 0);
+        else s.v[4 * b + j] = __builtin_amdgcn_raw_buffer_load_b16(rv, at_v, 0, 0);
+      }
+      load_steps<D>(s.vs[b], rvs, qd * 4 * GROUPS * 2);
+    }
+  };
+
+  // B operand of the scores: column = row l16 of tile nt
+  bf16x8 qf[NT][GROUPS][PIECES];
+  int pos[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int m = min(m0 + 16 * nt + l16, rows - 1), i = token(m), h = g * P.G + m - i * P.G;
+    pos[nt] = t.pos0 + i;
+    const T* const q = (const T*)P.q + ((int64_t)(t.row0 + i) * P.Hq + h) * D + 8 * qd;
+#pragma unroll
+    for (int c = 0; c < GROUPS; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float y = (float)q[32 * c + e];
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+          qf[nt][c][p][e] = (bf16)y;
+          y -= (float)qf[nt][c][p][e];
+        }
+      }
+  }
+  f32x4 acc[NT][TILES];
+  float top[NT], l[NT];  // largest score, in units of log 2, and this lane's share of the sum
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+    for (int d = 0; d < TILES; ++d) acc[nt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    top[nt] = -__builtin_inff();
+    l[nt] = 0.f;
+  }
+
+  auto work = [&](Strip<D>& s, int x) __attribute__((always_inline)) {
+    const int u0 = 32 * strips.at(begin + wave + NW * x);
+    const unsigned have = (1u << __builtin_amdgcn_readlane(there[0], x - x0)) - 1 | ((1u << __builtin_amdgcn_readlane(there[1], x - x0)) - 1) << 16;  // keys that exist
+    float sc[NT][2][4];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) sc[nt][b][v] = 0.f;
+#pragma unroll
+      for (int c = 0; c < GROUPS; ++c) {
+        const bf16x8 op = levels8(s.k[b][c]);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int p = PIECES - 1; p >= 0; --p) y = mfma16(op, qf[nt][c][p], y);
+#pragma unroll
+          for (int v = 0; v < 4; ++v) sc[nt][b][v] = __builtin_fmaf(y[v], s.k_step(b, v, c), sc[nt][b][v]);
+        }
+      }
+    }
+    const bool masked = u0 + 31 > ta || (last - u0 >= P.window && u0 + 31 >= P.sinks) || have != ~0u;
+    if (masked) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const int r = 16 * b + 4 * qd + v;
+            if (!sees(pos[nt], u0 + r, P.window, P.sinks) || !(have >> r & 1)) sc[nt][b][v] = -__builtin_inff();
+          }
+      // keys that do not exist have no steps either, whatever the page holds
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+          if (!(have >> (16 * b + 4 * qd + v) & 1)) {
+            if constexpr (GROUPS == 4) s.vs[b][2 * v] = s.vs[b][2 * v + 1] = 0;
+            else s.vs[b][v] = 0;
+          }
+    }
+    bf16x8 w[NT][GROUPS][PIECES];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float mx = -__builtin_inff();
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          sc[nt][b][v] *= P.scale_log2e;
+          mx = fmaxf(mx, sc[nt][b][v]);
+        }
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      mx = fmaxf(mx, top[nt]);
+      const float ref = mx == -__builtin_inff() ? 0.f : mx;  // nothing seen yet: keep the exponents finite
+      const float alpha = fast_exp2(top[nt] - ref);
+      top[nt] = mx;
+      l[nt] *= alpha;
+#pragma unroll
+      for (int d = 0; d < TILES; ++d)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) acc[nt][d][v] *= alpha;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float e = fast_exp2(sc[nt][b][v] - ref);
+          l[nt] += e;
+#pragma unroll
+          for (int c = 0; c < GROUPS; ++c) {
+            float y = e * s.v_step(b, v, c);
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) {
+              w[nt][c][p][4 * b + v] = (bf16)y;
+              y -= (float)w[nt][c][p][4 * b + v];
+            }
+          }
+        }
+    }
+    // levels of two keys side by side in a byte: even and odd tiles' (a word's nibble t is element 16 t + l16)
+    unsigned even[4], odd[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const unsigned a = s.v[2 * j], b = s.v[2 * j + 1];
+      even[j] = (a & 0x0f0f0f0fu) | (b << 4 & 0xf0f0f0f0u);
+      odd[j] = (a >> 4 & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u);
+    }
+    auto tile = [&](auto tc) __attribute__((always_inline)) {
+      constexpr int TT = decltype(tc)::value;
+      bf16x8 op;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bf16x2 y = levels<TT / 2>(TT & 1 ? odd[j] : even[j]);
+        op[2 * j] = y[0];
+        op[2 * j + 1] = y[1];
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int p = PIECES - 1; p >= 0; --p) acc[nt][TT] = mfma16(op, w[nt][TT / 2][p], acc[nt][TT]);
+    };
+    tile(std::integral_constant<int, 0>()); tile(std::integral_constant<int, 1>()); tile(std::integral_constant<int, 2>()); tile(std::integral_constant<int, 3>());
+    if constexpr (D == 128) {
+      tile(std::integral_constant<int, 4>()); tile(std::integral_constant<int, 5>()); tile(std::integral_constant<int, 6>()); tile(std::integral_constant<int, 7>());
+    }
+  };
+
+  if (turns > 0) {
+    Strip<D> s[2];
+    look_up(0);
+    load(s[0], 0);
+    for (int x = 0; x < turns; x += 2) {  // (64 strips a look-up: an even number)
+      load(s[1], x + 1);
+      work(s[0], x);
+      if (x + 1 >= turns) break;
+      if (x + 2 - x0 == 64 && x + 2 < turns) {  // the look-up takes the place of this strip's own
+        work(s[1], x + 1);
+        look_up(x + 2);
+        load(s[0], x + 2);
+      } else {
+        load(s[0], x + 2);
+        work(s[1], x + 1);
+      }
+    }
+  }
+  // the wavefronts' sums, through LDS
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    l[nt] += __shfl_xor(l[nt], 16, 64);
+    l[nt] += __shfl_xor(l[nt], 32, 64);
+#pragma unroll
+    for (int d = 0; d < TILES; ++d) *(f32x4*)&sums[wave][16 * nt + l16][16 * d + 4 * qd] = acc[nt][d];
+    if (qd == 0) { stats[0][wave][16 * nt + l16] = top[nt]; stats[1][wave][16 * nt + l16] = l[nt]; }
+  }
+  __syncthreads();
+  constexpr int LANES = D / 4;
+  const int c = threadIdx.x % LANES;
+  for (int r = threadIdx.x / LANES; r < mine; r += 64 * NW / LANES) {
+    float best = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) best = fmaxf(best, stats[0][w][r]);
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      if (stats[1][w][r] == 0.f) continue;
+      const float f = fast_exp2(stats[0][w][r] - best);
+      sum += f * stats[1][w][r];
+      x += f * *(const f32x4*)&sums[w][r][4 * c];
+    }
+    const int j = token(m0 + r), hh = g * P.G + m0 + r - j * P.G;
+    const int64_t row = (int64_t)(t.row0 + j) * P.Hq + hh;
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum, lse2 = sum == 0.f ? -__builtin_inff() : best + __builtin_log2f(sum);  // (a sum that is no number is passed on)
+    x *= inv;
+    if (P.splits > 1) {
+      const int64_t at = ((int64_t)z * P.part_rows + (P.part_seq_rows > 0 ? t.s * P.part_seq_rows : t.row0) + j) * P.Hq + hh;
+      if (c == 0) P.part_lse[at] = lse2;
+      if (sum != 0.f) *(f32x4*)(P.part_o + at * D + 4 * c) = x;
+    } else {
+      T* const to = (T*)P.o + row * D + 4 * c;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) to[e] = (T)x[e];
+      if (c == 0) P.lse[(int64_t)hh * P.T + t.row0 + j] = lse2 * 0.69314718055994531f;
+    }
+  }
+}
+
+// How the work is cut: tiles of rows, and the keys in runs of strips.
+struct Cache4Plan {
+  int64_t items;
+  int nt, splits, per_split, part_rows, part_seq_rows;
+  size_t part_o, bytes;
+};
+static Cache4Plan plan_cache4(const sb_cache4* c, const sb_chunk* n, int window, int sinks) {
+  Cache4Plan p{};
+  const int G = n->num_q_heads / c->num_kv_heads, S = n->num_seqs;
+  const int64_t most = (int64_t)std::min(n->max_new, n->total_new) * G;  // rows of a sequence
+  p.nt = c->dtype == SB_F32 || most <= 16 ? 1 : 2;
+  const int rows = 16 * p.nt;
+  p.items = std::min(row_tiles_most(n->total_new, S, G, rows), (most + rows - 1) / rows * S);
+  const int64_t in_window = (int64_t)window + (rows + G - 1) / G + sinks + 64;
+  const int64_t longest = std::min<int64_t>(n->max_length, (int64_t)c->max_pages * c->page_size);
+  const int64_t keys = std::min(in_window, longest), strips = (keys + 31) / 32;
+  // Two workgroups a CU; a strip for each wavefront at least, and where items are few 2048 keys at most, so that sequences of unequal lengths even out.
+  const int64_t workgroups = p.items * c->num_kv_heads;
+  int64_t per = (strips * workgroups + 511) / 512;
+  per = std::max<int64_t>((per + kWaves4 - 1) / kWaves4 * kWaves4, kWaves4);
+  if (workgroups < 2048) per = std::min<int64_t>(per, 64);
+  p.splits = (int)std::max<int64_t>((strips + per - 1) / per, 1);
+  p.per_split = (int)per;
+  p.part_rows = n->total_new;
+  const int seq_rows = std::min(n->max_new, n->total_new);
+  if ((int64_t)seq_rows * S < n->total_new) {
+    p.part_seq_rows = seq_rows;
+    p.part_rows = seq_rows * S;
+  }
+  const size_t sums = p.splits > 1 ? (size_t)p.splits * p.part_rows * n->num_q_heads : 0;
+  p.part_o = align_up(sums * sizeof(float));
+  p.bytes = align_up(p.part_o + sums * c->head_dim * sizeof(float));
+  return p;
+}
+static int check_cache4_attn(const sb_cache4* c, const sb_chunk* n, int32_t window, int32_t sinks) {
+  const int rc = check_cache4(c, n);
+  if (rc != SB_OK) return rc;
+  if (window < 1 || sinks < 0) { set_error("window (%d) must be at least 1 and sinks (%d) not negative", window, sinks); return SB_ERR_INVALID_ARG; }
+  return check_rows(n->total_new, n->num_q_heads / c->num_kv_heads);
+}
+
+}  // namespace sb
+
+using namespace sb;
+
+extern "C" {
+
+int sb_cache4_attn_ws_bytes(const sb_cache4* c, const sb_chunk* n, int32_t window, int32_t sinks, int64_t* bytes) {
+  if (!bytes) { set_error("null output"); return SB_ERR_INVALID_ARG; }
+  const int rc = check_cache4_attn(c, n, window, sinks);
+  if (rc != SB_OK) return rc;
+  *bytes = n->num_seqs == 0 || n->max_new == 0 ? 0 : (int64_t)plan_cache4(c, n, window, sinks).bytes;
+  return SB_OK;
+}
+
+int sb_cache4_attn(const sb_cache4* c, const sb_chunk* n, int32_t window, int32_t sinks, const void* q, void* o, float* lse, void* ws, void* stream) {
+  int rc = check_cache4_attn(c, n, window, sinks);
+  if (rc != SB_OK) return rc;
+  if (n->total_new == 0 || n->num_seqs == 0 || n->max_new == 0) return SB_OK;
+  if (!q || !o || !lse) { set_error("null argument"); return SB_ERR_INVALID_ARG; }
+  if ((rc = check_cache4_arrays(c, n)) != SB_OK) return rc;
+  const void* const buffers[] = {q, o, c->k, c->v, c->k_step, c->v_step, ws};
+  if ((rc = check_aligned(buffers, 7)) != SB_OK) return rc;
+  Cache4Params A{};
+  WindowParams& P = A.w;
+  P.q = q; P.o = o; P.lse = lse; P.cu = n->cu_new; P.cached = n->cached; P.max_new = n->max_new;
+  P.T = n->total_new; P.S = n->num_seqs; P.Hq = n->num_q_heads; P.Hkv = c->num_kv_heads; P.G = P.Hq / P.Hkv;
+  P.window = window; P.sinks = sinks;
+  P.scale = n->softmax_scale > 0.f ? n->softmax_scale : 1.0f / sqrtf((float)c->head_dim);
+  P.scale_log2e = P.scale * 1.4426950408889634f;
+  A.cache = make_paged(c);
+  const Cache4Plan plan = plan_cache4(c, n, window, sinks);
+  if (plan.splits > 1) {
+    if (!ws) { set_error("null argument"); return SB_ERR_INVALID_ARG; }
+    P.part_lse = (float*)ws;
+    P.part_o = (float*)((char*)ws + plan.part_o);
+  }
+  P.splits = plan.splits; P.per_split = plan.per_split; P.part_rows = plan.part_rows; P.part_seq_rows = plan.part_seq_rows;
+  P.rows_from = 0; P.rows_to = 0x7fffffff;
+  dim3 grid, rows;
+  const int seq_rows = std::min(P.max_new, P.T);
+  if ((rc = grid_of(plan.items * P.Hkv * plan.splits, 64 * kWaves4, &grid)) != SB_OK ||
+      (plan.splits > 1 && (rc = grid_of((plan.part_seq_rows > 0 ? (int64_t)seq_rows * P.S : P.T) * P.Hq, 256, &rows)) != SB_OK))
+    return rc;
+  const hipStream_t st = (hipStream_t)stream;
+  KernelTimer kt(K_CACHE_ATTN, st);
+  auto launch = [&](auto ty, auto d, auto nt, auto pieces) {
+    hipLaunchKernelGGL((cache4_split_kernel<decltype(ty), decltype(d)::value, decltype(nt)::value, decltype(pieces)::value>), grid, dim3(64 * kWaves4), 0, st, A);
+  };
+  auto with_d = [&](auto ty, auto nt, auto pieces) {
+    if (c->head_dim == 128) launch(ty, std::integral_constant<int, 128>(), nt, pieces); else launch(ty, std::integral_constant<int, 64>(), nt, pieces);
+  };
+  if (c->dtype == SB_F32) with_d(float(), std::integral_constant<int, 1>(), std::integral_constant<int, 3>());
+  else if (plan.nt == 1) with_d(bf16(), std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
+  else with_d(bf16(), std::integral_constant<int, 2>(), std::integral_constant<int, 1>());
+  SB_LAUNCH_CHECK("cache4_split_kernel");
+  if (plan.splits > 1) return launch_cache_merge(P, c->head_dim, c->dtype, rows, plan.part_seq_rows > 0 ? seq_rows : 0, st);
+  return SB_OK;
+}
+
+}  // extern "C"

@@ -324,6 +324,14 @@ __global__ __launch_bounds__(256) void cache_merge_kernel(WindowParams P, int se
   if (lane == 0) P.lse[(int64_t)h * P.T + tok] = sum == 0.f ? -__builtin_inff() : (best + __builtin_log2f(sum)) * 0.69314718055994531f;
 }
 
+int launch_cache_merge(const WindowParams& P, int D, int dtype, dim3 workgroups, int seq_rows, hipStream_t st) {
+  auto launch = [&](auto t, auto d) { hipLaunchKernelGGL((cache_merge_kernel<decltype(t), decltype(d)::value>), workgroups, dim3(256), 0, st, P, seq_rows); };
+  auto with_d = [&](auto t) { if (D == 128) launch(t, std::integral_constant<int, 128>()); else launch(t, std::integral_constant<int, 64>()); };
+  if (dtype == SB_F32) with_d(float()); else with_d(bf16());
+  SB_LAUNCH_CHECK("cache_merge_kernel");
+  return SB_OK;
+}
+
 // How the work is cut.  Sequences of up to kFewRows flattened rows are cache_split_kernel's (bfloat16), the others the packed batches' kernel's; a batch of one kind costs one launch.
 constexpr int kFewRows = 2 * kSplitRows;
 static int few_seq_rows(int G, int max_new) { return std::min(kFewRows / G, max_new); }  // tokens of such a sequence, at most
@@ -421,13 +429,7 @@ int sb_cache_attn(const sb_cache* c, const sb_chunk* n, int32_t window, int32_t 
       (plan.few.splits > 1 && (rc = grid_of(seq_rows * P.S * P.Hq, 256, &few_rows)) != SB_OK))
     return rc;
   KernelTimer kt(K_CACHE_ATTN, st);
-  auto merge = [&](dim3 workgroups, int seq_rows) {
-    auto launch = [&](auto t, auto d) { hipLaunchKernelGGL((cache_merge_kernel<decltype(t), decltype(d)::value>), workgroups, dim3(256), 0, st, P, seq_rows); };
-    auto with_d = [&](auto t) { if (c->head_dim == 128) launch(t, std::integral_constant<int, 128>()); else launch(t, std::integral_constant<int, 64>()); };
-    if (f32) with_d(float()); else with_d(bf16());
-    SB_LAUNCH_CHECK("cache_merge_kernel");
-    return (int)SB_OK;
-  };
+  auto merge = [&](dim3 workgroups, int seq_rows) { return launch_cache_merge(P, c->head_dim, c->dtype, workgroups, seq_rows, st); };
   if (plan.many.items > 0) {
     P.splits = plan.many.splits;
     P.per_split = plan.many.per_split;

@@ -1,4 +1,4 @@
-// Rotary positions of packed batches, and the append of new tokens to a paged cache, which is the same kernel with another destination.
+// Rotary positions of packed batches (one position a token, or one of every axis), and the append of new tokens to a paged cache, which is the same kernel with another destination.
 //
 // Pair (x, y) of a head becomes A (x cos a - y sin a, y cos a + x sin a), a = 2 pi pos turns_i.  The product is taken in float64 and reduced to
 // half a revolution either way before it is rounded, so an angle is off by 2^-24 of that at any position; products and sums are in
@@ -11,8 +11,9 @@
 // last-level cache).
 #include <math.h>
 
-#include "sb_cache.h"
-#include "sb_internal.h"
+#include <type_traits>
+
+#include "sb_rope.h"
 
 namespace sb {
 
@@ -28,14 +29,16 @@ struct RopeParams {
   const int32_t* cached;
   int max_new;
   int run;                                // tokens a wavefront takes
+  const int32_t* axis_positions;          // [axes][T]: with AXES
+  uint8_t axis[SB_ROPE_MAX_PAIRS];
   double turns[SB_ROPE_MAX_PAIRS];
 };
 
 template <typename T, int N> struct alignas(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Vec { T x[N]; };
 
 // PAGED: k and v go to the cache's pages.  VEC 8: rot is a multiple of 16 and everything is 16-byte aligned, so a unit is two 16-byte pieces
-// (float: 32 bytes); else single pairs.
-template <typename T, int D, int VEC, bool HALF, bool PAGED>
+// (float: 32 bytes); else single pairs.  AXES: every pair's position is that of its axis; each lane loads its own.
+template <typename T, int D, int VEC, bool HALF, bool PAGED, bool AXES>
 __global__ __launch_bounds__(256) void rope_kernel(RopeParams P) {
   constexpr int UNITS = D / 2 / VEC;          // of a head
   constexpr int PER = 64 / (UNITS < 64 ? UNITS : 64);  // heads a wavefront handles at a time
@@ -51,10 +54,11 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeParams P) {
   const int64_t tok0 = ((int64_t)blockIdx.x * 4 + wave) * P.run;
   float2* const cs = table[wave];
   const double turns = lane < P.rot / 2 ? P.turns[lane] : 0.0;
+  const int32_t* const axis_positions = AXES ? P.axis_positions + (lane < P.rot / 2 ? (int64_t)P.axis[lane] * P.T : 0) : nullptr;
   int s = 0, first = 0, behind = -1;  // the token's sequence, its first row and the one behind its last
   for (int64_t tok = tok0; tok < min(tok0 + P.run, (int64_t)P.T); ++tok) {
-    int64_t pos;
-    if (PAGED || !P.positions) {
+    int64_t pos = 0;
+    if (PAGED || (!AXES && !P.positions)) {
       if (tok >= behind) {
         s = sequence_of(P.cu, P.S, (int)tok, lane);
         if (s >= P.S) break;  // behind the last sequence
@@ -66,11 +70,11 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeParams P) {
         if (pos < 0 || pos >= P.max_new) continue;
         pos += max(P.cached[s], 0);
       }
-    } else {
+    } else if (!AXES) {
       pos = P.positions[tok];
     }
     {
-      double t = (double)pos * turns;
+      double t = (double)(AXES ? axis_positions[tok] : pos) * turns;
       t -= rint(t);
       float sn, cn;
       sincospif(2.0f * (float)t, &sn, &cn);
@@ -137,7 +141,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeParams P) {
   }
 }
 
-static int check_rope(const sb_rope* r, int head_dim) {
+int check_rope(const sb_rope* r, int head_dim) {
   if (r->rot_dim < 2 || r->rot_dim % 2 != 0 || r->rot_dim > head_dim) {
     set_error("rot_dim %d must be even and in 2 .. head_dim (%d)", r->rot_dim, head_dim);
     return SB_ERR_INVALID_ARG;
@@ -146,18 +150,27 @@ static int check_rope(const sb_rope* r, int head_dim) {
   return SB_OK;
 }
 
-static int check_pitch(const char* what, int64_t* pitch, int64_t contiguous) {
+int check_axes(const sb_rope* r, const sb_rope_axes* a, const int32_t* positions) {
+  if (!r || !a || !positions) { set_error("a rope, its axes and their positions are required"); return SB_ERR_INVALID_ARG; }
+  if (a->num_axes < 1 || a->num_axes > SB_ROPE_MAX_AXES) { set_error("num_axes %d must be in 1 .. %d", a->num_axes, SB_ROPE_MAX_AXES); return SB_ERR_INVALID_ARG; }
+  for (int i = 0; i < r->rot_dim / 2; ++i)
+    if (a->axis[i] >= a->num_axes) { set_error("pair %d is of axis %d: there are %d", i, a->axis[i], a->num_axes); return SB_ERR_INVALID_ARG; }
+  return SB_OK;
+}
+
+int check_pitch(const char* what, int64_t* pitch, int64_t contiguous) {
   if (*pitch == 0) *pitch = contiguous;
   if (*pitch < contiguous) { set_error("%s_pitch %lld is less than a token's %lld elements", what, (long long)*pitch, (long long)contiguous); return SB_ERR_INVALID_ARG; }
   return SB_OK;
 }
 
-static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-
 template <typename T, int D, int VEC, bool PAGED>
 static void launch_layout(const RopeParams& P, bool half, dim3 grid, hipStream_t st) {
-  if (half) hipLaunchKernelGGL((rope_kernel<T, D, VEC, true, PAGED>), grid, dim3(256), 0, st, P);
-  else hipLaunchKernelGGL((rope_kernel<T, D, VEC, false, PAGED>), grid, dim3(256), 0, st, P);
+  auto launch = [&](auto h, auto axes) {
+    hipLaunchKernelGGL((rope_kernel<T, D, VEC, decltype(h)::value, PAGED, decltype(axes)::value>), grid, dim3(256), 0, st, P);
+  };
+  auto with_axes = [&](auto h) { if (P.axis_positions) launch(h, std::true_type()); else launch(h, std::false_type()); };
+  if (half) with_axes(std::true_type()); else with_axes(std::false_type());
 }
 template <typename T, bool PAGED>
 static void launch_rope(const RopeParams& P, int D, bool half, bool wide, dim3 grid, hipStream_t st) {
@@ -190,6 +203,10 @@ static void set_rope(RopeParams* P, const sb_rope* r) {
   P->rot = r->rot_dim;
   P->amplitude = r->amplitude;
   for (int i = 0; i < r->rot_dim / 2; ++i) P->turns[i] = r->turns[i];
+}
+static void set_axes(RopeParams* P, const sb_rope* r, const sb_rope_axes* a, const int32_t* positions) {
+  P->axis_positions = positions;
+  for (int i = 0; i < r->rot_dim / 2; ++i) P->axis[i] = a->axis[i];
 }
 
 }  // namespace sb
@@ -242,13 +259,13 @@ int sb_rope_init(sb_rope* out, int32_t rot_dim, int32_t layout, double base, int
   return SB_OK;
 }
 
-int sb_rope_apply(const sb_problem* p, const sb_rope* r, const int32_t* positions, const void* q, int64_t q_pitch, const void* k, int64_t k_pitch,
-                  void* q_out, void* k_out, int direction, void* stream) {
+static int rope_apply(const sb_problem* p, const sb_rope* r, const sb_rope_axes* axes, bool with_axes, const int32_t* positions, const void* q, int64_t q_pitch, const void* k,
+                      int64_t k_pitch, void* q_out, void* k_out, int direction, void* stream) {
   Geo g;
   int rc = make_batch(p, &g);
   if (rc != SB_OK) return rc;
   if (!r) { set_error("null rope"); return SB_ERR_INVALID_ARG; }
-  if ((rc = check_rope(r, g.D)) != SB_OK) return rc;
+  if ((rc = check_rope(r, g.D)) != SB_OK || (with_axes && (rc = check_axes(r, axes, positions)) != SB_OK)) return rc;
   if (direction != SB_ROPE_FORWARD && direction != SB_ROPE_BACKWARD) { set_error("bad direction %d", direction); return SB_ERR_INVALID_ARG; }
   if ((rc = check_pitch("q", &q_pitch, (int64_t)g.Hq * g.D)) != SB_OK || (rc = check_pitch("k", &k_pitch, (int64_t)g.Hkv * g.D)) != SB_OK) return rc;
   if (!q != !q_out || !k != !k_out) { set_error("an input without its output, or the other way round"); return SB_ERR_INVALID_ARG; }
@@ -264,15 +281,66 @@ int sb_rope_apply(const sb_problem* p, const sb_rope* r, const int32_t* position
   P.T = g.T; P.S = g.S; P.Hq = g.Hq; P.Hkv = g.Hkv; P.heads = (q ? g.Hq : 0) + (k ? g.Hkv : 0);
   P.sign = direction == SB_ROPE_FORWARD ? 1.0f : -1.0f;
   set_rope(&P, r);
+  if (with_axes) set_axes(&P, r, axes, positions);
   return enqueue_rope(P, g.D, g.dtype, r->layout == SB_ROPE_HALF, false, (hipStream_t)stream);
 }
 
-int sb_cache_append(const sb_cache* c, const sb_chunk* n, const sb_rope* r, const void* q, int64_t q_pitch, const void* k, int64_t k_pitch,
-                    const void* v, int64_t v_pitch, void* q_out, void* stream) {
+int sb_rope_apply(const sb_problem* p, const sb_rope* r, const int32_t* positions, const void* q, int64_t q_pitch, const void* k, int64_t k_pitch,
+                  void* q_out, void* k_out, int direction, void* stream) {
+  return rope_apply(p, r, nullptr, false, positions, q, q_pitch, k, k_pitch, q_out, k_out, direction, stream);
+}
+
+int sb_rope_axes_init(sb_rope_axes* out, int32_t num_axes, const int32_t* pairs, int32_t order) {
+  if (!out || !pairs) { set_error("null argument"); return SB_ERR_INVALID_ARG; }
+  if (num_axes < 1 || num_axes > SB_ROPE_MAX_AXES) { set_error("num_axes %d must be in 1 .. %d", num_axes, SB_ROPE_MAX_AXES); return SB_ERR_INVALID_ARG; }
+  if (order != SB_AXES_SECTIONS && order != SB_AXES_IN_TURN) { set_error("bad order of axes %d", order); return SB_ERR_INVALID_ARG; }
+  int left[SB_ROPE_MAX_AXES], total = 0;
+  for (int a = 0; a < num_axes; ++a) {
+    if (pairs[a] < 0 || pairs[a] > SB_ROPE_MAX_PAIRS - total) { set_error("pairs of axes must be 0 .. %d in all", SB_ROPE_MAX_PAIRS); return SB_ERR_INVALID_ARG; }
+    total += left[a] = pairs[a];
+  }
+  if (total == 0) { set_error("no axis has any pair"); return SB_ERR_INVALID_ARG; }
+  sb_rope_axes x{};
+  x.num_axes = num_axes;
+  for (int i = 0; i < total;)
+    for (int a = 0; a < num_axes; ++a)
+      for (int n = order == SB_AXES_SECTIONS ? left[a] : left[a] > 0 ? 1 : 0; n > 0; --n, --left[a]) x.axis[i++] = (uint8_t)a;
+  for (int i = total; i < SB_ROPE_MAX_PAIRS; ++i) x.axis[i] = (uint8_t)num_axes;  // (so that a rope of more pairs than the axes have is refused)
+  *out = x;
+  return SB_OK;
+}
+
+int sb_rope_join(sb_rope* out, const sb_rope* ropes, int32_t num_ropes) {
+  if (!out || !ropes) { set_error("null rope"); return SB_ERR_INVALID_ARG; }
+  if (num_ropes < 1) { set_error("at least one rope is needed"); return SB_ERR_INVALID_ARG; }
+  sb_rope r = ropes[0];
+  r.rot_dim = 0;
+  int at = 0;
+  for (int a = 0; a < num_ropes; ++a) {
+    const int rc = check_rope(&ropes[a], 2 * SB_ROPE_MAX_PAIRS);
+    if (rc != SB_OK) return rc;
+    if (ropes[a].layout != r.layout || ropes[a].amplitude != r.amplitude) { set_error("joined ropes need one layout and one amplitude"); return SB_ERR_INVALID_ARG; }
+    const int n = ropes[a].rot_dim / 2;
+    if (n > SB_ROPE_MAX_PAIRS - at) { set_error("joined ropes have more than %d pairs", SB_ROPE_MAX_PAIRS); return SB_ERR_INVALID_ARG; }
+    for (int i = 0; i < n; ++i) r.turns[at++] = ropes[a].turns[i];
+  }
+  for (int i = at; i < SB_ROPE_MAX_PAIRS; ++i) r.turns[i] = 0.0;
+  r.rot_dim = 2 * at;
+  *out = r;
+  return SB_OK;
+}
+
+int sb_rope_axes_apply(const sb_problem* p, const sb_rope* r, const sb_rope_axes* axes, const int32_t* positions, const void* q, int64_t q_pitch, const void* k, int64_t k_pitch,
+                       void* q_out, void* k_out, int direction, void* stream) {
+  return rope_apply(p, r, axes, true, positions, q, q_pitch, k, k_pitch, q_out, k_out, direction, stream);
+}
+
+static int cache_append(const sb_cache* c, const sb_chunk* n, const sb_rope* r, const sb_rope_axes* axes, bool with_axes, const int32_t* positions, const void* q, int64_t q_pitch,
+                        const void* k, int64_t k_pitch, const void* v, int64_t v_pitch, void* q_out, void* stream) {
   int rc = check_cache(c, n);
   if (rc != SB_OK) return rc;
   const int D = c->head_dim, Hq = n->num_q_heads, Hkv = c->num_kv_heads;
-  if (r && (rc = check_rope(r, D)) != SB_OK) return rc;
+  if ((r && (rc = check_rope(r, D)) != SB_OK) || (with_axes && (rc = check_axes(r, axes, positions)) != SB_OK)) return rc;
   if ((rc = check_pitch("q", &q_pitch, (int64_t)Hq * D)) != SB_OK || (rc = check_pitch("k", &k_pitch, (int64_t)Hkv * D)) != SB_OK ||
       (rc = check_pitch("v", &v_pitch, (int64_t)Hkv * D)) != SB_OK)
     return rc;
@@ -288,7 +356,18 @@ int sb_cache_append(const sb_cache* c, const sb_chunk* n, const sb_rope* r, cons
   P.sign = 1.0f;
   P.cache = make_paged(c);
   if (r) set_rope(&P, r);
+  if (with_axes) set_axes(&P, r, axes, positions);
   return enqueue_rope(P, D, c->dtype, !r || r->layout == SB_ROPE_HALF, true, (hipStream_t)stream);
+}
+
+int sb_cache_append(const sb_cache* c, const sb_chunk* n, const sb_rope* r, const void* q, int64_t q_pitch, const void* k, int64_t k_pitch,
+                    const void* v, int64_t v_pitch, void* q_out, void* stream) {
+  return cache_append(c, n, r, nullptr, false, nullptr, q, q_pitch, k, k_pitch, v, v_pitch, q_out, stream);
+}
+
+int sb_cache_append_axes(const sb_cache* c, const sb_chunk* n, const sb_rope* r, const sb_rope_axes* axes, const int32_t* positions, const void* q, int64_t q_pitch, const void* k,
+                         int64_t k_pitch, const void* v, int64_t v_pitch, void* q_out, void* stream) {
+  return cache_append(c, n, r, axes, true, positions, q, q_pitch, k, k_pitch, v, v_pitch, q_out, stream);
 }
 
 }  // extern "C"

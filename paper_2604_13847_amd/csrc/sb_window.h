@@ -236,5 +236,7 @@ int64_t row_tiles_most(int total, int S, int G, int rows);          // where the
 constexpr int kWaves = 4;  // of a forward or dQ workgroup (bfloat16)
 constexpr int forward_rows(int dtype) { return dtype == SB_F32 ? 32 : 32 * kWaves; }
 int launch_window_fwd(const WindowParams& P, int D, int dtype, bool paged, int64_t tiles, hipStream_t st);
+// Joins the runs of keys that a launch before left in part_o and part_lse: a workgroup to a row and head, of all rows, or of the first seq_rows of every sequence.
+int launch_cache_merge(const WindowParams& P, int D, int dtype, dim3 workgroups, int seq_rows, hipStream_t st);
 
 }  // namespace sb
