@@ -9,7 +9,7 @@
 #include <type_traits>
 
 #include "sb_cache4.h"
-#include "sb_window.h"
+#include "sb_window_fwd.h"
 
 namespace sb {
 
@@ -28,6 +28,8 @@ __device__ inline bf16x8 levels8(unsigned x) {
   const bf16x2 a = levels<0>(x), b = levels<1>(x), c = levels<2>(x), d = levels<3>(x);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+template <int SEL> __device__ inline f32x2 numbers(unsigned x) { return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, 1.0f, SEL); }
 __device__ inline float step_at(unsigned pair, int i) { return __uint_as_float(i & 1 ? pair & 0xffff0000u : pair << 16); }
 
 // A strip: 32 keys, as a lane holds them.  Matrix instructions 16x16x32: lane = (l16, qd).
@@ -331,36 +333,163 @@ __global__ __launch_bounds__(64 * kWaves4) void cache4_split_kernel(Cache4Params
   }
 }
 
-// How the work is cut: tiles of rows, and the keys in runs of strips.
+// ---------------------------------------------------------------------------------------------
+// Many rows (bfloat16): the forward of packed batches (window_fwd_rows) over tiles that are expanded on their way into LDS.  Every value held is a bfloat16 number, so nothing is rounded on
+// the way.  Eight wavefronts of 32 rows share a tile: its expansion, two vector instructions an element, is then a third of what the products and probabilities of the tile take.
+// Wavefronts 0 .. 3 expand 16 rows of K each, a lane a quarter of a row (eight elements of every group of 32); wavefronts 4 .. 7 those of V, a lane four words of a row.  Codes of the
+// tile after the next are on their way to registers while the next one is expanded and the present one multiplied.
+constexpr int kChunkWaves = 8;
+template <int D>
+struct ExpandedTiles {
+  static constexpr int GROUPS = D / 32, TILE_B = 64 * D * 2;
+  const unsigned char* codes;  // of page 0, this KV head
+  const bf16* steps;
+  unsigned code[GROUPS], step[GROUPS / 2];
+  unsigned at;   // where the lane's elements go in a tile
+  int row, part; // of the tile; of the row
+  bool value;
+  int page;      // of this wavefront's rows in the tile that is loaded next
+  __device__ inline void init(const Cache4Params& A, const RowTile& t, const KeySource<D, true>& src, int g, int wave, int lane, unsigned tiles0) {
+    value = wave >= 4;
+    codes = (value ? A.cache.v : A.cache.k) + ((int64_t)g << A.cache.page_shift) * (D / 2);
+    steps = (value ? A.cache.v_step : A.cache.k_step) + ((int64_t)g << A.cache.page_shift) * GROUPS;
+    row = 16 * (wave & 3) + (lane >> 2);
+    part = lane & 3;
+    at = tiles0 + (value ? TILE_B : 0) + row * (D * 2);
+  }
+  __device__ __attribute__((always_inline)) inline int first_row(const KeyTiles<64>& keys, int x) const { return 64 * keys.at(x) + __builtin_amdgcn_readfirstlane(row & ~15); }
+  // page of this wavefront's rows of tile x, or -1: there are none that a row sees
+  __device__ __attribute__((always_inline)) inline void look_up(const Cache4Params& A, const KeyTiles<64>& keys, const KeySource<D, true>& src, int x, int count) {
+    page = -1;
+    if (x >= count) return;
+    const int u = first_row(keys, x);
+    if (u < src.end && (u + 16 > src.lo || u < A.w.sinks)) page = src.page_of(A.w, u);
+  }
+  // codes of tile x (its page is known); rows that are not there are zeros
+  __device__ __attribute__((always_inline)) inline void load(const Cache4Params& A, const KeyTiles<64>& keys, const KeySource<D, true>& src, int x) {
+    const int u = first_row(keys, x);
+    const int64_t from = (((int64_t)(unsigned)max(page, 0) * A.cache.Hkv) << A.cache.page_shift) + (u & (A.cache.page_size - 1));
+    const unsigned rows = page < 0 ? 0u : (unsigned)min(max(src.end - u, 0), 16);
+    const Rsrc rc = resource(codes + from * (D / 2), rows * (D / 2)), rs = resource(steps + from * GROUPS, rows * GROUPS * 2);
+    const int r = row & 15;
+    if constexpr (D == 128) {
+      const u32x4 y = __builtin_amdgcn_raw_buffer_load_b128(rc, r * (D / 2) + part * (D / 8), 0, 0);
+      const u32x2 z = __builtin_amdgcn_raw_buffer_load_b64(rs, r * GROUPS * 2, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) code[e] = y[e];
+      step[0] = z[0]; step[1] = z[1];
+    } else {
+      const u32x2 y = __builtin_amdgcn_raw_buffer_load_b64(rc, r * (D / 2) + part * (D / 8), 0, 0);
+      code[0] = y[0]; code[1] = y[1];
+      step[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, r * GROUPS * 2, 0, 0);
+    }
+  }
+  __device__ __attribute__((always_inline)) inline void expand(int buffer) const {
+    const unsigned to = at + buffer * 2 * TILE_B;
+    const int swizzle = chunk_swizzle<D>(row);
+    if (!value) {  // word c: elements 32 c + 8 part + (0 .. 7)
+#pragma unroll
+      for (int c = 0; c < GROUPS; ++c) {
+        const float f = step_at(step[c / 2], c);
+        bf16x8 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const f32x2 z = e == 0 ? numbers<0>(code[c]) : e == 1 ? numbers<1>(code[c]) : e == 2 ? numbers<2>(code[c]) : numbers<3>(code[c]);
+          y[2 * e] = (bf16)(z[0] * f);
+          y[2 * e + 1] = (bf16)(z[1] * f);
+        }
+        *(bf16x8 __attribute__((address_space(3)))*)(uintptr_t)(to + 16 * ((4 * c + part) ^ swizzle)) = y;
+      }
+    } else {  // words i = 4 part + (0 .. 3) of D/8 bits: byte e of word i holds elements 32 e + i and 32 e + 16 + i
+#pragma unroll
+      for (int e = 0; e < GROUPS; ++e) {
+        const float f = step_at(step[e / 2], e);
+        bf16x4 lo, hi;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          f32x2 z;
+          if constexpr (D == 128) z = e == 0 ? numbers<0>(code[w]) : e == 1 ? numbers<1>(code[w]) : e == 2 ? numbers<2>(code[w]) : numbers<3>(code[w]);
+          else z = 2 * (w & 1) + e == 0 ? numbers<0>(code[w / 2]) : 2 * (w & 1) + e == 1 ? numbers<1>(code[w / 2]) : 2 * (w & 1) + e == 2 ? numbers<2>(code[w / 2]) : numbers<3>(code[w / 2]);
+          lo[w] = (bf16)(z[0] * f);
+          hi[w] = (bf16)(z[1] * f);
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int d = 32 * e + 16 * half;  // and 4 part
+          *(bf16x4 __attribute__((address_space(3)))*)(uintptr_t)(to + 16 * (((d >> 3) + (part >> 1)) ^ swizzle) + 8 * (part & 1)) = half ? hi : lo;
+        }
+      }
+    }
+  }
+  __device__ __attribute__((always_inline)) inline void start(const Cache4Params& A, const KeyTiles<64>& keys, const KeySource<D, true>& src, int begin, int count) {
+    if (begin >= count) return;
+    look_up(A, keys, src, begin, count);
+    load(A, keys, src, begin);
+    look_up(A, keys, src, begin + 1, count);
+    expand(0);
+    if (begin + 1 < count) load(A, keys, src, begin + 1);
+    look_up(A, keys, src, begin + 2, count);
+  }
+  __device__ __attribute__((always_inline)) inline void arrive(const Cache4Params& A, const KeyTiles<64>& keys, const KeySource<D, true>& src, int x, int begin, int count) {
+    __syncthreads();
+    if (x + 1 < count) expand((x + 1 - begin) & 1);
+    if (x + 2 < count) load(A, keys, src, x + 2);
+    look_up(A, keys, src, x + 3, count);
+  }
+};
+template <int D>
+__global__ __launch_bounds__(64 * kChunkWaves) __attribute__((amdgpu_waves_per_eu(2))) void cache4_chunk_kernel(Cache4Params A) {
+  __shared__ __attribute__((aligned(1024))) char tiles[2][2][64 * D * 2];  // [buffer][K, V]
+  window_fwd_rows<D, true, kChunkWaves, ExpandedTiles<D>>(A.w, &tiles[0][0][0], A);
+}
+
+// How the work is cut.  Sequences of up to kFewRows4 flattened rows are cache4_split_kernel's (float32: all of them), the others cache4_chunk_kernel's; a batch of one kind costs one launch.
+constexpr int kFewRows4 = 64;
+struct Cache4Launch {
+  int64_t items;  // tiles of rows; 0: no such launch
+  int splits, per_split, part_rows, part_seq_rows;
+};
 struct Cache4Plan {
-  int64_t items;
-  int nt, splits, per_split, part_rows, part_seq_rows;
+  Cache4Launch few, many;
+  int nt;
   size_t part_o, bytes;
 };
+static int few_seq_rows4(const sb_cache4* c, int G, int max_new) { return c->dtype == SB_F32 ? max_new : std::min(kFewRows4 / G, max_new); }  // tokens of a sequence of few rows, at most
 static Cache4Plan plan_cache4(const sb_cache4* c, const sb_chunk* n, int window, int sinks) {
   Cache4Plan p{};
   const int G = n->num_q_heads / c->num_kv_heads, S = n->num_seqs;
+  const bool f32 = c->dtype == SB_F32;
   const int64_t most = (int64_t)std::min(n->max_new, n->total_new) * G;  // rows of a sequence
-  p.nt = c->dtype == SB_F32 || most <= 16 ? 1 : 2;
-  const int rows = 16 * p.nt;
-  p.items = std::min(row_tiles_most(n->total_new, S, G, rows), (most + rows - 1) / rows * S);
-  const int64_t in_window = (int64_t)window + (rows + G - 1) / G + sinks + 64;
-  const int64_t longest = std::min<int64_t>(n->max_length, (int64_t)c->max_pages * c->page_size);
-  const int64_t keys = std::min(in_window, longest), strips = (keys + 31) / 32;
+  auto launch = [&](int64_t most_rows, int rows, int tile, int64_t wanted, int64_t least, int64_t largest) {
+    Cache4Launch l{};
+    l.items = std::min(row_tiles_most(n->total_new, S, G, rows), (most_rows + rows - 1) / rows * S);
+    const int64_t in_window = (int64_t)window + (rows + G - 1) / G + sinks + 2 * tile;
+    const int64_t longest = std::min<int64_t>(n->max_length, (int64_t)c->max_pages * c->page_size);
+    const int64_t keys = std::min(in_window, longest), tiles = (keys + tile - 1) / tile, workgroups = l.items * c->num_kv_heads;
+    int64_t per = (tiles * workgroups + wanted - 1) / wanted;
+    per = std::max((per + least - 1) / least * least, least);
+    if (workgroups < 2048) per = std::min(per, largest);
+    l.splits = (int)std::max<int64_t>((tiles + per - 1) / per, 1);
+    l.per_split = (int)per;
+    l.part_rows = n->total_new;
+    return l;
+  };
+  p.few.splits = p.many.splits = 1;
+  p.nt = f32 || most <= 16 ? 1 : 2;
   // Two workgroups a CU; a strip for each wavefront at least, and where items are few 2048 keys at most, so that sequences of unequal lengths even out.
-  const int64_t workgroups = p.items * c->num_kv_heads;
-  int64_t per = (strips * workgroups + 511) / 512;
-  per = std::max<int64_t>((per + kWaves4 - 1) / kWaves4 * kWaves4, kWaves4);
-  if (workgroups < 2048) per = std::min<int64_t>(per, 64);
-  p.splits = (int)std::max<int64_t>((strips + per - 1) / per, 1);
-  p.per_split = (int)per;
-  p.part_rows = n->total_new;
-  const int seq_rows = std::min(n->max_new, n->total_new);
+  if (f32) p.few = launch(most, 16, 32, 512, kWaves4, 64);
+  else if (G <= kFewRows4 && (S > 1 || most <= kFewRows4)) p.few = launch(std::min<int64_t>(most, kFewRows4), 16 * p.nt, 32, 512, kWaves4, 64);
+  // A workgroup a CU, of 8 tiles at least.
+  if (!f32 && most > kFewRows4) p.many = launch(most, 32 * kChunkWaves, 64, 256, 8, 1 << 30);
+  // Sums of few rows are laid out by sequence where that is less: a prompt in the batch has none.
+  const int seq_rows = few_seq_rows4(c, G, std::min(n->max_new, n->total_new));
   if ((int64_t)seq_rows * S < n->total_new) {
-    p.part_seq_rows = seq_rows;
-    p.part_rows = seq_rows * S;
+    p.few.part_seq_rows = seq_rows;
+    p.few.part_rows = seq_rows * S;
   }
-  const size_t sums = p.splits > 1 ? (size_t)p.splits * p.part_rows * n->num_q_heads : 0;
+  size_t sums = 0;
+  for (const Cache4Launch* l : {&p.few, &p.many})
+    if (l->splits > 1) sums = std::max(sums, (size_t)l->splits * l->part_rows * n->num_q_heads);
   p.part_o = align_up(sums * sizeof(float));
   p.bytes = align_up(p.part_o + sums * c->head_dim * sizeof(float));
   return p;
@@ -402,32 +531,48 @@ int sb_cache4_attn(const sb_cache4* c, const sb_chunk* n, int32_t window, int32_
   P.scale = n->softmax_scale > 0.f ? n->softmax_scale : 1.0f / sqrtf((float)c->head_dim);
   P.scale_log2e = P.scale * 1.4426950408889634f;
   A.cache = make_paged(c);
+  P.cache = PagedCache{nullptr, nullptr, c->page_table, c->num_pages, c->max_pages, c->page_size, A.cache.page_shift, c->num_kv_heads};
   const Cache4Plan plan = plan_cache4(c, n, window, sinks);
-  if (plan.splits > 1) {
+  if (plan.few.splits > 1 || plan.many.splits > 1) {
     if (!ws) { set_error("null argument"); return SB_ERR_INVALID_ARG; }
     P.part_lse = (float*)ws;
     P.part_o = (float*)((char*)ws + plan.part_o);
   }
-  P.splits = plan.splits; P.per_split = plan.per_split; P.part_rows = plan.part_rows; P.part_seq_rows = plan.part_seq_rows;
-  P.rows_from = 0; P.rows_to = 0x7fffffff;
-  dim3 grid, rows;
-  const int seq_rows = std::min(P.max_new, P.T);
-  if ((rc = grid_of(plan.items * P.Hkv * plan.splits, 64 * kWaves4, &grid)) != SB_OK ||
-      (plan.splits > 1 && (rc = grid_of((plan.part_seq_rows > 0 ? (int64_t)seq_rows * P.S : P.T) * P.Hq, 256, &rows)) != SB_OK))
+  const bool f32 = c->dtype == SB_F32;
+  const int seq_rows = few_seq_rows4(c, P.G, std::min(P.max_new, P.T));
+  dim3 few_grid, many_grid, few_rows, all_rows;
+  if ((rc = grid_of(plan.few.items * P.Hkv * plan.few.splits, 64 * kWaves4, &few_grid)) != SB_OK ||
+      (rc = grid_of(plan.many.items * P.Hkv * plan.many.splits, 64 * kChunkWaves, &many_grid)) != SB_OK ||
+      (plan.many.splits > 1 && (rc = grid_of((int64_t)P.T * P.Hq, 256, &all_rows)) != SB_OK) ||
+      (plan.few.splits > 1 && (rc = grid_of((plan.few.part_seq_rows > 0 ? (int64_t)seq_rows * P.S : P.T) * P.Hq, 256, &few_rows)) != SB_OK))
     return rc;
   const hipStream_t st = (hipStream_t)stream;
   KernelTimer kt(K_CACHE_ATTN, st);
-  auto launch = [&](auto ty, auto d, auto nt, auto pieces) {
-    hipLaunchKernelGGL((cache4_split_kernel<decltype(ty), decltype(d)::value, decltype(nt)::value, decltype(pieces)::value>), grid, dim3(64 * kWaves4), 0, st, A);
+  auto part = [&](const Cache4Launch& l, int from, int to) {
+    P.splits = l.splits; P.per_split = l.per_split; P.part_rows = l.part_rows; P.part_seq_rows = l.part_seq_rows;
+    P.rows_from = from; P.rows_to = to;
   };
-  auto with_d = [&](auto ty, auto nt, auto pieces) {
-    if (c->head_dim == 128) launch(ty, std::integral_constant<int, 128>(), nt, pieces); else launch(ty, std::integral_constant<int, 64>(), nt, pieces);
-  };
-  if (c->dtype == SB_F32) with_d(float(), std::integral_constant<int, 1>(), std::integral_constant<int, 3>());
-  else if (plan.nt == 1) with_d(bf16(), std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
-  else with_d(bf16(), std::integral_constant<int, 2>(), std::integral_constant<int, 1>());
-  SB_LAUNCH_CHECK("cache4_split_kernel");
-  if (plan.splits > 1) return launch_cache_merge(P, c->head_dim, c->dtype, rows, plan.part_seq_rows > 0 ? seq_rows : 0, st);
+  if (plan.many.items > 0) {
+    part(plan.many, plan.few.items > 0 ? kFewRows4 + 1 : 0, 0x7fffffff);
+    if (c->head_dim == 128) hipLaunchKernelGGL((cache4_chunk_kernel<128>), many_grid, dim3(64 * kChunkWaves), 0, st, A);
+    else hipLaunchKernelGGL((cache4_chunk_kernel<64>), many_grid, dim3(64 * kChunkWaves), 0, st, A);
+    SB_LAUNCH_CHECK("cache4_chunk_kernel");
+    if (P.splits > 1 && (rc = launch_cache_merge(P, c->head_dim, c->dtype, all_rows, 0, st)) != SB_OK) return rc;
+  }
+  if (plan.few.items > 0) {
+    part(plan.few, 0, f32 ? 0x7fffffff : kFewRows4);
+    auto launch = [&](auto ty, auto d, auto nt, auto pieces) {
+      hipLaunchKernelGGL((cache4_split_kernel<decltype(ty), decltype(d)::value, decltype(nt)::value, decltype(pieces)::value>), few_grid, dim3(64 * kWaves4), 0, st, A);
+    };
+    auto with_d = [&](auto ty, auto nt, auto pieces) {
+      if (c->head_dim == 128) launch(ty, std::integral_constant<int, 128>(), nt, pieces); else launch(ty, std::integral_constant<int, 64>(), nt, pieces);
+    };
+    if (f32) with_d(float(), std::integral_constant<int, 1>(), std::integral_constant<int, 3>());
+    else if (plan.nt == 1) with_d(bf16(), std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
+    else with_d(bf16(), std::integral_constant<int, 2>(), std::integral_constant<int, 1>());
+    SB_LAUNCH_CHECK("cache4_split_kernel");
+    if (P.splits > 1) return launch_cache_merge(P, c->head_dim, c->dtype, few_rows, P.part_seq_rows > 0 ? seq_rows : 0, st);
+  }
   return SB_OK;
 }
 

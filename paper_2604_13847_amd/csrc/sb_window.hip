@@ -9,7 +9,7 @@
 
 #include <type_traits>
 
-#include "sb_window.h"
+#include "sb_window_fwd.h"
 
 namespace sb {
 
@@ -17,15 +17,6 @@ namespace sb {
 // float32 arithmetic throughout: v_mfma_f32_32x32x2_f32, operands straight from memory.  A workgroup owns 32 rows (or 32 keys) and walks strips of 32 keys (rows), in
 // turn to its wavefronts; the wavefronts' sums are added in order at the end.  Operand layout per lane: A row / B column = lane%32, contraction slot = lane/32.
 __device__ inline f32x16 mfma_f32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
-
-__device__ inline f32x4 load4(const float* p) { return *(const f32x4*)p; }
-__device__ inline void store4(float* p, f32x4 x) { *(f32x4*)p = x; }
-__device__ inline void store4(bf16* p, f32x4 x) {
-  bf16x4 y;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] = (bf16)x[e];
-  *(bf16x4*)p = y;
-}
 
 // A row of D elements as an operand of a product over d: step x covers d = 8x .. 8x + 7, four instructions with slot hf at 8x + 4hf + j.
 template <int D> struct RowOperand { f32x4 x[D / 8]; };
@@ -80,15 +71,6 @@ __device__ inline void add_rows(f32x16 (&acc)[D / 32], const float (&w)[16], con
       for (int dt = 0; dt < D / 32; ++dt) acc[dt] = mfma_f32(there[v] ? (float)x[v][dt] : 0.f, w[v0 + v], acc[dt]);
   }
 }
-template <int D, typename T>
-__device__ inline void store_column(T* to, const f32x16 (&acc)[D / 32], float f, int hf) {
-#pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-    for (int vg = 0; vg < 4; ++vg)
-      store4(to + 32 * dt + 8 * vg + 4 * hf, f32x4{acc[dt][4 * vg] * f, acc[dt][4 * vg + 1] * f, acc[dt][4 * vg + 2] * f, acc[dt][4 * vg + 3] * f});
-}
-
 // Keys that no row of the wavefront sees (behind the last row, between the sinks and the window) are not read: their weights are zero, but what they hold
 // may be no number.
 template <typename T, int D, bool PAGED>
@@ -107,9 +89,6 @@ struct Keys {
   __device__ inline const T* k(int u) const { const int64_t o = offset(u); return o < 0 ? nullptr : (const T*)(PAGED ? P.cache.k : P.k) + o; }
   __device__ inline const T* v(int u) const { const int64_t o = offset(u); return o < 0 ? nullptr : (const T*)(PAGED ? P.cache.v : P.v) + o; }
 };
-
-// LSE of a row without any score above -infinity.  Over a cache it may see no key; in a packed batch it sees itself, and has no softmax: NaN, as in the block-sparse forward.
-template <bool PAGED> __device__ inline float empty_lse() { return PAGED ? -__builtin_inff() : __builtin_nanf(""); }
 
 // The other wavefronts' registers for the first one
 template <int N, int W>
@@ -410,180 +389,8 @@ __global__ __launch_bounds__(256) void window_dkv_f32_join_kernel(WindowParams P
 // tokens in short ones 26 -> 20 us with four.
 template <int D, bool PAGED>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void window_fwd_kernel(WindowParams P) {
-  constexpr int ROWS = 32 * kWaves, ROW_B = D * 2, TILE_B = 64 * ROW_B, NOP = D / 16;
-  constexpr float kLazy = 8.0f;
-  __shared__ __attribute__((aligned(1024))) char tiles[2][2][TILE_B];  // [buffer][K, V]
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
-  const int splits = PAGED ? P.splits : 1, z = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (unsigned)P.Hkv % (unsigned)splits));
-  const RowTile t = locate_tile<ROWS, PAGED>(P, blockIdx.x / (unsigned)P.Hkv / (unsigned)splits);
-  if (t.s < 0) return;
-  const int g = __builtin_amdgcn_readfirstlane((int)(blockIdx.x % (unsigned)P.Hkv));
-  const int rows = t.n * P.G, mb = t.tile * ROWS, mw = mb + 32 * wave;
-  auto token = [&](int m) { return (int)((unsigned)min(m, rows - 1) / (unsigned)P.G); };
-  const int i = token(mw + l32), h = g * P.G + min(mw + l32, rows - 1) - i * P.G, pos = t.pos0 + i;
-  // (the same in every lane, but a division leaves it in vector registers, where what the loads' resources are made of must not come from)
-  auto position = [&](int m) { return __builtin_amdgcn_readfirstlane(t.pos0 + token(m)); };
-  const int ta = position(mb), all_rows = position(mb + ROWS - 1), tb = PAGED ? min(all_rows, P.cache.max_pages * P.cache.page_size - 1) : all_rows;
-  const int wa = position(mw), wb = position(mw + 31);  // this wavefront's
-  const bool working = mw < rows;
-  const KeyTiles<64> keys(ta, tb, P.window, P.sinks);
-  const int begin = PAGED ? (int)min((int64_t)z * P.per_split, (int64_t)keys.count()) : 0;
-  const int count = PAGED && z < splits - 1 ? min(begin + P.per_split, keys.count()) : keys.count();
-  KeySource<D, PAGED> src;
-  src.init(P, t, g, max(0, ta - P.window + 1), tb + 1);
-  RowsLoader<D, kWaves> loader;
-  loader.init(src.pitch, wave, lane);
-  const unsigned tiles0 = lds_offset(&tiles[0][0][0]);
-  auto issue = [&](int x) __attribute__((always_inline)) {
-    const int u = 64 * keys.at(x) + 64 / kWaves * wave;
-    int there;
-    const unsigned long long o = src.rows_at(P, u, 64 / kWaves, there);
-    const unsigned slot = tiles0 + ((x - begin) & 1) * 2 * TILE_B;
-    loader.issue(src.k + o, there, slot);
-    loader.issue(src.v + o, there, slot + TILE_B);
-  };
-
-  // B operand of S^T = K Q^T: column = row lane%32, slots = d 16ks + 8hf + (0..7)
-  bf16x8 qf[NOP];
-  {
-    const bf16* qp = (const bf16*)P.q + ((int64_t)(t.row0 + i) * P.Hq + h) * D + 8 * hf;
-#pragma unroll
-    for (int ks = 0; ks < NOP; ++ks) qf[ks] = *(const bf16x8*)(qp + 16 * ks);
-  }
-  // the query operands must have landed before the tile loads start: from here on only those are in flight, and waited for by hand
-#pragma unroll
-  for (int ks = 0; ks < NOP; ++ks) asm volatile("" : "+v"(qf[ks]));
-  if (begin < count) issue(begin);
-
-  unsigned row_a[NOP], tr_a[D / 32][2];
-#pragma unroll
-  for (int ks = 0; ks < NOP; ++ks) row_a[ks] = tiles0 + l32 * ROW_B + 16 * ((2 * ks + hf) ^ chunk_swizzle<D>(l32));
-#pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int r = 8 * half + 4 * hf + ((lane & 15) >> 2), d = 32 * dt + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-      tr_a[dt][half] = tiles0 + TILE_B + r * ROW_B + 16 * ((d >> 3) ^ chunk_swizzle<D>(r)) + 2 * (d & 7);
-    }
-  auto ld_row = [&](int ks, unsigned off) __attribute__((always_inline)) {
-    return *(const bf16x8 __attribute__((address_space(3)))*)(uintptr_t)(row_a[ks] + off);
-  };
-  // A operand of O^T += V^T P^T: row = d (32dt + lane%32), slots = keys 16kk + 8(e/4) + 4hf + e%4
-  auto ld_tr = [&](int kk, int dt, unsigned off) __attribute__((always_inline)) {
-    const unsigned o = off + kk * 16 * ROW_B;
-    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4 __attribute__((address_space(3)))*)(uintptr_t)(tr_a[dt][0] + o));
-    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((bf16x4 __attribute__((address_space(3)))*)(uintptr_t)(tr_a[dt][1] + o));
-    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-  };
-
-  f32x16 oacc[D / 32];
-#pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt) oacc[dt] = zero16();
-  float m = -__builtin_inff(), neg_m = 0.f, l = 0.f;
-  bf16x8 op[NOP];
-
-  auto tile = [&](auto buf_c, int u0, bool all, unsigned missing) __attribute__((always_inline)) {
-    constexpr unsigned BO = decltype(buf_c)::value * 2 * TILE_B;  // the tile's buffer, as an immediate offset of every LDS read
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {  // keys 32mt .. 32mt + 31 of the tile
-#pragma unroll
-      for (int ks = 0; ks < NOP; ++ks) op[ks] = ld_row(ks, BO + mt * 32 * ROW_B);  // K rows
-      __builtin_amdgcn_sched_barrier(0);
-      f32x16 sacc = zero16();
-#pragma unroll
-      for (int ks = 0; ks < NOP; ++ks) {  // S^T = K Q^T, refilling every operand register with a V^T operand
-        sacc = mfma32(op[ks], qf[ks], sacc);
-        op[ks] = ld_tr(2 * mt + ks / (D / 32), ks % (D / 32), BO);
-      }
-#pragma unroll
-      for (int x = 0; x < NOP; ++x) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      // max3 is inline asm, whose reads of a matrix instruction's result the compiler's hazard recogniser does not see: 12 wait states
-      asm volatile("s_nop 7\n\ts_nop 3" : "+v"(sacc));
-      if (!all) {  // (one body with the mask in a branch: with a masked form of its own the accumulators were copied where the two meet)
-        const Sight sees(pos, u0 + 32 * mt, hf, P.window, P.sinks);
-#pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (!sees(c_row(v, 0)) || (PAGED && (missing >> (2 * mt + (v >> 3)) & 1))) sacc[v] = -__builtin_inff();
-      }
-      // running maximum, followed lazily: the reference moves only when a score exceeds it by 2^kLazy
-      float mx = max3(sacc[0], sacc[1], sacc[2]);
-#pragma unroll
-      for (int v = 3; v < 15; v += 2) mx = max3(mx, sacc[v], sacc[v + 1]);
-      mx = max3(mx, sacc[15], sacc[15]);
-      if (__builtin_amdgcn_ballot_w64(!((mx - m) * P.scale_log2e <= kLazy)) != 0) {
-        mx = max_across_halves(mx);
-        const bool first = m == -__builtin_inff();  // nothing accumulated yet for this row
-        const bool move = first | ((mx - m) * P.scale_log2e > kLazy);
-        const float m_new = move ? fmaxf(m, mx) : m;
-        const float m_use = m_new == -__builtin_inff() ? 0.f : m_new;  // no key seen yet: keep the exponent finite
-        const float alpha = first ? 1.0f : fast_exp2((m - m_use) * P.scale_log2e);
-        neg_m = -m_use * P.scale_log2e;
-        m = m_new;
-        if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
-          l *= alpha;
-#pragma unroll
-          for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) oacc[dt][v] *= alpha;
-        }
-      }
-      // The sum is that of the probabilities before they are rounded to bf16 for the product with V: LSE keeps float32's precision
-      bf16x8 pb[2];
-      float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const float x = fast_exp2(__builtin_fmaf(sacc[v], P.scale_log2e, neg_m));
-        part[v & 3] += x;
-        pb[v >> 3][v & 7] = (bf16)x;
-      }
-      l += (part[0] + part[1]) + (part[2] + part[3]);
-#pragma unroll
-      for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt) oacc[dt] = mfma32(op[kk * (D / 32) + dt], pb[kk], oacc[dt]);
-    }
-  };
-  auto visit = [&](auto buf_c, int x) __attribute__((always_inline)) {
-    const int u0 = 64 * keys.at(x);
-    const unsigned missing = src.missing(P, u0);
-    wait_vmcnt<0>();
-    __builtin_amdgcn_s_barrier();  // tile x has landed for everyone; everyone is done with tile x - 1
-    if (x + 1 < count) issue(x + 1);
-    const bool none = !working || u0 > wb || (wa - (u0 + 63) >= P.window && u0 >= P.sinks);
-    const bool all = u0 + 63 <= wa && (wb - u0 < P.window || u0 + 63 < P.sinks) && missing == 0;
-    if (!none) tile(buf_c, u0, all, missing);
-  };
-  int x = begin;
-  for (; x + 2 <= count; x += 2) {  // two tiles a turn, so that a tile's buffer is known at compile time
-    visit(std::integral_constant<int, 0>(), x);
-    visit(std::integral_constant<int, 1>(), x + 1);
-  }
-  if (x < count) visit(std::integral_constant<int, 0>(), x);
-  wait_vmcnt<0>();
-
-  l += __shfl_xor(l, 32, 64);  // the two lane halves hold different keys of the same row
-  // (a sum that is no number is not one that saw nothing; in a packed batch a sum of zero makes O what it makes LSE: 0 / 0)
-  const float inv = PAGED && l == 0.f ? 0.f : 1.0f / l;
-  if (PAGED && splits > 1) {
-    if (mw + l32 >= rows) return;
-    const int64_t row = ((int64_t)z * P.T + t.row0 + i) * P.Hq + h;
-    if (hf == 0) P.part_lse[row] = l == 0.f ? -__builtin_inff() : m * P.scale_log2e + __builtin_log2f(l);
-    if (l != 0.f) store_column<D>(P.part_o + row * D, oacc, inv, hf);
-    return;
-  }
-  __syncthreads();  // the tiles' LDS is free
-  store_tile<D>(&tiles[0][0][0] + wave * 32 * ROW_B, lane, [&](int dt, int v) __attribute__((always_inline)) { return oacc[dt][v] * inv; },
-                [&](int r) __attribute__((always_inline)) -> bf16* {
-                  if (mw + r >= rows) return nullptr;
-                  const int j = token(mw + r);
-                  return (bf16*)P.o + ((int64_t)(t.row0 + j) * P.Hq + g * P.G + mw + r - j * P.G) * D;
-                });
-  if (hf == 0 && mw + l32 < rows)
-    P.lse[(int64_t)h * P.T + t.row0 + i] = l == 0.f ? empty_lse<PAGED>() : (m * P.scale_log2e + __builtin_log2f(l)) * 0.69314718055994531f;
+  __shared__ __attribute__((aligned(1024))) char tiles[2][2][64 * D * 2];  // [buffer][K, V]
+  window_fwd_rows<D, PAGED, kWaves, LoadedTiles<D, PAGED>>(P, &tiles[0][0][0], P);
 }
 
 // ---------------------------------------------------------------------------------------------
