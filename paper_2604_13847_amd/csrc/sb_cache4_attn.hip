@@ -29,6 +29,7 @@ __device__ inline bf16x8 levels8(unsigned x) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ inline Rsrc resource(const void* base, unsigned bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x20000); }
 template <int SEL> __device__ inline f32x2 numbers(unsigned x) { return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, 1.0f, SEL); }
 __device__ inline float step_at(unsigned pair, int i) { return __uint_as_float(i & 1 ? pair & 0xffff0000u : pair << 16); }
 
@@ -44,15 +45,13 @@ struct Strip {
   __device__ inline float k_step(int b, int v, int c) const { return step_at(ks[b][(v * GROUPS + c) / 2], c); }
   __device__ inline float v_step(int b, int v, int c) const { return step_at(vs[b][(v * GROUPS + c) / 2], c); }
 };
-
-__device__ inline Rsrc resource(const void* base, unsigned bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x20000); }
-template <int D>
-__device__ inline void load_steps(unsigned (&to)[2 * (D / 32)], Rsrc r, unsigned at) {
+template <int N> __device__ inline void load_words(unsigned* to, const unsigned char* from) {  // N x 4 bytes, so aligned
+  typedef struct alignas(N >= 4 ? 16 : 4 * N) { unsigned x[N >= 4 ? 4 : N]; } Piece;
 #pragma unroll
-  for (int i = 0; i < D / 64; ++i) {
-    const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(r, at + 16 * i, 0, 0);
+  for (int i = 0; i < (N + 3) / 4; ++i) {
+    const Piece y = ((const Piece*)from)[i];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) to[4 * i + e] = x[e];
+    for (int e = 0; e < (N >= 4 ? 4 : N); ++e) to[4 * i + e] = y.x[e];
   }
 }
 
@@ -60,10 +59,11 @@ __device__ inline void load_steps(unsigned (&to)[2 * (D / 32)], Rsrc r, unsigned
 // is worked on.  PIECES: a query and a probability as that many bfloat16 numbers.
 constexpr int kWaves4 = 4;
 template <typename T, int D, int NT, int PIECES>
-__global__ __launch_bounds__(64 * kWaves4) void cache4_split_kernel(Cache4Params A) {
+__global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(NT * PIECES == 1 ? 2 : 1))) void cache4_split_kernel(Cache4Params A) {
   const WindowParams& P = A.w;
   constexpr int NW = kWaves4, ROWS = 16 * NT, GROUPS = D / 32, TILES = D / 16;
   constexpr int OUT_P = D + 4;
+  constexpr float kLazy = 8.0f;
   __shared__ float sums[NW][ROWS][OUT_P];
   __shared__ float stats[2][NW][ROWS];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l16 = lane & 15, qd = lane >> 4;
@@ -78,10 +78,10 @@ __global__ __launch_bounds__(64 * kWaves4) void cache4_split_kernel(Cache4Params
   const KeyTiles<32> strips(ta, tb, P.window, P.sinks);
   const int begin = (int)min((int64_t)z * P.per_split, (int64_t)strips.count());
   const int count = z < P.splits - 1 ? min(begin + P.per_split, strips.count()) : strips.count();
-  const int turns = (count - begin - wave + NW - 1) / NW;  // strips of this wavefront: begin + wave + NW x (may be none)
+  const int turns = A.cache.num_pages == 0 ? 0 : (count - begin - wave + NW - 1) / NW;  // strips of this wavefront: begin + wave + NW x (may be none)
   const int32_t* const table = A.cache.table + (int64_t)t.s * A.cache.max_pages;
 
-  // Of strip begin + wave + NW (x0 + lane): the page of its keys 0 .. 15 and 16 .. 31, and how many of each exist (0: none)
+  // Of strip begin + wave + NW (x0 + lane): the page of its keys 0 .. 15 and 16 .. 31, and how many of each exist.  (Where none does, page 0 stands in: its rows are read and not used.)
   int where[2], there[2], x0 = 0;
   auto look_up = [&](int from) __attribute__((always_inline)) {
     x0 = from;
@@ -101,35 +101,26 @@ __global__ __launch_bounds__(64 * kWaves4) void cache4_split_kernel(Cache4Params
       }
     }
   };
-  auto load = [&](Strip<D>& s, int x) __attribute__((always_inline)) {  // strip x of this wavefront; past its last, nothing is read
-    const int at = min(x - x0, 63);
-    const int u = __builtin_amdgcn_readfirstlane(32 * strips.at(min(begin + wave + NW * x, max(strips.count() - 1, 0))));
+  const unsigned at_k = l16 * (D / 2) + qd * (D / 8), at_v = 4 * qd * (D / 2) + l16 * (D / 32), at_s = qd * 4 * GROUPS * 2;
+  const unsigned char* const k_step = (const unsigned char*)A.cache.k_step;
+  const unsigned char* const v_step = (const unsigned char*)A.cache.v_step;
+  auto load = [&](Strip<D>& s, int x) __attribute__((always_inline)) {  // strip x of this wavefront
+    const int u = __builtin_amdgcn_readfirstlane(32 * strips.at(begin + wave + NW * x));
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const unsigned page = (unsigned)__builtin_amdgcn_readlane(where[b], at);
-      const bool any = x < turns && __builtin_amdgcn_readlane(there[b], at) > 0;
+      const unsigned page = (unsigned)__builtin_amdgcn_readlane(where[b], x - x0);
       // (16 rows of a page, all of them in memory, whether or not they have been written)
-      const int64_t row = (((int64_t)page * A.cache.Hkv + g) << A.cache.page_shift) + ((u + 16 * b) & (A.cache.page_size - 1));
-      const unsigned code_b = any ? 16 * (D / 2) : 0, step_b = any ? 16 * GROUPS * 2 : 0;
-      const Rsrc rk = resource(A.cache.k + row * (D / 2), code_b), rv = resource(A.cache.v + row * (D / 2), code_b);
-      const Rsrc rks = resource(A.cache.k_step + row * GROUPS, step_b), rvs = resource(A.cache.v_step + row * GROUPS, step_b);
-      if constexpr (D == 128) {
-        const u32x4 y = __builtin_amdgcn_raw_buffer_load_b128(rk, l16 * (D / 2) + qd * (D / 8), 0, 0);
-#pragma unroll
-        for (int c = 0; c < GROUPS; ++c) s.k[b][c] = y[c];
-      } else {
-        const u32x2 y = __builtin_amdgcn_raw_buffer_load_b64(rk, l16 * (D / 2) + qd * (D / 8), 0, 0);
-#pragma unroll
-        for (int c = 0; c < GROUPS; ++c) s.k[b][c] = y[c];
-      }
-      load_steps<D>(s.ks[b], rks, qd * 4 * GROUPS * 2);
+      const uint64_t row = ((uint64_t)(page * (uint64_t)A.cache.Hkv + g) << A.cache.page_shift) + ((u + 16 * b) & (A.cache.page_size - 1));
+      const uint64_t code = row * (D / 2), step = row * (GROUPS * 2);
+      load_words<GROUPS>(s.k[b], A.cache.k + code + at_k);
+      load_words<2 * GROUPS>(s.ks[b], k_step + step + at_s);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const unsigned at_v = (4 * qd + j) * (D / 2) + l16 * (D / 32);
-        if constexpr (D == 128) s.v[4 * b + j] = __builtin_amdgcn_raw_buffer_load_b32(rv, at_v, 0, 0);
-        else s.v[4 * b + j] = __builtin_amdgcn_raw_buffer_load_b16(rv, at_v, 0, 0);
+        const unsigned char* const from = A.cache.v + code + at_v + j * (D / 2);
+        if constexpr (D == 128) s.v[4 * b + j] = *(const unsigned*)from;
+        else s.v[4 * b + j] = *(const unsigned short*)from;
       }
-      load_steps<D>(s.vs[b], rvs, qd * 4 * GROUPS * 2);
+      load_words<2 * GROUPS>(s.vs[b], v_step + step + at_s);
     }
   };
 
@@ -142,29 +133,35 @@ __global__ __launch_bounds__(64 * kWaves4) void cache4_split_kernel(Cache4Params
     pos[nt] = t.pos0 + i;
     const T* const q = (const T*)P.q + ((int64_t)(t.row0 + i) * P.Hq + h) * D + 8 * qd;
 #pragma unroll
-    for (int c = 0; c < GROUPS; ++c)
+    for (int c = 0; c < GROUPS; ++c) {
+      if constexpr (PIECES == 1) {
+        qf[nt][c][0] = *(const bf16x8*)(q + 32 * c);
+      } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float y = (float)q[32 * c + e];
+        for (int e = 0; e < 8; ++e) {
+          float y = (float)q[32 * c + e];
 #pragma unroll
-        for (int p = 0; p < PIECES; ++p) {
-          qf[nt][c][p][e] = (bf16)y;
-          y -= (float)qf[nt][c][p][e];
+          for (int p = 0; p < PIECES; ++p) {
+            qf[nt][c][p][e] = (bf16)y;
+            y -= (float)qf[nt][c][p][e];
+          }
         }
       }
+    }
   }
   f32x4 acc[NT][TILES];
-  float top[NT], l[NT];  // largest score, in units of log 2, and this lane's share of the sum
+  float top[NT], neg[NT], l[NT];  // the reference of the exponentials (a score, and what is added to them), this lane's share of their sum
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
     for (int d = 0; d < TILES; ++d) acc[nt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     top[nt] = -__builtin_inff();
+    neg[nt] = 0.f;
     l[nt] = 0.f;
   }
 
   auto work = [&](Strip<D>& s, int x) __attribute__((always_inline)) {
-    const int u0 = 32 * strips.at(begin + wave + NW * x);
+    const int u0 = __builtin_amdgcn_readfirstlane(32 * strips.at(begin + wave + NW * x));
     const unsigned have = (1u << __builtin_amdgcn_readlane(there[0], x - x0)) - 1 | ((1u << __builtin_amdgcn_readlane(there[1], x - x0)) - 1) << 16;  // keys that exist
     float sc[NT][2][4];
 #pragma unroll
@@ -182,12 +179,11 @@ __global__ __launch_bounds__(64 * kWaves4) void cache4_split_kernel(Cache4Params
 #pragma unroll
           for (int p = PIECES - 1; p >= 0; --p) y = mfma16(op, qf[nt][c][p], y);
 #pragma unroll
-          for (int v = 0; v < 4; ++v) sc[nt][b][v] = __builtin_fmaf(y[v], s.k_step(b, v, c), sc[nt][b][v]);
+          for (int v = 0; v < 4; ++v) sc[nt][b][v] = c == 0 ? y[v] * s.k_step(b, v, c) : __builtin_fmaf(y[v], s.k_step(b, v, c), sc[nt][b][v]);
         }
       }
     }
-    const bool masked = u0 + 31 > ta || (last - u0 >= P.window && u0 + 31 >= P.sinks) || have != ~0u;
-    if (masked) {
+    if (u0 + 31 > ta || (last - u0 >= P.window && u0 + 31 >= P.sinks) || have != ~0u) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -214,26 +210,31 @@ __global__ __launch_bounds__(64 * kWaves4) void cache4_split_kernel(Cache4Params
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          sc[nt][b][v] *= P.scale_log2e;
-          mx = fmaxf(mx, sc[nt][b][v]);
+        for (int v = 0; v < 4; ++v) mx = fmaxf(mx, sc[nt][b][v]);
+      // running maximum, followed lazily: the reference moves only when a score exceeds it by 2^kLazy
+      if (__builtin_amdgcn_ballot_w64(!((mx - top[nt]) * P.scale_log2e <= kLazy)) != 0) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const bool first = top[nt] == -__builtin_inff();  // nothing accumulated yet for this row
+        const bool move = first | ((mx - top[nt]) * P.scale_log2e > kLazy);
+        const float now = move ? fmaxf(top[nt], mx) : top[nt];
+        const float use = now == -__builtin_inff() ? 0.f : now;  // no key seen yet: keep the exponent finite
+        const float alpha = first ? 1.0f : fast_exp2((top[nt] - use) * P.scale_log2e);
+        neg[nt] = -use * P.scale_log2e;
+        top[nt] = now;
+        if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+          l[nt] *= alpha;
+#pragma unroll
+          for (int d = 0; d < TILES; ++d)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[nt][d][v] *= alpha;
         }
-      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      mx = fmaxf(mx, top[nt]);
-      const float ref = mx == -__builtin_inff() ? 0.f : mx;  // nothing seen yet: keep the exponents finite
-      const float alpha = fast_exp2(top[nt] - ref);
-      top[nt] = mx;
-      l[nt] *= alpha;
-#pragma unroll
-      for (int d = 0; d < TILES; ++d)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) acc[nt][d][v] *= alpha;
+      }
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          const float e = fast_exp2(sc[nt][b][v] - ref);
+          const float e = fast_exp2(__builtin_fmaf(sc[nt][b][v], P.scale_log2e, neg[nt]));
           l[nt] += e;
 #pragma unroll
           for (int c = 0; c < GROUPS; ++c) {
@@ -274,22 +275,17 @@ __global__ __launch_bounds__(64 * kWaves4) void cache4_split_kernel(Cache4Params
     }
   };
 
-  if (turns > 0) {
-    Strip<D> s[2];
-    look_up(0);
-    load(s[0], 0);
-    for (int x = 0; x < turns; x += 2) {  // (64 strips a look-up: an even number)
-      load(s[1], x + 1);
+  Strip<D> s[2];
+  for (int from = 0; from < turns; from += 64) {
+    const int to = min(from + 64, turns);
+    look_up(from);
+    load(s[0], from);
+    for (int x = from; x < to; x += 2) {
+      if (x + 1 < to) load(s[1], x + 1);
       work(s[0], x);
-      if (x + 1 >= turns) break;
-      if (x + 2 - x0 == 64 && x + 2 < turns) {  // the look-up takes the place of this strip's own
-        work(s[1], x + 1);
-        look_up(x + 2);
-        load(s[0], x + 2);
-      } else {
-        load(s[0], x + 2);
-        work(s[1], x + 1);
-      }
+      if (x + 1 >= to) break;
+      if (x + 2 < to) load(s[0], x + 2);
+      work(s[1], x + 1);
     }
   }
   // the wavefronts' sums, through LDS
@@ -299,7 +295,7 @@ __global__ __launch_bounds__(64 * kWaves4) void cache4_split_kernel(Cache4Params
     l[nt] += __shfl_xor(l[nt], 32, 64);
 #pragma unroll
     for (int d = 0; d < TILES; ++d) *(f32x4*)&sums[wave][16 * nt + l16][16 * d + 4 * qd] = acc[nt][d];
-    if (qd == 0) { stats[0][wave][16 * nt + l16] = top[nt]; stats[1][wave][16 * nt + l16] = l[nt]; }
+    if (qd == 0) { stats[0][wave][16 * nt + l16] = top[nt] * P.scale_log2e; stats[1][wave][16 * nt + l16] = l[nt]; }
   }
   __syncthreads();
   constexpr int LANES = D / 4;
@@ -326,8 +322,7 @@ __global__ __launch_bounds__(64 * kWaves4) void cache4_split_kernel(Cache4Params
       if (sum != 0.f) *(f32x4*)(P.part_o + at * D + 4 * c) = x;
     } else {
       T* const to = (T*)P.o + row * D + 4 * c;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) to[e] = (T)x[e];
+      store4(to, x);
       if (c == 0) P.lse[(int64_t)hh * P.T + t.row0 + j] = lse2 * 0.69314718055994531f;
     }
   }
