@@ -14,8 +14,9 @@
 namespace sb {
 
 struct Cache4Params {
-  WindowParams w;  // (its cache is not read)
+  WindowParams w;  // (of its cache, the page table alone is read)
   PagedCache4 cache;
+  int unit;  // see Stream
 };
 
 typedef __amdgpu_buffer_rsrc_t Rsrc;
@@ -55,11 +56,95 @@ template <int N> __device__ inline void load_words(unsigned* to, const unsigned 
   }
 }
 
-// An item is up to 16 NT flattened rows of a KV head and per_split strips; a wavefront takes every NW-th strip, straight into registers, the next one's loads on their way while one
+// The work of few rows as one stream of strips: sequence by sequence, KV head by head, tile of rows by tile, the strips that any row of the sequence sees.  (A tile's own strips are a
+// part of these, from the first on.)  Every workgroup takes as many neighbouring strips as the others, whatever the lengths, which only the device knows; where that
+// cuts an item, its parts are joined by a launch that follows.  Only a workgroup's first and last items can be cut, so two places a workgroup hold all parts.
+// Counted in units of 2^unit strips, so that 31 bits hold the stream.  Where P.splits is 1, an item counts as one unit, and a workgroup has whole items.
+// (64 sequences of 500 to 32768 tokens: items of 2048 keys, whose number goes by the longest sequence, left 3 of 4 workgroups without work: 175 us, 155 as a stream.)
+struct Item {
+  RowTile t;
+  int g;
+  int first, count;  // units of the stream
+};
+template <int ROWS>
+struct Stream {
+  int row0, n, pos0, tiles, count;  // of sequence base + lane
+  __device__ inline int size(const WindowParams& P) const { return tiles * count * P.Hkv; }
+  __device__ inline void load(const Cache4Params& A, int base, int lane) {
+    const WindowParams& P = A.w;
+    row0 = n = pos0 = tiles = count = 0;
+    if (base + lane < P.S) {
+      row0 = P.cu[base + lane];
+      n = P.cu[base + lane + 1];
+      pos0 = P.cached[base + lane];
+      row0 = min(max(row0, 0), P.T);
+      n = min(max(min(n, P.T) - row0, 0), P.max_new);
+      if (n * P.G > P.rows_to) n = 0;
+      pos0 = min(max(pos0, 0), 0x7fffffff - n);
+    }
+    if (n > 0) {
+      tiles = (int)(((unsigned)n * (unsigned)P.G + (unsigned)ROWS - 1) / (unsigned)ROWS);
+      count = KeyTiles<32>(pos0, min(pos0 + n - 1, P.cache.max_pages * P.cache.page_size - 1), P.window, P.sinks).count();
+      count = P.splits == 1 ? 1 : max((count + (1 << A.unit) - 1) >> A.unit, 1);  // (rows that see nothing have a result too)
+    }
+  }
+  // units of a workgroup.  With up to 64 sequences, these stay loaded
+  __device__ inline int share(const Cache4Params& A, int workgroups, int least, int lane) {
+    int sum = 0;
+    for (int base = 0; base < A.w.S; base += 64) {
+      load(A, base, lane);
+      sum += size(A.w);
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1)
+      if (off < A.w.S) sum += __shfl_xor(sum, off, 64);
+    if (A.w.splits == 1) return 1;
+    const unsigned all = (unsigned)__builtin_amdgcn_readfirstlane(sum), each = (all + (unsigned)workgroups - 1) / (unsigned)workgroups;
+    return __builtin_amdgcn_readfirstlane((int)((each + (unsigned)least - 1) / (unsigned)least * (unsigned)least));
+  }
+  // the item that unit x belongs to; s < 0: there are no so many.  fresh: up to 64 sequences are loaded
+  __device__ inline Item find(const Cache4Params& A, int x, int lane, bool fresh) {
+    const WindowParams& P = A.w;
+    int before = 0;
+    for (int base = 0; base < P.S; base += 64) {
+      if (!fresh || P.S > 64) load(A, base, lane);
+      const int mine = size(P);
+      int incl = mine;
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1)
+        if (off < P.S - base) {
+          const int y = __shfl_up(incl, off, 64);
+          if (lane >= off) incl += y;
+        }
+      const unsigned long long hit = __builtin_amdgcn_ballot_w64(base + lane < P.S && x - before < incl);
+      if (hit) {
+        const int src = __builtin_ctzll(hit);
+        Item r;
+        r.count = __builtin_amdgcn_readlane(count, src);
+        const unsigned tiles_ = (unsigned)__builtin_amdgcn_readlane(tiles, src);
+        const int start = before + __builtin_amdgcn_readlane(incl - mine, src);
+        const unsigned item = (unsigned)(x - start) / (unsigned)r.count;
+        r.first = __builtin_amdgcn_readfirstlane(start + (int)item * r.count);
+        const unsigned g = item / tiles_;
+        r.g = __builtin_amdgcn_readfirstlane((int)g);
+        r.t = RowTile{base + src, __builtin_amdgcn_readfirstlane((int)(item - g * tiles_)), __builtin_amdgcn_readlane(row0, src), __builtin_amdgcn_readlane(n, src),
+                      __builtin_amdgcn_readlane(pos0, src)};
+        return r;
+      }
+      before += __builtin_amdgcn_readlane(incl, min(P.S - base, 64) - 1);
+    }
+    Item none{};
+    none.t.s = -1;
+    return none;
+  }
+};
+
+// An item is up to 16 NT flattened rows of a KV head; a wavefront takes every NW-th of the workgroup's strips of it, straight into registers, the next one's loads on their way while one
 // is worked on.  PIECES: a query and a probability as that many bfloat16 numbers.
 constexpr int kWaves4 = 4;
+constexpr int split_waves(int D, int operands) { return (D == 64 ? 2 : 1) + (operands == 1); }  // of a SIMD, by registers
 template <typename T, int D, int NT, int PIECES>
-__global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(NT * PIECES == 1 ? 2 : 1))) void cache4_split_kernel(Cache4Params A) {
+__global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(split_waves(D, NT * PIECES)))) void cache4_split_kernel(Cache4Params A) {
   const WindowParams& P = A.w;
   constexpr int NW = kWaves4, ROWS = 16 * NT, GROUPS = D / 32, TILES = D / 16;
   constexpr int OUT_P = D + 4;
@@ -67,265 +152,366 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(NT
   __shared__ float sums[NW][ROWS][OUT_P];
   __shared__ float stats[2][NW][ROWS];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l16 = lane & 15, qd = lane >> 4;
-  const int z = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (unsigned)P.Hkv % (unsigned)P.splits));
-  const RowTile t = locate_tile<ROWS, true>(P, blockIdx.x / (unsigned)P.Hkv / (unsigned)P.splits);
-  if (t.s < 0) return;
-  const int g = __builtin_amdgcn_readfirstlane((int)(blockIdx.x % (unsigned)P.Hkv));
-  const int rows = t.n * P.G, m0 = t.tile * ROWS, mine = min(rows - m0, ROWS);
-  auto token = [&](int m) { return (int)((unsigned)min(m, rows - 1) / (unsigned)P.G); };
-  const int ta = __builtin_amdgcn_readfirstlane(t.pos0 + token(m0)), last = __builtin_amdgcn_readfirstlane(t.pos0 + token(m0 + ROWS - 1));
-  const int tb = min(last, A.cache.max_pages * A.cache.page_size - 1), end = tb + 1, lo = max(0, ta - P.window + 1);
-  const KeyTiles<32> strips(ta, tb, P.window, P.sinks);
-  const int begin = (int)min((int64_t)z * P.per_split, (int64_t)strips.count());
-  const int count = z < P.splits - 1 ? min(begin + P.per_split, strips.count()) : strips.count();
-  const int turns = A.cache.num_pages == 0 ? 0 : (count - begin - wave + NW - 1) / NW;  // strips of this wavefront: begin + wave + NW x (may be none)
-  const int32_t* const table = A.cache.table + (int64_t)t.s * A.cache.max_pages;
+  Stream<ROWS> stream;
+  const int share = stream.share(A, gridDim.x, NW >> A.unit > 0 ? NW >> A.unit : 1, lane);
+  const int64_t x_last = (int64_t)share * (blockIdx.x + 1);
+  if (x_last - share > 0x7fffffff) return;
+  int x_first = (int)(x_last - share);
+  const int x_end = (int)min(x_last, (int64_t)0x7fffffff);
+  Item item = stream.find(A, x_first, lane, true);
+  while (item.t.s >= 0) {
+    const RowTile t = item.t;
+    const int g = item.g, x_next = min(x_end, item.first + item.count);
+    const int rows = t.n * P.G, m0 = t.tile * ROWS, mine = min(rows - m0, ROWS);
+    auto token = [&](int m) { return (int)((unsigned)min(m, rows - 1) / (unsigned)P.G); };
+    const int ta = __builtin_amdgcn_readfirstlane(t.pos0 + token(m0)), last = __builtin_amdgcn_readfirstlane(t.pos0 + token(m0 + ROWS - 1));
+    const int tb = min(last, A.cache.max_pages * A.cache.page_size - 1), end = tb + 1, lo = max(0, ta - P.window + 1);
+    const KeyTiles<32> strips(ta, tb, P.window, P.sinks);
+    const int begin = (int)min((int64_t)(x_first - item.first) << A.unit, (int64_t)strips.count());
+    const int count = P.splits == 1 ? strips.count() : (int)min((int64_t)(x_next - item.first) << A.unit, (int64_t)strips.count());
+    const bool whole = x_first == item.first && x_next == item.first + item.count;
+    const int turns = A.cache.num_pages == 0 ? 0 : max(count - begin - wave + NW - 1, 0) / NW;  // strips of this wavefront: begin + wave + NW x (may be none)
+    const int32_t* const table = A.cache.table + (int64_t)t.s * A.cache.max_pages;
 
-  // Of strip begin + wave + NW (x0 + lane): the page of its keys 0 .. 15 and 16 .. 31, and how many of each exist.  (Where none does, page 0 stands in: its rows are read and not used.)
-  int where[2], there[2], x0 = 0;
-  auto look_up = [&](int from) __attribute__((always_inline)) {
-    x0 = from;
+    // Of strip begin + wave + NW (x0 + lane): the page of its keys 0 .. 15 and 16 .. 31, and how many of each exist.  (Where none does, page 0 stands in: its rows are read and not used.)
+    int where[2], there[2], x0 = 0;
+    auto look_up = [&](int from) __attribute__((always_inline)) {
+      x0 = from;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      where[b] = 0;
-      there[b] = 0;
-      if (from + lane < turns) {
-        const int u = 32 * strips.at(begin + wave + NW * (from + lane)) + 16 * b;
-        if (u < end && (u + 16 > lo || u < P.sinks)) {
-          const int page = table[u >> A.cache.page_shift];
-          if ((unsigned)page < (unsigned)A.cache.num_pages) {
-            there[b] = min(end - u, 16);
-            where[b] = page;
+      for (int b = 0; b < 2; ++b) {
+        where[b] = 0;
+        there[b] = 0;
+        if (from + lane < turns) {
+          const int u = 32 * strips.at(begin + wave + NW * (from + lane)) + 16 * b;
+          if (u < end && (u + 16 > lo || u < P.sinks)) {
+            const int page = table[u >> A.cache.page_shift];
+            if ((unsigned)page < (unsigned)A.cache.num_pages) {
+              there[b] = min(end - u, 16);
+              where[b] = page;
+            }
           }
         }
       }
-    }
-  };
-  const unsigned at_k = l16 * (D / 2) + qd * (D / 8), at_v = 4 * qd * (D / 2) + l16 * (D / 32), at_s = qd * 4 * GROUPS * 2;
-  const unsigned char* const k_step = (const unsigned char*)A.cache.k_step;
-  const unsigned char* const v_step = (const unsigned char*)A.cache.v_step;
-  auto load = [&](Strip<D>& s, int x) __attribute__((always_inline)) {  // strip x of this wavefront
-    const int u = __builtin_amdgcn_readfirstlane(32 * strips.at(begin + wave + NW * x));
+    };
+    const unsigned at_k = l16 * (D / 2) + qd * (D / 8), at_v = 4 * qd * (D / 2) + l16 * (D / 32), at_s = qd * 4 * GROUPS * 2;
+    const unsigned char* const k_step = (const unsigned char*)A.cache.k_step;
+    const unsigned char* const v_step = (const unsigned char*)A.cache.v_step;
+    auto load = [&](Strip<D>& s, int x) __attribute__((always_inline)) {  // strip x of this wavefront
+      const int u = __builtin_amdgcn_readfirstlane(32 * strips.at(begin + wave + NW * x));
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const unsigned page = (unsigned)__builtin_amdgcn_readlane(where[b], x - x0);
-      // (16 rows of a page, all of them in memory, whether or not they have been written)
-      const uint64_t row = ((uint64_t)(page * (uint64_t)A.cache.Hkv + g) << A.cache.page_shift) + ((u + 16 * b) & (A.cache.page_size - 1));
-      const uint64_t code = row * (D / 2), step = row * (GROUPS * 2);
-      load_words<GROUPS>(s.k[b], A.cache.k + code + at_k);
-      load_words<2 * GROUPS>(s.ks[b], k_step + step + at_s);
+      for (int b = 0; b < 2; ++b) {
+        const unsigned page = (unsigned)__builtin_amdgcn_readlane(where[b], x - x0);
+        // (16 rows of a page, all of them in memory, whether or not they have been written)
+        const uint64_t row = ((uint64_t)(page * (uint64_t)A.cache.Hkv + g) << A.cache.page_shift) + ((u + 16 * b) & (A.cache.page_size - 1));
+        const uint64_t code = row * (D / 2), step = row * (GROUPS * 2);
+        load_words<GROUPS>(s.k[b], A.cache.k + code + at_k);
+        load_words<2 * GROUPS>(s.ks[b], k_step + step + at_s);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const unsigned char* const from = A.cache.v + code + at_v + j * (D / 2);
-        if constexpr (D == 128) s.v[4 * b + j] = *(const unsigned*)from;
-        else s.v[4 * b + j] = *(const unsigned short*)from;
-      }
-      load_words<2 * GROUPS>(s.vs[b], v_step + step + at_s);
-    }
-  };
-
-  // B operand of the scores: column = row l16 of tile nt
-  bf16x8 qf[NT][GROUPS][PIECES];
-  int pos[NT];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int m = min(m0 + 16 * nt + l16, rows - 1), i = token(m), h = g * P.G + m - i * P.G;
-    pos[nt] = t.pos0 + i;
-    const T* const q = (const T*)P.q + ((int64_t)(t.row0 + i) * P.Hq + h) * D + 8 * qd;
-#pragma unroll
-    for (int c = 0; c < GROUPS; ++c) {
-      if constexpr (PIECES == 1) {
-        qf[nt][c][0] = *(const bf16x8*)(q + 32 * c);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float y = (float)q[32 * c + e];
-#pragma unroll
-          for (int p = 0; p < PIECES; ++p) {
-            qf[nt][c][p][e] = (bf16)y;
-            y -= (float)qf[nt][c][p][e];
-          }
+        for (int j = 0; j < 4; ++j) {
+          const unsigned char* const from = A.cache.v + code + at_v + j * (D / 2);
+          if constexpr (D == 128) s.v[4 * b + j] = *(const unsigned*)from;
+          else s.v[4 * b + j] = *(const unsigned short*)from;
         }
+        load_words<2 * GROUPS>(s.vs[b], v_step + step + at_s);
       }
-    }
-  }
-  f32x4 acc[NT][TILES];
-  float top[NT], neg[NT], l[NT];  // the reference of the exponentials (a score, and what is added to them), this lane's share of their sum
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-    for (int d = 0; d < TILES; ++d) acc[nt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    top[nt] = -__builtin_inff();
-    neg[nt] = 0.f;
-    l[nt] = 0.f;
-  }
+    };
 
-  auto work = [&](Strip<D>& s, int x) __attribute__((always_inline)) {
-    const int u0 = __builtin_amdgcn_readfirstlane(32 * strips.at(begin + wave + NW * x));
-    const unsigned have = (1u << __builtin_amdgcn_readlane(there[0], x - x0)) - 1 | ((1u << __builtin_amdgcn_readlane(there[1], x - x0)) - 1) << 16;  // keys that exist
-    float sc[NT][2][4];
+    // B operand of the scores: column = row l16 of tile nt
+    bf16x8 qf[NT][GROUPS][PIECES];
+    int pos[NT];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) sc[nt][b][v] = 0.f;
+    for (int nt = 0; nt < NT; ++nt) {
+      const int m = min(m0 + 16 * nt + l16, rows - 1), i = token(m), h = g * P.G + m - i * P.G;
+      pos[nt] = t.pos0 + i;
+      const T* const q = (const T*)P.q + ((int64_t)(t.row0 + i) * P.Hq + h) * D + 8 * qd;
 #pragma unroll
       for (int c = 0; c < GROUPS; ++c) {
-        const bf16x8 op = levels8(s.k[b][c]);
+        if constexpr (PIECES == 1) {
+          qf[nt][c][0] = *(const bf16x8*)(q + 32 * c);
+        } else {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          f32x4 y = {0.f, 0.f, 0.f, 0.f};
+          for (int e = 0; e < 8; ++e) {
+            float y = (float)q[32 * c + e];
 #pragma unroll
-          for (int p = PIECES - 1; p >= 0; --p) y = mfma16(op, qf[nt][c][p], y);
-#pragma unroll
-          for (int v = 0; v < 4; ++v) sc[nt][b][v] = c == 0 ? y[v] * s.k_step(b, v, c) : __builtin_fmaf(y[v], s.k_step(b, v, c), sc[nt][b][v]);
+            for (int p = 0; p < PIECES; ++p) {
+              qf[nt][c][p][e] = (bf16)y;
+              y -= (float)qf[nt][c][p][e];
+            }
+          }
         }
       }
     }
-    if (u0 + 31 > ta || (last - u0 >= P.window && u0 + 31 >= P.sinks) || have != ~0u) {
+    f32x4 acc[NT][TILES];
+    float top[NT], neg[NT], l[NT];  // the reference of the exponentials (a score, and what is added to them), this lane's share of their sum
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int d = 0; d < TILES; ++d) acc[nt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+      top[nt] = -__builtin_inff();
+      neg[nt] = 0.f;
+      l[nt] = 0.f;
+    }
+
+    auto work = [&](Strip<D>& s, int x) __attribute__((always_inline)) {
+      const int u0 = __builtin_amdgcn_readfirstlane(32 * strips.at(begin + wave + NW * x));
+      const unsigned have = (1u << __builtin_amdgcn_readlane(there[0], x - x0)) - 1 | ((1u << __builtin_amdgcn_readlane(there[1], x - x0)) - 1) << 16;  // keys that exist
+      float sc[NT][2][4];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) sc[nt][b][v] = 0.f;
+#pragma unroll
+        for (int c = 0; c < GROUPS; ++c) {
+          const bf16x8 op = levels8(s.k[b][c]);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int p = PIECES - 1; p >= 0; --p) y = mfma16(op, qf[nt][c][p], y);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) sc[nt][b][v] = c == 0 ? y[v] * s.k_step(b, v, c) : __builtin_fmaf(y[v], s.k_step(b, v, c), sc[nt][b][v]);
+          }
+        }
+      }
+      if (u0 + 31 > ta || (last - u0 >= P.window && u0 + 31 >= P.sinks) || have != ~0u) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const int r = 16 * b + 4 * qd + v;
+              if (!sees(pos[nt], u0 + r, P.window, P.sinks) || !(have >> r & 1)) sc[nt][b][v] = -__builtin_inff();
+            }
+        // keys that do not exist have no steps either, whatever the page holds
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            if (!(have >> (16 * b + 4 * qd + v) & 1)) {
+              if constexpr (GROUPS == 4) s.vs[b][2 * v] = s.vs[b][2 * v + 1] = 0;
+              else s.vs[b][v] = 0;
+            }
+      }
+      bf16x8 w[NT][GROUPS][PIECES];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float mx = -__builtin_inff();
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) mx = fmaxf(mx, sc[nt][b][v]);
+        // running maximum, followed lazily: the reference moves only when a score exceeds it by 2^kLazy
+        if (__builtin_amdgcn_ballot_w64(!((mx - top[nt]) * P.scale_log2e <= kLazy)) != 0) {
+          mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+          mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+          const bool first = top[nt] == -__builtin_inff();  // nothing accumulated yet for this row
+          const bool move = first | ((mx - top[nt]) * P.scale_log2e > kLazy);
+          const float now = move ? fmaxf(top[nt], mx) : top[nt];
+          const float use = now == -__builtin_inff() ? 0.f : now;  // no key seen yet: keep the exponent finite
+          const float alpha = first ? 1.0f : fast_exp2((top[nt] - use) * P.scale_log2e);
+          neg[nt] = -use * P.scale_log2e;
+          top[nt] = now;
+          if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+            l[nt] *= alpha;
+#pragma unroll
+            for (int d = 0; d < TILES; ++d)
+#pragma unroll
+              for (int v = 0; v < 4; ++v) acc[nt][d][v] *= alpha;
+          }
+        }
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
-            const int r = 16 * b + 4 * qd + v;
-            if (!sees(pos[nt], u0 + r, P.window, P.sinks) || !(have >> r & 1)) sc[nt][b][v] = -__builtin_inff();
-          }
-      // keys that do not exist have no steps either, whatever the page holds
+            const float e = fast_exp2(__builtin_fmaf(sc[nt][b][v], P.scale_log2e, neg[nt]));
+            l[nt] += e;
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+            for (int c = 0; c < GROUPS; ++c) {
+              float y = e * s.v_step(b, v, c);
 #pragma unroll
-        for (int v = 0; v < 4; ++v)
-          if (!(have >> (16 * b + 4 * qd + v) & 1)) {
-            if constexpr (GROUPS == 4) s.vs[b][2 * v] = s.vs[b][2 * v + 1] = 0;
-            else s.vs[b][v] = 0;
-          }
-    }
-    bf16x8 w[NT][GROUPS][PIECES];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      float mx = -__builtin_inff();
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) mx = fmaxf(mx, sc[nt][b][v]);
-      // running maximum, followed lazily: the reference moves only when a score exceeds it by 2^kLazy
-      if (__builtin_amdgcn_ballot_w64(!((mx - top[nt]) * P.scale_log2e <= kLazy)) != 0) {
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const bool first = top[nt] == -__builtin_inff();  // nothing accumulated yet for this row
-        const bool move = first | ((mx - top[nt]) * P.scale_log2e > kLazy);
-        const float now = move ? fmaxf(top[nt], mx) : top[nt];
-        const float use = now == -__builtin_inff() ? 0.f : now;  // no key seen yet: keep the exponent finite
-        const float alpha = first ? 1.0f : fast_exp2((top[nt] - use) * P.scale_log2e);
-        neg[nt] = -use * P.scale_log2e;
-        top[nt] = now;
-        if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
-          l[nt] *= alpha;
-#pragma unroll
-          for (int d = 0; d < TILES; ++d)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) acc[nt][d][v] *= alpha;
-        }
-      }
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const float e = fast_exp2(__builtin_fmaf(sc[nt][b][v], P.scale_log2e, neg[nt]));
-          l[nt] += e;
-#pragma unroll
-          for (int c = 0; c < GROUPS; ++c) {
-            float y = e * s.v_step(b, v, c);
-#pragma unroll
-            for (int p = 0; p < PIECES; ++p) {
-              w[nt][c][p][4 * b + v] = (bf16)y;
-              y -= (float)w[nt][c][p][4 * b + v];
+              for (int p = 0; p < PIECES; ++p) {
+                w[nt][c][p][4 * b + v] = (bf16)y;
+                y -= (float)w[nt][c][p][4 * b + v];
+              }
             }
           }
-        }
-    }
-    // levels of two keys side by side in a byte: even and odd tiles' (a word's nibble t is element 16 t + l16)
-    unsigned even[4], odd[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const unsigned a = s.v[2 * j], b = s.v[2 * j + 1];
-      even[j] = (a & 0x0f0f0f0fu) | (b << 4 & 0xf0f0f0f0u);
-      odd[j] = (a >> 4 & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u);
-    }
-    auto tile = [&](auto tc) __attribute__((always_inline)) {
-      constexpr int TT = decltype(tc)::value;
-      bf16x8 op;
+      }
+      // levels of two keys side by side in a byte: even and odd tiles' (a word's nibble t is element 16 t + l16)
+      unsigned even[4], odd[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const bf16x2 y = levels<TT / 2>(TT & 1 ? odd[j] : even[j]);
-        op[2 * j] = y[0];
-        op[2 * j + 1] = y[1];
+        const unsigned a = s.v[2 * j], b = s.v[2 * j + 1];
+        even[j] = (a & 0x0f0f0f0fu) | (b << 4 & 0xf0f0f0f0u);
+        odd[j] = (a >> 4 & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u);
       }
+      auto tile = [&](auto tc) __attribute__((always_inline)) {
+        constexpr int TT = decltype(tc)::value;
+        bf16x8 op;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+        for (int j = 0; j < 4; ++j) {
+          const bf16x2 y = levels<TT / 2>(TT & 1 ? odd[j] : even[j]);
+          op[2 * j] = y[0];
+          op[2 * j + 1] = y[1];
+        }
 #pragma unroll
-        for (int p = PIECES - 1; p >= 0; --p) acc[nt][TT] = mfma16(op, w[nt][TT / 2][p], acc[nt][TT]);
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int p = PIECES - 1; p >= 0; --p) acc[nt][TT] = mfma16(op, w[nt][TT / 2][p], acc[nt][TT]);
+      };
+      tile(std::integral_constant<int, 0>()); tile(std::integral_constant<int, 1>()); tile(std::integral_constant<int, 2>()); tile(std::integral_constant<int, 3>());
+      if constexpr (D == 128) {
+        tile(std::integral_constant<int, 4>()); tile(std::integral_constant<int, 5>()); tile(std::integral_constant<int, 6>()); tile(std::integral_constant<int, 7>());
+      }
     };
-    tile(std::integral_constant<int, 0>()); tile(std::integral_constant<int, 1>()); tile(std::integral_constant<int, 2>()); tile(std::integral_constant<int, 3>());
-    if constexpr (D == 128) {
-      tile(std::integral_constant<int, 4>()); tile(std::integral_constant<int, 5>()); tile(std::integral_constant<int, 6>()); tile(std::integral_constant<int, 7>());
-    }
-  };
 
-  Strip<D> s[2];
-  for (int from = 0; from < turns; from += 64) {
-    const int to = min(from + 64, turns);
-    look_up(from);
-    load(s[0], from);
-    for (int x = from; x < to; x += 2) {
-      if (x + 1 < to) load(s[1], x + 1);
-      work(s[0], x);
-      if (x + 1 >= to) break;
-      if (x + 2 < to) load(s[0], x + 2);
-      work(s[1], x + 1);
+    Strip<D> s[2];
+    for (int from = 0; from < turns; from += 64) {
+      const int to = min(from + 64, turns);
+      look_up(from);
+      load(s[0], from);
+      for (int x = from; x < to; x += 2) {
+        if (x + 1 < to) load(s[1], x + 1);
+        work(s[0], x);
+        if (x + 1 >= to) break;
+        if (x + 2 < to) load(s[0], x + 2);
+        work(s[1], x + 1);
+      }
+    }
+    // the wavefronts' sums, through LDS
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      l[nt] += __shfl_xor(l[nt], 16, 64);
+      l[nt] += __shfl_xor(l[nt], 32, 64);
+#pragma unroll
+      for (int d = 0; d < TILES; ++d) *(f32x4*)&sums[wave][16 * nt + l16][16 * d + 4 * qd] = acc[nt][d];
+      if (qd == 0) { stats[0][wave][16 * nt + l16] = top[nt] * P.scale_log2e; stats[1][wave][16 * nt + l16] = l[nt]; }
+    }
+    __syncthreads();
+    constexpr int LANES = D / 4;
+    const int c = threadIdx.x % LANES;
+    for (int r = threadIdx.x / LANES; r < mine; r += 64 * NW / LANES) {
+      float best = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) best = fmaxf(best, stats[0][w][r]);
+      f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        if (stats[1][w][r] == 0.f) continue;
+        const float f = fast_exp2(stats[0][w][r] - best);
+        sum += f * stats[1][w][r];
+        x += f * *(const f32x4*)&sums[w][r][4 * c];
+      }
+      const int j = token(m0 + r), hh = g * P.G + m0 + r - j * P.G;
+      const int64_t row = (int64_t)(t.row0 + j) * P.Hq + hh;
+      const float inv = sum == 0.f ? 0.f : 1.0f / sum, lse2 = sum == 0.f ? -__builtin_inff() : best + __builtin_log2f(sum);  // (a sum that is no number is passed on)
+      x *= inv;
+      if (whole) {
+        store4((T*)P.o + row * D + 4 * c, x);
+        if (c == 0) P.lse[(int64_t)hh * P.T + t.row0 + j] = lse2 * 0.69314718055994531f;
+      } else {  // place 0: an item that began before this workgroup's strips, 1: one that ends behind them
+        const int64_t at = ((int64_t)blockIdx.x * 2 + (x_first == item.first)) * ROWS + r;
+        if (c == 0) P.part_lse[at] = lse2;
+        *(f32x4*)(P.part_o + at * D + 4 * c) = x;
+      }
+    }
+    x_first = x_next;
+    if (x_first >= x_end) break;
+    __syncthreads();  // the sums' LDS is free
+    item = stream.find(A, x_first, lane, false);  // (loaded again: kept, the sequences' numbers would cost the strips registers)
+  }
+}
+
+// Joins the parts of the items that were cut: a workgroup to a row and head, every fourth part a wavefront's.  A part that saw nothing has LSE -infinity; one that saw what is no number
+// has left that, and so is the row's result.  Rows of no sequence, and of items that one workgroup has had, are left as they are.
+template <typename T, int D, int ROWS>
+__global__ __launch_bounds__(256) void cache4_join_kernel(Cache4Params A, int workgroups, int seq_rows) {
+  const WindowParams& P = A.w;
+  constexpr int E = D / 64, NW = kWaves4;
+  __shared__ float sums[4][E + 2][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int h = (int)(blockIdx.x % (unsigned)P.Hq), at = (int)(blockIdx.x / (unsigned)P.Hq), g = h / P.G;
+  const int s = seq_rows > 0 ? at / seq_rows : sequence_of(P.cu, P.S, at, lane);
+  if (s >= P.S) return;
+  const int row0 = min(max(P.cu[s], 0), P.T), tok = seq_rows > 0 ? row0 + at % seq_rows : at;
+  Stream<ROWS> stream;
+  const int share = stream.share(A, workgroups, NW >> A.unit > 0 ? NW >> A.unit : 1, lane);
+  if (share == 0) return;
+  // where the sequence begins in the stream
+  int start = 0, n = 0, tiles = 0, count = 0;
+  for (int base = 0; base <= s; base += 64) {
+    if (P.S > 64) stream.load(A, base, lane);
+    int x = base + lane < s ? stream.size(P) : 0;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1)
+      if (off < P.S) x += __shfl_xor(x, off, 64);
+    start += x;
+    if (s - base < 64) {
+      n = __builtin_amdgcn_readlane(stream.n, s - base);
+      tiles = __builtin_amdgcn_readlane(stream.tiles, s - base);
+      count = __builtin_amdgcn_readlane(stream.count, s - base);
     }
   }
-  // the wavefronts' sums, through LDS
+  if (tok - row0 < 0 || tok - row0 >= n) return;
+  const int m = (tok - row0) * P.G + h % P.G;
+  const unsigned first = (unsigned)(__builtin_amdgcn_readfirstlane(start) + (g * tiles + m / ROWS) * count), w0 = first / (unsigned)share, w1 = (first + (unsigned)count - 1) / (unsigned)share;
+  if (w0 == w1) return;
+  const int parts = (int)(w1 - w0) + 1;
+  constexpr int kRuns = 8;  // on their way at a time
+  float x[E] = {}, best = -__builtin_inff(), sum = 0.f;
+  for (int z0 = wave; z0 < parts; z0 += 4 * kRuns) {
+    float lse[kRuns], part[kRuns][E], top = best;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    l[nt] += __shfl_xor(l[nt], 16, 64);
-    l[nt] += __shfl_xor(l[nt], 32, 64);
+    for (int i = 0; i < kRuns; ++i) {  // (past the last part, it again)
+      const unsigned w = w0 + (unsigned)min(z0 + 4 * i, parts - 1);
+      const int64_t from = ((int64_t)w * 2 + ((uint64_t)w * (unsigned)share <= first)) * ROWS + m % ROWS;
+      lse[i] = P.part_lse[from];
 #pragma unroll
-    for (int d = 0; d < TILES; ++d) *(f32x4*)&sums[wave][16 * nt + l16][16 * d + 4 * qd] = acc[nt][d];
-    if (qd == 0) { stats[0][wave][16 * nt + l16] = top[nt] * P.scale_log2e; stats[1][wave][16 * nt + l16] = l[nt]; }
+      for (int e = 0; e < E; ++e) part[i][e] = P.part_o[from * D + E * lane + e];
+      if (z0 + 4 * i >= parts) lse[i] = -__builtin_inff();
+    }
+#pragma unroll
+    for (int i = 0; i < kRuns; ++i) top = fmaxf(top, lse[i]);
+    const float ref = top == -__builtin_inff() ? 0.f : top;  // nothing seen yet: keep the exponents finite
+    const float old = fast_exp2(best - ref);
+    sum *= old;
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] *= old;
+#pragma unroll
+    for (int i = 0; i < kRuns; ++i) {
+      const float f = fast_exp2(lse[i] - ref);
+      sum += f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(f, lse[i] == -__builtin_inff() ? 0.f : part[i][e], x[e]);
+    }
+    best = top;
   }
+#pragma unroll
+  for (int e = 0; e < E; ++e) sums[wave][e][lane] = x[e];
+  sums[wave][E][lane] = best;
+  sums[wave][E + 1][lane] = sum;
   __syncthreads();
-  constexpr int LANES = D / 4;
-  const int c = threadIdx.x % LANES;
-  for (int r = threadIdx.x / LANES; r < mine; r += 64 * NW / LANES) {
-    float best = -__builtin_inff(), sum = 0.f;
+  if (wave > 0) return;
+  best = -__builtin_inff();
 #pragma unroll
-    for (int w = 0; w < NW; ++w) best = fmaxf(best, stats[0][w][r]);
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int w = 0; w < 4; ++w) best = fmaxf(best, sums[w][E][lane]);
+  sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      if (stats[1][w][r] == 0.f) continue;
-      const float f = fast_exp2(stats[0][w][r] - best);
-      sum += f * stats[1][w][r];
-      x += f * *(const f32x4*)&sums[w][r][4 * c];
-    }
-    const int j = token(m0 + r), hh = g * P.G + m0 + r - j * P.G;
-    const int64_t row = (int64_t)(t.row0 + j) * P.Hq + hh;
-    const float inv = sum == 0.f ? 0.f : 1.0f / sum, lse2 = sum == 0.f ? -__builtin_inff() : best + __builtin_log2f(sum);  // (a sum that is no number is passed on)
-    x *= inv;
-    if (P.splits > 1) {
-      const int64_t at = ((int64_t)z * P.part_rows + (P.part_seq_rows > 0 ? t.s * P.part_seq_rows : t.row0) + j) * P.Hq + hh;
-      if (c == 0) P.part_lse[at] = lse2;
-      if (sum != 0.f) *(f32x4*)(P.part_o + at * D + 4 * c) = x;
-    } else {
-      T* const to = (T*)P.o + row * D + 4 * c;
-      store4(to, x);
-      if (c == 0) P.lse[(int64_t)hh * P.T + t.row0 + j] = lse2 * 0.69314718055994531f;
-    }
+  for (int e = 0; e < E; ++e) x[e] = 0.f;
+  const float ref = best == -__builtin_inff() ? 0.f : best;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float f = fast_exp2(sums[w][E][lane] - ref);
+    sum += f * sums[w][E + 1][lane];
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(f, sums[w][e][lane], x[e]);
   }
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+#pragma unroll
+  for (int e = 0; e < E; ++e) ((T*)P.o)[((int64_t)tok * P.Hq + h) * D + E * lane + e] = (T)(x[e] * inv);
+  if (lane == 0) P.lse[(int64_t)h * P.T + tok] = sum == 0.f ? -__builtin_inff() : (best + __builtin_log2f(sum)) * 0.69314718055994531f;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -440,53 +626,51 @@ __global__ __launch_bounds__(64 * kChunkWaves) __attribute__((amdgpu_waves_per_e
 
 // How the work is cut.  Sequences of up to kFewRows4 flattened rows are cache4_split_kernel's (float32: all of them), the others cache4_chunk_kernel's; a batch of one kind costs one launch.
 constexpr int kFewRows4 = 64;
-struct Cache4Launch {
-  int64_t items;  // tiles of rows; 0: no such launch
-  int splits, per_split, part_rows, part_seq_rows;
-};
 struct Cache4Plan {
-  Cache4Launch few, many;
-  int nt;
+  int64_t few, many;      // tiles of rows; 0: no such launch
+  int rows;               // of a tile of few rows
+  int workgroups;         // of few rows; 0: whole items, a workgroup each
+  int unit;
+  int splits, per_split;  // of many rows: keys in `splits` runs of per_split tiles
   size_t part_o, bytes;
 };
 static int few_seq_rows4(const sb_cache4* c, int G, int max_new) { return c->dtype == SB_F32 ? max_new : std::min(kFewRows4 / G, max_new); }  // tokens of a sequence of few rows, at most
 static Cache4Plan plan_cache4(const sb_cache4* c, const sb_chunk* n, int window, int sinks) {
   Cache4Plan p{};
-  const int G = n->num_q_heads / c->num_kv_heads, S = n->num_seqs;
+  const int G = n->num_q_heads / c->num_kv_heads, S = n->num_seqs, D = c->head_dim;
   const bool f32 = c->dtype == SB_F32;
   const int64_t most = (int64_t)std::min(n->max_new, n->total_new) * G;  // rows of a sequence
-  auto launch = [&](int64_t most_rows, int rows, int tile, int64_t wanted, int64_t least, int64_t largest) {
-    Cache4Launch l{};
-    l.items = std::min(row_tiles_most(n->total_new, S, G, rows), (most_rows + rows - 1) / rows * S);
+  auto items = [&](int64_t most_rows, int rows) { return std::min(row_tiles_most(n->total_new, S, G, rows), (most_rows + rows - 1) / rows * S); };
+  auto tiles = [&](int rows, int tile) {  // of keys of an item, about: what max_length, the page table, the window and the sinks leave
     const int64_t in_window = (int64_t)window + (rows + G - 1) / G + sinks + 2 * tile;
     const int64_t longest = std::min<int64_t>(n->max_length, (int64_t)c->max_pages * c->page_size);
-    const int64_t keys = std::min(in_window, longest), tiles = (keys + tile - 1) / tile, workgroups = l.items * c->num_kv_heads;
-    int64_t per = (tiles * workgroups + wanted - 1) / wanted;
-    per = std::max((per + least - 1) / least * least, least);
-    if (workgroups < 2048) per = std::min(per, largest);
-    l.splits = (int)std::max<int64_t>((tiles + per - 1) / per, 1);
-    l.per_split = (int)per;
-    l.part_rows = n->total_new;
-    return l;
+    return (std::min(in_window, longest) + tile - 1) / tile;
   };
-  p.few.splits = p.many.splits = 1;
-  p.nt = f32 || most <= 16 ? 1 : 2;
-  // Two workgroups a CU; a strip for each wavefront at least, and where items are few 2048 keys at most, so that sequences of unequal lengths even out.
-  if (f32) p.few = launch(most, 16, 32, 512, kWaves4, 64);
-  else if (G <= kFewRows4 && (S > 1 || most <= kFewRows4)) p.few = launch(std::min<int64_t>(most, kFewRows4), 16 * p.nt, 32, 512, kWaves4, 64);
-  // A workgroup a CU, of 8 tiles at least.
-  if (!f32 && most > kFewRows4) p.many = launch(most, 32 * kChunkWaves, 64, 256, 8, 1 << 30);
-  // Sums of few rows are laid out by sequence where that is less: a prompt in the batch has none.
-  const int seq_rows = few_seq_rows4(c, G, std::min(n->max_new, n->total_new));
-  if ((int64_t)seq_rows * S < n->total_new) {
-    p.few.part_seq_rows = seq_rows;
-    p.few.part_rows = seq_rows * S;
-  }
+  p.rows = f32 || most <= 16 ? 16 : 32;
+  if (f32) p.few = items(most, 16);
+  else if (G <= kFewRows4 && (S > 1 || most <= kFewRows4)) p.few = items(std::min<int64_t>(most, kFewRows4), p.rows);
+  p.splits = 1;
   size_t sums = 0;
-  for (const Cache4Launch* l : {&p.few, &p.many})
-    if (l->splits > 1) sums = std::max(sums, (size_t)l->splits * l->part_rows * n->num_q_heads);
+  if (p.few > 0) {
+    // As many workgroups as the chip holds.  Whole items, without the launch that joins parts, where two strips a wavefront are all there is, and for float32 prompts, whose
+    // items are many and alike.
+    if (tiles(p.rows, 32) > 2 * kWaves4 && !(f32 && most > kFewRows4 && p.few * c->num_kv_heads >= 4096))
+      p.workgroups = 256 * split_waves(D, p.rows / 16 * (f32 ? 3 : 1));
+    sums = (size_t)p.workgroups * 2 * p.rows;
+    const int64_t strips = ((int64_t)c->max_pages * c->page_size + 31) / 32 + 2;  // of an item, at most
+    while (p.few * c->num_kv_heads * (((strips - 1) >> p.unit) + 1) > 0x40000000ll && p.unit < 26) ++p.unit;
+  }
+  if (!f32 && most > kFewRows4) {
+    p.many = items(most, 32 * kChunkWaves);
+    // A workgroup a CU, of 8 tiles at least.
+    const int64_t all = tiles(32 * kChunkWaves, 64);
+    const int64_t per = std::max<int64_t>(((all * p.many * c->num_kv_heads + 255) / 256 + 7) / 8 * 8, 8);
+    p.splits = (int)std::max<int64_t>((all + per - 1) / per, 1);
+    p.per_split = (int)per;
+    if (p.splits > 1) sums = std::max(sums, (size_t)p.splits * n->total_new * n->num_q_heads);
+  }
   p.part_o = align_up(sums * sizeof(float));
-  p.bytes = align_up(p.part_o + sums * c->head_dim * sizeof(float));
+  p.bytes = align_up(p.part_o + sums * D * sizeof(float));
   return p;
 }
 static int check_cache4_attn(const sb_cache4* c, const sb_chunk* n, int32_t window, int32_t sinks) {
@@ -528,45 +712,51 @@ int sb_cache4_attn(const sb_cache4* c, const sb_chunk* n, int32_t window, int32_
   A.cache = make_paged(c);
   P.cache = PagedCache{nullptr, nullptr, c->page_table, c->num_pages, c->max_pages, c->page_size, A.cache.page_shift, c->num_kv_heads};
   const Cache4Plan plan = plan_cache4(c, n, window, sinks);
-  if (plan.few.splits > 1 || plan.many.splits > 1) {
+  if (plan.workgroups > 0 || plan.splits > 1) {
     if (!ws) { set_error("null argument"); return SB_ERR_INVALID_ARG; }
     P.part_lse = (float*)ws;
     P.part_o = (float*)((char*)ws + plan.part_o);
   }
   const bool f32 = c->dtype == SB_F32;
-  const int seq_rows = few_seq_rows4(c, P.G, std::min(P.max_new, P.T));
+  int seq_rows = few_seq_rows4(c, P.G, std::min(P.max_new, P.T));
+  if ((int64_t)seq_rows * P.S >= P.T) seq_rows = 0;  // (a prompt beside others has no parts of few rows)
   dim3 few_grid, many_grid, few_rows, all_rows;
-  if ((rc = grid_of(plan.few.items * P.Hkv * plan.few.splits, 64 * kWaves4, &few_grid)) != SB_OK ||
-      (rc = grid_of(plan.many.items * P.Hkv * plan.many.splits, 64 * kChunkWaves, &many_grid)) != SB_OK ||
-      (plan.many.splits > 1 && (rc = grid_of((int64_t)P.T * P.Hq, 256, &all_rows)) != SB_OK) ||
-      (plan.few.splits > 1 && (rc = grid_of((plan.few.part_seq_rows > 0 ? (int64_t)seq_rows * P.S : P.T) * P.Hq, 256, &few_rows)) != SB_OK))
+  if ((rc = grid_of(plan.workgroups > 0 ? plan.workgroups : plan.few * P.Hkv, 64 * kWaves4, &few_grid)) != SB_OK ||
+      (rc = grid_of(plan.many * P.Hkv * plan.splits, 64 * kChunkWaves, &many_grid)) != SB_OK || (plan.splits > 1 && (rc = grid_of((int64_t)P.T * P.Hq, 256, &all_rows)) != SB_OK) ||
+      (plan.workgroups > 0 && (rc = grid_of((seq_rows > 0 ? (int64_t)seq_rows * P.S : P.T) * P.Hq, 256, &few_rows)) != SB_OK))
     return rc;
   const hipStream_t st = (hipStream_t)stream;
   KernelTimer kt(K_CACHE_ATTN, st);
-  auto part = [&](const Cache4Launch& l, int from, int to) {
-    P.splits = l.splits; P.per_split = l.per_split; P.part_rows = l.part_rows; P.part_seq_rows = l.part_seq_rows;
-    P.rows_from = from; P.rows_to = to;
-  };
-  if (plan.many.items > 0) {
-    part(plan.many, plan.few.items > 0 ? kFewRows4 + 1 : 0, 0x7fffffff);
+  if (plan.many > 0) {
+    P.splits = plan.splits; P.per_split = plan.per_split; P.part_rows = P.T;
+    P.rows_from = plan.few > 0 ? kFewRows4 + 1 : 0;
+    P.rows_to = 0x7fffffff;
     if (c->head_dim == 128) hipLaunchKernelGGL((cache4_chunk_kernel<128>), many_grid, dim3(64 * kChunkWaves), 0, st, A);
     else hipLaunchKernelGGL((cache4_chunk_kernel<64>), many_grid, dim3(64 * kChunkWaves), 0, st, A);
     SB_LAUNCH_CHECK("cache4_chunk_kernel");
     if (P.splits > 1 && (rc = launch_cache_merge(P, c->head_dim, c->dtype, all_rows, 0, st)) != SB_OK) return rc;
   }
-  if (plan.few.items > 0) {
-    part(plan.few, 0, f32 ? 0x7fffffff : kFewRows4);
+  if (plan.few > 0) {
+    P.splits = plan.workgroups > 0 ? 0 : 1;
+    A.unit = plan.unit;
+    P.rows_to = f32 ? 0x7fffffff : kFewRows4;
     auto launch = [&](auto ty, auto d, auto nt, auto pieces) {
-      hipLaunchKernelGGL((cache4_split_kernel<decltype(ty), decltype(d)::value, decltype(nt)::value, decltype(pieces)::value>), few_grid, dim3(64 * kWaves4), 0, st, A);
+      typedef decltype(ty) Type;
+      constexpr int DD = decltype(d)::value, NT = decltype(nt)::value;
+      hipLaunchKernelGGL((cache4_split_kernel<Type, DD, NT, decltype(pieces)::value>), few_grid, dim3(64 * kWaves4), 0, st, A);
+      SB_LAUNCH_CHECK("cache4_split_kernel");
+      if (plan.workgroups > 0) {
+        hipLaunchKernelGGL((cache4_join_kernel<Type, DD, 16 * NT>), few_rows, dim3(256), 0, st, A, plan.workgroups, seq_rows);
+        SB_LAUNCH_CHECK("cache4_join_kernel");
+      }
+      return (int)SB_OK;
     };
     auto with_d = [&](auto ty, auto nt, auto pieces) {
-      if (c->head_dim == 128) launch(ty, std::integral_constant<int, 128>(), nt, pieces); else launch(ty, std::integral_constant<int, 64>(), nt, pieces);
+      return c->head_dim == 128 ? launch(ty, std::integral_constant<int, 128>(), nt, pieces) : launch(ty, std::integral_constant<int, 64>(), nt, pieces);
     };
-    if (f32) with_d(float(), std::integral_constant<int, 1>(), std::integral_constant<int, 3>());
-    else if (plan.nt == 1) with_d(bf16(), std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
-    else with_d(bf16(), std::integral_constant<int, 2>(), std::integral_constant<int, 1>());
-    SB_LAUNCH_CHECK("cache4_split_kernel");
-    if (P.splits > 1) return launch_cache_merge(P, c->head_dim, c->dtype, few_rows, P.part_seq_rows > 0 ? seq_rows : 0, st);
+    if (f32) return with_d(float(), std::integral_constant<int, 1>(), std::integral_constant<int, 3>());
+    if (plan.rows == 16) return with_d(bf16(), std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
+    return with_d(bf16(), std::integral_constant<int, 2>(), std::integral_constant<int, 1>());
   }
   return SB_OK;
 }
