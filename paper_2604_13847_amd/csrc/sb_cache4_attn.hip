@@ -46,15 +46,104 @@ struct Strip {
   __device__ inline float k_step(int b, int v, int c) const { return step_at(ks[b][(v * GROUPS + c) / 2], c); }
   __device__ inline float v_step(int b, int v, int c) const { return step_at(vs[b][(v * GROUPS + c) / 2], c); }
 };
-template <int N> __device__ inline void load_words(unsigned* to, const unsigned char* from) {  // N x 4 bytes, so aligned
-  typedef struct alignas(N >= 4 ? 16 : 4 * N) { unsigned x[N >= 4 ? 4 : N]; } Piece;
-#pragma unroll
-  for (int i = 0; i < (N + 3) / 4; ++i) {
-    const Piece y = ((const Piece*)from)[i];
-#pragma unroll
-    for (int e = 0; e < (N >= 4 ? 4 : N); ++e) to[4 * i + e] = y.x[e];
+// A strip on its way: a wavefront's own place in LDS, filled by asynchronous loads of 16 bytes (codes) and 4 bytes (steps) a lane, each lane's bytes behind the lane's before it.
+//   head_dim 128: K in two loads of 16 rows, 16-byte piece b of row r at 4 r + (b ^ r / 4), so that the 16 rows of an operand lie in different banks; V likewise, row r at
+//   16 (r % 4) + 4 (r / 4), so that the four rows that a slot's quarters read lie side by side; the steps of K, and of V, in one load of 32 rows each
+//   head_dim 64: K and V in one load of 32 rows each, in order; the steps of both in one
+template <int D>
+struct StripLoader {
+  static constexpr int LOADS = D == 128 ? 6 : 3, CODES = 32 * D / 2, STEPS = 32 * D / 16, BYTES = 2 * CODES + 2 * STEPS;
+  unsigned k_at, v_at, step_at_;  // bytes from the first row of the lane's 16 to what the lane loads
+  bool upper;                     // the lane's rows are the strip's second 16 (head_dim 128: of the steps)
+  __device__ inline void init(int lane) {
+    if constexpr (D == 128) {
+      const int r = lane >> 2, r_v = (r & 3) * 4 + (r >> 2);
+      k_at = r * 64 + 16 * ((lane & 3) ^ (r >> 2));
+      v_at = r_v * 64 + 16 * (lane & 3);
+      step_at_ = (lane & 31) * 4;
+    } else {
+      k_at = v_at = (lane & 31) * 16;
+      step_at_ = (lane & 15) * 4;
+    }
+    upper = lane >= 32;
   }
-}
+  static __device__ __attribute__((always_inline)) inline void issue16(unsigned off, const void* base, unsigned slot) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %2" : : "v"(off), "s"(slot), "s"(base) : "memory", "m0");
+  }
+  static __device__ __attribute__((always_inline)) inline void issue16(const void* from, unsigned slot) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(slot) : "memory", "m0");
+  }
+  static __device__ __attribute__((always_inline)) inline void issue4(const void* from, unsigned slot) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 4\n\tglobal_load_lds_dword %0, off" : : "v"(from), "s"(slot) : "memory", "m0");
+  }
+  // row0, row1: first rows of the strip's two 16 in the cache's arrays; slot: where in LDS (both wave-uniform)
+  __device__ __attribute__((always_inline)) inline void issue(const PagedCache4& c, uint64_t row0, uint64_t row1, unsigned slot, int lane) const {
+    if constexpr (D == 128) {
+      issue16(k_at, c.k + row0 * 64, slot);
+      issue16(k_at, c.k + row1 * 64, slot + CODES / 2);
+      issue16(v_at, c.v + row0 * 64, slot + CODES);
+      issue16(v_at, c.v + row1 * 64, slot + CODES + CODES / 2);
+      const uint64_t at = (upper ? row1 : row0) * 8 + step_at_;
+      issue4((const char*)c.k_step + at, slot + 2 * CODES);
+      issue4((const char*)c.v_step + at, slot + 2 * CODES + STEPS);
+    } else {
+      const uint64_t at = (upper ? row1 : row0) * 32 + k_at;
+      issue16(c.k + at, slot);
+      issue16(c.v + at, slot + CODES);
+      issue4((const char*)(upper ? c.v_step : c.k_step) + ((lane & 16) ? row1 : row0) * 4 + step_at_, slot + 2 * CODES);
+    }
+  }
+};
+template <int D>
+struct StripReader {
+  static constexpr int GROUPS = D / 32, CODES = StripLoader<D>::CODES, STEPS = StripLoader<D>::STEPS;
+  unsigned k_at, v_at, s_at;
+  __device__ inline void init(int l16, int qd) {
+    if constexpr (D == 128) {
+      k_at = l16 * 64 + 16 * (qd ^ (l16 >> 2));
+      v_at = CODES + qd * 64 + l16 * 4;  // row 4 qd + j: at 64 (4 j + qd)
+    } else {
+      k_at = l16 * 32 + qd * 8;
+      v_at = CODES + qd * 128 + l16 * 2;
+    }
+    s_at = 2 * CODES + qd * 4 * GROUPS * 2;
+  }
+  template <typename V> static __device__ __attribute__((always_inline)) inline V at(unsigned a) { return *(const V __attribute__((address_space(3)))*)(uintptr_t)a; }
+  __device__ __attribute__((always_inline)) inline void keys(Strip<D>& s, unsigned slot) const {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      if constexpr (D == 128) {
+        const u32x4 y = at<u32x4>(slot + k_at + b * (CODES / 2));
+#pragma unroll
+        for (int c = 0; c < GROUPS; ++c) s.k[b][c] = y[c];
+      } else {
+        const u32x2 y = at<u32x2>(slot + k_at + b * (CODES / 2));
+#pragma unroll
+        for (int c = 0; c < GROUPS; ++c) s.k[b][c] = y[c];
+      }
+      steps(s.ks[b], slot + s_at + b * (STEPS / 2));
+    }
+  }
+  __device__ __attribute__((always_inline)) inline void values(Strip<D>& s, unsigned slot) const {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (D == 128) s.v[4 * b + j] = at<unsigned>(slot + v_at + b * (CODES / 2) + 256 * j);
+        else s.v[4 * b + j] = at<unsigned short>(slot + v_at + b * (CODES / 2) + 32 * j);
+      }
+      steps(s.vs[b], slot + s_at + STEPS + b * (STEPS / 2));
+    }
+  }
+  static __device__ __attribute__((always_inline)) inline void steps(unsigned (&to)[2 * GROUPS], unsigned from) {
+#pragma unroll
+    for (int i = 0; i < GROUPS / 2; ++i) {
+      const u32x4 y = at<u32x4>(from + 16 * i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) to[4 * i + e] = y[e];
+    }
+  }
+};
 
 // The work of few rows as one stream of strips: sequence by sequence, KV head by head, tile of rows by tile, the strips that any row of the sequence sees.  (A tile's own strips are a
 // part of these, from the first on.)  Every workgroup takes as many neighbouring strips as the others, whatever the lengths, which only the device knows; where that
@@ -139,19 +228,26 @@ struct Stream {
   }
 };
 
-// An item is up to 16 NT flattened rows of a KV head; a wavefront takes every NW-th of the workgroup's strips of it, straight into registers, the next one's loads on their way while one
-// is worked on.  PIECES: a query and a probability as that many bfloat16 numbers.
+// An item is up to 16 NT flattened rows of a KV head; a wavefront takes every NW-th of the workgroup's strips of it through its own ring in LDS, without any barrier, the next three on their
+// way while one is worked on.  PIECES: a query and a probability as that many bfloat16 numbers.
 constexpr int kWaves4 = 4;
-constexpr int split_waves(int D, int operands) { return (D == 64 ? 2 : 1) + (operands == 1); }  // of a SIMD, by registers
+constexpr int split_waves(int D, int operands) { return D == 128 ? (operands == 2 ? 1 : 2) : operands == 1 ? 4 : 3; }  // of a SIMD, by registers; the rings of as many workgroups fit a CU
 template <typename T, int D, int NT, int PIECES>
 __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(split_waves(D, NT * PIECES)))) void cache4_split_kernel(Cache4Params A) {
   const WindowParams& P = A.w;
   constexpr int NW = kWaves4, ROWS = 16 * NT, GROUPS = D / 32, TILES = D / 16;
-  constexpr int OUT_P = D + 4;
+  constexpr int OUT_P = D + 4;  // floats from row to row of a wavefront's sums in LDS
+  constexpr int STAGES = 4, LOADS = StripLoader<D>::LOADS, SLOT = StripLoader<D>::BYTES;
   constexpr float kLazy = 8.0f;
-  __shared__ float sums[NW][ROWS][OUT_P];
+  __shared__ __attribute__((aligned(1024))) char ring[NW][STAGES * SLOT];
+  static_assert(ROWS * OUT_P * 4 <= STAGES * SLOT && STAGES * SLOT % 16 == 0, "the sums take the strips' place");
   __shared__ float stats[2][NW][ROWS];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l16 = lane & 15, qd = lane >> 4;
+  const unsigned ring0 = __builtin_amdgcn_readfirstlane((int)lds_offset(ring[wave]));
+  StripLoader<D> loader;
+  loader.init(lane);
+  StripReader<D> reader;
+  reader.init(l16, qd);
   Stream<ROWS> stream;
   const int share = stream.share(A, gridDim.x, NW >> A.unit > 0 ? NW >> A.unit : 1, lane);
   const int64_t x_last = (int64_t)share * (blockIdx.x + 1);
@@ -193,27 +289,16 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
         }
       }
     };
-    const unsigned at_k = l16 * (D / 2) + qd * (D / 8), at_v = 4 * qd * (D / 2) + l16 * (D / 32), at_s = qd * 4 * GROUPS * 2;
-    const unsigned char* const k_step = (const unsigned char*)A.cache.k_step;
-    const unsigned char* const v_step = (const unsigned char*)A.cache.v_step;
-    auto load = [&](Strip<D>& s, int x) __attribute__((always_inline)) {  // strip x of this wavefront
+    auto issue = [&](int x) __attribute__((always_inline)) {  // strip x of this wavefront
       const int u = __builtin_amdgcn_readfirstlane(32 * strips.at(begin + wave + NW * x));
+      uint64_t row[2];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const unsigned page = (unsigned)__builtin_amdgcn_readlane(where[b], x - x0);
         // (16 rows of a page, all of them in memory, whether or not they have been written)
-        const uint64_t row = ((uint64_t)(page * (uint64_t)A.cache.Hkv + g) << A.cache.page_shift) + ((u + 16 * b) & (A.cache.page_size - 1));
-        const uint64_t code = row * (D / 2), step = row * (GROUPS * 2);
-        load_words<GROUPS>(s.k[b], A.cache.k + code + at_k);
-        load_words<2 * GROUPS>(s.ks[b], k_step + step + at_s);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const unsigned char* const from = A.cache.v + code + at_v + j * (D / 2);
-          if constexpr (D == 128) s.v[4 * b + j] = *(const unsigned*)from;
-          else s.v[4 * b + j] = *(const unsigned short*)from;
-        }
-        load_words<2 * GROUPS>(s.vs[b], v_step + step + at_s);
+        row[b] = ((uint64_t)(page * (uint64_t)A.cache.Hkv + g) << A.cache.page_shift) + ((u + 16 * b) & (A.cache.page_size - 1));
       }
+      loader.issue(A.cache, row[0], row[1], ring0 + (x & (STAGES - 1)) * SLOT, lane);
     };
 
     // B operand of the scores: column = row l16 of tile nt
@@ -252,7 +337,10 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
       l[nt] = 0.f;
     }
 
-    auto work = [&](Strip<D>& s, int x) __attribute__((always_inline)) {
+    auto work = [&](int x) __attribute__((always_inline)) {
+      Strip<D> s;
+      const unsigned slot = ring0 + (x & (STAGES - 1)) * SLOT;
+      reader.keys(s, slot);
       const int u0 = __builtin_amdgcn_readfirstlane(32 * strips.at(begin + wave + NW * x));
       const unsigned have = (1u << __builtin_amdgcn_readlane(there[0], x - x0)) - 1 | ((1u << __builtin_amdgcn_readlane(there[1], x - x0)) - 1) << 16;  // keys that exist
       float sc[NT][2][4];
@@ -275,6 +363,7 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
           }
         }
       }
+      reader.values(s, slot);
       if (u0 + 31 > ta || (last - u0 >= P.window && u0 + 31 >= P.sinks) || have != ~0u) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -367,17 +456,29 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
       }
     };
 
-    Strip<D> s[2];
-    for (int from = 0; from < turns; from += 64) {
+    // the query operands must have landed before the strips' loads start: from there on only those are in flight, and waited for by hand
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int c = 0; c < GROUPS; ++c)
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) asm volatile("" : "+v"(qf[nt][c][p]));
+    for (int from = 0; from < turns; from += 64) {  // (a look-up's worth)
       const int to = min(from + 64, turns);
       look_up(from);
-      load(s[0], from);
-      for (int x = from; x < to; x += 2) {
-        if (x + 1 < to) load(s[1], x + 1);
-        work(s[0], x);
-        if (x + 1 >= to) break;
-        if (x + 2 < to) load(s[0], x + 2);
-        work(s[1], x + 1);
+      asm volatile("s_waitcnt vmcnt(0)" : "+v"(where[0]), "+v"(where[1]), "+v"(there[0]), "+v"(there[1]) : : "memory");
+#pragma unroll
+      for (int i = 0; i < STAGES - 1; ++i)
+        if (from + i < to) issue(from + i);
+      for (int x = from; x < to; ++x) {
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the strip before has been read: its place is free
+        if (x + STAGES - 1 < to) issue(x + STAGES - 1);
+        const int behind = to - 1 - x;  // strips on their way behind this one
+        if (behind >= 3) wait_vmcnt<3 * LOADS>();
+        else if (behind == 2) wait_vmcnt<2 * LOADS>();
+        else if (behind == 1) wait_vmcnt<LOADS>();
+        else wait_vmcnt<0>();
+        work(x);
       }
     }
     // the wavefronts' sums, through LDS
@@ -386,7 +487,7 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
       l[nt] += __shfl_xor(l[nt], 16, 64);
       l[nt] += __shfl_xor(l[nt], 32, 64);
 #pragma unroll
-      for (int d = 0; d < TILES; ++d) *(f32x4*)&sums[wave][16 * nt + l16][16 * d + 4 * qd] = acc[nt][d];
+      for (int d = 0; d < TILES; ++d) *(f32x4*)((float*)ring[wave] + (16 * nt + l16) * OUT_P + 16 * d + 4 * qd) = acc[nt][d];
       if (qd == 0) { stats[0][wave][16 * nt + l16] = top[nt] * P.scale_log2e; stats[1][wave][16 * nt + l16] = l[nt]; }
     }
     __syncthreads();
@@ -402,7 +503,7 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
         if (stats[1][w][r] == 0.f) continue;
         const float f = fast_exp2(stats[0][w][r] - best);
         sum += f * stats[1][w][r];
-        x += f * *(const f32x4*)&sums[w][r][4 * c];
+        x += f * *(const f32x4*)((const float*)ring[w] + r * OUT_P + 4 * c);
       }
       const int j = token(m0 + r), hh = g * P.G + m0 + r - j * P.G;
       const int64_t row = (int64_t)(t.row0 + j) * P.Hq + hh;
