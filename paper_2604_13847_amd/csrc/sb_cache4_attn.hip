@@ -34,18 +34,13 @@ __device__ inline Rsrc resource(const void* base, unsigned bytes) { return __bui
 template <int SEL> __device__ inline f32x2 numbers(unsigned x) { return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, 1.0f, SEL); }
 __device__ inline float step_at(unsigned pair, int i) { return __uint_as_float(i & 1 ? pair & 0xffff0000u : pair << 16); }
 
-// A strip: 32 keys, as a lane holds them.  Matrix instructions 16x16x32: lane = (l16, qd).
-//   scores S^T = K Q^T: A row = key 16 b + l16, slots of quarter qd = elements 32 c + 8 qd + (0 .. 7); C row 4 qd + v = key 16 b + 4 qd + v, column l16 = query
+// Matrix instructions 16x16x32 over a strip of 32 keys: lane = (l16, qd).
+//   scores S^T = K Q^T: A row = key 16 b + l16, slots of quarter qd = elements 32 c + 8 qd + (0 .. 7); C row 4 qd + v = key 16 b + 4 qd + v, column l16
 //   output O^T += V^T P^T: slot j of quarter qd = key 16 (j / 4) + 4 qd + j % 4, which is where the scores are; A row = element 16 t + l16 of tile t
-template <int D>
-struct Strip {
-  static constexpr int GROUPS = D / 32;
-  unsigned k[2][GROUPS];          // [b][c]
-  unsigned v[8];                  // word l16 of slot j's key (head_dim 64: 16 bits)
-  unsigned ks[2][2 * GROUPS], vs[2][2 * GROUPS];  // steps of keys 16 b + 4 qd + (0 .. 3): pairs of bfloat16
-  __device__ inline float k_step(int b, int v, int c) const { return step_at(ks[b][(v * GROUPS + c) / 2], c); }
-  __device__ inline float v_step(int b, int v, int c) const { return step_at(vs[b][(v * GROUPS + c) / 2], c); }
-};
+// A tile of R = 16 / PARTS rows takes all 16 columns: row l16 / PARTS, PARTS times, each time for GROUPS / PARTS of the groups of 32 elements.  A column's query is zero in the groups
+// that are not its own, so that one chain of products leaves every column with its own group's share of the score, to be multiplied by that group's step and added up over
+// the columns of a row; and the probabilities that it multiplies with its own group's steps are right for that group's tiles of the output, the others of which are not used.
+// So four rows (a token of four heads) cost a step's multiplication once and not four times.
 // A strip on its way: a wavefront's own place in LDS, filled by asynchronous loads of 16 bytes (codes) and 4 bytes (steps) a lane, each lane's bytes behind the lane's before it.
 //   head_dim 128: K in two loads of 16 rows, 16-byte piece b of row r at 4 r + (b ^ r / 4), so that the 16 rows of an operand lie in different banks; V likewise, row r at
 //   16 (r % 4) + 4 (r / 4), so that the four rows that a slot's quarters read lie side by side; the steps of K, and of V, in one load of 32 rows each
@@ -94,11 +89,12 @@ struct StripLoader {
     }
   }
 };
-template <int D>
+// What a lane reads of a strip.  OWN: the lane's own groups, part OWN + (0 .. OWN - 1).
+template <int D, int OWN>
 struct StripReader {
   static constexpr int GROUPS = D / 32, CODES = StripLoader<D>::CODES, STEPS = StripLoader<D>::STEPS;
   unsigned k_at, v_at, s_at;
-  __device__ inline void init(int l16, int qd) {
+  __device__ inline void init(int l16, int qd, int part) {
     if constexpr (D == 128) {
       k_at = l16 * 64 + 16 * (qd ^ (l16 >> 2));
       v_at = CODES + qd * 64 + l16 * 4;  // row 4 qd + j: at 64 (4 j + qd)
@@ -106,44 +102,65 @@ struct StripReader {
       k_at = l16 * 32 + qd * 8;
       v_at = CODES + qd * 128 + l16 * 2;
     }
-    s_at = 2 * CODES + qd * 4 * GROUPS * 2;
+    s_at = 2 * CODES + qd * 4 * GROUPS * 2 + part * OWN * 2;
   }
   template <typename V> static __device__ __attribute__((always_inline)) inline V at(unsigned a) { return *(const V __attribute__((address_space(3)))*)(uintptr_t)a; }
-  __device__ __attribute__((always_inline)) inline void keys(Strip<D>& s, unsigned slot) const {
+  __device__ __attribute__((always_inline)) inline void keys(unsigned (&k)[2][GROUPS], unsigned slot) const {  // [b][c]
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      if constexpr (D == 128) {
-        const u32x4 y = at<u32x4>(slot + k_at + b * (CODES / 2));
+      typedef typename std::conditional<D == 128, u32x4, u32x2>::type Piece;
+      const Piece y = at<Piece>(slot + k_at + b * (CODES / 2));
 #pragma unroll
-        for (int c = 0; c < GROUPS; ++c) s.k[b][c] = y[c];
-      } else {
-        const u32x2 y = at<u32x2>(slot + k_at + b * (CODES / 2));
-#pragma unroll
-        for (int c = 0; c < GROUPS; ++c) s.k[b][c] = y[c];
-      }
-      steps(s.ks[b], slot + s_at + b * (STEPS / 2));
+      for (int c = 0; c < GROUPS; ++c) k[b][c] = y[c];
     }
   }
-  __device__ __attribute__((always_inline)) inline void values(Strip<D>& s, unsigned slot) const {
+  __device__ __attribute__((always_inline)) inline void values(unsigned (&v)[8], unsigned slot) const {  // word l16 of slot j's key (head_dim 64: 16 bits)
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if constexpr (D == 128) s.v[4 * b + j] = at<unsigned>(slot + v_at + b * (CODES / 2) + 256 * j);
-        else s.v[4 * b + j] = at<unsigned short>(slot + v_at + b * (CODES / 2) + 32 * j);
+        if constexpr (D == 128) v[4 * b + j] = at<unsigned>(slot + v_at + b * (CODES / 2) + 256 * j);
+        else v[4 * b + j] = at<unsigned short>(slot + v_at + b * (CODES / 2) + 32 * j);
       }
-      steps(s.vs[b], slot + s_at + STEPS + b * (STEPS / 2));
-    }
   }
-  static __device__ __attribute__((always_inline)) inline void steps(unsigned (&to)[2 * GROUPS], unsigned from) {
+  // of keys 16 b + 4 qd + v: steps of the lane's own groups
+  __device__ __attribute__((always_inline)) inline void steps(float (&to)[2][4][OWN], unsigned slot, bool of_values) const {
 #pragma unroll
-    for (int i = 0; i < GROUPS / 2; ++i) {
-      const u32x4 y = at<u32x4>(from + 16 * i);
+    for (int b = 0; b < 2; ++b) {
+      const unsigned from = slot + s_at + (of_values ? STEPS : 0) + b * (STEPS / 2);
+      if constexpr (OWN == 1) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) to[4 * i + e] = y[e];
+        for (int v = 0; v < 4; ++v) to[b][v][0] = __uint_as_float((unsigned)at<unsigned short>(from + v * GROUPS * 2) << 16);
+      } else if constexpr (OWN == GROUPS) {  // all of them: 16 bytes at a time
+        unsigned x[2 * GROUPS];
+#pragma unroll
+        for (int i = 0; i < GROUPS / 2; ++i) {
+          const u32x4 y = at<u32x4>(from + 16 * i);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[4 * i + e] = y[e];
+        }
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+#pragma unroll
+          for (int o = 0; o < OWN; ++o) to[b][v][o] = step_at(x[(v * GROUPS + o) / 2], o);
+      } else {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const unsigned y = at<unsigned>(from + v * GROUPS * 2);
+#pragma unroll
+          for (int o = 0; o < OWN; ++o) to[b][v][o] = step_at(y, o);
+        }
+      }
     }
   }
 };
+// over the columns of a row: lanes that differ in the lowest bits.  (The same in all of them, bit for bit.)
+template <int PARTS> __device__ inline float add_parts(float x) {
+  auto swapped = [](float y, auto ctrl) { return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(y), decltype(ctrl)::value, 0xf, 0xf, false)); };
+  if constexpr (PARTS >= 2) x += swapped(x, std::integral_constant<int, 0xb1>());  // 1, 0, 3, 2
+  if constexpr (PARTS >= 4) x += swapped(x, std::integral_constant<int, 0x4e>());  // 2, 3, 0, 1
+  return x;
+}
 
 // The work of few rows as one stream of strips: sequence by sequence, KV head by head, tile of rows by tile, the strips that any row of the sequence sees.  (A tile's own strips are a
 // part of these, from the first on.)  Every workgroup takes as many neighbouring strips as the others, whatever the lengths, which only the device knows; where that
@@ -228,26 +245,31 @@ struct Stream {
   }
 };
 
-// An item is up to 16 NT flattened rows of a KV head; a wavefront takes every NW-th of the workgroup's strips of it through its own ring in LDS, without any barrier, the next three on their
+// An item is up to 16 NT / PARTS flattened rows of a KV head; a wavefront takes every NW-th of the workgroup's strips of it through its own ring in LDS, without any barrier, the next ones on their
 // way while one is worked on.  PIECES: a query and a probability as that many bfloat16 numbers.
 constexpr int kWaves4 = 4;
-constexpr int split_waves(int D, int operands) { return D == 128 ? (operands == 2 ? 1 : 2) : operands == 1 ? 4 : 3; }  // of a SIMD, by registers; the rings of as many workgroups fit a CU
-template <typename T, int D, int NT, int PIECES>
-__global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(split_waves(D, NT * PIECES)))) void cache4_split_kernel(Cache4Params A) {
+// Wavefronts of a SIMD, by registers, and stages of a ring, so that the rings of as many workgroups fit a CU.  64 sequences of 500 to 32768 tokens, 32/8 heads: 150 us with two wavefronts
+// and four stages, 136 with three and two (124 without the arithmetic, 89 without the loads), 139 with four, which spill.
+constexpr int split_waves(int D, int rows, int pieces) { return D == 64 ? (pieces == 3 ? 3 : rows == 32 ? 2 : 4) : rows == 32 ? 1 : rows == 4 || (rows == 8 && pieces == 1) ? 3 : 2; }
+constexpr int split_stages(int D, int rows, int pieces) { return D == 128 && split_waves(D, rows, pieces) == 3 ? 2 : 4; }
+template <typename T, int D, int PARTS, int NT, int PIECES>
+__global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(split_waves(D, 16 * NT / PARTS, PIECES)))) void cache4_split_kernel(Cache4Params A) {
   const WindowParams& P = A.w;
-  constexpr int NW = kWaves4, ROWS = 16 * NT, GROUPS = D / 32, TILES = D / 16;
+  constexpr int NW = kWaves4, R = 16 / PARTS, ROWS = R * NT, GROUPS = D / 32, OWN = GROUPS / PARTS, TILES = D / 16;
+  static_assert(OWN * PARTS == GROUPS, "every column has groups of its own");
   constexpr int OUT_P = D + 4;  // floats from row to row of a wavefront's sums in LDS
-  constexpr int STAGES = 4, LOADS = StripLoader<D>::LOADS, SLOT = StripLoader<D>::BYTES;
+  constexpr int STAGES = split_stages(D, ROWS, PIECES), LOADS = StripLoader<D>::LOADS, SLOT = StripLoader<D>::BYTES;
   constexpr float kLazy = 8.0f;
   __shared__ __attribute__((aligned(1024))) char ring[NW][STAGES * SLOT];
   static_assert(ROWS * OUT_P * 4 <= STAGES * SLOT && STAGES * SLOT % 16 == 0, "the sums take the strips' place");
   __shared__ float stats[2][NW][ROWS];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l16 = lane & 15, qd = lane >> 4;
+  const int part = l16 % PARTS, r16 = l16 / PARTS;
   const unsigned ring0 = __builtin_amdgcn_readfirstlane((int)lds_offset(ring[wave]));
   StripLoader<D> loader;
   loader.init(lane);
-  StripReader<D> reader;
-  reader.init(l16, qd);
+  StripReader<D, OWN> reader;
+  reader.init(l16, qd, part);
   Stream<ROWS> stream;
   const int share = stream.share(A, gridDim.x, NW >> A.unit > 0 ? NW >> A.unit : 1, lane);
   const int64_t x_last = (int64_t)share * (blockIdx.x + 1);
@@ -301,12 +323,12 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
       loader.issue(A.cache, row[0], row[1], ring0 + (x & (STAGES - 1)) * SLOT, lane);
     };
 
-    // B operand of the scores: column = row l16 of tile nt
+    // B operand of the scores: column = row r16 of tile nt, zero in groups that are not the column's own
     bf16x8 qf[NT][GROUPS][PIECES];
     int pos[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int m = min(m0 + 16 * nt + l16, rows - 1), i = token(m), h = g * P.G + m - i * P.G;
+      const int m = min(m0 + R * nt + r16, rows - 1), i = token(m), h = g * P.G + m - i * P.G;
       pos[nt] = t.pos0 + i;
       const T* const q = (const T*)P.q + ((int64_t)(t.row0 + i) * P.Hq + h) * D + 8 * qd;
 #pragma unroll
@@ -324,6 +346,9 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
             }
           }
         }
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p)
+          if (PARTS > 1 && part != c / OWN) qf[nt][c][p] = zero_bf16x8();
       }
     }
     f32x4 acc[NT][TILES];
@@ -338,32 +363,41 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
     }
 
     auto work = [&](int x) __attribute__((always_inline)) {
-      Strip<D> s;
       const unsigned slot = ring0 + (x & (STAGES - 1)) * SLOT;
-      reader.keys(s, slot);
+      unsigned keys[2][GROUPS], values[8];
+      float k_step[2][4][OWN], v_step[2][4][OWN];
+      reader.keys(keys, slot);
+      reader.steps(k_step, slot, false);
       const int u0 = __builtin_amdgcn_readfirstlane(32 * strips.at(begin + wave + NW * x));
       const unsigned have = (1u << __builtin_amdgcn_readlane(there[0], x - x0)) - 1 | ((1u << __builtin_amdgcn_readlane(there[1], x - x0)) - 1) << 16;  // keys that exist
       float sc[NT][2][4];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
+        f32x4 y[NT][OWN];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int v = 0; v < 4; ++v) sc[nt][b][v] = 0.f;
+          for (int o = 0; o < OWN; ++o) y[nt][o] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < GROUPS; ++c) {
-          const bf16x8 op = levels8(s.k[b][c]);
+          const bf16x8 op = levels8(keys[b][c]);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            f32x4 y = {0.f, 0.f, 0.f, 0.f};
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int p = PIECES - 1; p >= 0; --p) y = mfma16(op, qf[nt][c][p], y);
-#pragma unroll
-            for (int v = 0; v < 4; ++v) sc[nt][b][v] = c == 0 ? y[v] * s.k_step(b, v, c) : __builtin_fmaf(y[v], s.k_step(b, v, c), sc[nt][b][v]);
-          }
+            for (int p = PIECES - 1; p >= 0; --p) y[nt][c % OWN] = mfma16(op, qf[nt][c][p], y[nt][c % OWN]);
         }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            float z = y[nt][0][v] * k_step[b][v][0];
+#pragma unroll
+            for (int o = 1; o < OWN; ++o) z = __builtin_fmaf(y[nt][o][v], k_step[b][v][o], z);
+            sc[nt][b][v] = add_parts<PARTS>(z);
+          }
       }
-      reader.values(s, slot);
+      reader.values(values, slot);
+      reader.steps(v_step, slot, true);
       if (u0 + 31 > ta || (last - u0 >= P.window && u0 + 31 >= P.sinks) || have != ~0u) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -379,12 +413,11 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int v = 0; v < 4; ++v)
-            if (!(have >> (16 * b + 4 * qd + v) & 1)) {
-              if constexpr (GROUPS == 4) s.vs[b][2 * v] = s.vs[b][2 * v + 1] = 0;
-              else s.vs[b][v] = 0;
-            }
+#pragma unroll
+            for (int o = 0; o < OWN; ++o)
+              if (!(have >> (16 * b + 4 * qd + v) & 1)) v_step[b][v][o] = 0.f;
       }
-      bf16x8 w[NT][GROUPS][PIECES];
+      bf16x8 w[NT][OWN][PIECES];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float mx = -__builtin_inff();
@@ -418,12 +451,12 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
             const float e = fast_exp2(__builtin_fmaf(sc[nt][b][v], P.scale_log2e, neg[nt]));
             l[nt] += e;
 #pragma unroll
-            for (int c = 0; c < GROUPS; ++c) {
-              float y = e * s.v_step(b, v, c);
+            for (int o = 0; o < OWN; ++o) {
+              float y = e * v_step[b][v][o];
 #pragma unroll
               for (int p = 0; p < PIECES; ++p) {
-                w[nt][c][p][4 * b + v] = (bf16)y;
-                y -= (float)w[nt][c][p][4 * b + v];
+                w[nt][o][p][4 * b + v] = (bf16)y;
+                y -= (float)w[nt][o][p][4 * b + v];
               }
             }
           }
@@ -432,7 +465,7 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
       unsigned even[4], odd[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const unsigned a = s.v[2 * j], b = s.v[2 * j + 1];
+        const unsigned a = values[2 * j], b = values[2 * j + 1];
         even[j] = (a & 0x0f0f0f0fu) | (b << 4 & 0xf0f0f0f0u);
         odd[j] = (a >> 4 & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u);
       }
@@ -448,7 +481,7 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int p = PIECES - 1; p >= 0; --p) acc[nt][TT] = mfma16(op, w[nt][TT / 2][p], acc[nt][TT]);
+          for (int p = PIECES - 1; p >= 0; --p) acc[nt][TT] = mfma16(op, w[nt][TT / 2 % OWN][p], acc[nt][TT]);
       };
       tile(std::integral_constant<int, 0>()); tile(std::integral_constant<int, 1>()); tile(std::integral_constant<int, 2>()); tile(std::integral_constant<int, 3>());
       if constexpr (D == 128) {
@@ -474,9 +507,9 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
         asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the strip before has been read: its place is free
         if (x + STAGES - 1 < to) issue(x + STAGES - 1);
         const int behind = to - 1 - x;  // strips on their way behind this one
-        if (behind >= 3) wait_vmcnt<3 * LOADS>();
-        else if (behind == 2) wait_vmcnt<2 * LOADS>();
-        else if (behind == 1) wait_vmcnt<LOADS>();
+        if (STAGES == 4 && behind >= 3) wait_vmcnt<3 * LOADS>();
+        else if (STAGES == 4 && behind == 2) wait_vmcnt<2 * LOADS>();
+        else if (behind >= 1) wait_vmcnt<LOADS>();
         else wait_vmcnt<0>();
         work(x);
       }
@@ -487,8 +520,9 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
       l[nt] += __shfl_xor(l[nt], 16, 64);
       l[nt] += __shfl_xor(l[nt], 32, 64);
 #pragma unroll
-      for (int d = 0; d < TILES; ++d) *(f32x4*)((float*)ring[wave] + (16 * nt + l16) * OUT_P + 16 * d + 4 * qd) = acc[nt][d];
-      if (qd == 0) { stats[0][wave][16 * nt + l16] = top[nt] * P.scale_log2e; stats[1][wave][16 * nt + l16] = l[nt]; }
+      for (int d = 0; d < TILES; ++d)  // (what is right of a column)
+        if (PARTS == 1 || part == d / 2 / OWN) *(f32x4*)((float*)ring[wave] + (R * nt + r16) * OUT_P + 16 * d + 4 * qd) = acc[nt][d];
+      if (qd == 0 && part == 0) { stats[0][wave][R * nt + r16] = top[nt] * P.scale_log2e; stats[1][wave][R * nt + r16] = l[nt]; }
     }
     __syncthreads();
     constexpr int LANES = D / 4;
@@ -534,14 +568,17 @@ __global__ __launch_bounds__(256) void cache4_join_kernel(Cache4Params A, int wo
   __shared__ float sums[4][E + 2][64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int h = (int)(blockIdx.x % (unsigned)P.Hq), at = (int)(blockIdx.x / (unsigned)P.Hq), g = h / P.G;
-  const int s = seq_rows > 0 ? at / seq_rows : sequence_of(P.cu, P.S, at, lane);
-  if (s >= P.S) return;
-  const int row0 = min(max(P.cu[s], 0), P.T), tok = seq_rows > 0 ? row0 + at % seq_rows : at;
   Stream<ROWS> stream;
   const int share = stream.share(A, workgroups, NW >> A.unit > 0 ? NW >> A.unit : 1, lane);
   if (share == 0) return;
-  // where the sequence begins in the stream
-  int start = 0, n = 0, tiles = 0, count = 0;
+  // the row's sequence, and where that begins in the stream
+  int s = seq_rows > 0 ? at / seq_rows : P.S <= 64 ? 0 : sequence_of(P.cu, P.S, at, lane);
+  if (seq_rows == 0 && P.S <= 64) {
+    const unsigned long long mine = __builtin_amdgcn_ballot_w64(at >= stream.row0 && at < stream.row0 + stream.n);
+    s = mine ? __builtin_ctzll(mine) : P.S;
+  }
+  if (s >= P.S) return;
+  int start = 0, row0 = 0, n = 0, tiles = 0, count = 0;
   for (int base = 0; base <= s; base += 64) {
     if (P.S > 64) stream.load(A, base, lane);
     int x = base + lane < s ? stream.size(P) : 0;
@@ -550,11 +587,14 @@ __global__ __launch_bounds__(256) void cache4_join_kernel(Cache4Params A, int wo
       if (off < P.S) x += __shfl_xor(x, off, 64);
     start += x;
     if (s - base < 64) {
-      n = __builtin_amdgcn_readlane(stream.n, s - base);
-      tiles = __builtin_amdgcn_readlane(stream.tiles, s - base);
-      count = __builtin_amdgcn_readlane(stream.count, s - base);
+      const int src = s - base;
+      row0 = __builtin_amdgcn_readlane(stream.row0, src);
+      n = __builtin_amdgcn_readlane(stream.n, src);
+      tiles = __builtin_amdgcn_readlane(stream.tiles, src);
+      count = __builtin_amdgcn_readlane(stream.count, src);
     }
   }
+  const int tok = seq_rows > 0 ? row0 + at % seq_rows : at;
   if (tok - row0 < 0 || tok - row0 >= n) return;
   const int m = (tok - row0) * P.G + h % P.G;
   const unsigned first = (unsigned)(__builtin_amdgcn_readfirstlane(start) + (g * tiles + m / ROWS) * count), w0 = first / (unsigned)share, w1 = (first + (unsigned)count - 1) / (unsigned)share;
@@ -747,8 +787,8 @@ static Cache4Plan plan_cache4(const sb_cache4* c, const sb_chunk* n, int window,
     const int64_t longest = std::min<int64_t>(n->max_length, (int64_t)c->max_pages * c->page_size);
     return (std::min(in_window, longest) + tile - 1) / tile;
   };
-  p.rows = f32 || most <= 16 ? 16 : 32;
-  if (f32) p.few = items(most, 16);
+  p.rows = most <= 4 && D == 128 ? 4 : most <= 8 ? 8 : f32 || most <= 16 ? 16 : 32;
+  if (f32) p.few = items(most, p.rows);
   else if (G <= kFewRows4 && (S > 1 || most <= kFewRows4)) p.few = items(std::min<int64_t>(most, kFewRows4), p.rows);
   p.splits = 1;
   size_t sums = 0;
@@ -756,7 +796,7 @@ static Cache4Plan plan_cache4(const sb_cache4* c, const sb_chunk* n, int window,
     // As many workgroups as the chip holds.  Whole items, without the launch that joins parts, where two strips a wavefront are all there is, and for float32 prompts, whose
     // items are many and alike.
     if (tiles(p.rows, 32) > 2 * kWaves4 && !(f32 && most > kFewRows4 && p.few * c->num_kv_heads >= 4096))
-      p.workgroups = 256 * split_waves(D, p.rows / 16 * (f32 ? 3 : 1));
+      p.workgroups = 256 * split_waves(D, p.rows, f32 ? 3 : 1);
     sums = (size_t)p.workgroups * 2 * p.rows;
     const int64_t strips = ((int64_t)c->max_pages * c->page_size + 31) / 32 + 2;  // of an item, at most
     while (p.few * c->num_kv_heads * (((strips - 1) >> p.unit) + 1) > 0x40000000ll && p.unit < 26) ++p.unit;
@@ -841,23 +881,29 @@ int sb_cache4_attn(const sb_cache4* c, const sb_chunk* n, int32_t window, int32_
     P.splits = plan.workgroups > 0 ? 0 : 1;
     A.unit = plan.unit;
     P.rows_to = f32 ? 0x7fffffff : kFewRows4;
-    auto launch = [&](auto ty, auto d, auto nt, auto pieces) {
+    auto launch = [&](auto ty, auto d, auto rows, auto pieces) {
       typedef decltype(ty) Type;
-      constexpr int DD = decltype(d)::value, NT = decltype(nt)::value;
-      hipLaunchKernelGGL((cache4_split_kernel<Type, DD, NT, decltype(pieces)::value>), few_grid, dim3(64 * kWaves4), 0, st, A);
+      constexpr int DD = decltype(d)::value, ROWS = decltype(rows)::value;
+      hipLaunchKernelGGL((cache4_split_kernel<Type, DD, ROWS < 16 ? 16 / ROWS : 1, ROWS < 16 ? 1 : ROWS / 16, decltype(pieces)::value>), few_grid, dim3(64 * kWaves4), 0, st, A);
       SB_LAUNCH_CHECK("cache4_split_kernel");
       if (plan.workgroups > 0) {
-        hipLaunchKernelGGL((cache4_join_kernel<Type, DD, 16 * NT>), few_rows, dim3(256), 0, st, A, plan.workgroups, seq_rows);
+        hipLaunchKernelGGL((cache4_join_kernel<Type, DD, ROWS>), few_rows, dim3(256), 0, st, A, plan.workgroups, seq_rows);
         SB_LAUNCH_CHECK("cache4_join_kernel");
       }
       return (int)SB_OK;
     };
-    auto with_d = [&](auto ty, auto nt, auto pieces) {
-      return c->head_dim == 128 ? launch(ty, std::integral_constant<int, 128>(), nt, pieces) : launch(ty, std::integral_constant<int, 64>(), nt, pieces);
+    auto with_rows = [&](auto ty, auto d, auto pieces) {
+      if constexpr (decltype(d)::value == 128)
+        if (plan.rows == 4) return launch(ty, d, std::integral_constant<int, 4>(), pieces);
+      if (plan.rows == 8) return launch(ty, d, std::integral_constant<int, 8>(), pieces);
+      if constexpr (decltype(pieces)::value == 1)
+        if (plan.rows == 32) return launch(ty, d, std::integral_constant<int, 32>(), pieces);
+      return launch(ty, d, std::integral_constant<int, 16>(), pieces);
     };
-    if (f32) return with_d(float(), std::integral_constant<int, 1>(), std::integral_constant<int, 3>());
-    if (plan.rows == 16) return with_d(bf16(), std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
-    return with_d(bf16(), std::integral_constant<int, 2>(), std::integral_constant<int, 1>());
+    auto with_d = [&](auto ty, auto pieces) {
+      return c->head_dim == 128 ? with_rows(ty, std::integral_constant<int, 128>(), pieces) : with_rows(ty, std::integral_constant<int, 64>(), pieces);
+    };
+    return f32 ? with_d(float(), std::integral_constant<int, 3>()) : with_d(bf16(), std::integral_constant<int, 1>());
   }
   return SB_OK;
 }
