@@ -13,10 +13,15 @@
 
 namespace sb {
 
+struct CutItem {  // an item that a workgroup has the first part of
+  int row0, rows, m0, g;  // its sequence's first packed row and flattened rows, its own first, its KV head
+  int parts, reserved[3];
+};
 struct Cache4Params {
   WindowParams w;  // (of its cache, the page table alone is read)
   PagedCache4 cache;
   int unit;  // see Stream
+  CutItem* cuts;  // of every workgroup
 };
 
 typedef __amdgpu_buffer_rsrc_t Rsrc;
@@ -273,10 +278,10 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
   Stream<ROWS> stream;
   const int share = stream.share(A, gridDim.x, NW >> A.unit > 0 ? NW >> A.unit : 1, lane);
   const int64_t x_last = (int64_t)share * (blockIdx.x + 1);
-  if (x_last - share > 0x7fffffff) return;
-  int x_first = (int)(x_last - share);
+  int x_first = (int)min(x_last - share, (int64_t)0x7fffffff);  // (the stream ends before)
   const int x_end = (int)min(x_last, (int64_t)0x7fffffff);
   Item item = stream.find(A, x_first, lane, true);
+  CutItem cut{};
   while (item.t.s >= 0) {
     const RowTile t = item.t;
     const int g = item.g, x_next = min(x_end, item.first + item.count);
@@ -322,6 +327,8 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
       }
       loader.issue(A.cache, row[0], row[1], ring0 + (x & (STAGES - 1)) * SLOT, lane);
     };
+
+    look_up(0);  // (on its way beside the queries)
 
     // B operand of the scores: column = row r16 of tile nt, zero in groups that are not the column's own
     bf16x8 qf[NT][GROUPS][PIECES];
@@ -498,7 +505,7 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
         for (int p = 0; p < PIECES; ++p) asm volatile("" : "+v"(qf[nt][c][p]));
     for (int from = 0; from < turns; from += 64) {  // (a look-up's worth)
       const int to = min(from + 64, turns);
-      look_up(from);
+      if (from > 0) look_up(from);
       asm volatile("s_waitcnt vmcnt(0)" : "+v"(where[0]), "+v"(where[1]), "+v"(there[0]), "+v"(there[1]) : : "memory");
 #pragma unroll
       for (int i = 0; i < STAGES - 1; ++i)
@@ -552,107 +559,74 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
         *(f32x4*)(P.part_o + at * D + 4 * c) = x;
       }
     }
+    if (!whole && x_first == item.first) cut = CutItem{t.row0, rows, m0, g, (int)((unsigned)(item.first + item.count - 1) / (unsigned)share) - (int)blockIdx.x + 1, {}};
     x_first = x_next;
     if (x_first >= x_end) break;
     __syncthreads();  // the sums' LDS is free
     item = stream.find(A, x_first, lane, false);  // (loaded again: kept, the sequences' numbers would cost the strips registers)
   }
+  if (P.splits != 1 && threadIdx.x == 0) A.cuts[blockIdx.x] = cut;  // every workgroup, so that nothing of an earlier call is left
 }
 
-// Joins the parts of the items that were cut: a workgroup to a row and head, every fourth part a wavefront's.  A part that saw nothing has LSE -infinity; one that saw what is no number
-// has left that, and so is the row's result.  Rows of no sequence, and of items that one workgroup has had, are left as they are.
+// Joins the parts of the items that were cut: a workgroup to four rows of an item that began in workgroup blockIdx.x of the launch before, its threads' groups every NG-th part.  A part that saw
+// nothing has LSE -infinity; one that saw what is no number has left that, and so is the row's result.
 template <typename T, int D, int ROWS>
-__global__ __launch_bounds__(256) void cache4_join_kernel(Cache4Params A, int workgroups, int seq_rows) {
+__global__ __launch_bounds__(512) void cache4_join_kernel(Cache4Params A) {
   const WindowParams& P = A.w;
-  constexpr int E = D / 64, NW = kWaves4;
-  __shared__ float sums[4][E + 2][64];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int h = (int)(blockIdx.x % (unsigned)P.Hq), at = (int)(blockIdx.x / (unsigned)P.Hq), g = h / P.G;
-  Stream<ROWS> stream;
-  const int share = stream.share(A, workgroups, NW >> A.unit > 0 ? NW >> A.unit : 1, lane);
-  if (share == 0) return;
-  // the row's sequence, and where that begins in the stream
-  int s = seq_rows > 0 ? at / seq_rows : P.S <= 64 ? 0 : sequence_of(P.cu, P.S, at, lane);
-  if (seq_rows == 0 && P.S <= 64) {
-    const unsigned long long mine = __builtin_amdgcn_ballot_w64(at >= stream.row0 && at < stream.row0 + stream.n);
-    s = mine ? __builtin_ctzll(mine) : P.S;
-  }
-  if (s >= P.S) return;
-  int start = 0, row0 = 0, n = 0, tiles = 0, count = 0;
-  for (int base = 0; base <= s; base += 64) {
-    if (P.S > 64) stream.load(A, base, lane);
-    int x = base + lane < s ? stream.size(P) : 0;
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1)
-      if (off < P.S) x += __shfl_xor(x, off, 64);
-    start += x;
-    if (s - base < 64) {
-      const int src = s - base;
-      row0 = __builtin_amdgcn_readlane(stream.row0, src);
-      n = __builtin_amdgcn_readlane(stream.n, src);
-      tiles = __builtin_amdgcn_readlane(stream.tiles, src);
-      count = __builtin_amdgcn_readlane(stream.count, src);
-    }
-  }
-  const int tok = seq_rows > 0 ? row0 + at % seq_rows : at;
-  if (tok - row0 < 0 || tok - row0 >= n) return;
-  const int m = (tok - row0) * P.G + h % P.G;
-  const unsigned first = (unsigned)(__builtin_amdgcn_readfirstlane(start) + (g * tiles + m / ROWS) * count), w0 = first / (unsigned)share, w1 = (first + (unsigned)count - 1) / (unsigned)share;
-  if (w0 == w1) return;
-  const int parts = (int)(w1 - w0) + 1;
-  constexpr int kRuns = 8;  // on their way at a time
-  float x[E] = {}, best = -__builtin_inff(), sum = 0.f;
-  for (int z0 = wave; z0 < parts; z0 += 4 * kRuns) {
-    float lse[kRuns], part[kRuns][E], top = best;
+  constexpr int NG = 512 / D, kRuns = 8;  // on their way at a time
+  __shared__ __attribute__((aligned(16))) float sums[NG][4][D + 4];  // (and what they are relative to, their weight)
+  const CutItem cut = A.cuts[blockIdx.x];
+  const int group = threadIdx.x / D, i4 = threadIdx.x % D, r = i4 / (D / 4), c = 4 * (i4 % (D / 4));
+  const int m = cut.m0 + 4 * (int)blockIdx.y + r;
+  if (cut.parts == 0) return;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  float best = -__builtin_inff(), sum = 0.f;
+  for (int z0 = group; z0 < cut.parts; z0 += NG * kRuns) {
+    float lse[kRuns], top = best;
+    f32x4 part[kRuns];
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) {  // (past the last part, it again)
-      const unsigned w = w0 + (unsigned)min(z0 + 4 * i, parts - 1);
-      const int64_t from = ((int64_t)w * 2 + ((uint64_t)w * (unsigned)share <= first)) * ROWS + m % ROWS;
+      const int z = min(z0 + NG * i, cut.parts - 1);
+      const int64_t from = (((int64_t)blockIdx.x + z) * 2 + (z == 0)) * ROWS + 4 * blockIdx.y + r;
       lse[i] = P.part_lse[from];
-#pragma unroll
-      for (int e = 0; e < E; ++e) part[i][e] = P.part_o[from * D + E * lane + e];
-      if (z0 + 4 * i >= parts) lse[i] = -__builtin_inff();
+      part[i] = *(const f32x4*)(P.part_o + from * D + c);
+      if (z0 + NG * i >= cut.parts) lse[i] = -__builtin_inff();
     }
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) top = fmaxf(top, lse[i]);
     const float ref = top == -__builtin_inff() ? 0.f : top;  // nothing seen yet: keep the exponents finite
     const float old = fast_exp2(best - ref);
     sum *= old;
-#pragma unroll
-    for (int e = 0; e < E; ++e) x[e] *= old;
+    x *= old;
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) {
       const float f = fast_exp2(lse[i] - ref);
       sum += f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(f, lse[i] == -__builtin_inff() ? 0.f : part[i][e], x[e]);
+      if (lse[i] != -__builtin_inff()) x += f * part[i];
     }
     best = top;
   }
-#pragma unroll
-  for (int e = 0; e < E; ++e) sums[wave][e][lane] = x[e];
-  sums[wave][E][lane] = best;
-  sums[wave][E + 1][lane] = sum;
+  *(f32x4*)&sums[group][r][c] = x;
+  if (c == 0) { sums[group][r][D] = best; sums[group][r][D + 1] = sum; }
   __syncthreads();
-  if (wave > 0) return;
+  if (group > 0 || m >= cut.rows) return;
   best = -__builtin_inff();
 #pragma unroll
-  for (int w = 0; w < 4; ++w) best = fmaxf(best, sums[w][E][lane]);
+  for (int w = 0; w < NG; ++w) best = fmaxf(best, sums[w][r][D]);
   sum = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) x[e] = 0.f;
+  x = f32x4{0.f, 0.f, 0.f, 0.f};
   const float ref = best == -__builtin_inff() ? 0.f : best;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const float f = fast_exp2(sums[w][E][lane] - ref);
-    sum += f * sums[w][E + 1][lane];
+  for (int w = 0; w < NG; ++w) {
+    const float f = fast_exp2(sums[w][r][D] - ref);
+    sum += f * sums[w][r][D + 1];
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(f, sums[w][e][lane], x[e]);
+    for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(f, sums[w][r][c + e], x[e]);
   }
-  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-#pragma unroll
-  for (int e = 0; e < E; ++e) ((T*)P.o)[((int64_t)tok * P.Hq + h) * D + E * lane + e] = (T)(x[e] * inv);
-  if (lane == 0) P.lse[(int64_t)h * P.T + tok] = sum == 0.f ? -__builtin_inff() : (best + __builtin_log2f(sum)) * 0.69314718055994531f;
+  const int j = (int)((unsigned)m / (unsigned)P.G), h = cut.g * P.G + m - j * P.G, tok = cut.row0 + j;
+  x *= sum == 0.f ? 0.f : 1.0f / sum;
+  store4((T*)P.o + ((int64_t)tok * P.Hq + h) * D + c, x);
+  if (c == 0) P.lse[(int64_t)h * P.T + tok] = sum == 0.f ? -__builtin_inff() : (best + __builtin_log2f(sum)) * 0.69314718055994531f;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -773,9 +747,8 @@ struct Cache4Plan {
   int workgroups;         // of few rows; 0: whole items, a workgroup each
   int unit;
   int splits, per_split;  // of many rows: keys in `splits` runs of per_split tiles
-  size_t part_o, bytes;
+  size_t part_lse, part_o, bytes;
 };
-static int few_seq_rows4(const sb_cache4* c, int G, int max_new) { return c->dtype == SB_F32 ? max_new : std::min(kFewRows4 / G, max_new); }  // tokens of a sequence of few rows, at most
 static Cache4Plan plan_cache4(const sb_cache4* c, const sb_chunk* n, int window, int sinks) {
   Cache4Plan p{};
   const int G = n->num_q_heads / c->num_kv_heads, S = n->num_seqs, D = c->head_dim;
@@ -810,7 +783,8 @@ static Cache4Plan plan_cache4(const sb_cache4* c, const sb_chunk* n, int window,
     p.per_split = (int)per;
     if (p.splits > 1) sums = std::max(sums, (size_t)p.splits * n->total_new * n->num_q_heads);
   }
-  p.part_o = align_up(sums * sizeof(float));
+  p.part_lse = align_up(p.workgroups * sizeof(CutItem));
+  p.part_o = align_up(p.part_lse + sums * sizeof(float));
   p.bytes = align_up(p.part_o + sums * D * sizeof(float));
   return p;
 }
@@ -855,16 +829,15 @@ int sb_cache4_attn(const sb_cache4* c, const sb_chunk* n, int32_t window, int32_
   const Cache4Plan plan = plan_cache4(c, n, window, sinks);
   if (plan.workgroups > 0 || plan.splits > 1) {
     if (!ws) { set_error("null argument"); return SB_ERR_INVALID_ARG; }
-    P.part_lse = (float*)ws;
+    A.cuts = (CutItem*)ws;
+    P.part_lse = (float*)((char*)ws + plan.part_lse);
     P.part_o = (float*)((char*)ws + plan.part_o);
   }
   const bool f32 = c->dtype == SB_F32;
-  int seq_rows = few_seq_rows4(c, P.G, std::min(P.max_new, P.T));
-  if ((int64_t)seq_rows * P.S >= P.T) seq_rows = 0;  // (a prompt beside others has no parts of few rows)
-  dim3 few_grid, many_grid, few_rows, all_rows;
+  if (plan.few * P.Hkv > 0x40000000ll) { set_error("too many tiles for one launch"); return SB_ERR_UNSUPPORTED; }
+  dim3 few_grid, many_grid, all_rows;
   if ((rc = grid_of(plan.workgroups > 0 ? plan.workgroups : plan.few * P.Hkv, 64 * kWaves4, &few_grid)) != SB_OK ||
-      (rc = grid_of(plan.many * P.Hkv * plan.splits, 64 * kChunkWaves, &many_grid)) != SB_OK || (plan.splits > 1 && (rc = grid_of((int64_t)P.T * P.Hq, 256, &all_rows)) != SB_OK) ||
-      (plan.workgroups > 0 && (rc = grid_of((seq_rows > 0 ? (int64_t)seq_rows * P.S : P.T) * P.Hq, 256, &few_rows)) != SB_OK))
+      (rc = grid_of(plan.many * P.Hkv * plan.splits, 64 * kChunkWaves, &many_grid)) != SB_OK || (plan.splits > 1 && (rc = grid_of((int64_t)P.T * P.Hq, 256, &all_rows)) != SB_OK))
     return rc;
   const hipStream_t st = (hipStream_t)stream;
   KernelTimer kt(K_CACHE_ATTN, st);
@@ -887,7 +860,7 @@ int sb_cache4_attn(const sb_cache4* c, const sb_chunk* n, int32_t window, int32_
       hipLaunchKernelGGL((cache4_split_kernel<Type, DD, ROWS < 16 ? 16 / ROWS : 1, ROWS < 16 ? 1 : ROWS / 16, decltype(pieces)::value>), few_grid, dim3(64 * kWaves4), 0, st, A);
       SB_LAUNCH_CHECK("cache4_split_kernel");
       if (plan.workgroups > 0) {
-        hipLaunchKernelGGL((cache4_join_kernel<Type, DD, ROWS>), few_rows, dim3(256), 0, st, A, plan.workgroups, seq_rows);
+        hipLaunchKernelGGL((cache4_join_kernel<Type, DD, ROWS>), dim3(plan.workgroups, ROWS / 4), dim3(512), 0, st, A);
         SB_LAUNCH_CHECK("cache4_join_kernel");
       }
       return (int)SB_OK;
