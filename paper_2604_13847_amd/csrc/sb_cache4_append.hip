@@ -1,7 +1,7 @@
 // Append of new tokens to a paged cache in four bits: keys turned by their positions, keys and values rounded to four bits, queries turned.
 //
-// Memory-bound: q is read and written once, k and v are read once and written in a third of their size (and once more where the caller asks for the values as held).  A workgroup takes a
-// token at a time, each of its four wavefronts every fourth batch of heads.
+// Memory-bound: q is read and written once, k and v are read once and written in a third of their size (and once more where the caller asks for the values as held).  A
+// wavefront takes a token at a time (or, of few tokens, every fourth batch of heads of one), the next heads' loads on their way.
 //
 // What four bits a key gets must not depend on how its turn is computed (in another order of operations an element next to a threshold would get another code), so angles, sines and the
 // turn itself are float64, rounded to float32 once.  Sine and cosine come from their Taylor series on an eighth of a revolution either way, eight terms each: off by less than 2^-45.
@@ -24,7 +24,8 @@ struct Append4Params {
   int rot;
   float amplitude;
   PagedCache4 cache;
-  int run;  // tokens a workgroup takes
+  int waves;  // to a token: 4 or 1
+  int run;    // tokens of these, one after the other
   uint8_t axis[SB_ROPE_MAX_PAIRS];
   double turns[SB_ROPE_MAX_PAIRS];
 };
@@ -60,56 +61,66 @@ __device__ inline unsigned step_of(unsigned largest) {
   const unsigned r = (__float_as_uint(sixth) + 0x20000u) & ~0x3ffffu;
   return min(r, 0x7e280000u);  // 1.3125 * 2^125
 }
-// The code of the number nearest x / step, ties to the even code
+// The code of the number nearest x / step, ties to the even code: at the thresholds of even levels (0.75, 1.75, 3.5 steps) the upper one, at the others the lower one.  Three comparisons, each
+// with a threshold that goes by those before.
 __device__ inline unsigned code_of(float x, float step) {
-  const float y = fabsf(x);
-  const unsigned level = (y > 0.25f * step) + (y >= 0.75f * step) + (y > 1.25f * step) + (y >= 1.75f * step) + (y > 2.5f * step) + (y >= 3.5f * step) + (y > 5.0f * step);
-  return level | (__float_as_uint(x) >> 31 << 3);
+  const float y = fabsf(x), t1 = 0.25f * step, t2 = 0.75f * step, t3 = 1.25f * step, t4 = 1.75f * step, t5 = 2.5f * step, t6 = 3.5f * step, t7 = 5.0f * step;
+  const bool c4 = y >= t4;
+  const float even = c4 ? t6 : t2, low = c4 ? t5 : t1, high = c4 ? t7 : t3;
+  const bool c2 = y >= even;
+  const float odd = c2 ? high : low;
+  return (unsigned)c4 * 4 + (unsigned)c2 * 2 + (unsigned)(y > odd) + (__float_as_uint(x) >> 31 << 3);
 }
-__device__ inline float level_of(unsigned code) {
-  const unsigned m = code & 7;
-  const float y = m < 4 ? 0.5f * (float)m : m < 6 ? (float)m - 2.0f : 2.0f * (float)m - 8.0f;
-  return code & 8 ? -y : y;
+// Eight neighbouring elements as they lie in memory
+template <typename T> struct alignas(16) Eight { T x[8]; };
+template <typename T, bool WIDE> __device__ inline Eight<T> load8(const T* from) {
+  if (WIDE) return *(const Eight<T>*)from;
+  Eight<T> y;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y.x[e] = from[e];
+  return y;
 }
-
-template <typename T> __device__ inline void load8(float (&x)[8], const T* from, bool wide) {
-  T y[8];
-  if (wide) {
-    typedef struct alignas(16) { T x[16 / sizeof(T)]; } Piece;
+__device__ inline void store8(bf16* to, const float (&x)[8]) {  // 16-byte aligned
+  bf16x8 y;
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) *(Piece*)(y + i * 16 / sizeof(T)) = ((const Piece*)from)[i];
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = from[e];
-  }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = (float)y[e];
+  for (int e = 0; e < 8; ++e) y[e] = (bf16)x[e];
+  *(bf16x8*)to = y;
 }
-template <typename T> __device__ inline void store8(T* to, const float (&x)[8]) {  // 16-byte aligned
-  typedef struct alignas(16) { T x[16 / sizeof(T)]; } Piece;
-#pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-    Piece p;
-#pragma unroll
-    for (int e = 0; e < (int)(16 / sizeof(T)); ++e) p.x[e] = (T)x[i * (16 / sizeof(T)) + e];
-    ((Piece*)to)[i] = p;
-  }
+__device__ inline void store8(float* to, const float (&x)[8]) {
+  *(f32x4*)to = f32x4{x[0], x[1], x[2], x[3]};
+  *(f32x4*)(to + 4) = f32x4{x[4], x[5], x[6], x[7]};
 }
 
-// A lane holds eight neighbouring elements, 8 x .. 8 x + 7 of a head (x = lane % (D/8)); four lanes a group of 32.  WIDE: rows of q, k, v are 16-byte aligned.
+// A lane holds eight neighbouring elements, 8 x .. 8 x + 7 of a head (x = lane % (D/8)); four lanes a group of 32.  WIDE: rows of q, k, v are 16-byte aligned, and (HALF) what a lane's
+// elements are paired with is eight neighbours too.
 template <typename T, int D, bool HALF, bool TURN, bool WIDE>
 __global__ __launch_bounds__(256) void cache4_append_kernel(Append4Params P) {
   constexpr int LPH = D / 8, PER = 64 / LPH;  // lanes a head, heads a wavefront takes at a time
-  __shared__ double2 table[4][SB_ROPE_MAX_PAIRS];
+  // What every element of a head is multiplied with, and what its other one is; element 8 x + e at 16 e + x (D/8 e + x), so that lanes side by side read places side by side
+  __shared__ double2 table[4][TURN ? D : 1];
+  __shared__ float2 table_q[4][TURN ? D : 1];
   __shared__ __attribute__((aligned(16))) unsigned codes[4][64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int x = lane % LPH, sub = lane / LPH;
+  const int x = lane % LPH, sub = lane / LPH, half = P.rot / 2;
   double2* const cs = table[wave];
-  const double turns = TURN && lane < P.rot / 2 ? P.turns[lane] : 0.0;
-  const int32_t* const axis_positions = P.axis_positions ? P.axis_positions + (lane < P.rot / 2 ? (int64_t)P.axis[lane] * P.T : 0) : nullptr;
-  const int heads = (P.q ? P.Hq : 0) + 2 * P.Hkv, hv = P.Hkv;  // in this order: k, v, q
-  const int64_t tok0 = (int64_t)blockIdx.x * P.run;
+  float2* const cs_q = table_q[wave];
+  const double turns = TURN && lane < half ? P.turns[lane] : 0.0;
+  const int32_t* const axis_positions = P.axis_positions ? P.axis_positions + (lane < half ? (int64_t)P.axis[lane] * P.T : 0) : nullptr;
+  const int kv_units = (P.Hkv + PER - 1) / PER, units = 2 * kv_units + (P.q ? (P.Hq + PER - 1) / PER : 0);  // of PER heads: k, v, q
+  const bool turned = TURN && 8 * x < P.rot;       // some of the lane's elements are
+  // the two elements of pair `lane`, and their places in the tables
+  auto place = [](int d) { return (d & 7) * LPH + (d >> 3); };
+  const int place_a = place(HALF ? lane : 2 * lane), place_b = place(HALF ? lane + half : 2 * lane + 1);
+  if (TURN)
+    for (int d = P.rot + lane; d < D; d += 64) {  // what is not turned
+      cs[place(d)] = make_double2(1.0, 0.0);
+      cs_q[place(d)] = make_float2(1.f, 0.f);
+    }
+  const int away = !HALF ? 0 : 8 * x < half ? half : -half;  // where their others are (WIDE)
+  const int step = P.waves, unit0 = step == 1 ? 0 : wave;
+  const int64_t tok0 = (step == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x) * P.run;
   int s = 0, first = 0, behind = -1;
+  Eight<T> mine{}, other{}, next{}, next_other{};
   for (int64_t tok = tok0; tok < min(tok0 + P.run, (int64_t)P.T); ++tok) {
     if (tok >= behind) {
       s = sequence_of(P.cu, P.S, (int)tok, lane);
@@ -120,89 +131,125 @@ __global__ __launch_bounds__(256) void cache4_append_kernel(Append4Params P) {
     int64_t pos = tok - first;
     if (pos < 0 || pos >= P.max_new) continue;
     pos += max(P.cached[s], 0);
-    if (TURN) {
-      double t = (double)(axis_positions ? axis_positions[tok] : pos) * turns;
-      t -= rint(t);
-      const double2 z = turn_of(t);
-      cs[lane] = make_double2(z.x * (double)P.amplitude, z.y * (double)P.amplitude);
-    }
-    asm volatile("" ::: "memory");  // (LDS operations of a wavefront complete in order)
     const int64_t row0 = P.cache.row_of(s, pos, 0);
-    for (int h0 = wave * PER; h0 < heads; h0 += 4 * PER) {
-      const int h = h0 + sub;
-      const bool there = h < heads;
-      const int kind = !there ? 3 : h < hv ? 0 : h < 2 * hv ? 1 : 2, g = kind == 0 ? h : kind == 1 ? h - hv : h - 2 * hv;
-      const T* const from = kind == 0 ? (const T*)P.k + tok * P.k_pitch + g * D : kind == 1 ? (const T*)P.v + tok * P.v_pitch + g * D
-                            : kind == 2 ? (const T*)P.q + tok * P.q_pitch + g * D : nullptr;
-      float a[8] = {};
-      if (there) load8(a, from + 8 * x, WIDE);
-      if (TURN && (kind == 0 || kind == 2)) {
-        // the other elements of the pairs: another eight (HALF), or these themselves
-        float b[8];
-        if (HALF) {
+    double t = TURN ? (double)(axis_positions ? axis_positions[tok] : pos) * turns : 0.0;
+    bool ready = !TURN;
+    auto kind_of = [&](int u) { return u < kv_units ? 0 : u < 2 * kv_units ? 1 : 2; };  // k, v, q
+    auto load = [&](int u, Eight<T>& a, Eight<T>& b) __attribute__((always_inline)) {
+      const int kind = kind_of(u), g = (u - kind * kv_units) * PER + sub;
+      if (u >= units || g >= (kind == 2 ? P.Hq : P.Hkv)) return;
+      const T* const from = (kind == 0 ? (const T*)P.k + tok * P.k_pitch : kind == 1 ? (const T*)P.v + tok * P.v_pitch : (const T*)P.q + tok * P.q_pitch) + g * D + 8 * x;
+      a = load8<T, WIDE>(from);
+      if (HALF && turned && kind != 1) {
+        if (WIDE) {
+          b = load8<T, true>(from + away);
+        } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const int d = 8 * x + e, half = P.rot / 2;
-            b[e] = d < P.rot ? (float)from[d < half ? d + half : d - half] : 0.f;
+            const int d = 8 * x + e;
+            b.x[e] = d < P.rot ? from[d < half ? half + e : e - half] : (T)0.f;
           }
         }
-        float r[8];
+      }
+    };
+    load(unit0, mine, other);
+    for (int u = unit0; u < units; u += step) {
+      const int kind = kind_of(u), g = (u - kind * kv_units) * PER + sub;
+      const bool there = g < (kind == 2 ? P.Hq : P.Hkv);
+      load(u + step, next, next_other);
+      if (!ready) {  // (while the loads are on their way)
+        t -= rint(t);
+        double2 z = turn_of(t);
+        z.x *= (double)P.amplitude;
+        z.y *= (double)P.amplitude;
+        if (lane < half) {
+          cs[place_a] = make_double2(z.x, -z.y);
+          cs[place_b] = z;
+          cs_q[place_a] = make_float2((float)z.x, -(float)z.y);
+          cs_q[place_b] = make_float2((float)z.x, (float)z.y);
+        }
+        ready = true;
+      }
+      asm volatile("" ::: "memory");  // (LDS operations of a wavefront complete in order)
+      float a[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int d = 8 * x + e, half = P.rot / 2;
-          const bool is_x = HALF ? d < half : (e & 1) == 0;
-          const int pair = HALF ? (d < half ? d : d - half) : d >> 1;
-          const double2 z = cs[pair & (SB_ROPE_MAX_PAIRS - 1)];
-          const float mine = a[e], other = HALF ? b[e] : a[e ^ 1];
-          if (kind == 0) r[e] = (float)((double)mine * z.x + (double)other * (is_x ? -z.y : z.y));
-          else r[e] = __builtin_fmaf(mine, (float)z.x, other * (float)(is_x ? -z.y : z.y));
-          if (d >= P.rot) r[e] = mine;
+      for (int e = 0; e < 8; ++e) a[e] = there ? (float)mine.x[e] : 0.f;
+      if (TURN && kind != 1 && turned) {
+        float b[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b[e] = HALF ? (float)other.x[e] : a[e ^ 1];
+        if (kind == 0) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const double2 z = cs[e * LPH + x];
+            b[e] = (float)__builtin_fma((double)a[e], z.x, (double)b[e] * z.y);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float2 z = cs_q[e * LPH + x];
+            b[e] = __builtin_fmaf(a[e], z.x, b[e] * z.y);
+          }
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) a[e] = r[e];
+        for (int e = 0; e < 8; ++e)
+          if (8 * x + e < P.rot) a[e] = b[e];  // (the others as they were: a factor of zero may have an infinity beside it)
       }
-      if (kind == 2) store8((T*)P.q_out + (tok * P.Hq + g) * D + 8 * x, a);
+      if (kind == 2) {
+        if (there) store8((T*)P.q_out + (tok * P.Hq + g) * D + 8 * x, a);
+        mine = next;
+        other = next_other;
+        continue;
+      }
       // (all lanes take part in what follows)
       unsigned largest = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) largest = max(largest, __float_as_uint(a[e]) & 0x7fffffffu);
-      largest = max(largest, (unsigned)__shfl_xor((int)largest, 1, 64));
-      largest = max(largest, (unsigned)__shfl_xor((int)largest, 2, 64));
+      largest = max(largest, (unsigned)__builtin_amdgcn_update_dpp(0, (int)largest, 0xb1, 0xf, 0xf, false));  // lanes 1, 0, 3, 2 of four
+      largest = max(largest, (unsigned)__builtin_amdgcn_update_dpp(0, (int)largest, 0x4e, 0xf, 0xf, false));  // 2, 3, 0, 1
       const unsigned bits = step_of(largest);
       const float step = __uint_as_float(bits);
       unsigned word = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) word |= code_of(a[e], step) << 4 * e;
       if (!(step > 0.f)) word = 0;
-      codes[wave][lane] = word;
-      asm volatile("" ::: "memory");
-      if (kind < 2) {
-        if (row0 >= 0) {
-          const int64_t row = row0 + (int64_t)g * P.cache.page_size;
-          if (x % 4 == 0) ((unsigned short*)(kind == 0 ? P.cache.k_step : P.cache.v_step))[row * (D / 32) + x / 4] = (unsigned short)(bits >> 16);
-          if (kind == 0) {
-            *(unsigned*)(P.cache.k + row * (D / 2) + (x % 4) * (D / 8) + 4 * (x / 4)) = word;
-          } else {  // word i of 16, the head's lanes two (D = 64: half) a word
+      const int64_t row = row0 + (int64_t)g * P.cache.page_size;
+      const bool kept = there && row0 >= 0;
+      if (kept && x % 4 == 0) ((unsigned short*)(kind == 0 ? P.cache.k_step : P.cache.v_step))[row * (D / 32) + x / 4] = (unsigned short)(bits >> 16);
+      if (kind == 0) {
+        if (kept) *(unsigned*)(P.cache.k + row * (D / 2) + (x % 4) * (D / 8) + 4 * (x / 4)) = word;
+      } else {  // word i of 16, the head's lanes two (D = 64: half) a word
+        codes[wave][lane] = word;
+        asm volatile("" ::: "memory");
 #pragma unroll
-            for (int i = x; i < 16; i += LPH) {
-              unsigned w = 0;
+        for (int w16 = 0; w16 < 16; w16 += LPH) {
+          const int i16 = w16 + x;
+          unsigned w = 0;
 #pragma unroll
-              for (int j = 0; j < D / 16; ++j) w |= (codes[wave][sub * LPH + 2 * j + (i >> 3)] >> 4 * (i & 7) & 15u) << 4 * j;
-              if (D == 128) *(unsigned*)(P.cache.v + row * (D / 2) + 4 * i) = w;
-              else *(unsigned short*)(P.cache.v + row * (D / 2) + 2 * i) = (unsigned short)w;
-            }
-          }
+          for (int j = 0; j < D / 16; ++j) w |= (codes[wave][sub * LPH + 2 * j + (i16 >> 3)] >> 4 * (i16 & 7) & 15u) << 4 * j;
+          if (!kept) continue;
+          if (D == 128) *(unsigned*)(P.cache.v + row * (D / 2) + 4 * i16) = w;
+          else *(unsigned short*)(P.cache.v + row * (D / 2) + 2 * i16) = (unsigned short)w;
         }
-        T* const held = (T*)(kind == 0 ? P.k_held : P.v_held);
-        if (held) {
-          float y[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = level_of(word >> 4 * e & 15u) * step;
-          store8(held + (tok * P.Hkv + g) * D + 8 * x, y);
-        }
+        asm volatile("" ::: "memory");
       }
-      asm volatile("" ::: "memory");
+      T* const held = (T*)(kind == 0 ? P.k_held : P.v_held);
+      if (held && there) {
+        float y[8];
+        auto put = [&](auto sel) __attribute__((always_inline)) {
+          constexpr int SEL = decltype(sel)::value;
+          typedef float f32x2 __attribute__((ext_vector_type(2)));
+          const f32x2 z = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.0f, SEL);
+          y[2 * SEL] = z[0] * step;
+          y[2 * SEL + 1] = z[1] * step;
+        };
+        put(std::integral_constant<int, 0>()); put(std::integral_constant<int, 1>()); put(std::integral_constant<int, 2>()); put(std::integral_constant<int, 3>());
+        store8(held + (tok * P.Hkv + g) * D + 8 * x, y);
+      }
+      mine = next;
+      other = next_other;
     }
+    asm volatile("" ::: "memory");
   }
 }
 
@@ -255,10 +302,14 @@ extern "C" int sb_cache4_append(const sb_cache4* c, const sb_chunk* n, const sb_
     for (int i = 0; i < r->rot_dim / 2; ++i) { P.turns[i] = r->turns[i]; P.axis[i] = axes ? axes->axis[i] : 0; }
   }
   const int esize = c->dtype == SB_F32 ? 4 : 2;
-  const bool wide = aligned16(q) && aligned16(k) && aligned16(v) && q_pitch * esize % 16 == 0 && k_pitch * esize % 16 == 0 && v_pitch * esize % 16 == 0;
-  P.run = P.T / 2048 < 1 ? 1 : P.T / 2048 > 8 ? 8 : P.T / 2048;
-  if (P.T >> 23 > P.run) P.run = P.T >> 23;  // (a launch has fewer than 2^32 threads)
-  const dim3 grid((unsigned)(((int64_t)P.T + P.run - 1) / P.run));
+  const bool wide = aligned16(q) && aligned16(k) && aligned16(v) && q_pitch * esize % 16 == 0 && k_pitch * esize % 16 == 0 && v_pitch * esize % 16 == 0 &&
+                    (!r || r->layout != SB_ROPE_HALF || r->rot_dim % 16 == 0);
+  // Four wavefronts to a token where tokens are few; where they fill the chip, one, which looks up and computes what a token has once.
+  P.waves = P.T < 2048 ? 4 : 1;
+  P.run = P.T <= 4096 ? 1 : P.T <= 8192 ? 2 : 4;  // (4096 wavefronts fill it: 8000 tokens in one round 48.5 us, in two 50.4)
+  if (P.T >> 25 > P.run) P.run = P.T >> 25;  // (a launch has fewer than 2^32 threads)
+  const int64_t per = (int64_t)P.run * 4 / P.waves;
+  const dim3 grid((unsigned)((P.T + per - 1) / per));
   const hipStream_t st = (hipStream_t)stream;
   KernelTimer kt(K_ROPE, st);
   auto launch = [&](auto t, auto d, auto half, auto turn, auto w) {
