@@ -396,6 +396,11 @@ def _address(t):
     return None if t is None else t.data_ptr()
 
 
+def _like(t, shape):
+    """A contiguous tensor of t's type on its device; the cheaper call where t lies so itself."""
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(shape)
+
+
 def _workspace(ws, need, device):
     if ws is None:
         return _bytes(need, torch.device("cuda", device)) if need else None
@@ -472,14 +477,14 @@ def sb_rope_axes_apply(pb: Problem, rope: Rope, axes: RopeAxes, positions, q, k,
         shape = (pb.T, pb.Hq, pb.D)
         _tensor("q", q, shape, dt, device, pitch=True)
         if q_out is None:
-            q_out = torch.empty(shape, dtype=dt, device=q.device)
+            q_out = _like(q, shape)
         else:
             _tensor("q_out", q_out, shape, dt, device)
     if k is not None:
         shape = (pb.T, pb.Hkv, pb.D)
         _tensor("k", k, shape, dt, device, pitch=True)
         if k_out is None:
-            k_out = torch.empty(shape, dtype=dt, device=k.device)
+            k_out = _like(k, shape)
         else:
             _tensor("k_out", k_out, shape, dt, device)
     _tensor("positions", positions, (axes.c.num_axes, pb.T), torch.int32, device)
@@ -648,7 +653,7 @@ def sb_cache_append_axes(cache: Cache, chunk: Chunk, k, v, rope: Rope, axes: Rop
     if q is not None:
         _tensor("q", q, queries, dt, device, pitch=True)
         if q_out is None:
-            q_out = torch.empty(queries, dtype=dt, device=q.device)
+            q_out = _like(q, queries)
         else:
             _tensor("q_out", q_out, queries, dt, device)
     elif q_out is not None:
@@ -697,17 +702,22 @@ def sb_cache_tables(pool: PagePool, cached, added, total_new, cu_new=None, posit
     _tensor("added", added, (S,), torch.int32, device)
     if not 0 <= total_new < 2 ** 31:
         raise SparseBalError(f"total_new: {total_new} does not fit 31 bits")
-    out = []
-    for name, x, shape, dt in (("cu_new", cu_new, (S + 1,), torch.int32), ("positions", positions, (total_new,), torch.int32), ("slots", slots, (total_new,), torch.int64),
-                               ("missing", missing, (1,), torch.int32)):
-        if x is None:
-            x = torch.empty(shape, dtype=dt, device=cached.device)
-        else:
-            _tensor(name, x, shape, dt, device)
-        out.append(x)
-    _call("sb_cache_tables", C.addressof(pool.c), cached.data_ptr(), added.data_ptr(), int(total_new), out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), out[3].data_ptr(),
+    if cu_new is None and positions is None and missing is None:
+        cu_new, missing, positions = cached.new_empty(S + 2 + total_new).split_with_sizes([S + 1, 1, total_new])  # (one allocation)
+    else:
+        cu_new = cached.new_empty(S + 1) if cu_new is None else cu_new
+        positions = cached.new_empty(total_new) if positions is None else positions
+        missing = cached.new_empty(1) if missing is None else missing
+        _tensor("cu_new", cu_new, (S + 1,), torch.int32, device)
+        _tensor("positions", positions, (total_new,), torch.int32, device)
+        _tensor("missing", missing, (1,), torch.int32, device)
+    if slots is None:
+        slots = cached.new_empty(total_new, dtype=torch.int64)
+    else:
+        _tensor("slots", slots, (total_new,), torch.int64, device)
+    _call("sb_cache_tables", C.addressof(pool.c), cached.data_ptr(), added.data_ptr(), int(total_new), cu_new.data_ptr(), positions.data_ptr(), slots.data_ptr(), missing.data_ptr(),
           stream)
-    return tuple(out)
+    return cu_new, positions, slots, missing
 
 
 class Cache4:
@@ -746,7 +756,7 @@ def sb_cache4_append(cache: Cache4, chunk: Chunk, k, v, rope: Rope = None, axes:
     if q is not None:
         _tensor("q", q, queries, dt, device, pitch=True)
         if q_out is None:
-            q_out = torch.empty(queries, dtype=dt, device=q.device)
+            q_out = _like(q, queries)
         else:
             _tensor("q_out", q_out, queries, dt, device)
     elif q_out is not None:
@@ -756,11 +766,11 @@ def sb_cache4_append(cache: Cache4, chunk: Chunk, k, v, rope: Rope = None, axes:
     if axes is not None:
         _tensor("positions", positions, (axes.c.num_axes, n), torch.int32, device)
     if held and k_held is None:
-        k_held = torch.empty(keys, dtype=dt, device=k.device)
+        k_held = _like(k, keys)
     elif k_held is not None:
         _tensor("k_held", k_held, keys, dt, device)
     if held and v_held is None:
-        v_held = torch.empty(keys, dtype=dt, device=k.device)
+        v_held = _like(v, keys)
     elif v_held is not None:
         _tensor("v_held", v_held, keys, dt, device)
     _call("sb_cache4_append", C.addressof(cache.c), C.addressof(chunk.c), C.addressof(rope.c) if rope is not None else None, C.addressof(axes.c) if axes is not None else None,
@@ -785,7 +795,7 @@ def sb_cache4_attn(cache: Cache4, chunk: Chunk, q, window=2 ** 31 - 1, sinks=0, 
     else:
         _tensor("o", o, queries, dt, device)
     if lse is None:
-        lse = torch.empty(rows, dtype=torch.float32, device=q.device)
+        lse = q.new_empty(rows, dtype=torch.float32)
     else:
         _tensor("lse", lse, rows, torch.float32, device)
     window, sinks = _window(window, sinks)
