@@ -255,7 +255,7 @@ struct Stream {
 constexpr int kWaves4 = 4;
 // Wavefronts of a SIMD, by registers, and stages of a ring, so that the rings of as many workgroups fit a CU.  64 sequences of 500 to 32768 tokens, 32/8 heads: 150 us with two wavefronts
 // and four stages, 136 with three and two (124 without the arithmetic, 89 without the loads), 139 with four, which spill.
-constexpr int split_waves(int D, int rows, int pieces) { return D == 64 ? (pieces == 3 ? 3 : rows == 32 ? 2 : 4) : rows == 32 ? 1 : rows == 4 || (rows == 8 && pieces == 1) ? 3 : 2; }
+constexpr int split_waves(int D, int rows, int pieces) { return D == 64 ? (pieces == 3 ? 3 : rows == 32 ? 2 : 4) : rows == 4 || (rows == 8 && pieces == 1) ? 3 : 2; }
 constexpr int split_stages(int D, int rows, int pieces) { return D == 128 && split_waves(D, rows, pieces) == 3 ? 2 : 4; }
 template <typename T, int D, int PARTS, int NT, int PIECES>
 __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(split_waves(D, 16 * NT / PARTS, PIECES)))) void cache4_split_kernel(Cache4Params A) {
@@ -403,6 +403,7 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
             sc[nt][b][v] = add_parts<PARTS>(z);
           }
       }
+      if constexpr (NT > 1) __builtin_amdgcn_sched_barrier(0);
       reader.values(values, slot);
       reader.steps(v_step, slot, true);
       if (u0 + 31 > ta || (last - u0 >= P.window && u0 + 31 >= P.sinks) || have != ~0u) {
@@ -424,7 +425,6 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
             for (int o = 0; o < OWN; ++o)
               if (!(have >> (16 * b + 4 * qd + v) & 1)) v_step[b][v][o] = 0.f;
       }
-      bf16x8 w[NT][OWN][PIECES];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float mx = -__builtin_inff();
@@ -455,17 +455,8 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
-            const float e = fast_exp2(__builtin_fmaf(sc[nt][b][v], P.scale_log2e, neg[nt]));
-            l[nt] += e;
-#pragma unroll
-            for (int o = 0; o < OWN; ++o) {
-              float y = e * v_step[b][v][o];
-#pragma unroll
-              for (int p = 0; p < PIECES; ++p) {
-                w[nt][o][p][4 * b + v] = (bf16)y;
-                y -= (float)w[nt][o][p][4 * b + v];
-              }
-            }
+            sc[nt][b][v] = fast_exp2(__builtin_fmaf(sc[nt][b][v], P.scale_log2e, neg[nt]));
+            l[nt] += sc[nt][b][v];
           }
       }
       // levels of two keys side by side in a byte: even and odd tiles' (a word's nibble t is element 16 t + l16)
@@ -476,6 +467,23 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
         even[j] = (a & 0x0f0f0f0fu) | (b << 4 & 0xf0f0f0f0u);
         odd[j] = (a >> 4 & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u);
       }
+      bf16x8 w[NT][PIECES];
+      auto weights = [&](auto oc) __attribute__((always_inline)) {  // probabilities times the steps of one of the lane's groups
+        constexpr int O = decltype(oc)::value;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              float y = sc[nt][b][v] * v_step[b][v][O];
+#pragma unroll
+              for (int p = 0; p < PIECES; ++p) {
+                w[nt][p][4 * b + v] = (bf16)y;
+                y -= (float)w[nt][p][4 * b + v];
+              }
+            }
+      };
       auto tile = [&](auto tc) __attribute__((always_inline)) {
         constexpr int TT = decltype(tc)::value;
         bf16x8 op;
@@ -488,12 +496,21 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int p = PIECES - 1; p >= 0; --p) acc[nt][TT] = mfma16(op, w[nt][TT / 2 % OWN][p], acc[nt][TT]);
+          for (int p = PIECES - 1; p >= 0; --p) acc[nt][TT] = mfma16(op, w[nt][p], acc[nt][TT]);
       };
-      tile(std::integral_constant<int, 0>()); tile(std::integral_constant<int, 1>()); tile(std::integral_constant<int, 2>()); tile(std::integral_constant<int, 3>());
-      if constexpr (D == 128) {
-        tile(std::integral_constant<int, 4>()); tile(std::integral_constant<int, 5>()); tile(std::integral_constant<int, 6>()); tile(std::integral_constant<int, 7>());
-      }
+      auto group = [&](auto oc) __attribute__((always_inline)) {  // groups O, O + OWN, ..: two tiles each
+        constexpr int O = decltype(oc)::value;
+        if constexpr (NT > 1) __builtin_amdgcn_sched_barrier(0);  // (one group's numbers at a time: all of them spill)
+        weights(oc);
+        tile(std::integral_constant<int, 2 * O>());
+        tile(std::integral_constant<int, 2 * O + 1>());
+        if constexpr (O + OWN < GROUPS) { tile(std::integral_constant<int, 2 * (O + OWN)>()); tile(std::integral_constant<int, 2 * (O + OWN) + 1>()); }
+        if constexpr (O + 2 * OWN < GROUPS) { tile(std::integral_constant<int, 2 * (O + 2 * OWN)>()); tile(std::integral_constant<int, 2 * (O + 2 * OWN) + 1>()); }
+        if constexpr (O + 3 * OWN < GROUPS) { tile(std::integral_constant<int, 2 * (O + 3 * OWN)>()); tile(std::integral_constant<int, 2 * (O + 3 * OWN) + 1>()); }
+      };
+      group(std::integral_constant<int, 0>());
+      if constexpr (OWN > 1) group(std::integral_constant<int, 1>());
+      if constexpr (OWN > 2) { group(std::integral_constant<int, 2>()); group(std::integral_constant<int, 3>()); }
     };
 
     // the query operands must have landed before the strips' loads start: from there on only those are in flight, and waited for by hand
@@ -760,7 +777,9 @@ static Cache4Plan plan_cache4(const sb_cache4* c, const sb_chunk* n, int window,
     const int64_t longest = std::min<int64_t>(n->max_length, (int64_t)c->max_pages * c->page_size);
     return (std::min(in_window, longest) + tile - 1) / tile;
   };
-  p.rows = most <= 4 && D == 128 ? 4 : most <= 8 ? 8 : f32 || most <= 16 ? 16 : 32;
+  // (32 rows a tile cost 1.55 to 1.9 times what 16 do: two tiles' worth where their number is even, three in two would not pay.  8 sequences of 20000, 32/8 heads, 64 rows: 144 -> 112 us;
+  // 64 of 500 to 8000, 28/4 heads, 35 rows: 96 us in tiles of 16, 99 of 32.)
+  p.rows = most <= 4 && D == 128 ? 4 : most <= 8 ? 8 : f32 || (most + 15) / 16 % 2 != 0 ? 16 : 32;
   if (f32) p.few = items(most, p.rows);
   else if (G <= kFewRows4 && (S > 1 || most <= kFewRows4)) p.few = items(std::min<int64_t>(most, kFewRows4), p.rows);
   p.splits = 1;
