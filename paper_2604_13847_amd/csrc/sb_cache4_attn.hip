@@ -167,8 +167,8 @@ template <int PARTS> __device__ inline float add_parts(float x) {
   return x;
 }
 
-// The work of few rows as one stream of strips: sequence by sequence, KV head by head, tile of rows by tile, the strips that any row of the sequence sees.  (A tile's own strips are a
-// part of these, from the first on.)  Every workgroup takes as many neighbouring strips as the others, whatever the lengths, which only the device knows; where that
+// The work as one stream of strips (of TILE keys): sequence by sequence, KV head by head, tile of rows by tile, as many strips as any tile of the sequence has.  (A tile's own are the
+// first of these.)  Every workgroup takes as many neighbouring strips as the others, whatever the lengths, which only the device knows; where that
 // cuts an item, its parts are joined by a launch that follows.  Only a workgroup's first and last items can be cut, so two places a workgroup hold all parts.
 // Counted in units of 2^unit strips, so that 31 bits hold the stream.  Where P.splits is 1, an item counts as one unit, and a workgroup has whole items.
 // (64 sequences of 500 to 32768 tokens: items of 2048 keys, whose number goes by the longest sequence, left 3 of 4 workgroups without work: 175 us, 155 as a stream.)
@@ -177,7 +177,7 @@ struct Item {
   int g;
   int first, count;  // units of the stream
 };
-template <int ROWS>
+template <int ROWS, int TILE>
 struct Stream {
   int row0, n, pos0, tiles, count;  // of sequence base + lane
   __device__ inline int size(const WindowParams& P) const { return tiles * count * P.Hkv; }
@@ -190,12 +190,15 @@ struct Stream {
       pos0 = P.cached[base + lane];
       row0 = min(max(row0, 0), P.T);
       n = min(max(min(n, P.T) - row0, 0), P.max_new);
-      if (n * P.G > P.rows_to) n = 0;
+      if (n * P.G < P.rows_from || n * P.G > P.rows_to) n = 0;
       pos0 = min(max(pos0, 0), 0x7fffffff - n);
     }
     if (n > 0) {
       tiles = (int)(((unsigned)n * (unsigned)P.G + (unsigned)ROWS - 1) / (unsigned)ROWS);
-      count = KeyTiles<32>(pos0, min(pos0 + n - 1, P.cache.max_pages * P.cache.page_size - 1), P.window, P.sinks).count();
+      count = KeyTiles<TILE>(pos0, min(pos0 + n - 1, P.cache.max_pages * P.cache.page_size - 1), P.window, P.sinks).count();
+      // and no more than fit the window of a tile's rows (of `length` tokens and keys in a row, at most) and the sinks
+      const int64_t length = (int64_t)P.window + (ROWS + P.G - 2) / P.G;
+      count = (int)min((int64_t)count, (length + TILE - 2) / TILE + 1 + ((int64_t)P.sinks + TILE - 1) / TILE);
       count = P.splits == 1 ? 1 : max((count + (1 << A.unit) - 1) >> A.unit, 1);  // (rows that see nothing have a result too)
     }
   }
@@ -275,7 +278,7 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
   loader.init(lane);
   StripReader<D, OWN> reader;
   reader.init(l16, qd, part);
-  Stream<ROWS> stream;
+  Stream<ROWS, 32> stream;
   const int share = stream.share(A, gridDim.x, NW >> A.unit > 0 ? NW >> A.unit : 1, lane);
   const int64_t x_last = (int64_t)share * (blockIdx.x + 1);
   int x_first = (int)min(x_last - share, (int64_t)0x7fffffff);  // (the stream ends before)
@@ -595,7 +598,7 @@ __global__ __launch_bounds__(512) void cache4_join_kernel(Cache4Params A) {
   const CutItem cut = A.cuts[blockIdx.x];
   const int group = threadIdx.x / D, i4 = threadIdx.x % D, r = i4 / (D / 4), c = 4 * (i4 % (D / 4));
   const int m = cut.m0 + 4 * (int)blockIdx.y + r;
-  if (cut.parts == 0) return;
+  if (cut.parts == 0 || m - r >= cut.rows) return;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
   float best = -__builtin_inff(), sum = 0.f;
   for (int z0 = group; z0 < cut.parts; z0 += NG * kRuns) {
@@ -750,10 +753,48 @@ struct ExpandedTiles {
     look_up(A, keys, src, x + 3, count);
   }
 };
+// An item a workgroup, the last tiles of rows of a sequence first; its keys in P.splits runs, joined by cache_merge_kernel.
 template <int D>
 __global__ __launch_bounds__(64 * kChunkWaves) __attribute__((amdgpu_waves_per_eu(2))) void cache4_chunk_kernel(Cache4Params A) {
   __shared__ __attribute__((aligned(1024))) char tiles[2][2][64 * D * 2];  // [buffer][K, V]
-  window_fwd_rows<D, true, kChunkWaves, ExpandedTiles<D>>(A.w, &tiles[0][0][0], A);
+  const WindowParams& P = A.w;
+  const int z = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (unsigned)P.Hkv % (unsigned)P.splits));
+  const RowTile t = locate_tile<32 * kChunkWaves, true>(P, blockIdx.x / (unsigned)P.Hkv / (unsigned)P.splits);
+  if (t.s < 0) return;
+  const int g = __builtin_amdgcn_readfirstlane((int)(blockIdx.x % (unsigned)P.Hkv));
+  const int64_t from = (int64_t)z * P.per_split, to = z < P.splits - 1 ? from + P.per_split : 0x7fffffff;
+  window_fwd_rows<D, true, kChunkWaves, ExpandedTiles<D>>(P, &tiles[0][0][0], A, t, g, threadIdx.x & 63, from, to, P.splits > 1,
+                                                          [&](int i, int h, int) __attribute__((always_inline)) { return ((int64_t)z * P.T + t.row0 + i) * P.Hq + h; });
+}
+// Equal shares of the stream of 64-key tiles.  (A kernel of its own: the loop over items costs a workgroup of one item 4 %.)
+template <int D>
+__global__ __launch_bounds__(64 * kChunkWaves) __attribute__((amdgpu_waves_per_eu(2))) void cache4_chunk_stream_kernel(Cache4Params A) {
+  constexpr int ROWS = 32 * kChunkWaves;
+  __shared__ __attribute__((aligned(1024))) char tiles[2][2][64 * D * 2];  // [buffer][K, V]
+  const int lane = threadIdx.x & 63;
+  Stream<ROWS, 64> stream;
+  const int share = stream.share(A, gridDim.x, 8, lane);
+  const int64_t x_last = (int64_t)share * (blockIdx.x + 1);
+  int x_first = (int)min(x_last - share, (int64_t)0x7fffffff);  // (the stream ends before)
+  const int x_end = (int)min(x_last, (int64_t)0x7fffffff);
+  Item item = stream.find(A, x_first, lane, true);
+  CutItem cut{};
+  while (item.t.s >= 0) {
+    const int x_next = min(x_end, item.first + item.count);
+    const bool begins = x_first == item.first, part = !begins || x_next != item.first + item.count;
+    const int64_t at = ((int64_t)blockIdx.x * 2 + begins) * ROWS;
+    int here = lane;
+    asm volatile("" : "+v"(here));  // (what follows from it stays in the loop: in front of it, it would be kept, and spilled)
+    window_fwd_rows<D, true, kChunkWaves, ExpandedTiles<D>>(A.w, &tiles[0][0][0], A, item.t, item.g, here, (int64_t)(x_first - item.first) << A.unit,
+                                                            part ? (int64_t)(x_next - item.first) << A.unit : 0x7fffffff, part,
+                                                            [&](int, int, int row) __attribute__((always_inline)) { return at + row; });
+    if (part && begins) cut = CutItem{item.t.row0, item.t.n * A.w.G, item.t.tile * ROWS, item.g, (int)((unsigned)(item.first + item.count - 1) / (unsigned)share) - (int)blockIdx.x + 1, {}};
+    x_first = x_next;
+    if (x_first >= x_end) break;
+    __syncthreads();  // the tiles' LDS is free
+    item = stream.find(A, x_first, lane, false);
+  }
+  if (threadIdx.x == 0) A.cuts[blockIdx.x] = cut;
 }
 
 // How the work is cut.  Sequences of up to kFewRows4 flattened rows are cache4_split_kernel's (float32: all of them), the others cache4_chunk_kernel's; a batch of one kind costs one launch.
@@ -763,7 +804,8 @@ struct Cache4Plan {
   int rows;               // of a tile of few rows
   int workgroups;         // of few rows; 0: whole items, a workgroup each
   int unit;
-  int splits, per_split;  // of many rows: keys in `splits` runs of per_split tiles
+  int many_workgroups;    // of many rows, in equal shares; 0: whole items, their keys in `splits` runs of per_split tiles
+  int splits, per_split;
   size_t part_lse, part_o, bytes;
 };
 static Cache4Plan plan_cache4(const sb_cache4* c, const sb_chunk* n, int window, int sinks) {
@@ -779,10 +821,15 @@ static Cache4Plan plan_cache4(const sb_cache4* c, const sb_chunk* n, int window,
   };
   // (32 rows a tile cost 1.55 to 1.9 times what 16 do: two tiles' worth where their number is even, three in two would not pay.  8 sequences of 20000, 32/8 heads, 64 rows: 144 -> 112 us;
   // 64 of 500 to 8000, 28/4 heads, 35 rows: 96 us in tiles of 16, 99 of 32.)
+  auto unit_of = [&](int64_t items, int tile) {  // see Stream
+    const int64_t strips = ((int64_t)c->max_pages * c->page_size + tile - 1) / tile + 2;  // of an item, at most
+    int unit = 0;
+    while (items * (((strips - 1) >> unit) + 1) > 0x40000000ll && unit < 26) ++unit;
+    return unit;
+  };
   p.rows = most <= 4 && D == 128 ? 4 : most <= 8 ? 8 : f32 || (most + 15) / 16 % 2 != 0 ? 16 : 32;
   if (f32) p.few = items(most, p.rows);
   else if (G <= kFewRows4 && (S > 1 || most <= kFewRows4)) p.few = items(std::min<int64_t>(most, kFewRows4), p.rows);
-  p.splits = 1;
   size_t sums = 0;
   if (p.few > 0) {
     // As many workgroups as the chip holds.  Whole items, without the launch that joins parts, where two strips a wavefront are all there is, and for float32 prompts, whose
@@ -790,19 +837,28 @@ static Cache4Plan plan_cache4(const sb_cache4* c, const sb_chunk* n, int window,
     if (tiles(p.rows, 32) > 2 * kWaves4 && !(f32 && most > kFewRows4 && p.few * c->num_kv_heads >= 4096))
       p.workgroups = 256 * split_waves(D, p.rows, f32 ? 3 : 1);
     sums = (size_t)p.workgroups * 2 * p.rows;
-    const int64_t strips = ((int64_t)c->max_pages * c->page_size + 31) / 32 + 2;  // of an item, at most
-    while (p.few * c->num_kv_heads * (((strips - 1) >> p.unit) + 1) > 0x40000000ll && p.unit < 26) ++p.unit;
+    p.unit = unit_of(p.few * c->num_kv_heads, 32);
   }
   if (!f32 && most > kFewRows4) {
     p.many = items(most, 32 * kChunkWaves);
-    // A workgroup a CU, of 8 tiles at least.
-    const int64_t all = tiles(32 * kChunkWaves, 64);
-    const int64_t per = std::max<int64_t>(((all * p.many * c->num_kv_heads + 255) / 256 + 7) / 8 * 8, 8);
-    p.splits = (int)std::max<int64_t>((all + per - 1) / per, 1);
-    p.per_split = (int)per;
-    if (p.splits > 1) sums = std::max(sums, (size_t)p.splits * n->total_new * n->num_q_heads);
+    // Very few items: their keys in runs of 8 tiles or more.  Else equal shares where the keys are mostly cached or behind a window, so that items are alike, and whole ones would not fill the
+    // chip evenly.  The others, a first prompt's, are of all lengths, the longest first, and even out by themselves.
+    //   runs, whole items and shares, in us: one chunk of 200 behind 30000, 32/8 heads 168, 1102, 191;  1000 behind 8000, one head 35, 331, 46;  two of 2000 behind 20000 and 30000,
+    //   window 8192, 28/4 heads (440 items) -, 605, 588;  three of 700 behind 5000 to 20000 1126, 765, 522;  a prompt of 6001 -, 374, 690, of 1000 77, 45, 79;  of 2000, 4/2 heads 47, 80, 81
+    const int64_t workgroups = p.many * c->num_kv_heads, rounds = (workgroups + 255) / 256, all = tiles(32 * kChunkWaves, 64);
+    p.splits = 1;
+    if (workgroups < 64) {
+      p.per_split = (int)std::max<int64_t>(((all * workgroups + 255) / 256 + 7) / 8 * 8, 8);
+      p.splits = (int)std::max<int64_t>((all + p.per_split - 1) / p.per_split, 1);
+      if (p.splits > 1) sums = std::max(sums, (size_t)p.splits * n->total_new * n->num_q_heads);
+    } else if (64 * all >= 4 * (int64_t)n->max_new && workgroups < 2048 && (8 * rounds * 256 > 9 * workgroups || (S > 1 && workgroups < 1024))) {
+      p.many_workgroups = 256;
+      p.splits = 0;
+      sums = std::max(sums, (size_t)p.many_workgroups * 2 * 32 * kChunkWaves);
+      p.unit = std::max(p.unit, unit_of(workgroups, 64));
+    }
   }
-  p.part_lse = align_up(p.workgroups * sizeof(CutItem));
+  p.part_lse = align_up(std::max(p.workgroups, p.many_workgroups) * sizeof(CutItem));
   p.part_o = align_up(p.part_lse + sums * sizeof(float));
   p.bytes = align_up(p.part_o + sums * D * sizeof(float));
   return p;
@@ -846,17 +902,19 @@ int sb_cache4_attn(const sb_cache4* c, const sb_chunk* n, int32_t window, int32_
   A.cache = make_paged(c);
   P.cache = PagedCache{nullptr, nullptr, c->page_table, c->num_pages, c->max_pages, c->page_size, A.cache.page_shift, c->num_kv_heads};
   const Cache4Plan plan = plan_cache4(c, n, window, sinks);
-  if (plan.workgroups > 0 || plan.splits > 1) {
+  if (plan.workgroups > 0 || plan.many_workgroups > 0 || plan.splits > 1) {
     if (!ws) { set_error("null argument"); return SB_ERR_INVALID_ARG; }
     A.cuts = (CutItem*)ws;
     P.part_lse = (float*)((char*)ws + plan.part_lse);
     P.part_o = (float*)((char*)ws + plan.part_o);
   }
   const bool f32 = c->dtype == SB_F32;
-  if (plan.few * P.Hkv > 0x40000000ll) { set_error("too many tiles for one launch"); return SB_ERR_UNSUPPORTED; }
+  A.unit = plan.unit;
+  if ((plan.few + plan.many) * P.Hkv > 0x40000000ll) { set_error("too many tiles for one launch"); return SB_ERR_UNSUPPORTED; }
   dim3 few_grid, many_grid, all_rows;
   if ((rc = grid_of(plan.workgroups > 0 ? plan.workgroups : plan.few * P.Hkv, 64 * kWaves4, &few_grid)) != SB_OK ||
-      (rc = grid_of(plan.many * P.Hkv * plan.splits, 64 * kChunkWaves, &many_grid)) != SB_OK || (plan.splits > 1 && (rc = grid_of((int64_t)P.T * P.Hq, 256, &all_rows)) != SB_OK))
+      (rc = grid_of(plan.many_workgroups > 0 ? plan.many_workgroups : plan.many * P.Hkv * plan.splits, 64 * kChunkWaves, &many_grid)) != SB_OK ||
+      (plan.splits > 1 && (rc = grid_of((int64_t)P.T * P.Hq, 256, &all_rows)) != SB_OK))
     return rc;
   const hipStream_t st = (hipStream_t)stream;
   KernelTimer kt(K_CACHE_ATTN, st);
@@ -864,14 +922,24 @@ int sb_cache4_attn(const sb_cache4* c, const sb_chunk* n, int32_t window, int32_
     P.splits = plan.splits; P.per_split = plan.per_split; P.part_rows = P.T;
     P.rows_from = plan.few > 0 ? kFewRows4 + 1 : 0;
     P.rows_to = 0x7fffffff;
-    if (c->head_dim == 128) hipLaunchKernelGGL((cache4_chunk_kernel<128>), many_grid, dim3(64 * kChunkWaves), 0, st, A);
-    else hipLaunchKernelGGL((cache4_chunk_kernel<64>), many_grid, dim3(64 * kChunkWaves), 0, st, A);
-    SB_LAUNCH_CHECK("cache4_chunk_kernel");
-    if (P.splits > 1 && (rc = launch_cache_merge(P, c->head_dim, c->dtype, all_rows, 0, st)) != SB_OK) return rc;
+    auto launch = [&](auto d) {
+      constexpr int DD = decltype(d)::value;
+      if (plan.many_workgroups > 0) {
+        hipLaunchKernelGGL((cache4_chunk_stream_kernel<DD>), many_grid, dim3(64 * kChunkWaves), 0, st, A);
+        SB_LAUNCH_CHECK("cache4_chunk_stream_kernel");
+        hipLaunchKernelGGL((cache4_join_kernel<bf16, DD, 32 * kChunkWaves>), dim3(plan.many_workgroups, 8 * kChunkWaves), dim3(512), 0, st, A);
+        SB_LAUNCH_CHECK("cache4_join_kernel");
+        return (int)SB_OK;
+      }
+      hipLaunchKernelGGL((cache4_chunk_kernel<DD>), many_grid, dim3(64 * kChunkWaves), 0, st, A);
+      SB_LAUNCH_CHECK("cache4_chunk_kernel");
+      return P.splits > 1 ? launch_cache_merge(P, DD, SB_BF16, all_rows, 0, st) : (int)SB_OK;
+    };
+    if ((rc = c->head_dim == 128 ? launch(std::integral_constant<int, 128>()) : launch(std::integral_constant<int, 64>())) != SB_OK) return rc;
   }
   if (plan.few > 0) {
     P.splits = plan.workgroups > 0 ? 0 : 1;
-    A.unit = plan.unit;
+    P.rows_from = 0;
     P.rows_to = f32 ? 0x7fffffff : kFewRows4;
     auto launch = [&](auto ty, auto d, auto rows, auto pieces) {
       typedef decltype(ty) Type;

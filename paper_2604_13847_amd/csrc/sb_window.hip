@@ -390,7 +390,13 @@ __global__ __launch_bounds__(256) void window_dkv_f32_join_kernel(WindowParams P
 template <int D, bool PAGED>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void window_fwd_kernel(WindowParams P) {
   __shared__ __attribute__((aligned(1024))) char tiles[2][2][64 * D * 2];  // [buffer][K, V]
-  window_fwd_rows<D, PAGED, kWaves, LoadedTiles<D, PAGED>>(P, &tiles[0][0][0], P);
+  const int splits = PAGED ? P.splits : 1, z = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (unsigned)P.Hkv % (unsigned)splits));
+  const RowTile t = locate_tile<32 * kWaves, PAGED>(P, blockIdx.x / (unsigned)P.Hkv / (unsigned)splits);
+  if (t.s < 0) return;
+  const int g = __builtin_amdgcn_readfirstlane((int)(blockIdx.x % (unsigned)P.Hkv));
+  const int64_t from = (int64_t)z * P.per_split, to = z < splits - 1 ? from + P.per_split : 0x7fffffff;
+  window_fwd_rows<D, PAGED, kWaves, LoadedTiles<D, PAGED>>(P, &tiles[0][0][0], P, t, g, threadIdx.x & 63, from, to, splits > 1,
+                                                           [&](int i, int h, int) __attribute__((always_inline)) { return ((int64_t)z * P.T + t.row0 + i) * P.Hq + h; });
 }
 
 // ---------------------------------------------------------------------------------------------

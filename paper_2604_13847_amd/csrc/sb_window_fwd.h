@@ -58,16 +58,14 @@ struct LoadedTiles {
   }
 };
 
-// A workgroup's 32 WAVES flattened rows, walked over their tiles.  `tiles`: LDS [2][2][64 * D * 2], tile x of the walk in buffer (x - begin) % 2, K and V.
-template <int D, bool PAGED, int WAVES, typename Tiles, typename Params>
-__device__ __attribute__((always_inline)) inline void window_fwd_rows(const WindowParams& P, char* tiles, const Params& params) {
+// A workgroup's 32 WAVES flattened rows of KV head g, walked over tiles from .. to - 1 (those of them that there are) of their keys.  `tiles`: LDS [2][2][64 * D * 2], tile x of the walk in
+// buffer (x - begin) % 2, K and V.  part: these are not all tiles that the rows see; what they add up to goes to row place(token, head, row of these) of part_o and part_lse.
+template <int D, bool PAGED, int WAVES, typename Tiles, typename Params, typename Place>
+__device__ __attribute__((always_inline)) inline void window_fwd_rows(const WindowParams& P, char* tiles, const Params& params, const RowTile& t, int g, int lane, int64_t from, int64_t to, bool part,
+                                                                      Place place) {
   constexpr int ROWS = 32 * WAVES, ROW_B = D * 2, TILE_B = 64 * ROW_B, NOP = D / 16;
   constexpr float kLazy = 8.0f;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
-  const int splits = PAGED ? P.splits : 1, z = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (unsigned)P.Hkv % (unsigned)splits));
-  const RowTile t = locate_tile<ROWS, PAGED>(P, blockIdx.x / (unsigned)P.Hkv / (unsigned)splits);
-  if (t.s < 0) return;
-  const int g = __builtin_amdgcn_readfirstlane((int)(blockIdx.x % (unsigned)P.Hkv));
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, hf = lane >> 5;
   const int rows = t.n * P.G, mb = t.tile * ROWS, mw = mb + 32 * wave;
   auto token = [&](int m) { return (int)((unsigned)min(m, rows - 1) / (unsigned)P.G); };
   const int i = token(mw + l32), h = g * P.G + min(mw + l32, rows - 1) - i * P.G, pos = t.pos0 + i;
@@ -77,8 +75,7 @@ __device__ __attribute__((always_inline)) inline void window_fwd_rows(const Wind
   const int wa = position(mw), wb = position(mw + 31);  // this wavefront's
   const bool working = mw < rows;
   const KeyTiles<64> keys(ta, tb, P.window, P.sinks);
-  const int begin = PAGED ? (int)min((int64_t)z * P.per_split, (int64_t)keys.count()) : 0;
-  const int count = PAGED && z < splits - 1 ? min(begin + P.per_split, keys.count()) : keys.count();
+  const int begin = PAGED ? (int)min(from, (int64_t)keys.count()) : 0, count = PAGED ? (int)min(to, (int64_t)keys.count()) : keys.count();
   KeySource<D, PAGED> src;
   src.init(P, t, g, max(0, ta - P.window + 1), tb + 1);
   const unsigned tiles0 = lds_offset(tiles);
@@ -208,9 +205,9 @@ __device__ __attribute__((always_inline)) inline void window_fwd_rows(const Wind
   l += __shfl_xor(l, 32, 64);  // the two lane halves hold different keys of the same row
   // (a sum that is no number is not one that saw nothing; in a packed batch a sum of zero makes O what it makes LSE: 0 / 0)
   const float inv = PAGED && l == 0.f ? 0.f : 1.0f / l;
-  if (PAGED && splits > 1) {
+  if (PAGED && part) {
     if (mw + l32 >= rows) return;
-    const int64_t row = ((int64_t)z * P.T + t.row0 + i) * P.Hq + h;
+    const int64_t row = place(i, h, 32 * wave + l32);
     if (hf == 0) P.part_lse[row] = l == 0.f ? -__builtin_inff() : m * P.scale_log2e + __builtin_log2f(l);
     if (l != 0.f) store_column<D>(P.part_o + row * D, oacc, inv, hf);
     return;
