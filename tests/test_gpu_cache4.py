@@ -139,6 +139,16 @@ def test_append_of_what_is_hard_to_round():
     assert float(((held - v).abs() / step.repeat_interleave(32, -1))[:, 1].max()) <= 1.0 + 2.0 ** -5 * 6
 
 
+def test_what_is_not_turned_is_not_touched():
+    """Infinities and negative zeros beside elements that are: in the same pair of a lane, and in the same eight."""
+    x = Served4([5], [3], 1, 1, 64, 16, "f32", fill=False)
+    for rot, layout in ((22, 1), (30, 1), (22, 0), (48, 0)):
+        q = normal(1, 3, 1, 64, dtype=torch.float32)
+        q[0, 0, rot:], q[1, 0, rot:], q[2, 0, rot:] = INF, -0.0, float("nan")
+        qn = sb.sb_cache4_append(x.cache, x.chunk, q, q, rope=sb.Rope(rot, layout=layout), q=q)
+        assert torch.equal(qn[..., rot:].view(torch.int32), q[..., rot:].view(torch.int32)) and bool(torch.isfinite(qn[..., :rot]).all())
+
+
 def test_append_from_slices_and_without_queries():
     D = 128
     x, y = (Served4([10, 0], [5, 30], 4, 2, D, 16, fill=False) for _ in range(2))
@@ -180,6 +190,37 @@ MORE = [([0], [1], 1, 1, 64, 16, NONE, 0), ([31, 32, 33, 127, 128, 129], [1] * 6
 @pytest.mark.parametrize("have,new,Hq,Hkv,D,page,window,sinks", SERVED + MORE)
 def test_attention(have, new, Hq, Hkv, D, page, window, sinks, dtype):
     Served4(have, new, Hq, Hkv, D, page, dtype, spare_rows=3, spare_pages=2).check(window, sinks)
+
+
+# equal shares of tiles (items alike, uneven), with windows and sinks, chunks of unequal lengths and single tokens beside them; keys in runs; whole items
+CHUNKS = [([2600, 2000, 3001], [400, 399, 130], 16, 8, 128, 64, NONE, 0), ([2600, 2000, 3001], [400, 399, 401], 16, 8, 64, 16, 900, 70), ([3000, 2500, 100, 2900], [300, 300, 1, 77], 24, 8, 128, 32, 500, 5),
+          ([9000], [150], 4, 2, 128, 16, NONE, 0), ([0, 0], [700, 650], 16, 8, 128, 16, NONE, 0), ([1], [1300], 8, 1, 64, 64, 200, 300)]
+
+
+@pytest.mark.parametrize("have,new,Hq,Hkv,D,page,window,sinks", CHUNKS)
+def test_chunks(have, new, Hq, Hkv, D, page, window, sinks):
+    x = Served4(have, new, Hq, Hkv, D, page, spare_rows=2, spare_pages=1)
+    a = x.check(window, sinks)
+    b = x.attend(window, sinks)
+    assert torch.equal(a[0][: x.rows], b[0][: x.rows]) and torch.equal(a[1][:, : x.rows], b[1][:, : x.rows])
+
+
+def test_chunks_without_pages():
+    x = Served4([2600, 2000, 3001], [400, 399, 130], 16, 8, 128, 64)
+    x.table[0, 7], x.table[0, 46], x.table[2, 0] = -1, 10 ** 8, -7
+    x.table[1] = -1
+    gone = {0: (7, 46), 1: range(999), 2: (0,)}
+    o, lse = x.check(there=lambda s, u: torch.tensor([int(i) // 64 not in gone[s] for i in u], device=DEV))
+    rows = slice(x.cu[1], x.cu[2])
+    assert float(o[rows].abs().max()) == 0 and bool((lse[:, rows] == -INF).all())
+
+
+@pytest.mark.parametrize("dtype,spare_pages", [("bf16", 0), ("f32", 0), ("bf16", 1 << 19)])
+def test_many_sequences(dtype, spare_pages):
+    """More sequences than a wavefront has lanes, most of them short, one long; and with so wide a table that strips are counted by fours."""
+    have = [(37 * i) % 150 for i in range(300)]
+    have[211] = 3000
+    Served4(have, [i % 3 for i in range(300)], 16, 8, 64, 64, dtype, spare_rows=2, spare_pages=spare_pages).check()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
