@@ -658,35 +658,60 @@ constexpr int kChunkWaves = 8;
 template <int D>
 struct ExpandedTiles {
   static constexpr int GROUPS = D / 32, TILE_B = 64 * D * 2;
-  const unsigned char* codes;  // of page 0, this KV head
-  const bf16* steps;
+  unsigned long long codes;  // of page 0, this KV head
+  unsigned long long steps;
   unsigned code[GROUPS], step[GROUPS / 2];
-  unsigned at;   // where the lane's elements go in a tile
-  int row, part; // of the tile; of the row
+  unsigned at;     // where the lane's elements go in a tile
+  int row, part;   // of the tile; of the row
   bool value;
-  int page;      // of this wavefront's rows in the tile that is loaded next
+  int page;        // of this wavefront's rows in the tile that is loaded next
+  int pages[4];    // of the 16 rows each of the tile that is worked on next, as the table has them
   __device__ inline void init(const Cache4Params& A, const RowTile& t, const KeySource<D, true>& src, int g, int wave, int lane, unsigned tiles0) {
     value = wave >= 4;
-    codes = (value ? A.cache.v : A.cache.k) + ((int64_t)g << A.cache.page_shift) * (D / 2);
-    steps = (value ? A.cache.v_step : A.cache.k_step) + ((int64_t)g << A.cache.page_shift) * GROUPS;
+    codes = (unsigned long long)(value ? A.cache.v : A.cache.k) + ((unsigned long long)g << A.cache.page_shift) * (D / 2);
+    steps = (unsigned long long)(value ? A.cache.v_step : A.cache.k_step) + ((unsigned long long)g << A.cache.page_shift) * (GROUPS * 2);
     row = 16 * (wave & 3) + (lane >> 2);
     part = lane & 3;
     at = tiles0 + (value ? TILE_B : 0) + row * (D * 2);
   }
   __device__ __attribute__((always_inline)) inline int first_row(const KeyTiles<64>& keys, int x) const { return 64 * keys.at(x) + __builtin_amdgcn_readfirstlane(row & ~15); }
-  // page of this wavefront's rows of tile x, or -1: there are none that a row sees
+  // An entry of the sequence's row of the page table, whatever it says; behind the row's end its last one
+  __device__ __attribute__((always_inline)) inline int entry(const Cache4Params& A, const KeySource<D, true>& src, int u) const {
+    if (A.cache.max_pages == 0) return -1;
+    return ((const __attribute__((address_space(4))) int32_t*)(uintptr_t)src.pages)[min(u >> A.cache.page_shift, A.cache.max_pages - 1)];
+  }
+  // page of this wavefront's rows of tile x; used, and looked at, a tile later
   __device__ __attribute__((always_inline)) inline void look_up(const Cache4Params& A, const KeyTiles<64>& keys, const KeySource<D, true>& src, int x, int count) {
-    page = -1;
-    if (x >= count) return;
-    const int u = first_row(keys, x);
-    if (u < src.end && (u + 16 > src.lo || u < A.w.sinks)) page = src.page_of(A.w, u);
+    page = entry(A, src, first_row(keys, min(x, count - 1)));
+  }
+  __device__ __attribute__((always_inline)) inline void look_up_all(const Cache4Params& A, const KeyTiles<64>& keys, const KeySource<D, true>& src, int x, int count) {
+    const int u = 64 * keys.at(min(x, count - 1));
+    pages[0] = entry(A, src, u);
+    if (A.cache.page_size < 64)
+#pragma unroll
+      for (int i = 1; i < 4; ++i) pages[i] = entry(A, src, u + 16 * i);
+  }
+  // bit i: keys 16 i .. + 15 of the tile have no page
+  __device__ __attribute__((always_inline)) inline unsigned missing(const Cache4Params& A, const KeyTiles<64>& keys, const KeySource<D, true>& src, int x) const {
+    const int u = 64 * keys.at(x);
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int p = A.cache.page_size < 64 ? pages[i] : pages[0];
+      if (u + 16 * i >= src.end || (unsigned)p >= (unsigned)A.cache.num_pages) m |= 1u << i;
+    }
+    return m;
   }
   // codes of tile x (its page is known); rows that are not there are zeros
   __device__ __attribute__((always_inline)) inline void load(const Cache4Params& A, const KeyTiles<64>& keys, const KeySource<D, true>& src, int x) {
     const int u = first_row(keys, x);
-    const int64_t from = (((int64_t)(unsigned)max(page, 0) * A.cache.Hkv) << A.cache.page_shift) + (u & (A.cache.page_size - 1));
-    const unsigned rows = page < 0 ? 0u : (unsigned)min(max(src.end - u, 0), 16);
-    const Rsrc rc = resource(codes + from * (D / 2), rows * (D / 2)), rs = resource(steps + from * GROUPS, rows * GROUPS * 2);
+    const bool any = u < src.end && (u + 16 > src.lo || u < A.w.sinks) && (unsigned)page < (unsigned)A.cache.num_pages;
+    const unsigned long long from = (((unsigned long long)(unsigned)(any ? page : 0) * A.cache.Hkv) << A.cache.page_shift) + (u & (A.cache.page_size - 1));
+    const unsigned rows = __builtin_amdgcn_readfirstlane(any ? min(src.end - u, 16) : 0);
+    auto scalar = [](unsigned long long a) __attribute__((always_inline)) {  // (else a loop over the lanes' resources, which are all the same)
+      return (const void*)(((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(a >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)a));
+    };
+    const Rsrc rc = resource(scalar(codes + from * (D / 2)), rows * (D / 2)), rs = resource(scalar(steps + from * (GROUPS * 2)), rows * GROUPS * 2);
     const int r = row & 15;
     if constexpr (D == 128) {
       const u32x4 y = __builtin_amdgcn_raw_buffer_load_b128(rc, r * (D / 2) + part * (D / 8), 0, 0);
@@ -740,6 +765,7 @@ struct ExpandedTiles {
   __device__ __attribute__((always_inline)) inline void start(const Cache4Params& A, const KeyTiles<64>& keys, const KeySource<D, true>& src, int begin, int count) {
     if (begin >= count) return;
     look_up(A, keys, src, begin, count);
+    look_up_all(A, keys, src, begin, count);
     load(A, keys, src, begin);
     look_up(A, keys, src, begin + 1, count);
     expand(0);
@@ -751,6 +777,7 @@ struct ExpandedTiles {
     if (x + 1 < count) expand((x + 1 - begin) & 1);
     if (x + 2 < count) load(A, keys, src, x + 2);
     look_up(A, keys, src, x + 3, count);
+    look_up_all(A, keys, src, x + 1, count);
   }
 };
 // An item a workgroup, the last tiles of rows of a sequence first; its keys in P.splits runs, joined by cache_merge_kernel.

@@ -48,6 +48,9 @@ struct LoadedTiles {
     loader.issue(src.k + o, there, slot);
     loader.issue(src.v + o, there, slot + TILE_B);
   }
+  __device__ __attribute__((always_inline)) inline unsigned missing(const WindowParams& P, const KeyTiles<64>& keys, const KeySource<D, PAGED>& src, int x) const {
+    return src.missing(P, 64 * keys.at(x));
+  }
   __device__ __attribute__((always_inline)) inline void start(const WindowParams& P, const KeyTiles<64>& keys, const KeySource<D, PAGED>& src, int begin, int count) const {
     if (begin < count) issue(P, keys, src, begin, begin);
   }
@@ -188,7 +191,7 @@ __device__ __attribute__((always_inline)) inline void window_fwd_rows(const Wind
   };
   auto visit = [&](auto buf_c, int x) __attribute__((always_inline)) {
     const int u0 = 64 * keys.at(x);
-    const unsigned missing = src.missing(P, u0);
+    const unsigned missing = source.missing(params, keys, src, x);
     source.arrive(params, keys, src, x, begin, count);  // tile x is there for everyone; everyone is done with tile x - 1
     const bool none = !working || u0 > wb || (wa - (u0 + 63) >= P.window && u0 >= P.sinks);
     const bool all = u0 + 63 <= wa && (wb - u0 < P.window || u0 + 63 < P.sinks) && missing == 0;
