@@ -3,6 +3,12 @@
 //   S_tu = scale sum_c step_uc (sum over d in group c of q_td n_ud),   O_td = sum_u (P_tu step_uc) m_ud   (c: d's group)
 //
 // n and m, the levels of keys and values, are exact as operands of matrix instructions; steps are applied in float32, to the scores of a group's product and to the probabilities.
+//
+// Few new tokens (cache4_split_kernel): bound by the cache's bytes, 80 a token and KV head each for K and V at head_dim 128.  64 sequences of 500 to 32768 tokens, 32/8 heads: 134 us with
+// the join, 4.2 TB/s (what such bytes take at the rate of a copy: 114; without the arithmetic 124, without the loads 89).  One of 4097: 13.9 us, two launches' latency.  In float32 each product
+// is three of bfloat16.
+// Many (cache4_chunk_kernel, cache4_chunk_stream_kernel): bound by the matrix and vector instructions of a tile.  2 x 2000 tokens behind 20000 and 30001, window 8192, 28/4 heads: 518 us,
+// 853 TFLOP/s; a prompt of 6001, 32/8 heads: 338 us, 873 TFLOP/s.
 #include <math.h>
 
 #include <algorithm>
@@ -171,7 +177,7 @@ template <int PARTS> __device__ inline float add_parts(float x) {
 // first of these.)  Every workgroup takes as many neighbouring strips as the others, whatever the lengths, which only the device knows; where that
 // cuts an item, its parts are joined by a launch that follows.  Only a workgroup's first and last items can be cut, so two places a workgroup hold all parts.
 // Counted in units of 2^unit strips, so that 31 bits hold the stream.  Where P.splits is 1, an item counts as one unit, and a workgroup has whole items.
-// (64 sequences of 500 to 32768 tokens: items of 2048 keys, whose number goes by the longest sequence, left 3 of 4 workgroups without work: 175 us, 155 as a stream.)
+// (64 sequences of 500 to 32768 tokens, before the strips went through LDS: items of 2048 keys, whose number goes by the longest sequence, left 3 of 4 workgroups without work: 175 us, 155 as a stream.)
 struct Item {
   RowTile t;
   int g;
@@ -252,6 +258,9 @@ struct Stream {
     return none;
   }
 };
+
+// Parts of a cut item that begins in this workgroup and has the stream's unit `last`.  (No more than there are workgroups from here on, whatever cu_new says.)
+__device__ inline int parts_of(int last, int share) { return (int)min((unsigned)last / (unsigned)share, gridDim.x - 1) - (int)blockIdx.x + 1; }
 
 // An item is up to 16 NT / PARTS flattened rows of a KV head; a wavefront takes every NW-th of the workgroup's strips of it through its own ring in LDS, without any barrier, the next ones on their
 // way while one is worked on.  PIECES: a query and a probability as that many bfloat16 numbers.
@@ -579,7 +588,7 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
         *(f32x4*)(P.part_o + at * D + 4 * c) = x;
       }
     }
-    if (!whole && x_first == item.first) cut = CutItem{t.row0, rows, m0, g, (int)((unsigned)(item.first + item.count - 1) / (unsigned)share) - (int)blockIdx.x + 1, {}};
+    if (!whole && x_first == item.first) cut = CutItem{t.row0, rows, m0, g, parts_of(item.first + item.count - 1, share), {}};
     x_first = x_next;
     if (x_first >= x_end) break;
     __syncthreads();  // the sums' LDS is free
@@ -805,7 +814,7 @@ __global__ __launch_bounds__(64 * kChunkWaves) __attribute__((amdgpu_waves_per_e
     window_fwd_rows<D, true, kChunkWaves, ExpandedTiles<D>>(A.w, &tiles[0][0][0], A, item.t, item.g, here, (int64_t)(x_first - item.first) << A.unit,
                                                             part ? (int64_t)(x_next - item.first) << A.unit : 0x7fffffff, part,
                                                             [&](int, int, int row) __attribute__((always_inline)) { return at + row; });
-    if (part && begins) cut = CutItem{item.t.row0, item.t.n * A.w.G, item.t.tile * ROWS, item.g, (int)((unsigned)(item.first + item.count - 1) / (unsigned)share) - (int)blockIdx.x + 1, {}};
+    if (part && begins) cut = CutItem{item.t.row0, item.t.n * A.w.G, item.t.tile * ROWS, item.g, parts_of(item.first + item.count - 1, share), {}};
     x_first = x_next;
     if (x_first >= x_end) break;
     __syncthreads();  // the tiles' LDS is free
@@ -815,6 +824,7 @@ __global__ __launch_bounds__(64 * kChunkWaves) __attribute__((amdgpu_waves_per_e
 }
 
 // How the work is cut.  Sequences of up to kFewRows4 flattened rows are cache4_split_kernel's (float32: all of them), the others cache4_chunk_kernel's; a batch of one kind costs one launch.
+// 8 sequences of 20000 tokens, 32/8 heads, with 32, 64, 96 and 128 rows: 72, 113, 150 and 190 us by the first, 146, 150, 153 and 160 by the second.
 constexpr int kFewRows4 = 64;
 struct Cache4Plan {
   int64_t few, many;      // tiles of rows; 0: no such launch
@@ -836,7 +846,7 @@ static Cache4Plan plan_cache4(const sb_cache4* c, const sb_chunk* n, int window,
     const int64_t longest = std::min<int64_t>(n->max_length, (int64_t)c->max_pages * c->page_size);
     return (std::min(in_window, longest) + tile - 1) / tile;
   };
-  // (32 rows a tile cost 1.55 to 1.9 times what 16 do: two tiles' worth where their number is even, three in two would not pay.  8 sequences of 20000, 32/8 heads, 64 rows: 144 -> 112 us;
+  // (32 rows a tile cost 1.55 to 1.9 times what 16 do: two tiles' worth where their number is even, three in two would not pay.  8 sequences of 20000, 32/8 heads, 64 rows: 144 us in tiles of 16, 113 of 32;
   // 64 of 500 to 8000, 28/4 heads, 35 rows: 96 us in tiles of 16, 99 of 32.)
   auto unit_of = [&](int64_t items, int tile) {  // see Stream
     const int64_t strips = ((int64_t)c->max_pages * c->page_size + tile - 1) / tile + 2;  // of an item, at most
@@ -860,8 +870,8 @@ static Cache4Plan plan_cache4(const sb_cache4* c, const sb_chunk* n, int window,
     p.many = items(most, 32 * kChunkWaves);
     // Very few items: their keys in runs of 8 tiles or more.  Else equal shares where the keys are mostly cached or behind a window, so that items are alike, and whole ones would not fill the
     // chip evenly.  The others, a first prompt's, are of all lengths, the longest first, and even out by themselves.
-    //   runs, whole items and shares, in us: one chunk of 200 behind 30000, 32/8 heads 168, 1102, 191;  1000 behind 8000, one head 35, 331, 46;  two of 2000 behind 20000 and 30000,
-    //   window 8192, 28/4 heads (440 items) -, 605, 588;  three of 700 behind 5000 to 20000 1126, 765, 522;  a prompt of 6001 -, 374, 690, of 1000 77, 45, 79;  of 2000, 4/2 heads 47, 80, 81
+    //   runs, whole items and shares, in us: one chunk of 200 behind 30000, 32/8 heads 149, 912, 163;  1000 behind 8000, one head 33, 274, 42;  two of 2000 behind 20000 and 30000,
+    //   window 8192, 28/4 heads (440 items) -, 544, 522;  three of 700 behind 5000 to 20000 1021, 638, 454;  a prompt of 6001 -, 342, 587, of 1000 76, 40, 75;  of 2000, 4/2 heads 46, 67, 59
     const int64_t workgroups = p.many * c->num_kv_heads, rounds = (workgroups + 255) / 256, all = tiles(32 * kChunkWaves, 64);
     p.splits = 1;
     if (workgroups < 64) {

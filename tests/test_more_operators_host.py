@@ -142,6 +142,20 @@ def test_cache_refusals(cache, chunk, code, text):
     refused(append(c, n), code, text)
 
 
+def test_append_overlaps():
+    """5 new tokens of 4 query and 2 KV heads of 128 in bfloat16: 5120 and 2560 bytes."""
+    c, n = serving({}, dict(total_new=5, num_q_heads=4))
+    for out, size in (("qo", 5120), ("kh", 2560), ("vh", 2560)):
+        at = dict(k=C.c_void_p(1 << 20), v=C.c_void_p(2 << 20), q=C.c_void_p(3 << 20), qo=C.c_void_p(4 << 20), kh=C.c_void_p(5 << 20), vh=C.c_void_p(6 << 20))
+        for other, there in (("k", 2560), ("v", 2560), ("q", 5120), ("qo", 5120), ("kh", 2560), ("vh", 2560)):
+            if other == out:
+                continue
+            for place in (at[other].value - size + 16, at[other].value, at[other].value + there - 16):
+                refused(append(c, n, **{**at, out: C.c_void_p(place)}), -1, "in the place of inputs or of each other")
+    # a slice of a fused projection: what lies between its tokens counts
+    refused(append(c, n, k=C.c_void_p(1 << 20), kp=4096, v=C.c_void_p(2 << 20), kh=C.c_void_p((1 << 20) + 4 * 8192)), -1, "in the place of inputs")
+
+
 def test_append_refusals():
     c, n = serving()
     r, a = sb.Rope(128).ref(), sb.RopeAxes((32, 32)).ref()
