@@ -165,8 +165,10 @@ struct StripReader {
     }
   }
 };
-// over the columns of a row: lanes that differ in the lowest bits.  (The same in all of them, bit for bit.)
+// over the columns of a row: lanes that differ in the lowest bits.  The same in all of them, bit for bit: columns that disagreed about the maximum of their row would be relative to different
+// references.  So x is rounded first: as a sum of products, of which one is rounded and the other is not, it would depend on whose is the lane's own.
 template <int PARTS> __device__ inline float add_parts(float x) {
+  if constexpr (PARTS > 1) asm("" : "+v"(x));
   auto swapped = [](float y, auto ctrl) { return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(y), decltype(ctrl)::value, 0xf, 0xf, false)); };
   if constexpr (PARTS >= 2) x += swapped(x, std::integral_constant<int, 0xb1>());  // 1, 0, 3, 2
   if constexpr (PARTS >= 4) x += swapped(x, std::integral_constant<int, 0x4e>());  // 2, 3, 0, 1

@@ -271,6 +271,45 @@ def test_what_is_no_number(new):
     assert bool(torch.isnan(o[0, 3]).all()) and torch.equal(o[0, :2], before[0][0, :2])
 
 
+def between():
+    """Products p0 = y0 k0 and p1 = y1 k1 of whole numbers times 2^-24 and steps of six bits, whose sum in float32 is 8 if p1 alone is rounded before it, and the next number if p0 alone is."""
+    rng = np.random.default_rng(5)
+    exact = lambda y, k: float(y) * 2.0 ** -24 * float(k)  # 24 and 6 bits: exact in float64, as the sums below are
+    while True:
+        k0, k1 = rng.integers(48, 64) / 64.0, rng.integers(33, 63) / 64.0
+        y0 = int(rng.integers(int(5.0 / k0 * 2 ** 24), int(5.9 / k0 * 2 ** 24))) & ~7
+        y1 = int((8.0 + 2.0 ** -21 - exact(y0, k0)) / k1 * 2 ** 24) & ~3
+        for z1 in range(y1 - 8, y1 + 12, 4):
+            p0, p1 = exact(y0, k0), exact(z1, k1)
+            if np.float32(p0 + float(np.float32(p1))) <= 8 < np.float32(p1 + float(np.float32(p0))) and z1 < 2 ** 26:
+                return y0, k0, z1, k1
+
+
+@pytest.mark.parametrize("D,Hq", [(128, 4), (128, 8), (64, 8)])
+def test_columns_of_a_row_agree(D, Hq):
+    """Where a row is several columns of a product, each with groups of its own, all of them have to follow the row's maximum alike, also where the order of their sums decides whether it
+    is followed."""
+    y0, k0, y1, k1 = between()
+    x = Served4([255], [1], Hq, 1, D, 16, seed=3)
+    x.codes[0].zero_()
+    x.x[0][0].zero_()
+    half = 32 if Hq == 4 or D == 64 else 64  # a column's elements
+    p, u = int(x.table[0, 130 // 16]), 130 % 16  # (the second strip of its wavefront)
+    code = torch.zeros(1, 1, D, dtype=torch.long, device=DEV)
+    code[..., :32], code[..., half: half + 32] = 2, 2  # levels of 1
+    x.codes[0][p, :, u] = plain.pack(code, False)[0]
+    x.steps[0][p, :, u] = 1.0
+    x.steps[0][p, :, u, 0], x.steps[0][p, :, u, half // 32] = k0, k1
+    x.x[0][0][130] = plain.value(code, x.steps[0][p, :, u][None])[0]
+    x.q.zero_()
+    for y, at in ((y0, 0), (y1, half)):  # eight bits an element
+        for e in range(4):
+            x.q[0, :, at + e] = float(y >> 8 * e & 255) * 2.0 ** (8 * e - 24)
+    scale = next(s for s in (np.float32(0.6931472) + np.float32(i * 2.0 ** -24) for i in range(-8, 9)) if np.float32(s * np.float32(1.4426950408889634)) == 1)
+    x.chunk = sb.Chunk(x.cu_dev, x.cached, Hq, 1, 1, 256, softmax_scale=float(scale))
+    x.check(scale=float(scale))
+
+
 def test_scores_of_minus_infinity_and_far_apart():
     """Steps so large that scores overflow, rows all of whose scores are -infinity, and scores thousands apart."""
     x = Served4([40], [3], 2, 1, 64, 16, "f32")
