@@ -4,9 +4,9 @@
 //
 // n and m, the levels of keys and values, are exact as operands of matrix instructions; steps are applied in float32, to the scores of a group's product and to the probabilities.
 //
-// Few new tokens (cache4_split_kernel): bound by the cache's bytes, 80 a token and KV head each for K and V at head_dim 128.  64 sequences of 500 to 32768 tokens, 32/8 heads: 134 us with
-// the join, 4.2 TB/s (what such bytes take at the rate of a copy: 114; without the arithmetic 124, without the loads 89).  One of 4097: 13.9 us, two launches' latency.  In float32 each product
-// is three of bfloat16.
+// Few new tokens (cache4_split_kernel): bound by the cache's bytes, 80 a token and KV head each for K and V at head_dim 128.  64 sequences of 500 to 32768 tokens, 32/8 heads: 130 us with
+// the join, 4.3 TB/s (such bytes at the rate of a copy: 113); head_dim 64: 78 (57), where the arithmetic of a strip is not all hidden.  One of 4097: 13.9 us, two launches' latency.  In float32
+// each product is three of bfloat16.
 // Many (cache4_chunk_kernel, cache4_chunk_stream_kernel): bound by the matrix and vector instructions of a tile.  2 x 2000 tokens behind 20000 and 30001, window 8192, 28/4 heads: 518 us,
 // 853 TFLOP/s; a prompt of 6001, 32/8 heads: 338 us, 873 TFLOP/s.
 #include <math.h>
@@ -33,6 +33,7 @@ struct Cache4Params {
 typedef __amdgpu_buffer_rsrc_t Rsrc;
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 __device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 // byte SEL of x, two levels, as bfloat16: lower half first
 template <int SEL> __device__ inline bf16x2 levels(unsigned x) { return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, 1.0f, SEL); }
@@ -42,6 +43,27 @@ __device__ inline bf16x8 levels8(unsigned x) {
 }
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 __device__ inline Rsrc resource(const void* base, unsigned bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x20000); }
+// Eight numbers as PIECES bfloat16 numbers each: one, rounded, or three of eight significant bits that add up to it.
+template <int PIECES> __device__ __attribute__((always_inline)) inline void pieces_of(const float (&x)[8], bf16x8 (&to)[PIECES]) {
+  if constexpr (PIECES == 1) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) to[0][e] = (bf16)x[e];
+  } else {
+    u32x4 y[PIECES];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float a = x[2 * e], b = x[2 * e + 1];
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) {
+        y[p][e] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);  // their upper halves
+        a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
+        b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) to[p] = __builtin_bit_cast(bf16x8, y[p]);
+  }
+}
 template <int SEL> __device__ inline f32x2 numbers(unsigned x) { return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, 1.0f, SEL); }
 __device__ inline float step_at(unsigned pair, int i) { return __uint_as_float(i & 1 ? pair & 0xffff0000u : pair << 16); }
 
@@ -105,6 +127,7 @@ template <int D, int OWN>
 struct StripReader {
   static constexpr int GROUPS = D / 32, CODES = StripLoader<D>::CODES, STEPS = StripLoader<D>::STEPS;
   unsigned k_at, v_at, s_at;
+  unsigned mine;  // OWN == 1: the bytes of the lane's own step, of a key's (zeros below them); OWN == 2: which half of them
   __device__ inline void init(int l16, int qd, int part) {
     if constexpr (D == 128) {
       k_at = l16 * 64 + 16 * (qd ^ (l16 >> 2));
@@ -113,7 +136,8 @@ struct StripReader {
       k_at = l16 * 32 + qd * 8;
       v_at = CODES + qd * 128 + l16 * 2;
     }
-    s_at = 2 * CODES + qd * 4 * GROUPS * 2 + part * OWN * 2;
+    s_at = 2 * CODES + qd * 4 * GROUPS * 2;
+    mine = OWN == 1 ? 0x01000c0cu + 0x02020000u * part : part;
   }
   template <typename V> static __device__ __attribute__((always_inline)) inline V at(unsigned a) { return *(const V __attribute__((address_space(3)))*)(uintptr_t)a; }
   __device__ __attribute__((always_inline)) inline void keys(unsigned (&k)[2][GROUPS], unsigned slot) const {  // [b][c]
@@ -125,41 +149,43 @@ struct StripReader {
       for (int c = 0; c < GROUPS; ++c) k[b][c] = y[c];
     }
   }
-  __device__ __attribute__((always_inline)) inline void values(unsigned (&v)[8], unsigned slot) const {  // word l16 of slot j's key (head_dim 64: 16 bits)
+  // Word l16 of slot j's key (head_dim 64: 16 bits).  v: those of slots 0, 1, .. 7 (head_dim 64: of 0 and 2, 1 and 3, 4 and 6, 5 and 7)
+  static constexpr int WORDS = D / 16;
+  __device__ __attribute__((always_inline)) inline void values(unsigned (&v)[WORDS], unsigned slot) const {
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if constexpr (D == 128) v[4 * b + j] = at<unsigned>(slot + v_at + b * (CODES / 2) + 256 * j);
-        else v[4 * b + j] = at<unsigned short>(slot + v_at + b * (CODES / 2) + 32 * j);
+      for (int j = 0; j < WORDS / 2; ++j) {
+        const unsigned from = slot + v_at + b * (CODES / 2);
+        if constexpr (D == 128) v[4 * b + j] = at<unsigned>(from + 256 * j);
+        else v[2 * b + j] = __builtin_bit_cast(unsigned, u16x2{at<unsigned short>(from + 32 * j), at<unsigned short>(from + 32 * (j + 2))});
       }
   }
-  // of keys 16 b + 4 qd + v: steps of the lane's own groups
+  // of keys 16 b + 4 qd + v: steps of the lane's own groups.  16 bytes at a time, all groups', of which a lane keeps its own
   __device__ __attribute__((always_inline)) inline void steps(float (&to)[2][4][OWN], unsigned slot, bool of_values) const {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const unsigned from = slot + s_at + (of_values ? STEPS : 0) + b * (STEPS / 2);
-      if constexpr (OWN == 1) {
+      unsigned x[2 * GROUPS];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) to[b][v][0] = __uint_as_float((unsigned)at<unsigned short>(from + v * GROUPS * 2) << 16);
-      } else if constexpr (OWN == GROUPS) {  // all of them: 16 bytes at a time
-        unsigned x[2 * GROUPS];
+      for (int i = 0; i < GROUPS / 2; ++i) {
+        const u32x4 y = at<u32x4>(from + 16 * i);
 #pragma unroll
-        for (int i = 0; i < GROUPS / 2; ++i) {
-          const u32x4 y = at<u32x4>(from + 16 * i);
+        for (int e = 0; e < 4; ++e) x[4 * i + e] = y[e];
+      }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[4 * i + e] = y[e];
-        }
+      for (int v = 0; v < 4; ++v) {
+        const unsigned* const of = x + v * GROUPS / 2;  // key v's
+        if constexpr (OWN == 1) {
+          to[b][v][0] = __uint_as_float(__builtin_amdgcn_perm(of[GROUPS / 2 - 1], of[0], mine));
+        } else if constexpr (OWN == GROUPS) {
 #pragma unroll
-        for (int v = 0; v < 4; ++v)
-#pragma unroll
-          for (int o = 0; o < OWN; ++o) to[b][v][o] = step_at(x[(v * GROUPS + o) / 2], o);
-      } else {
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const unsigned y = at<unsigned>(from + v * GROUPS * 2);
-#pragma unroll
-          for (int o = 0; o < OWN; ++o) to[b][v][o] = step_at(y, o);
+          for (int o = 0; o < OWN; ++o) to[b][v][o] = step_at(of[o / 2], o);
+        } else {
+          static_assert(OWN == 2 && GROUPS == 4, "a lane's own two groups are a word");
+          const unsigned y = mine ? of[1] : of[0];
+          to[b][v][0] = step_at(y, 0);
+          to[b][v][1] = step_at(y, 1);
         }
       }
     }
@@ -169,9 +195,10 @@ struct StripReader {
 // references.  So x is rounded first: as a sum of products, of which one is rounded and the other is not, it would depend on whose is the lane's own.
 template <int PARTS> __device__ inline float add_parts(float x) {
   if constexpr (PARTS > 1) asm("" : "+v"(x));
-  auto swapped = [](float y, auto ctrl) { return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(y), decltype(ctrl)::value, 0xf, 0xf, false)); };
+  auto swapped = [](float y, auto ctrl) { return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(y), decltype(ctrl)::value, 0xf, 0xf, true)); };  // (so written, it becomes part of the sum)
   if constexpr (PARTS >= 2) x += swapped(x, std::integral_constant<int, 0xb1>());  // 1, 0, 3, 2
   if constexpr (PARTS >= 4) x += swapped(x, std::integral_constant<int, 0x4e>());  // 2, 3, 0, 1
+  if constexpr (PARTS > 1) asm("" : "+v"(x));  // (moved behind a branch, the sum would not be one instruction)
   return x;
 }
 
@@ -267,10 +294,14 @@ __device__ inline int parts_of(int last, int share) { return (int)min((unsigned)
 // An item is up to 16 NT / PARTS flattened rows of a KV head; a wavefront takes every NW-th of the workgroup's strips of it through its own ring in LDS, without any barrier, the next ones on their
 // way while one is worked on.  PIECES: a query and a probability as that many bfloat16 numbers.
 constexpr int kWaves4 = 4;
-// Wavefronts of a SIMD, by registers, and stages of a ring, so that the rings of as many workgroups fit a CU.  64 sequences of 500 to 32768 tokens, 32/8 heads: 150 us with two wavefronts
-// and four stages, 136 with three and two (124 without the arithmetic, 89 without the loads), 139 with four, which spill.
-constexpr int split_waves(int D, int rows, int pieces) { return D == 64 ? (pieces == 3 ? 3 : rows == 32 ? 2 : 4) : rows == 4 || (rows == 8 && pieces == 1) ? 3 : 2; }
-constexpr int split_stages(int D, int rows, int pieces) { return D == 128 && split_waves(D, rows, pieces) == 3 ? 2 : 4; }
+// Wavefronts of a SIMD, as many as the registers of a strip's numbers allow, and stages of a ring, so that the rings of as many workgroups fit a CU: what a strip takes is one product, sum and
+// exponential after the other, which other wavefronts have to fill.  64 sequences of 500 to 32768 tokens, 32/8 heads, with one wavefront less and with these: head_dim 128 134 and 130 us,
+// head_dim 64 84 and 78 (and with one more, which spills, 102); float32, 28/4 heads, 500 to 8000: 47 and 42.
+constexpr int split_waves(int D, int rows, int pieces) {
+  if (D == 64) return pieces == 3 ? (rows == 8 ? 4 : 3) : rows == 8 ? 5 : rows == 16 ? 4 : 2;
+  return rows == 4 && pieces == 1 ? 4 : rows <= 8 ? 3 : 2;
+}
+constexpr int split_stages(int D, int rows, int pieces) { return split_waves(D, rows, pieces) >= (D == 64 ? 5 : 3) ? 2 : 4; }
 template <typename T, int D, int PARTS, int NT, int PIECES>
 __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(split_waves(D, 16 * NT / PARTS, PIECES)))) void cache4_split_kernel(Cache4Params A) {
   const WindowParams& P = A.w;
@@ -357,15 +388,10 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
         if constexpr (PIECES == 1) {
           qf[nt][c][0] = *(const bf16x8*)(q + 32 * c);
         } else {
+          float y[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            float y = (float)q[32 * c + e];
-#pragma unroll
-            for (int p = 0; p < PIECES; ++p) {
-              qf[nt][c][p][e] = (bf16)y;
-              y -= (float)qf[nt][c][p][e];
-            }
-          }
+          for (int e = 0; e < 8; ++e) y[e] = (float)q[32 * c + e];
+          pieces_of<PIECES>(y, qf[nt][c]);
         }
 #pragma unroll
         for (int p = 0; p < PIECES; ++p)
@@ -385,7 +411,8 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
 
     auto work = [&](int x) __attribute__((always_inline)) {
       const unsigned slot = ring0 + (x & (STAGES - 1)) * SLOT;
-      unsigned keys[2][GROUPS], values[8];
+      constexpr int WORDS = StripReader<D, OWN>::WORDS;
+      unsigned keys[2][GROUPS], values[WORDS];
       float k_step[2][4][OWN], v_step[2][4][OWN];
       reader.keys(keys, slot);
       reader.steps(k_step, slot, false);
@@ -474,9 +501,9 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
           }
       }
       // levels of two keys side by side in a byte: even and odd tiles' (a word's nibble t is element 16 t + l16)
-      unsigned even[4], odd[4];
+      unsigned even[WORDS / 2], odd[WORDS / 2];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < WORDS / 2; ++j) {
         const unsigned a = values[2 * j], b = values[2 * j + 1];
         even[j] = (a & 0x0f0f0f0fu) | (b << 4 & 0xf0f0f0f0u);
         odd[j] = (a >> 4 & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u);
@@ -485,25 +512,20 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
       auto weights = [&](auto oc) __attribute__((always_inline)) {  // probabilities times the steps of one of the lane's groups
         constexpr int O = decltype(oc)::value;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
+          float y[8];
 #pragma unroll
-          for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              float y = sc[nt][b][v] * v_step[b][v][O];
-#pragma unroll
-              for (int p = 0; p < PIECES; ++p) {
-                w[nt][p][4 * b + v] = (bf16)y;
-                y -= (float)w[nt][p][4 * b + v];
-              }
-            }
+          for (int j = 0; j < 8; ++j) y[j] = sc[nt][j / 4][j % 4] * v_step[j / 4][j % 4][O];
+          pieces_of<PIECES>(y, w[nt]);
+        }
       };
       auto tile = [&](auto tc) __attribute__((always_inline)) {
         constexpr int TT = decltype(tc)::value;
         bf16x8 op;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const bf16x2 y = levels<TT / 2>(TT & 1 ? odd[j] : even[j]);
+          const unsigned from = TT & 1 ? odd[j * WORDS / 8] : even[j * WORDS / 8];
+          const bf16x2 y = D == 128 || j % 2 == 0 ? levels<TT / 2>(from) : levels<(TT / 2 + 2) % 4>(from);
           op[2 * j] = y[0];
           op[2 * j + 1] = y[1];
         }

@@ -38,7 +38,7 @@ def test_waits_of_the_chunks(functions):
 
 
 def test_loads_of_the_strips(functions):
-    """An asynchronous load's place is set right in front of it, five wait states before it; no kernel spills but that of 32 rows, and that one outside its loop over strips."""
+    """An asynchronous load's place is set right in front of it, five wait states before it; what does not fit the registers is kept in memory outside the loop over strips only."""
     seen = 0
     for name, lines in functions.items():
         if "split" not in name:
@@ -51,11 +51,8 @@ def test_loads_of_the_strips(functions):
             assert text[i - 1] == "s_nop 4" and text[i - 2].startswith("s_mov_b32 m0"), text[i - 3: i + 1]
         products = [i for i, l in enumerate(text) if l.startswith("v_mfma")]
         spills = [i for i, l in enumerate(text) if l.startswith("scratch_")]
-        if "Li128ELi1ELi2ELi1E" in name:
-            # between a strip's first product and its last, nothing is kept in memory
-            assert not [i for i in spills if products[0] < i < products[-1]], name
-        else:
-            assert not spills, name
+        # (loads of spilled numbers would be waited for together with the strips': none between a strip's first product and its last)
+        assert len(spills) <= 20 and not [i for i in spills if products[0] < i < products[-1]], name
         seen += 1
     assert seen == 12
 
@@ -77,7 +74,7 @@ else:
     c = sb.sb_cache4(1 << 20, 64, Hkv, D, dtype, length // 64 + 1, 4096, 4096, 4096, 4096, 4096)
     n = sb.sb_chunk(S, Hq, total, most, length, 0.0, 4096, 4096)
     if kind == "append":
-        sb._check(lib.sb_cache4_append(C.byref(c), C.byref(n), sb.Rope(D).ref(), None, None, b, z, b, z, b, z, C.c_void_p(8192), None, None, None))
+        sb._check(lib.sb_cache4_append(C.byref(c), C.byref(n), sb.Rope(D).ref(), None, None, b, z, b, z, b, z, C.c_void_p(1 << 50), None, None, None))
     else:
         sb._check(lib.sb_cache4_attn(C.byref(c), C.byref(n), window, 0, b, b, b, b, None))
 out = np.zeros((256, 6), dtype=np.uint32)
@@ -102,14 +99,14 @@ def launches(tmp_path_factory):
 
 def test_launches_of_few_rows(launches):
     # as many workgroups as the chip holds, whatever the lengths, and their parts joined four rows a workgroup
-    assert launches("attn", 1, 1, 1, 4098, 32, 8, 128, 0, NONE) == [("cache4_split_kernel", 768, 1), ("cache4_join_kernel", 768, 1)]
-    assert launches("attn", 64, 64, 1, 32769, 32, 8, 128, 0, NONE) == [("cache4_split_kernel", 768, 1), ("cache4_join_kernel", 768, 1)]
+    assert launches("attn", 1, 1, 1, 4098, 32, 8, 128, 0, NONE) == [("cache4_split_kernel", 1024, 1), ("cache4_join_kernel", 1024, 1)]
+    assert launches("attn", 64, 64, 1, 32769, 32, 8, 128, 0, NONE) == [("cache4_split_kernel", 1024, 1), ("cache4_join_kernel", 1024, 1)]
     assert launches("attn", 64, 128, 2, 32769, 32, 8, 128, 0, NONE) == [("cache4_split_kernel", 768, 1), ("cache4_join_kernel", 768, 2)]       # 8 rows
     assert launches("attn", 64, 64, 1, 32769, 16, 1, 128, 0, NONE) == [("cache4_split_kernel", 512, 1), ("cache4_join_kernel", 512, 4)]         # 16
     assert launches("attn", 64, 512, 8, 32769, 32, 8, 128, 0, NONE) == [("cache4_split_kernel", 512, 1), ("cache4_join_kernel", 512, 8)]        # 32
     assert launches("attn", 64, 320, 5, 32769, 28, 4, 128, 0, NONE) == [("cache4_split_kernel", 512, 1), ("cache4_join_kernel", 512, 4)]        # 35: three tiles of 16
-    assert launches("attn", 64, 64, 1, 32769, 32, 8, 64, 0, NONE) == [("cache4_split_kernel", 1024, 1), ("cache4_join_kernel", 1024, 2)]
-    assert launches("attn", 64, 64, 1, 32769, 32, 8, 64, 1, NONE) == [("cache4_split_kernel", 768, 1), ("cache4_join_kernel", 768, 2)]
+    assert launches("attn", 64, 64, 1, 32769, 32, 8, 64, 0, NONE) == [("cache4_split_kernel", 1280, 1), ("cache4_join_kernel", 1280, 2)]
+    assert launches("attn", 64, 64, 1, 32769, 32, 8, 64, 1, NONE) == [("cache4_split_kernel", 1024, 1), ("cache4_join_kernel", 1024, 2)]
     # two strips a wavefront, or a window of that: whole items, nothing to join
     assert launches("attn", 64, 64, 1, 256, 32, 8, 128, 0, NONE) == [("cache4_split_kernel", 512, 1)]
     assert launches("attn", 64, 64, 1, 1 << 20, 32, 8, 128, 0, 100) == [("cache4_split_kernel", 512, 1)]
