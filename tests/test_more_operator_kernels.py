@@ -52,7 +52,7 @@ def test_loads_of_the_strips(functions):
         products = [i for i, l in enumerate(text) if l.startswith("v_mfma")]
         spills = [i for i, l in enumerate(text) if l.startswith("scratch_")]
         # (loads of spilled numbers would be waited for together with the strips': none between a strip's first product and its last)
-        assert len(spills) <= 20 and not [i for i in spills if products[0] < i < products[-1]], name
+        assert len(spills) <= 24 and not [i for i in spills if products[0] < i < products[-1]], name
         seen += 1
     assert seen == 12
 
