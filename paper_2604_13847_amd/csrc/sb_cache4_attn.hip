@@ -883,10 +883,10 @@ static Cache4Plan plan_cache4(const sb_cache4* c, const sb_chunk* n, int window,
   else if (G <= kFewRows4 && (S > 1 || most <= kFewRows4)) p.few = items(std::min<int64_t>(most, kFewRows4), p.rows);
   size_t sums = 0;
   if (p.few > 0) {
-    // As many workgroups as the chip holds.  Whole items, without the launch that joins parts, where two strips a wavefront are all there is, and for float32 prompts, whose
+    // As many workgroups as the chip holds, or as have a strip a wavefront if sequences are as long as they may be.  Whole items, without the launch that joins parts, where two strips a wavefront are all there is, and for float32 prompts, whose
     // items are many and alike.
     if (tiles(p.rows, 32) > 2 * kWaves4 && !(f32 && most > kFewRows4 && p.few * c->num_kv_heads >= 4096))
-      p.workgroups = 256 * split_waves(D, p.rows, f32 ? 3 : 1);
+      p.workgroups = (int)std::min<int64_t>(256 * split_waves(D, p.rows, f32 ? 3 : 1), (p.few * c->num_kv_heads * tiles(p.rows, 32) + kWaves4 - 1) / kWaves4);
     sums = (size_t)p.workgroups * 2 * p.rows;
     p.unit = unit_of(p.few * c->num_kv_heads, 32);
   }

@@ -46,7 +46,7 @@ def test_loads_of_the_strips(functions):
         text = [l.split(";")[0].strip() for l in lines]
         text = [l for l in text if l and not l.startswith(".")] 
         loads = [i for i, l in enumerate(text) if l.startswith("global_load_lds")]
-        assert len(loads) >= 12
+        assert len(loads) >= 6
         for i in loads:
             assert text[i - 1] == "s_nop 4" and text[i - 2].startswith("s_mov_b32 m0"), text[i - 3: i + 1]
         products = [i for i, l in enumerate(text) if l.startswith("v_mfma")]
@@ -98,8 +98,8 @@ def launches(tmp_path_factory):
 
 
 def test_launches_of_few_rows(launches):
-    # as many workgroups as the chip holds, whatever the lengths, and their parts joined four rows a workgroup
-    assert launches("attn", 1, 1, 1, 4098, 32, 8, 128, 0, NONE) == [("cache4_split_kernel", 1024, 1), ("cache4_join_kernel", 1024, 1)]
+    # as many workgroups as the chip holds, or as there are strips at most, and their parts joined four rows a workgroup
+    assert launches("attn", 1, 1, 1, 4098, 32, 8, 128, 0, NONE) == [("cache4_split_kernel", 258, 1), ("cache4_join_kernel", 258, 1)]  # 8 x 129 strips, four at a time
     assert launches("attn", 64, 64, 1, 32769, 32, 8, 128, 0, NONE) == [("cache4_split_kernel", 1024, 1), ("cache4_join_kernel", 1024, 1)]
     assert launches("attn", 64, 128, 2, 32769, 32, 8, 128, 0, NONE) == [("cache4_split_kernel", 768, 1), ("cache4_join_kernel", 768, 2)]       # 8 rows
     assert launches("attn", 64, 64, 1, 32769, 16, 1, 128, 0, NONE) == [("cache4_split_kernel", 512, 1), ("cache4_join_kernel", 512, 4)]         # 16
