@@ -621,61 +621,68 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
   if (P.splits != 1 && threadIdx.x == 0) A.cuts[blockIdx.x] = cut;  // every workgroup, so that nothing of an earlier call is left
 }
 
-// Joins the parts of the items that were cut: a workgroup to four rows of an item that began in workgroup blockIdx.x of the launch before, its threads' groups every NG-th part.  A part that saw
-// nothing has LSE -infinity; one that saw what is no number has left that, and so is the row's result.
+// Joins the parts of the items that were cut: a workgroup to some rows of an item that began in workgroup blockIdx.x of the launch before, each of its NG groups of threads every NG-th part, RUNS
+// of them on their way at a time.  Few rows have many parts, so there are as many groups as there is room for beside four rows.  Chunks have two or three, and many rows, so one group takes
+// all of them (2 x 2000 tokens, 67 MB of parts: 48 us by four groups of 8 parts, 14 so).  A part that saw nothing has LSE -infinity; one that saw what is no number has left that, and so is
+// the row's result.
+constexpr int join_groups(int D, int rows) { return rows <= 32 ? 512 / D : 1; }
+constexpr int join_rows(int D, int rows) { return 4 * 512 / D / join_groups(D, rows); }  // of a workgroup
 template <typename T, int D, int ROWS>
 __global__ __launch_bounds__(512) void cache4_join_kernel(Cache4Params A) {
   const WindowParams& P = A.w;
-  constexpr int NG = 512 / D, kRuns = 8;  // on their way at a time
-  __shared__ __attribute__((aligned(16))) float sums[NG][4][D + 4];  // (and what they are relative to, their weight)
+  constexpr int NG = join_groups(D, ROWS), RUNS = NG > 1 ? 8 : 2, MINE = join_rows(D, ROWS), LANES = D / 4;
   const CutItem cut = A.cuts[blockIdx.x];
-  const int group = threadIdx.x / D, i4 = threadIdx.x % D, r = i4 / (D / 4), c = 4 * (i4 % (D / 4));
-  const int m = cut.m0 + 4 * (int)blockIdx.y + r;
+  const int group = threadIdx.x / (MINE * LANES), lane = threadIdx.x % (MINE * LANES), r = lane / LANES, c = 4 * (lane % LANES);
+  const int m = cut.m0 + MINE * (int)blockIdx.y + r;
   if (cut.parts == 0 || m - r >= cut.rows) return;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
   float best = -__builtin_inff(), sum = 0.f;
-  for (int z0 = group; z0 < cut.parts; z0 += NG * kRuns) {
-    float lse[kRuns], top = best;
-    f32x4 part[kRuns];
+  for (int z0 = group; z0 < cut.parts; z0 += NG * RUNS) {
+    float lse[RUNS], top = best;
+    f32x4 part[RUNS];
 #pragma unroll
-    for (int i = 0; i < kRuns; ++i) {  // (past the last part, it again)
+    for (int i = 0; i < RUNS; ++i) {  // (past the last part, it again)
       const int z = min(z0 + NG * i, cut.parts - 1);
-      const int64_t from = (((int64_t)blockIdx.x + z) * 2 + (z == 0)) * ROWS + 4 * blockIdx.y + r;
+      const int64_t from = (((int64_t)blockIdx.x + z) * 2 + (z == 0)) * ROWS + MINE * blockIdx.y + r;
       lse[i] = P.part_lse[from];
       part[i] = *(const f32x4*)(P.part_o + from * D + c);
       if (z0 + NG * i >= cut.parts) lse[i] = -__builtin_inff();
     }
 #pragma unroll
-    for (int i = 0; i < kRuns; ++i) top = fmaxf(top, lse[i]);
+    for (int i = 0; i < RUNS; ++i) top = fmaxf(top, lse[i]);
     const float ref = top == -__builtin_inff() ? 0.f : top;  // nothing seen yet: keep the exponents finite
     const float old = fast_exp2(best - ref);
     sum *= old;
     x *= old;
 #pragma unroll
-    for (int i = 0; i < kRuns; ++i) {
+    for (int i = 0; i < RUNS; ++i) {
       const float f = fast_exp2(lse[i] - ref);
       sum += f;
       if (lse[i] != -__builtin_inff()) x += f * part[i];
     }
     best = top;
   }
-  *(f32x4*)&sums[group][r][c] = x;
-  if (c == 0) { sums[group][r][D] = best; sums[group][r][D + 1] = sum; }
-  __syncthreads();
-  if (group > 0 || m >= cut.rows) return;
-  best = -__builtin_inff();
+  if constexpr (NG > 1) {
+    __shared__ __attribute__((aligned(16))) float sums[NG][MINE][D + 4];  // (and what they are relative to, their weight)
+    *(f32x4*)&sums[group][r][c] = x;
+    if (c == 0) { sums[group][r][D] = best; sums[group][r][D + 1] = sum; }
+    __syncthreads();
+    if (group > 0) return;
+    best = -__builtin_inff();
 #pragma unroll
-  for (int w = 0; w < NG; ++w) best = fmaxf(best, sums[w][r][D]);
-  sum = 0.f;
-  x = f32x4{0.f, 0.f, 0.f, 0.f};
-  const float ref = best == -__builtin_inff() ? 0.f : best;
+    for (int w = 0; w < NG; ++w) best = fmaxf(best, sums[w][r][D]);
+    sum = 0.f;
+    x = f32x4{0.f, 0.f, 0.f, 0.f};
+    const float ref = best == -__builtin_inff() ? 0.f : best;
 #pragma unroll
-  for (int w = 0; w < NG; ++w) {
-    const float f = fast_exp2(sums[w][r][D] - ref);
-    sum += f * sums[w][r][D + 1];
+    for (int w = 0; w < NG; ++w) {
+      const float f = fast_exp2(sums[w][r][D] - ref);
+      sum += f * sums[w][r][D + 1];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(f, sums[w][r][c + e], x[e]);
+      for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(f, sums[w][r][c + e], x[e]);
+    }
   }
+  if (m >= cut.rows) return;
   const int j = (int)((unsigned)m / (unsigned)P.G), h = cut.g * P.G + m - j * P.G, tok = cut.row0 + j;
   x *= sum == 0.f ? 0.f : 1.0f / sum;
   store4((T*)P.o + ((int64_t)tok * P.Hq + h) * D + c, x);
@@ -978,7 +985,7 @@ int sb_cache4_attn(const sb_cache4* c, const sb_chunk* n, int32_t window, int32_
       if (plan.many_workgroups > 0) {
         hipLaunchKernelGGL((cache4_chunk_stream_kernel<DD>), many_grid, dim3(64 * kChunkWaves), 0, st, A);
         SB_LAUNCH_CHECK("cache4_chunk_stream_kernel");
-        hipLaunchKernelGGL((cache4_join_kernel<bf16, DD, 32 * kChunkWaves>), dim3(plan.many_workgroups, 8 * kChunkWaves), dim3(512), 0, st, A);
+        hipLaunchKernelGGL((cache4_join_kernel<bf16, DD, 32 * kChunkWaves>), dim3(plan.many_workgroups, 32 * kChunkWaves / join_rows(DD, 32 * kChunkWaves)), dim3(512), 0, st, A);
         SB_LAUNCH_CHECK("cache4_join_kernel");
         return (int)SB_OK;
       }
@@ -998,7 +1005,7 @@ int sb_cache4_attn(const sb_cache4* c, const sb_chunk* n, int32_t window, int32_
       hipLaunchKernelGGL((cache4_split_kernel<Type, DD, ROWS < 16 ? 16 / ROWS : 1, ROWS < 16 ? 1 : ROWS / 16, decltype(pieces)::value>), few_grid, dim3(64 * kWaves4), 0, st, A);
       SB_LAUNCH_CHECK("cache4_split_kernel");
       if (plan.workgroups > 0) {
-        hipLaunchKernelGGL((cache4_join_kernel<Type, DD, ROWS>), dim3(plan.workgroups, ROWS / 4), dim3(512), 0, st, A);
+        hipLaunchKernelGGL((cache4_join_kernel<Type, DD, ROWS>), dim3(plan.workgroups, ROWS / join_rows(DD, ROWS)), dim3(512), 0, st, A);
         SB_LAUNCH_CHECK("cache4_join_kernel");
       }
       return (int)SB_OK;

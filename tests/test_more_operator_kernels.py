@@ -121,7 +121,7 @@ def test_launches_of_chunks(launches):
     assert names(1, 200, 200, 30000, 32, 8, 128, 0, NONE) == ["cache4_chunk_kernel", "cache_merge_kernel"]
     assert names(1, 1000, 1000, 1000, 32, 8, 128, 0, NONE) == ["cache4_chunk_kernel"]
     # mostly cached keys: equal shares; a batch of several may have sequences of few rows besides
-    assert launches("attn", 1, 1000, 1000, 20000, 32, 8, 128, 0, NONE) == [("cache4_chunk_stream_kernel", 256, 1), ("cache4_join_kernel", 256, 64)]
+    assert launches("attn", 1, 1000, 1000, 20000, 32, 8, 128, 0, NONE) == [("cache4_chunk_stream_kernel", 256, 1), ("cache4_join_kernel", 256, 16)]
     assert names(2, 4000, 2000, 30000, 28, 4, 128, 0, 8192) == ["cache4_chunk_stream_kernel", "cache4_join_kernel", "cache4_split_kernel", "cache4_join_kernel"]
     # rows that a tile's shares never cut: 131072 new tokens are one launch
     assert names(1, 131072, 131072, 131072, 32, 8, 128, 0, NONE) == ["cache4_chunk_kernel"]
