@@ -7,8 +7,8 @@
 // Few new tokens (cache4_split_kernel): bound by the cache's bytes, 80 a token and KV head each for K and V at head_dim 128.  64 sequences of 500 to 32768 tokens, 32/8 heads: 130 us with
 // the join, 4.3 TB/s (such bytes at the rate of a copy: 113); head_dim 64: 78 (57), where the arithmetic of a strip is not all hidden.  One of 4097: 13.9 us, two launches' latency.  In float32
 // each product is three of bfloat16.
-// Many (cache4_chunk_kernel, cache4_chunk_stream_kernel): bound by the matrix and vector instructions of a tile.  2 x 2000 tokens behind 20000 and 30001, window 8192, 28/4 heads: 518 us,
-// 853 TFLOP/s; a prompt of 6001, 32/8 heads: 338 us, 873 TFLOP/s.
+// Many (cache4_chunk_kernel, cache4_chunk_stream_kernel): bound by the matrix and vector instructions of a tile.  2 x 2000 tokens behind 20000 and 30001, window 8192, 28/4 heads: 488 us,
+// 905 TFLOP/s; a prompt of 6001, 32/8 heads: 337 us, 876 TFLOP/s.
 #include <math.h>
 
 #include <algorithm>
@@ -901,8 +901,8 @@ static Cache4Plan plan_cache4(const sb_cache4* c, const sb_chunk* n, int window,
     p.many = items(most, 32 * kChunkWaves);
     // Very few items: their keys in runs of 8 tiles or more.  Else equal shares where the keys are mostly cached or behind a window, so that items are alike, and whole ones would not fill the
     // chip evenly.  The others, a first prompt's, are of all lengths, the longest first, and even out by themselves.
-    //   runs, whole items and shares, in us: one chunk of 200 behind 30000, 32/8 heads 149, 912, 163;  1000 behind 8000, one head 33, 274, 42;  two of 2000 behind 20000 and 30000,
-    //   window 8192, 28/4 heads (440 items) -, 544, 522;  three of 700 behind 5000 to 20000 1021, 638, 454;  a prompt of 6001 -, 342, 587, of 1000 76, 40, 75;  of 2000, 4/2 heads 46, 67, 59
+    //   runs, whole items and shares, in us: one chunk of 200 behind 30000, 32/8 heads 148, 910, 154;  1000 behind 8000, one head 33, 275, 41;  two of 2000 behind 20000 and 30000,
+    //   window 8192, 28/4 heads (440 items) -, 539, 483;  three of 700 behind 5000 to 20000 1021, 636, 415;  a prompt of 6001 -, 342, 587, of 1000 76, 40, 75;  of 2000, 4/2 heads 46, 67, 59
     const int64_t workgroups = p.many * c->num_kv_heads, rounds = (workgroups + 255) / 256, all = tiles(32 * kChunkWaves, 64);
     p.splits = 1;
     if (workgroups < 64) {
