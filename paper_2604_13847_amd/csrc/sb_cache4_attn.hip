@@ -704,8 +704,7 @@ struct ExpandedTiles {
   unsigned at;     // where the lane's elements go in a tile
   int row, part;   // of the tile; of the row
   bool value;
-  unsigned page;   // of this wavefront's rows in the tile that is loaded next
-  unsigned pages;  // of rows 16 part .. + 15 of the tile that is worked on next
+  PagesAhead<D> ahead;
   __device__ inline void init(const Cache4Params& A, const RowTile& t, const KeySource<D, true>& src, int g, int wave, int lane, unsigned tiles0) {
     value = wave >= 4;
     codes = (unsigned long long)(value ? A.cache.v : A.cache.k) + ((unsigned long long)g << A.cache.page_shift) * (D / 2);
@@ -715,29 +714,20 @@ struct ExpandedTiles {
     at = tiles0 + (value ? TILE_B : 0) + row * (D * 2);
   }
   __device__ __attribute__((always_inline)) inline int first_row(const KeyTiles<64>& keys, int x) const { return 64 * keys.at(x) + __builtin_amdgcn_readfirstlane(row & ~15); }
-  // Entries of the sequence's row of the page table (behind its end: 0), used a tile later.  By vector loads: waits for scalar ones are waits for LDS too.
-  __device__ __attribute__((always_inline)) inline unsigned entry(const Cache4Params& A, const KeySource<D, true>& src, int u) const {
-    return __builtin_amdgcn_raw_buffer_load_b32(resource(src.pages, (unsigned)A.cache.max_pages * 4), (u >> A.cache.page_shift) * 4, 0, 0);
-  }
-  // of this wavefront's rows of tile x
   __device__ __attribute__((always_inline)) inline void look_up(const Cache4Params& A, const KeyTiles<64>& keys, const KeySource<D, true>& src, int x, int count) {
-    page = entry(A, src, first_row(keys, min(x, count - 1)));
+    ahead.look_up(A.w, src, first_row(keys, min(x, count - 1)));
   }
-  // of all rows of tile x, 16 a lane
   __device__ __attribute__((always_inline)) inline void look_up_all(const Cache4Params& A, const KeyTiles<64>& keys, const KeySource<D, true>& src, int x, int count) {
-    pages = entry(A, src, 64 * keys.at(min(x, count - 1)) + 16 * part);
+    ahead.look_up_all(A.w, src, 64 * keys.at(min(x, count - 1)), part);
   }
-  // bit i: keys 16 i .. + 15 of the tile have no page
   __device__ __attribute__((always_inline)) inline unsigned missing(const Cache4Params& A, const KeyTiles<64>& keys, const KeySource<D, true>& src, int x) const {
-    return (unsigned)__builtin_amdgcn_ballot_w64(64 * keys.at(x) + 16 * part >= src.end || pages >= (unsigned)A.cache.num_pages) & 15;
+    return ahead.missing(A.w, src, 64 * keys.at(x), part);
   }
   // codes of tile x (its page is known); rows that are not there are zeros
   __device__ __attribute__((always_inline)) inline void load(const Cache4Params& A, const KeyTiles<64>& keys, const KeySource<D, true>& src, int x) {
-    const int u = first_row(keys, x);
-    const unsigned mine = (unsigned)__builtin_amdgcn_readfirstlane((int)page);
-    const bool any = u < src.end && (u + 16 > src.lo || u < A.w.sinks) && mine < (unsigned)A.cache.num_pages;
-    const unsigned long long from = (((unsigned long long)(any ? mine : 0) * A.cache.Hkv) << A.cache.page_shift) + (u & (A.cache.page_size - 1));
-    const unsigned rows = __builtin_amdgcn_readfirstlane(any ? min(src.end - u, 16) : 0);
+    int there;
+    const unsigned long long from = ahead.rows_at(A.w, src, first_row(keys, x), there);
+    const unsigned rows = __builtin_amdgcn_readfirstlane(there);
     auto scalar = [](unsigned long long a) __attribute__((always_inline)) {  // (else a loop over the lanes' resources, which are all the same)
       return (const void*)(((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(a >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)a));
     };

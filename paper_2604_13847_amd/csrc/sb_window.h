@@ -174,28 +174,11 @@ struct KeySource {
     end = end_;
     lo = lo_;
   }
-  __device__ inline int page_of(const WindowParams& P, int u) const {  // of a key that is read, or -1
-    const int p = ((const __attribute__((address_space(4))) int32_t*)(uintptr_t)pages)[u >> P.cache.page_shift];
-    return (unsigned)p < (unsigned)P.cache.num_pages ? p : -1;
-  }
-  // rows u .. u + n - 1 (n <= 16, u a multiple of n): bytes from the first row, and how many exist from there on
+  // rows u .. u + n - 1 of a packed batch: bytes from the first row, and how many exist from there on
   __device__ inline unsigned long long rows_at(const WindowParams& P, int u, int n, int& rows) const {
     rows = min(end - u, n);
     if (u + n <= lo && u >= P.sinks) rows = 0;
-    if (!PAGED) return (unsigned long long)(unsigned)u * pitch;
-    if (rows <= 0) return 0;
-    const int p = page_of(P, u);
-    if (p < 0) { rows = 0; return 0; }
-    return (((unsigned long long)(unsigned)p * P.Hkv << P.cache.page_shift) + (unsigned)(u & (P.cache.page_size - 1))) * (D * 2);
-  }
-  // bit x: keys u0 + 16x .. + 15 have no page.  (Those behind `end` too: where that is the page table's end, rows behind it would take them, zeros in LDS, for keys.)
-  __device__ inline unsigned missing(const WindowParams& P, int u0) const {
-    if (!PAGED) return 0;
-    unsigned m = 0;
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-      if (u0 + 16 * x >= end || page_of(P, u0 + 16 * x) < 0) m |= 1u << x;
-    return m;
+    return (unsigned long long)(unsigned)u * pitch;
   }
 };
 

@@ -28,36 +28,81 @@ __device__ inline void store_column(T* to, const f32x16 (&acc)[D / 32], float f,
 // LSE of a row without any score above -infinity.  Over a cache it may see no key; in a packed batch it sees itself, and has no softmax: NaN, as in the block-sparse forward.
 template <bool PAGED> __device__ inline float empty_lse() { return PAGED ? -__builtin_inff() : __builtin_nanf(""); }
 
+// Pages of the tiles that come, looked up in the sequence's row of the page table (behind its end: 0) a tile before they are used.  By vector loads: waits for scalar ones are waits for LDS
+// too, and all of a tile's would be waited for.
+template <int D>
+struct PagesAhead {
+  unsigned mine;  // of this wavefront's 16 rows of the tile that is loaded next
+  unsigned all;   // lane: of rows 16 (lane % 4) .. + 15 of the tile that is worked on next
+  typedef KeySource<D, true> Source;
+  static __device__ __attribute__((always_inline)) inline unsigned entry(const WindowParams& P, const Source& src, int u) {
+    return __builtin_amdgcn_raw_buffer_load_b32(__builtin_amdgcn_make_buffer_rsrc((void*)src.pages, 0, (unsigned)P.cache.max_pages * 4, 0x20000), (u >> P.cache.page_shift) * 4, 0, 0);
+  }
+  __device__ __attribute__((always_inline)) inline void look_up(const WindowParams& P, const Source& src, int u) { mine = entry(P, src, u); }
+  __device__ __attribute__((always_inline)) inline void look_up_all(const WindowParams& P, const Source& src, int u0, int lane) { all = entry(P, src, u0 + 16 * (lane & 3)); }
+  // rows u .. u + 15, whose page is looked up: the first one's place among the pages' rows (of KV head 0), and how many exist from there on
+  __device__ __attribute__((always_inline)) inline unsigned long long rows_at(const WindowParams& P, const Source& src, int u, int& rows) const {
+    const unsigned p = (unsigned)__builtin_amdgcn_readfirstlane((int)mine);
+    const bool any = u < src.end && (u + 16 > src.lo || u < P.sinks) && p < (unsigned)P.cache.num_pages;
+    rows = any ? min(src.end - u, 16) : 0;
+    return ((unsigned long long)(any ? p : 0) * P.Hkv << P.cache.page_shift) + (unsigned)(u & (P.cache.page_size - 1));
+  }
+  // bit x: keys u0 + 16x .. + 15 have no page.  (Those behind `end` too: where that is the page table's end, rows behind it would take them, zeros in LDS, for keys.)
+  __device__ __attribute__((always_inline)) inline unsigned missing(const WindowParams& P, const Source& src, int u0, int lane) const {
+    return (unsigned)__builtin_amdgcn_ballot_w64(u0 + 16 * (lane & 3) >= src.end || all >= (unsigned)P.cache.num_pages) & 15;
+  }
+};
+struct NoPages {};
+
 // Tiles of K and V that lie in memory as the matrix instructions take them: asynchronous loads, the next tile's while one is worked on.
 template <int D, bool PAGED>
 struct LoadedTiles {
   static constexpr int TILE_B = 64 * D * 2;
   RowsLoader<D, kWaves> loader;
+  typename std::conditional<PAGED, PagesAhead<D>, NoPages>::type ahead;
   unsigned tiles0;
-  int wave;
-  __device__ inline void init(const WindowParams& P, const RowTile& t, const KeySource<D, PAGED>& src, int g, int wave_, int lane, unsigned tiles0_) {
-    loader.init(src.pitch, wave_, lane);
+  int wave, lane;
+  typedef KeySource<D, PAGED> Source;
+  static_assert(64 / kWaves == 16, "a wavefront's rows of a tile lie in one page");
+  __device__ inline void init(const WindowParams& P, const RowTile& t, const Source& src, int g, int wave_, int lane_, unsigned tiles0_) {
+    loader.init(src.pitch, wave_, lane_);
     tiles0 = tiles0_;
     wave = wave_;
+    lane = lane_;
   }
-  __device__ __attribute__((always_inline)) inline void issue(const WindowParams& P, const KeyTiles<64>& keys, const KeySource<D, PAGED>& src, int x, int begin) const {
-    const int u = 64 * keys.at(x) + 64 / kWaves * wave;
+  __device__ __attribute__((always_inline)) inline void issue(const WindowParams& P, const KeyTiles<64>& keys, const Source& src, int x, int begin) const {
+    const int u = 64 * keys.at(x) + 16 * wave;
     int there;
-    const unsigned long long o = src.rows_at(P, u, 64 / kWaves, there);
+    unsigned long long o;
+    if constexpr (PAGED) o = ahead.rows_at(P, src, u, there) * (D * 2);
+    else o = src.rows_at(P, u, 16, there);
     const unsigned slot = tiles0 + ((x - begin) & 1) * 2 * TILE_B;
     loader.issue(src.k + o, there, slot);
     loader.issue(src.v + o, there, slot + TILE_B);
   }
-  __device__ __attribute__((always_inline)) inline unsigned missing(const WindowParams& P, const KeyTiles<64>& keys, const KeySource<D, PAGED>& src, int x) const {
-    return src.missing(P, 64 * keys.at(x));
+  __device__ __attribute__((always_inline)) inline unsigned missing(const WindowParams& P, const KeyTiles<64>& keys, const Source& src, int x) const {
+    if constexpr (PAGED) return ahead.missing(P, src, 64 * keys.at(x), lane);
+    else return 0;
   }
-  __device__ __attribute__((always_inline)) inline void start(const WindowParams& P, const KeyTiles<64>& keys, const KeySource<D, PAGED>& src, int begin, int count) const {
-    if (begin < count) issue(P, keys, src, begin, begin);
+  __device__ __attribute__((always_inline)) inline void look_up(const WindowParams& P, const KeyTiles<64>& keys, const Source& src, int x, int count) {
+    if constexpr (PAGED) ahead.look_up(P, src, 64 * keys.at(min(x, count - 1)) + 16 * wave);
   }
-  __device__ __attribute__((always_inline)) inline void arrive(const WindowParams& P, const KeyTiles<64>& keys, const KeySource<D, PAGED>& src, int x, int begin, int count) const {
+  __device__ __attribute__((always_inline)) inline void look_up_all(const WindowParams& P, const KeyTiles<64>& keys, const Source& src, int x, int count) {
+    if constexpr (PAGED) ahead.look_up_all(P, src, 64 * keys.at(min(x, count - 1)), lane);
+  }
+  __device__ __attribute__((always_inline)) inline void start(const WindowParams& P, const KeyTiles<64>& keys, const Source& src, int begin, int count) {
+    if (begin >= count) return;
+    look_up(P, keys, src, begin, count);
+    issue(P, keys, src, begin, begin);
+    look_up(P, keys, src, begin + 1, count);
+    look_up_all(P, keys, src, begin, count);
+  }
+  __device__ __attribute__((always_inline)) inline void arrive(const WindowParams& P, const KeyTiles<64>& keys, const Source& src, int x, int begin, int count) {
     wait_vmcnt<0>();
     __builtin_amdgcn_s_barrier();
     if (x + 1 < count) issue(P, keys, src, x + 1, begin);
+    look_up(P, keys, src, x + 2, count);
+    look_up_all(P, keys, src, x + 1, count);
   }
 };
 
