@@ -251,40 +251,48 @@ struct Stream {
     const unsigned all = (unsigned)__builtin_amdgcn_readfirstlane(sum), each = (all + (unsigned)workgroups - 1) / (unsigned)workgroups;
     return __builtin_amdgcn_readfirstlane((int)((each + (unsigned)least - 1) / (unsigned)least * (unsigned)least));
   }
-  // the item that unit x belongs to; s < 0: there are no so many.  fresh: up to 64 sequences are loaded
-  __device__ inline Item find(const Cache4Params& A, int x, int lane, bool fresh) {
+  // The sequence that the last item found was of: where it is among the stream's units, its tiles and units of each, and the 64 that it was loaded with.  (Wave-uniform.  Its other items are
+  // found without a load, and the next sequence from there on: 600 sequences of 100 to 8000 478 -> 350 us.)
+  RowTile seq;
+  int start, end, seq_tiles, seq_count, base, before;
+  // the item that unit x belongs to; s < 0: there are no so many.  first: nothing was asked before, and up to 64 sequences are loaded; else x is no less than the last one
+  __device__ inline Item find(const Cache4Params& A, int x, int lane, bool first) {
     const WindowParams& P = A.w;
-    int before = 0;
-    for (int base = 0; base < P.S; base += 64) {
-      if (!fresh || P.S > 64) load(A, base, lane);
-      const int mine = size(P);
-      int incl = mine;
+    Item r{};
+    r.t.s = -1;
+    if (first) base = before = end = 0;
+    if (first || x >= end) {
+      for (; base < P.S; base += 64) {
+        if (!first || P.S > 64) load(A, base, lane);
+        const int mine = size(P);
+        int incl = mine;
 #pragma unroll
-      for (int off = 1; off < 64; off <<= 1)
-        if (off < P.S - base) {
-          const int y = __shfl_up(incl, off, 64);
-          if (lane >= off) incl += y;
+        for (int off = 1; off < 64; off <<= 1)
+          if (off < P.S - base) {
+            const int y = __shfl_up(incl, off, 64);
+            if (lane >= off) incl += y;
+          }
+        const unsigned long long hit = __builtin_amdgcn_ballot_w64(base + lane < P.S && x - before < incl);
+        if (hit) {
+          const int src = __builtin_ctzll(hit);
+          seq = RowTile{base + src, 0, __builtin_amdgcn_readlane(row0, src), __builtin_amdgcn_readlane(n, src), __builtin_amdgcn_readlane(pos0, src)};
+          seq_tiles = __builtin_amdgcn_readlane(tiles, src);
+          seq_count = __builtin_amdgcn_readlane(count, src);
+          start = before + __builtin_amdgcn_readlane(incl - mine, src);
+          end = before + __builtin_amdgcn_readlane(incl, src);
+          break;
         }
-      const unsigned long long hit = __builtin_amdgcn_ballot_w64(base + lane < P.S && x - before < incl);
-      if (hit) {
-        const int src = __builtin_ctzll(hit);
-        Item r;
-        r.count = __builtin_amdgcn_readlane(count, src);
-        const unsigned tiles_ = (unsigned)__builtin_amdgcn_readlane(tiles, src);
-        const int start = before + __builtin_amdgcn_readlane(incl - mine, src);
-        const unsigned item = (unsigned)(x - start) / (unsigned)r.count;
-        r.first = __builtin_amdgcn_readfirstlane(start + (int)item * r.count);
-        const unsigned g = item / tiles_;
-        r.g = __builtin_amdgcn_readfirstlane((int)g);
-        r.t = RowTile{base + src, __builtin_amdgcn_readfirstlane((int)(item - g * tiles_)), __builtin_amdgcn_readlane(row0, src), __builtin_amdgcn_readlane(n, src),
-                      __builtin_amdgcn_readlane(pos0, src)};
-        return r;
+        before += __builtin_amdgcn_readlane(incl, min(P.S - base, 64) - 1);
       }
-      before += __builtin_amdgcn_readlane(incl, min(P.S - base, 64) - 1);
+      if (base >= P.S) return r;
     }
-    Item none{};
-    none.t.s = -1;
-    return none;
+    const unsigned item = (unsigned)(x - start) / (unsigned)seq_count, g = item / (unsigned)seq_tiles;
+    r.count = seq_count;
+    r.first = __builtin_amdgcn_readfirstlane(start + (int)item * seq_count);
+    r.g = __builtin_amdgcn_readfirstlane((int)g);
+    r.t = seq;
+    r.t.tile = __builtin_amdgcn_readfirstlane((int)(item - g * (unsigned)seq_tiles));
+    return r;
   }
 };
 
@@ -880,10 +888,14 @@ static Cache4Plan plan_cache4(const sb_cache4* c, const sb_chunk* n, int window,
   else if (G <= kFewRows4 && (S > 1 || most <= kFewRows4)) p.few = items(std::min<int64_t>(most, kFewRows4), p.rows);
   size_t sums = 0;
   if (p.few > 0) {
-    // As many workgroups as the chip holds, or as have a strip a wavefront if sequences are as long as they may be.  Whole items, without the launch that joins parts, where two strips a wavefront are all there is, and for float32 prompts, whose
-    // items are many and alike.
-    if (tiles(p.rows, 32) > 2 * kWaves4 && !(f32 && most > kFewRows4 && p.few * c->num_kv_heads >= 4096))
-      p.workgroups = (int)std::min<int64_t>(256 * split_waves(D, p.rows, f32 ? 3 : 1), (p.few * c->num_kv_heads * tiles(p.rows, 32) + kWaves4 - 1) / kWaves4);
+    // Whole items, without the launch that joins parts, where a wavefront has few strips of an item, or not many and there are many items; and for float32 prompts, whose items are many and
+    // alike.  Else equal shares, for as many workgroups as the chip holds, or as have a strip a wavefront if sequences are as long as they may be: one long sequence among short ones would be
+    // waited for.
+    //   32/8 heads, equal shares and whole items, in us: one sequence of 400 14.9 and 10.8, of 1000 12.8 and 13.7, of 2000 14.9 and 21.1;  16 of 1000 19.3 and 14.0, of 2000 22.7 and 22.3;  64 of
+    //   2000 39.8 and 30.9, of 100 to 2000 32.1 and 23.9, four of 2000 and 60 of 200 21.4 and 22.3;  64 of 4000 61.9 and 53.8, of 500 to 4000 39.2 and 41.0, one of 4000 and 63 of 100 16 and 37
+    const int64_t of_wave = (tiles(p.rows, 32) + kWaves4 - 1) / kWaves4, all = p.few * c->num_kv_heads;
+    if (!(of_wave <= 8 || (of_wave <= 16 && all >= 256) || (f32 && most > kFewRows4 && all >= 4096)))
+      p.workgroups = (int)std::min<int64_t>(256 * split_waves(D, p.rows, f32 ? 3 : 1), all * of_wave);
     sums = (size_t)p.workgroups * 2 * p.rows;
     p.unit = unit_of(p.few * c->num_kv_heads, 32);
   }

@@ -99,7 +99,7 @@ def launches(tmp_path_factory):
 
 def test_launches_of_few_rows(launches):
     # as many workgroups as the chip holds, or as there are strips at most, and their parts joined four rows a workgroup
-    assert launches("attn", 1, 1, 1, 4098, 32, 8, 128, 0, NONE) == [("cache4_split_kernel", 258, 1), ("cache4_join_kernel", 258, 1)]  # 8 x 129 strips, four at a time
+    assert launches("attn", 1, 1, 1, 4098, 32, 8, 128, 0, NONE) == [("cache4_split_kernel", 264, 1), ("cache4_join_kernel", 264, 1)]  # 8 items of 33 strips a wavefront
     assert launches("attn", 64, 64, 1, 32769, 32, 8, 128, 0, NONE) == [("cache4_split_kernel", 1024, 1), ("cache4_join_kernel", 1024, 1)]
     assert launches("attn", 64, 128, 2, 32769, 32, 8, 128, 0, NONE) == [("cache4_split_kernel", 768, 1), ("cache4_join_kernel", 768, 2)]       # 8 rows
     assert launches("attn", 64, 64, 1, 32769, 16, 1, 128, 0, NONE) == [("cache4_split_kernel", 512, 1), ("cache4_join_kernel", 512, 4)]         # 16
@@ -107,7 +107,10 @@ def test_launches_of_few_rows(launches):
     assert launches("attn", 64, 320, 5, 32769, 28, 4, 128, 0, NONE) == [("cache4_split_kernel", 512, 1), ("cache4_join_kernel", 512, 4)]        # 35: three tiles of 16
     assert launches("attn", 64, 64, 1, 32769, 32, 8, 64, 0, NONE) == [("cache4_split_kernel", 1280, 1), ("cache4_join_kernel", 1280, 2)]
     assert launches("attn", 64, 64, 1, 32769, 32, 8, 64, 1, NONE) == [("cache4_split_kernel", 1024, 1), ("cache4_join_kernel", 1024, 2)]
-    # two strips a wavefront, or a window of that: whole items, nothing to join
+    # eight strips a wavefront, a window of that, or sixteen where items are many: whole items, nothing to join
+    assert launches("attn", 1, 1, 1, 1024, 32, 8, 128, 0, NONE) == [("cache4_split_kernel", 8, 1)]
+    assert launches("attn", 32, 32, 1, 2048, 32, 8, 128, 0, NONE) == [("cache4_split_kernel", 256, 1)]
+    assert len(launches("attn", 31, 31, 1, 2048, 32, 8, 128, 0, NONE)) == len(launches("attn", 32, 32, 1, 2049, 32, 8, 128, 0, NONE)) == 2
     assert launches("attn", 64, 64, 1, 256, 32, 8, 128, 0, NONE) == [("cache4_split_kernel", 512, 1)]
     assert launches("attn", 64, 64, 1, 1 << 20, 32, 8, 128, 0, 100) == [("cache4_split_kernel", 512, 1)]
     # float32 prompts: tiles of 16 rows, whole where there are many
