@@ -216,13 +216,18 @@ template <int ROWS, int TILE>
 struct Stream {
   int row0, n, pos0, tiles, count;  // of sequence base + lane
   __device__ inline int size(const WindowParams& P) const { return tiles * count * P.Hkv; }
-  __device__ inline void load(const Cache4Params& A, int base, int lane) {
+  struct Lengths { int from, to, cached; };  // as they are in memory
+  static __device__ inline Lengths fetch(const Cache4Params& A, int base, int lane) {
+    const int s = base + lane;
+    return (unsigned)s < (unsigned)A.w.S ? Lengths{A.w.cu[s], A.w.cu[s + 1], A.w.cached[s]} : Lengths{};
+  }
+  __device__ inline void take(const Cache4Params& A, const Lengths& x, int base, int lane) {
     const WindowParams& P = A.w;
     row0 = n = pos0 = tiles = count = 0;
     if (base + lane < P.S) {
-      row0 = P.cu[base + lane];
-      n = P.cu[base + lane + 1];
-      pos0 = P.cached[base + lane];
+      row0 = x.from;
+      n = x.to;
+      pos0 = x.cached;
       row0 = min(max(row0, 0), P.T);
       n = min(max(min(n, P.T) - row0, 0), P.max_new);
       if (n * P.G < P.rows_from || n * P.G > P.rows_to) n = 0;
@@ -237,17 +242,23 @@ struct Stream {
       count = P.splits == 1 ? 1 : max((count + (1 << A.unit) - 1) >> A.unit, 1);  // (rows that see nothing have a result too)
     }
   }
-  // units of a workgroup.  With up to 64 sequences, these stay loaded
+  // units of a workgroup.  With up to 64 sequences, these stay loaded.  (600 sequences of 100 to 500 tokens: 81 us with every 64 loaded when it was their turn, 66 so.)
   __device__ inline int share(const Cache4Params& A, int workgroups, int least, int lane) {
+    Lengths next = fetch(A, 0, lane);
+    if (A.w.splits == 1) {
+      if (A.w.S <= 64) take(A, next, 0, lane);
+      return 1;
+    }
     int sum = 0;
     for (int base = 0; base < A.w.S; base += 64) {
-      load(A, base, lane);
+      const Lengths x = next;
+      next = fetch(A, base + 64, lane);  // (on its way while these are worked on)
+      take(A, x, base, lane);
       sum += size(A.w);
     }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1)
       if (off < A.w.S) sum += __shfl_xor(sum, off, 64);
-    if (A.w.splits == 1) return 1;
     const unsigned all = (unsigned)__builtin_amdgcn_readfirstlane(sum), each = (all + (unsigned)workgroups - 1) / (unsigned)workgroups;
     return __builtin_amdgcn_readfirstlane((int)((each + (unsigned)least - 1) / (unsigned)least * (unsigned)least));
   }
@@ -262,8 +273,15 @@ struct Stream {
     r.t.s = -1;
     if (first) base = before = end = 0;
     if (first || x >= end) {
+      const bool loaded = first && P.S <= 64;
+      Lengths next{};
+      if (!loaded) next = fetch(A, base, lane);
       for (; base < P.S; base += 64) {
-        if (!first || P.S > 64) load(A, base, lane);
+        if (!loaded) {
+          const Lengths here = next;
+          next = fetch(A, base + 64, lane);
+          take(A, here, base, lane);
+        }
         const int mine = size(P);
         int incl = mine;
 #pragma unroll
