@@ -435,7 +435,8 @@ typedef struct sb_cache4 {
 } sb_cache4;
 
 /* sb_cache_append (axes and positions null) or sb_cache_append_axes into such pages.  r may be null only without axes.  k_held, v_held (dev, contiguous, [total_new][Hkv][D] in c->dtype, or null): the
- * values as they are held from now on, for attention over the packed tokens of a first prompt.  Outputs lie apart from the inputs and from each other (checked). */
+ * values as they are held from now on, for attention over the packed tokens of a first prompt.  q_out, k_held and v_held lie apart from each other, from all inputs and from the pages (checked); so do
+ * the pages from q, k, v and the other inputs, and the cache's arrays from each other (not checked). */
 int sb_cache4_append(const sb_cache4 *c, const sb_chunk *n, const sb_rope *r, const sb_rope_axes *axes, const int32_t *positions, const void *q, int64_t q_pitch, const void *k,
                      int64_t k_pitch, const void *v, int64_t v_pitch, void *q_out, void *k_held, void *v_held, void *stream);
 

@@ -303,6 +303,13 @@ extern "C" int sb_cache4_append(const sb_cache4* c, const sb_chunk* n, const sb_
         set_error("outputs in the place of inputs or of each other are not supported");
         return SB_ERR_INVALID_ARG;
       }
+  const int64_t rows = (int64_t)c->num_pages * Hkv * c->page_size;
+  const Range others[] = {{(const char*)c->k, rows * (D / 2)}, {(const char*)c->v, rows * (D / 2)}, {(const char*)c->k_step, rows * (D / 16)}, {(const char*)c->v_step, rows * (D / 16)},
+                          {(const char*)c->page_table, (int64_t)n->num_seqs * c->max_pages * 4}, {(const char*)n->cu_new, ((int64_t)n->num_seqs + 1) * 4},
+                          {(const char*)n->cached, (int64_t)n->num_seqs * 4}, {(const char*)positions, positions ? (int64_t)axes->num_axes * n->total_new * 4 : 0}};
+  for (const Range& w : written)
+    for (const Range& x : others)
+      if (meet(w, x)) { set_error("outputs in the place of the pages, their table, positions, cu_new or cached are not supported"); return SB_ERR_INVALID_ARG; }
   Append4Params P{};
   P.q = q; P.k = k; P.v = v; P.q_out = q_out; P.k_held = k_held; P.v_held = v_held; P.q_pitch = q_pitch; P.k_pitch = k_pitch; P.v_pitch = v_pitch;
   P.cu = n->cu_new; P.cached = n->cached; P.max_new = n->max_new; P.axis_positions = positions;

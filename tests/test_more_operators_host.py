@@ -156,6 +156,19 @@ def test_append_overlaps():
     refused(append(c, n, k=C.c_void_p(1 << 20), kp=4096, v=C.c_void_p(2 << 20), kh=C.c_void_p((1 << 20) + 4 * 8192)), -1, "in the place of inputs")
 
 
+def test_append_overlaps_of_what_is_not_a_tensor():
+    """Outputs in the place of the pages, of their steps, of the page table or of what else a call reads: 81920 bytes of codes, 10240 of steps."""
+    M = 1 << 20
+    there = dict(k=(10, 81920), v=(11, 81920), k_step=(12, 10240), v_step=(13, 10240), page_table=(14, 48), cu_new=(15, 16), cached=(16, 12), positions=(17, 2 * 20 * 4))
+    base = dict(k=C.c_void_p(1 * M), v=C.c_void_p(2 * M), q=C.c_void_p(3 * M), qo=C.c_void_p(4 * M), kh=C.c_void_p(5 * M), vh=C.c_void_p(6 * M))
+    c, n = serving({name: there[name][0] * M for name in ("k", "v", "k_step", "v_step", "page_table")}, dict(cu_new=15 * M, cached=16 * M))
+    r, a, pos = sb.Rope(128).ref(), sb.RopeAxes((32, 32)).ref(), C.c_void_p(17 * M)
+    for out, size in (("qo", 20 * 4 * 128 * 2), ("kh", 20 * 2 * 128 * 2), ("vh", 20 * 2 * 128 * 2)):
+        for name, (at, bytes_) in there.items():
+            for place in (at * M - size + 16, at * M, at * M + (bytes_ - 1) // 16 * 16):
+                refused(append(c, n, r, a, pos, **{**base, out: C.c_void_p(place)}), -1, "in the place of the pages")
+
+
 def test_append_refusals():
     c, n = serving()
     r, a = sb.Rope(128).ref(), sb.RopeAxes((32, 32)).ref()
