@@ -1,0 +1,85 @@
+"""The four-bit cache on the GPU in the forms that small calls do not take: an append of thousands of tokens, bit for bit."""
+import random
+
+import pytest
+import torch
+
+import four_bits as plain
+import operator_reference as ref
+from paper_2604_13847_amd import binding as sb
+from test_gpu_operators import DEV, TYPE, nan, normal
+from test_gpu_rope_axes import positions, turned
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------- append of many tokens
+MOST, SPARE = 48, 3  # tokens of a sequence that are taken; rows behind the last one
+
+
+def lengths(total, seed):
+    """Short sequences of all lengths, empty ones and some with more than MOST tokens among them: a wavefront's run of tokens crosses their borders everywhere."""
+    rng, out = random.Random(seed), []
+    while sum(out) < total - SPARE:
+        out.append(min(rng.choice([0, 0, 1, 1, 2, 3, 5, 17, 33, 64]), total - SPARE - sum(out)))
+    return out
+
+
+@pytest.mark.parametrize("total", [2047, 2048, 4097, 8197, 12301])
+@pytest.mark.parametrize("rot,layout,axes,dtype,Hq,Hkv,D,page,odd", [
+    (128, 0, (16, 24, 24), "bf16", 10, 5, 128, 16, False), (64, 1, None, "bf16", 9, 9, 64, 32, False), (40, 0, None, "f32", 4, 2, 128, 16, False), (48, 1, (8, 8, 8), "f32", 3, 1, 64, 64, True),
+    (None, 0, None, "bf16", 6, 2, 128, 16, True), (64, 0, (20, 12), "bf16", 2, 1, 64, 16, True)])
+def test_append_of_many_tokens(rot, layout, axes, dtype, Hq, Hkv, D, page, odd, total):
+    """Codes, steps, held values and queries of every token; what belongs to no sequence, is beyond max_new or has no page is left as it was, in the outputs or in the pages."""
+    t, new = TYPE[dtype][0], lengths(total, total + D)
+    S, rows = len(new), sum(new)
+    have = torch.randint(-2, 90, (S,), generator=torch.Generator(device=DEV).manual_seed(1), dtype=torch.int32, device=DEV)
+    count = torch.tensor(new, device=DEV)
+    cu = torch.cat([count.new_zeros(1), count.cumsum(0)]).int()
+    columns = (90 + MOST) // page + 1
+    table = torch.randperm(S * columns, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV).int().view(S, columns)
+    table[3::7, 1], table[5::11, 0] = -1, S * columns
+    codes = [torch.full((S * columns, Hkv, page, D // 2), 255, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    steps = [nan(S * columns, Hkv, page, D // 32) for _ in range(2)]
+
+    def tensor(seed, H):
+        x = normal(seed, total, H, D, dtype=t)
+        if odd:  # off a 16-byte boundary
+            y = torch.empty(x.numel() + 1, dtype=t, device=DEV)[1:].view(x.shape)
+            x = y.copy_(x)
+        return x
+    q, k, v = tensor(3, Hq), tensor(4, Hkv), tensor(5, Hkv)
+    rope = sb.Rope(rot, layout=layout) if rot else None
+    ax, pos = (sb.RopeAxes(axes), positions(6, len(axes), total, 1 << 16)) if axes else (None, None)
+    qn, held = nan(total, Hq, D, dtype=t), [nan(total, Hkv, D, dtype=t) for _ in range(2)]
+    cache, chunk = sb.Cache4(codes[0], codes[1], steps[0], steps[1], table, dtype=t), sb.Chunk(cu, have, Hq, total, MOST, 90 + MOST)
+    sb.sb_cache4_append(cache, chunk, k, v, rope=rope, axes=ax, positions=pos, q=q, q_out=qn, held=True, k_held=held[0], v_held=held[1])
+
+    of = torch.repeat_interleave(torch.arange(S, device=DEV), count)
+    i = torch.arange(rows, device=DEV) - cu[:-1][of]
+    taken, at = i < MOST, have.clamp_min(0)[of] + i
+    assert int((~taken).sum()) > 16
+    where = torch.zeros(1, total, dtype=torch.int32, device=DEV)
+    where[0, :rows] = at
+    if rope:
+        one, at_axes = ax or sb.RopeAxes((rot // 2,)), pos if axes else where
+        want_q, tol = turned(q.double(), at_axes, rope, one, layout == 0)
+        ref.check("q", qn[:rows][taken], want_q[:rows][taken], (tol + ref.HALF[t] * want_q.abs())[:rows][taken])
+        want_k = turned(k.double(), at_axes, rope, one, layout == 0)[0].float()
+    else:
+        assert torch.equal(qn[:rows][taken], q[:rows][taken])
+        want_k = k.float()
+    for x in (qn, *held):
+        assert bool(torch.isnan(x[rows:]).all()) and bool(torch.isnan(x[:rows][~taken]).all())
+    page_of = table[of, (at // page).clamp_max(columns - 1).long()].long()
+    kept = taken & (page_of >= 0) & (page_of < S * columns)
+    assert int((taken & ~kept).sum()) > 16
+    p, u = page_of[kept], (at % page).long()[kept]
+    seen = torch.zeros(S * columns, page, dtype=torch.bool, device=DEV)
+    seen[p, u] = True
+    for w, y in enumerate((want_k, v.float())):
+        step = plain.step_of(y)
+        code = plain.code_of(y, step)
+        assert torch.equal(held[w][:rows][taken].double(), plain.value(code, step)[:rows][taken])
+        assert torch.equal(codes[w][p, :, u], plain.pack(code[:rows][kept], w == 1)) and torch.equal(steps[w][p, :, u].double(), step[:rows][kept])
+        assert bool((codes[w].transpose(1, 2)[~seen] == 255).all()) and bool(torch.isnan(steps[w].transpose(1, 2)[~seen]).all())
