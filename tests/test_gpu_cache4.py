@@ -192,7 +192,7 @@ def test_attention(have, new, Hq, Hkv, D, page, window, sinks, dtype):
     Served4(have, new, Hq, Hkv, D, page, dtype, spare_rows=3, spare_pages=2).check(window, sinks)
 
 
-# equal shares of tiles (items alike, uneven), with windows and sinks, chunks of unequal lengths and single tokens beside them; keys in runs; whole items
+# equal shares of tiles; whole items with windows and sinks, chunks of unequal lengths and single tokens beside them; keys in runs, without and with a window; whole items  (equal shares with windows: cache4_forms.py)
 CHUNKS = [([2600, 2000, 3001], [400, 399, 130], 16, 8, 128, 64, NONE, 0), ([2600, 2000, 3001], [400, 399, 401], 16, 8, 64, 16, 900, 70), ([3000, 2500, 100, 2900], [300, 300, 1, 77], 24, 8, 128, 32, 500, 5),
           ([9000], [150], 4, 2, 128, 16, NONE, 0), ([0, 0], [700, 650], 16, 8, 128, 16, NONE, 0), ([1], [1300], 8, 1, 64, 64, 200, 300)]
 

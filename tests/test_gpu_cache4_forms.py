@@ -1,12 +1,15 @@
-"""The four-bit cache on the GPU in the forms that small calls do not take: an append of thousands of tokens, bit for bit."""
+"""The four-bit cache on the GPU in the forms that small calls do not take: an append of thousands of tokens, bit for bit; attention in equal shares with windows and sinks, whose kernels
+test_more_operator_forms.py names."""
 import random
 
 import pytest
 import torch
 
+import cache4_forms as forms
 import four_bits as plain
 import operator_reference as ref
 from paper_2604_13847_amd import binding as sb
+from test_gpu_cache4 import Served4
 from test_gpu_operators import DEV, TYPE, nan, normal
 from test_gpu_rope_axes import positions, turned
 
@@ -83,3 +86,27 @@ def test_append_of_many_tokens(rot, layout, axes, dtype, Hq, Hkv, D, page, odd, 
         assert torch.equal(held[w][:rows][taken].double(), plain.value(code, step)[:rows][taken])
         assert torch.equal(codes[w][p, :, u], plain.pack(code[:rows][kept], w == 1)) and torch.equal(steps[w][p, :, u].double(), step[:rows][kept])
         assert bool((codes[w].transpose(1, 2)[~seen] == 255).all()) and bool(torch.isnan(steps[w].transpose(1, 2)[~seen]).all())
+
+
+# ---------------------------------------------------------------- attention in equal shares
+def same(a, b, x):
+    return torch.equal(a[0][: x.rows], b[0][: x.rows]) and torch.equal(a[1][:, : x.rows], b[1][:, : x.rows])
+
+
+@pytest.mark.parametrize("case", forms.SHARED_CHUNKS, ids=lambda c: "-".join(map(str, c)))
+def test_chunks_in_equal_shares(case):
+    have, new, Hq, Hkv, D, page, window, sinks = case
+    x = Served4(have, new, Hq, Hkv, D, page, spare_rows=2)
+    a = x.check(window, sinks)
+    for _ in range(3):
+        assert same(a, x.attend(window, sinks), x)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,case", forms.SHARED_ROWS, ids=lambda c: "-".join(map(str, c)) if isinstance(c, tuple) else str(c))
+def test_few_rows_in_equal_shares(rows, case, dtype):
+    have, new, Hq, Hkv, D, page, window, sinks = case
+    x = Served4(have, new, Hq, Hkv, D, page, dtype, spare_rows=2)
+    a = x.check(window, sinks)
+    for _ in range(3):
+        assert same(a, x.attend(window, sinks), x)

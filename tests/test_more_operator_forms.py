@@ -1,7 +1,67 @@
-"""Which launches the four-bit cache's calls make, so that a change of the rules does not leave forms without a test of their values."""
+"""Which kernels the calls of cache4_forms.py take, so that a change of the rules does not leave forms of the four-bit cache's attention without a test of their values."""
+import json
+import os
+import re
+import subprocess
+import sys
+
 import pytest
 
+import cache4_forms as forms
 from test_more_operator_kernels import launches  # noqa: F401 (a fixture)
+from test_operator_kernels import ROOT
+
+CALLS = """
+import ctypes as C, json, sys
+shim = C.CDLL(sys.argv[1], mode=C.RTLD_GLOBAL)
+shim.recorded_kernel.restype = C.c_char_p
+import numpy as np
+from paper_2604_13847_amd import binding as sb
+b, lib, at = C.c_void_p(4096), sb.lib(), 0
+for have, new, Hq, Hkv, D, page, window, sinks, dtype, extra in json.loads(sys.argv[2]):
+    need = [-(-(a + n) // page) for a, n in zip(have, new)]
+    c = sb.sb_cache4(sum(need) + 2, page, Hkv, D, dtype, max(need) + extra, *[4096] * 5)
+    n = sb.sb_chunk(len(have), Hq, sum(new), max(new), max(a + m for a, m in zip(have, new)), 0.0, 4096, 4096)
+    sb._check(lib.sb_cache4_attn(C.byref(c), C.byref(n), window, sinks, b, b, b, b, None))
+    count = shim.recorded_launches(np.zeros((256, 6), dtype=np.uint32).ctypes.data_as(C.c_void_p))
+    print("call", *[shim.recorded_kernel(i).decode() for i in range(at, count)])
+    at = count
+"""
+
+
+@pytest.fixture(scope="module")
+def taken(tmp_path_factory):
+    shim = str(tmp_path_factory.mktemp("launch") / "record_launches.so")
+    subprocess.run(["gcc", "-O1", "-shared", "-fPIC", "-o", shim, os.path.join(ROOT, "tests", "launch", "record_launches.c")], check=True)
+
+    def of(calls):
+        r = subprocess.run([sys.executable, "-c", CALLS, shim, json.dumps(calls)], cwd=ROOT, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        assert r.returncode == 0, r.stdout[-3000:]
+        # (name, template arguments)
+        names = lambda l: [(m[1], [a or b for a, b in re.findall(r"L[ij](\d+)E|(?<=I)(f|DF16b)(?=L)", k)]) for k in l.split()[1:] for m in [re.search(r"\d+((?:cache)\w+?_kernel)", k)]]
+        out = [names(l) for l in r.stdout.splitlines() if l.startswith("call")]
+        assert len(out) == len(calls)
+        return out
+
+    return of
+
+
+def test_chunks_in_equal_shares(taken):
+    calls = [(*c, 0, 0) for c in forms.SHARED_CHUNKS]
+    for call, got in zip(calls, taken(calls)):
+        D = str(call[4])
+        assert got[:2] == [("cache4_chunk_stream_kernel", [D]), ("cache4_join_kernel", ["DF16b", D, "256"])], (call, got)
+
+
+def test_few_rows_in_equal_shares(taken):
+    for dtype, name in ((0, "DF16b"), (1, "f")):
+        calls = [(*c, dtype, 0) for _, c in forms.SHARED_ROWS]
+        for (rows, call), got in zip(forms.SHARED_ROWS, taken(calls)):
+            rows = min(rows, 16) if dtype else rows
+            D, (split, join) = str(call[4]), got
+            parts, tiles = 16 // min(rows, 16), max(rows // 16, 1)
+            assert split == ("cache4_split_kernel", [name, D, str(parts), str(tiles), "3" if dtype else "1"]), (call, got)
+            assert join == ("cache4_join_kernel", [name, D, str(rows)]), (call, got)
 
 
 @pytest.mark.parametrize("dtype,total,workgroups", [(0, 2048, 512), (0, 4096, 1024), (0, 4097, 1025), (0, 6000, 1500), (0, 7680, 1920), (0, 8193, 2049), (0, 10000, 2500), (0, 16384, 4096),
