@@ -441,8 +441,10 @@ int sb_cache4_append(const sb_cache4 *c, const sb_chunk *n, const sb_rope *r, co
                      int64_t k_pitch, const void *v, int64_t v_pitch, void *q_out, void *k_held, void *v_held, void *stream);
 
 /* sb_cache_attn over such pages: the same rows, mask and outputs.  In SB_BF16 probabilities are rounded to bfloat16 once for the product with V; in SB_F32 queries and probabilities are taken as
- * three bfloat16 numbers that add up to them, so that products are exact but for 2^-24.  Keys that a row does not see reach it only where their steps are no numbers, and then
- * only from the same tile of 64 keys.  ws: dev, sb_cache4_attn_ws_bytes (host only). */
+ * three bfloat16 numbers that add up to them, so that products are exact but for 2^-24 (of values above 2^-100).  A step that is no number makes the rows that see it NaN: of a key their O and LSE, of
+ * a value (with a probability above 0) the 32 elements of O that share it.  What the mask hides from a row reaches it nowhere, whatever it holds, in SB_F32 and where min(max_new, total_new) * Hq/Hkv is at most
+ * 64; in longer chunks a value's step that is no number may reach O of rows that see any key of its tile of 64 keys (counted from the sequence's start), and of rows up to 31 tokens from such, in its KV
+ * head.  ws: dev, sb_cache4_attn_ws_bytes (host only). */
 int sb_cache4_attn_ws_bytes(const sb_cache4 *c, const sb_chunk *n, int32_t window, int32_t sinks, int64_t *bytes_out);
 int sb_cache4_attn(const sb_cache4 *c, const sb_chunk *n, int32_t window, int32_t sinks, const void *q, void *o, float *lse, void *ws, void *stream);
 

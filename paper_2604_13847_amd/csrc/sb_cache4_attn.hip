@@ -17,6 +17,9 @@
 #include "sb_cache4.h"
 #include "sb_window_fwd.h"
 
+// x y, and 0 where either is 0, whatever the other is (v_mul_legacy_f32: as fast as the other product, subnormal numbers alike)
+extern "C" __device__ float zero_product(float x, float y) __asm("llvm.amdgcn.fmul.legacy");
+
 namespace sb {
 
 struct CutItem {  // an item that a workgroup has the first part of
@@ -483,14 +486,6 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
               const int r = 16 * b + 4 * qd + v;
               if (!sees(pos[nt], u0 + r, P.window, P.sinks) || !(have >> r & 1)) sc[nt][b][v] = -__builtin_inff();
             }
-        // keys that do not exist have no steps either, whatever the page holds
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int v = 0; v < 4; ++v)
-#pragma unroll
-            for (int o = 0; o < OWN; ++o)
-              if (!(have >> (16 * b + 4 * qd + v) & 1)) v_step[b][v][o] = 0.f;
       }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -535,13 +530,14 @@ __global__ __launch_bounds__(64 * kWaves4) __attribute__((amdgpu_waves_per_eu(sp
         odd[j] = (a >> 4 & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u);
       }
       bf16x8 w[NT][PIECES];
-      auto weights = [&](auto oc) __attribute__((always_inline)) {  // probabilities times the steps of one of the lane's groups
+      // Probabilities times the steps of one of the lane's groups.  Where a key is hidden from a row, or does not exist, the probability is 0, and whatever step it has, a NaN too, reaches nothing.
+      auto weights = [&](auto oc) __attribute__((always_inline)) {
         constexpr int O = decltype(oc)::value;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float y[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) y[j] = sc[nt][j / 4][j % 4] * v_step[j / 4][j % 4][O];
+          for (int j = 0; j < 8; ++j) y[j] = zero_product(sc[nt][j / 4][j % 4], v_step[j / 4][j % 4][O]);
           pieces_of<PIECES>(y, w[nt]);
         }
       };

@@ -1,5 +1,5 @@
 """The four-bit cache on the GPU in the forms that small calls do not take: an append of thousands of tokens, bit for bit; attention in equal shares with windows and sinks, whose kernels
-test_more_operator_forms.py names."""
+test_more_operator_forms.py names; and how far steps that are no numbers reach."""
 import random
 
 import pytest
@@ -110,3 +110,78 @@ def test_few_rows_in_equal_shares(rows, case, dtype):
     a = x.check(window, sinks)
     for _ in range(3):
         assert same(a, x.attend(window, sinks), x)
+
+
+# ---------------------------------------------------------------- steps that are no numbers
+def spoil(x, s, u, g, c):
+    """Step of group c of the value of token u of sequence s, KV head g."""
+    x.steps[1][int(x.table[s, u // x.page]), g, u % x.page, c] = float("nan")
+
+
+def spoiled(x, s, u, g, c, window, sinks):
+    """[rows, Hq, D]: what has to become NaN by that."""
+    out = torch.zeros(x.rows, x.Hq, x.D, dtype=torch.bool, device=DEV)
+    t = torch.arange(x.have[s], x.have[s] + x.new[s], device=DEV)
+    sees = ref.visible(t, torch.tensor([u], device=DEV), window, sinks)[:, 0]
+    G = x.Hq // (x.codes[0].shape[1])
+    out[x.cu[s]: x.cu[s + 1], g * G: (g + 1) * G, 32 * c: 32 * c + 32] = sees[:, None, None]
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("have,new,Hq,Hkv,D,page,window,sinks", [
+    ([100, 333], [3, 1], 4, 2, 64, 16, forms.NONE, 0), ([100, 333], [4, 4], 2, 2, 128, 16, 40, 3), ([100, 70], [5, 2], 4, 4, 128, 32, 50, 0), ([100, 61], [6, 6], 10, 5, 64, 16, 33, 7),
+    ([500, 9], [16, 16], 4, 2, 64, 64, 90, 40), ([500, 9], [16, 16], 4, 2, 128, 16, 90, 40), ([500, 9], [30, 20], 4, 2, 128, 16, 64, 35), ([4000, 3000], [16, 16], 8, 2, 128, 64, 3000, 70)])
+def test_hidden_values_that_are_no_numbers_reach_no_row(have, new, Hq, Hkv, D, page, window, sinks, dtype):
+    """Of few rows (all in float32): a drafted token behind the row's own, the token that has just left its window and the one behind the sinks may be no numbers, in whatever strip they
+    lie; the rows that see them have NaN in the 32 elements that share the step, and nothing else."""
+    x = Served4(have, new, Hq, Hkv, D, page, dtype)
+    o, lse = x.attend(window, sinks)
+    assert not bool(torch.isnan(o).any() | torch.isnan(lse).any())
+    clean = [y.clone() for y in x.steps]
+    for s in range(len(have)):
+        first, last = have[s], have[s] + new[s] - 1
+        places = {first, last, (first + last) // 2, first - window, last - window, (first + last) // 2 - window, first - window + 1, sinks - 1, sinks, 0}
+        for n, u in enumerate(sorted(p for p in places if 0 <= p <= last)):
+            g, c = n % Hkv, n % (D // 32)
+            spoil(x, s, u, g, c)
+            got, got_lse = x.attend(window, sinks)
+            bad = spoiled(x, s, u, g, c, window, sinks)
+            assert bool(torch.isnan(got[bad]).all()), (s, u)
+            assert torch.equal(got[~bad], o[~bad]) and torch.equal(got_lse, lse), (s, u, torch.isnan(got).any(-1).any(-1).nonzero().flatten().tolist())
+            x.steps[1].copy_(clean[1])
+    # several at once, in all groups and heads, hidden from some rows and seen by others
+    bad = torch.zeros_like(o, dtype=torch.bool)
+    for s in range(len(have)):
+        for u in (have[s] + new[s] - 1, have[s] + new[s] // 2, max(have[s] - window, 0)):
+            for g in range(Hkv):
+                for c in range(D // 32):
+                    if (u + g + c) % 3:
+                        spoil(x, s, u, g, c)
+                        bad |= spoiled(x, s, u, g, c, window, sinks)
+    got, got_lse = x.attend(window, sinks)
+    assert bool(torch.isnan(got[bad]).all()) and torch.equal(got[~bad], o[~bad]) and torch.equal(got_lse, lse)
+
+
+@pytest.mark.parametrize("have,new,Hq,Hkv,D,window,sinks", [([130, 40], [300, 200], 4, 2, 64, forms.NONE, 0), ([130, 40], [300, 200], 8, 2, 128, 70, 3), ([3000, 2500, 3100], [300, 300, 299], 16, 8, 128, 2500, 70)])
+def test_values_of_chunks_that_are_no_numbers_stay_in_their_tile(have, new, Hq, Hkv, D, window, sinks):
+    """Of many rows: rows that see any key of the value's 64, and rows up to 31 tokens from such, may be NaN where the mask hides the value; no others, no other KV head and no other sequence."""
+    x = Served4(have, new, Hq, Hkv, D, 16)
+    o, lse = x.attend(window, sinks)
+    clean = x.steps[1].clone()
+    for s in range(2):
+        t = torch.arange(have[s], have[s] + new[s], device=DEV)
+        for n, u in enumerate((have[s] + new[s] - 1, have[s] + 64, have[s] + 100, max(have[s] - window, 1), 2)):
+            g, c = n % Hkv, n % (D // 32)
+            spoil(x, s, u, g, c)
+            got, got_lse = x.attend(window, sinks)
+            bad = spoiled(x, s, u, g, c, window, sinks)
+            assert bool(torch.isnan(got[bad]).all()), (s, u)
+            keys = torch.arange(u // 64 * 64, u // 64 * 64 + 64, device=DEV)
+            near = ref.visible(t, keys, window, sinks).any(-1)
+            near = ((t[:, None] - t).abs() <= 31)[:, near].any(-1)
+            may = torch.zeros_like(bad)
+            may[x.cu[s]: x.cu[s + 1], g * (Hq // Hkv): (g + 1) * (Hq // Hkv)] = near[:, None, None]
+            assert not bool((bad & ~may).any())
+            assert torch.equal(got[~may], o[~may]) and torch.equal(got_lse, lse), (s, u)
+            x.steps[1].copy_(clean)
