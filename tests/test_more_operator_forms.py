@@ -1,4 +1,5 @@
-"""Which kernels the calls of cache4_forms.py take, so that a change of the rules does not leave forms of the four-bit cache's attention without a test of their values."""
+"""Which kernels the calls of cache4_forms.py take, so that a change of the rules does not leave forms of the four-bit cache's attention without a test of their values; and what the
+compiler made of the loops over strips."""
 import json
 import os
 import re
@@ -8,7 +9,7 @@ import sys
 import pytest
 
 import cache4_forms as forms
-from test_more_operator_kernels import launches  # noqa: F401 (a fixture)
+from test_more_operator_kernels import functions, launches  # noqa: F401 (fixtures)
 from test_operator_kernels import ROOT
 
 CALLS = """
@@ -69,3 +70,67 @@ def test_few_rows_in_equal_shares(taken):
 def test_append_of_many_tokens_fills_the_chip(launches, dtype, total, workgroups):  # noqa: F811
     """A token more never makes much fewer wavefronts than the 4096 that fill the chip: four to a workgroup, a token each."""
     assert launches("append", 2, total, total, 9000, 32, 8, 128, dtype, 1) == [("cache4_append_kernel", workgroups, 1)]
+
+
+def loops(lines):
+    """Bodies of a function's natural loops, smallest first."""
+    code, labels = [], {}
+    for line in (l.split(";")[0].strip() for l in lines):
+        m = re.match(r"([\w.$]+):$", line)
+        if m:
+            labels[m[1]] = len(code)
+        elif line and line[0] != ".":
+            code.append(line)
+    after, before = [[] for _ in code], [[] for _ in code]
+    for i, x in enumerate(code):
+        words = x.split()
+        if words[0].startswith(("s_branch", "s_cbranch")):
+            after[i].append(labels[words[1]])
+        if words[0] not in ("s_branch", "s_endpgm") and i + 1 < len(code):
+            after[i].append(i + 1)
+    for i, targets in enumerate(after):
+        for j in targets:
+            before[j].append(i)
+
+    def reached(i, without):
+        """Whether the start leads to i on a way round `without`: a branch there is no loop then."""
+        seen, todo = {without}, [0]
+        while todo:
+            n = todo.pop()
+            if n not in seen:
+                seen.add(n)
+                todo += after[n]
+        return i in seen and i != without
+
+    found = []
+    for i, targets in enumerate(after):
+        for head in (j for j in targets if j <= i and not reached(i, j)):
+            body, todo = {head, i}, [i]
+            while todo:
+                n = todo.pop()
+                for j in before[n] if n != head else ():
+                    if j not in body:
+                        body.add(j)
+                        todo.append(j)
+            found.append([code[n] for n in sorted(body)])
+    return sorted(found, key=len)
+
+
+def test_loops():
+    """Of two loops, one in the other, where the inner one's body goes on behind the outer one's end."""
+    outer, inner = loops(["a:", "v_x", "b:", "v_y", "s_cbranch_scc1 c", "d:", "v_z", "s_cbranch_scc0 b", "s_cbranch_scc1 a", "s_endpgm", "c:", "v_w", "s_branch d"])[::-1]
+    assert [x.split()[0] for x in inner] == ["v_y", "s_cbranch_scc1", "v_z", "s_cbranch_scc0", "v_w", "s_branch"] and "v_x" in outer and len(outer) == 8
+
+
+def test_nothing_is_spilled_in_the_loop_over_strips(functions):  # noqa: F811
+    """From the loop's head, where the next strip's loads are issued, to its end: a spilled number there would be waited for together with the strips."""
+    seen = 0
+    for name, lines in functions.items():
+        if "split" not in name:
+            continue
+        body = next(b for b in loops(lines) if any(x.startswith("v_mfma") for x in b))
+        assert sum(x.startswith("global_load_lds") for x in body) == (6 if "Li128E" in name else 3), name
+        assert sum(x.startswith("v_mfma") for x in body) == sum(x.split()[0].startswith("v_mfma") for l in lines for x in [l.strip()] if x), name  # all products of a strip
+        assert not [x for x in body if x.startswith("scratch_")], name
+        seen += 1
+    assert seen == 12
