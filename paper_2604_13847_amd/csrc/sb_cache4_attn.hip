@@ -890,7 +890,8 @@ static Cache4Plan plan_cache4(const sb_cache4* c, const sb_chunk* n, int window,
     return (std::min(in_window, longest) + tile - 1) / tile;
   };
   // (32 rows a tile cost 1.55 to 1.9 times what 16 do: two tiles' worth where their number is even, three in two would not pay.  8 sequences of 20000, 32/8 heads, 64 rows: 144 us in tiles of 16, 113 of 32;
-  // 64 of 500 to 8000, 28/4 heads, 35 rows: 96 us in tiles of 16, 99 of 32.)
+  // 64 of 500 to 8000, 28/4 heads, 35 rows: 96 us in tiles of 16, 99 of 32.  Float32, where a row's numbers take three times the registers, in tiles of 16 and 32: 16 of 500 to 20000, 32/8 heads, 32 rows 74
+  // and 114, 64 rows 131 and 192;  16/4 heads of 64, 32 rows 32 and 40;  2000 behind 20000 2690 and 4340, a prompt of 2000 195 and 304.)
   auto unit_of = [&](int64_t items, int tile) {  // see Stream
     const int64_t strips = ((int64_t)c->max_pages * c->page_size + tile - 1) / tile + 2;  // of an item, at most
     int unit = 0;
@@ -907,8 +908,11 @@ static Cache4Plan plan_cache4(const sb_cache4* c, const sb_chunk* n, int window,
     // waited for.
     //   32/8 heads, equal shares and whole items, in us: one sequence of 400 14.9 and 10.8, of 1000 12.8 and 13.7, of 2000 14.9 and 21.1;  16 of 1000 19.3 and 14.0, of 2000 22.7 and 22.3;  64 of
     //   2000 39.8 and 30.9, of 100 to 2000 32.1 and 23.9, four of 2000 and 60 of 200 21.4 and 22.3;  64 of 4000 61.9 and 53.8, of 500 to 4000 39.2 and 41.0, one of 4000 and 63 of 100 16 and 37
+    //   float32 chunks, likewise (items in brackets): 300 behind 8000 193 and 222 (600), 512 307 and 294 (1024), 700 441 and 428 (1400), 1200 778 and 717 (2400);  2 x 600 behind 1000 to 8000, 14/2 heads of
+    //   64 183 and 196 (1052), 2 x 800 242 and 234 (1400);  2 x 800, 28/4 heads 838 and 745 (2800);  16 x 50, one of them behind 20000, the others 100 190 and 238 (1408), 8 x 100 288 and 239 (1408);
+    //   2000 behind 20000 3060 and 2690 (4000);  a prompt of 6001 2470 and 1285 (12008)
     const int64_t of_wave = (tiles(p.rows, 32) + kWaves4 - 1) / kWaves4, all = p.few * c->num_kv_heads;
-    if (!(of_wave <= 8 || (of_wave <= 16 && all >= 256) || (f32 && most > kFewRows4 && all >= 4096)))
+    if (!(of_wave <= 8 || (of_wave <= 16 && all >= 256) || (f32 && most > kFewRows4 && all >= 1280)))
       p.workgroups = (int)std::min<int64_t>(256 * split_waves(D, p.rows, f32 ? 3 : 1), all * of_wave);
     sums = (size_t)p.workgroups * 2 * p.rows;
     p.unit = unit_of(p.few * c->num_kv_heads, 32);

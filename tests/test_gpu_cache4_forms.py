@@ -102,6 +102,14 @@ def test_chunks_in_equal_shares(case):
         assert same(a, x.attend(window, sinks), x)
 
 
+@pytest.mark.parametrize("case", forms.WHOLE_FLOATS + forms.SHARED_FLOATS, ids=lambda c: "-".join(map(str, c)))
+def test_float32_chunks(case):
+    have, new, Hq, Hkv, D, page, window, sinks = case
+    x = Served4(have, new, Hq, Hkv, D, page, "f32", spare_rows=2)
+    a = x.check(window, sinks)
+    assert same(a, x.attend(window, sinks), x)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,case", forms.SHARED_ROWS, ids=lambda c: "-".join(map(str, c)) if isinstance(c, tuple) else str(c))
 def test_few_rows_in_equal_shares(rows, case, dtype):

@@ -65,6 +65,21 @@ def test_few_rows_in_equal_shares(taken):
             assert join == ("cache4_join_kernel", [name, D, str(rows)]), (call, got)
 
 
+def test_float32_chunks(taken):
+    for calls, join in ((forms.WHOLE_FLOATS, False), (forms.SHARED_FLOATS, True)):
+        calls = [(*c, 1, 0) for c in calls]
+        for call, got in zip(calls, taken(calls)):
+            D = str(call[4])
+            assert got == [("cache4_split_kernel", ["f", D, "1", "1", "3"]), ("cache4_join_kernel", ["f", D, "16"])][: 1 + join], (call, got)
+
+
+def test_whole_items_of_float32_chunks(launches):  # noqa: F811
+    """From 1280 items of 16 rows on, which is where they even out by themselves, both sides measured."""
+    assert launches("attn", 1, 700, 700, 8700, 32, 8, 128, 1, forms.NONE) == [("cache4_split_kernel", 8 * 175, 1)]
+    assert launches("attn", 1, 2000, 2000, 22000, 32, 8, 128, 1, forms.NONE) == [("cache4_split_kernel", 8 * 500, 1)]
+    assert launches("attn", 1, 300, 300, 8300, 32, 8, 128, 1, forms.NONE) == [("cache4_split_kernel", 512, 1), ("cache4_join_kernel", 512, 4)]
+
+
 @pytest.mark.parametrize("dtype,total,workgroups", [(0, 2048, 512), (0, 4096, 1024), (0, 4097, 1025), (0, 6000, 1500), (0, 7680, 1920), (0, 8193, 2049), (0, 10000, 2500), (0, 16384, 4096),
                                                     (0, 100000, 25000), (1, 4097, 1025), (1, 8192, 2048), (1, 8193, 2049)])
 def test_append_of_many_tokens_fills_the_chip(launches, dtype, total, workgroups):  # noqa: F811
