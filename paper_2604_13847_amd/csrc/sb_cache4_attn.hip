@@ -245,7 +245,7 @@ struct Stream {
       count = P.splits == 1 ? 1 : max((count + (1 << A.unit) - 1) >> A.unit, 1);  // (rows that see nothing have a result too)
     }
   }
-  // units of a workgroup.  With up to 64 sequences, these stay loaded.  (600 sequences of 100 to 500 tokens: 81 us with every 64 loaded when it was their turn, 66 so.)
+  // units of a workgroup.  With up to 64 sequences, these stay loaded.  (600 sequences of 100 to 500 tokens: 79 us with every 64 loaded when it was their turn, 64 so.)
   __device__ inline int share(const Cache4Params& A, int workgroups, int least, int lane) {
     Lengths next = fetch(A, 0, lane);
     if (A.w.splits == 1) {
@@ -255,7 +255,7 @@ struct Stream {
     int sum = 0;
     for (int base = 0; base < A.w.S; base += 64) {
       const Lengths x = next;
-      next = fetch(A, base + 64, lane);  // (on its way while these are worked on)
+      if (base + 64 < A.w.S) next = fetch(A, base + 64, lane);  // (on its way while these are worked on)
       take(A, x, base, lane);
       sum += size(A.w);
     }
