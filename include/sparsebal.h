@@ -424,7 +424,7 @@ int sb_cache_tables(const sb_page_pool *pool, const int32_t *cached, const int32
  * not depend on how the turn is computed.
  *
  * Per token and KV head D/2 bytes of codes (the lower half of a byte first) and D/32 steps (bfloat16).  Byte D/8 b + 4 c + e of a key holds elements 32 c + 8 b + 2 e and
- * the next (c < D/32, b < 4, e < 4); byte D/32 i + e of a value holds elements 32 e + i and 32 e + 16 + i (i < 16).  80 bytes at head_dim 128 where bfloat16 takes 256. */
+ * the next (c < D/32, b < 4, e < 4); byte D/32 i + e of a value holds elements 32 e + i and 32 e + 16 + i (i < 16).  72 bytes at head_dim 128 where bfloat16 takes 256. */
 typedef struct sb_cache4 {
   int32_t num_pages, page_size;          /* as in sb_cache */
   int32_t num_kv_heads, head_dim, dtype; /* dtype: of the new tokens, the queries and the output (SB_BF16 | SB_F32); the pages are the same */

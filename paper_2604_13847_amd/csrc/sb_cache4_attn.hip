@@ -4,11 +4,12 @@
 //
 // n and m, the levels of keys and values, are exact as operands of matrix instructions; steps are applied in float32, to the scores of a group's product and to the probabilities.
 //
-// Few new tokens (cache4_split_kernel): bound by the cache's bytes, 80 a token and KV head each for K and V at head_dim 128.  64 sequences of 500 to 32768 tokens, 32/8 heads: 130 us with
-// the join, 4.3 TB/s (such bytes at the rate of a copy: 113); head_dim 64: 78 (57), where the arithmetic of a strip is not all hidden.  One of 4097: 13.9 us, two launches' latency.  In float32
+// Few new tokens (cache4_split_kernel): bound by the cache's bytes, 72 a token and KV head each for K and V at head_dim 128.  64 sequences of 500 to 32768 tokens, 32/8 heads: 130 us with
+// the join, 4.4 TB/s (such bytes at the rate of a copy: 113); head_dim 64: 76 (57), where the arithmetic of a strip is not all hidden.  More rows are bound by it: 8 sequences of 20000, 16 rows a KV head 55 us, 32 73, 64
+// 111 (37; vector instructions 67 % of the cycles at 64).  One of 4097: 14.1 us, 9.8 and 3.5 of its two launches, each a chain of dependent loads.  In float32
 // each product is three of bfloat16.
-// Many (cache4_chunk_kernel, cache4_chunk_stream_kernel): bound by the matrix and vector instructions of a tile.  2 x 2000 tokens behind 20000 and 30001, window 8192, 28/4 heads: 489 us,
-// 903 TFLOP/s; a prompt of 6001, 32/8 heads: 331 to 337 us, 0.88 PFLOP/s.
+// Many (cache4_chunk_kernel, cache4_chunk_stream_kernel): bound by the matrix and vector instructions of a tile.  2 x 2000 tokens behind 20000 and 30001, window 8192, 28/4 heads: 483 us,
+// 914 TFLOP/s; a prompt of 6001, 32/8 heads: 334 us, 0.88 PFLOP/s.
 #include <math.h>
 
 #include <algorithm>

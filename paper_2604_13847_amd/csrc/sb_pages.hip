@@ -6,8 +6,8 @@
 // Nothing here is large: a step moves a few pages, and what it takes is a chain of dependent loads.  So one workgroup does all the tables (a thread a sequence, sums over the
 // workgroup, then a thread a moved page, found in the sums by bisection in LDS, four at a time), and writes slots and positions too where tokens are few; many tokens are a
 // second launch over the chip, which finds each token's sequence in cu_new.  Of few sequences the workgroup is small: its barriers are cheaper.
-// 64 sequences with a token each: 3.8 us on the GPU (host and launch 9).  1000 with 8 prompts of up to 4096 tokens: 10 us and 4.6 for the tokens; by scans through LDS and one entry a thread
-// at a time it was 17.
+// 64 sequences with four tokens each, one in 16 finished: 3.8 us on the GPU (host and launch 9).  1000 with 8 prompts of 12288 to 16384 tokens, pages of 16: 10 us and 4.6 for the tokens' slots; by scans through
+// LDS and one entry a thread at a time it was 17.
 #include <algorithm>
 #include <type_traits>
 
