@@ -325,8 +325,8 @@ extern "C" int sb_cache4_append(const sb_cache4* c, const sb_chunk* n, const sb_
   // Four wavefronts to a token where tokens are few; where they fill the chip, one, which looks up and computes what a token has once.
   // (32/8 heads, one and four, in us: 512 tokens 15.0 and 13.7, 1536 17.9 and 14.9, 2048 18.2 both, 4096 24.4 and 29.0, 8192 42.0 and 47.2)
   P.waves = P.T < 2048 ? 4 : 1;
-  // A token each: 4096 wavefronts fill the chip, and those behind them start as others end.  Two, where all are there at once and take 15/16 of that or more: then nobody starts twice.  (In float32, of
-  // which fewer fit, never.)  32/8 heads, one and two each, in us: 4600 tokens 33.3 and 39.4, 6500 42.6 and 44.7, 7500 46.1 both, 8000 47.1 and 46.6, 8192 47.6 and 46.8, 8300 54.2 and 63.5, 10000 62.0
+  // A token each: 4096 wavefronts fill the chip, and those behind them start as others end.  Two, where all are there at once and take 15/16 of that or more: then nobody starts twice.  (In float32,
+  // where a token is twice the bytes, never.)  32/8 heads, one and two each, in us: 4600 tokens 33.3 and 39.4, 6500 42.6 and 44.7, 7500 46.1 both, 8000 47.1 and 46.6, 8192 47.6 and 46.8, 8300 54.2 and 63.5, 10000 62.0
   // and 71.2, 16384 95.5 and 99.7;  8 heads of 128 8192 28.1 and 26.9, 8300 30.4 and 34.6;  14/2 of 64 19.8 and 19.0, 21.7 and 23.9;  float32 8192 87.1 and 95.4.  Four: 8192 66.5, 32768 186 (one 183)
   P.run = esize == 2 && P.T <= 8192 && P.T > 8192 / 16 * 15 ? 2 : 1;
   if (P.T >> 25 > P.run) P.run = P.T >> 25;  // (a launch has fewer than 2^32 threads)
