@@ -112,16 +112,16 @@ __global__ __launch_bounds__(THREADS) void page_tables_kernel(PoolParams P) {
   __shared__ int firsts[THREADS];    // the first of them
   __shared__ int32_t cu[THREADS], have[THREADS];
   const int tid = threadIdx.x;
-  struct Row { int want, held, added, cached; };
+  struct Row { int want, held, said, added, cached; };  // said: held as it stands in memory
   auto row = [&](int s) {
     Row r{};
     if (s >= P.S) return r;
     r.added = P.added[s];
     r.cached = max(P.cached[s], 0);
-    const int held = P.held[s];
+    r.said = P.held[s];
     const int64_t length = r.added < 0 ? 0 : (int64_t)r.cached + r.added;
     r.want = (int)min((length + (1 << P.page_shift) - 1) >> P.page_shift, (int64_t)P.max_pages);
-    r.held = min(max(held, 0), P.max_pages);
+    r.held = min(max(r.said, 0), P.max_pages);
     return r;
   };
   auto sums_of = [&](const Row& r) { return Three{{(unsigned)max(r.held - r.want, 0), (unsigned)max(r.want - r.held, 0), (unsigned)max(r.added, 0)}}; };  // given back, lacking, new tokens
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(THREADS) void page_tables_kernel(PoolParams P) {
     const int32_t end = (int32_t)min(tokens + c.x[2], (int64_t)0x7fffffff);
     if (s < P.S) {
       const int64_t got = min(max(now - lacked - ((int64_t)c.x[1] - lack), (int64_t)0), lack);
-      if (r.want != r.held) P.held[s] = lack > 0 ? r.held + (int)got : r.want;
+      if (r.want != r.said) P.held[s] = lack > 0 ? r.held + (int)got : r.want;
       P.cu[s + 1] = end;
     }
     if (one) {

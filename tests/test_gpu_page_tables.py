@@ -90,6 +90,16 @@ def test_lengths_that_the_table_cannot_hold_and_counts_that_cannot_be():
     assert pool.held.tolist()[0] == 1 and int(pool.free_count[0]) == 9 and int(pool.page_table[0, 0]) == 9
 
 
+def test_counts_that_cannot_be_are_put_right():
+    """Also where a row neither gives back nor lacks a page."""
+    pool = sb.PagePool.empty(4, 4, 30, 16)
+    sb.sb_cache_tables(pool, ints([0] * 4), ints([64, 64, 64, 0]), 192)
+    table = pool.page_table.clone()
+    pool.held.copy_(ints([99, 4, 2 ** 31 - 1, -2 ** 31]))
+    missing = sb.sb_cache_tables(pool, ints([64, 64, 50, 0]), ints([0, 5000, 0, 0]), 0)[3]
+    assert pool.held.tolist() == [4, 4, 4, 0] and torch.equal(pool.page_table, table) and int(pool.free_count[0]) == 18 and int(missing[0]) == 0
+
+
 def test_sums_of_tokens_stop_at_31_bits():
     pool = sb.PagePool.empty(3, 2, 10, 16)
     cu = sb.sb_cache_tables(pool, ints([0] * 3), ints([2 ** 31 - 1] * 3), 5)[0]
