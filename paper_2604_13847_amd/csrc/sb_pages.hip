@@ -249,7 +249,7 @@ using namespace sb;
 extern "C" int sb_cache_tables(const sb_page_pool* pool, const int32_t* cached, const int32_t* added, int32_t total_new, int32_t* cu_new, int32_t* positions, int64_t* slots,
                                int32_t* missing, void* stream) {
   if (!pool) { set_error("null pool"); return SB_ERR_INVALID_ARG; }
-  if (pool->num_seqs < 0 || pool->max_pages < 0 || pool->num_pages < 0 || total_new < 0) { set_error("negative size"); return SB_ERR_INVALID_ARG; }
+  if (pool->num_seqs < 0 || pool->max_pages < 0 || pool->num_pages < 0 || ((positions || slots) && total_new < 0)) { set_error("negative size"); return SB_ERR_INVALID_ARG; }
   if (pool->page_size < 16 || pool->page_size > 1024 || (pool->page_size & (pool->page_size - 1)) != 0) {
     set_error("page_size %d unsupported (a power of two, 16 .. 1024)", pool->page_size);
     return SB_ERR_UNSUPPORTED;

@@ -101,6 +101,12 @@ def test_page_table_refusals():
         refused(tables(**{missing: None}), -1, "null argument")
 
 
+def test_page_tables_without_arrays_of_tokens_do_not_read_their_size():
+    for positions, slots in ((BUF, BUF), (BUF, None), (None, BUF)):
+        refused(tables(total=-1, positions=positions, slots=slots), -1, "negative")
+    refused(tables(pool=dict(page_size=48), total=-1, positions=None, slots=None), -2, "page_size")  # (the next refusal, so that nothing is launched)
+
+
 def test_plain_tables_undo():
     """(the lists that the GPU's tables are held to)"""
     x = plain.Pool(3, 10, 20, 16, [7, 3, 9, 1] + list(range(10, 26)))
